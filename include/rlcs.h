@@ -407,6 +407,97 @@ int rlcs_episodic_prefix_sum_bf16(const uint16_t* x, const uint8_t* dones, uint1
                                   int starts_at, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * ROLLOUT AND POLICY OPERATORS: what stands before and after the scans when actions come from logits over a discrete
+ * set, a handful of actions or a token vocabulary.  Plain names take fp32 logits, *_bf16 names bfloat16 ones
+ * (uint16_t storage); all arithmetic is fp32 or wider.  The conventions on pointers, execution and determinism above
+ * hold; layout, sizes and the treatment of infinities and NaN are said with each.
+ */
+
+/*
+ * Actions from logits [R, A], row r at logits + r*ld (ld >= A elements, any alignment of a row), A <= 2^22.
+ * Per row: temperature, top_k, top_p, min_p, each read from its [R] array, or the *_all value where that is NULL.
+ *   d_j = (l_j - max l) * (1/temperature)   (0 where l_j = max l),   e_j = exp(d_j),   w_j = floor(2^31 e_j + 1/2)
+ *   candidates, ordered by (logit descending, index ascending): the first top_k of them with e_j >= min_p; of those
+ *   the shortest leading part that holds top_p of their weight (one stays while the weight before it < top_p * W1)
+ *   action = the first index, in index order, whose kept weights sum to more than floor(uniform * W2), W2 = kept weight
+ *   log_probs[r] = d_a - log(sum_j w_j / 2^31),   kept_log_probs[r] = d_a - log(W2 / 2^31)
+ * The most likely candidate always stays.  temperature <= 0 (or NaN): that candidate is taken, log_probs at
+ * temperature 1, kept_log_probs 0.  top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN: no such limit.  uniforms [R]
+ * in [0, 1).  A logit of -inf or NaN is never drawn; a row with no other gets action -1 and log-probs -inf.  Weights
+ * are whole numbers, so their sums, and with them the actions, do not depend on how a row is split over threads; an
+ * action less likely than 2^-32 of the most likely one has weight 0.
+ */
+int rlcs_sample_actions(const float* logits, int64_t ld, const float* uniforms, const float* temperature, const int32_t* top_k,
+                        const float* top_p, const float* min_p, float temperature_all, int32_t top_k_all, float top_p_all,
+                        float min_p_all, int32_t* actions, float* log_probs, float* kept_log_probs, int64_t R, int64_t A,
+                        void* cuda_stream);
+int rlcs_sample_actions_bf16(const uint16_t* logits, int64_t ld, const float* uniforms, const float* temperature,
+                             const int32_t* top_k, const float* top_p, const float* min_p, float temperature_all, int32_t top_k_all,
+                             float top_p_all, float min_p_all, int32_t* actions, float* log_probs, float* kept_log_probs, int64_t R,
+                             int64_t A, void* cuda_stream);
+
+/*
+ * Log-probability, entropy and policy loss of given actions, and the loss's gradient, from logits [R, A] (row r at
+ * logits + r*ld) in one launch.  x = logits / temperature, lp = log softmax(x), a = actions[r]:
+ *   log_probs[r] = lp_a;   entropy[r] = H = -sum_j p_j lp_j;   loss[r] = -scale * (gain + entropy_coef * H)
+ *   gain = advantages[r] * lp_a                        where old_log_probs is NULL (policy gradient; V-trace's
+ *                                                      pg_advantages, GAE's advantages)
+ *        = min(rho adv, clip(rho, 1-clip, 1+clip) adv) otherwise, rho = exp(lp_a - old_log_probs[r])
+ *   dlogits[r,j] = d loss[r] / d logits[r,j]           (row r at dlogits + r*ldd; rounded once to the logits' type)
+ * A row whose mask is 0 (mask may be NULL: all rows live), whose action lies outside [0, A) or whose logits are all -inf is
+ * left out: its logits may hold anything, its outputs and gradient are 0.  In other rows logits of -inf have probability 0
+ * and gradient 0 (an action of probability 0: log_prob -inf); a NaN makes the row's outputs NaN.
+ * loss and dlogits may be NULL; with both NULL, advantages and old_log_probs may be too (scoring only).  dlogits may be
+ * the logits themselves (same pointer, ldd = ld).  temperature > 0, clip >= 0.
+ */
+int rlcs_policy_grad(const float* logits, int64_t ld, const int32_t* actions, const uint8_t* mask, const float* advantages,
+                     const float* old_log_probs, float* loss, float* log_probs, float* entropy, float* dlogits, int64_t ldd,
+                     int64_t R, int64_t A, float temperature, float clip, float entropy_coef, float scale, void* cuda_stream);
+int rlcs_policy_grad_bf16(const uint16_t* logits, int64_t ld, const int32_t* actions, const uint8_t* mask, const float* advantages,
+                          const float* old_log_probs, float* loss, float* log_probs, float* entropy, uint16_t* dlogits, int64_t ldd,
+                          int64_t R, int64_t A, float temperature, float clip, float entropy_coef, float scale, void* cuda_stream);
+
+/*
+ * Attention of one query a trajectory over a paged cache whose trajectories share their group's prompt.
+ * q [B, H, d], row b at q + b*q_stride (heads contiguous); out [B, H, d] contiguous; lse [B, H] or NULL.  Key and value of
+ * the token at place i of page p for key head h lie at cache + p*page_stride + i*token_stride + h*head_stride
+ * (d contiguous; both [pages, page, Hk, d] and [pages, Hk, page, d] layouts).  H a multiple of Hk: head h reads key
+ * head h / (H/Hk).  d a multiple of 8, 8 to 128; page_size 1 to 32768; pointers of bfloat16 tensors and all strides are
+ * multiples of 16 bytes.
+ *   rows group_offsets[g] to group_offsets[g+1]-1 (ascending, within [0, B]) form group g; a row outside all of them has no
+ *   prefix (groups = 0: none has).  Keys of a row: the first prefix_lens[g] tokens of the pages prefix_table[g, :]
+ *   ([groups, prefix_width]), then the first lens[b] tokens of the pages block_table[b, :] ([B, own_width]).
+ *   out = sum_j exp(scale q.k_j - lse) v_j,   lse = log sum_j exp(scale q.k_j);   a row without keys: out 0, lse -inf.
+ * Lengths are cut to max_prefix_len and max_len, the host's upper bounds from which the launch is sized.  A page number
+ * outside [0, pages) and a place beyond the table's width hold no keys.  Memory beyond a length is never used.  Products are
+ * summed in fp32; the softmax weights enter the second product as two bfloat16 parts (16 bits of mantissa).
+ * scale > 0.  workspace: at least rlcs_prefix_attention_workspace_bytes(...) bytes, 16-byte aligned, no initialisation.
+ */
+size_t rlcs_prefix_attention_workspace_bytes(int64_t B, int64_t H, int64_t Hk, int64_t d, int64_t page_size, int64_t groups,
+                                             int64_t max_prefix_len, int64_t max_len);
+int rlcs_prefix_attention_bf16(const uint16_t* q, int64_t q_stride, const uint16_t* k_cache, const uint16_t* v_cache, int64_t pages,
+                               int64_t page_stride, int64_t token_stride, int64_t head_stride, const int32_t* prefix_table,
+                               int64_t prefix_width, const int32_t* prefix_lens, const int32_t* group_offsets, const int32_t* block_table,
+                               int64_t own_width, const int32_t* lens, uint16_t* out, float* lse, int64_t B, int64_t H, int64_t Hk,
+                               int64_t d, int64_t page_size, int64_t groups, int64_t max_prefix_len, int64_t max_len, float scale,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Page tables, slot maps and positions of one step of a paged cache, from lengths on the GPU.  Row b holds cached[b] tokens
+ * and gets added[b] more (negative counts as 0; each row's and the step's total below 2^31).
+ *   have = ceil(cached / page_size), need = ceil((cached + added) / page_size), both at most `width`
+ *   block_table[b, j] ([B, width], in place): unchanged for j < have, for have <= j < need the next number of free_pages
+ *   [free_count] in row order, -1 from need on; -1 as well where the list has run out
+ *   tokens of the step, row after row: slots[t] = page number * page_size + place, -1 without a page; positions[t] = place in
+ *   its trajectory; both -1 from the step's total to num_slots (tokens beyond num_slots are left out)
+ *   offsets[b], page_offsets[b] ([B + 1] each) = tokens / new pages of the rows before b; the last entries are the totals
+ * The caller sees that the list ran out by page_offsets[B] > free_count.
+ */
+int rlcs_block_tables(const int32_t* cached, const int32_t* added, const int32_t* free_pages, int32_t* block_table,
+                      int64_t* slots, int32_t* positions, int32_t* offsets, int32_t* page_offsets, int64_t B,
+                      int64_t width, int64_t free_count, int64_t num_slots, int64_t page_size, void* cuda_stream);
+
+/*
  * Test hook: the bare scan of Eq. 1 / Eq. 2 on caller-supplied coefficients, every row with
  * boundary carry 0 (the paper's generic kernel of Section 4.1).
  *   forward == 0:  out_t = alpha_t + (t < T-1 ? beta_t * out_{t+1} : 0)

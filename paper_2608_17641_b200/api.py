@@ -181,3 +181,96 @@ def compute_episodic_prefix_sum(x, dones, *, boundary="ends_at", time_major=Fals
     fn = {"f32": _B.rlcs_episodic_prefix_sum, "bf16": _B.rlcs_episodic_prefix_sum_bf16,
           "tm": _B.rlcs_episodic_prefix_sum_time_major}[kind]
     return fn(x, _mask(dones), starts_at=(boundary == "starts_at"), workspace=_ws_for(kind, x, N, T, workspace, stream), stream=stream)
+
+
+# ------------------------------------------------------------------ rollout and policy operators
+_scratch: dict = {}
+
+
+def _scratch_of(like, nbytes: int, stream):
+    """Uninitialised workspace of at least nbytes, one per (device, stream); replaced by a larger one when a call needs it."""
+    torch = _torch()
+    s = torch.cuda.current_stream(like.device) if stream is None else stream
+    key = (like.device, int(s.cuda_stream))
+    buf = _scratch.get(key)
+    if buf is None or buf.numel() < nbytes:
+        buf = _B._alloc((max(nbytes, 1 << 20),), torch.uint8, like.device)
+        if stream is not None:
+            buf.record_stream(stream)
+        _scratch[key] = buf
+    return buf
+
+
+def _flat_rows(logits):
+    """[..., A] logits as [rows, A] (a view) and the leading shape."""
+    if logits.dim() == 2:
+        return logits, None
+    return logits.reshape(-1, logits.shape[-1]) if logits.is_contiguous() else logits.view(-1, logits.shape[-1]), logits.shape[:-1]
+
+
+def _by_dtype(logits, f32, bf16):
+    return {"f32": f32, "bf16": bf16}[_kind(logits, False)]
+
+
+def sample_actions(logits, uniforms, *, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """Actions drawn from logits [..., A] (float32 or bfloat16) with one given uniform in [0, 1) a row, and their log-probabilities:
+    (actions int32, log_probs, kept_log_probs).  log_probs is under the whole softmax at that temperature (the behaviour policy of
+    V-trace, Retrace and clipped losses), kept_log_probs under what top_k, min_p and top_p leave.  Parameters are numbers or
+    tensors of one value a row; temperature 0 takes the most likely action; a row that allows none (all -inf) gets action -1."""
+    rows, lead = _flat_rows(logits)
+    flat = lambda v: v.reshape(-1) if lead is not None and hasattr(v, "reshape") else v
+    fn = _by_dtype(logits, _B.rlcs_sample_actions, _B.rlcs_sample_actions_bf16)
+    got = fn(rows, flat(uniforms), temperature=flat(temperature), top_k=flat(top_k), top_p=flat(top_p), min_p=flat(min_p), stream=stream)
+    return got if lead is None else tuple(v.view(lead) for v in got)
+
+
+def compute_policy_gradient(logits, actions, advantages, *, old_log_probs=None, mask=None, temperature=1.0, clip=0.2,
+                            entropy_coef=0.0, scale=1.0, in_place=False, stream=None):
+    """Policy loss of the given actions and its gradient in the logits [..., A]: (loss, log_probs, entropy, dlogits).  Without
+    old_log_probs the policy-gradient loss -scale (adv lp + entropy_coef H), with them the clipped-ratio one.  loss is per row:
+    its sum is what dlogits differentiates, so scale = 1 / rows gives the mean.  Rows with mask 0 or an action outside [0, A)
+    count as absent.  in_place=True overwrites the logits with the gradient."""
+    rows, lead = _flat_rows(logits)
+    flat = lambda v: v.reshape(-1) if lead is not None and v is not None else v
+    fn = _by_dtype(logits, _B.rlcs_policy_grad, _B.rlcs_policy_grad_bf16)
+    loss, lp, ent, grad = fn(rows, flat(actions), flat(advantages), old_log_probs=flat(old_log_probs), mask=flat(_mask(mask)),
+                             temperature=temperature, clip=clip, entropy_coef=entropy_coef, scale=scale,
+                             dlogits=rows if in_place else None, stream=stream)
+    if lead is None:
+        return loss, lp, ent, grad
+    return loss.view(lead), lp.view(lead), ent.view(lead), grad.view(logits.shape)
+
+
+def compute_log_probs(logits, actions, *, mask=None, temperature=1.0, stream=None):
+    """Log-probability of the given actions and entropy of each row of logits [..., A]: (log_probs, entropy)."""
+    rows, lead = _flat_rows(logits)
+    flat = lambda v: v.reshape(-1) if lead is not None and v is not None else v
+    fn = _by_dtype(logits, _B.rlcs_policy_grad, _B.rlcs_policy_grad_bf16)
+    got = fn(rows, flat(actions), mask=flat(_mask(mask)), temperature=temperature, stream=stream)
+    return got if lead is None else tuple(v.view(lead) for v in got)
+
+
+def shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, block_table, lens, *, scale=None,
+                            max_prefix_len=None, max_len=None, workspace=None, stream=None):
+    """Attention of one query a trajectory, q [B, H, d] bfloat16, over the paged prompt that its group shares and its own pages:
+    (out [B, H, d], lse [B, H]).  Caches [pages, page, Hk, d]; group g holds rows group_offsets[g] to group_offsets[g+1]-1.
+    scale defaults to d ** -0.5; max_prefix_len and max_len bound the lengths (by default what the tables can hold): closer
+    bounds give better launches."""
+    scale = q.shape[-1] ** -0.5 if scale is None else scale
+    if workspace is None:
+        page, groups = k_cache.shape[1], 0 if prefix_table is None else prefix_table.shape[0]
+        room = 0 if prefix_table is None else prefix_table.shape[1] * page, block_table.shape[1] * page
+        most = [r if m is None else min(int(m), r) for r, m in zip(room, (max_prefix_len, max_len))]
+        need = int(_B.lib().rlcs_prefix_attention_workspace_bytes(q.shape[0], q.shape[1], k_cache.shape[2], q.shape[2], page, groups, *most))
+        workspace = _scratch_of(q, need, stream)
+    return _B.rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, block_table, lens, scale=scale,
+                                         max_prefix_len=max_prefix_len, max_len=max_len, workspace=workspace, stream=stream)
+
+
+def build_block_tables(cached, added, free_pages, block_table, *, page_size, num_slots, stream=None):
+    """Page table, slot map and positions of one step of a paged cache, from lengths on the GPU: (slots, positions, offsets,
+    pages_used); block_table is extended in place with pages taken from free_pages in row order.  pages_used (one element) above
+    free_pages.numel() says that the list ran out: the rows without a page have -1 in the table and in slots."""
+    slots, positions, offsets, page_offsets = _B.rlcs_block_tables(cached, added, free_pages, block_table, page_size=page_size,
+                                                                   num_slots=num_slots, stream=stream)
+    return slots, positions, offsets, page_offsets[-1:]

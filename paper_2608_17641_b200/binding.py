@@ -18,6 +18,7 @@ RLCS_ERR_NULL, RLCS_ERR_SIZE, RLCS_ERR_ARG, RLCS_ERR_ALIGN = 1, 2, 3, 4
 RLCS_ERR_WORKSPACE, RLCS_ERR_CUDA, RLCS_ERR_TIMEOUT, RLCS_ERR_LIMIT, RLCS_ERR_CAPTURE = 5, 6, 7, 8, 9
 
 _vp, _i64, _f, _sz, _int = ctypes.c_void_p, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t, ctypes.c_int
+_i32 = ctypes.c_int32
 _TAIL = [_vp, _sz, _vp]          # workspace, workspace_bytes, cuda_stream
 
 # name -> argtypes, exactly the declarations of include/rlcs.h
@@ -60,6 +61,14 @@ SIGNATURES = {
     "rlcs_discounted_return_bf16": ([_vp] * 6 + [_i64, _i64, _f] + _TAIL, _int),
     "rlcs_elig_trace_bf16": ([_vp] * 3 + [_i64, _i64, _f, _f] + _TAIL, _int),
     "rlcs_episodic_prefix_sum_bf16": ([_vp] * 3 + [_i64, _i64, _int] + _TAIL, _int),
+    "rlcs_sample_actions": ([_vp, _i64] + [_vp] * 5 + [_f, _i32, _f, _f] + [_vp] * 3 + [_i64, _i64, _vp], _int),
+    "rlcs_sample_actions_bf16": ([_vp, _i64] + [_vp] * 5 + [_f, _i32, _f, _f] + [_vp] * 3 + [_i64, _i64, _vp], _int),
+    "rlcs_policy_grad": ([_vp, _i64] + [_vp] * 8 + [_i64] * 3 + [_f] * 4 + [_vp], _int),
+    "rlcs_policy_grad_bf16": ([_vp, _i64] + [_vp] * 8 + [_i64] * 3 + [_f] * 4 + [_vp], _int),
+    "rlcs_prefix_attention_workspace_bytes": ([_i64] * 8, _sz),
+    "rlcs_prefix_attention_bf16": ([_vp, _i64, _vp, _vp] + [_i64] * 4 + [_vp, _i64, _vp, _vp, _vp, _i64] + [_vp] * 3 + [_i64] * 8
+                                   + [_f] + _TAIL, _int),
+    "rlcs_block_tables": ([_vp] * 8 + [_i64] * 5 + [_vp], _int),
     "rlcs_affine_scan": ([_vp] * 3 + [_i64, _i64, _int] + _TAIL, _int),
     "rlcs_debug_set_tile_variant": ([_int], _int),
     "rlcs_debug_tile_elems": ([_int], _int),
@@ -723,3 +732,194 @@ def rlcs_episodic_prefix_sum_time_major(x, dones, *, starts_at=False, sums=None,
     _check(lib().rlcs_episodic_prefix_sum_time_major(_ptr(x, "f32"), _ptr(dones, "u8", (T, N)), _ptr(out, "f32", (T, N)),
                                                      N, T, int(bool(starts_at)), wp, wb, _stream(stream)))
     return out
+
+
+# ------------------------------------------------------------------ rollout and policy operators
+_KINDS = {"f32": "float32", "bf16": "bfloat16", "i32": "int32", "i64": "int64"}
+
+
+def _typed(t, kind: str, shape=None, what="tensor"):
+    """Pointer of a contiguous tensor of one of _KINDS (None -> NULL)."""
+    if t is None:
+        return None
+    torch = _torch()
+    if not t.is_cuda:
+        raise TypeError("rlcs takes CUDA tensors (device pointers); there is no CPU path")
+    _require_current_device(t, what)
+    if t.dtype != getattr(torch, _KINDS[kind]):
+        raise TypeError(f"expected {_KINDS[kind]} for {what}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected shape {tuple(shape)} for {what}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _rows(t, kind: str, what: str, shape=None):
+    """(pointer, row stride) of a 2-D tensor whose rows are contiguous and do not overlap."""
+    torch = _torch()
+    if not t.is_cuda:
+        raise TypeError("rlcs takes CUDA tensors (device pointers); there is no CPU path")
+    _require_current_device(t, what)
+    if t.dtype != getattr(torch, _KINDS[kind]):
+        raise TypeError(f"expected {_KINDS[kind]} for {what}, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{what} must be 2-D [rows, actions]")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected shape {tuple(shape)} for {what}, got {tuple(t.shape)}")
+    R, A = t.shape
+    ld = t.stride(0) if R > 1 else max(A, 1)
+    if (A > 1 and t.stride(1) != 1) or ld < A:
+        raise ValueError(f"rows of {what} must be contiguous and must not overlap")
+    return t.data_ptr(), ld
+
+
+def _per_row(value, kind: str, R: int, default, what: str):
+    """A per-row parameter: (pointer, unused) for an [R] tensor, (NULL, value) for a number or None."""
+    if value is None:
+        return None, default
+    if isinstance(value, (int, float)):
+        return None, value
+    return _typed(value, kind, (R,), what), default
+
+
+def _sample_actions(name, kind, logits, uniforms, temperature, top_k, top_p, min_p, actions, log_probs, kept_log_probs, stream):
+    torch = _torch()
+    ptr, ld = _rows(logits, kind, "logits")
+    R, A = logits.shape
+    t, t_all = _per_row(temperature, "f32", R, 1.0, "temperature")
+    k, k_all = _per_row(top_k, "i32", R, 0, "top_k")
+    p, p_all = _per_row(top_p, "f32", R, 1.0, "top_p")
+    m, m_all = _per_row(min_p, "f32", R, 0.0, "min_p")
+    a = _alloc((R,), torch.int32, logits.device) if actions is None else actions
+    lp = _alloc((R,), torch.float32, logits.device) if log_probs is None else log_probs
+    kp = _alloc((R,), torch.float32, logits.device) if kept_log_probs is None else kept_log_probs
+    _check(getattr(lib(), name)(ptr, ld, _typed(uniforms, "f32", (R,), "uniforms"), t, k, p, m, t_all, min(int(k_all), 2 ** 31 - 1),
+                                p_all, m_all, _typed(a, "i32", (R,), "actions"), _typed(lp, "f32", (R,), "log_probs"),
+                                _typed(kp, "f32", (R,), "kept_log_probs"), R, A, _stream(stream)))
+    return a, lp, kp
+
+
+def rlcs_sample_actions(logits, uniforms, *, temperature=None, top_k=None, top_p=None, min_p=None, actions=None, log_probs=None,
+                        kept_log_probs=None, stream=None):
+    """Actions drawn from float32 logits [R, A] (rows may be strided) with one uniform a row; temperature, top_k (int32), top_p
+    and min_p are numbers or [R] tensors.  Returns (actions int32, log_probs, kept_log_probs), all [R]."""
+    return _sample_actions("rlcs_sample_actions", "f32", logits, uniforms, temperature, top_k, top_p, min_p, actions, log_probs,
+                           kept_log_probs, stream)
+
+
+def rlcs_sample_actions_bf16(logits, uniforms, *, temperature=None, top_k=None, top_p=None, min_p=None, actions=None, log_probs=None,
+                             kept_log_probs=None, stream=None):
+    """rlcs_sample_actions on bfloat16 logits."""
+    return _sample_actions("rlcs_sample_actions_bf16", "bf16", logits, uniforms, temperature, top_k, top_p, min_p, actions, log_probs,
+                           kept_log_probs, stream)
+
+
+def _policy_grad(name, kind, logits, actions, advantages, old_log_probs, mask, temperature, clip, entropy_coef, scale, want_grad,
+                 loss, log_probs, entropy, dlogits, stream):
+    torch = _torch()
+    ptr, ld = _rows(logits, kind, "logits")
+    R, A = logits.shape
+    lp = _alloc((R,), torch.float32, logits.device) if log_probs is None else log_probs
+    ent = _alloc((R,), torch.float32, logits.device) if entropy is None else entropy
+    dptr, ldd = None, 0
+    if advantages is None:
+        if old_log_probs is not None or loss is not None or dlogits is not None:
+            raise ValueError("old_log_probs, loss and dlogits go with advantages")
+    else:
+        loss = _alloc((R,), torch.float32, logits.device) if loss is None else loss
+        if dlogits is None and want_grad:
+            dlogits = _alloc((R, A), logits.dtype, logits.device)
+        if dlogits is not None:
+            dptr, ldd = _rows(dlogits, kind, "dlogits", (R, A))
+    _check(getattr(lib(), name)(ptr, ld, _typed(actions, "i32", (R,), "actions"), _ptr(mask, "u8", (R,)),
+                                _typed(advantages, "f32", (R,), "advantages"), _typed(old_log_probs, "f32", (R,), "old_log_probs"),
+                                _typed(loss, "f32", (R,), "loss"), _typed(lp, "f32", (R,), "log_probs"),
+                                _typed(ent, "f32", (R,), "entropy"), dptr, ldd, R, A, temperature, clip, entropy_coef, scale,
+                                _stream(stream)))
+    if advantages is None:
+        return lp, ent
+    return (loss, lp, ent, dlogits) if dlogits is not None else (loss, lp, ent)
+
+
+def rlcs_policy_grad(logits, actions, advantages=None, *, old_log_probs=None, mask=None, temperature=1.0, clip=0.2, entropy_coef=0.0,
+                     scale=1.0, want_grad=True, loss=None, log_probs=None, entropy=None, dlogits=None, stream=None):
+    """Policy loss of float32 logits [R, A] (rows may be strided) and its gradient: (loss, log_probs, entropy, dlogits), without
+    dlogits if want_grad is False, and (log_probs, entropy) alone without advantages.  dlogits may be logits itself."""
+    return _policy_grad("rlcs_policy_grad", "f32", logits, actions, advantages, old_log_probs, mask, temperature, clip, entropy_coef,
+                        scale, want_grad, loss, log_probs, entropy, dlogits, stream)
+
+
+def rlcs_policy_grad_bf16(logits, actions, advantages=None, *, old_log_probs=None, mask=None, temperature=1.0, clip=0.2,
+                          entropy_coef=0.0, scale=1.0, want_grad=True, loss=None, log_probs=None, entropy=None, dlogits=None,
+                          stream=None):
+    """rlcs_policy_grad on bfloat16 logits (dlogits bfloat16, the per-row outputs float32)."""
+    return _policy_grad("rlcs_policy_grad_bf16", "bf16", logits, actions, advantages, old_log_probs, mask, temperature, clip,
+                        entropy_coef, scale, want_grad, loss, log_probs, entropy, dlogits, stream)
+
+
+def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, block_table, lens, *, scale,
+                               max_prefix_len=None, max_len=None, want_lse=True, out=None, lse=None, workspace=None, stream=None):
+    """One query a row over its group's paged prefix and its own pages.  q [B, H, d] (rows may be strided), caches
+    [pages, page, Hk, d] (any strides with contiguous d), tables and lengths int32; prefix_table, prefix_lens and group_offsets
+    None: no prefixes.  Returns (out, lse), or out without lse."""
+    torch = _torch()
+    if q.dim() != 3 or k_cache.dim() != 4 or tuple(v_cache.shape) != tuple(k_cache.shape):
+        raise ValueError("expected q [B, H, d] and caches [pages, page, Hk, d] of one shape")
+    for t, what in ((q, "q"), (k_cache, "k_cache"), (v_cache, "v_cache")):
+        if not t.is_cuda:
+            raise TypeError("rlcs takes CUDA tensors (device pointers); there is no CPU path")
+        _require_current_device(t, what)
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"expected bfloat16 for {what}, got {t.dtype}")
+    B, H, d = q.shape
+    pages, page, Hk = k_cache.shape[:3]
+    if k_cache.shape[3] != d or q.stride(2) != 1 or (H > 1 and q.stride(1) != d) or k_cache.stride(3) != 1:
+        raise ValueError("q and the caches must agree in d, with heads of q and d of both contiguous")
+    if k_cache.stride() != v_cache.stride():
+        raise ValueError("k_cache and v_cache must have the same strides")
+    if (prefix_table is None) != (prefix_lens is None) or (prefix_table is None) != (group_offsets is None):
+        raise ValueError("prefix_table, prefix_lens and group_offsets go together")
+    groups = 0 if prefix_table is None else prefix_table.shape[0]
+    widths = 0 if prefix_table is None else prefix_table.shape[1], block_table.shape[1]
+    mp = widths[0] * page if max_prefix_len is None else min(int(max_prefix_len), widths[0] * page)
+    ml = widths[1] * page if max_len is None else min(int(max_len), widths[1] * page)
+    if out is None:
+        out = _alloc((B, H, d), torch.bfloat16, q.device)
+    if lse is None and want_lse:
+        lse = _alloc((B, H), torch.float32, q.device)
+    need = int(lib().rlcs_prefix_attention_workspace_bytes(B, H, Hk, d, page, groups, mp, ml))
+    if workspace is None:
+        workspace = _alloc((max(need, 16),), torch.uint8, q.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    _require_current_device(workspace, "workspace")
+    sp, st, sh = k_cache.stride()[:3]
+    _check(lib().rlcs_prefix_attention_bf16(
+        q.data_ptr(), q.stride(0) if B > 1 else H * d, k_cache.data_ptr(), v_cache.data_ptr(), pages, sp, st, sh,
+        _typed(prefix_table, "i32", (groups, widths[0]), "prefix_table"), widths[0], _typed(prefix_lens, "i32", (groups,), "prefix_lens"),
+        _typed(group_offsets, "i32", (groups + 1,), "group_offsets"), _typed(block_table, "i32", (B, widths[1]), "block_table"),
+        widths[1], _typed(lens, "i32", (B,), "lens"), _typed(out, "bf16", (B, H, d), "out"), _typed(lse, "f32", (B, H), "lse"),
+        B, H, Hk, d, page, groups, mp, ml, scale, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out if lse is None else (out, lse)
+
+
+def rlcs_block_tables(cached, added, free_pages, block_table, *, page_size, num_slots, slots=None, positions=None, offsets=None,
+                      page_offsets=None, stream=None):
+    """One step's page tables (block_table [B, width], in place), slot map and positions from int32 lengths on the GPU.  Returns
+    (slots int64 [num_slots], positions int32 [num_slots], offsets int32 [B + 1], page_offsets int32 [B + 1])."""
+    torch = _torch()
+    if cached.dim() != 1 or free_pages.dim() != 1 or block_table.dim() != 2:
+        raise ValueError("expected cached [B], free_pages [F], block_table [B, width]")
+    B, width = block_table.shape
+    dev = cached.device
+    slots = _alloc((num_slots,), torch.int64, dev) if slots is None else slots
+    positions = _alloc((num_slots,), torch.int32, dev) if positions is None else positions
+    offsets = _alloc((B + 1,), torch.int32, dev) if offsets is None else offsets
+    page_offsets = _alloc((B + 1,), torch.int32, dev) if page_offsets is None else page_offsets
+    _check(lib().rlcs_block_tables(
+        _typed(cached, "i32", (B,), "cached"), _typed(added, "i32", (B,), "added"), _typed(free_pages, "i32", None, "free_pages"),
+        _typed(block_table, "i32", None, "block_table"), _typed(slots, "i64", (num_slots,), "slots"),
+        _typed(positions, "i32", (num_slots,), "positions"), _typed(offsets, "i32", (B + 1,), "offsets"),
+        _typed(page_offsets, "i32", (B + 1,), "page_offsets"), B, width, free_pages.numel(), num_slots, page_size, _stream(stream)))
+    return slots, positions, offsets, page_offsets
