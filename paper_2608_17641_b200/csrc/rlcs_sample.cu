@@ -3,16 +3,21 @@
 // All choices go by whole weights w_j = floor(2^31 exp((l_j - max) / T) + 1/2): their sums are exact in 64-bit integers,
 // so the drawn action does not depend on how a row is split over threads, and every comparison of the filters is
 // made between the same numbers on every run.
+#include <cooperative_groups.h>
+
 #include <cmath>
 #include <cstdint>
 
 #include "../../include/rlcs.h"
+#include "rlcs_device.cuh"
 #include "rlcs_rows.cuh"
 
 namespace {
 
 using namespace rlcs_rows;
 typedef unsigned long long u64;
+
+constexpr int64_t kMostBlocks = (int64_t(1) << 31) - 1;
 
 template <typename T> struct SampleParams {
     const T* logits;
@@ -31,16 +36,23 @@ template <typename T> struct SampleParams {
     int A;
 };
 
+// Unsigned key in the order of the floats, and back.  bfloat16 values have 16 bits of key.
+template <typename T> struct Key {
+    static constexpr int kDown = sizeof(T) == 2 ? 16 : 0;
+    static __device__ __forceinline__ uint32_t of(float f) {
+        const uint32_t u = __float_as_uint(f);
+        return (u ^ (((int32_t)u >> 31) | 0x80000000u)) >> kDown;
+    }
+    static __device__ __forceinline__ float value(uint32_t key) {
+        const uint32_t u = key << kDown;
+        return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~(u | (kDown ? 0xffffu : 0u)));
+    }
+};
+
 // The logit as compared: NaN counts as -inf (never drawn), -0 as +0.
-template <typename T> __device__ __forceinline__ float logit(const T* x, int j) { return fmaxf(Vec<T>::load(x + j), -INFINITY) + 0.f; }
+__device__ __forceinline__ float clean(float f) { return fmaxf(f, -INFINITY) + 0.f; }
 
-// Unsigned key in the order of the floats.
-__device__ __forceinline__ uint32_t key_of(float f) {
-    const uint32_t u = __float_as_uint(f);
-    return u ^ (((int32_t)u >> 31) | 0x80000000u);
-}
-
-__device__ __forceinline__ float exp_rel(float x, float m, float inv_t) { return expf(x == m ? 0.f : (x - m) * inv_t); }
+__device__ __forceinline__ float scaled(float x, float m, float inv_t) { return x == m ? 0.f : (x - m) * inv_t; }
 
 // floor(2^31 e + 1/2) for 0 <= e <= 1: the fraction's 24 bits shifted by the exponent, the last place rounded half up.
 __device__ __forceinline__ uint32_t weight_of(float e) {
@@ -50,190 +62,710 @@ __device__ __forceinline__ uint32_t weight_of(float e) {
     return down == 0 ? frac : down > 32 ? 0u : ((frac >> (down - 1)) + 1) >> 1;
 }
 
-template <int NT> struct Group {                 // NT threads that share a row: a warp, or a whole block
-    int tid;
-    u64* scratch;                                // NT / 32 words
+// A row's settings, with the cases that leave one candidate folded into limit = 1.
+struct Rules {
+    float inv_t, p, low;
+    int limit;
+};
 
-    __device__ __forceinline__ u64 sum(u64 v) {
-        v = warp_sum(v);
-        if constexpr (NT > 32) {
-            __syncthreads();
-            if ((tid & 31) == 0) scratch[tid >> 5] = v;
-            __syncthreads();
-            v = 0;
-            for (int k = 0; k < NT / 32; ++k) v += scratch[k];
-        }
-        return v;
+template <typename T> __device__ __forceinline__ Rules rules_of(const SampleParams<T>& P, int64_t row) {
+    const float t = P.temperature != nullptr ? P.temperature[row] : P.temperature_all;
+    const int k = P.top_k != nullptr ? P.top_k[row] : P.top_k_all;
+    Rules r;
+    r.p = P.top_p != nullptr ? P.top_p[row] : P.top_p_all;
+    r.low = P.min_p != nullptr ? P.min_p[row] : P.min_p_all;
+    const bool greedy = !(t > 0.f);
+    r.inv_t = greedy ? 1.f : 1.f / t;
+    r.limit = k > 0 && k < P.A ? k : P.A;
+    if (greedy || r.p <= 0.f || r.low > 1.f) r.limit = 1;
+    if (!(r.low > 0.f) || r.low > 1.f) r.low = 0.f;
+    if (!(r.p < 1.f)) r.p = 1.f;
+    return r;
+}
+
+__device__ __forceinline__ uint32_t weight_at(float x, float m, const Rules& r) {
+    const float e = expf(scaled(x, m, r.inv_t));
+    return e >= r.low ? weight_of(e) : 0u;
+}
+
+__device__ __forceinline__ u64 target_of(float uniform, u64 kept) {
+    const double u = (double)uniform;
+    const u64 t = u > 0. ? (u64)(u * (double)kept) : 0;
+    return t < kept ? t : kept - 1;
+}
+
+// How many of equally weighted candidates stay when `above` lies before them: the least n with above + n w >= enough.
+__device__ __forceinline__ int ties_until(double enough, u64 above, uint32_t w) {
+    if (w == 0) return 1;
+    int n = (int)((enough - (double)above) / (double)w);
+    while (n > 0 && (double)(above + (u64)(n - 1) * w) >= enough) --n;
+    while ((double)(above + (u64)n * w) < enough) ++n;
+    return n;
+}
+
+template <typename T>
+__device__ __forceinline__ void write_row(const SampleParams<T>& P, int64_t row, int action, float x, float m, float inv_t, u64 all, u64 kept) {
+    const double d = (double)scaled(x, m, inv_t);
+    P.actions[row] = action;
+    P.log_probs[row] = (float)(d - log((double)all * 0x1p-31));
+    P.kept_log_probs[row] = (float)(d - log((double)kept * 0x1p-31));
+}
+
+template <typename T> __device__ __forceinline__ void write_none(const SampleParams<T>& P, int64_t row) {
+    P.actions[row] = -1;
+    P.log_probs[row] = -INFINITY;
+    P.kept_log_probs[row] = -INFINITY;
+}
+
+// ---------------------------------------------------------------------------------------------- up to 64 actions
+// One thread a row.  The block copies its rows to shared memory (coalesced; an odd row stride keeps the threads' walks
+// in different banks); a thread then walks its row, and takes candidates one by one where there are filters.
+constexpr int kSmallRows = 128, kSmallA = 64;
+
+template <typename T>
+__global__ void __launch_bounds__(kSmallRows) sample_small_kernel(const __grid_constant__ SampleParams<T> P, uint32_t a_mul) {
+    extern __shared__ float tile[];
+    const int A = P.A, stride = A | 1;
+    const int64_t row0 = (int64_t)blockIdx.x * kSmallRows, row = row0 + threadIdx.x;
+    const int rows = P.R - row0 < kSmallRows ? (int)(P.R - row0) : kSmallRows;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < rows * A; i += kSmallRows) {
+        const int r = a_mul != 0 ? (int)__umulhi((uint32_t)i, a_mul) : i, j = i - r * A;
+        tile[r * stride + j] = clean(Vec<T>::load(P.logits + (row0 + r) * P.ld + j));
     }
-    __device__ __forceinline__ uint32_t max(uint32_t v) {
-        v = warp_max(v);
-        if constexpr (NT > 32) {
-            __syncthreads();
-            if ((tid & 31) == 0) scratch[tid >> 5] = v;
-            __syncthreads();
-            v = 0;
-            for (int k = 0; k < NT / 32; ++k) v = scratch[k] > v ? (uint32_t)scratch[k] : v;
-        }
-        return v;
+    __syncthreads();
+    if (row >= P.R) return;
+    float* x = tile + threadIdx.x * stride;
+    const Rules r = rules_of(P, row);
+    float m = -INFINITY;
+    for (int j = 0; j < A; ++j) m = fmaxf(m, x[j]);
+    if (m == -INFINITY) return write_none(P, row);
+    u64 all = 0, kept = 0, stay = 0;
+    for (int j = 0; j < A; ++j) {
+        const float e = expf(scaled(x[j], m, r.inv_t));
+        const uint32_t w = weight_of(e);
+        all += w;
+        if (e >= r.low) { kept += w; stay |= 1ull << j; }
     }
-    // this warp's value summed over the warps before it; *all = over all warps
-    __device__ __forceinline__ u64 before(u64 v, u64* all) {
-        u64 mine = 0, total = v;
-        if constexpr (NT > 32) {
-            __syncthreads();
-            if ((tid & 31) == 0) scratch[tid >> 5] = v;
-            __syncthreads();
-            total = 0;
-            for (int k = 0; k < NT / 32; ++k) {
-                if (k == (tid >> 5)) mine = total;
-                total += scratch[k];
+    // the first candidate behind (value, index) in order
+    auto next = [&](float v, int at, u64 among) {
+        float best = -INFINITY;
+        int where = -1;
+        for (int j = 0; j < A; ++j)
+            if ((among >> j & 1) && (x[j] < v || (x[j] == v && j > at)) && (where < 0 || x[j] > best)) { best = x[j]; where = j; }
+        return where;
+    };
+    if (r.limit < A) {
+        u64 some = 0;
+        kept = 0;
+        float v = INFINITY;
+        int at = -1;
+        for (int n = 0; n < r.limit; ++n) {
+            at = next(v, at, ~0ull);
+            v = x[at];
+            if (!(stay >> at & 1)) continue;
+            some |= 1ull << at;
+            kept += weight_at(v, m, r);
+        }
+        stay = some;
+    }
+    if (r.p < 1.f && r.limit > 1) {
+        const double enough = (double)r.p * (double)kept;
+        u64 some = 0;
+        kept = 0;
+        float v = INFINITY;
+        int at = -1;
+        do {
+            at = next(v, at, stay);
+            v = x[at];
+            some |= 1ull << at;
+            kept += weight_at(v, m, r);
+        } while ((double)kept < enough && some != stay);
+        stay = some;
+    }
+    const u64 target = target_of(P.uniforms[row], kept);
+    u64 sum = 0;
+    for (int j = 0; j < A; ++j) {
+        if (!(stay >> j & 1)) continue;
+        sum += weight_at(x[j], m, r);
+        if (sum > target) return write_row(P, row, j, x[j], m, r.inv_t, all, kept);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- up to 1024 actions
+// One warp a row, the row's keys and weights in registers (lane l holds elements l, l + 32, ...).  A cut is found bit by
+// bit from the top: 32 (16) rounds of a comparison and an addition an element.
+template <typename T, int PER>
+__global__ void __launch_bounds__(256) sample_warp_kernel(const __grid_constant__ SampleParams<T> P) {
+    typedef Key<T> K;
+    const int lane = threadIdx.x & 31, A = P.A;
+    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (row >= P.R) return;
+    const T* x = P.logits + row * P.ld;
+    const Rules r = rules_of(P, row);
+    uint32_t key[PER], w[PER];
+    uint32_t top_key = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int j = i * 32 + lane;
+        key[i] = j < A ? K::of(clean(Vec<T>::load(x + j))) : 0u;          // 0: below every logit
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) top_key = max(top_key, key[i]);
+    top_key = warp_max(top_key);
+    const float m = K::value(top_key);
+    if (m == -INFINITY) {
+        if (lane == 0) write_none(P, row);
+        return;
+    }
+    u64 all = 0, kept = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const float e = key[i] ? expf(scaled(K::value(key[i]), m, r.inv_t)) : 0.f;
+        w[i] = weight_of(e);
+        all += w[i];
+        if (!(e >= r.low)) w[i] = 0;
+        kept += w[i];
+    }
+    all = warp_sum(all);
+    kept = r.low > 0.f ? warp_sum(kept) : all;
+    uint32_t cut = 0;
+    int ties = A;
+    if (r.limit == 1) {
+        cut = top_key;
+        ties = 1;
+        kept = 0x80000000u;
+    } else if (r.limit < A) {
+        for (int b = 31 - K::kDown; b >= 0; --b) {
+            const uint32_t next = cut | (1u << b);
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) n += key[i] >= next;
+            if (__reduce_add_sync(~0u, n) >= r.limit) cut = next;
+        }
+        int n = 0;
+        kept = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            n += key[i] > cut;
+            kept += key[i] > cut ? w[i] : 0u;
+        }
+        ties = r.limit - __reduce_add_sync(~0u, n);
+        kept = warp_sum(kept) + (u64)ties * weight_at(K::value(cut), m, r);
+    }
+    if (r.p < 1.f && r.limit > 1) {
+        const double enough = (double)r.p * (double)kept;
+        uint32_t c = cut;                                        // everything from the cut up weighs enough
+        for (int b = 31 - K::kDown; b >= 0; --b) {
+            const uint32_t next = (c & ~((2u << b) - 1)) | (c & (1u << b)) | (1u << b);
+            if (next <= c) continue;                             // the bit is set already
+            u64 n = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) n += key[i] >= next ? w[i] : 0u;
+            if ((double)warp_sum(n) >= enough) c = next;
+        }
+        u64 above = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) above += key[i] > c ? w[i] : 0u;
+        above = warp_sum(above);
+        const uint32_t at = weight_at(K::value(c), m, r);
+        const int more = ties_until(enough, above, at);
+        if (c > cut || more < ties) ties = more;
+        cut = c;
+        kept = above + (u64)ties * at;
+    }
+    const u64 target = target_of(P.uniforms[row], kept);
+    u64 sum = 0;
+    int seen = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const bool tied = key[i] == cut;
+        const unsigned tie_lanes = __ballot_sync(~0u, tied);
+        const bool in = key[i] > cut || (tied && seen + __popc(tie_lanes & ((1u << lane) - 1)) < ties);
+        seen += __popc(tie_lanes);
+        const u64 mine = in ? w[i] : 0u;
+        const u64 step = warp_sum(mine);
+        if (sum + step > target) {
+            u64 run = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 v = __shfl_up_sync(~0u, run, o);
+                run += lane >= o ? v : 0;
             }
+            const unsigned past = __ballot_sync(~0u, sum + run > target);
+            if (lane == __ffs(past) - 1) write_row(P, row, i * 32 + lane, K::value(key[i]), m, r.inv_t, all, kept);
+            return;
         }
-        *all = total;
-        return mine;
+        sum += step;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- more actions
+// One cluster of 1 to 8 blocks a row, each with a part of it that its passes find in L1 or L2 again; every warp has a
+// contiguous range, so that sums in index order are sums over warps in order.
+//   no cut (no top-k, no top-p):  maximum; weights by warp; one warp walks the range that holds the target.
+//   top-k up to 192: the k-th largest of the threads' own maxima bounds the k-th largest logit from below, so that few
+//     candidates pass it (about 200 of 131072 for k = 192 and 2048 threads); one block sorts them and does the rest.
+//   otherwise a histogram of weights and counts over 32 steps of (l - max) / T, one column a lane and so without atomics,
+//     finds the step that holds a cut; histograms over the keys of that step alone narrow it to one key.
+constexpr int kT = 256, kW = kT / 32, kCoarse = 32, kFine = 1024, kList = 2048, kListLimit = 192, kMaxCluster = 8;
+constexpr u64 kCountOne = 1ull << 48;                        // a column's entry: count above, weight below bit 48
+
+struct Shared {
+    union {
+        u64 column[kW][kCoarse][32];
+        struct {
+            u64 weight[kFine];
+            uint32_t count[kFine];
+        } fine;
+        struct {
+            u64 list[kList];                                 // (key, ~index)
+            uint32_t maxima[kMaxCluster * kT];
+            uint32_t digit[256];
+        };
+    };
+    u64 trade[2][kW];
+    u64 coarse_weight[kCoarse];
+    uint32_t coarse_count[kCoarse];
+    u64 scan_weight[kW];
+    uint32_t scan_count[kW];
+    u64 found_weight;
+    uint32_t found_count, found_at, found_bin, listed, bound;
+};
+
+template <typename T> struct ClusterRow {
+    typedef Key<T> K;
+    const T* x;
+    Shared& sh;
+    int A, lane, warp, rank, ranks, turn;
+    Span sp;
+    int v0, v1;                                              // this warp's vectors
+
+    __device__ __forceinline__ void sync() {
+        if (ranks > 1) cooperative_groups::this_cluster().sync(); else __syncthreads();
+    }
+    __device__ __forceinline__ Shared& other(int rank_) {
+        return ranks > 1 ? *cooperative_groups::this_cluster().map_shared_rank(&sh, rank_) : sh;
+    }
+    __device__ __forceinline__ bool first_warp() const { return rank == 0 && warp == 0; }
+    __device__ __forceinline__ bool last_warp() const { return rank == ranks - 1 && warp == kW - 1; }
+    __device__ __forceinline__ int tail_at() const { return sp.head + sp.vecs * Vec<T>::N; }
+
+    // f(logit, index) for every element of the warp's range
+    template <typename F> __device__ __forceinline__ void each(F f) const {
+        constexpr int N = Vec<T>::N;
+        if (first_warp() && lane < sp.head) f(clean(Vec<T>::load(x + lane)), lane);
+#pragma unroll 2
+        for (int v = v0 + lane; v < v1; v += 32) {
+            const int at = sp.head + v * N;
+            float g[N];
+            Vec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(x + at)), g);
+#pragma unroll
+            for (int k = 0; k < N; ++k) f(clean(g[k]), at + k);
+        }
+        if (last_warp() && tail_at() + lane < A) f(clean(Vec<T>::load(x + tail_at() + lane)), tail_at() + lane);
+    }
+    // over the cluster: the sum of all warps' values, and of those of the warps before this one
+    __device__ __forceinline__ u64 gather(u64 v, u64* before) {
+        v = warp_sum(v);
+        turn ^= 1;
+        if (lane == 0) sh.trade[turn][warp] = v;
+        sync();
+        u64 total = 0, mine = 0;
+        for (int i = lane; i < ranks * kW; i += 32) {
+            const u64 u = other(i / kW).trade[turn][i % kW];
+            total += u;
+            if (i < rank * kW + warp) mine += u;
+        }
+        if (before != nullptr) *before = warp_sum(mine);
+        return warp_sum(total);
+    }
+    __device__ __forceinline__ u64 gather_max(u64 v) {
+        v = warp_max(v);
+        turn ^= 1;
+        if (lane == 0) sh.trade[turn][warp] = v;
+        sync();
+        u64 top = 0;
+        for (int i = lane; i < ranks * kW; i += 32) { const u64 u = other(i / kW).trade[turn][i % kW]; top = u > top ? u : top; }
+        return warp_max(top);
+    }
+    // This warp's range in index order: the element at which the running sum, `sum` before the range, passes the target.
+    template <typename F> __device__ __forceinline__ int walk(u64 sum, u64 target, F value) const {
+        constexpr int N = Vec<T>::N;
+        int found = -1;
+        auto step = [&](const float* g, int n, int at) {     // n elements a lane, lane after lane
+            u64 mine = 0;
+#pragma unroll
+            for (int k = 0; k < N; ++k) if (k < n) mine += value(g[k], at + k);
+            u64 run = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 u = __shfl_up_sync(~0u, run, o);
+                run += lane >= o ? u : 0;
+            }
+            const unsigned past = __ballot_sync(~0u, sum + run > target);
+            if (past) {
+                u64 s = sum + run - mine;
+                int hit = -1;
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (k < n) {
+                        s += value(g[k], at + k);
+                        if (hit < 0 && s > target) hit = at + k;
+                    }
+                found = __shfl_sync(~0u, hit, __ffs(past) - 1);
+            }
+            sum += __shfl_sync(~0u, run, 31);
+        };
+        float g[N];
+        if (first_warp() && sp.head > 0) {
+            if (lane < sp.head) g[0] = clean(Vec<T>::load(x + lane));
+            step(g, lane < sp.head ? 1 : 0, lane);
+        }
+        for (int base = v0; base < v1 && found < 0; base += 32) {
+            const int v = base + lane, at = sp.head + v * N;
+            if (v < v1) {
+                Vec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(x + at)), g);
+#pragma unroll
+                for (int k = 0; k < N; ++k) g[k] = clean(g[k]);
+            }
+            step(g, v < v1 ? N : 0, at);
+        }
+        if (last_warp() && tail_at() < A && found < 0) {
+            const bool in = tail_at() + lane < A;
+            if (in) g[0] = clean(Vec<T>::load(x + tail_at() + lane));
+            step(g, in ? 1 : 0, tail_at() + lane);
+        }
+        return found;
     }
 };
 
-template <typename T, int NT>
-__global__ void __launch_bounds__(NT < 256 ? 256 : NT) sample_rows_kernel(const __grid_constant__ SampleParams<T> P) {
-    constexpr int kRows = NT < 256 ? 256 / NT : 1;
-    __shared__ u64 scratch[NT / 32];
-    Group<NT> group = {(int)threadIdx.x % NT, scratch};
-    const int tid = group.tid, lane = tid & 31, A = P.A;
-    // a warp's own part of the row, a whole number of 32-element steps
-    const int part = ((A + NT - 1) / NT) * 32, lo = (tid >> 5) * part, hi = lo + part < A ? lo + part : A;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT; row < P.R; row += (int64_t)gridDim.x * kRows) {
-        const T* x = P.logits + row * P.ld;
-        const float t = P.temperature != nullptr ? P.temperature[row] : P.temperature_all;
-        const int k_asked = P.top_k != nullptr ? P.top_k[row] : P.top_k_all;
-        const float p = P.top_p != nullptr ? P.top_p[row] : P.top_p_all;
-        float low = P.min_p != nullptr ? P.min_p[row] : P.min_p_all;
-        const bool greedy = !(t > 0.f);
-        const float inv_t = greedy ? 1.f : 1.f / t;
-        int limit = k_asked > 0 && k_asked < A ? k_asked : A;
-        if (greedy || p <= 0.f || low > 1.f) limit = 1;
-        if (!(low > 0.f) || low > 1.f) low = 0.f;
+// A cut being narrowed: keys in [lo, hi] hold it; `above` sums what lies over hi.
+struct Cut {
+    uint32_t lo, hi, above_count, at_count;
+    u64 above_weight;
+};
 
-        uint32_t top_key = 0;
-        for (int j = tid; j < A; j += NT) { const uint32_t k = key_of(logit(x, j)); top_key = k > top_key ? k : top_key; }
-        top_key = group.max(top_key);
-        const float m = __uint_as_float(top_key & 0x80000000u ? top_key ^ 0x80000000u : ~top_key);
-        if (m == -INFINITY) {
-            if (tid == 0) {
-                P.actions[row] = -1;
-                P.log_probs[row] = -INFINITY;
-                P.kept_log_probs[row] = -INFINITY;
-            }
-            continue;
-        }
+template <typename T>
+__global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constant__ SampleParams<T> P) {
+    typedef Key<T> K;
+    extern __shared__ __align__(16) char raw[];
+    Shared& sh = *reinterpret_cast<Shared*>(raw);
+    const int ranks = (int)cooperative_groups::this_cluster().num_blocks(), rank = (int)cooperative_groups::this_cluster().block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row = blockIdx.x / ranks;
+    const T* x = P.logits + row * P.ld;
+    ClusterRow<T> row_ = {x, sh, P.A, lane, warp, rank, ranks, 0, span_of(x, P.A), 0, 0};
+    {
+        const int per = (row_.sp.vecs + ranks * kW - 1) / (ranks * kW), at = (rank * kW + warp) * per;
+        row_.v0 = min(at, row_.sp.vecs);
+        row_.v1 = min(at + per, row_.sp.vecs);
+    }
+    const Rules r = rules_of(P, row);
+
+    uint32_t my_top = 0;
+    row_.each([&](float f, int) { my_top = max(my_top, K::of(f)); });
+    const uint32_t top_key = (uint32_t)row_.gather_max(my_top);
+    const float m = K::value(top_key);
+    const float exp2_t = r.inv_t * 1.4426950408889634f;
+    // a quick exponential where only its sum's logarithm counts (ex2.approx: 2^-22), not a choice
+    auto quick = [&](float f) {
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f == m ? 0.f : (f - m) * exp2_t));
+        return e;
+    };
+    auto all_of = [&](float part) { return row_.gather((u64)((double)part * 0x1p31 + 0.5), nullptr); };
+    auto finish = [&](u64 kept, u64 all, u64 before, u64 mine, uint32_t cut, int tie_end) {
+        const u64 target = target_of(P.uniforms[row], kept);
+        if (target < before || target >= before + mine) return;
+        const int a = row_.walk(before, target, [&](float f, int j) -> u64 {
+            const uint32_t k = K::of(f);
+            return k > cut || (k == cut && j < tie_end) ? weight_at(f, m, r) : 0u;
+        });
+        if (lane == 0 && a >= 0) write_row(P, row, a, clean(Vec<T>::load(x + a)), m, r.inv_t, all, kept);
+    };
+
+    if (m == -INFINITY) {
+        if (rank == 0 && tid == 0) write_none(P, row);
+    } else if (r.limit == 1) {
+        float part = 0.f;
+        uint32_t first = 0;                                  // ~index, so that the lowest wins
+        row_.each([&](float f, int j) {
+            part += quick(f);
+            if (K::of(f) == top_key) first = max(first, ~(uint32_t)j);
+        });
+        const u64 all = all_of(part);
+        const int a = (int)~(uint32_t)row_.gather_max(first);
+        if (rank == 0 && tid == 0) write_row(P, row, a, m, m, r.inv_t, all, 0x80000000ull);
+    } else if (r.limit == P.A && r.p >= 1.f) {
+        u64 mine = 0, before;
+        float part = 0.f;
+        if (r.low > 0.f) row_.each([&](float f, int) { part += quick(f); mine += weight_at(f, m, r); });
+        else row_.each([&](float f, int) { mine += weight_at(f, m, r); });
+        const u64 kept = row_.gather(mine, &before);
+        finish(kept, r.low > 0.f ? all_of(part) : kept, before, warp_sum(mine), 0, 0);
+    } else {
+        bool done = false;
         u64 all = 0;
-        for (int j = tid; j < A; j += NT) all += weight_of(exp_rel(logit(x, j), m, inv_t));
-        all = group.sum(all);
-
-        // kept: every key above `cut`, and the first `ties` of those that equal it (where the weight is not below min-p)
-        uint32_t cut = 0;
-        int ties = A;
-        if (limit < A) {
-            cut = limit == 1 ? top_key : 0;
-            if (limit > 1)
-                for (int b = 31; b >= 0; --b) {
-                    const uint32_t next = cut | (1u << b);
-                    u64 n = 0;
-                    for (int j = tid; j < A; j += NT) n += key_of(logit(x, j)) >= next;
-                    if (group.sum(n) >= (u64)limit) cut = next;
-                }
-            u64 above = 0;
-            for (int j = tid; j < A; j += NT) above += key_of(logit(x, j)) > cut;
-            ties = limit - (int)group.sum(above);
-        }
-        auto weight = [&](float f) {
-            const float e = exp_rel(f, m, inv_t);
-            return e >= low ? weight_of(e) : 0u;
-        };
-        u64 kept = all;
-        if (limit < A || low > 0.f) {
-            kept = 0;
-            for (int j = tid; j < A; j += NT) { const float f = logit(x, j); kept += key_of(f) > cut ? weight(f) : 0u; }
-            kept = group.sum(kept);
-            if (limit < A) kept += (u64)ties * weight(__uint_as_float(cut & 0x80000000u ? cut ^ 0x80000000u : ~cut));
-        }
-        if (p < 1.f && limit > 1) {
-            const double enough = (double)p * (double)kept;
-            uint32_t c = 0;
-            for (int b = 31; b >= 0; --b) {
-                const uint32_t next = c | (1u << b);
-                u64 n = 0;
-                if (next >= cut || limit == A)
-                    for (int j = tid; j < A; j += NT) { const float f = logit(x, j); n += key_of(f) >= next ? weight(f) : 0u; }
-                else
-                    n = ~0ull >> 16;
-                n = next >= cut || limit == A ? group.sum(n) : n;
-                if ((double)n >= enough) c = next;
-            }
-            u64 above = 0;
-            for (int j = tid; j < A; j += NT) { const float f = logit(x, j); above += key_of(f) > c ? weight(f) : 0u; }
-            above = group.sum(above);
-            const uint32_t w = weight(__uint_as_float(c & 0x80000000u ? c ^ 0x80000000u : ~c));
-            int more = w ? (int)((enough - (double)above) / (double)w) : 0;
-            while (more > 0 && (double)(above + (u64)(more - 1) * w) >= enough) --more;
-            while (w != 0 && (double)(above + (u64)more * w) < enough) ++more;
-            if (c > cut || more < ties || limit == A) ties = more;
-            cut = c;
-            kept = above + (u64)ties * w;
-        }
-        const double u = (double)P.uniforms[row];
-        u64 target = u > 0. ? (u64)(u * (double)kept) : 0;
-        if (target >= kept) target = kept - 1;
-
-        // the action: the first index whose kept weights, summed in index order, pass the target
-        u64 ties_all = 0;
-        int n = 0;
-        for (int j = lo + lane; j < hi; j += 32) n += key_of(logit(x, j)) == cut;
-        n = warp_sum(n);
-        const int ties_before = (int)group.before((u64)n, &ties_all);
-        u64 mine = 0;
-        int seen = ties_before;
-        for (int base = lo; base < hi; base += 32) {
-            const int j = base + lane;
-            const float f = j < hi ? logit(x, j) : -INFINITY;
-            const uint32_t key = j < hi ? key_of(f) : 0;
-            const unsigned tied = __ballot_sync(~0u, j < hi && key == cut);
-            const bool in = j < hi && (key > cut || (key == cut && seen + __popc(tied & ((1u << lane) - 1)) < ties));
-            mine += in ? weight(f) : 0u;
-            seen += __popc(tied);
-        }
-        mine = warp_sum(mine);
-        u64 total = 0;
-        u64 sum = group.before(mine, &total);
-        if (target >= sum && target < sum + mine) {
-            seen = ties_before;
-            for (int base = lo; base < hi; base += 32) {
-                const int j = base + lane;
-                const float f = j < hi ? logit(x, j) : -INFINITY;
-                const uint32_t key = j < hi ? key_of(f) : 0;
-                const unsigned tied = __ballot_sync(~0u, j < hi && key == cut);
-                const bool in = j < hi && (key > cut || (key == cut && seen + __popc(tied & ((1u << lane) - 1)) < ties));
-                u64 w = in ? weight(f) : 0u;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const u64 v = __shfl_up_sync(~0u, w, o);
-                    w += lane >= o ? v : 0;
-                }
-                const unsigned past = __ballot_sync(~0u, sum + w > target);
-                if (past) {
-                    if (lane == __ffs(past) - 1) {
-                        const double d = f == m ? 0. : (double)((f - m) * inv_t);
-                        P.actions[row] = j;
-                        P.log_probs[row] = (float)(d - log((double)all * 0x1p-31));
-                        P.kept_log_probs[row] = (float)(d - log((double)kept * 0x1p-31));
+        if (r.limit <= kListLimit) {
+            Shared& lead = row_.other(0);
+            lead.maxima[rank * kT + tid] = my_top;
+            if (rank == 0 && tid == 0) sh.listed = 0;
+            row_.sync();
+            if (rank == 0) {
+                // the limit-th largest of the maxima, its upper 16 bits
+                uint32_t prefix = 0, want = r.limit;
+                constexpr int kTop = 32 - K::kDown;
+                for (int round = 0; round < 2; ++round) {
+                    const int shift = kTop - 8 * (round + 1);
+                    sh.digit[tid] = 0;
+                    __syncthreads();
+                    for (int i = tid; i < ranks * kT; i += kT)
+                        if (round == 0 || sh.maxima[i] >> (shift + 8) == prefix) atomicAdd(&sh.digit[(sh.maxima[i] >> shift) & 255], 1u);
+                    __syncthreads();
+                    if (warp == 0) {                         // lane l: digits 255 - 8l down to 248 - 8l
+                        uint32_t n[8], sum = 0;
+                        for (int k = 0; k < 8; ++k) sum += n[k] = sh.digit[255 - 8 * lane - k];
+                        uint32_t run = sum;
+                        for (int o = 1; o < 32; o <<= 1) {
+                            const uint32_t u = __shfl_up_sync(~0u, run, o);
+                            run += lane >= o ? u : 0;
+                        }
+                        if (run >= want && run - sum < want) {
+                            uint32_t s = run - sum;
+                            int k = 0;
+                            while (s + n[k] < want) s += n[k++];
+                            sh.found_bin = prefix << 8 | (255 - 8 * lane - k);
+                            sh.found_count = want - s;
+                        }
                     }
-                    break;
+                    __syncthreads();
+                    prefix = sh.found_bin;
+                    want = sh.found_count;
                 }
-                sum += __shfl_sync(~0u, w, 31);
-                seen += __popc(tied);
+                if (tid == 0) sh.bound = prefix << (kTop - 16);
             }
+            row_.sync();
+            const uint32_t bound = lead.bound;
+            float part = 0.f;
+            row_.each([&](float f, int j) {
+                part += quick(f);
+                const uint32_t k = K::of(f);
+                if (k >= bound) {
+                    const uint32_t at = atomicAdd(&lead.listed, 1u);
+                    if (at < kList) lead.list[at] = (u64)k << 32 | ~(uint32_t)j;
+                }
+            });
+            all = all_of(part);                              // its barrier also completes the list
+            const uint32_t listed = lead.listed;
+            done = listed <= kList;
+            row_.sync();                                     // read by all before the room is used again
+            if (done && rank == 0) {
+                int size = 32;
+                while (size < (int)listed) size *= 2;
+                for (int i = tid; i < size; i += kT) if (i >= (int)listed) sh.list[i] = 0;
+                __syncthreads();
+                for (int k = 2; k <= size; k *= 2)
+                    for (int j = k / 2; j > 0; j /= 2) {
+                        for (int i = tid; i < size / 2; i += kT) {
+                            const int a = 2 * i - (i & (j - 1)), b = a + j;
+                            const u64 u = sh.list[a], v = sh.list[b];
+                            if ((u < v) == ((a & k) == 0)) { sh.list[a] = v; sh.list[b] = u; }
+                        }
+                        __syncthreads();
+                    }
+                const u64 entry = tid < r.limit ? sh.list[tid] : 0;
+                const int index = (int)~(uint32_t)entry;
+                const float f = K::value((uint32_t)(entry >> 32));
+                uint32_t w = tid < r.limit ? weight_at(f, m, r) : 0u;
+                u64 run = w;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const u64 u = __shfl_up_sync(~0u, run, o);
+                    run += lane >= o ? u : 0;
+                }
+                if (lane == 31) sh.scan_weight[warp] = run;
+                __syncthreads();
+                u64 total = 0, ahead = 0;
+                for (int k = 0; k < kW; ++k) { if (k < warp) ahead += sh.scan_weight[k]; total += sh.scan_weight[k]; }
+                const double enough = (double)r.p * (double)total;
+                if (r.p < 1.f && tid > 0 && !((double)(ahead + run - w) < enough)) w = 0;
+                __syncthreads();
+                sh.list[tid] = (u64)w;                       // weights and indices of the kept, in order
+                sh.maxima[tid] = (uint32_t)index;
+                const u64 part_kept = warp_sum((u64)w);
+                if (lane == 0) sh.scan_weight[warp] = part_kept;
+                __syncthreads();
+                u64 kept = 0;
+                for (int k = 0; k < kW; ++k) kept += sh.scan_weight[k];
+                const u64 target = target_of(P.uniforms[row], kept);
+                if (w != 0) {
+                    u64 upto = 0;
+                    for (int k = 0; k < r.limit; ++k) upto += sh.maxima[k] <= (uint32_t)index ? sh.list[k] : 0;
+                    if (upto > target && upto - w <= target) write_row(P, row, index, f, m, r.inv_t, all, kept);
+                }
+            }
+        }
+        if (!done) {
+            constexpr float kSteps = kCoarse / 22.25f;       // weights are 0 from 22.18 below the maximum on
+            auto bin_of = [&](float f) { return min((int)(scaled(f, m, r.inv_t) * -kSteps), kCoarse - 1); };
+            for (int i = tid; i < kW * kCoarse * 32; i += kT) (&sh.column[0][0][0])[i] = 0;
+            __syncthreads();
+            u64* column = &sh.column[warp][0][lane];
+            row_.each([&](float f, int) {
+                const float d = scaled(f, m, r.inv_t), e = expf(d);
+                const uint32_t w = weight_of(e);
+                if (w != 0) column[min((int)(d * -kSteps), kCoarse - 1) * 32] += kCountOne + (e >= r.low ? w : 0u);
+            });
+            __syncthreads();
+            for (int b = warp; b < kCoarse; b += kW) {
+                u64 w = 0;
+                uint32_t n = 0;
+                for (int k = 0; k < kW; ++k) { const u64 u = sh.column[k][b][lane]; w += u & (kCountOne - 1); n += (uint32_t)(u >> 48); }
+                w = warp_sum(w);
+                n = warp_sum(n);
+                if (lane == 0) { sh.coarse_weight[b] = w; sh.coarse_count[b] = n; }
+            }
+            row_.sync();
+            u64 bin_weight = 0, to_weight;                   // lane = step: its own, and up to and with it
+            uint32_t bin_count = 0, to_count;
+            for (int k = 0; k < ranks; ++k) { bin_weight += row_.other(k).coarse_weight[lane]; bin_count += row_.other(k).coarse_count[lane]; }
+            to_weight = bin_weight;
+            to_count = bin_count;
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 u = __shfl_up_sync(~0u, to_weight, o);
+                const uint32_t n = __shfl_up_sync(~0u, to_count, o);
+                if (lane >= o) { to_weight += u; to_count += n; }
+            }
+            const u64 weighed = __shfl_sync(~0u, to_weight, 31);
+            const uint32_t counted = __shfl_sync(~0u, to_count, 31);
+            if (r.low == 0.f && all == 0) all = weighed;
+            if (all == 0) {
+                float part = 0.f;
+                row_.each([&](float f, int) { part += quick(f); });
+                all = all_of(part);
+            }
+            // the cut where `want` candidates, or `enough` weight, are reached: first the step, then its keys by histograms
+            auto narrow = [&](bool by_count, uint32_t want, double enough) {
+                auto reached = [&](uint32_t n, u64 w) { return by_count ? n >= want : (double)w >= enough; };
+                const int b = __ffs(__ballot_sync(~0u, reached(to_count, to_weight))) - 1;
+                Cut c;
+                c.above_weight = __shfl_sync(~0u, to_weight - bin_weight, b);
+                c.above_count = __shfl_sync(~0u, to_count - bin_count, b);
+                c.at_count = __shfl_sync(~0u, bin_count, b);
+                auto least = [&](int bin) {                  // the least key whose step is at most `bin`
+                    uint32_t lo = K::of(-INFINITY), hi = top_key;
+                    while (lo < hi) {
+                        const uint32_t mid = lo + (hi - lo) / 2;
+                        if (bin_of(K::value(mid)) <= bin) hi = mid; else lo = mid + 1;
+                    }
+                    return lo;
+                };
+                c.lo = least(b);
+                c.hi = b == 0 ? top_key : least(b - 1) - 1;
+                while (c.lo < c.hi) {
+                    int shift = 0;
+                    while ((c.hi - c.lo) >> shift >= kFine) ++shift;
+                    row_.sync();                             // the room, and what others still read there
+                    for (int i = tid; i < kFine; i += kT) { sh.fine.weight[i] = 0; sh.fine.count[i] = 0; }
+                    __syncthreads();
+                    row_.each([&](float f, int) {
+                        const uint32_t k = K::of(f);
+                        if (k < c.lo || k > c.hi) return;
+                        const float e = expf(scaled(f, m, r.inv_t));
+                        const uint32_t w = weight_of(e);
+                        if (w == 0) return;
+                        const uint32_t at = (c.hi - k) >> shift;
+                        atomicAdd(&sh.fine.count[at], 1u);
+                        if (e >= r.low) atomicAdd(&sh.fine.weight[at], (u64)w);
+                    });
+                    row_.sync();
+                    u64 w[kFine / kT], sum_w = 0;
+                    uint32_t n[kFine / kT], sum_n = 0;
+#pragma unroll
+                    for (int k = 0; k < kFine / kT; ++k) {
+                        w[k] = 0;
+                        n[k] = 0;
+                        for (int q = 0; q < ranks; ++q) {
+                            const Shared& o = row_.other(q);
+                            w[k] += o.fine.weight[tid * (kFine / kT) + k];
+                            n[k] += o.fine.count[tid * (kFine / kT) + k];
+                        }
+                        sum_w += w[k];
+                        sum_n += n[k];
+                    }
+                    u64 run_w = sum_w;
+                    uint32_t run_n = sum_n;
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const u64 u = __shfl_up_sync(~0u, run_w, o);
+                        const uint32_t v = __shfl_up_sync(~0u, run_n, o);
+                        if (lane >= o) { run_w += u; run_n += v; }
+                    }
+                    if (lane == 31) { sh.scan_weight[warp] = run_w; sh.scan_count[warp] = run_n; }
+                    __syncthreads();
+                    u64 aw = c.above_weight;
+                    uint32_t an = c.above_count;
+                    for (int k = 0; k < warp; ++k) { aw += sh.scan_weight[k]; an += sh.scan_count[k]; }
+                    aw += run_w - sum_w;
+                    an += run_n - sum_n;
+                    if (!reached(an, aw) && reached(an + sum_n, aw + sum_w)) {
+                        int k = 0;
+                        while (k < kFine / kT - 1 && !reached(an + n[k], aw + w[k])) { an += n[k]; aw += w[k]; ++k; }
+                        sh.found_bin = tid * (kFine / kT) + k;
+                        sh.found_weight = aw;
+                        sh.found_count = an;
+                        sh.found_at = n[k];
+                    }
+                    __syncthreads();
+                    c.above_weight = sh.found_weight;
+                    c.above_count = sh.found_count;
+                    c.at_count = sh.found_at;
+                    c.hi -= sh.found_bin << shift;
+                    const uint32_t width = (1u << shift) - 1;
+                    c.lo = c.hi - c.lo > width ? c.hi - width : c.lo;
+                }
+                return c;
+            };
+            uint32_t cut = 0;
+            int ties = P.A, at_cut = P.A;
+            u64 kept = weighed;
+            if ((uint32_t)r.limit < counted) {
+                const Cut c = narrow(true, r.limit, 0.);
+                cut = c.lo;
+                ties = r.limit - (int)c.above_count;
+                at_cut = (int)c.at_count;
+                kept = c.above_weight + (u64)ties * weight_at(K::value(cut), m, r);
+            }
+            if (r.p < 1.f) {
+                const double enough = (double)r.p * (double)kept;
+                const Cut c = narrow(false, 0, enough);
+                const uint32_t w = weight_at(K::value(c.lo), m, r);
+                const int more = ties_until(enough, c.above_weight, w);
+                if (c.lo > cut || more < ties) ties = more;
+                cut = c.lo;
+                at_cut = (int)c.at_count;
+                kept = c.above_weight + (u64)ties * w;
+            }
+            int tie_end = P.A;
+            if (ties < at_cut) {                             // where in the row the kept ones of the cut's key end
+                auto tied = [&](float f, int) -> u64 { return K::of(f) == cut; };
+                u64 mine = 0, before;
+                row_.each([&](float f, int j) { mine += tied(f, j); });
+                row_.gather(mine, &before);
+                mine = warp_sum(mine);
+                const u64 last = (u64)ties - 1;
+                const int at = last >= before && last < before + mine ? row_.walk(before, last, tied) : -1;
+                tie_end = (int)row_.gather_max((u64)(uint32_t)(at + 1));
+            }
+            u64 mine = 0, before;
+            row_.each([&](float f, int j) {
+                const uint32_t k = K::of(f);
+                if (k > cut || (k == cut && j < tie_end)) mine += weight_at(f, m, r);
+            });
+            row_.gather(mine, &before);
+            finish(kept, all, before, warp_sum(mine), cut, tie_end);
         }
     }
+    row_.sync();                                             // no block ends while another may read its memory
 }
 
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -251,11 +783,35 @@ int sample_run(const SampleParams<T>& P, int64_t A, void* stream) {
         if (!aligned_to(p, 4)) return RLCS_ERR_ALIGN;
     if (!aligned_to(P.logits, sizeof(T))) return RLCS_ERR_ALIGN;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (A <= 1024) {
-        const int64_t blocks = (P.R + 7) / 8;
-        sample_rows_kernel<T, 32><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, s>>>(P);
+    const int64_t warps = (P.R + 7) / 8;
+    if (A <= kSmallA) {
+        const int64_t blocks = (P.R + kSmallRows - 1) / kSmallRows;
+        if (blocks > kMostBlocks) return RLCS_ERR_SIZE;
+        const uint32_t mul = A > 1 ? (uint32_t)(((uint64_t(1) << 32) + A - 1) / A) : 0;
+        sample_small_kernel<T><<<(unsigned)blocks, kSmallRows, kSmallRows * (A | 1) * sizeof(float), s>>>(P, mul);
+    } else if (A <= 1024) {
+        if (warps > kMostBlocks) return RLCS_ERR_SIZE;
+        if (A <= 256) sample_warp_kernel<T, 8><<<(unsigned)warps, 256, 0, s>>>(P);
+        else sample_warp_kernel<T, 32><<<(unsigned)warps, 256, 0, s>>>(P);
     } else {
-        sample_rows_kernel<T, 1024><<<(unsigned)(P.R < (1 << 20) ? P.R : (1 << 20)), 1024, 0, s>>>(P);
+        // blocks a row: until the GPU has four a multiprocessor, or a part would fall below 4096 actions
+        int ranks = 1;
+        while (ranks < kMaxCluster && P.R * ranks < 4 * rlcs_device::limits().sms && A / (2 * ranks) >= 4096) ranks *= 2;
+        if (P.R * ranks > kMostBlocks) return RLCS_ERR_SIZE;
+        if (cudaFuncSetAttribute(sample_cluster_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)) != cudaSuccess)
+            return RLCS_ERR_CUDA;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(P.R * ranks));
+        cfg.blockDim = dim3(kT);
+        cfg.dynamicSmemBytes = sizeof(Shared);
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = ranks;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaLaunchKernelEx(&cfg, sample_cluster_kernel<T>, P) != cudaSuccess) return RLCS_ERR_CUDA;
     }
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }
