@@ -189,12 +189,10 @@ _scratch: dict = {}
 
 def _scratch_of(like, nbytes: int, stream):
     """Uninitialised workspace of at least nbytes, one per (device, stream); replaced by a larger one when a call needs it."""
-    torch = _torch()
-    s = torch.cuda.current_stream(like.device) if stream is None else stream
-    key = (like.device, int(s.cuda_stream))
+    key = (like.device, _B._stream(stream))
     buf = _scratch.get(key)
     if buf is None or buf.numel() < nbytes:
-        buf = _B._alloc((max(nbytes, 1 << 20),), torch.uint8, like.device)
+        buf = _B._alloc((max(nbytes, 1 << 20),), _torch().uint8, like.device)
         if stream is not None:
             buf.record_stream(stream)
         _scratch[key] = buf
@@ -202,10 +200,10 @@ def _scratch_of(like, nbytes: int, stream):
 
 
 def _flat_rows(logits):
-    """[..., A] logits as [rows, A] (a view) and the leading shape."""
+    """[..., A] logits as [rows, A] (a view) and the leading shape, None where it is [rows, A] already."""
     if logits.dim() == 2:
         return logits, None
-    return logits.reshape(-1, logits.shape[-1]) if logits.is_contiguous() else logits.view(-1, logits.shape[-1]), logits.shape[:-1]
+    return logits.view(-1, logits.shape[-1]), logits.shape[:-1]
 
 
 def _by_dtype(logits, f32, bf16):
@@ -217,9 +215,9 @@ def sample_actions(logits, uniforms, *, temperature=None, top_k=None, top_p=None
     (actions int32, log_probs, kept_log_probs).  log_probs is under the whole softmax at that temperature (the behaviour policy of
     V-trace, Retrace and clipped losses), kept_log_probs under what top_k, min_p and top_p leave.  Parameters are numbers or
     tensors of one value a row; temperature 0 takes the most likely action; a row that allows none (all -inf) gets action -1."""
+    fn = _by_dtype(logits, _B.rlcs_sample_actions, _B.rlcs_sample_actions_bf16)
     rows, lead = _flat_rows(logits)
     flat = lambda v: v.reshape(-1) if lead is not None and hasattr(v, "reshape") else v
-    fn = _by_dtype(logits, _B.rlcs_sample_actions, _B.rlcs_sample_actions_bf16)
     got = fn(rows, flat(uniforms), temperature=flat(temperature), top_k=flat(top_k), top_p=flat(top_p), min_p=flat(min_p), stream=stream)
     return got if lead is None else tuple(v.view(lead) for v in got)
 
@@ -258,11 +256,7 @@ def shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, grou
     bounds give better launches."""
     scale = q.shape[-1] ** -0.5 if scale is None else scale
     if workspace is None:
-        page, groups = k_cache.shape[1], 0 if prefix_table is None else prefix_table.shape[0]
-        room = 0 if prefix_table is None else prefix_table.shape[1] * page, block_table.shape[1] * page
-        most = [r if m is None else min(int(m), r) for r, m in zip(room, (max_prefix_len, max_len))]
-        need = int(_B.lib().rlcs_prefix_attention_workspace_bytes(q.shape[0], q.shape[1], k_cache.shape[2], q.shape[2], page, groups, *most))
-        workspace = _scratch_of(q, need, stream)
+        workspace = lambda nbytes: _scratch_of(q, nbytes, stream)
     return _B.rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, block_table, lens, scale=scale,
                                          max_prefix_len=max_prefix_len, max_len=max_len, workspace=workspace, stream=stream)
 

@@ -242,10 +242,18 @@ def _alloc(shape, dtype, device):
     return _torch().empty(shape, dtype=dtype, device=device)
 
 
+_raw_stream = None
+
+
 def _stream(stream=None):
-    torch = _torch()
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    """Raw handle of the given stream, or of the current one (asked for without building a Stream object where torch allows)."""
+    global _raw_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        torch = _torch()
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream().cuda_stream)
+    return _raw_stream(_current_device())
 
 
 class Workspace:
@@ -736,37 +744,59 @@ def rlcs_episodic_prefix_sum_time_major(x, dones, *, starts_at=False, sums=None,
 
 # ------------------------------------------------------------------ rollout and policy operators
 _KINDS = {"f32": "float32", "bf16": "bfloat16", "i32": "int32", "i64": "int64"}
+_dtypes: dict = {}
 
 
-def _typed(t, kind: str, shape=None, what="tensor"):
-    """Pointer of a contiguous tensor of one of _KINDS (None -> NULL)."""
-    if t is None:
-        return None
-    torch = _torch()
+def _dtype(kind: str):
+    dt = _dtypes.get(kind)
+    if dt is None:
+        dt = _dtypes[kind] = getattr(_torch(), _KINDS[kind])
+    return dt
+
+
+def _device_for(t) -> int:
+    """The current device, once the call's first tensor is known to be a CUDA tensor."""
+    if not t.is_cuda:
+        raise TypeError("rlcs takes CUDA tensors (device pointers); there is no CPU path")
+    return _current_device()
+
+
+def _refuse(t, kind, shape, what):
+    """Says why _typed() or _rows() does not take a tensor."""
     if not t.is_cuda:
         raise TypeError("rlcs takes CUDA tensors (device pointers); there is no CPU path")
     _require_current_device(t, what)
-    if t.dtype != getattr(torch, _KINDS[kind]):
+    if t.dtype != _dtype(kind):
         raise TypeError(f"expected {_KINDS[kind]} for {what}, got {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"expected shape {tuple(shape)} for {what}, got {tuple(t.shape)}")
+    raise ValueError(f"{what} must be contiguous")
+
+
+def _typed(t, kind: str, shape, what: str, device: int):
+    """Pointer of a contiguous tensor of one of _KINDS on the current device (None -> NULL)."""
+    if t is None:
+        return None
+    if not (t.dtype == _dtype(kind) and t.is_cuda and t.get_device() == device and t.is_contiguous()
+            and (shape is None or t.shape == shape)):
+        _refuse(t, kind, shape, what)
     return t.data_ptr()
 
 
-def _rows(t, kind: str, what: str, shape=None):
+def _output(t, kind: str, shape, what: str, where, device: int):
+    """(tensor, pointer) of an output: the caller's, checked, or a new one."""
+    if t is None:
+        t = _alloc(shape, _dtype(kind), where)
+        return t, t.data_ptr()
+    return t, _typed(t, kind, shape, what, device)
+
+
+def _rows(t, kind: str, what: str, device: int, shape=None):
     """(pointer, row stride) of a 2-D tensor whose rows are contiguous and do not overlap."""
-    torch = _torch()
-    if not t.is_cuda:
-        raise TypeError("rlcs takes CUDA tensors (device pointers); there is no CPU path")
-    _require_current_device(t, what)
-    if t.dtype != getattr(torch, _KINDS[kind]):
-        raise TypeError(f"expected {_KINDS[kind]} for {what}, got {t.dtype}")
+    if not (t.dtype == _dtype(kind) and t.is_cuda and t.get_device() == device and (shape is None or t.shape == shape)):
+        _refuse(t, kind, shape, what)
     if t.dim() != 2:
         raise ValueError(f"{what} must be 2-D [rows, actions]")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"expected shape {tuple(shape)} for {what}, got {tuple(t.shape)}")
     R, A = t.shape
     ld = t.stride(0) if R > 1 else max(A, 1)
     if (A > 1 and t.stride(1) != 1) or ld < A:
@@ -774,29 +804,30 @@ def _rows(t, kind: str, what: str, shape=None):
     return t.data_ptr(), ld
 
 
-def _per_row(value, kind: str, R: int, default, what: str):
+def _per_row(value, kind: str, shape, default, what: str, device: int):
     """A per-row parameter: (pointer, unused) for an [R] tensor, (NULL, value) for a number or None."""
     if value is None:
         return None, default
     if isinstance(value, (int, float)):
         return None, value
-    return _typed(value, kind, (R,), what), default
+    return _typed(value, kind, shape, what, device), default
 
 
 def _sample_actions(name, kind, logits, uniforms, temperature, top_k, top_p, min_p, actions, log_probs, kept_log_probs, stream):
-    torch = _torch()
-    ptr, ld = _rows(logits, kind, "logits")
+    dev = _device_for(logits)
+    ptr, ld = _rows(logits, kind, "logits", dev)
     R, A = logits.shape
-    t, t_all = _per_row(temperature, "f32", R, 1.0, "temperature")
-    k, k_all = _per_row(top_k, "i32", R, 0, "top_k")
-    p, p_all = _per_row(top_p, "f32", R, 1.0, "top_p")
-    m, m_all = _per_row(min_p, "f32", R, 0.0, "min_p")
-    a = _alloc((R,), torch.int32, logits.device) if actions is None else actions
-    lp = _alloc((R,), torch.float32, logits.device) if log_probs is None else log_probs
-    kp = _alloc((R,), torch.float32, logits.device) if kept_log_probs is None else kept_log_probs
-    _check(getattr(lib(), name)(ptr, ld, _typed(uniforms, "f32", (R,), "uniforms"), t, k, p, m, t_all, min(int(k_all), 2 ** 31 - 1),
-                                p_all, m_all, _typed(a, "i32", (R,), "actions"), _typed(lp, "f32", (R,), "log_probs"),
-                                _typed(kp, "f32", (R,), "kept_log_probs"), R, A, _stream(stream)))
+    n = (R,)
+    t, t_all = _per_row(temperature, "f32", n, 1.0, "temperature", dev)
+    k, k_all = _per_row(top_k, "i32", n, 0, "top_k", dev)
+    p, p_all = _per_row(top_p, "f32", n, 1.0, "top_p", dev)
+    m, m_all = _per_row(min_p, "f32", n, 0.0, "min_p", dev)
+    where = logits.device
+    a, ap = _output(actions, "i32", n, "actions", where, dev)
+    lp, lpp = _output(log_probs, "f32", n, "log_probs", where, dev)
+    kp, kpp = _output(kept_log_probs, "f32", n, "kept_log_probs", where, dev)
+    _check(getattr(lib(), name)(ptr, ld, _typed(uniforms, "f32", n, "uniforms", dev), t, k, p, m, t_all, min(int(k_all), 2 ** 31 - 1),
+                                p_all, m_all, ap, lpp, kpp, R, A, _stream(stream)))
     return a, lp, kp
 
 
@@ -817,25 +848,26 @@ def rlcs_sample_actions_bf16(logits, uniforms, *, temperature=None, top_k=None, 
 
 def _policy_grad(name, kind, logits, actions, advantages, old_log_probs, mask, temperature, clip, entropy_coef, scale, want_grad,
                  loss, log_probs, entropy, dlogits, stream):
-    torch = _torch()
-    ptr, ld = _rows(logits, kind, "logits")
+    dev = _device_for(logits)
+    ptr, ld = _rows(logits, kind, "logits", dev)
     R, A = logits.shape
-    lp = _alloc((R,), torch.float32, logits.device) if log_probs is None else log_probs
-    ent = _alloc((R,), torch.float32, logits.device) if entropy is None else entropy
-    dptr, ldd = None, 0
+    n, where = (R,), logits.device
+    lp, lpp = _output(log_probs, "f32", n, "log_probs", where, dev)
+    ent, entp = _output(entropy, "f32", n, "entropy", where, dev)
+    dptr, ldd, lossp = None, 0, None
     if advantages is None:
         if old_log_probs is not None or loss is not None or dlogits is not None:
             raise ValueError("old_log_probs, loss and dlogits go with advantages")
     else:
-        loss = _alloc((R,), torch.float32, logits.device) if loss is None else loss
-        if dlogits is None and want_grad:
-            dlogits = _alloc((R, A), logits.dtype, logits.device)
+        loss, lossp = _output(loss, "f32", n, "loss", where, dev)
         if dlogits is not None:
-            dptr, ldd = _rows(dlogits, kind, "dlogits", (R, A))
-    _check(getattr(lib(), name)(ptr, ld, _typed(actions, "i32", (R,), "actions"), _ptr(mask, "u8", (R,)),
-                                _typed(advantages, "f32", (R,), "advantages"), _typed(old_log_probs, "f32", (R,), "old_log_probs"),
-                                _typed(loss, "f32", (R,), "loss"), _typed(lp, "f32", (R,), "log_probs"),
-                                _typed(ent, "f32", (R,), "entropy"), dptr, ldd, R, A, temperature, clip, entropy_coef, scale,
+            dptr, ldd = _rows(dlogits, kind, "dlogits", dev, (R, A))
+        elif want_grad:
+            dlogits = _alloc((R, A), logits.dtype, where)
+            dptr, ldd = dlogits.data_ptr(), A
+    _check(getattr(lib(), name)(ptr, ld, _typed(actions, "i32", n, "actions", dev), _ptr(mask, "u8", n),
+                                _typed(advantages, "f32", n, "advantages", dev), _typed(old_log_probs, "f32", n, "old_log_probs", dev),
+                                lossp, lpp, entp, dptr, ldd, R, A, temperature, clip, entropy_coef, scale,
                                 _stream(stream)))
     if advantages is None:
         return lp, ent
@@ -863,44 +895,46 @@ def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, g
     """One query a row over its group's paged prefix and its own pages.  q [B, H, d] (rows may be strided), caches
     [pages, page, Hk, d] (any strides with contiguous d), tables and lengths int32; prefix_table, prefix_lens and group_offsets
     None: no prefixes.  Returns (out, lse), or out without lse."""
-    torch = _torch()
-    if q.dim() != 3 or k_cache.dim() != 4 or tuple(v_cache.shape) != tuple(k_cache.shape):
+    if q.dim() != 3 or k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
         raise ValueError("expected q [B, H, d] and caches [pages, page, Hk, d] of one shape")
+    dev = _device_for(q)
     for t, what in ((q, "q"), (k_cache, "k_cache"), (v_cache, "v_cache")):
-        if not t.is_cuda:
-            raise TypeError("rlcs takes CUDA tensors (device pointers); there is no CPU path")
-        _require_current_device(t, what)
-        if t.dtype != torch.bfloat16:
-            raise TypeError(f"expected bfloat16 for {what}, got {t.dtype}")
+        if not (t.dtype == _dtype("bf16") and t.is_cuda and t.get_device() == dev):
+            _refuse(t, "bf16", None, what)
     B, H, d = q.shape
-    pages, page, Hk = k_cache.shape[:3]
-    if k_cache.shape[3] != d or q.stride(2) != 1 or (H > 1 and q.stride(1) != d) or k_cache.stride(3) != 1:
+    pages, page, Hk, dk = k_cache.shape
+    sq, sk = q.stride(), k_cache.stride()
+    if dk != d or (d > 1 and sq[2] != 1) or (H > 1 and sq[1] != d) or sk[3] != 1:
         raise ValueError("q and the caches must agree in d, with heads of q and d of both contiguous")
-    if k_cache.stride() != v_cache.stride():
+    if sk != v_cache.stride():
         raise ValueError("k_cache and v_cache must have the same strides")
     if (prefix_table is None) != (prefix_lens is None) or (prefix_table is None) != (group_offsets is None):
         raise ValueError("prefix_table, prefix_lens and group_offsets go together")
-    groups = 0 if prefix_table is None else prefix_table.shape[0]
-    widths = 0 if prefix_table is None else prefix_table.shape[1], block_table.shape[1]
-    mp = widths[0] * page if max_prefix_len is None else min(int(max_prefix_len), widths[0] * page)
-    ml = widths[1] * page if max_len is None else min(int(max_len), widths[1] * page)
-    if out is None:
-        out = _alloc((B, H, d), torch.bfloat16, q.device)
-    if lse is None and want_lse:
-        lse = _alloc((B, H), torch.float32, q.device)
-    need = int(lib().rlcs_prefix_attention_workspace_bytes(B, H, Hk, d, page, groups, mp, ml))
-    if workspace is None:
-        workspace = _alloc((max(need, 16),), torch.uint8, q.device)
-        if stream is not None:
-            workspace.record_stream(stream)
-    _require_current_device(workspace, "workspace")
-    sp, st, sh = k_cache.stride()[:3]
+    groups, prefix_width = (0, 0) if prefix_table is None else prefix_table.shape
+    own_width = block_table.shape[1]
+    mp = prefix_width * page if max_prefix_len is None else min(int(max_prefix_len), prefix_width * page)
+    ml = own_width * page if max_len is None else min(int(max_len), own_width * page)
+    out, outp = _output(out, "bf16", (B, H, d), "out", q.device, dev)
+    lsep = None
+    if lse is not None or want_lse:
+        lse, lsep = _output(lse, "f32", (B, H), "lse", q.device, dev)
+    if workspace is None or callable(workspace):
+        need = lib().rlcs_prefix_attention_workspace_bytes(B, H, Hk, d, page, groups, mp, ml)
+        if workspace is not None:
+            workspace = workspace(need)
+        else:
+            workspace = _alloc((max(need, 16),), _torch().uint8, q.device)
+            if stream is not None:
+                workspace.record_stream(stream)
+    if workspace.get_device() != dev:
+        _require_current_device(workspace, "workspace")
     _check(lib().rlcs_prefix_attention_bf16(
-        q.data_ptr(), q.stride(0) if B > 1 else H * d, k_cache.data_ptr(), v_cache.data_ptr(), pages, sp, st, sh,
-        _typed(prefix_table, "i32", (groups, widths[0]), "prefix_table"), widths[0], _typed(prefix_lens, "i32", (groups,), "prefix_lens"),
-        _typed(group_offsets, "i32", (groups + 1,), "group_offsets"), _typed(block_table, "i32", (B, widths[1]), "block_table"),
-        widths[1], _typed(lens, "i32", (B,), "lens"), _typed(out, "bf16", (B, H, d), "out"), _typed(lse, "f32", (B, H), "lse"),
-        B, H, Hk, d, page, groups, mp, ml, scale, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+        q.data_ptr(), sq[0] if B > 1 else H * d, k_cache.data_ptr(), v_cache.data_ptr(), pages, sk[0], sk[1], sk[2],
+        _typed(prefix_table, "i32", (groups, prefix_width), "prefix_table", dev), prefix_width,
+        _typed(prefix_lens, "i32", (groups,), "prefix_lens", dev), _typed(group_offsets, "i32", (groups + 1,), "group_offsets", dev),
+        _typed(block_table, "i32", (B, own_width), "block_table", dev), own_width, _typed(lens, "i32", (B,), "lens", dev),
+        outp, lsep, B, H, Hk, d, page, groups, mp, ml, scale,
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
     return out if lse is None else (out, lse)
 
 
@@ -908,18 +942,16 @@ def rlcs_block_tables(cached, added, free_pages, block_table, *, page_size, num_
                       page_offsets=None, stream=None):
     """One step's page tables (block_table [B, width], in place), slot map and positions from int32 lengths on the GPU.  Returns
     (slots int64 [num_slots], positions int32 [num_slots], offsets int32 [B + 1], page_offsets int32 [B + 1])."""
-    torch = _torch()
     if cached.dim() != 1 or free_pages.dim() != 1 or block_table.dim() != 2:
         raise ValueError("expected cached [B], free_pages [F], block_table [B, width]")
     B, width = block_table.shape
-    dev = cached.device
-    slots = _alloc((num_slots,), torch.int64, dev) if slots is None else slots
-    positions = _alloc((num_slots,), torch.int32, dev) if positions is None else positions
-    offsets = _alloc((B + 1,), torch.int32, dev) if offsets is None else offsets
-    page_offsets = _alloc((B + 1,), torch.int32, dev) if page_offsets is None else page_offsets
+    where, dev = cached.device, _device_for(cached)
+    slots, sp = _output(slots, "i64", (num_slots,), "slots", where, dev)
+    positions, pp = _output(positions, "i32", (num_slots,), "positions", where, dev)
+    offsets, op = _output(offsets, "i32", (B + 1,), "offsets", where, dev)
+    page_offsets, gp = _output(page_offsets, "i32", (B + 1,), "page_offsets", where, dev)
     _check(lib().rlcs_block_tables(
-        _typed(cached, "i32", (B,), "cached"), _typed(added, "i32", (B,), "added"), _typed(free_pages, "i32", None, "free_pages"),
-        _typed(block_table, "i32", None, "block_table"), _typed(slots, "i64", (num_slots,), "slots"),
-        _typed(positions, "i32", (num_slots,), "positions"), _typed(offsets, "i32", (B + 1,), "offsets"),
-        _typed(page_offsets, "i32", (B + 1,), "page_offsets"), B, width, free_pages.numel(), num_slots, page_size, _stream(stream)))
+        _typed(cached, "i32", (B,), "cached", dev), _typed(added, "i32", (B,), "added", dev),
+        _typed(free_pages, "i32", None, "free_pages", dev), _typed(block_table, "i32", None, "block_table", dev),
+        sp, pp, op, gp, B, width, free_pages.shape[0], num_slots, page_size, _stream(stream)))
     return slots, positions, offsets, page_offsets

@@ -35,7 +35,8 @@ struct AttnParams {
     int max_prefix, max_len;
     int prefix_seg, own_seg;       // keys a segment
     int prefix_segs, own_segs;     // segments a row
-    int prefix_tiles, own_tiles;   // tiles of 64 rows over all groups; tiles of 16 rows a trajectory
+    int prefix_rows;               // rows of a prefix tile: 128 (tensor memory) or 16
+    int prefix_tiles, own_tiles;   // slots of prefix tiles over all groups; tiles of 16 rows a trajectory
     int prefix_blocks;             // thread blocks of the prefix part
     float scale_log2;
 };
@@ -85,25 +86,30 @@ template <int D> __device__ __forceinline__ uint32_t piece(int row, int c) { ret
 // Page (from the segment's first) of place `in` of that page's and the following tokens; in and page below 2^16.
 __device__ __forceinline__ int page_of(const AttnParams& P, int in) { return P.page_mul != 0 ? (int)__umulhi((uint32_t)in, P.page_mul) : in; }
 
-// One segment of keys against 16 rows a warp.  KEYS_SPLIT: the block's four warps share the 16 rows and take 16 of each
-// tile's 64 keys each; otherwise every warp has 16 rows of its own and all of the keys.
-template <int D, bool KEYS_SPLIT>
-__device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* ids, const int32_t* table, int table_width, int begin,
-                                        int end, int kv_head, int first_row, int rows, int b0, int slot) {
-    constexpr int kPieces = D / 8, kTileBytes = kTile * D * 2, kSteps = D / 16;
-    constexpr int kCols = KEYS_SPLIT ? 2 : 8;                 // 8-key columns a warp computes
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+__device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-    // page numbers of the segment; a page that is not there masks its keys
-    const int first_page = begin / P.page, offset = begin - first_page * P.page;
-    const int n_ids = (end - 1) / P.page - first_page + 1;
+// Page numbers of the keys [begin, end); a page that is not there (-1) masks its keys.  Returns whether there is one.
+__device__ __forceinline__ int read_ids(const AttnParams& P, int* ids, const int32_t* table, int width, int begin, int end, int tid, int threads) {
+    const int first = begin / P.page, n = (end - 1) / P.page - first + 1;
     int missing = 0;
-    for (int i = tid; i < n_ids; i += kThreads) {
-        int id = first_page + i < table_width ? table[first_page + i] : -1;
+    for (int i = tid; i < n; i += threads) {
+        int id = first + i < width ? table[first + i] : -1;
         if (id < 0 || id >= P.pages) { id = -1; missing = 1; }
         ids[i] = id;
     }
-    missing = __syncthreads_or(missing);
+    return __syncthreads_or(missing);
+}
+
+// One segment of keys against 16 rows: the block's four warps share the rows and take 16 of each tile's 64 keys each.
+template <int D>
+__device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* ids, const int32_t* table, int table_width, int begin,
+                                        int end, int kv_head, int first_row, int rows, int b0, int slot) {
+    constexpr int kPieces = D / 8, kTileBytes = kTile * D * 2, kSteps = D / 16;
+    constexpr int kCols = 2;                                  // 8-key columns a warp computes
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    const int offset = begin % P.page;
+    const int missing = read_ids(P, ids, table, table_width, begin, end, tid, kThreads);
 
     auto load = [&](int base, char* k_at, char* v_at) {       // keys [base, base + 64) of the segment, zeros where there are none
 #pragma unroll 4
@@ -127,21 +133,18 @@ __device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* id
 
     // queries as the left operand: rows lane / 4 and lane / 4 + 8 of the warp's 16
     uint32_t qf[kSteps][4];
-    int64_t out_row[2];
-    bool row_in[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int row = first_row + (KEYS_SPLIT ? 0 : warp * 16) + (lane >> 2) + h * 8;
-        row_in[h] = row < rows;
+        const int row = first_row + (lane >> 2) + h * 8;
+        const bool in = row < rows;
         const int b = b0 + row / P.r, head = kv_head * P.r + row % P.r;
-        out_row[h] = (int64_t)b * P.H + head;
-        const __nv_bfloat16* src = P.q + (row_in[h] ? (int64_t)b * P.q_stride + (int64_t)head * P.d : 0);
+        const __nv_bfloat16* src = P.q + (in ? (int64_t)b * P.q_stride + (int64_t)head * P.d : 0);
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int col = s * 16 + e * 8 + (lane & 3) * 2;
-                qf[s][e * 2 + h] = row_in[h] && col < P.d ? *reinterpret_cast<const uint32_t*>(src + col) : 0u;
+                qf[s][e * 2 + h] = in && col < P.d ? *reinterpret_cast<const uint32_t*>(src + col) : 0u;
             }
     }
     float o[D / 8][4] = {};
@@ -159,7 +162,7 @@ __device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* id
             asm volatile("cp.async.wait_group 0;");
         }
         __syncthreads();
-        const int key0 = KEYS_SPLIT ? warp * 16 : 0;
+        const int key0 = warp * 16;
         float s[kCols][4] = {};
 #pragma unroll
         for (int j = 0; j < kCols; j += 2) {
@@ -236,17 +239,7 @@ __device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* id
         l[h] += __shfl_xor_sync(~0u, l[h], 2);
     }
     const int64_t seg_rows = (int64_t)slot * P.B * P.H;
-    if constexpr (!KEYS_SPLIT) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (!row_in[h]) continue;
-            float* dst = P.part_o + (seg_rows + out_row[h]) * D;
-#pragma unroll
-            for (int n = 0; n < D / 8; ++n)
-                *reinterpret_cast<float2*>(dst + n * 8 + (lane & 3) * 2) = make_float2(o[n][h * 2], o[n][h * 2 + 1]);
-            if ((lane & 3) == 0) P.part_ml[seg_rows + out_row[h]] = make_float2(m[h], l[h]);
-        }
-    } else {
+    {
         // the four warps' shares, joined through shared memory (the tiles are done with)
         float* so = reinterpret_cast<float*>(smem);           // [4][16][D]
         float2* sml = reinterpret_cast<float2*>(smem + 4 * 16 * D * 4);
@@ -281,31 +274,45 @@ __device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* id
     }
 }
 
-__device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+// Which rows and keys a block of the prefix part has.
+struct PrefixTile {
+    int group, kv_head, seg, first_row, rows, b0, begin, end;      // rows from first_row of the group's `rows`
+};
 
+__device__ __forceinline__ bool prefix_tile(const AttnParams& P, int block, PrefixTile* t) {
+    const int slot = block % P.prefix_tiles;
+    block /= P.prefix_tiles;
+    t->kv_head = block % P.Hk;
+    t->seg = block / P.Hk;
+    // group g's tiles start at slot floor(offset_g r / tile rows) + g: at least as many slots as tiles for any sizes
+    int lo = 0, hi = P.groups - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((int64_t)clamp_to(P.group_offsets[mid], 0, P.B) * P.r / P.prefix_rows + mid <= slot) lo = mid; else hi = mid - 1;
+    }
+    t->group = lo;
+    t->b0 = clamp_to(P.group_offsets[lo], 0, P.B);
+    t->rows = (clamp_to(P.group_offsets[lo + 1], t->b0, P.B) - t->b0) * P.r;
+    t->first_row = (slot - (int)((int64_t)t->b0 * P.r / P.prefix_rows + lo)) * P.prefix_rows;
+    const int len = clamp_to(P.prefix_lens[lo], 0, P.max_prefix);
+    t->begin = t->seg * P.prefix_seg;
+    t->end = min(len, t->begin + P.prefix_seg);
+    return t->first_row >= 0 && t->first_row < t->rows && t->begin < t->end;
+}
+
+// Tiles of 16 rows: a trajectory's own keys, and prefixes of groups with few rows (blocks below `prefix_blocks`).
 template <int D>
-__global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_constant__ AttnParams P) {
+__global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_constant__ AttnParams P, int prefix_blocks) {
     extern __shared__ __align__(128) char smem[];
     __shared__ int ids[kMaxIds];
     int block = blockIdx.x;
-    if (block < P.prefix_blocks) {
-        const int tile_slot = block % P.prefix_tiles;
-        block /= P.prefix_tiles;
-        const int kv_head = block % P.Hk, seg = block / P.Hk;
-        // group g's tiles start at slot floor(offset_g r / 64) + g: at least as many slots as tiles for any sizes
-        int lo = 0, hi = P.groups - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if ((int64_t)clamp_to(P.group_offsets[mid], 0, P.B) * P.r / 64 + mid <= tile_slot) lo = mid; else hi = mid - 1;
-        }
-        const int b0 = clamp_to(P.group_offsets[lo], 0, P.B), b1 = clamp_to(P.group_offsets[lo + 1], b0, P.B);
-        const int tile = tile_slot - (int)((int64_t)b0 * P.r / 64 + lo), rows = (b1 - b0) * P.r;
-        const int len = clamp_to(P.prefix_lens[lo], 0, P.max_prefix), begin = seg * P.prefix_seg, end = min(len, begin + P.prefix_seg);
-        if (tile < 0 || tile * 64 >= rows || begin >= end) return;
-        segment<D, false>(P, smem, ids, P.prefix_table + (int64_t)lo * P.prefix_width, P.prefix_width, begin, end, kv_head, tile * 64,
-                          rows, b0, seg);
+    if (block < prefix_blocks) {
+        PrefixTile t;
+        if (!prefix_tile(P, block, &t)) return;
+        segment<D>(P, smem, ids, P.prefix_table + (int64_t)t.group * P.prefix_width, P.prefix_width, t.begin, t.end, t.kv_head, t.first_row,
+                   t.rows, t.b0, t.seg);
     } else {
-        block -= P.prefix_blocks;
+        block -= prefix_blocks;
         const int tile = block % P.own_tiles;
         block /= P.own_tiles;
         const int kv_head = block % P.Hk;
@@ -313,8 +320,291 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_consta
         const int b = block % P.B, seg = block / P.B;
         const int len = clamp_to(P.lens[b], 0, P.max_len), begin = seg * P.own_seg, end = min(len, begin + P.own_seg);
         if (begin >= end) return;
-        segment<D, true>(P, smem, ids, P.block_table + (int64_t)b * P.own_width, P.own_width, begin, end, kv_head, tile * 16, P.r, b,
-                         P.prefix_segs + seg);
+        segment<D>(P, smem, ids, P.block_table + (int64_t)b * P.own_width, P.own_width, begin, end, kv_head, tile * 16, P.r, b,
+                   P.prefix_segs + seg);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- prefixes of many rows
+// 128 rows a block on tcgen05: scores S = Q K^T of 64 keys at a time into one of two 64-column buffers of tensor memory, the
+// weights back over them as two bfloat16 parts (32 columns each), O += P V accumulated in tensor memory.  Warps 0-3: one
+// row a thread (maximum, exponentials, sums).  Warps 4-6 copy keys and values through the page table into a ring of slots
+// in the layout that the matrix instructions read (128-byte rows, pieces exchanged by row).  Warp 7: one thread issues.
+// Two blocks share a multiprocessor, so that one's exponentials run under the other's products.
+constexpr int kPrefixThreads = 256, kLoaders = 96;       // warps 4-6 load, warp 7 issues
+
+template <int D> struct PrefixShape {
+    static constexpr int kSlot = kTile * D * 2, kSlots = D == 128 ? 4 : 8, kQ = 128 * D * 2;
+    static constexpr int kBytes = kQ + kSlots * kSlot + 1024;      // + alignment
+};
+
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// Bounded: a wait that runs out of polls, or sees that another did, gives up, and the block's rows come out NaN.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int* gave_up) {
+    for (int polls = 0; polls < (1 << 20); ++polls) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+        if ((polls & 63) == 63 && *gave_up) return false;
+    }
+    *gave_up = 1;
+    return false;
+}
+
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// 128-byte rows with exchanged pieces; `lead`: bytes between blocks of 64 along the contiguous dimension (not used where
+// that is the summed one), 1024 bytes between groups of eight rows.
+__device__ __forceinline__ uint64_t describe(uint32_t at, uint32_t lead) {
+    return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, int add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"(add) : "memory");
+}
+
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, int add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"(add) : "memory");
+}
+
+__device__ __forceinline__ void tmem_load32(uint32_t* r, uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+                 "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]) : "r"(at) : "memory");
+}
+
+__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+                 "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+                 "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+                 "r"(r[30]), "r"(r[31]) : "memory");
+}
+
+__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <int D>
+__global__ void __launch_bounds__(kPrefixThreads, 2) prefix_kernel(const __grid_constant__ AttnParams P) {
+    typedef PrefixShape<D> Shape;
+    constexpr int kSlots = Shape::kSlots, kPieces = D / 8, kColumns = 256;
+    constexpr uint32_t kScores = 1u << 4 | 1u << 7 | 1u << 10 | (kTile >> 3) << 17 | (128 >> 4) << 24;
+    constexpr uint32_t kValues = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 16 | (D >> 3) << 17 | (128 >> 4) << 24;      // V: keys by rows
+    extern __shared__ char raw[];
+    __shared__ int ids[kMaxIds];
+    __shared__ __align__(8) uint64_t bars[2 * kSlots + 6];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    PrefixTile t;
+    if (!prefix_tile(P, blockIdx.x, &t)) return;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t q_at = (smem_at(raw) + 1023) & ~1023u, ring = q_at + Shape::kQ;
+    const uint32_t full = smem_at(bars), empty = full + 8 * kSlots, s_full = empty + 8 * kSlots, p_full = s_full + 16, o_done = p_full + 16,
+                   drained = o_done + 8;
+    if (warp == 7) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_at)), "n"(kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (tid == 0) {
+        gave_up = 0;
+        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, kLoaders); bar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(p_full + 8 * i, 128); }
+        bar_init(o_done, 1);
+        bar_init(drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    // queries, zeros where there are none
+    for (int i = tid; i < 128 * kPieces; i += kPrefixThreads) {
+        const int row = i / kPieces, c = i % kPieces, at = t.first_row + row;
+        uint4 v = {0, 0, 0, 0};
+        if (at < t.rows && c * 8 < P.d)
+            v = *reinterpret_cast<const uint4*>(P.q + (int64_t)(t.b0 + at / P.r) * P.q_stride + (int64_t)(t.kv_head * P.r + at % P.r) * P.d + c * 8);
+        const uint32_t dst = q_at + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    }
+    fence_async();
+    fence_before();
+    const int missing = read_ids(P, ids, P.prefix_table + (int64_t)t.group * P.prefix_width, P.prefix_width, t.begin, t.end, tid, kPrefixThreads);
+    fence_after();
+    const uint32_t tmem = tmem_at, o_at = tmem + 128;
+    const int offset = t.begin % P.page, tiles = (t.end - t.begin + kTile - 1) / kTile;
+
+    if (warp < 4) {
+        const uint32_t mine = (uint32_t)(warp * 32) << 16;
+        const bool any_row = t.first_row + warp * 32 < t.rows;
+        float m = -INFINITY, l = 0.f;
+        bool fine = true;
+        for (int i = 0; i < tiles; ++i) {
+            const uint32_t at = tmem + mine + (i & 1) * kTile;
+            fine = __all_sync(~0u, bar_wait(s_full + 8 * (i & 1), (i >> 1) & 1, &gave_up));
+            if (!fine) break;
+            fence_after();
+            if (any_row) {
+                uint32_t s[kTile];
+                tmem_load32(s, at);
+                tmem_load32(s + 32, at + 32);
+                tmem_wait_load();
+                const int left = t.end - t.begin - i * kTile;
+                if (left < kTile || missing) {
+#pragma unroll
+                    for (int k = 0; k < kTile; ++k) {
+                        const bool there = k < left && (!missing || ids[page_of(P, offset + i * kTile + k)] >= 0);
+                        if (!there) s[k] = __float_as_uint(-INFINITY);
+                    }
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < kTile; ++k) top[k & 3] = fmaxf(top[k & 3], __uint_as_float(s[k]));
+                const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * P.scale_log2;
+                // the base follows the maximum only when it is 2^8 behind: the weights stay below 2^8, and O is seldom rescaled
+                if (__any_sync(~0u, now > m + 8.f)) {
+                    const float next = fmaxf(m, now), fade = m == -INFINITY ? 0.f : exp2_of(m - next);
+                    if (i > 0) {
+                        fine = __all_sync(~0u, bar_wait(o_done, (i - 1) & 1, &gave_up));
+                        if (!fine) break;
+                        fence_after();
+#pragma unroll
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t o[32];
+                            tmem_load32(o, o_at + mine + c);
+                            tmem_wait_load();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fade);
+                            tmem_store32(o_at + mine + c, o);
+                        }
+                    }
+                    l *= fade;
+                    m = next;
+                }
+                const float base = m == -INFINITY ? 0.f : m;
+                float sum[2] = {0.f, 0.f};
+                uint32_t lo[kTile / 2];
+#pragma unroll
+                for (int k = 0; k < kTile; k += 2) {
+                    const float a = exp2_of(fmaf(__uint_as_float(s[k]), P.scale_log2, -base));
+                    const float b = exp2_of(fmaf(__uint_as_float(s[k + 1]), P.scale_log2, -base));
+                    sum[0] += a;
+                    sum[1] += b;
+                    const uint32_t hi = pack2(a, b);
+                    lo[k / 2] = pack2(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+                    s[k / 2] = hi;
+                }
+                l += sum[0] + sum[1];
+                tmem_store32(at, s);
+                tmem_store32(at + 32, lo);
+                tmem_wait_store();
+            }
+            fence_before();
+            bar_arrive(p_full + 8 * (i & 1));
+        }
+        if (fine) fine = __all_sync(~0u, bar_wait(o_done, (tiles - 1) & 1, &gave_up));
+        fence_after();
+        const int at = t.first_row + warp * 32 + lane;
+        const int64_t dst = (int64_t)t.seg * P.B * P.H + (int64_t)(t.b0 + at / P.r) * P.H + t.kv_head * P.r + at % P.r;
+        if (any_row) {
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tmem_load32(o, o_at + mine + c);
+                tmem_wait_load();
+                if (at < t.rows)
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        *reinterpret_cast<uint4*>(P.part_o + dst * D + c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+            }
+            if (at < t.rows) P.part_ml[dst] = fine ? make_float2(m, l) : make_float2(0.f, __int_as_float(0x7fffffff));
+        }
+        fence_before();
+    } else if (warp < 7) {
+        const int me = tid - 128, c = me % kPieces, row0 = me / kPieces;
+        constexpr int kStep = kLoaders / kPieces, kAhead = kSlots - 2;      // slots being filled
+        const int items = 2 * tiles;
+        for (int i = 0; i < items + kAhead; ++i) {
+            if (i < items) {
+                const int slot = i % kSlots, round = i / kSlots, base = (i >> 1) * kTile;
+                if (round > 0 && !bar_wait(empty + 8 * slot, (round - 1) & 1, &gave_up)) break;
+                const __nv_bfloat16* from = (i & 1 ? P.v : P.k) + t.kv_head * P.head_stride + c * 8;
+                const uint32_t dst = ring + slot * Shape::kSlot + (c >> 3) * (kTile * 128);
+#pragma unroll 8
+                for (int row = row0; row < kTile; row += kStep) {
+                    const int local = base + row;
+                    bool there = t.begin + local < t.end && c * 8 < P.d;
+                    int64_t at = 0;
+                    if (there) {
+                        const int in = offset + local, pg = page_of(P, in), id = ids[pg];
+                        there = id >= 0;
+                        if (there) at = id * P.page_stride + (in - pg * P.page) * P.token_stride;
+                    }
+                    copy16(dst + row * 128 + (((c & 7) ^ (row & 7)) << 4), there ? from + at : P.k, there);
+                }
+            }
+            asm volatile("cp.async.commit_group;");
+            if (i >= kAhead) {                                    // the copies of kAhead items ago are complete
+                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+                fence_async();
+                bar_arrive(full + 8 * ((i - kAhead) % kSlots));
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (lane == 0) {
+        auto scores = [&](int i) {
+            const int item = 2 * i, slot = item % kSlots;
+            if (!bar_wait(full + 8 * slot, (item / kSlots) & 1, &gave_up)) return false;
+            fence_after();
+            const uint32_t k_at = ring + slot * Shape::kSlot;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s)
+                mma_ss(tmem + (i & 1) * kTile, describe(q_at + (s >> 2) * (128 * 128) + (s & 3) * 32, 16),
+                       describe(k_at + (s >> 2) * (kTile * 128) + (s & 3) * 32, 16), kScores, s > 0);
+            commit(s_full + 8 * (i & 1));
+            commit(empty + 8 * slot);
+            return true;
+        };
+        bool fine = scores(0);
+        for (int i = 0; fine && i < tiles; ++i) {
+            if (i + 1 < tiles) {
+                // the buffer's weights must have been multiplied before new scores go there
+                if (i > 0) fine = bar_wait(o_done, (i - 1) & 1, &gave_up);
+                fine = fine && scores(i + 1);
+                if (!fine) break;
+            }
+            const int item = 2 * i + 1, slot = item % kSlots;
+            fine = bar_wait(p_full + 8 * (i & 1), (i >> 1) & 1, &gave_up) && bar_wait(full + 8 * slot, (item / kSlots) & 1, &gave_up);
+            if (!fine) break;
+            fence_after();
+            const uint32_t v_at = ring + slot * Shape::kSlot, p_at = tmem + (i & 1) * kTile;
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int s = 0; s < kTile / 16; ++s)
+                    mma_ts(o_at, p_at + part * 32 + s * 8, describe(v_at + s * 2048, kTile * 128), kValues, i > 0 || part > 0 || s > 0);
+            commit(empty + 8 * slot);
+            commit(o_done);
+        }
+        commit(drained);                                          // nothing in flight when the memory is given back
+        int late = 0;
+        bar_wait(drained, 0, &late);
+    }
+    __syncwarp();
+    __syncthreads();
+    if (warp == 7) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kColumns) : "memory");
     }
 }
 
@@ -370,11 +660,28 @@ int plan_segment(int64_t longest, int64_t units, int page, int64_t most) {
     return (int)(len < by_ids ? len : by_ids);
 }
 
+// The prefix kernel runs two blocks a multiprocessor: the number of segments that makes its rounds of blocks shortest, a
+// segment costing three tiles beyond its own (start, first loads, the partial result).
+int plan_prefix(int64_t longest, int64_t units, int page) {
+    const int64_t tiles = divide_up(longest, kTile), slots = 2 * rlcs_device::limits().sms;
+    const int64_t by_ids = (int64_t)(kMaxIds - 2) * page / kTile, most = by_ids < 256 ? by_ids : 256;
+    int64_t best = 1, cost = INT64_MAX;
+    for (int64_t segs = divide_up(tiles, most); segs <= tiles && segs <= 256; ++segs) {
+        const int64_t c = divide_up(units * segs, slots) * (int64_t)(divide_up(tiles, segs) + 3);
+        if (c < cost) { cost = c; best = divide_up(tiles, segs); }
+    }
+    return (int)((cost == INT64_MAX ? most : best) * kTile);
+}
+
 int plan(AttnParams& P) {
+    const int64_t rows = (int64_t)P.B * P.r;
     P.own_tiles = divide_up(P.r, 16);
-    P.prefix_tiles = P.groups > 0 ? (int)((int64_t)P.B * P.r / 64) + P.groups : 0;
-    P.prefix_seg = plan_segment(P.max_prefix, (int64_t)P.Hk * (P.B * (int64_t)P.r / 64 > 0 ? P.B * (int64_t)P.r / 64 : 1), P.page, 16384);
-    P.own_seg = plan_segment(P.max_len, (int64_t)P.B * P.Hk * P.own_tiles, P.page, 1024);
+    P.prefix_rows = P.groups > 0 && rows > 16 * (int64_t)P.groups ? 128 : 16;
+    P.prefix_tiles = P.groups > 0 ? (int)(rows / P.prefix_rows) + P.groups : 0;
+    const int64_t units = P.groups > 0 ? (int64_t)P.Hk * P.groups * divide_up(divide_up(rows, P.groups), P.prefix_rows) : 0;
+    P.prefix_seg = P.max_prefix <= 0 ? kTile : P.prefix_rows == 128 ? plan_prefix(P.max_prefix, units, P.page)
+                                                                    : plan_segment(P.max_prefix, units, P.page, 1024);
+    P.own_seg = plan_segment(P.max_len, rows > 0 ? (int64_t)P.B * P.Hk * P.own_tiles : 1, P.page, 1024);
     P.prefix_segs = P.groups > 0 ? divide_up(P.max_prefix, P.prefix_seg) : 0;
     P.own_segs = divide_up(P.max_len, P.own_seg);
     const int64_t pb = (int64_t)P.prefix_tiles * P.Hk * P.prefix_segs, ob = (int64_t)P.own_tiles * P.Hk * P.B * P.own_segs;
@@ -409,13 +716,27 @@ size_t workspace_of(const AttnParams& P) {
     return rows * ((P.d <= 64 ? 64 : 128) + 2) * sizeof(float) + 16;
 }
 
+// Room beyond 48 KB of shared memory, asked for once a device.
+template <typename F> bool grant(F kernel, int bytes, bool* granted) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    if (!granted[dev]) granted[dev] = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+    return granted[dev];
+}
+
 template <int D> int launch(const AttnParams& P, cudaStream_t s) {
-    constexpr int kSmem = 4 * kTile * D * 2 + 16;
-    static_assert(4 * kTile * D * 2 >= 4 * 16 * D * 4, "the warps' shares are joined in the tiles' room");
-    const int bytes = kSmem + 4 * 16 * 8;
-    if (cudaFuncSetAttribute(attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return RLCS_ERR_CUDA;
-    const int64_t blocks = P.prefix_blocks + (int64_t)P.own_tiles * P.Hk * P.B * P.own_segs;
-    if (blocks > 0) attention_kernel<D><<<(unsigned)blocks, kThreads, bytes, s>>>(P);
+    constexpr int kBytes = 4 * kTile * D * 2;
+    static_assert(kBytes >= 4 * 16 * D * 4 + 4 * 16 * 8, "the warps' shares are joined in the tiles' room");
+    static bool granted[64], granted_prefix[64];
+    if (!grant(attention_kernel<D>, kBytes, granted)) return RLCS_ERR_CUDA;
+    const bool wide = P.prefix_rows == 128;
+    if (wide && P.prefix_blocks > 0) {
+        if (!grant(prefix_kernel<D>, PrefixShape<D>::kBytes, granted_prefix)) return RLCS_ERR_CUDA;
+        prefix_kernel<D><<<(unsigned)P.prefix_blocks, kPrefixThreads, PrefixShape<D>::kBytes, s>>>(P);
+    }
+    const int narrow_blocks = wide ? 0 : P.prefix_blocks;
+    const int64_t blocks = narrow_blocks + (int64_t)P.own_tiles * P.Hk * P.B * P.own_segs;
+    if (blocks > 0) attention_kernel<D><<<(unsigned)blocks, kThreads, kBytes, s>>>(P, narrow_blocks);
     join_kernel<D><<<(unsigned)divide_up((int64_t)P.B * P.H, kThreads / 32), kThreads, 0, s>>>(P);
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }

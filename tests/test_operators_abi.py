@@ -115,16 +115,16 @@ def test_binding_checks(monkeypatch):
         def stride(self, i=None):
             return self._s if i is None else self._s[i]
 
-    assert binding._rows(Rows(torch.float32, (2, 8), (11, 1)), "f32", "logits")[1] == 11
-    assert binding._rows(Rows(torch.float32, (1, 8), (0, 1)), "f32", "logits")[1] == 8
+    assert binding._rows(Rows(torch.float32, (2, 8), (11, 1)), "f32", "logits", 0)[1] == 11
+    assert binding._rows(Rows(torch.float32, (1, 8), (0, 1)), "f32", "logits", 0)[1] == 8
     for strides in ((8, 2), (7, 1), (0, 1)):
         with pytest.raises(ValueError):
-            binding._rows(Rows(torch.float32, (2, 8), strides), "f32", "logits")
+            binding._rows(Rows(torch.float32, (2, 8), strides), "f32", "logits", 0)
     with pytest.raises(TypeError):
-        binding._rows(Rows(torch.bfloat16, (2, 8), (8, 1)), "f32", "logits")
+        binding._rows(Rows(torch.bfloat16, (2, 8), (8, 1)), "f32", "logits", 0)
     with pytest.raises(ValueError):
-        binding._rows(Rows(torch.float32, (2, 8), (8, 1)), "f32", "dlogits", (2, 9))
+        binding._rows(Rows(torch.float32, (2, 8), (8, 1)), "f32", "dlogits", 0, (2, 9))
     with pytest.raises(ValueError):
-        binding._typed(_FakeTensor(0, torch.int32, (3,)), "i32", (2,), "actions")
+        binding._typed(_FakeTensor(0, torch.int32, (3,)), "i32", (2,), "actions", 0)
     with pytest.raises(TypeError):
-        binding._typed(_FakeTensor(0, torch.int64, (2,)), "i32", (2,), "actions")
+        binding._typed(_FakeTensor(0, torch.int64, (2,)), "i32", (2,), "actions", 0)
