@@ -6,6 +6,7 @@
 // A group's prefix is multiplied with all of the group's queries at once: the queries of all its rows and of the heads
 // that share a key head are the rows of one tile.  A row's own tokens meet the heads that share a key head only.  Both
 // run over key segments that leave (running maximum, sum, product) behind; a second kernel joins a row's segments.
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include <cmath>
@@ -43,7 +44,7 @@ struct AttnParams {
 
 constexpr int kTile = 64;                       // keys a step
 constexpr int kThreads = 128;
-constexpr int kMaxIds = 2048;                   // page numbers a segment may need
+constexpr int kMaxIds = 2048;                   // page numbers a segment may need; its last tile may look up a tile's more
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -304,7 +305,7 @@ __device__ __forceinline__ bool prefix_tile(const AttnParams& P, int block, Pref
 template <int D>
 __global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_constant__ AttnParams P, int prefix_blocks) {
     extern __shared__ __align__(128) char smem[];
-    __shared__ int ids[kMaxIds];
+    __shared__ int ids[kMaxIds + kTile];
     int block = blockIdx.x;
     if (block < prefix_blocks) {
         PrefixTile t;
@@ -331,6 +332,8 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_consta
 // row a thread (maximum, exponentials, sums).  Warps 4-6 copy keys and values through the page table into a ring of slots
 // in the layout that the matrix instructions read (128-byte rows, pieces exchanged by row).  Warp 7: one thread issues.
 // Two blocks share a multiprocessor, so that one's exponentials run under the other's products.
+// Pages that divide a tile of 64 keys into parts of at least eight rows, or are whole tiles, are copied by TMA boxes (TMA =
+// true; a segment's last, partial tile apart, whose missing keys must be zeros); other page sizes piece by piece.
 constexpr int kPrefixThreads = 256, kLoaders = 96;       // warps 4-6 load, warp 7 issues
 
 template <int D> struct PrefixShape {
@@ -399,14 +402,24 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-template <int D>
-__global__ void __launch_bounds__(kPrefixThreads, 2) prefix_kernel(const __grid_constant__ AttnParams P) {
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+
+template <int D, bool TMA>
+__global__ void __launch_bounds__(kPrefixThreads, 2)
+prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     typedef PrefixShape<D> Shape;
     constexpr int kSlots = Shape::kSlots, kPieces = D / 8, kColumns = 256;
     constexpr uint32_t kScores = 1u << 4 | 1u << 7 | 1u << 10 | (kTile >> 3) << 17 | (128 >> 4) << 24;
     constexpr uint32_t kValues = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 16 | (D >> 3) << 17 | (128 >> 4) << 24;      // V: keys by rows
     extern __shared__ char raw[];
-    __shared__ int ids[kMaxIds];
+    __shared__ int ids[kMaxIds + kTile];
     __shared__ __align__(8) uint64_t bars[2 * kSlots + 6];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
@@ -422,7 +435,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 2) prefix_kernel(const __grid_
     }
     if (tid == 0) {
         gave_up = 0;
-        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, kLoaders); bar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kLoaders); bar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(p_full + 8 * i, 128); }
         bar_init(o_done, 1);
         bar_init(drained, 1);
@@ -532,32 +545,74 @@ __global__ void __launch_bounds__(kPrefixThreads, 2) prefix_kernel(const __grid_
         fence_before();
     } else if (warp < 7) {
         const int me = tid - 128, c = me % kPieces, row0 = me / kPieces;
-        constexpr int kStep = kLoaders / kPieces, kAhead = kSlots - 2;      // slots being filled
-        const int items = 2 * tiles;
-        for (int i = 0; i < items + kAhead; ++i) {
-            if (i < items) {
-                const int slot = i % kSlots, round = i / kSlots, base = (i >> 1) * kTile;
-                if (round > 0 && !bar_wait(empty + 8 * slot, (round - 1) & 1, &gave_up)) break;
-                const __nv_bfloat16* from = (i & 1 ? P.v : P.k) + t.kv_head * P.head_stride + c * 8;
-                const uint32_t dst = ring + slot * Shape::kSlot + (c >> 3) * (kTile * 128);
-#pragma unroll 8
-                for (int row = row0; row < kTile; row += kStep) {
-                    const int local = base + row;
-                    bool there = t.begin + local < t.end && c * 8 < P.d;
-                    int64_t at = 0;
-                    if (there) {
-                        const int in = offset + local, pg = page_of(P, in), id = ids[pg];
-                        there = id >= 0;
-                        if (there) at = id * P.page_stride + (in - pg * P.page) * P.token_stride;
+        constexpr int kStep = kLoaders / kPieces, kRows = (kTile + kStep - 1) / kStep;
+        constexpr int kAhead = kSlots - 2;                        // slots being filled
+        const __nv_bfloat16* from[2] = {P.k + t.kv_head * P.head_stride + c * 8, P.v + t.kv_head * P.head_stride + c * 8};
+        const uint32_t lane_at = ring + (c >> 3) * (kTile * 128);
+        int64_t place[kRows];                                     // of the thread's rows in the caches, -1: no such key
+        auto places = [&](int tile) {
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) {
+                const int local = tile * kTile + row0 + k * kStep, in = offset + local, pg = page_of(P, in), id = ids[pg];
+                const int64_t at = id * P.page_stride + (in - pg * P.page) * P.token_stride;
+                place[k] = t.begin + local < t.end && c * 8 < P.d && id >= 0 ? at : -1;
+            }
+        };
+        auto pieces = [&](int item) {
+            const __nv_bfloat16* base = from[item & 1];
+            const uint32_t dst = lane_at + (item % kSlots) * Shape::kSlot;
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) {
+                const int row = row0 + k * kStep;
+                if (row < kTile) copy16(dst + row * 128 + (((c & 7) ^ (row & 7)) << 4), base + (place[k] < 0 ? 0 : place[k]), place[k] >= 0);
+            }
+        };
+        auto room = [&](int item) { return item < kSlots || bar_wait(empty + 8 * (item % kSlots), (item / kSlots - 1) & 1, &gave_up); };
+        bool fine = true;
+        if constexpr (TMA) {
+            const int whole = (t.end - t.begin) / kTile, box = P.page < kTile ? P.page : kTile;
+            if (me == 0)
+                for (int i = 0; i < 2 * whole && fine; ++i) {
+                    fine = room(i);
+                    if (!fine) break;
+                    const uint32_t bar = full + 8 * (i % kSlots), dst = ring + (i % kSlots) * Shape::kSlot;
+                    bar_expect(bar, Shape::kSlot);
+                    for (int row = 0; row < kTile; row += box) {
+                        const int in = offset + (i >> 1) * kTile + row, pg = page_of(P, in);
+#pragma unroll
+                        for (int half = 0; half < D / 64; ++half)     // a page number of -1 lies outside the map: zeros
+                            box_load(dst + half * (kTile * 128) + row * 128, i & 1 ? &v_map : &k_map, bar, half * 64, in - pg * P.page, t.kv_head, ids[pg]);
                     }
-                    copy16(dst + row * 128 + (((c & 7) ^ (row & 7)) << 4), there ? from + at : P.k, there);
+                }
+            if (whole < tiles) {
+                asm volatile("bar.sync 1, %0;" ::"n"(kLoaders) : "memory");
+                places(whole);
+                for (int i = 2 * whole; i < 2 * whole + 2 && fine; ++i) {
+                    fine = room(i);
+                    if (fine) pieces(i);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_async();
+                asm volatile("bar.sync 1, %0;" ::"n"(kLoaders) : "memory");
+                if (me == 0 && fine) {
+                    bar_arrive(full + 8 * (2 * whole % kSlots));
+                    bar_arrive(full + 8 * ((2 * whole + 1) % kSlots));
                 }
             }
-            asm volatile("cp.async.commit_group;");
-            if (i >= kAhead) {                                    // the copies of kAhead items ago are complete
-                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
-                fence_async();
-                bar_arrive(full + 8 * ((i - kAhead) % kSlots));
+        } else {
+            for (int i = 0; i < 2 * tiles + kAhead && fine; ++i) {
+                if (i < 2 * tiles) {
+                    if ((i & 1) == 0) places(i >> 1);
+                    fine = room(i);
+                    if (!fine) break;
+                    pieces(i);
+                }
+                asm volatile("cp.async.commit_group;");
+                if (i >= kAhead) {                                // the copies of kAhead items ago are complete
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+                    fence_async();
+                    bar_arrive(full + 8 * ((i - kAhead) % kSlots));
+                }
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
@@ -724,15 +779,40 @@ template <typename F> bool grant(F kernel, int bytes, bool* granted) {
     return granted[dev];
 }
 
+// The cache as a map of boxes [rows of a page, 64 dimensions]; false where the driver takes no such strides.
+bool box_map(CUtensorMap* map, const AttnParams& P, const void* base) {
+    typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess) fn = nullptr;
+        return reinterpret_cast<Encode>(fn);
+    }();
+    if (encode == nullptr || P.pages < 1) return false;
+    const cuuint64_t extent[4] = {(cuuint64_t)P.d, (cuuint64_t)P.page, (cuuint64_t)P.Hk, (cuuint64_t)P.pages};
+    const cuuint64_t stride[3] = {(cuuint64_t)P.token_stride * 2, (cuuint64_t)P.head_stride * 2, (cuuint64_t)P.page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(P.page < kTile ? P.page : kTile), 1, 1}, step[4] = {1, 1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D> int launch(const AttnParams& P, cudaStream_t s) {
-    constexpr int kBytes = 4 * kTile * D * 2;
+    constexpr int kBytes = 4 * kTile * D * 2, kPrefixBytes = PrefixShape<D>::kBytes;
     static_assert(kBytes >= 4 * 16 * D * 4 + 4 * 16 * 8, "the warps' shares are joined in the tiles' room");
-    static bool granted[64], granted_prefix[64];
+    static bool granted[64], granted_tma[64], granted_pieces[64];
     if (!grant(attention_kernel<D>, kBytes, granted)) return RLCS_ERR_CUDA;
     const bool wide = P.prefix_rows == 128;
     if (wide && P.prefix_blocks > 0) {
-        if (!grant(prefix_kernel<D>, PrefixShape<D>::kBytes, granted_prefix)) return RLCS_ERR_CUDA;
-        prefix_kernel<D><<<(unsigned)P.prefix_blocks, kPrefixThreads, PrefixShape<D>::kBytes, s>>>(P);
+        CUtensorMap k_map = {}, v_map = {};
+        const bool boxes = P.page >= kTile ? P.page % kTile == 0 : P.page >= 8 && kTile % P.page == 0;
+        if (boxes && box_map(&k_map, P, P.k) && box_map(&v_map, P, P.v)) {
+            if (!grant(prefix_kernel<D, true>, kPrefixBytes, granted_tma)) return RLCS_ERR_CUDA;
+            prefix_kernel<D, true><<<(unsigned)P.prefix_blocks, kPrefixThreads, kPrefixBytes, s>>>(P, k_map, v_map);
+        } else {
+            if (!grant(prefix_kernel<D, false>, kPrefixBytes, granted_pieces)) return RLCS_ERR_CUDA;
+            prefix_kernel<D, false><<<(unsigned)P.prefix_blocks, kPrefixThreads, kPrefixBytes, s>>>(P, k_map, v_map);
+        }
     }
     const int narrow_blocks = wide ? 0 : P.prefix_blocks;
     const int64_t blocks = narrow_blocks + (int64_t)P.own_tiles * P.Hk * P.B * P.own_segs;
