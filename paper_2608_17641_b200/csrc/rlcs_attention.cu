@@ -36,7 +36,7 @@ struct AttnParams {
     int max_prefix, max_len;
     int prefix_seg, own_seg;       // keys a segment
     int prefix_segs, own_segs;     // segments a row
-    int prefix_rows;               // rows of a prefix tile: 128 (tensor memory) or 16
+    int prefix_rows;               // rows of a prefix block: 256 or 128 (tensor memory), or 16
     int prefix_tiles, own_tiles;   // slots of prefix tiles over all groups; tiles of 16 rows a trajectory
     int prefix_blocks;             // thread blocks of the prefix part
     float scale_log2;
@@ -327,18 +327,20 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------- prefixes of many rows
-// 128 rows a block on tcgen05: scores S = Q K^T of 64 keys at a time into one of two 64-column buffers of tensor memory, the
-// weights back over them as two bfloat16 parts (32 columns each), O += P V accumulated in tensor memory.  Warps 0-3: one
-// row a thread (maximum, exponentials, sums).  Warps 4-6 copy keys and values through the page table into a ring of slots
-// in the layout that the matrix instructions read (128-byte rows, pieces exchanged by row).  Warp 7: one thread issues.
-// Two blocks share a multiprocessor, so that one's exponentials run under the other's products.
+// RT tiles of 128 rows a block (RT = 2 where groups have more than 128) on tcgen05, each tile: scores S = Q K^T of 64 keys at a time into one of two 64-column buffers of tensor memory, the
+// weights back over them as two bfloat16 parts (32 columns each), O += P V accumulated in tensor memory.  Four warps a row
+// tile: one row a thread (maximum, exponentials, sums).  Two warps copy keys and values through the page table into a ring of
+// slots in the layout that the matrix instructions read (128-byte rows, pieces exchanged by row).  Two warps a row tile issue
+// its products, one the scores and one the values: an issuing warp waits about 100 cycles at each barrier, in which the others
+// keep the matrix unit busy.  With one row tile a block, two blocks share a multiprocessor to the same end.
 // Pages that divide a tile of 64 keys into parts of at least eight rows, or are whole tiles, are copied by TMA boxes (TMA =
 // true; a segment's last, partial tile apart, whose missing keys must be zeros); other page sizes piece by piece.
-constexpr int kPrefixThreads = 256, kLoaders = 96;       // warps 4-6 load, warp 7 issues
+constexpr int kLoaders = 64;
 
-template <int D> struct PrefixShape {
-    static constexpr int kSlot = kTile * D * 2, kSlots = D == 128 ? 4 : 8, kQ = 128 * D * 2;
-    static constexpr int kBytes = kQ + kSlots * kSlot + 1024;      // + alignment
+template <int D, int RT> struct PrefixShape {
+    static constexpr int kThreads = RT * 192 + kLoaders, kSlot = kTile * D * 2, kSlots = D == 128 && RT == 1 ? 4 : 8;
+    static constexpr int kQ = 128 * D * 2, kColumns = 256 * RT;    // of tensor memory: two score buffers and O, a row tile
+    static constexpr int kBytes = RT * kQ + kSlots * kSlot + 1024; // + alignment
 };
 
 __device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
@@ -358,8 +360,11 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int*
     return false;
 }
 
+// Matrix instructions and their commits are reached by the whole warp and issued by its elected lane, the same one every
+// time, so that their operands stay in uniform registers.
 __device__ __forceinline__ void commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
+                 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar) : "memory");
 }
 
 // 128-byte rows with exchanged pieces; `lead`: bytes between blocks of 64 along the contiguous dimension (not used where
@@ -369,12 +374,12 @@ __device__ __forceinline__ uint64_t describe(uint32_t at, uint32_t lead) {
 }
 
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, int add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+    asm volatile("{\n.reg .pred e, p;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %4, 0;\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"(add) : "memory");
 }
 
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, int add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+    asm volatile("{\n.reg .pred e, p;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %4, 0;\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
                  ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"(add) : "memory");
 }
 
@@ -387,13 +392,16 @@ __device__ __forceinline__ void tmem_load32(uint32_t* r, uint32_t at) {
                    "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]) : "r"(at) : "memory");
 }
 
-__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
-                 "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+__device__ __forceinline__ void tmem_load16(uint32_t* r, uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+}
+
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                  ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-                 "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-                 "r"(r[30]), "r"(r[31]) : "memory");
+                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
 __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -411,60 +419,62 @@ __device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap* map, u
                  ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 
-template <int D, bool TMA>
-__global__ void __launch_bounds__(kPrefixThreads, 2)
+template <int D, bool TMA, int RT>
+__global__ void __launch_bounds__(PrefixShape<D, RT>::kThreads, 3 - RT)
 prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
-    typedef PrefixShape<D> Shape;
-    constexpr int kSlots = Shape::kSlots, kPieces = D / 8, kColumns = 256;
+    typedef PrefixShape<D, RT> Shape;
+    constexpr int kSlots = Shape::kSlots, kPieces = D / 8, kIssuer = RT * 4 + kLoaders / 32;
     constexpr uint32_t kScores = 1u << 4 | 1u << 7 | 1u << 10 | (kTile >> 3) << 17 | (128 >> 4) << 24;
     constexpr uint32_t kValues = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 16 | (D >> 3) << 17 | (128 >> 4) << 24;      // V: keys by rows
     extern __shared__ char raw[];
     __shared__ int ids[kMaxIds + kTile];
-    __shared__ __align__(8) uint64_t bars[2 * kSlots + 6];
+    __shared__ __align__(8) uint64_t bars[2 * kSlots + 6 * RT + 1];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
     PrefixTile t;
     if (!prefix_tile(P, blockIdx.x, &t)) return;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t q_at = (smem_at(raw) + 1023) & ~1023u, ring = q_at + Shape::kQ;
-    const uint32_t full = smem_at(bars), empty = full + 8 * kSlots, s_full = empty + 8 * kSlots, p_full = s_full + 16, o_done = p_full + 16,
-                   drained = o_done + 8;
-    if (warp == 7) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_at)), "n"(kColumns) : "memory");
+    const uint32_t q_at = (smem_at(raw) + 1023) & ~1023u, ring = q_at + RT * Shape::kQ;
+    const uint32_t full = smem_at(bars), empty = full + 8 * kSlots, drained = empty + 8 * kSlots;
+    const uint32_t s_full = drained + 8, p_full = s_full + 16 * RT, o_done = p_full + 16 * RT;      // two a row tile, taken in turn
+    const int row_tiles = RT == 2 && t.rows - t.first_row <= 128 ? 1 : RT;
+    if (warp == kIssuer) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_at)), "n"(Shape::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) {
         gave_up = 0;
-        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kLoaders); bar_init(empty + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(p_full + 8 * i, 128); }
-        bar_init(o_done, 1);
-        bar_init(drained, 1);
+        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kLoaders); bar_init(empty + 8 * i, row_tiles); }
+        for (int i = 0; i < 2 * RT; ++i) { bar_init(s_full + 8 * i, 1); bar_init(p_full + 8 * i, 128); bar_init(o_done + 8 * i, 1); }
+        bar_init(drained, 2 * RT);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     // queries, zeros where there are none
-    for (int i = tid; i < 128 * kPieces; i += kPrefixThreads) {
+    for (int i = tid; i < RT * 128 * kPieces; i += Shape::kThreads) {
         const int row = i / kPieces, c = i % kPieces, at = t.first_row + row;
         uint4 v = {0, 0, 0, 0};
         if (at < t.rows && c * 8 < P.d)
             v = *reinterpret_cast<const uint4*>(P.q + (int64_t)(t.b0 + at / P.r) * P.q_stride + (int64_t)(t.kv_head * P.r + at % P.r) * P.d + c * 8);
-        const uint32_t dst = q_at + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+        const uint32_t dst = q_at + (row >> 7) * Shape::kQ + (c >> 3) * (128 * 128) + (row & 127) * 128 + (((c & 7) ^ (row & 7)) << 4);
         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
     }
     fence_async();
     fence_before();
-    const int missing = read_ids(P, ids, P.prefix_table + (int64_t)t.group * P.prefix_width, P.prefix_width, t.begin, t.end, tid, kPrefixThreads);
+    const int missing = read_ids(P, ids, P.prefix_table + (int64_t)t.group * P.prefix_width, P.prefix_width, t.begin, t.end, tid, Shape::kThreads);
     fence_after();
-    const uint32_t tmem = tmem_at, o_at = tmem + 128;
+    const uint32_t tmem = tmem_at;
     const int offset = t.begin % P.page, tiles = (t.end - t.begin + kTile - 1) / kTile;
 
-    if (warp < 4) {
-        const uint32_t mine = (uint32_t)(warp * 32) << 16;
+    if (warp < 4 * RT) {
+        const int rt = warp >> 2;
+        const uint32_t mine = ((uint32_t)((warp & 3) * 32) << 16) + rt * 256, o_at = tmem + mine + 128;
+        const uint32_t my_s = s_full + 16 * rt, my_p = p_full + 16 * rt, my_o = o_done + 16 * rt;
         const bool any_row = t.first_row + warp * 32 < t.rows;
         float m = -INFINITY, l = 0.f;
         bool fine = true;
-        for (int i = 0; i < tiles; ++i) {
+        for (int i = 0; i < tiles && rt < row_tiles; ++i) {
             const uint32_t at = tmem + mine + (i & 1) * kTile;
-            fine = __all_sync(~0u, bar_wait(s_full + 8 * (i & 1), (i >> 1) & 1, &gave_up));
+            fine = __all_sync(~0u, bar_wait(my_s + 8 * (i & 1), (i >> 1) & 1, &gave_up));
             if (!fine) break;
             fence_after();
             if (any_row) {
@@ -488,17 +498,17 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
                 if (__any_sync(~0u, now > m + 8.f)) {
                     const float next = fmaxf(m, now), fade = m == -INFINITY ? 0.f : exp2_of(m - next);
                     if (i > 0) {
-                        fine = __all_sync(~0u, bar_wait(o_done, (i - 1) & 1, &gave_up));
+                        fine = __all_sync(~0u, bar_wait(my_o + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, &gave_up));
                         if (!fine) break;
                         fence_after();
 #pragma unroll
-                        for (int c = 0; c < D; c += 32) {
-                            uint32_t o[32];
-                            tmem_load32(o, o_at + mine + c);
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_load16(o, o_at + c);
                             tmem_wait_load();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fade);
-                            tmem_store32(o_at + mine + c, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fade);
+                            tmem_store16(o_at + c, o);
                         }
                     }
                     l *= fade;
@@ -506,34 +516,37 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
                 }
                 const float base = m == -INFINITY ? 0.f : m;
                 float sum[2] = {0.f, 0.f};
-                uint32_t lo[kTile / 2];
 #pragma unroll
-                for (int k = 0; k < kTile; k += 2) {
-                    const float a = exp2_of(fmaf(__uint_as_float(s[k]), P.scale_log2, -base));
-                    const float b = exp2_of(fmaf(__uint_as_float(s[k + 1]), P.scale_log2, -base));
-                    sum[0] += a;
-                    sum[1] += b;
-                    const uint32_t hi = pack2(a, b);
-                    lo[k / 2] = pack2(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
-                    s[k / 2] = hi;
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t hi[16], lo[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float a = exp2_of(fmaf(__uint_as_float(s[half * 32 + 2 * k]), P.scale_log2, -base));
+                        const float b = exp2_of(fmaf(__uint_as_float(s[half * 32 + 2 * k + 1]), P.scale_log2, -base));
+                        sum[0] += a;
+                        sum[1] += b;
+                        hi[k] = pack2(a, b);
+                        lo[k] = pack2(a - __uint_as_float(hi[k] << 16), b - __uint_as_float(hi[k] & 0xffff0000u));
+                    }
+                    tmem_store16(at + half * 16, hi);
+                    tmem_store16(at + 32 + half * 16, lo);
                 }
                 l += sum[0] + sum[1];
-                tmem_store32(at, s);
-                tmem_store32(at + 32, lo);
                 tmem_wait_store();
             }
             fence_before();
-            bar_arrive(p_full + 8 * (i & 1));
+            bar_arrive(my_p + 8 * (i & 1));
         }
-        if (fine) fine = __all_sync(~0u, bar_wait(o_done, (tiles - 1) & 1, &gave_up));
-        fence_after();
-        const int at = t.first_row + warp * 32 + lane;
-        const int64_t dst = (int64_t)t.seg * P.B * P.H + (int64_t)(t.b0 + at / P.r) * P.H + t.kv_head * P.r + at % P.r;
         if (any_row) {
+            for (int i = max(tiles - 2, 0); i < tiles && fine; ++i)
+                fine = __all_sync(~0u, bar_wait(my_o + 8 * (i & 1), (i >> 1) & 1, &gave_up));
+            fence_after();
+            const int at = t.first_row + warp * 32 + lane;
+            const int64_t dst = (int64_t)t.seg * P.B * P.H + (int64_t)(t.b0 + at / P.r) * P.H + t.kv_head * P.r + at % P.r;
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
                 uint32_t o[32];
-                tmem_load32(o, o_at + mine + c);
+                tmem_load32(o, o_at + c);
                 tmem_wait_load();
                 if (at < t.rows)
 #pragma unroll
@@ -543,8 +556,8 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
             if (at < t.rows) P.part_ml[dst] = fine ? make_float2(m, l) : make_float2(0.f, __int_as_float(0x7fffffff));
         }
         fence_before();
-    } else if (warp < 7) {
-        const int me = tid - 128, c = me % kPieces, row0 = me / kPieces;
+    } else if (warp < kIssuer) {
+        const int me = tid - RT * 128, c = me % kPieces, row0 = me / kPieces;
         constexpr int kStep = kLoaders / kPieces, kRows = (kTile + kStep - 1) / kStep;
         constexpr int kAhead = kSlots - 2;                        // slots being filled
         const __nv_bfloat16* from[2] = {P.k + t.kv_head * P.head_stride + c * 8, P.v + t.kv_head * P.head_stride + c * 8};
@@ -616,40 +629,46 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (lane == 0) {
-        auto scores = [&](int i) {
-            const int item = 2 * i, slot = item % kSlots;
-            if (!bar_wait(full + 8 * slot, (item / kSlots) & 1, &gave_up)) return false;
-            fence_after();
-            const uint32_t k_at = ring + slot * Shape::kSlot;
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s)
-                mma_ss(tmem + (i & 1) * kTile, describe(q_at + (s >> 2) * (128 * 128) + (s & 3) * 32, 16),
-                       describe(k_at + (s >> 2) * (kTile * 128) + (s & 3) * 32, 16), kScores, s > 0);
-            commit(s_full + 8 * (i & 1));
-            commit(empty + 8 * slot);
-            return true;
-        };
-        bool fine = scores(0);
-        for (int i = 0; fine && i < tiles; ++i) {
-            if (i + 1 < tiles) {
+    } else {
+        const int rt = (warp - kIssuer) >> 1;
+        const uint32_t base = __shfl_sync(~0u, tmem, 0) + rt * 256;
+        const uint32_t my_s = s_full + 16 * rt, my_p = p_full + 16 * rt, my_o = o_done + 16 * rt;
+        auto wait = [&](uint32_t bar, int parity) { return (bool)__all_sync(~0u, bar_wait(bar, parity & 1, &gave_up)); };
+        const int n = rt < row_tiles ? tiles : 0;
+        bool fine = true;
+        if (((warp - kIssuer) & 1) == 0) {
+            const uint64_t q_desc = describe(q_at + rt * Shape::kQ, 16), k_desc = describe(ring, 16);
+            for (int i = 0; i < n; ++i) {
+                const int item = 2 * i, slot = item % kSlots;
                 // the buffer's weights must have been multiplied before new scores go there
-                if (i > 0) fine = bar_wait(o_done, (i - 1) & 1, &gave_up);
-                fine = fine && scores(i + 1);
+                fine = (i < 2 || wait(my_o + 8 * (i & 1), (i - 2) >> 1)) && wait(full + 8 * slot, item / kSlots);
                 if (!fine) break;
+                fence_after();
+                const uint64_t k_at = k_desc + slot * (Shape::kSlot >> 4);
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+                    mma_ss(base + (i & 1) * kTile, q_desc + (((s >> 2) * (128 * 128) + (s & 3) * 32) >> 4),
+                           k_at + (((s >> 2) * (kTile * 128) + (s & 3) * 32) >> 4), kScores, s > 0);
+                commit(my_s + 8 * (i & 1));
+                commit(empty + 8 * slot);
             }
-            const int item = 2 * i + 1, slot = item % kSlots;
-            fine = bar_wait(p_full + 8 * (i & 1), (i >> 1) & 1, &gave_up) && bar_wait(full + 8 * slot, (item / kSlots) & 1, &gave_up);
-            if (!fine) break;
-            fence_after();
-            const uint32_t v_at = ring + slot * Shape::kSlot, p_at = tmem + (i & 1) * kTile;
+        } else {
+            const uint64_t v_desc = describe(ring, kTile * 128);
+            for (int i = 0; i < n; ++i) {
+                const int item = 2 * i + 1, slot = item % kSlots;
+                fine = wait(full + 8 * slot, item / kSlots) && wait(my_p + 8 * (i & 1), i >> 1);
+                if (!fine) break;
+                fence_after();
+                const uint64_t v_at = v_desc + slot * (Shape::kSlot >> 4);
+                const uint32_t p_at = base + (i & 1) * kTile;
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+                for (int part = 0; part < 2; ++part)
 #pragma unroll
-                for (int s = 0; s < kTile / 16; ++s)
-                    mma_ts(o_at, p_at + part * 32 + s * 8, describe(v_at + s * 2048, kTile * 128), kValues, i > 0 || part > 0 || s > 0);
-            commit(empty + 8 * slot);
-            commit(o_done);
+                    for (int s = 0; s < kTile / 16; ++s)
+                        mma_ts(base + 128, p_at + part * 32 + s * 8, v_at + ((s * 2048) >> 4), kValues, i > 0 || part > 0 || s > 0);
+                commit(my_o + 8 * (i & 1));
+                commit(empty + 8 * slot);
+            }
         }
         commit(drained);                                          // nothing in flight when the memory is given back
         int late = 0;
@@ -657,9 +676,9 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
     }
     __syncwarp();
     __syncthreads();
-    if (warp == 7) {
+    if (warp == kIssuer) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kColumns) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Shape::kColumns) : "memory");
     }
 }
 
@@ -715,10 +734,10 @@ int plan_segment(int64_t longest, int64_t units, int page, int64_t most) {
     return (int)(len < by_ids ? len : by_ids);
 }
 
-// The prefix kernel runs two blocks a multiprocessor: the number of segments that makes its rounds of blocks shortest, a
+// The prefix kernel runs `slots` blocks at once: the number of segments that makes its rounds of blocks shortest, a
 // segment costing three tiles beyond its own (start, first loads, the partial result).
-int plan_prefix(int64_t longest, int64_t units, int page) {
-    const int64_t tiles = divide_up(longest, kTile), slots = 2 * rlcs_device::limits().sms;
+int plan_prefix(int64_t longest, int64_t units, int page, int64_t slots) {
+    const int64_t tiles = divide_up(longest, kTile);
     const int64_t by_ids = (int64_t)(kMaxIds - 2) * page / kTile, most = by_ids < 256 ? by_ids : 256;
     int64_t best = 1, cost = INT64_MAX;
     for (int64_t segs = divide_up(tiles, most); segs <= tiles && segs <= 256; ++segs) {
@@ -731,11 +750,11 @@ int plan_prefix(int64_t longest, int64_t units, int page) {
 int plan(AttnParams& P) {
     const int64_t rows = (int64_t)P.B * P.r;
     P.own_tiles = divide_up(P.r, 16);
-    P.prefix_rows = P.groups > 0 && rows > 16 * (int64_t)P.groups ? 128 : 16;
+    P.prefix_rows = P.groups <= 0 || rows <= 16 * (int64_t)P.groups ? 16 : rows <= 128 * (int64_t)P.groups ? 128 : 256;
     P.prefix_tiles = P.groups > 0 ? (int)(rows / P.prefix_rows) + P.groups : 0;
     const int64_t units = P.groups > 0 ? (int64_t)P.Hk * P.groups * divide_up(divide_up(rows, P.groups), P.prefix_rows) : 0;
-    P.prefix_seg = P.max_prefix <= 0 ? kTile : P.prefix_rows == 128 ? plan_prefix(P.max_prefix, units, P.page)
-                                                                    : plan_segment(P.max_prefix, units, P.page, 1024);
+    P.prefix_seg = P.max_prefix <= 0 ? kTile : P.prefix_rows == 16 ? plan_segment(P.max_prefix, units, P.page, 1024)
+                   : plan_prefix(P.max_prefix, units, P.page, rlcs_device::limits().sms * (P.prefix_rows == 128 ? 2 : 1));
     P.own_seg = plan_segment(P.max_len, rows > 0 ? (int64_t)P.B * P.Hk * P.own_tiles : 1, P.page, 1024);
     P.prefix_segs = P.groups > 0 ? divide_up(P.max_prefix, P.prefix_seg) : 0;
     P.own_segs = divide_up(P.max_len, P.own_seg);
@@ -797,22 +816,28 @@ bool box_map(CUtensorMap* map, const AttnParams& P, const void* base) {
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <int D, bool TMA, int RT>
+int launch_prefix(const AttnParams& P, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t s) {
+    typedef PrefixShape<D, RT> Shape;
+    static bool granted[64];
+    if (!grant(prefix_kernel<D, TMA, RT>, Shape::kBytes, granted)) return RLCS_ERR_CUDA;
+    prefix_kernel<D, TMA, RT><<<(unsigned)P.prefix_blocks, Shape::kThreads, Shape::kBytes, s>>>(P, k_map, v_map);
+    return RLCS_OK;
+}
+
 template <int D> int launch(const AttnParams& P, cudaStream_t s) {
-    constexpr int kBytes = 4 * kTile * D * 2, kPrefixBytes = PrefixShape<D>::kBytes;
+    constexpr int kBytes = 4 * kTile * D * 2;
     static_assert(kBytes >= 4 * 16 * D * 4 + 4 * 16 * 8, "the warps' shares are joined in the tiles' room");
-    static bool granted[64], granted_tma[64], granted_pieces[64];
+    static bool granted[64];
     if (!grant(attention_kernel<D>, kBytes, granted)) return RLCS_ERR_CUDA;
-    const bool wide = P.prefix_rows == 128;
+    const bool wide = P.prefix_rows > 16;
     if (wide && P.prefix_blocks > 0) {
         CUtensorMap k_map = {}, v_map = {};
-        const bool boxes = P.page >= kTile ? P.page % kTile == 0 : P.page >= 8 && kTile % P.page == 0;
-        if (boxes && box_map(&k_map, P, P.k) && box_map(&v_map, P, P.v)) {
-            if (!grant(prefix_kernel<D, true>, kPrefixBytes, granted_tma)) return RLCS_ERR_CUDA;
-            prefix_kernel<D, true><<<(unsigned)P.prefix_blocks, kPrefixThreads, kPrefixBytes, s>>>(P, k_map, v_map);
-        } else {
-            if (!grant(prefix_kernel<D, false>, kPrefixBytes, granted_pieces)) return RLCS_ERR_CUDA;
-            prefix_kernel<D, false><<<(unsigned)P.prefix_blocks, kPrefixThreads, kPrefixBytes, s>>>(P, k_map, v_map);
-        }
+        const bool boxes = (P.page >= kTile ? P.page % kTile == 0 : P.page >= 8 && kTile % P.page == 0) && box_map(&k_map, P, P.k) &&
+                           box_map(&v_map, P, P.v);
+        const int st = P.prefix_rows == 256 ? (boxes ? launch_prefix<D, true, 2>(P, k_map, v_map, s) : launch_prefix<D, false, 2>(P, k_map, v_map, s))
+                                            : (boxes ? launch_prefix<D, true, 1>(P, k_map, v_map, s) : launch_prefix<D, false, 1>(P, k_map, v_map, s));
+        if (st != RLCS_OK) return st;
     }
     const int narrow_blocks = wide ? 0 : P.prefix_blocks;
     const int64_t blocks = narrow_blocks + (int64_t)P.own_tiles * P.Hk * P.B * P.own_segs;

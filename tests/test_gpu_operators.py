@@ -449,6 +449,15 @@ def test_attention_many_rows_share_a_prompt(api, d):
     check_attention(api, [3000], [33], [i for i in range(33)], 16, 2, d, 64)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [1, 8, 24, 64, 128])
+@pytest.mark.parametrize("prefix", [1, 64, 65, 640, 1500])
+def test_attention_blocks_of_128_and_256_rows(api, prefix, page, d):
+    """One and two row tiles a block, the second one partly filled or empty; pages copied by boxes and piece by piece."""
+    check_attention(api, [prefix, max(1, prefix // 2)], [20, 28], [i % 3 for i in range(48)], 4, 1, d, page, seed=prefix)       # 80, 112 rows
+    check_attention(api, [prefix, max(1, prefix // 3)], [40, 73], [i % 3 for i in range(113)], 4, 1, d, page, seed=prefix)      # 160, 292 rows
+
+
 def test_attention_groups_of_any_size_and_rows_outside(api):
     check_attention(api, [40, 0, 33, 70], [0, 4, 1, 0], [3, 1, 0, 9, 12], 8, 4, 64, 16)
     check_attention(api, [40, 33], [2, 2], [3, 1, 0, 9, 12, 0, 5], 8, 4, 64, 16, first=2)      # rows before and after
