@@ -337,6 +337,21 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_consta
 // true; a segment's last, partial tile apart, whose missing keys must be zeros); other page sizes piece by piece.
 constexpr int kLoaders = 64;
 
+// Two fp32 operations an instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 x, x, y, z;\nmov.b64 {%0, %1}, x;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n.reg .b64 x, y;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
 template <int D, int RT> struct PrefixShape {
     static constexpr int kThreads = RT * 192 + kLoaders, kSlot = kTile * D * 2, kSlots = D == 128 && RT == 1 ? 4 : 8;
     static constexpr int kQ = 128 * D * 2, kColumns = 256 * RT;    // of tensor memory: two score buffers and O, a row tile
@@ -492,7 +507,9 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
                 }
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int k = 0; k < kTile; ++k) top[k & 3] = fmaxf(top[k & 3], __uint_as_float(s[k]));
+                for (int k = 0; k < kTile; k += 8)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) top[c] = fmaxf(fmaxf(top[c], __uint_as_float(s[k + 2 * c])), __uint_as_float(s[k + 2 * c + 1]));
                 const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * P.scale_log2;
                 // the base follows the maximum only when it is 2^8 behind: the weights stay below 2^8, and O is seldom rescaled
                 if (__any_sync(~0u, now > m + 8.f)) {
@@ -515,23 +532,24 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
                     m = next;
                 }
                 const float base = m == -INFINITY ? 0.f : m;
-                float sum[2] = {0.f, 0.f};
+                const float2 scale = {P.scale_log2, P.scale_log2}, less = {-base, -base}, minus = {-1.f, -1.f};
+                float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t hi[16], lo[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        const float a = exp2_of(fmaf(__uint_as_float(s[half * 32 + 2 * k]), P.scale_log2, -base));
-                        const float b = exp2_of(fmaf(__uint_as_float(s[half * 32 + 2 * k + 1]), P.scale_log2, -base));
-                        sum[0] += a;
-                        sum[1] += b;
-                        hi[k] = pack2(a, b);
-                        lo[k] = pack2(a - __uint_as_float(hi[k] << 16), b - __uint_as_float(hi[k] & 0xffff0000u));
+                        float2 p = fma2(make_float2(__uint_as_float(s[half * 32 + 2 * k]), __uint_as_float(s[half * 32 + 2 * k + 1])), scale, less);
+                        p = make_float2(exp2_of(p.x), exp2_of(p.y));
+                        sum[k & 1] = add2(sum[k & 1], p);
+                        hi[k] = pack2(p.x, p.y);
+                        p = fma2(make_float2(__uint_as_float(hi[k] << 16), __uint_as_float(hi[k] & 0xffff0000u)), minus, p);
+                        lo[k] = pack2(p.x, p.y);
                     }
                     tmem_store16(at + half * 16, hi);
                     tmem_store16(at + 32 + half * 16, lo);
                 }
-                l += sum[0] + sum[1];
+                l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
                 tmem_wait_store();
             }
             fence_before();
