@@ -80,9 +80,33 @@ __device__ __forceinline__ float exp2_of(float x) {
     return r;
 }
 
-// byte offset of 16-byte piece c of row `row` in a tile whose rows hold D values: pieces exchanged within
-// groups of eight rows, so that the eight rows of an 8x8 matrix lie in different banks
-template <int D> __device__ __forceinline__ uint32_t piece(int row, int c) { return row * (D * 2) + ((c ^ (row & 7)) << 4); }
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// Bounded: a wait that runs out of polls, or sees that another did, gives up, and the block's rows come out NaN.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int* gave_up) {
+    for (int polls = 0; polls < (1 << 20); ++polls) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+        if ((polls & 63) == 63 && *gave_up) return false;
+    }
+    *gave_up = 1;
+    return false;
+}
+
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // Page (from the segment's first) of place `in` of that page's and the following tokens; in and page below 2^16.
 __device__ __forceinline__ int page_of(const AttnParams& P, int in) { return P.page_mul != 0 ? (int)__umulhi((uint32_t)in, P.page_mul) : in; }
@@ -101,36 +125,73 @@ __device__ __forceinline__ int read_ids(const AttnParams& P, int* ids, const int
     return __syncthreads_or(missing);
 }
 
-// One segment of keys against 16 rows: the block's four warps share the rows and take 16 of each tile's 64 keys each.
-template <int D>
-__device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* ids, const int32_t* table, int table_width, int begin,
-                                        int end, int kv_head, int first_row, int rows, int b0, int slot) {
-    constexpr int kPieces = D / 8, kTileBytes = kTile * D * 2, kSteps = D / 16;
+// One segment of keys against 16 rows.  The block's four warps share the rows and take 16 of every 64 keys each, without
+// waiting for one another: a warp keeps a ring of 16-key stages of its own (keys and values in 128-byte rows whose 16-byte
+// pieces are exchanged by row, as the copies' boxes write them and the 8x8 matrix loads want them) and joins the others
+// after the last.
+constexpr int kPart = 16;                       // keys a warp and step
+
+template <int D> struct OwnShape {
+    static constexpr int kHalf = kPart * 128, kStage = 2 * (D / 64) * kHalf, kStages = D == 128 ? 3 : 4;      // K, then V
+    static constexpr int kBytes = 4 * kStages * kStage + 1024;                                                 // + alignment
+    static_assert(4 * kStages * kStage >= 4 * 16 * D * 4 + 4 * 16 * 8, "the warps' shares are joined in the stages' room");
+};
+
+template <int D, bool TMA>
+__device__ __forceinline__ void segment(const AttnParams& P, const CUtensorMap* k_map, const CUtensorMap* v_map, char* raw, int* ids,
+                                        uint64_t* bars, int* gave_up, const int32_t* table, int table_width, int begin, int end, int kv_head,
+                                        int first_row, int rows, int b0, int slot) {
+    typedef OwnShape<D> Shape;
+    constexpr int kSteps = D / 16, kStages = Shape::kStages, kHalf = Shape::kHalf, kValues = (D / 64) * kHalf;
     constexpr int kCols = 2;                                  // 8-key columns a warp computes
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    char* const smem = raw + ((1024 - (smem_at(raw) & 1023)) & 1023);
+    const uint32_t ring = smem_at(smem) + warp * kStages * Shape::kStage, bar = smem_at(bars) + warp * kStages * 8;
 
     const int offset = begin % P.page;
+    if (TMA && tid < 4 * kStages) {
+        bar_init(smem_at(bars) + 8 * tid, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (tid == 0) *gave_up = 0;
     const int missing = read_ids(P, ids, table, table_width, begin, end, tid, kThreads);
 
-    auto load = [&](int base, char* k_at, char* v_at) {       // keys [base, base + 64) of the segment, zeros where there are none
-#pragma unroll 4
-        for (int i = tid; i < kTile * kPieces; i += kThreads) {
-            const int row = i / kPieces, c = i % kPieces, local = base + row;
-            bool there = begin + local < end && c * 8 < P.d;
-            int64_t at = 0;
-            if (there) {
-                const int in = offset + local, pg = page_of(P, in);
-                const int id = ids[pg];
-                there = id >= 0;
-                if (there) at = id * P.page_stride + (in - pg * P.page) * P.token_stride + kv_head * P.head_stride + c * 8;
+    const int len = end - begin - warp * kPart, steps = len > 0 ? (len + kTile - 1) / kTile : 0;      // every 64th key on from the warp's first
+    auto at = [&](int row, int c) { return (uint32_t)((c >> 3) * kHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4)); };
+    auto load = [&](int t) {
+        const uint32_t dst = ring + (t % kStages) * Shape::kStage;
+        const int local = warp * kPart + t * kTile;
+        if constexpr (TMA) {
+            if (t < steps && lane == 0) {
+                const uint32_t b = bar + 8 * (t % kStages);
+                const int box = P.page < kPart ? P.page : kPart;
+                bar_expect(b, Shape::kStage);
+                for (int row = 0; row < kPart; row += box) {
+                    const int in = offset + local + row, pg = page_of(P, in);
+                    const int id = local + row < end - begin ? ids[pg] : -1;      // -1 lies outside the map: zeros
+#pragma unroll
+                    for (int half = 0; half < D / 64; ++half) {
+                        box_load(dst + half * kHalf + row * 128, k_map, b, half * 64, in - pg * P.page, kv_head, id);
+                        box_load(dst + kValues + half * kHalf + row * 128, v_map, b, half * 64, in - pg * P.page, kv_head, id);
+                    }
+                }
             }
-            copy16(smem_at(k_at) + piece<D>(row, c), P.k + at, there);
-            copy16(smem_at(v_at) + piece<D>(row, c), P.v + at, there);
+        } else {
+            if (t < steps) {
+#pragma unroll
+                for (int i = lane; i < kPart * (D / 8); i += 32) {
+                    const int row = i / (D / 8), c = i % (D / 8), in = offset + local + row, pg = page_of(P, in), id = ids[pg];
+                    const bool there = local + row < end - begin && c * 8 < P.d && id >= 0;
+                    const int64_t from = there ? id * P.page_stride + (in - pg * P.page) * P.token_stride + kv_head * P.head_stride + c * 8 : 0;
+                    copy16(dst + at(row, c), P.k + from, there);
+                    copy16(dst + kValues + at(row, c), P.v + from, there);
+                }
+            }
+            asm volatile("cp.async.commit_group;");
         }
-        asm volatile("cp.async.commit_group;");
     };
-    char* ring = smem;
-    load(0, ring, ring + kTileBytes);
+#pragma unroll
+    for (int t = 0; t < kStages; ++t) load(t);
 
     // queries as the left operand: rows lane / 4 and lane / 4 + 8 of the warp's 16
     uint32_t qf[kSteps][4];
@@ -151,39 +212,36 @@ __device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* id
     float o[D / 8][4] = {};
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
-    const int tiles = (end - begin + kTile - 1) / kTile;
-    for (int t = 0; t < tiles; ++t) {
-        char* kt = ring + (t & 1) * 2 * kTileBytes;
-        char* vt = kt + kTileBytes;
-        if (t + 1 < tiles) {
-            char* next = ring + ((t + 1) & 1) * 2 * kTileBytes;
-            load((t + 1) * kTile, next, next + kTileBytes);
-            asm volatile("cp.async.wait_group 1;");
+    bool fine = true;
+    for (int t = 0; t < steps; ++t) {
+        const uint32_t kt = ring + (t % kStages) * Shape::kStage, vt = kt + kValues;
+        const int left = len - t * kTile;                     // keys that are there
+        if constexpr (TMA) {
+            fine = __all_sync(~0u, bar_wait(bar + 8 * (t % kStages), (t / kStages) & 1, gave_up)) && fine;
+            if (left < kPart) {                               // values behind the last key: zeros, whatever the page holds
+                for (int i = lane; i < (kPart - left) * (D / 8); i += 32)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vt + at(left + i / (D / 8), i % (D / 8))), "r"(0) : "memory");
+                __syncwarp();
+            }
         } else {
-            asm volatile("cp.async.wait_group 0;");
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            __syncwarp();
         }
-        __syncthreads();
-        const int key0 = warp * 16;
         float s[kCols][4] = {};
 #pragma unroll
-        for (int j = 0; j < kCols; j += 2) {
-#pragma unroll
-            for (int st = 0; st < kSteps; ++st) {
-                uint32_t b[4];                                // keys j*8 .. j*8+15, dimensions st*16 .. +15
-                const int row = key0 + j * 8 + (lane & 7) + ((lane >> 4) << 3);
-                ldsm4(b, smem_at(kt) + piece<D>(row, st * 2 + ((lane >> 3) & 1)));
-                mma(s[j], qf[st], b);
-                mma(s[j + 1], qf[st], b + 2);
-            }
+        for (int st = 0; st < kSteps; ++st) {
+            uint32_t b[4];                                    // 16 keys, dimensions st*16 .. +15
+            ldsm4(b, kt + at((lane & 7) + ((lane >> 4) << 3), st * 2 + ((lane >> 3) & 1)));
+            mma(s[0], qf[st], b);
+            mma(s[1], qf[st], b + 2);
         }
-        const int left = end - begin - t * kTile;             // keys that are there
-        if (left < kTile || missing) {
+        if (left < kPart || missing) {
 #pragma unroll
             for (int j = 0; j < kCols; ++j)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int key = key0 + j * 8 + (lane & 3) * 2 + e;
-                    const bool there = key < left && (!missing || ids[page_of(P, offset + t * kTile + key)] >= 0);
+                    const int key = j * 8 + (lane & 3) * 2 + e;
+                    const bool there = key < left && (!missing || ids[page_of(P, offset + warp * kPart + t * kTile + key)] >= 0);
                     if (!there) s[j][e] = s[j][2 + e] = -INFINITY;
                 }
         }
@@ -212,28 +270,27 @@ __device__ __forceinline__ void segment(const AttnParams& P, char* smem, int* id
             for (int n = 0; n < D / 8; ++n) { o[n][h * 2] *= fade; o[n][h * 2 + 1] *= fade; }
         }
         // the weights as two bfloat16 parts: what one rounding would lose is as large as the output's own
+        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int j = 0; j < kCols; j += 2) {
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float a = s[j + (e >> 1)][(e & 1) * 2], b = s[j + (e >> 1)][(e & 1) * 2 + 1];
-                hi[e] = pack2(a, b);
-                lo[e] = pack2(a - __uint_as_float(hi[e] << 16), b - __uint_as_float(hi[e] & 0xffff0000u));
-            }
-#pragma unroll
-            for (int n = 0; n < D / 8; n += 2) {
-                uint32_t b[4];                                // keys j*8 .. +15, dimensions n*8 .. +15
-                const int row = key0 + j * 8 + (lane & 15);
-                ldsm4t(b, smem_at(vt) + piece<D>(row, n + (lane >> 4)));
-                mma(o[n], hi, b);
-                mma(o[n], lo, b);
-                mma(o[n + 1], hi, b + 2);
-                mma(o[n + 1], lo, b + 2);
-            }
+        for (int e = 0; e < 4; ++e) {
+            const float x = s[e >> 1][(e & 1) * 2], y = s[e >> 1][(e & 1) * 2 + 1];
+            hi[e] = pack2(x, y);
+            lo[e] = pack2(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xffff0000u));
         }
-        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < D / 8; n += 2) {
+            uint32_t b[4];                                    // 16 keys, dimensions n*8 .. +15
+            ldsm4t(b, vt + at(lane & 15, n + (lane >> 4)));
+            mma(o[n], hi, b);
+            mma(o[n], lo, b);
+            mma(o[n + 1], hi, b + 2);
+            mma(o[n + 1], lo, b + 2);
+        }
+        __syncwarp();
+        load(t + kStages);
     }
+    if (!fine) l[0] = l[1] = __int_as_float(0x7fffffff);
+    __syncthreads();                                          // every warp is done with its stages
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         l[h] += __shfl_xor_sync(~0u, l[h], 1);
@@ -302,15 +359,18 @@ __device__ __forceinline__ bool prefix_tile(const AttnParams& P, int block, Pref
 }
 
 // Tiles of 16 rows: a trajectory's own keys, and prefixes of groups with few rows (blocks below `prefix_blocks`).
-template <int D>
-__global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_constant__ AttnParams P, int prefix_blocks) {
-    extern __shared__ __align__(128) char smem[];
+template <int D, bool TMA>
+__global__ void __launch_bounds__(kThreads)
+attention_kernel(const __grid_constant__ AttnParams P, int prefix_blocks, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    extern __shared__ char raw[];
     __shared__ int ids[kMaxIds + kTile];
+    __shared__ __align__(8) uint64_t bars[4 * OwnShape<D>::kStages];
+    __shared__ int gave_up;
     int block = blockIdx.x;
     if (block < prefix_blocks) {
         PrefixTile t;
         if (!prefix_tile(P, block, &t)) return;
-        segment<D>(P, smem, ids, P.prefix_table + (int64_t)t.group * P.prefix_width, P.prefix_width, t.begin, t.end, t.kv_head, t.first_row,
+        segment<D, TMA>(P, &k_map, &v_map, raw, ids, bars, &gave_up, P.prefix_table + (int64_t)t.group * P.prefix_width, P.prefix_width, t.begin, t.end, t.kv_head, t.first_row,
                    t.rows, t.b0, t.seg);
     } else {
         block -= prefix_blocks;
@@ -321,7 +381,7 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(const __grid_consta
         const int b = block % P.B, seg = block / P.B;
         const int len = clamp_to(P.lens[b], 0, P.max_len), begin = seg * P.own_seg, end = min(len, begin + P.own_seg);
         if (begin >= end) return;
-        segment<D>(P, smem, ids, P.block_table + (int64_t)b * P.own_width, P.own_width, begin, end, kv_head, tile * 16, P.r, b,
+        segment<D, TMA>(P, &k_map, &v_map, raw, ids, bars, &gave_up, P.block_table + (int64_t)b * P.own_width, P.own_width, begin, end, kv_head, tile * 16, P.r, b,
                    P.prefix_segs + seg);
     }
 }
@@ -357,23 +417,6 @@ template <int D, int RT> struct PrefixShape {
     static constexpr int kQ = 128 * D * 2, kColumns = 256 * RT;    // of tensor memory: two score buffers and O, a row tile
     static constexpr int kBytes = RT * kQ + kSlots * kSlot + 1024; // + alignment
 };
-
-__device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
-
-__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
-
-// Bounded: a wait that runs out of polls, or sees that another did, gives up, and the block's rows come out NaN.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int* gave_up) {
-    for (int polls = 0; polls < (1 << 20); ++polls) {
-        uint32_t done;
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return true;
-        if ((polls & 63) == 63 && *gave_up) return false;
-    }
-    *gave_up = 1;
-    return false;
-}
 
 // Matrix instructions and their commits are reached by the whole warp and issued by its elected lane, the same one every
 // time, so that their operands stay in uniform registers.
@@ -423,17 +466,6 @@ __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::l
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-
-__device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
-}
-
 template <int D, bool TMA, int RT>
 __global__ void __launch_bounds__(PrefixShape<D, RT>::kThreads, 3 - RT)
 prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -816,8 +848,10 @@ template <typename F> bool grant(F kernel, int bytes, bool* granted) {
     return granted[dev];
 }
 
-// The cache as a map of boxes [rows of a page, 64 dimensions]; false where the driver takes no such strides.
-bool box_map(CUtensorMap* map, const AttnParams& P, const void* base) {
+// The cache as a map of boxes [at most `rows` places of a page, 64 dimensions]; false where pages cannot be cut into such boxes of at
+// least eight places, or the driver takes no such strides.
+bool box_map(CUtensorMap* map, const AttnParams& P, const void* base, int rows) {
+    if (P.page >= rows ? P.page % rows != 0 : P.page < 8 || rows % P.page != 0) return false;
     typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     static const Encode encode = [] {
@@ -829,7 +863,7 @@ bool box_map(CUtensorMap* map, const AttnParams& P, const void* base) {
     if (encode == nullptr || P.pages < 1) return false;
     const cuuint64_t extent[4] = {(cuuint64_t)P.d, (cuuint64_t)P.page, (cuuint64_t)P.Hk, (cuuint64_t)P.pages};
     const cuuint64_t stride[3] = {(cuuint64_t)P.token_stride * 2, (cuuint64_t)P.head_stride * 2, (cuuint64_t)P.page_stride * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)(P.page < kTile ? P.page : kTile), 1, 1}, step[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(P.page < rows ? P.page : rows), 1, 1}, step[4] = {1, 1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -843,23 +877,31 @@ int launch_prefix(const AttnParams& P, const CUtensorMap& k_map, const CUtensorM
     return RLCS_OK;
 }
 
-template <int D> int launch(const AttnParams& P, cudaStream_t s) {
-    constexpr int kBytes = 4 * kTile * D * 2;
-    static_assert(kBytes >= 4 * 16 * D * 4 + 4 * 16 * 8, "the warps' shares are joined in the tiles' room");
+template <int D, bool TMA>
+int launch_own(const AttnParams& P, int64_t blocks, int prefix_blocks, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t s) {
     static bool granted[64];
-    if (!grant(attention_kernel<D>, kBytes, granted)) return RLCS_ERR_CUDA;
+    if (!grant(attention_kernel<D, TMA>, OwnShape<D>::kBytes, granted)) return RLCS_ERR_CUDA;
+    attention_kernel<D, TMA><<<(unsigned)blocks, kThreads, OwnShape<D>::kBytes, s>>>(P, prefix_blocks, k_map, v_map);
+    return RLCS_OK;
+}
+
+template <int D> int launch(const AttnParams& P, cudaStream_t s) {
+    CUtensorMap k_map = {}, v_map = {};
+    int st = RLCS_OK;
     const bool wide = P.prefix_rows > 16;
     if (wide && P.prefix_blocks > 0) {
-        CUtensorMap k_map = {}, v_map = {};
-        const bool boxes = (P.page >= kTile ? P.page % kTile == 0 : P.page >= 8 && kTile % P.page == 0) && box_map(&k_map, P, P.k) &&
-                           box_map(&v_map, P, P.v);
-        const int st = P.prefix_rows == 256 ? (boxes ? launch_prefix<D, true, 2>(P, k_map, v_map, s) : launch_prefix<D, false, 2>(P, k_map, v_map, s))
-                                            : (boxes ? launch_prefix<D, true, 1>(P, k_map, v_map, s) : launch_prefix<D, false, 1>(P, k_map, v_map, s));
+        const bool boxes = box_map(&k_map, P, P.k, kTile) && box_map(&v_map, P, P.v, kTile);
+        st = P.prefix_rows == 256 ? (boxes ? launch_prefix<D, true, 2>(P, k_map, v_map, s) : launch_prefix<D, false, 2>(P, k_map, v_map, s))
+                                  : (boxes ? launch_prefix<D, true, 1>(P, k_map, v_map, s) : launch_prefix<D, false, 1>(P, k_map, v_map, s));
         if (st != RLCS_OK) return st;
     }
     const int narrow_blocks = wide ? 0 : P.prefix_blocks;
     const int64_t blocks = narrow_blocks + (int64_t)P.own_tiles * P.Hk * P.B * P.own_segs;
-    if (blocks > 0) attention_kernel<D><<<(unsigned)blocks, kThreads, kBytes, s>>>(P, narrow_blocks);
+    if (blocks > 0) {
+        const bool boxes = box_map(&k_map, P, P.k, kPart) && box_map(&v_map, P, P.v, kPart);
+        st = boxes ? launch_own<D, true>(P, blocks, narrow_blocks, k_map, v_map, s) : launch_own<D, false>(P, blocks, narrow_blocks, k_map, v_map, s);
+        if (st != RLCS_OK) return st;
+    }
     join_kernel<D><<<(unsigned)divide_up((int64_t)P.B * P.H, kThreads / 32), kThreads, 0, s>>>(P);
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }
