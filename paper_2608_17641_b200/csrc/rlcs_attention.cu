@@ -132,7 +132,7 @@ __device__ __forceinline__ int read_ids(const AttnParams& P, int* ids, const int
 constexpr int kPart = 16;                       // keys a warp and step
 
 template <int D> struct OwnShape {
-    static constexpr int kHalf = kPart * 128, kStage = 2 * (D / 64) * kHalf, kStages = D == 128 ? 3 : 4;      // K, then V
+    static constexpr int kHalf = kPart * 128, kStage = 2 * (D / 64) * kHalf, kStages = D == 128 ? 2 : 4;      // K, then V
     static constexpr int kBytes = 4 * kStages * kStage + 1024;                                                 // + alignment
     static_assert(4 * kStages * kStage >= 4 * 16 * D * 4 + 4 * 16 * 8, "the warps' shares are joined in the stages' room");
 };
@@ -227,14 +227,18 @@ __device__ __forceinline__ void segment(const AttnParams& P, const CUtensorMap* 
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             __syncwarp();
         }
-        float s[kCols][4] = {};
+        float s[kCols][4] = {}, s2[kCols][4] = {};            // even and odd dimension steps: shorter chains of products
 #pragma unroll
         for (int st = 0; st < kSteps; ++st) {
             uint32_t b[4];                                    // 16 keys, dimensions st*16 .. +15
             ldsm4(b, kt + at((lane & 7) + ((lane >> 4) << 3), st * 2 + ((lane >> 3) & 1)));
-            mma(s[0], qf[st], b);
-            mma(s[1], qf[st], b + 2);
+            mma(st & 1 ? s2[0] : s[0], qf[st], b);
+            mma(st & 1 ? s2[1] : s[1], qf[st], b + 2);
         }
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[j][e] += s2[j][e];
         if (left < kPart || missing) {
 #pragma unroll
             for (int j = 0; j < kCols; ++j)
@@ -252,10 +256,16 @@ __device__ __forceinline__ void segment(const AttnParams& P, const CUtensorMap* 
             for (int j = 0; j < kCols; ++j) top = fmaxf(top, fmaxf(s[j][h * 2], s[j][h * 2 + 1]));
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-            const float now = fmaxf(m[h], top * P.scale_log2);
-            const float base = now == -INFINITY ? 0.f : now;
-            const float fade = exp2_of(m[h] - base);
-            m[h] = now;
+            // the base follows the maximum only when it is 2^8 behind: the weights stay below 2^8, and sums are seldom rescaled
+            const float now = top * P.scale_log2;
+            if (__any_sync(~0u, now > m[h] + 8.f)) {
+                const float next = fmaxf(m[h], now), fade = m[h] == -INFINITY ? 0.f : exp2_of(m[h] - next);
+                m[h] = next;
+                l[h] *= fade;
+#pragma unroll
+                for (int n = 0; n < D / 8; ++n) { o[n][h * 2] *= fade; o[n][h * 2 + 1] *= fade; }
+            }
+            const float base = m[h] == -INFINITY ? 0.f : m[h];
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < kCols; ++j)
@@ -265,9 +275,7 @@ __device__ __forceinline__ void segment(const AttnParams& P, const CUtensorMap* 
                     s[j][h * 2 + e] = p;
                     sum += p;
                 }
-            l[h] = l[h] * fade + sum;
-#pragma unroll
-            for (int n = 0; n < D / 8; ++n) { o[n][h * 2] *= fade; o[n][h * 2 + 1] *= fade; }
+            l[h] += sum;
         }
         // the weights as two bfloat16 parts: what one rounding would lose is as large as the output's own
         uint32_t hi[4], lo[4];
