@@ -14,8 +14,11 @@
 
 #include "../../include/rlcs.h"
 #include "rlcs_device.cuh"
+#include "rlcs_pair.cuh"
 
 namespace {
+
+using namespace rlcs_pair;
 
 struct AttnParams {
     const __nv_bfloat16* q;
@@ -71,12 +74,6 @@ __device__ __forceinline__ void mma(float* c, const uint32_t* a, const uint32_t*
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-__device__ __forceinline__ float exp2_of(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 
@@ -404,21 +401,6 @@ attention_kernel(const __grid_constant__ AttnParams P, int prefix_blocks, const 
 // Pages that divide a tile of 64 keys into parts of at least eight rows, or are whole tiles, are copied by TMA boxes (TMA =
 // true; a segment's last, partial tile apart, whose missing keys must be zeros); other page sizes piece by piece.
 constexpr int kLoaders = 64;
-
-// Two fp32 operations an instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 r;
-    asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 x, x, y, z;\nmov.b64 {%0, %1}, x;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return r;
-}
-
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 r;
-    asm("{\n.reg .b64 x, y;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
 
 template <int D, int RT> struct PrefixShape {
     static constexpr int kThreads = RT * 192 + kLoaders, kSlot = kTile * D * 2, kSlots = D == 128 && RT == 1 ? 4 : 8;

@@ -8,14 +8,19 @@
 // With y_j = l_j - max l, S = sum exp(y_j / T) and U = sum exp(y_j / T) y_j:  lp_j = y_j / T - log S, H = log S - U / (S T),
 // and the bracket is p_j (s + c (H - log S) + (c / T) y_j): one multiply-add a logit on top of its exponential.  The maximum is
 // taken off before the division, so that a masked logit of the type's lowest value cannot overflow.
+#include <cooperative_groups.h>
+
 #include <cmath>
 #include <cstdint>
 
 #include "../../include/rlcs.h"
+#include "rlcs_device.cuh"
+#include "rlcs_pair.cuh"
 #include "rlcs_rows.cuh"
 
 namespace {
 
+using namespace rlcs_pair;
 using namespace rlcs_rows;
 
 template <typename T> struct PolicyParams {
@@ -36,12 +41,6 @@ template <typename T> struct PolicyParams {
 };
 
 constexpr float kLowest = -1.0e30f;      // stands for y = -inf where y multiplies exp(y / T) = 0
-
-__device__ __forceinline__ float exp2_of(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 
 // running maximum with the sums relative to it
 struct Stat {
@@ -64,6 +63,7 @@ __device__ __forceinline__ Stat join(Stat a, Stat b, float exp2_t) {
 // What the gradient pass needs of a row.
 struct RowGrad {
     float c0, c1, inv_s, m, hit;          // dl_j = exp(y / T) * inv_s * (c0 + c1 y), minus `hit` at the action
+                                          // (y times `unit` is y / T)
     bool live;
 };
 
@@ -72,14 +72,15 @@ __device__ __forceinline__ float grad_of(float x, const RowGrad& g, float exp2_t
     return exp2_of(y * exp2_t) * g.inv_s * fmaf(g.c1, fmaxf(y, kLowest), g.c0);
 }
 
+// `d`: (l_a - max) / T; `mean`: U / S in the same unit; `unit`: what turns the sums' unit into that one.
 template <typename T>
-__device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t row, Stat st, float xa, bool live, bool write) {
+__device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t row, Stat st, float d, float mean, float unit, bool live, bool write) {
     live = live && st.m != -INFINITY;
     float loss = 0.f, lp = 0.f, h = 0.f, slope = 0.f;
     const float log_s = logf(st.s);
     if (live) {
-        lp = (xa - st.m) * P.inv_t - log_s;
-        h = log_s - st.u / st.s * P.inv_t;
+        lp = d - log_s;
+        h = log_s - mean;
         if (P.advantages != nullptr) {
             const float adv = P.advantages[row];
             float gain = adv * lp;
@@ -103,20 +104,17 @@ __device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t 
     g.m = st.m;
     g.inv_s = P.inv_t / st.s;
     g.c0 = P.scale * (slope + P.bonus * (h - log_s));
-    g.c1 = P.scale * P.bonus * P.inv_t;
+    g.c1 = P.scale * P.bonus * unit;
     g.hit = P.scale * slope * P.inv_t;
     return g;
 }
 
-// One thread group a row: NT threads of a block (a warp, or the whole block).  Two passes over the row, the second from
-// L2: a thread takes kAhead vectors at a time, so that enough loads are in flight (one at a time: 57 % of the copy
-// bandwidth at 4096 x 131072 bfloat16).
-template <typename T, int NT>
-__global__ void __launch_bounds__(NT < 256 ? 256 : NT) policy_rows_kernel(const __grid_constant__ PolicyParams<T> P) {
-    constexpr int N = Vec<T>::N, kAhead = 4;
-    constexpr int kRows = NT < 256 ? 256 / NT : 1;
-    const int tid = threadIdx.x % NT;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT; row < P.R; row += (int64_t)gridDim.x * kRows) {
+// 65 to 2048 actions: one warp a row, two passes over it, the second from L1 or L2.
+template <typename T>
+__global__ void __launch_bounds__(256) policy_warp_kernel(const __grid_constant__ PolicyParams<T> P) {
+    constexpr int N = Vec<T>::N, kAhead = 2, NT = 32;
+    const int tid = threadIdx.x & 31;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < P.R; row += (int64_t)gridDim.x * 8) {
         const T* x = P.logits + row * P.ld;
         const int a = P.actions[row];
         const bool live = (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < P.A;
@@ -171,15 +169,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) policy_rows_kernel(const 
             const Stat other = {__shfl_xor_sync(~0u, st.m, o), __shfl_xor_sync(~0u, st.s, o), __shfl_xor_sync(~0u, st.u, o)};
             st = join(st, other, P.exp2_t);
         }
-        if constexpr (NT > 32) {
-            __shared__ Stat part[NT / 32];
-            __syncthreads();
-            if ((tid & 31) == 0) part[tid >> 5] = st;
-            __syncthreads();
-            st = part[0];
-            for (int k = 1; k < NT / 32; ++k) st = join(st, part[k], P.exp2_t);
-        }
-        const RowGrad g = finish_row(P, row, st, xa, live, tid == 0);
+        const RowGrad g = finish_row(P, row, st, (xa - st.m) * P.inv_t, st.u / st.s * P.inv_t, P.inv_t, live, tid == 0);
         if (P.dlogits == nullptr) continue;
         T* y = P.dlogits + row * P.ldd;
         if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0) {
@@ -218,6 +208,210 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) policy_rows_kernel(const 
                 Vec<T>::store(y + j, g.live ? grad_of(Vec<T>::load(x + j), g, P.exp2_t) - (j == a ? g.hit : 0.f) : 0.f);
         }
     }
+}
+
+// More actions: one cluster of `ranks` blocks a row.  Each block reads its part once, in batches of four vectors a thread, keeps it in
+// shared memory (STAGED: parts of up to 64 KB, so that three blocks share a multiprocessor), and writes the gradient from there: one
+// read and one write of global memory.  Without the staging the second read of a row came from HBM, not L2: 592 rows of 256 KB in
+// flight are more than it holds (0.68 of the copy bandwidth at 4096 x 131072).  Rows too long for eight parts are read twice.
+//
+// Sums here are in units of log2: t_j = l_j log2(e) / T - M with one fused multiply-add, M the thread's running maximum so
+// scaled (any M serves: it cancels), two logits an instruction.  Logits are held above -1e30, so that t is finite where exp2(t) is
+// 0; a row whose largest logit lies as low as that goes through exact() again.
+constexpr int kBlock = 256, kPart = 64 * 1024, kMostRanks = 8;
+
+template <typename T, bool STAGED>
+__global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_constant__ PolicyParams<T> P) {
+    constexpr int N = Vec<T>::N, kAhead = 4, kWarps = kBlock / 32;
+    constexpr float kLn2 = 0.6931471805599453f;
+    extern __shared__ uint4 held[];
+    __shared__ Stat part[kWarps], cta[2], joined;
+    __shared__ RowGrad grad;
+    namespace cg = cooperative_groups;
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row = blockIdx.x / ranks;
+    const T* x = P.logits + row * P.ld;
+    T* y = P.dlogits != nullptr ? P.dlogits + row * P.ldd : nullptr;
+    const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0;
+    const int a = P.actions[row];
+    bool live = (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < P.A;
+    const Span sp = span_of(x, P.A);
+    const int rest = sp.head + sp.vecs * N, per = (sp.vecs + ranks - 1) / ranks, v0 = min(rank * per, sp.vecs), n = min(per, sp.vecs - v0);
+    const uint4* body = reinterpret_cast<const uint4*>(x + sp.head) + v0;
+    uint4* out = reinterpret_cast<uint4*>(y + sp.head) + v0;
+    // the single elements before and behind the vectors: the first block's first threads
+    const int singles = rank == 0 ? sp.head + P.A - rest : 0, single = tid < sp.head ? tid : rest + tid - sp.head;
+    if (!live) {
+        if (rank == 0 && tid == 0) finish_row(P, row, Stat{-INFINITY, 0.f, 0.f}, 0.f, 0.f, 0.f, false, true);
+        if (y == nullptr) return;
+        if (same) for (int i = tid; i < n; i += kBlock) out[i] = make_uint4(0, 0, 0, 0);
+        else for (int i = tid; i < n * N; i += kBlock) Vec<T>::store(y + sp.head + v0 * N + i, 0.f);
+        if (tid < singles) Vec<T>::store(y + single, 0.f);
+        return;
+    }
+    const float xa = Vec<T>::load(x + a), k = P.exp2_t;
+    const float alone = tid < singles ? Vec<T>::load(x + single) : -INFINITY;
+
+    // `width` lanes' sums joined: the maximum first, then one rescaling a lane
+    auto shuffled = [&](Stat st, int width) {
+        float m = st.m;
+        for (int o = width / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+        if (m != -INFINITY) st = rebase(st, m, 1.f);
+        for (int o = width / 2; o; o >>= 1) {
+            st.s += __shfl_xor_sync(~0u, st.s, o);
+            st.u += __shfl_xor_sync(~0u, st.u, o);
+        }
+        return st;
+    };
+    // over the cluster, for the first warp, the same on every block of it
+    int turn = 0;
+    auto gather = [&](Stat st) {
+        st = shuffled(st, 32);
+        __syncthreads();
+        if (lane == 0) part[warp] = st;
+        __syncthreads();
+        if (warp == 0) st = shuffled(part[lane % kWarps], kWarps);
+        if (ranks > 1) {
+            if (tid == 0) cta[turn] = st;
+            cluster.sync();
+            if (warp == 0) st = shuffled(*cluster.map_shared_rank(&cta[turn], lane % ranks), ranks);
+            turn ^= 1;
+        }
+        return st;
+    };
+    auto gather_all = [&](Stat st) {
+        st = gather(st);
+        if (tid == 0) joined = st;
+        __syncthreads();
+        return joined;
+    };
+    // the plain way, for rows whose logits are all about the lowest there are: (l - max) first
+    auto exact = [&]() {
+        float m = -INFINITY;
+        for (int i = tid; i < n; i += kBlock) {
+            float f[N];
+            Vec<T>::unpack(body[i], f);
+            for (int j = 0; j < N; ++j) m = max_nan(m, f[j]);
+        }
+        m = max_nan(m, alone);
+        m = gather_all(Stat{m, 0.f, 0.f}).m;
+        Stat st = {0.f, 0.f, 0.f};
+        auto take = [&](float f) {
+            const float t = (f - m) * k, w = exp2_of(t);
+            st.s += w;
+            st.u = fmaf(w, fmaxf(t, kLowest), st.u);
+        };
+        if (m != -INFINITY) {
+            for (int i = tid; i < n; i += kBlock) {
+                float f[N];
+                Vec<T>::unpack(body[i], f);
+                for (int j = 0; j < N; ++j) take(f[j]);
+            }
+            if (tid < singles) take(alone);
+        }
+        st = gather_all(st);
+        st.m = m;
+        return st;
+    };
+
+    Stat st = {-INFINITY, 0.f, 0.f};
+    if (tid < singles && alone != -INFINITY) {
+        const float f = max_nan(alone, kLowest);
+        st.m = f * k;
+        st.s = f == f ? 1.f : f;
+    }
+    for (int i = tid; i < n; i += kAhead * kBlock) {
+        uint4 v[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            v[q] = i + q * kBlock < n ? body[i + q * kBlock] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+        uint32_t most = Vec<T>::kNothing;
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            most = Vec<T>::most(most, Vec<T>::most(Vec<T>::most(v[q].x, v[q].y), Vec<T>::most(v[q].z, v[q].w)));
+            v[q].x = Vec<T>::most(v[q].x, Vec<T>::kFloor);
+            v[q].y = Vec<T>::most(v[q].y, Vec<T>::kFloor);
+            v[q].z = Vec<T>::most(v[q].z, Vec<T>::kFloor);
+            v[q].w = Vec<T>::most(v[q].w, Vec<T>::kFloor);
+            if (STAGED && i + q * kBlock < n) held[i + q * kBlock] = v[q];
+        }
+        const float top = Vec<T>::most_of(most);
+        if (top == -INFINITY) continue;
+        const float M = max_nan(top, kLowest) * k;
+        if (M > st.m) st = rebase(st, M, 1.f);
+        const float2 scale = {k, k}, less = {-st.m, -st.m};
+        float2 s = {0.f, 0.f}, u = {0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            float f[N];
+            Vec<T>::unpack(v[q], f);
+#pragma unroll
+            for (int j = 0; j < N; j += 2) {
+                const float2 t = fma2(make_float2(f[j], f[j + 1]), scale, less), w = make_float2(exp2_of(t.x), exp2_of(t.y));
+                s = add2(s, w);
+                u = fma2(w, t, u);
+            }
+        }
+        st.s += s.x + s.y;
+        st.u += u.x + u.y;
+    }
+    st = gather(st);
+    if (warp == 0) {
+        const float d = xa < kLowest ? xa * P.inv_t : fmaf(xa, k, -st.m) * kLn2;
+        // a temperature that takes -1e30 out of range, or logits as low as that: again, the plain way
+        const bool again = k > 1e7f || !(st.m > -1e29f * k);
+        RowGrad g = finish_row(P, row, st, d, st.u / st.s * kLn2, kLn2, true, !again && rank == 0 && tid == 0);
+        g.live = !again;
+        if (tid == 0) grad = g;
+    }
+    __syncthreads();
+    RowGrad g = grad;
+    const bool plain = !g.live;
+    if (plain) {
+        st = exact();
+        g = finish_row(P, row, st, (xa - st.m) * P.inv_t, st.u / st.s * kLn2, kLn2, true, rank == 0 && tid == 0);
+    }
+    if (ranks > 1) cluster.barrier_arrive();                 // done with the others' memory
+    if (y != nullptr) {
+        const float c0 = g.c0 * g.inv_s, c1 = g.c1 * g.inv_s;
+        auto slow = [&](float f, int j) {
+            const float t = plain ? (f - g.m) * k : fmaf(max_nan(f, kLowest), k, -g.m);
+            return g.live ? exp2_of(t) * fmaf(c1, fmaxf(t, kLowest), c0) - (j == a ? g.hit : 0.f) : 0.f;
+        };
+        const float2 scale = {k, k}, less = {-g.m, -g.m}, two0 = {c0, c0}, two1 = {c1, c1};
+        for (int i = tid; i < n; i += kBlock) {
+            const uint4 v = STAGED && !plain ? held[i] : body[i];
+            const int at = sp.head + (v0 + i) * N;
+            float f[N];
+            Vec<T>::unpack(v, f);
+            if (plain || !STAGED) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] = slow(f[j], at + j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; j += 2) {
+                    const float2 t = fma2(make_float2(f[j], f[j + 1]), scale, less);
+                    const float2 r = mul2(make_float2(exp2_of(t.x), exp2_of(t.y)), fma2(two1, t, two0));
+                    f[j] = r.x;
+                    f[j + 1] = r.y;
+                }
+                if (a >= at && a < at + N) {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) f[j] -= at + j == a ? g.hit : 0.f;
+                }
+            }
+            if (same) {
+                out[i] = Vec<T>::pack(f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) Vec<T>::store(y + at + j, f[j]);
+            }
+        }
+        if (tid < singles) Vec<T>::store(y + single, slow(alone, single));
+    }
+    if (ranks > 1) cluster.barrier_wait();                   // no block ends while another may read its memory
 }
 
 // Up to 64 actions: one thread a row.  The block brings its rows to shared memory as fp32 (whole 16-byte vectors where rows follow
@@ -276,7 +470,7 @@ __global__ void __launch_bounds__(kSmallRows) policy_small_kernel(const __grid_c
                 st.u = fmaf(w, fmaxf(y, kLowest), st.u);
             });
         }
-        const RowGrad g = finish_row(P, row, st, xa, live, true);
+        const RowGrad g = finish_row(P, row, st, (xa - st.m) * P.inv_t, st.u / st.s * P.inv_t, P.inv_t, live, true);
         if (to != nullptr) {
             each([&](int j) { x[j] = g.live ? grad_of(x[j], g, P.exp2_t) : 0.f; });
             if (g.live) x[a] -= g.hit;
@@ -333,9 +527,30 @@ int policy_run(const T* logits, int64_t ld, const int32_t* actions, const uint8_
         policy_small_kernel<T><<<(unsigned)blocks, kSmallRows, kSmallRows * A * sizeof(float), s>>>(P, mul);
     } else if (A <= 2048) {
         const int64_t blocks = (R + 7) / 8;
-        policy_rows_kernel<T, 32><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, s>>>(P);
+        policy_warp_kernel<T><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, s>>>(P);
     } else {
-        policy_rows_kernel<T, 512><<<(unsigned)(R < (1 << 20) ? R : (1 << 20)), 512, 0, s>>>(P);
+        // blocks a row: parts of at most 64 KB; more while the GPU has room for two a multiprocessor and a part keeps 8 KB
+        const int64_t bytes = A * (int64_t)sizeof(T);
+        int ranks = 1;
+        while (ranks < kMostRanks && (bytes > (int64_t)ranks * kPart || (R * ranks < 2 * rlcs_device::limits().sms && bytes / (2 * ranks) >= 8192)))
+            ranks *= 2;
+        if (R * ranks > (int64_t(1) << 31) - 1) return RLCS_ERR_SIZE;
+        const bool staged = bytes <= (int64_t)ranks * kPart;
+        const int room = staged ? (int)((bytes / 16 + ranks) / ranks * 16) : 0;
+        const auto kernel = staged ? policy_block_kernel<T, true> : policy_block_kernel<T, false>;
+        if (staged && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPart + 16) != cudaSuccess) return RLCS_ERR_CUDA;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(R * ranks));
+        cfg.blockDim = dim3(kBlock);
+        cfg.dynamicSmemBytes = room;
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = ranks;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaLaunchKernelEx(&cfg, kernel, P) != cudaSuccess) return RLCS_ERR_CUDA;
     }
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }

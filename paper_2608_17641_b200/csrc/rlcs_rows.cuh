@@ -12,6 +12,18 @@ struct bf16 { uint16_t bits; };
 
 template <typename T> struct Vec;                       // one 16-byte access
 
+__device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 template <> struct Vec<float> {
     static constexpr int N = 4;
     static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
@@ -21,6 +33,12 @@ template <> struct Vec<float> {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
     }
     static __device__ __forceinline__ float load(const float* p) { return *p; }
+    static constexpr uint32_t kNothing = 0xff800000u;           // -inf throughout
+    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
+        return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
+    }
+    static __device__ __forceinline__ float most_of(uint32_t a) { return __uint_as_float(a); }
+    static constexpr uint32_t kFloor = 0xf149f2cau;             // -1e30
     static __device__ __forceinline__ void store(float* p, float v) { *p = v; }
 };
 
@@ -41,6 +59,12 @@ template <> struct Vec<bf16> {
     static __device__ __forceinline__ uint4 pack(const float* f) {
         return make_uint4(pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7]));
     }
+    static constexpr uint32_t kNothing = 0xff80ff80u;
+    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) { return max_nan_bf16x2(a, b); }
+    static __device__ __forceinline__ float most_of(uint32_t a) {
+        return max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+    }
+    static constexpr uint32_t kFloor = 0xf149f149u;
     static __device__ __forceinline__ float load(const bf16* p) { return __uint_as_float((uint32_t)p->bits << 16); }
     static __device__ __forceinline__ void store(bf16* p, float v) { p->bits = (uint16_t)(pair(v, 0.f) & 0xffffu); }
 };
