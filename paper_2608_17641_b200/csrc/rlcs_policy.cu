@@ -73,8 +73,18 @@ __device__ __forceinline__ float grad_of(float x, const RowGrad& g, float exp2_t
 }
 
 // `d`: (l_a - max) / T; `mean`: U / S in the same unit; `unit`: what turns the sums' unit into that one.
+// Loaded ahead of the sums: a row's advantage and acting log-probability.
+struct Given {
+    float advantage, old_log_prob;
+};
+
+template <typename T> __device__ __forceinline__ Given given_of(const PolicyParams<T>& P, int64_t row, bool live) {
+    return Given{live && P.advantages != nullptr ? P.advantages[row] : 0.f, live && P.old_log_probs != nullptr ? P.old_log_probs[row] : 0.f};
+}
+
 template <typename T>
-__device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t row, Stat st, float d, float mean, float unit, bool live, bool write) {
+__device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t row, const Given& given, Stat st, float d, float mean, float unit,
+                                              bool live, bool write) {
     live = live && st.m != -INFINITY;
     float loss = 0.f, lp = 0.f, h = 0.f, slope = 0.f;
     const float log_s = logf(st.s);
@@ -82,11 +92,11 @@ __device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t 
         lp = d - log_s;
         h = log_s - mean;
         if (P.advantages != nullptr) {
-            const float adv = P.advantages[row];
+            const float adv = given.advantage;
             float gain = adv * lp;
             slope = adv;
             if (P.old_log_probs != nullptr) {
-                const float ratio = expf(lp - P.old_log_probs[row]);
+                const float ratio = expf(lp - given.old_log_prob);
                 const float free_ = ratio * adv, held = fminf(fmaxf(ratio, 1.f - P.clip), 1.f + P.clip) * adv;
                 gain = fminf(free_, held);
                 slope = free_ <= held ? free_ : 0.f;
@@ -118,6 +128,7 @@ __global__ void __launch_bounds__(256) policy_warp_kernel(const __grid_constant_
         const T* x = P.logits + row * P.ld;
         const int a = P.actions[row];
         const bool live = (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < P.A;
+        const Given given = given_of(P, row, live);
         const Span sp = span_of(x, P.A);
         const int rest = sp.head + sp.vecs * N;
         const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
@@ -169,7 +180,7 @@ __global__ void __launch_bounds__(256) policy_warp_kernel(const __grid_constant_
             const Stat other = {__shfl_xor_sync(~0u, st.m, o), __shfl_xor_sync(~0u, st.s, o), __shfl_xor_sync(~0u, st.u, o)};
             st = join(st, other, P.exp2_t);
         }
-        const RowGrad g = finish_row(P, row, st, (xa - st.m) * P.inv_t, st.u / st.s * P.inv_t, P.inv_t, live, tid == 0);
+        const RowGrad g = finish_row(P, row, given, st, (xa - st.m) * P.inv_t, st.u / st.s * P.inv_t, P.inv_t, live, tid == 0);
         if (P.dlogits == nullptr) continue;
         T* y = P.dlogits + row * P.ldd;
         if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0) {
@@ -210,50 +221,82 @@ __global__ void __launch_bounds__(256) policy_warp_kernel(const __grid_constant_
     }
 }
 
-// More actions: one cluster of `ranks` blocks a row.  Each block reads its part once, in batches of four vectors a thread, keeps it in
-// shared memory (STAGED: parts of up to 64 KB, so that three blocks share a multiprocessor), and writes the gradient from there: one
-// read and one write of global memory.  Without the staging the second read of a row came from HBM, not L2: 592 rows of 256 KB in
-// flight are more than it holds (0.68 of the copy bandwidth at 4096 x 131072).  Rows too long for eight parts are read twice.
+// More actions: one cluster of `ranks` blocks a row, row after row.  Each block copies its part of a row to shared memory once (STAGED:
+// parts of up to 64 KB in four chunks, so that three blocks share a multiprocessor), sums, and writes the gradient from there; as
+// a chunk's gradient is written, the next row's chunk is on its way into its place.  One read and one write of global memory:
+// without the staging a row's second read came from HBM, not L2 (592 rows of 256 KB in flight are more than it holds; 0.68 of the copy
+// bandwidth at 4096 x 131072).  Rows too long for eight parts are read twice.
 //
 // Sums here are in units of log2: t_j = l_j log2(e) / T - M with one fused multiply-add, M the thread's running maximum so
 // scaled (any M serves: it cancels), two logits an instruction.  Logits are held above -1e30, so that t is finite where exp2(t) is
 // 0; a row whose largest logit lies as low as that goes through exact() again.
-constexpr int kBlock = 256, kPart = 64 * 1024, kMostRanks = 8;
+constexpr int kBlock = 256, kChunk = 4 * kBlock, kChunks = 4, kPart = kChunks * kChunk * 16, kMostRanks = 8;
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// Bounded; a wait that runs out leaves NaN in the row's outputs.
+__device__ __forceinline__ bool chunk_wait(uint32_t bar, int parity) {
+    for (int polls = 0; polls < (1 << 20); ++polls) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+
+// One row as a block of the cluster sees it.
+template <typename T> struct RowPart {
+    int64_t row;
+    const T* x;
+    int a, v0, n;                        // its vectors: n from v0 on
+    Span sp;
+    bool live;
+
+    __device__ __forceinline__ RowPart(const PolicyParams<T>& P, int64_t row_, int rank, int ranks) : row(row_) {
+        live = false;
+        x = nullptr;
+        a = v0 = n = 0;
+        sp = Span{0, 0};
+        if (row >= P.R) return;
+        x = P.logits + row * P.ld;
+        a = P.actions[row];
+        live = (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < P.A;
+        sp = span_of(x, P.A);
+        const int per = (sp.vecs + ranks - 1) / ranks;
+        v0 = min(rank * per, sp.vecs);
+        n = min(per, sp.vecs - v0);
+    }
+    __device__ __forceinline__ const uint4* body() const { return reinterpret_cast<const uint4*>(x + sp.head) + v0; }
+};
 
 template <typename T, bool STAGED>
 __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_constant__ PolicyParams<T> P) {
-    constexpr int N = Vec<T>::N, kAhead = 4, kWarps = kBlock / 32;
+    constexpr int N = Vec<T>::N, kAhead = kChunk / kBlock, kWarps = kBlock / 32;
     constexpr float kLn2 = 0.6931471805599453f;
     extern __shared__ uint4 held[];
     __shared__ Stat part[kWarps], cta[2], joined;
     __shared__ RowGrad grad;
+    __shared__ __align__(8) uint64_t full[kChunks];
     namespace cg = cooperative_groups;
     const cg::cluster_group cluster = cg::this_cluster();
-    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), clusters = gridDim.x / ranks;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t row = blockIdx.x / ranks;
-    const T* x = P.logits + row * P.ld;
-    T* y = P.dlogits != nullptr ? P.dlogits + row * P.ldd : nullptr;
-    const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0;
-    const int a = P.actions[row];
-    bool live = (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < P.A;
-    const Span sp = span_of(x, P.A);
-    const int rest = sp.head + sp.vecs * N, per = (sp.vecs + ranks - 1) / ranks, v0 = min(rank * per, sp.vecs), n = min(per, sp.vecs - v0);
-    const uint4* body = reinterpret_cast<const uint4*>(x + sp.head) + v0;
-    uint4* out = reinterpret_cast<uint4*>(y + sp.head) + v0;
-    // the single elements before and behind the vectors: the first block's first threads
-    const int singles = rank == 0 ? sp.head + P.A - rest : 0, single = tid < sp.head ? tid : rest + tid - sp.head;
-    if (!live) {
-        if (rank == 0 && tid == 0) finish_row(P, row, Stat{-INFINITY, 0.f, 0.f}, 0.f, 0.f, 0.f, false, true);
-        if (y == nullptr) return;
-        if (same) for (int i = tid; i < n; i += kBlock) out[i] = make_uint4(0, 0, 0, 0);
-        else for (int i = tid; i < n * N; i += kBlock) Vec<T>::store(y + sp.head + v0 * N + i, 0.f);
-        if (tid < singles) Vec<T>::store(y + single, 0.f);
-        return;
+    const float k = P.exp2_t;
+    if (STAGED && tid < kChunks) {
+        asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"(smem_at(&full[tid])));
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    const float xa = Vec<T>::load(x + a), k = P.exp2_t;
-    const float alone = tid < singles ? Vec<T>::load(x + single) : -INFINITY;
+    __syncthreads();
 
+    auto fetch = [&](const RowPart<T>& r, int c) {           // by one thread; every chunk of a live row, empty ones too
+        const int left = r.n - c * kChunk, count = left < 0 ? 0 : min(left, kChunk);
+        const uint32_t bar = smem_at(&full[c]);
+        asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(count * 16) : "memory");
+        if (count > 0)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(smem_at(held + c * kChunk)), "l"(r.body() + c * kChunk), "r"(count * 16), "r"(bar) : "memory");
+    };
     // `width` lanes' sums joined: the maximum first, then one rescaling a lane
     auto shuffled = [&](Stat st, int width) {
         float m = st.m;
@@ -269,7 +312,6 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
     int turn = 0;
     auto gather = [&](Stat st) {
         st = shuffled(st, 32);
-        __syncthreads();
         if (lane == 0) part[warp] = st;
         __syncthreads();
         if (warp == 0) st = shuffled(part[lane % kWarps], kWarps);
@@ -285,133 +327,176 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         st = gather(st);
         if (tid == 0) joined = st;
         __syncthreads();
-        return joined;
-    };
-    // the plain way, for rows whose logits are all about the lowest there are: (l - max) first
-    auto exact = [&]() {
-        float m = -INFINITY;
-        for (int i = tid; i < n; i += kBlock) {
-            float f[N];
-            Vec<T>::unpack(body[i], f);
-            for (int j = 0; j < N; ++j) m = max_nan(m, f[j]);
-        }
-        m = max_nan(m, alone);
-        m = gather_all(Stat{m, 0.f, 0.f}).m;
-        Stat st = {0.f, 0.f, 0.f};
-        auto take = [&](float f) {
-            const float t = (f - m) * k, w = exp2_of(t);
-            st.s += w;
-            st.u = fmaf(w, fmaxf(t, kLowest), st.u);
-        };
-        if (m != -INFINITY) {
-            for (int i = tid; i < n; i += kBlock) {
-                float f[N];
-                Vec<T>::unpack(body[i], f);
-                for (int j = 0; j < N; ++j) take(f[j]);
-            }
-            if (tid < singles) take(alone);
-        }
-        st = gather_all(st);
-        st.m = m;
+        st = joined;
+        __syncthreads();
         return st;
     };
 
-    Stat st = {-INFINITY, 0.f, 0.f};
-    if (tid < singles && alone != -INFINITY) {
-        const float f = max_nan(alone, kLowest);
-        st.m = f * k;
-        st.s = f == f ? 1.f : f;
-    }
-    for (int i = tid; i < n; i += kAhead * kBlock) {
-        uint4 v[kAhead];
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q)
-            v[q] = i + q * kBlock < n ? body[i + q * kBlock] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
-        uint32_t most = Vec<T>::kNothing;
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            most = Vec<T>::most(most, Vec<T>::most(Vec<T>::most(v[q].x, v[q].y), Vec<T>::most(v[q].z, v[q].w)));
-            v[q].x = Vec<T>::most(v[q].x, Vec<T>::kFloor);
-            v[q].y = Vec<T>::most(v[q].y, Vec<T>::kFloor);
-            v[q].z = Vec<T>::most(v[q].z, Vec<T>::kFloor);
-            v[q].w = Vec<T>::most(v[q].w, Vec<T>::kFloor);
-            if (STAGED && i + q * kBlock < n) held[i + q * kBlock] = v[q];
-        }
-        const float top = Vec<T>::most_of(most);
-        if (top == -INFINITY) continue;
-        const float M = max_nan(top, kLowest) * k;
-        if (M > st.m) st = rebase(st, M, 1.f);
-        const float2 scale = {k, k}, less = {-st.m, -st.m};
-        float2 s = {0.f, 0.f}, u = {0.f, 0.f};
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            float f[N];
-            Vec<T>::unpack(v[q], f);
-#pragma unroll
-            for (int j = 0; j < N; j += 2) {
-                const float2 t = fma2(make_float2(f[j], f[j + 1]), scale, less), w = make_float2(exp2_of(t.x), exp2_of(t.y));
-                s = add2(s, w);
-                u = fma2(w, t, u);
+    RowPart<T> now(P, blockIdx.x / ranks, rank, ranks);
+    int loads = 0;                                           // rows fetched: the chunks' barriers go by its last bit
+    if (STAGED && tid == 0 && now.live)
+        for (int c = 0; c < kChunks; ++c) fetch(now, c);
+    while (now.row < P.R) {
+        const RowPart<T> next(P, now.row + clusters, rank, ranks);
+        const T* x = now.x;
+        T* y = P.dlogits != nullptr ? P.dlogits + now.row * P.ldd : nullptr;
+        const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0;
+        const int a = now.a, head = now.sp.head, rest = head + now.sp.vecs * N, v0 = now.v0, n = now.n;
+        const uint4* body = now.body();
+        uint4* out = reinterpret_cast<uint4*>(y + head) + v0;
+        // the single elements before and behind the vectors: the first block's first threads
+        const int singles = rank == 0 ? head + P.A - rest : 0, single = tid < head ? tid : rest + tid - head;
+        const Given given = given_of(P, now.row, now.live);
+        if (!now.live) {
+            if (rank == 0 && tid == 0) finish_row(P, now.row, given, Stat{-INFINITY, 0.f, 0.f}, 0.f, 0.f, 0.f, false, true);
+            if (y != nullptr) {
+                if (same) for (int i = tid; i < n; i += kBlock) out[i] = make_uint4(0, 0, 0, 0);
+                else for (int i = tid; i < n * N; i += kBlock) Vec<T>::store(y + head + v0 * N + i, 0.f);
+                if (tid < singles) Vec<T>::store(y + single, 0.f);
             }
+            if (STAGED && tid == 0 && next.live)
+                for (int c = 0; c < kChunks; ++c) fetch(next, c);
+            now = next;
+            continue;
         }
-        st.s += s.x + s.y;
-        st.u += u.x + u.y;
-    }
-    st = gather(st);
-    if (warp == 0) {
-        const float d = xa < kLowest ? xa * P.inv_t : fmaf(xa, k, -st.m) * kLn2;
-        // a temperature that takes -1e30 out of range, or logits as low as that: again, the plain way
-        const bool again = k > 1e7f || !(st.m > -1e29f * k);
-        RowGrad g = finish_row(P, row, st, d, st.u / st.s * kLn2, kLn2, true, !again && rank == 0 && tid == 0);
-        g.live = !again;
-        if (tid == 0) grad = g;
-    }
-    __syncthreads();
-    RowGrad g = grad;
-    const bool plain = !g.live;
-    if (plain) {
-        st = exact();
-        g = finish_row(P, row, st, (xa - st.m) * P.inv_t, st.u / st.s * kLn2, kLn2, true, rank == 0 && tid == 0);
-    }
-    if (ranks > 1) cluster.barrier_arrive();                 // done with the others' memory
-    if (y != nullptr) {
+        const float xa = Vec<T>::load(x + a);
+        const float alone = tid < singles ? Vec<T>::load(x + single) : -INFINITY;
+        // the plain way, for rows whose logits are all about the lowest there are: (l - max) first
+        auto exact = [&]() {
+            float m = -INFINITY;
+            for (int i = tid; i < n; i += kBlock) {
+                float f[N];
+                Vec<T>::unpack(body[i], f);
+                for (int j = 0; j < N; ++j) m = max_nan(m, f[j]);
+            }
+            m = max_nan(m, alone);
+            m = gather_all(Stat{m, 0.f, 0.f}).m;
+            Stat st = {0.f, 0.f, 0.f};
+            auto take = [&](float f) {
+                const float t = (f - m) * k, w = exp2_of(t);
+                st.s += w;
+                st.u = fmaf(w, fmaxf(t, kLowest), st.u);
+            };
+            if (m != -INFINITY) {
+                for (int i = tid; i < n; i += kBlock) {
+                    float f[N];
+                    Vec<T>::unpack(body[i], f);
+                    for (int j = 0; j < N; ++j) take(f[j]);
+                }
+                if (tid < singles) take(alone);
+            }
+            st = gather_all(st);
+            st.m = m;
+            return st;
+        };
+
+        Stat st = {-INFINITY, 0.f, 0.f};
+        if (tid < singles && alone != -INFINITY) {
+            const float f = max_nan(alone, kLowest);
+            st.m = f * k;
+            st.s = f == f ? 1.f : f;
+        }
+        for (int c = 0; c * kChunk < n; ++c) {
+            if (STAGED && !chunk_wait(smem_at(&full[c & (kChunks - 1)]), loads & 1)) st.s = __int_as_float(0x7fffffff);
+            const uint4* from = STAGED ? held : body;
+            const int i = c * kChunk + tid;
+            uint4 v[kAhead];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                v[q] = i + q * kBlock < n ? from[i + q * kBlock] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+            uint32_t most = Vec<T>::kNothing;
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) most = Vec<T>::most(most, Vec<T>::most(Vec<T>::most(v[q].x, v[q].y), Vec<T>::most(v[q].z, v[q].w)));
+            const float top = Vec<T>::most_of(most);
+            if (top == -INFINITY) continue;
+            const float M = max_nan(top, kLowest) * k;
+            if (M > st.m) st = rebase(st, M, 1.f);
+            const float2 scale = {k, k}, less = {-st.m, -st.m};
+            float2 s = {0.f, 0.f}, u = {0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                float f[N];
+                Vec<T>::unpack(Vec<T>::floored(v[q]), f);
+#pragma unroll
+                for (int j = 0; j < N; j += 2) {
+                    const float2 t = fma2(make_float2(f[j], f[j + 1]), scale, less), w = make_float2(exp2_of(t.x), exp2_of(t.y));
+                    s = add2(s, w);
+                    u = fma2(w, t, u);
+                }
+            }
+            st.s += s.x + s.y;
+            st.u += u.x + u.y;
+        }
+        if (STAGED)                                          // empty chunks have a phase too
+            for (int c = (n + kChunk - 1) / kChunk; c < kChunks; ++c) chunk_wait(smem_at(&full[c]), loads & 1);
+        ++loads;
+        st = gather(st);
+        if (warp == 0) {
+            const float d = xa < kLowest ? xa * P.inv_t : fmaf(xa, k, -st.m) * kLn2;
+            // a temperature that takes -1e30 out of range, or logits as low as that: again, the plain way
+            const bool again = k > 1e7f || !(st.m > -1e29f * k);
+            RowGrad g = finish_row(P, now.row, given, st, d, st.u / st.s * kLn2, kLn2, true, !again && rank == 0 && tid == 0);
+            g.live = !again;
+            if (tid == 0) grad = g;
+        }
+        __syncthreads();
+        RowGrad g = grad;
+        const bool plain = !g.live;
+        if (plain) {
+            st = exact();
+            g = finish_row(P, now.row, given, st, (xa - st.m) * P.inv_t, st.u / st.s * kLn2, kLn2, true, rank == 0 && tid == 0);
+        }
+        if (ranks > 1) cluster.barrier_arrive();             // done with the others' memory
         const float c0 = g.c0 * g.inv_s, c1 = g.c1 * g.inv_s;
+        const float2 scale = {k, k}, less = {-g.m, -g.m}, two0 = {c0, c0}, two1 = {c1, c1};
         auto slow = [&](float f, int j) {
             const float t = plain ? (f - g.m) * k : fmaf(max_nan(f, kLowest), k, -g.m);
             return g.live ? exp2_of(t) * fmaf(c1, fmaxf(t, kLowest), c0) - (j == a ? g.hit : 0.f) : 0.f;
         };
-        const float2 scale = {k, k}, less = {-g.m, -g.m}, two0 = {c0, c0}, two1 = {c1, c1};
-        for (int i = tid; i < n; i += kBlock) {
-            const uint4 v = STAGED && !plain ? held[i] : body[i];
-            const int at = sp.head + (v0 + i) * N;
-            float f[N];
-            Vec<T>::unpack(v, f);
-            if (plain || !STAGED) {
+        for (int c = 0; c < kChunks || c * kChunk < n; ++c) {
+            if (y != nullptr) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) f[j] = slow(f[j], at + j);
-            } else {
+                for (int q = 0; q < kAhead; ++q) {
+                    const int i = c * kChunk + q * kBlock + tid;
+                    if (i >= n) break;
+                    const int at = head + (v0 + i) * N;
+                    float f[N];
+                    if (plain) {
+                        Vec<T>::unpack(body[i], f);
 #pragma unroll
-                for (int j = 0; j < N; j += 2) {
-                    const float2 t = fma2(make_float2(f[j], f[j + 1]), scale, less);
-                    const float2 r = mul2(make_float2(exp2_of(t.x), exp2_of(t.y)), fma2(two1, t, two0));
-                    f[j] = r.x;
-                    f[j + 1] = r.y;
-                }
-                if (a >= at && a < at + N) {
+                        for (int j = 0; j < N; ++j) f[j] = slow(f[j], at + j);
+                    } else {
+                        Vec<T>::unpack(Vec<T>::floored(STAGED ? held[i] : body[i]), f);
 #pragma unroll
-                    for (int j = 0; j < N; ++j) f[j] -= at + j == a ? g.hit : 0.f;
+                        for (int j = 0; j < N; j += 2) {
+                            const float2 t = fma2(make_float2(f[j], f[j + 1]), scale, less);
+                            const float2 r = mul2(make_float2(exp2_of(t.x), exp2_of(t.y)), fma2(two1, t, two0));
+                            f[j] = r.x;
+                            f[j + 1] = r.y;
+                        }
+                        if (a >= at && a < at + N) {
+#pragma unroll
+                            for (int j = 0; j < N; ++j) f[j] -= at + j == a ? g.hit : 0.f;
+                        }
+                    }
+                    if (same) {
+                        out[i] = Vec<T>::pack(f);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < N; ++j) Vec<T>::store(y + at + j, f[j]);
+                    }
                 }
             }
-            if (same) {
-                out[i] = Vec<T>::pack(f);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) Vec<T>::store(y + at + j, f[j]);
+            if (STAGED) {
+                __syncthreads();                             // the chunk's place is free
+                if (tid == 0 && next.live) fetch(next, c);
             }
         }
-        if (tid < singles) Vec<T>::store(y + single, slow(alone, single));
+        if (y != nullptr && tid < singles) Vec<T>::store(y + single, slow(alone, single));
+        if (ranks > 1) cluster.barrier_wait();               // the others are done with this block's memory
+        else if (!STAGED) __syncthreads();
+        now = next;
     }
-    if (ranks > 1) cluster.barrier_wait();                   // no block ends while another may read its memory
 }
 
 // Up to 64 actions: one thread a row.  The block brings its rows to shared memory as fp32 (whole 16-byte vectors where rows follow
@@ -450,6 +535,7 @@ __global__ void __launch_bounds__(kSmallRows) policy_small_kernel(const __grid_c
         float* x = tile + tid * A;
         const int a = P.actions[row];
         const bool live = (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < A;
+        const Given given = given_of(P, row, live);
         const int first = A & 1 ? 0 : tid % A;
         // every element once, from the thread's own place on
         auto each = [&](auto f) {
@@ -470,7 +556,7 @@ __global__ void __launch_bounds__(kSmallRows) policy_small_kernel(const __grid_c
                 st.u = fmaf(w, fmaxf(y, kLowest), st.u);
             });
         }
-        const RowGrad g = finish_row(P, row, st, (xa - st.m) * P.inv_t, st.u / st.s * P.inv_t, P.inv_t, live, true);
+        const RowGrad g = finish_row(P, row, given, st, (xa - st.m) * P.inv_t, st.u / st.s * P.inv_t, P.inv_t, live, true);
         if (to != nullptr) {
             each([&](int j) { x[j] = g.live ? grad_of(x[j], g, P.exp2_t) : 0.f; });
             if (g.live) x[a] -= g.hit;
@@ -500,6 +586,36 @@ __global__ void __launch_bounds__(kSmallRows) policy_small_kernel(const __grid_c
 }
 
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// One cluster a row, as many as the GPU holds at once: asked for once a device and cluster size, with the room of the largest part
+// (a cluster too many would start when the others have ended and double the time).
+template <typename T, bool STAGED>
+int launch_block(const PolicyParams<T>& P, int ranks, int room, cudaStream_t s) {
+    const auto kernel = policy_block_kernel<T, STAGED>;
+    static int at_once[64][kMostRanks + 1];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RLCS_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ranks);
+    cfg.blockDim = dim3(kBlock);
+    cfg.dynamicSmemBytes = STAGED ? kPart + 16 : 0;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (at_once[dev][ranks] == 0) {
+        if (STAGED && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPart + 16) != cudaSuccess) return RLCS_ERR_CUDA;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return RLCS_ERR_CUDA;
+        at_once[dev][ranks] = n;
+    }
+    cfg.gridDim = dim3((unsigned)((P.R < at_once[dev][ranks] ? P.R : at_once[dev][ranks]) * ranks));
+    cfg.dynamicSmemBytes = room;
+    return cudaLaunchKernelEx(&cfg, kernel, P) == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
+}
 
 template <typename T>
 int policy_run(const T* logits, int64_t ld, const int32_t* actions, const uint8_t* mask, const float* advantages,
@@ -534,23 +650,9 @@ int policy_run(const T* logits, int64_t ld, const int32_t* actions, const uint8_
         int ranks = 1;
         while (ranks < kMostRanks && (bytes > (int64_t)ranks * kPart || (R * ranks < 2 * rlcs_device::limits().sms && bytes / (2 * ranks) >= 8192)))
             ranks *= 2;
-        if (R * ranks > (int64_t(1) << 31) - 1) return RLCS_ERR_SIZE;
         const bool staged = bytes <= (int64_t)ranks * kPart;
-        const int room = staged ? (int)((bytes / 16 + ranks) / ranks * 16) : 0;
-        const auto kernel = staged ? policy_block_kernel<T, true> : policy_block_kernel<T, false>;
-        if (staged && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPart + 16) != cudaSuccess) return RLCS_ERR_CUDA;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(R * ranks));
-        cfg.blockDim = dim3(kBlock);
-        cfg.dynamicSmemBytes = room;
-        cfg.stream = s;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = ranks;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        if (cudaLaunchKernelEx(&cfg, kernel, P) != cudaSuccess) return RLCS_ERR_CUDA;
+        const int st = staged ? launch_block<T, true>(P, ranks, (int)((bytes / 16 + ranks) / ranks * 16), s) : launch_block<T, false>(P, ranks, 0, s);
+        if (st != RLCS_OK) return st;
     }
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }

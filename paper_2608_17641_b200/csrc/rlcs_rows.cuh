@@ -39,6 +39,9 @@ template <> struct Vec<float> {
     }
     static __device__ __forceinline__ float most_of(uint32_t a) { return __uint_as_float(a); }
     static constexpr uint32_t kFloor = 0xf149f2cau;             // -1e30
+    static __device__ __forceinline__ uint4 floored(const uint4& v) {      // nothing below about -1e30
+        return make_uint4(most(v.x, kFloor), most(v.y, kFloor), most(v.z, kFloor), most(v.w, kFloor));
+    }
     static __device__ __forceinline__ void store(float* p, float v) { *p = v; }
 };
 
@@ -65,6 +68,9 @@ template <> struct Vec<bf16> {
         return max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
     }
     static constexpr uint32_t kFloor = 0xf149f149u;
+    static __device__ __forceinline__ uint4 floored(const uint4& v) {      // nothing below about -1e30
+        return make_uint4(most(v.x, kFloor), most(v.y, kFloor), most(v.z, kFloor), most(v.w, kFloor));
+    }
     static __device__ __forceinline__ float load(const bf16* p) { return __uint_as_float((uint32_t)p->bits << 16); }
     static __device__ __forceinline__ void store(bf16* p, float v) { p->bits = (uint16_t)(pair(v, 0.f) & 0xffffu); }
 };
