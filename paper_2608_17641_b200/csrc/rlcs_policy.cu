@@ -222,15 +222,18 @@ __global__ void __launch_bounds__(256) policy_warp_kernel(const __grid_constant_
 }
 
 // More actions: one cluster of `ranks` blocks a row, row after row.  Each block copies its part of a row to shared memory once (STAGED:
-// parts of up to 64 KB in four chunks, so that three blocks share a multiprocessor), sums, and writes the gradient from there; as
-// a chunk's gradient is written, the next row's chunk is on its way into its place.  One read and one write of global memory:
+// parts of up to 64 KB, so that three blocks share a multiprocessor), sums, and writes the gradient from there.  Every warp has
+// a contiguous share in four chunks, which it fetches itself: as a chunk's gradient is written, the next row's chunk is on
+// its way into its place, without a barrier.  The blocks of a cluster send one another their sums (st.async onto a barrier that
+// counts bytes): a cluster barrier would wait for the gradient's stores.  One read and one write of global memory:
 // without the staging a row's second read came from HBM, not L2 (592 rows of 256 KB in flight are more than it holds; 0.68 of the copy
 // bandwidth at 4096 x 131072).  Rows too long for eight parts are read twice.
 //
 // Sums here are in units of log2: t_j = l_j log2(e) / T - M with one fused multiply-add, M the thread's running maximum so
 // scaled (any M serves: it cancels), two logits an instruction.  Logits are held above -1e30, so that t is finite where exp2(t) is
 // 0; a row whose largest logit lies as low as that goes through exact() again.
-constexpr int kBlock = 256, kChunk = 4 * kBlock, kChunks = 4, kPart = kChunks * kChunk * 16, kMostRanks = 8;
+constexpr int kBlock = 256, kWarps = kBlock / 32, kAhead = 4, kChunk = kAhead * 32, kChunks = 4, kShare = kChunks * kChunk;      // vectors of a warp
+constexpr int kPart = kWarps * kShare * 16, kMostRanks = 8;
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -238,14 +241,14 @@ __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__
 __device__ __forceinline__ bool chunk_wait(uint32_t bar, int parity) {
     for (int polls = 0; polls < (1 << 20); ++polls) {
         uint32_t done;
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
         if (done) return true;
     }
     return false;
 }
 
-// One row as a block of the cluster sees it.
+// One row as a warp of the cluster sees it.
 template <typename T> struct RowPart {
     int64_t row;
     const T* x;
@@ -253,7 +256,8 @@ template <typename T> struct RowPart {
     Span sp;
     bool live;
 
-    __device__ __forceinline__ RowPart(const PolicyParams<T>& P, int64_t row_, int rank, int ranks) : row(row_) {
+    // `log_warps`: log2 of the cluster's warps
+    __device__ __forceinline__ RowPart(const PolicyParams<T>& P, int64_t row_, int warp, int log_warps) : row(row_) {
         live = false;
         x = nullptr;
         a = v0 = n = 0;
@@ -263,8 +267,8 @@ template <typename T> struct RowPart {
         a = P.actions[row];
         live = (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < P.A;
         sp = span_of(x, P.A);
-        const int per = (sp.vecs + ranks - 1) / ranks;
-        v0 = min(rank * per, sp.vecs);
+        const int per = (sp.vecs + (1 << log_warps) - 1) >> log_warps;
+        v0 = min(warp * per, sp.vecs);
         n = min(per, sp.vecs - v0);
     }
     __device__ __forceinline__ const uint4* body() const { return reinterpret_cast<const uint4*>(x + sp.head) + v0; }
@@ -272,26 +276,27 @@ template <typename T> struct RowPart {
 
 template <typename T, bool STAGED>
 __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_constant__ PolicyParams<T> P) {
-    constexpr int N = Vec<T>::N, kAhead = kChunk / kBlock, kWarps = kBlock / 32;
+    constexpr int N = Vec<T>::N;
     constexpr float kLn2 = 0.6931471805599453f;
-    extern __shared__ uint4 held[];
-    __shared__ Stat part[kWarps], cta[2], joined;
+    extern __shared__ uint4 held_all[];
+    __shared__ Stat part[kWarps], joined;
+    __shared__ __align__(16) float4 sent[2][kMostRanks];
     __shared__ RowGrad grad;
-    __shared__ __align__(8) uint64_t full[kChunks];
+    __shared__ __align__(8) uint64_t full[kWarps][kChunks], got[2];
     namespace cg = cooperative_groups;
     const cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), clusters = gridDim.x / ranks;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, my_warp = rank * kWarps + warp, log_warps = 31 - __clz(ranks * kWarps);
     const float k = P.exp2_t;
-    if (STAGED && tid < kChunks) {
-        asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"(smem_at(&full[tid])));
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
+    uint4* const held = held_all + warp * kShare;
+    if (tid < kWarps * kChunks) asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"(smem_at(&full[0][0] + tid)));
+    if (tid < 2) asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"(smem_at(&got[tid])));
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    cluster.sync();
 
-    auto fetch = [&](const RowPart<T>& r, int c) {           // by one thread; every chunk of a live row, empty ones too
+    auto fetch = [&](const RowPart<T>& r, int c) {           // by one lane; every chunk of a live row, empty ones too
         const int left = r.n - c * kChunk, count = left < 0 ? 0 : min(left, kChunk);
-        const uint32_t bar = smem_at(&full[c]);
+        const uint32_t bar = smem_at(&full[warp][c]);
         asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(count * 16) : "memory");
         if (count > 0)
             asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -308,19 +313,32 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         }
         return st;
     };
-    // over the cluster, for the first warp, the same on every block of it
-    int turn = 0;
+    // Over the cluster, for the first warp, the same on every block of it.  Two sets of places for what the blocks send, taken in
+    // turn: a block sends the sums after the next only when it has everybody's next, and nobody sends those before it has read.
+    int turns = 0;
     auto gather = [&](Stat st) {
         st = shuffled(st, 32);
         if (lane == 0) part[warp] = st;
         __syncthreads();
-        if (warp == 0) st = shuffled(part[lane % kWarps], kWarps);
-        if (ranks > 1) {
-            if (tid == 0) cta[turn] = st;
-            cluster.sync();
-            if (warp == 0) st = shuffled(*cluster.map_shared_rank(&cta[turn], lane % ranks), ranks);
-            turn ^= 1;
+        if (warp == 0) {
+            st = shuffled(part[lane % kWarps], kWarps);
+            if (ranks > 1) {
+                const int turn = turns & 1;
+                const uint32_t bar = smem_at(&got[turn]), place = smem_at(&sent[turn][rank]);
+                if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(ranks * 16) : "memory");
+                if (lane < ranks) {
+                    uint32_t there, its_bar;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(place), "r"(lane));
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(its_bar) : "r"(bar), "r"(lane));
+                    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                                 ::"r"(there), "r"(__float_as_uint(st.m)), "r"(__float_as_uint(st.s)), "r"(__float_as_uint(st.u)), "r"(0), "r"(its_bar) : "memory");
+                }
+                const bool fine = chunk_wait(bar, (turns >> 1) & 1);
+                const float4 v = sent[turn][lane % ranks];
+                st = shuffled(Stat{v.x, fine ? v.y : __int_as_float(0x7fffffff), v.z}, ranks);
+            }
         }
+        ++turns;
         return st;
     };
     auto gather_all = [&](Stat st) {
@@ -332,12 +350,12 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         return st;
     };
 
-    RowPart<T> now(P, blockIdx.x / ranks, rank, ranks);
+    RowPart<T> now(P, blockIdx.x / ranks, my_warp, log_warps);
     int loads = 0;                                           // rows fetched: the chunks' barriers go by its last bit
-    if (STAGED && tid == 0 && now.live)
+    if (STAGED && lane == 0 && now.live)
         for (int c = 0; c < kChunks; ++c) fetch(now, c);
     while (now.row < P.R) {
-        const RowPart<T> next(P, now.row + clusters, rank, ranks);
+        const RowPart<T> next(P, now.row + clusters, my_warp, log_warps);
         const T* x = now.x;
         T* y = P.dlogits != nullptr ? P.dlogits + now.row * P.ldd : nullptr;
         const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0;
@@ -350,11 +368,11 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         if (!now.live) {
             if (rank == 0 && tid == 0) finish_row(P, now.row, given, Stat{-INFINITY, 0.f, 0.f}, 0.f, 0.f, 0.f, false, true);
             if (y != nullptr) {
-                if (same) for (int i = tid; i < n; i += kBlock) out[i] = make_uint4(0, 0, 0, 0);
-                else for (int i = tid; i < n * N; i += kBlock) Vec<T>::store(y + head + v0 * N + i, 0.f);
+                if (same) for (int i = lane; i < n; i += 32) out[i] = make_uint4(0, 0, 0, 0);
+                else for (int i = lane; i < n * N; i += 32) Vec<T>::store(y + head + v0 * N + i, 0.f);
                 if (tid < singles) Vec<T>::store(y + single, 0.f);
             }
-            if (STAGED && tid == 0 && next.live)
+            if (STAGED && lane == 0 && next.live)
                 for (int c = 0; c < kChunks; ++c) fetch(next, c);
             now = next;
             continue;
@@ -364,7 +382,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         // the plain way, for rows whose logits are all about the lowest there are: (l - max) first
         auto exact = [&]() {
             float m = -INFINITY;
-            for (int i = tid; i < n; i += kBlock) {
+            for (int i = lane; i < n; i += 32) {
                 float f[N];
                 Vec<T>::unpack(body[i], f);
                 for (int j = 0; j < N; ++j) m = max_nan(m, f[j]);
@@ -378,7 +396,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
                 st.u = fmaf(w, fmaxf(t, kLowest), st.u);
             };
             if (m != -INFINITY) {
-                for (int i = tid; i < n; i += kBlock) {
+                for (int i = lane; i < n; i += 32) {
                     float f[N];
                     Vec<T>::unpack(body[i], f);
                     for (int j = 0; j < N; ++j) take(f[j]);
@@ -397,13 +415,13 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             st.s = f == f ? 1.f : f;
         }
         for (int c = 0; c * kChunk < n; ++c) {
-            if (STAGED && !chunk_wait(smem_at(&full[c & (kChunks - 1)]), loads & 1)) st.s = __int_as_float(0x7fffffff);
+            if (STAGED && !chunk_wait(smem_at(&full[warp][c & (kChunks - 1)]), loads & 1)) st.s = __int_as_float(0x7fffffff);
             const uint4* from = STAGED ? held : body;
-            const int i = c * kChunk + tid;
+            const int i = c * kChunk + lane;
             uint4 v[kAhead];
 #pragma unroll
             for (int q = 0; q < kAhead; ++q)
-                v[q] = i + q * kBlock < n ? from[i + q * kBlock] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+                v[q] = i + q * 32 < n ? from[i + q * 32] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
             uint32_t most = Vec<T>::kNothing;
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) most = Vec<T>::most(most, Vec<T>::most(Vec<T>::most(v[q].x, v[q].y), Vec<T>::most(v[q].z, v[q].w)));
@@ -428,7 +446,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             st.u += u.x + u.y;
         }
         if (STAGED)                                          // empty chunks have a phase too
-            for (int c = (n + kChunk - 1) / kChunk; c < kChunks; ++c) chunk_wait(smem_at(&full[c]), loads & 1);
+            for (int c = (n + kChunk - 1) / kChunk; c < kChunks; ++c) chunk_wait(smem_at(&full[warp][c]), loads & 1);
         ++loads;
         st = gather(st);
         if (warp == 0) {
@@ -446,7 +464,6 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             st = exact();
             g = finish_row(P, now.row, given, st, (xa - st.m) * P.inv_t, st.u / st.s * kLn2, kLn2, true, rank == 0 && tid == 0);
         }
-        if (ranks > 1) cluster.barrier_arrive();             // done with the others' memory
         const float c0 = g.c0 * g.inv_s, c1 = g.c1 * g.inv_s;
         const float2 scale = {k, k}, less = {-g.m, -g.m}, two0 = {c0, c0}, two1 = {c1, c1};
         auto slow = [&](float f, int j) {
@@ -457,7 +474,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             if (y != nullptr) {
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q) {
-                    const int i = c * kChunk + q * kBlock + tid;
+                    const int i = c * kChunk + q * 32 + lane;
                     if (i >= n) break;
                     const int at = head + (v0 + i) * N;
                     float f[N];
@@ -488,13 +505,11 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
                 }
             }
             if (STAGED) {
-                __syncthreads();                             // the chunk's place is free
-                if (tid == 0 && next.live) fetch(next, c);
+                __syncwarp();                                // the chunk's place is free
+                if (lane == 0 && next.live) fetch(next, c);
             }
         }
         if (y != nullptr && tid < singles) Vec<T>::store(y + single, slow(alone, single));
-        if (ranks > 1) cluster.barrier_wait();               // the others are done with this block's memory
-        else if (!STAGED) __syncthreads();
         now = next;
     }
 }
@@ -587,10 +602,9 @@ __global__ void __launch_bounds__(kSmallRows) policy_small_kernel(const __grid_c
 
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// One cluster a row, as many as the GPU holds at once: asked for once a device and cluster size, with the room of the largest part
-// (a cluster too many would start when the others have ended and double the time).
+// One cluster a row, as many as the GPU holds at once: asked for once a device and cluster size (a cluster too many would start when the others have ended and double the time).
 template <typename T, bool STAGED>
-int launch_block(const PolicyParams<T>& P, int ranks, int room, cudaStream_t s) {
+int launch_block(const PolicyParams<T>& P, int ranks, cudaStream_t s) {
     const auto kernel = policy_block_kernel<T, STAGED>;
     static int at_once[64][kMostRanks + 1];
     int dev = 0;
@@ -598,7 +612,7 @@ int launch_block(const PolicyParams<T>& P, int ranks, int room, cudaStream_t s) 
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ranks);
     cfg.blockDim = dim3(kBlock);
-    cfg.dynamicSmemBytes = STAGED ? kPart + 16 : 0;
+    cfg.dynamicSmemBytes = STAGED ? kPart : 0;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -607,13 +621,12 @@ int launch_block(const PolicyParams<T>& P, int ranks, int room, cudaStream_t s) 
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (at_once[dev][ranks] == 0) {
-        if (STAGED && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPart + 16) != cudaSuccess) return RLCS_ERR_CUDA;
+        if (STAGED && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPart) != cudaSuccess) return RLCS_ERR_CUDA;
         int n = 0;
         if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return RLCS_ERR_CUDA;
         at_once[dev][ranks] = n;
     }
     cfg.gridDim = dim3((unsigned)((P.R < at_once[dev][ranks] ? P.R : at_once[dev][ranks]) * ranks));
-    cfg.dynamicSmemBytes = room;
     return cudaLaunchKernelEx(&cfg, kernel, P) == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }
 
@@ -651,7 +664,7 @@ int policy_run(const T* logits, int64_t ld, const int32_t* actions, const uint8_
         while (ranks < kMostRanks && (bytes > (int64_t)ranks * kPart || (R * ranks < 2 * rlcs_device::limits().sms && bytes / (2 * ranks) >= 8192)))
             ranks *= 2;
         const bool staged = bytes <= (int64_t)ranks * kPart;
-        const int st = staged ? launch_block<T, true>(P, ranks, (int)((bytes / 16 + ranks) / ranks * 16), s) : launch_block<T, false>(P, ranks, 0, s);
+        const int st = staged ? launch_block<T, true>(P, ranks, s) : launch_block<T, false>(P, ranks, s);
         if (st != RLCS_OK) return st;
     }
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
