@@ -414,19 +414,18 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             st.m = f * k;
             st.s = f == f ? 1.f : f;
         }
-        for (int c = 0; c * kChunk < n; ++c) {
-            if (STAGED && !chunk_wait(smem_at(&full[warp][c & (kChunks - 1)]), loads & 1)) st.s = __int_as_float(0x7fffffff);
-            const uint4* from = STAGED ? held : body;
-            const int i = c * kChunk + lane;
+        auto sum_chunk = [&](int c, auto whole) {            // whole: no vector of the chunk lies behind the row's end
+            const uint4* from = (STAGED ? held : body) + c * kChunk + lane;
+            const int left = n - c * kChunk - lane;
             uint4 v[kAhead];
 #pragma unroll
             for (int q = 0; q < kAhead; ++q)
-                v[q] = i + q * 32 < n ? from[i + q * 32] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+                v[q] = whole() || q * 32 < left ? from[q * 32] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
             uint32_t most = Vec<T>::kNothing;
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) most = Vec<T>::most(most, Vec<T>::most(Vec<T>::most(v[q].x, v[q].y), Vec<T>::most(v[q].z, v[q].w)));
             const float top = Vec<T>::most_of(most);
-            if (top == -INFINITY) continue;
+            if (top == -INFINITY) return;
             const float M = max_nan(top, kLowest) * k;
             if (M > st.m) st = rebase(st, M, 1.f);
             const float2 scale = {k, k}, less = {-st.m, -st.m};
@@ -444,6 +443,10 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             }
             st.s += s.x + s.y;
             st.u += u.x + u.y;
+        };
+        for (int c = 0; c * kChunk < n; ++c) {
+            if (STAGED && !chunk_wait(smem_at(&full[warp][c & (kChunks - 1)]), loads & 1)) st.s = __int_as_float(0x7fffffff);
+            if ((c + 1) * kChunk <= n) sum_chunk(c, [] { return true; }); else sum_chunk(c, [] { return false; });
         }
         if (STAGED)                                          // empty chunks have a phase too
             for (int c = (n + kChunk - 1) / kChunk; c < kChunks; ++c) chunk_wait(smem_at(&full[warp][c]), loads & 1);
@@ -470,39 +473,46 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             const float t = plain ? (f - g.m) * k : fmaf(max_nan(f, kLowest), k, -g.m);
             return g.live ? exp2_of(t) * fmaf(c1, fmaxf(t, kLowest), c0) - (j == a ? g.hit : 0.f) : 0.f;
         };
-        for (int c = 0; c < kChunks || c * kChunk < n; ++c) {
-            if (y != nullptr) {
+        auto give_chunk = [&](int c, auto whole) {           // whole: as above, and the action is in none of its vectors
+            const uint4* from = (STAGED ? held : body) + c * kChunk + lane;
+            uint4* to = out + c * kChunk + lane;
+            const int left = n - c * kChunk - lane;
 #pragma unroll
-                for (int q = 0; q < kAhead; ++q) {
-                    const int i = c * kChunk + q * 32 + lane;
-                    if (i >= n) break;
-                    const int at = head + (v0 + i) * N;
-                    float f[N];
-                    if (plain) {
-                        Vec<T>::unpack(body[i], f);
+            for (int q = 0; q < kAhead; ++q) {
+                if (!whole() && q * 32 >= left) break;
+                const int at = head + (v0 + c * kChunk + q * 32 + lane) * N;
+                float f[N];
+                if (!whole() && plain) {
+                    Vec<T>::unpack(body[c * kChunk + q * 32 + lane], f);
 #pragma unroll
-                        for (int j = 0; j < N; ++j) f[j] = slow(f[j], at + j);
-                    } else {
-                        Vec<T>::unpack(Vec<T>::floored(STAGED ? held[i] : body[i]), f);
+                    for (int j = 0; j < N; ++j) f[j] = slow(f[j], at + j);
+                } else {
+                    Vec<T>::unpack(Vec<T>::floored(from[q * 32]), f);
 #pragma unroll
-                        for (int j = 0; j < N; j += 2) {
-                            const float2 t = fma2(make_float2(f[j], f[j + 1]), scale, less);
-                            const float2 r = mul2(make_float2(exp2_of(t.x), exp2_of(t.y)), fma2(two1, t, two0));
-                            f[j] = r.x;
-                            f[j + 1] = r.y;
-                        }
-                        if (a >= at && a < at + N) {
-#pragma unroll
-                            for (int j = 0; j < N; ++j) f[j] -= at + j == a ? g.hit : 0.f;
-                        }
+                    for (int j = 0; j < N; j += 2) {
+                        const float2 t = fma2(make_float2(f[j], f[j + 1]), scale, less);
+                        const float2 r = mul2(make_float2(exp2_of(t.x), exp2_of(t.y)), fma2(two1, t, two0));
+                        f[j] = r.x;
+                        f[j + 1] = r.y;
                     }
-                    if (same) {
-                        out[i] = Vec<T>::pack(f);
-                    } else {
+                    if (!whole()) {
 #pragma unroll
-                        for (int j = 0; j < N; ++j) Vec<T>::store(y + at + j, f[j]);
+                        for (int j = 0; j < N; ++j) f[j] -= at + j == a ? g.hit : 0.f;
                     }
                 }
+                if (whole() || same) {
+                    to[q * 32] = Vec<T>::pack(f);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) Vec<T>::store(y + at + j, f[j]);
+                }
+            }
+        };
+        const int hit_at = a < head ? -1 : (a - head) / N - v0;      // the action's vector of this warp's
+        for (int c = 0; c < kChunks || c * kChunk < n; ++c) {
+            if (y != nullptr) {
+                const bool hit = hit_at >= c * kChunk && hit_at < (c + 1) * kChunk;
+                if ((c + 1) * kChunk <= n && !hit && same && !plain) give_chunk(c, [] { return true; }); else give_chunk(c, [] { return false; });
             }
             if (STAGED) {
                 __syncwarp();                                // the chunk's place is free
