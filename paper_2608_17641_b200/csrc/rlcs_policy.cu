@@ -72,7 +72,7 @@ __device__ __forceinline__ float grad_of(float x, const RowGrad& g, float exp2_t
     return exp2_of(y * exp2_t) * g.inv_s * fmaf(g.c1, fmaxf(y, kLowest), g.c0);
 }
 
-// `d`: (l_a - max) / T; `mean`: U / S in the same unit; `unit`: what turns the sums' unit into that one.
+// `d`: (l_a - max) / T; `unit`: what turns the unit of U into that of d.
 // Loaded ahead of the sums: a row's advantage and acting log-probability.
 struct Given {
     float advantage, old_log_prob;
@@ -83,14 +83,14 @@ template <typename T> __device__ __forceinline__ Given given_of(const PolicyPara
 }
 
 template <typename T>
-__device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t row, const Given& given, Stat st, float d, float mean, float unit,
-                                              bool live, bool write) {
+__device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t row, const Given& given, Stat st, float d, float unit, bool live,
+                                              bool write) {
     live = live && st.m != -INFINITY;
     float loss = 0.f, lp = 0.f, h = 0.f, slope = 0.f;
-    const float log_s = logf(st.s);
+    const float log_s = logf(st.s), inv = 1.f / st.s;
     if (live) {
         lp = d - log_s;
-        h = log_s - mean;
+        h = log_s - st.u * inv * unit;
         if (P.advantages != nullptr) {
             const float adv = given.advantage;
             float gain = adv * lp;
@@ -112,7 +112,7 @@ __device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t 
     RowGrad g;
     g.live = live;
     g.m = st.m;
-    g.inv_s = P.inv_t / st.s;
+    g.inv_s = P.inv_t * inv;
     g.c0 = P.scale * (slope + P.bonus * (h - log_s));
     g.c1 = P.scale * P.bonus * unit;
     g.hit = P.scale * slope * P.inv_t;
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(256) policy_warp_kernel(const __grid_constant_
             const Stat other = {__shfl_xor_sync(~0u, st.m, o), __shfl_xor_sync(~0u, st.s, o), __shfl_xor_sync(~0u, st.u, o)};
             st = join(st, other, P.exp2_t);
         }
-        const RowGrad g = finish_row(P, row, given, st, (xa - st.m) * P.inv_t, st.u / st.s * P.inv_t, P.inv_t, live, tid == 0);
+        const RowGrad g = finish_row(P, row, given, st, (xa - st.m) * P.inv_t, P.inv_t, live, tid == 0);
         if (P.dlogits == nullptr) continue;
         T* y = P.dlogits + row * P.ldd;
         if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0) {
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         const int singles = rank == 0 ? head + P.A - rest : 0, single = tid < head ? tid : rest + tid - head;
         const Given given = given_of(P, now.row, now.live);
         if (!now.live) {
-            if (rank == 0 && tid == 0) finish_row(P, now.row, given, Stat{-INFINITY, 0.f, 0.f}, 0.f, 0.f, 0.f, false, true);
+            if (rank == 0 && tid == 0) finish_row(P, now.row, given, Stat{-INFINITY, 0.f, 0.f}, 0.f, 0.f, false, true);
             if (y != nullptr) {
                 if (same) for (int i = lane; i < n; i += 32) out[i] = make_uint4(0, 0, 0, 0);
                 else for (int i = lane; i < n * N; i += 32) Vec<T>::store(y + head + v0 * N + i, 0.f);
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             const float d = xa < kLowest ? xa * P.inv_t : fmaf(xa, k, -st.m) * kLn2;
             // a temperature that takes -1e30 out of range, or logits as low as that: again, the plain way
             const bool again = k > 1e7f || !(st.m > -1e29f * k);
-            RowGrad g = finish_row(P, now.row, given, st, d, st.u / st.s * kLn2, kLn2, true, !again && rank == 0 && tid == 0);
+            RowGrad g = finish_row(P, now.row, given, st, d, kLn2, true, !again && rank == 0 && tid == 0);
             g.live = !again;
             if (tid == 0) grad = g;
         }
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         const bool plain = !g.live;
         if (plain) {
             st = exact();
-            g = finish_row(P, now.row, given, st, (xa - st.m) * P.inv_t, st.u / st.s * kLn2, kLn2, true, rank == 0 && tid == 0);
+            g = finish_row(P, now.row, given, st, (xa - st.m) * P.inv_t, kLn2, true, rank == 0 && tid == 0);
         }
         const float c0 = g.c0 * g.inv_s, c1 = g.c1 * g.inv_s;
         const float2 scale = {k, k}, less = {-g.m, -g.m}, two0 = {c0, c0}, two1 = {c1, c1};
@@ -524,67 +524,100 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
     }
 }
 
-// Up to 64 actions: one thread a row.  The block brings its rows to shared memory as fp32 (whole 16-byte vectors where rows follow
-// one another), a thread walks its own row there, and the gradients leave the same way.  Rows of an even number of actions are
-// walked from a place of their own each, so that the threads of a warp meet different banks.
+// Up to 64 actions: one thread a row.  The block brings its rows to shared memory as fp32 (16-byte loads where rows follow one
+// another), a thread walks its own row there, and the gradients leave the same way.  Rows lie an odd number of words apart, so that
+// the threads of a warp meet different banks, and every thread takes the same number of steps (walking from a place of its own
+// instead cost four times the instructions).
 constexpr int kSmallRows = 128, kSmallA = 64;
 
 template <typename T>
 __global__ void __launch_bounds__(kSmallRows) policy_small_kernel(const __grid_constant__ PolicyParams<T> P, uint32_t a_mul) {
     constexpr int N = Vec<T>::N;
     extern __shared__ __align__(16) float tile[];
-    const int A = P.A, tid = threadIdx.x;
+    const int A = P.A, stride = A | 1, gap = stride - A, tid = threadIdx.x;
     const int64_t row0 = (int64_t)blockIdx.x * kSmallRows, row = row0 + tid;
     const int rows = P.R - row0 < kSmallRows ? (int)(P.R - row0) : kSmallRows, n = rows * A;
     const T* from = P.logits + row0 * P.ld;
     T* to = P.dlogits != nullptr ? P.dlogits + row0 * P.ldd : nullptr;
     auto of = [&](int i) { return a_mul != 0 ? (int)__umulhi((uint32_t)i, a_mul) : i; };      // the row of flat element i
+    // flat vectors to and from the rows' places
+    auto put = [&](int i, const float* f) {
+        if (gap == 0) {
+#pragma unroll
+            for (int k = 0; k < N; k += 4) *reinterpret_cast<float4*>(tile + i + k) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k += 2) {                 // A is even, and so is i: two neighbours share a row
+                const int at = i + k + (int)__umulhi((uint32_t)(i + k), a_mul);
+                tile[at] = f[k];
+                tile[at + 1] = f[k + 1];
+            }
+        }
+    };
+    auto get = [&](int i, float* f) {
+        if (gap == 0) {
+#pragma unroll
+            for (int k = 0; k < N; k += 4) {
+                const float4 v = *reinterpret_cast<const float4*>(tile + i + k);
+                f[k] = v.x; f[k + 1] = v.y; f[k + 2] = v.z; f[k + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k += 2) {
+                const int at = i + k + (int)__umulhi((uint32_t)(i + k), a_mul);
+                f[k] = tile[at];
+                f[k + 1] = tile[at + 1];
+            }
+        }
+    };
+    const int a = tid < rows ? P.actions[row] : -1;
+    const bool live = tid < rows && (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < A;
+    const Given given = given_of(P, row, live);
     if (P.ld == A && (reinterpret_cast<uintptr_t>(from) & 15) == 0) {
 #pragma unroll 4
         for (int i = tid * N; i < n - N + 1; i += kSmallRows * N) {
             float f[N];
             Vec<T>::unpack(*reinterpret_cast<const uint4*>(from + i), f);
-#pragma unroll
-            for (int k = 0; k < N; k += 4) *reinterpret_cast<float4*>(tile + i + k) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
+            put(i, f);
         }
-        for (int i = n / N * N + tid; i < n; i += kSmallRows) tile[i] = Vec<T>::load(from + i);
+        for (int i = n / N * N + tid; i < n; i += kSmallRows) tile[i + gap * of(i)] = Vec<T>::load(from + i);
     } else {
 #pragma unroll 4
         for (int i = tid; i < n; i += kSmallRows) {
             const int r = of(i);
-            tile[i] = Vec<T>::load(from + r * P.ld + (i - r * A));
+            tile[i + gap * r] = Vec<T>::load(from + r * P.ld + (i - r * A));
         }
     }
     __syncthreads();
     if (tid < rows) {
-        float* x = tile + tid * A;
-        const int a = P.actions[row];
-        const bool live = (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < A;
-        const Given given = given_of(P, row, live);
-        const int first = A & 1 ? 0 : tid % A;
-        // every element once, from the thread's own place on
-        auto each = [&](auto f) {
-#pragma unroll 4
-            for (int j = first; j < A; ++j) f(j);
-#pragma unroll 4
-            for (int j = 0; j < first; ++j) f(j);
-        };
+        float* x = tile + tid * stride;
         Stat st = {-INFINITY, 0.f, 0.f};
         float xa = 0.f;
         if (live) {
             xa = x[a];
-            each([&](int j) { st.m = fmaxf(st.m, x[j]); });
+#pragma unroll 4
+            for (int j = 0; j < A; ++j) st.m = fmaxf(st.m, x[j]);
             const float base = st.m == -INFINITY ? 0.f : st.m;
-            each([&](int j) {
+#pragma unroll 4
+            for (int j = 0; j < A; ++j) {
                 const float y = x[j] - base, w = exp2_of(y * P.exp2_t);
                 st.s += w;
                 st.u = fmaf(w, fmaxf(y, kLowest), st.u);
-            });
+            }
         }
-        const RowGrad g = finish_row(P, row, given, st, (xa - st.m) * P.inv_t, st.u / st.s * P.inv_t, P.inv_t, live, true);
+        const RowGrad g = finish_row(P, row, given, st, (xa - st.m) * P.inv_t, P.inv_t, live, true);
         if (to != nullptr) {
-            each([&](int j) { x[j] = g.live ? grad_of(x[j], g, P.exp2_t) : 0.f; });
-            if (g.live) x[a] -= g.hit;
+            const float c0 = g.c0 * g.inv_s, c1 = g.c1 * g.inv_s;
+            if (g.live) {
+#pragma unroll 4
+                for (int j = 0; j < A; ++j) {
+                    const float y = x[j] - g.m;
+                    x[j] = exp2_of(y * P.exp2_t) * fmaf(c1, fmaxf(y, kLowest), c0);
+                }
+                x[a] -= g.hit;
+            } else {
+                for (int j = 0; j < A; ++j) x[j] = 0.f;
+            }
         }
     }
     if (to == nullptr) return;
@@ -593,19 +626,15 @@ __global__ void __launch_bounds__(kSmallRows) policy_small_kernel(const __grid_c
 #pragma unroll 4
         for (int i = tid * N; i < n - N + 1; i += kSmallRows * N) {
             float f[N];
-#pragma unroll
-            for (int k = 0; k < N; k += 4) {
-                const float4 v = *reinterpret_cast<const float4*>(tile + i + k);
-                f[k] = v.x; f[k + 1] = v.y; f[k + 2] = v.z; f[k + 3] = v.w;
-            }
+            get(i, f);
             *reinterpret_cast<uint4*>(to + i) = Vec<T>::pack(f);
         }
-        for (int i = n / N * N + tid; i < n; i += kSmallRows) Vec<T>::store(to + i, tile[i]);
+        for (int i = n / N * N + tid; i < n; i += kSmallRows) Vec<T>::store(to + i, tile[i + gap * of(i)]);
     } else {
 #pragma unroll 4
         for (int i = tid; i < n; i += kSmallRows) {
             const int r = of(i);
-            Vec<T>::store(to + r * P.ldd + (i - r * A), tile[i]);
+            Vec<T>::store(to + r * P.ldd + (i - r * A), tile[i + gap * r]);
         }
     }
 }
@@ -663,7 +692,7 @@ int policy_run(const T* logits, int64_t ld, const int32_t* actions, const uint8_
         const int64_t blocks = (R + kSmallRows - 1) / kSmallRows;
         if (blocks > (int64_t(1) << 31) - 1) return RLCS_ERR_SIZE;
         const uint32_t mul = A > 1 ? (uint32_t)(((uint64_t(1) << 32) + A - 1) / A) : 0;
-        policy_small_kernel<T><<<(unsigned)blocks, kSmallRows, kSmallRows * A * sizeof(float), s>>>(P, mul);
+        policy_small_kernel<T><<<(unsigned)blocks, kSmallRows, kSmallRows * (A | 1) * sizeof(float), s>>>(P, mul);
     } else if (A <= 2048) {
         const int64_t blocks = (R + 7) / 8;
         policy_warp_kernel<T><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, s>>>(P);
