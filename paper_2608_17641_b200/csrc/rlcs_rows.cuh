@@ -38,6 +38,10 @@ template <> struct Vec<float> {
         return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
     }
     static __device__ __forceinline__ float most_of(uint32_t a) { return __uint_as_float(a); }
+    static __device__ __forceinline__ uint32_t most_number(uint32_t a, uint32_t b) {      // NaN aside
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }
+    static __device__ __forceinline__ float most_number_of(uint32_t a) { return fmaxf(__uint_as_float(a), -INFINITY); }
     static constexpr uint32_t kFloor = 0xf149f2cau;             // -1e30
     static __device__ __forceinline__ uint4 floored(const uint4& v) {      // nothing below about -1e30
         return make_uint4(most(v.x, kFloor), most(v.y, kFloor), most(v.z, kFloor), most(v.w, kFloor));
@@ -66,6 +70,14 @@ template <> struct Vec<bf16> {
     static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) { return max_nan_bf16x2(a, b); }
     static __device__ __forceinline__ float most_of(uint32_t a) {
         return max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+    }
+    static __device__ __forceinline__ uint32_t most_number(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ float most_number_of(uint32_t a) {
+        return fmaxf(fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u)), -INFINITY);
     }
     static constexpr uint32_t kFloor = 0xf149f149u;
     static __device__ __forceinline__ uint4 floored(const uint4& v) {      // nothing below about -1e30

@@ -10,10 +10,12 @@
 
 #include "../../include/rlcs.h"
 #include "rlcs_device.cuh"
+#include "rlcs_pair.cuh"
 #include "rlcs_rows.cuh"
 
 namespace {
 
+using namespace rlcs_pair;
 using namespace rlcs_rows;
 typedef unsigned long long u64;
 
@@ -75,7 +77,7 @@ template <typename T> __device__ __forceinline__ Rules rules_of(const SamplePara
     r.p = P.top_p != nullptr ? P.top_p[row] : P.top_p_all;
     r.low = P.min_p != nullptr ? P.min_p[row] : P.min_p_all;
     const bool greedy = !(t > 0.f);
-    r.inv_t = greedy ? 1.f : 1.f / t;
+    r.inv_t = greedy ? 1.f : fminf(1.f / t, 3.4028235e38f);       // finite: 0 stays 0 in what it multiplies
     r.limit = k > 0 && k < P.A ? k : P.A;
     if (greedy || r.p <= 0.f || r.low > 1.f) r.limit = 1;
     if (!(r.low > 0.f) || r.low > 1.f) r.low = 0.f;
@@ -351,19 +353,49 @@ template <typename T> struct ClusterRow {
     __device__ __forceinline__ bool last_warp() const { return rank == ranks - 1 && warp == kW - 1; }
     __device__ __forceinline__ int tail_at() const { return sp.head + sp.vecs * Vec<T>::N; }
 
-    // f(logit, index) for every element of the warp's range
+    // f(logit, index) for every element of the warp's range, four vectors of a lane in flight; places behind the range hold
+    // -inf.  Logits come as they are: NaN compares false and -0 equal to 0.
     template <typename F> __device__ __forceinline__ void each(F f) const {
-        constexpr int N = Vec<T>::N;
-        if (first_warp() && lane < sp.head) f(clean(Vec<T>::load(x + lane)), lane);
-#pragma unroll 2
-        for (int v = v0 + lane; v < v1; v += 32) {
-            const int at = sp.head + v * N;
-            float g[N];
-            Vec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(x + at)), g);
+        constexpr int N = Vec<T>::N, kAhead = 4;
+        const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
+        const uint4 nothing = make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+        uint4 g[kAhead];
 #pragma unroll
-            for (int k = 0; k < N; ++k) f(clean(g[k]), at + k);
+        for (int q = 0; q < kAhead; ++q) g[q] = v0 + lane + 32 * q < v1 ? __ldg(body + v0 + lane + 32 * q) : nothing;
+#pragma unroll 1
+        for (int v = v0 + lane; v - lane < v1; v += 32) {    // one copy of f's code a vector: the kernel has many such passes
+            float e[N];
+            Vec<T>::unpack(g[0], e);
+#pragma unroll
+            for (int q = 0; q + 1 < kAhead; ++q) g[q] = g[q + 1];
+            g[kAhead - 1] = v + 32 * kAhead < v1 ? __ldg(body + v + 32 * kAhead) : nothing;
+#pragma unroll
+            for (int k = 0; k < N; ++k) f(e[k], sp.head + v * N + k);
         }
-        if (last_warp() && tail_at() + lane < A) f(clean(Vec<T>::load(x + tail_at() + lane)), tail_at() + lane);
+        const int singles = first_warp() ? sp.head : 0, ends = last_warp() ? A - tail_at() : 0;
+        if (lane < singles + ends) {
+            const int j = lane < singles ? lane : tail_at() + lane - singles;
+            f(Vec<T>::load(x + j), j);
+        }
+    }
+    // the largest logit of the lane's elements
+    __device__ __forceinline__ float most() const {
+        constexpr int kAhead = 8;
+        uint32_t top = Vec<T>::kNothing;
+        const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
+        for (int v = v0 + lane; v < v1; v += 32 * kAhead) {
+            uint4 g[kAhead];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                g[q] = v + 32 * q < v1 ? __ldg(body + v + 32 * q) : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                top = Vec<T>::most_number(top, Vec<T>::most_number(Vec<T>::most_number(g[q].x, g[q].y), Vec<T>::most_number(g[q].z, g[q].w)));
+        }
+        float f = Vec<T>::most_number_of(top);
+        if (first_warp() && lane < sp.head) f = fmaxf(f, Vec<T>::load(x + lane));
+        if (last_warp() && tail_at() + lane < A) f = fmaxf(f, Vec<T>::load(x + tail_at() + lane));
+        return f + 0.f;
     }
     // over the cluster: the sum of all warps' values, and of those of the warps before this one
     __device__ __forceinline__ u64 gather(u64 v, u64* before) {
@@ -419,21 +451,17 @@ template <typename T> struct ClusterRow {
         };
         float g[N];
         if (first_warp() && sp.head > 0) {
-            if (lane < sp.head) g[0] = clean(Vec<T>::load(x + lane));
+            if (lane < sp.head) g[0] = Vec<T>::load(x + lane);
             step(g, lane < sp.head ? 1 : 0, lane);
         }
         for (int base = v0; base < v1 && found < 0; base += 32) {
             const int v = base + lane, at = sp.head + v * N;
-            if (v < v1) {
-                Vec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(x + at)), g);
-#pragma unroll
-                for (int k = 0; k < N; ++k) g[k] = clean(g[k]);
-            }
+            if (v < v1) Vec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(x + at)), g);
             step(g, v < v1 ? N : 0, at);
         }
         if (last_warp() && tail_at() < A && found < 0) {
             const bool in = tail_at() + lane < A;
-            if (in) g[0] = clean(Vec<T>::load(x + tail_at() + lane));
+            if (in) g[0] = Vec<T>::load(x + tail_at() + lane);
             step(g, in ? 1 : 0, tail_at() + lane);
         }
         return found;
@@ -447,7 +475,7 @@ struct Cut {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constant__ SampleParams<T> P) {
+__global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_constant__ SampleParams<T> P) {
     typedef Key<T> K;
     extern __shared__ __align__(16) char raw[];
     Shared& sh = *reinterpret_cast<Shared*>(raw);
@@ -463,36 +491,46 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
     }
     const Rules r = rules_of(P, row);
 
-    uint32_t my_top = 0;
-    row_.each([&](float f, int) { my_top = max(my_top, K::of(f)); });
-    const uint32_t top_key = (uint32_t)row_.gather_max(my_top);
+    const uint32_t my_top = K::of(row_.most()), top_key = (uint32_t)row_.gather_max(my_top);
     const float m = K::value(top_key);
-    const float exp2_t = r.inv_t * 1.4426950408889634f;
-    // a quick exponential where only its sum's logarithm counts (ex2.approx: 2^-22), not a choice
-    auto quick = [&](float f) {
-        float e;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f == m ? 0.f : (f - m) * exp2_t));
-        return e;
+    const float exp2_t = fminf(r.inv_t * 1.4426950408889634f, 3.4028235e38f);
+    // For a finite m.  A quick exponential where only its sum's logarithm counts (ex2.approx: 2^-22), not a choice;
+    // far below the maximum, -inf and NaN: 0.
+    auto quick = [&](float f) { return exp2_of(fmaxf((f - m) * exp2_t, -1000.f)); };
+    auto relative = [&](float f) { return fmaxf((f - m) * r.inv_t, -1000.f); };
+    auto weight = [&](float f) {
+        const float e = expf(relative(f));
+        return e >= r.low ? weight_of(e) : 0u;
     };
     auto all_of = [&](float part) { return row_.gather((u64)((double)part * 0x1p31 + 0.5), nullptr); };
-    auto finish = [&](u64 kept, u64 all, u64 before, u64 mine, uint32_t cut, int tie_end) {
+    auto finish = [&](u64 kept, u64 all, u64 before, u64 mine, float cut, int tie_end) {
         const u64 target = target_of(P.uniforms[row], kept);
         if (target < before || target >= before + mine) return;
-        const int a = row_.walk(before, target, [&](float f, int j) -> u64 {
-            const uint32_t k = K::of(f);
-            return k > cut || (k == cut && j < tie_end) ? weight_at(f, m, r) : 0u;
-        });
+        const int a = row_.walk(before, target, [&](float f, int j) -> u64 { return f > cut || (f == cut && j < tie_end) ? weight(f) : 0u; });
         if (lane == 0 && a >= 0) write_row(P, row, a, clean(Vec<T>::load(x + a)), m, r.inv_t, all, kept);
     };
 
     if (m == -INFINITY) {
         if (rank == 0 && tid == 0) write_none(P, row);
+    } else if (m == INFINITY) {                              // the infinite ones share the probability
+        auto equal = [&](float f, int) -> u64 { return f == m; };
+        u64 mine = 0, before;
+        row_.each([&](float f, int j) { mine += equal(f, j); });
+        const u64 there = row_.gather(mine, &before);
+        mine = warp_sum(mine);
+        u64 ties = there < (u64)r.limit ? there : (u64)r.limit;
+        if (r.p < 1.f) ties = min(ties, (u64)ties_until((double)r.p * (double)(ties << 31), 0, 0x80000000u));
+        const u64 at = target_of(P.uniforms[row], ties << 31) >> 31;
+        if (at >= before && at < before + mine) {
+            const int a = row_.walk(before, at, equal);
+            if (lane == 0 && a >= 0) write_row(P, row, a, m, m, r.inv_t, there << 31, ties << 31);
+        }
     } else if (r.limit == 1) {
         float part = 0.f;
         uint32_t first = 0;                                  // ~index, so that the lowest wins
         row_.each([&](float f, int j) {
             part += quick(f);
-            if (K::of(f) == top_key) first = max(first, ~(uint32_t)j);
+            if (f == m) first = max(first, ~(uint32_t)j);
         });
         const u64 all = all_of(part);
         const int a = (int)~(uint32_t)row_.gather_max(first);
@@ -500,10 +538,10 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
     } else if (r.limit == P.A && r.p >= 1.f) {
         u64 mine = 0, before;
         float part = 0.f;
-        if (r.low > 0.f) row_.each([&](float f, int) { part += quick(f); mine += weight_at(f, m, r); });
-        else row_.each([&](float f, int) { mine += weight_at(f, m, r); });
+        if (r.low > 0.f) row_.each([&](float f, int) { part += quick(f); mine += weight(f); });
+        else row_.each([&](float f, int) { mine += weight_of(expf(relative(f))); });
         const u64 kept = row_.gather(mine, &before);
-        finish(kept, r.low > 0.f ? all_of(part) : kept, before, warp_sum(mine), 0, 0);
+        finish(kept, r.low > 0.f ? all_of(part) : kept, before, warp_sum(mine), -INFINITY, 0);
     } else {
         bool done = false;
         u64 all = 0;
@@ -546,14 +584,13 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
                 if (tid == 0) sh.bound = prefix << (kTop - 16);
             }
             row_.sync();
-            const uint32_t bound = lead.bound;
+            const float bound = K::value(max(lead.bound, K::of(-INFINITY)));
             float part = 0.f;
             row_.each([&](float f, int j) {
                 part += quick(f);
-                const uint32_t k = K::of(f);
-                if (k >= bound) {
+                if (f >= bound && j < P.A) {
                     const uint32_t at = atomicAdd(&lead.listed, 1u);
-                    if (at < kList) lead.list[at] = (u64)k << 32 | ~(uint32_t)j;
+                    if (at < kList) lead.list[at] = (u64)K::of(f + 0.f) << 32 | ~(uint32_t)j;
                 }
             });
             all = all_of(part);                              // its barrier also completes the list
@@ -577,7 +614,7 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
                 const u64 entry = tid < r.limit ? sh.list[tid] : 0;
                 const int index = (int)~(uint32_t)entry;
                 const float f = K::value((uint32_t)(entry >> 32));
-                uint32_t w = tid < r.limit ? weight_at(f, m, r) : 0u;
+                uint32_t w = tid < r.limit ? weight(f) : 0u;
                 u64 run = w;
                 for (int o = 1; o < 32; o <<= 1) {
                     const u64 u = __shfl_up_sync(~0u, run, o);
@@ -607,12 +644,12 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
         }
         if (!done) {
             constexpr float kSteps = kCoarse / 22.25f;       // weights are 0 from 22.18 below the maximum on
-            auto bin_of = [&](float f) { return min((int)(scaled(f, m, r.inv_t) * -kSteps), kCoarse - 1); };
+            auto bin_of = [&](float f) { return min((int)(relative(f) * -kSteps), kCoarse - 1); };
             for (int i = tid; i < kW * kCoarse * 32; i += kT) (&sh.column[0][0][0])[i] = 0;
             __syncthreads();
             u64* column = &sh.column[warp][0][lane];
             row_.each([&](float f, int) {
-                const float d = scaled(f, m, r.inv_t), e = expf(d);
+                const float d = relative(f), e = expf(d);
                 const uint32_t w = weight_of(e);
                 if (w != 0) column[min((int)(d * -kSteps), kCoarse - 1) * 32] += kCountOne + (e >= r.low ? w : 0u);
             });
@@ -668,10 +705,12 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
                     row_.sync();                             // the room, and what others still read there
                     for (int i = tid; i < kFine; i += kT) { sh.fine.weight[i] = 0; sh.fine.count[i] = 0; }
                     __syncthreads();
+                    const float low_f = K::value(c.lo), high_f = K::value(c.hi);
                     row_.each([&](float f, int) {
-                        const uint32_t k = K::of(f);
-                        if (k < c.lo || k > c.hi) return;
-                        const float e = expf(scaled(f, m, r.inv_t));
+                        if (!(f >= low_f && f <= high_f)) return;
+                        const uint32_t k = K::of(f + 0.f);
+                        if (k < c.lo || k > c.hi) return;    // 0 and -0 compare equal
+                        const float e = expf(relative(f));
                         const uint32_t w = weight_of(e);
                         if (w == 0) return;
                         const uint32_t at = (c.hi - k) >> shift;
@@ -725,7 +764,7 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
                 }
                 return c;
             };
-            uint32_t cut = 0;
+            uint32_t cut = K::of(-INFINITY);                 // nothing cut: -inf weighs 0
             int ties = P.A, at_cut = P.A;
             u64 kept = weighed;
             if ((uint32_t)r.limit < counted) {
@@ -733,21 +772,22 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
                 cut = c.lo;
                 ties = r.limit - (int)c.above_count;
                 at_cut = (int)c.at_count;
-                kept = c.above_weight + (u64)ties * weight_at(K::value(cut), m, r);
+                kept = c.above_weight + (u64)ties * weight(K::value(cut));
             }
             if (r.p < 1.f) {
                 const double enough = (double)r.p * (double)kept;
                 const Cut c = narrow(false, 0, enough);
-                const uint32_t w = weight_at(K::value(c.lo), m, r);
+                const uint32_t w = weight(K::value(c.lo));
                 const int more = ties_until(enough, c.above_weight, w);
                 if (c.lo > cut || more < ties) ties = more;
                 cut = c.lo;
                 at_cut = (int)c.at_count;
                 kept = c.above_weight + (u64)ties * w;
             }
+            const float cut_f = K::value(cut);
             int tie_end = P.A;
             if (ties < at_cut) {                             // where in the row the kept ones of the cut's key end
-                auto tied = [&](float f, int) -> u64 { return K::of(f) == cut; };
+                auto tied = [&](float f, int) -> u64 { return f == cut_f; };
                 u64 mine = 0, before;
                 row_.each([&](float f, int j) { mine += tied(f, j); });
                 row_.gather(mine, &before);
@@ -758,11 +798,10 @@ __global__ void __launch_bounds__(kT) sample_cluster_kernel(const __grid_constan
             }
             u64 mine = 0, before;
             row_.each([&](float f, int j) {
-                const uint32_t k = K::of(f);
-                if (k > cut || (k == cut && j < tie_end)) mine += weight_at(f, m, r);
+                if (f > cut_f || (f == cut_f && j < tie_end)) mine += weight(f);
             });
             row_.gather(mine, &before);
-            finish(kept, all, before, warp_sum(mine), cut, tie_end);
+            finish(kept, all, before, warp_sum(mine), cut_f, tie_end);
         }
     }
     row_.sync();                                             // no block ends while another may read its memory

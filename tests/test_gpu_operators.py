@@ -163,6 +163,57 @@ def test_sample_empty_masked_and_infinite_rows(api, A, dtype):
     check_sample(api, x, u, t=1e30)
 
 
+def rule_sample(x, u, t, k, p, low):
+    """The same rule as plain_sample() for wide rows, on the GPU: a stable sort and exact 64-bit sums."""
+    x = torch.where(torch.isnan(x.float()), -math.inf, x.float())
+    R, A = x.shape
+    top = x.amax(1, keepdim=True)
+    greedy = ~(t > 0)
+    inv = (1.0 / torch.where(greedy, 1.0, t))[:, None]
+    e = torch.exp(torch.where(x == top, 0.0, (x - top) * inv))
+    w = torch.floor(e.double() * 2.0 ** 31 + 0.5).long()
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices
+    rank = torch.arange(A, device=x.device)[None]
+    limit = torch.where(greedy, 1, torch.where(k > 0, k.long(), A))[:, None]
+    keep = (rank < limit) & ((rank == 0) | ~(low > 0)[:, None] | (e.gather(1, order) >= low[:, None]))
+    ws = torch.where(keep, w.gather(1, order), 0)
+    before = torch.cumsum(ws, 1) - ws
+    keep &= (rank == 0) | ~(p < 1)[:, None] | (before.double() < p.double()[:, None] * ws.sum(1, keepdim=True).double())
+    kept = torch.zeros_like(w).scatter_(1, order, torch.where(keep, ws, 0))
+    total = kept.sum(1)
+    target = torch.minimum(torch.floor(u.double() * total.double()).long(), total - 1)
+    a = (torch.cumsum(kept, 1) <= target[:, None]).sum(1)
+    d = torch.where(x == top, 0.0, (x - top) * inv).double()
+    z = torch.exp(d)
+    at = d.gather(1, a[:, None])[:, 0]
+    return a.int(), at - z.sum(1).log(), at - torch.where(kept > 0, z, 0.0).sum(1).log()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,A", [(1, 131072), (3, 262143), (40, 33001), (130, 9000), (300, 8200), (700, 1200), (2, 1000001)])
+@pytest.mark.parametrize("kind", ["peaked", "flat", "steps"])
+def test_sample_wide_rows(api, R, A, dtype, kind):
+    """Every cluster size and way through the large-row kernel: equal to the rule, whatever the settings."""
+    g = torch.Generator(device="cuda").manual_seed(A + R)
+    rand = lambda: torch.rand(R, device="cuda", generator=g)
+    x = torch.randn(R, A, device="cuda", generator=g) * {"peaked": 3.0, "flat": 0.05, "steps": 4.0}[kind]
+    if kind == "steps":
+        x = x.round()                                        # thousands of equal logits at every cut
+    x = x.to(dtype)
+    one = torch.ones(R, device="cuda")
+    none = torch.zeros(R, device="cuda", dtype=torch.int32)
+    ks = torch.randint(1, 400, (R,), device="cuda", generator=g, dtype=torch.int32)
+    for t, k, p, low in ((one, none, one, 0 * one), (rand() + 0.3, ks, one, 0 * one), (rand() + 0.5, none, rand(), 0 * one),
+                         (rand() * 3 + 0.1, ks * 40, rand() * 0.3 + 0.7, rand() * 0.02), (one, none, one, rand() * 0.1), (0 * one, none, one, 0 * one),
+                         (one * 0.05, ks, rand(), rand() * 0.2)):
+        u = rand()
+        want = rule_sample(x, u, t, k, p, low)
+        got = api.sample_actions(x, u, temperature=t, top_k=k, top_p=p, min_p=low)
+        assert torch.equal(got[0], want[0]), (got[0] != want[0]).sum()
+        for v, r in zip(got[1:], want[1:]):
+            assert ((v.double() - r).abs() <= 1e-5 + 2.0 ** -22 * r.abs()).all()
+
+
 def test_sample_parameters_that_limit_nothing(api):
     x = torch.randn(5, 300, generator=torch.Generator().manual_seed(9))
     u = torch.rand(5, generator=torch.Generator().manual_seed(8))
