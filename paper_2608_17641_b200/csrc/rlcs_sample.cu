@@ -326,13 +326,26 @@ struct Shared {
             uint32_t digit[256];
         };
     };
-    u64 trade[2][kW];
+    u64 trade[2][kW], near[kW];
+    uint32_t trade_ties[2][kW], near_ties[kW];
     u64 coarse_weight[kCoarse];
     uint32_t coarse_count[kCoarse];
     u64 scan_weight[kW];
     uint32_t scan_count[kW];
     u64 found_weight;
-    uint32_t found_count, found_at, found_bin, listed, bound;
+    uint32_t found_count, found_bin, listed, bound;
+};
+
+struct Range {
+    int v0, v1;                                              // vectors of the row
+    bool head, tail;                                         // and the elements before the first, behind the last
+};
+
+// Where a target lies among parts in order: which part, and the weight and ties before it.
+struct Located {
+    int part;
+    u64 before, total;
+    uint32_t ties_before;
 };
 
 template <typename T> struct ClusterRow {
@@ -341,38 +354,43 @@ template <typename T> struct ClusterRow {
     Shared& sh;
     int A, lane, warp, rank, ranks, turn;
     Span sp;
-    int v0, v1;                                              // this warp's vectors
+    Range mine;                                              // this warp's
 
+    // Part `i` of `n` equal ones of a range: its vectors, and the single elements before and behind the row's if it is the
+    // first or the last.
+    static __device__ __forceinline__ Range part_of(const Range& r, int i, int n) {
+        const int per = (r.v1 - r.v0 + n - 1) / n, at = min(r.v0 + i * per, r.v1);
+        return Range{at, min(at + per, r.v1), r.head && i == 0, r.tail && i == n - 1};
+    }
+    __device__ __forceinline__ Range all() const { return Range{0, sp.vecs, true, true}; }
     __device__ __forceinline__ void sync() {
         if (ranks > 1) cooperative_groups::this_cluster().sync(); else __syncthreads();
     }
     __device__ __forceinline__ Shared& other(int rank_) {
         return ranks > 1 ? *cooperative_groups::this_cluster().map_shared_rank(&sh, rank_) : sh;
     }
-    __device__ __forceinline__ bool first_warp() const { return rank == 0 && warp == 0; }
-    __device__ __forceinline__ bool last_warp() const { return rank == ranks - 1 && warp == kW - 1; }
     __device__ __forceinline__ int tail_at() const { return sp.head + sp.vecs * Vec<T>::N; }
 
-    // f(logit, index) for every element of the warp's range, four vectors of a lane in flight; places behind the range hold
-    // -inf.  Logits come as they are: NaN compares false and -0 equal to 0.
-    template <typename F> __device__ __forceinline__ void each(F f) const {
+    // f(logit, index) for every element of a range, four vectors of a lane in flight; places behind the range hold -inf.
+    // Logits come as they are: NaN compares false and -0 equal to 0.
+    template <typename F> __device__ __forceinline__ void each(const Range& r, F f) const {
         constexpr int N = Vec<T>::N, kAhead = 4;
         const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
         const uint4 nothing = make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
         uint4 g[kAhead];
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q) g[q] = v0 + lane + 32 * q < v1 ? __ldg(body + v0 + lane + 32 * q) : nothing;
+        for (int q = 0; q < kAhead; ++q) g[q] = r.v0 + lane + 32 * q < r.v1 ? __ldg(body + r.v0 + lane + 32 * q) : nothing;
 #pragma unroll 1
-        for (int v = v0 + lane; v - lane < v1; v += 32) {    // one copy of f's code a vector: the kernel has many such passes
+        for (int v = r.v0 + lane; v - lane < r.v1; v += 32) {      // one copy of f's code a vector: the kernel has many such passes
             float e[N];
             Vec<T>::unpack(g[0], e);
 #pragma unroll
             for (int q = 0; q + 1 < kAhead; ++q) g[q] = g[q + 1];
-            g[kAhead - 1] = v + 32 * kAhead < v1 ? __ldg(body + v + 32 * kAhead) : nothing;
+            g[kAhead - 1] = v + 32 * kAhead < r.v1 ? __ldg(body + v + 32 * kAhead) : nothing;
 #pragma unroll
             for (int k = 0; k < N; ++k) f(e[k], sp.head + v * N + k);
         }
-        const int singles = first_warp() ? sp.head : 0, ends = last_warp() ? A - tail_at() : 0;
+        const int singles = r.head ? sp.head : 0, ends = r.tail ? A - tail_at() : 0;
         if (lane < singles + ends) {
             const int j = lane < singles ? lane : tail_at() + lane - singles;
             f(Vec<T>::load(x + j), j);
@@ -383,33 +401,28 @@ template <typename T> struct ClusterRow {
         constexpr int kAhead = 8;
         uint32_t top = Vec<T>::kNothing;
         const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
-        for (int v = v0 + lane; v < v1; v += 32 * kAhead) {
+        for (int v = mine.v0 + lane; v < mine.v1; v += 32 * kAhead) {
             uint4 g[kAhead];
 #pragma unroll
             for (int q = 0; q < kAhead; ++q)
-                g[q] = v + 32 * q < v1 ? __ldg(body + v + 32 * q) : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+                g[q] = v + 32 * q < mine.v1 ? __ldg(body + v + 32 * q) : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
 #pragma unroll
             for (int q = 0; q < kAhead; ++q)
                 top = Vec<T>::most_number(top, Vec<T>::most_number(Vec<T>::most_number(g[q].x, g[q].y), Vec<T>::most_number(g[q].z, g[q].w)));
         }
         float f = Vec<T>::most_number_of(top);
-        if (first_warp() && lane < sp.head) f = fmaxf(f, Vec<T>::load(x + lane));
-        if (last_warp() && tail_at() + lane < A) f = fmaxf(f, Vec<T>::load(x + tail_at() + lane));
+        if (mine.head && lane < sp.head) f = fmaxf(f, Vec<T>::load(x + lane));
+        if (mine.tail && tail_at() + lane < A) f = fmaxf(f, Vec<T>::load(x + tail_at() + lane));
         return f + 0.f;
     }
-    // over the cluster: the sum of all warps' values, and of those of the warps before this one
-    __device__ __forceinline__ u64 gather(u64 v, u64* before) {
+    // over the cluster: the sum of all warps' values
+    __device__ __forceinline__ u64 gather(u64 v) {
         v = warp_sum(v);
         turn ^= 1;
         if (lane == 0) sh.trade[turn][warp] = v;
         sync();
-        u64 total = 0, mine = 0;
-        for (int i = lane; i < ranks * kW; i += 32) {
-            const u64 u = other(i / kW).trade[turn][i % kW];
-            total += u;
-            if (i < rank * kW + warp) mine += u;
-        }
-        if (before != nullptr) *before = warp_sum(mine);
+        u64 total = 0;
+        for (int i = lane; i < ranks * kW; i += 32) total += other(i / kW).trade[turn][i % kW];
         return warp_sum(total);
     }
     __device__ __forceinline__ u64 gather_max(u64 v) {
@@ -421,15 +434,69 @@ template <typename T> struct ClusterRow {
         for (int i = lane; i < ranks * kW; i += 32) { const u64 u = other(i / kW).trade[turn][i % kW]; top = u > top ? u : top; }
         return warp_max(top);
     }
-    // This warp's range in index order: the element at which the running sum, `sum` before the range, passes the target.
-    template <typename F> __device__ __forceinline__ int walk(u64 sum, u64 target, F value) const {
+    // Kept are all above the cut (their weights are in the parts' sums) and the first `ties` that equal it, of weight `each_tie`.
+    // Parts in order, two a lane: which one holds the target, a share `uniform` of all kept weight (or that very target, where given).
+    template <typename Entry>
+    __device__ __forceinline__ Located locate(int n, Entry entry, u64 ties, uint32_t each_tie, float uniform, const u64* given) const {
+        u64 w[2] = {0, 0};
+        uint32_t t[2] = {0, 0};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (2 * lane + h < n) entry(2 * lane + h, &w[h], &t[h]);
+        uint32_t t_run = t[0] + t[1];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t u = __shfl_up_sync(~0u, t_run, o);
+            t_run += lane >= o ? u : 0;
+        }
+        const uint32_t t0 = t_run - t[0] - t[1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u64 at = h == 0 ? t0 : t0 + t[0], left = at < ties ? ties - at : 0;
+            w[h] += (left < t[h] ? left : t[h]) * each_tie;
+        }
+        u64 run = w[0] + w[1];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 u = __shfl_up_sync(~0u, run, o);
+            run += lane >= o ? u : 0;
+        }
+        Located r;
+        r.total = __shfl_sync(~0u, run, 31);
+        const u64 target = given != nullptr ? *given : target_of(uniform, r.total), before = run - w[0] - w[1];
+        const unsigned past = __ballot_sync(~0u, run > target);
+        const int src = past ? __ffs(past) - 1 : 31;
+        const bool second = !(before + w[0] > target);
+        r.part = 2 * src + __shfl_sync(~0u, (int)second, src);
+        r.before = __shfl_sync(~0u, second ? before + w[0] : before, src);
+        r.ties_before = __shfl_sync(~0u, second ? t0 + t[0] : t0, src);
+        return r;
+    }
+    // A range in index order, by one warp: the element at which the running kept weight passes the target.
+    template <typename F>
+    __device__ __forceinline__ int walk(const Range& r, float cut, u64 ties, uint32_t each_tie, u64 target, F weight) const {
         constexpr int N = Vec<T>::N;
         int found = -1;
+        u64 sum = 0, seen = 0;
         auto step = [&](const float* g, int n, int at) {     // n elements a lane, lane after lane
-            u64 mine = 0;
+            u64 w = 0;
+            uint32_t t = 0;
+            u64 each_w[N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) if (k < n) mine += value(g[k], at + k);
-            u64 run = mine;
+            for (int k = 0; k < N; ++k) {
+                each_w[k] = k < n && g[k] > cut ? weight(g[k]) : 0u;
+                w += each_w[k];
+                t += k < n && g[k] == cut;
+            }
+            uint32_t t_run = t;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t u = __shfl_up_sync(~0u, t_run, o);
+                t_run += lane >= o ? u : 0;
+            }
+            const u64 rank_ = seen + t_run - t, left = rank_ < ties ? ties - rank_ : 0;
+            const u64 mine_ = w + (left < t ? left : t) * each_tie;
+            u64 run = mine_;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const u64 u = __shfl_up_sync(~0u, run, o);
@@ -437,40 +504,84 @@ template <typename T> struct ClusterRow {
             }
             const unsigned past = __ballot_sync(~0u, sum + run > target);
             if (past) {
-                u64 s = sum + run - mine;
+                u64 s_ = sum + run - mine_, q = rank_;
                 int hit = -1;
 #pragma unroll
                 for (int k = 0; k < N; ++k)
                     if (k < n) {
-                        s += value(g[k], at + k);
-                        if (hit < 0 && s > target) hit = at + k;
+                        s_ += each_w[k];
+                        if (g[k] == cut && q++ < ties) s_ += each_tie;
+                        if (hit < 0 && s_ > target) hit = at + k;
                     }
                 found = __shfl_sync(~0u, hit, __ffs(past) - 1);
             }
             sum += __shfl_sync(~0u, run, 31);
+            seen += __shfl_sync(~0u, t_run, 31);
         };
-        float g[N];
-        if (first_warp() && sp.head > 0) {
-            if (lane < sp.head) g[0] = Vec<T>::load(x + lane);
-            step(g, lane < sp.head ? 1 : 0, lane);
-        }
-        for (int base = v0; base < v1 && found < 0; base += 32) {
-            const int v = base + lane, at = sp.head + v * N;
-            if (v < v1) Vec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(x + at)), g);
-            step(g, v < v1 ? N : 0, at);
-        }
-        if (last_warp() && tail_at() < A && found < 0) {
-            const bool in = tail_at() + lane < A;
-            if (in) g[0] = Vec<T>::load(x + tail_at() + lane);
-            step(g, in ? 1 : 0, tail_at() + lane);
+        const int singles = r.head ? sp.head : 0, ends = r.tail ? A - tail_at() : 0;
+#pragma unroll 1
+        for (int base = singles ? r.v0 - 32 : r.v0; base < (ends ? r.v1 + 32 : r.v1) && found < 0; base += 32) {
+            // one step of the single elements before, steps of vectors, one of those behind
+            float g[N];
+            int n = 0, at = 0;
+            if (base < r.v0) {
+                at = lane;
+                n = lane < singles;
+            } else if (base < r.v1) {
+                at = sp.head + (base + lane) * N;
+                n = base + lane < r.v1 ? N : 0;
+            } else {
+                at = tail_at() + lane;
+                n = lane < ends;
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) g[k] = -INFINITY;
+            if (n == N) Vec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(x + at)), g);
+            else if (n == 1) g[0] = Vec<T>::load(x + at);
+            step(g, n, at);
+            if (base < r.v1 && base + 32 >= r.v1 && base >= r.v0) base = r.v1 - 32;      // the step behind the vectors starts at their end
         }
         return found;
+    }
+    // The action: the warps' sums (weights above the cut, ties) find the warp, its block's warps its part, one of them the element.
+    // `done(element, kept weight)` is called by that warp.
+    template <typename F, typename G>
+    __device__ __forceinline__ void pick(u64 w, uint32_t t, float cut, u64 ties, uint32_t each_tie, float uniform, F weight, G done) {
+        w = warp_sum(w);
+        t = __reduce_add_sync(~0u, t);
+        turn ^= 1;
+        if (lane == 0) { sh.trade[turn][warp] = w; sh.trade_ties[turn][warp] = t; }
+        sync();
+        const int trade_turn = turn;
+        const Located far = locate(ranks * kW, [&](int i, u64* ew, uint32_t* et) {
+            Shared& o = other(i / kW);
+            *ew = o.trade[trade_turn][i % kW];
+            *et = o.trade_ties[trade_turn][i % kW];
+        }, ties, each_tie, uniform, nullptr);
+        if (far.part / kW != rank) return;
+        u64 target = target_of(uniform, far.total) - far.before;
+        ties = far.ties_before < ties ? ties - far.ties_before : 0;
+        const Range near = part_of(part_of(all(), far.part, ranks * kW), warp, kW);
+        w = 0;
+        t = 0;
+        each(near, [&](float f, int) {
+            if (f > cut) w += weight(f);
+            t += f == cut;
+        });
+        w = warp_sum(w);
+        t = __reduce_add_sync(~0u, t);
+        if (lane == 0) { sh.near[warp] = w; sh.near_ties[warp] = t; }
+        __syncthreads();
+        const Located here = locate(kW, [&](int i, u64* ew, uint32_t* et) { *ew = sh.near[i]; *et = sh.near_ties[i]; }, ties, each_tie, 0.f, &target);
+        if (here.part != warp) return;
+        const int a = walk(near, cut, here.ties_before < ties ? ties - here.ties_before : 0, each_tie, target - here.before, weight);
+        if (a >= 0) done(a, far.total);
     }
 };
 
 // A cut being narrowed: keys in [lo, hi] hold it; `above` sums what lies over hi.
 struct Cut {
-    uint32_t lo, hi, above_count, at_count;
+    uint32_t lo, hi, above_count;
     u64 above_weight;
 };
 
@@ -483,12 +594,8 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = blockIdx.x / ranks;
     const T* x = P.logits + row * P.ld;
-    ClusterRow<T> row_ = {x, sh, P.A, lane, warp, rank, ranks, 0, span_of(x, P.A), 0, 0};
-    {
-        const int per = (row_.sp.vecs + ranks * kW - 1) / (ranks * kW), at = (rank * kW + warp) * per;
-        row_.v0 = min(at, row_.sp.vecs);
-        row_.v1 = min(at + per, row_.sp.vecs);
-    }
+    ClusterRow<T> row_ = {x, sh, P.A, lane, warp, rank, ranks, 0, span_of(x, P.A), {0, 0, false, false}};
+    row_.mine = row_.part_of(row_.all(), rank * kW + warp, ranks * kW);
     const Rules r = rules_of(P, row);
 
     const uint32_t my_top = K::of(row_.most()), top_key = (uint32_t)row_.gather_max(my_top);
@@ -502,49 +609,45 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
         const float e = expf(relative(f));
         return e >= r.low ? weight_of(e) : 0u;
     };
-    auto all_of = [&](float part) { return row_.gather((u64)((double)part * 0x1p31 + 0.5), nullptr); };
-    auto finish = [&](u64 kept, u64 all, u64 before, u64 mine, float cut, int tie_end) {
-        const u64 target = target_of(P.uniforms[row], kept);
-        if (target < before || target >= before + mine) return;
-        const int a = row_.walk(before, target, [&](float f, int j) -> u64 { return f > cut || (f == cut && j < tie_end) ? weight(f) : 0u; });
-        if (lane == 0 && a >= 0) write_row(P, row, a, clean(Vec<T>::load(x + a)), m, r.inv_t, all, kept);
+    auto all_of = [&](float part) { return row_.gather((u64)((double)part * 0x1p31 + 0.5)); };
+    const float uniform = P.uniforms[row];
+    u64 all = 0;
+    auto done = [&](int a, u64 kept) {
+        if (lane == 0) write_row(P, row, a, clean(Vec<T>::load(x + a)), m, r.inv_t, all != 0 ? all : kept, kept);
     };
 
     if (m == -INFINITY) {
         if (rank == 0 && tid == 0) write_none(P, row);
     } else if (m == INFINITY) {                              // the infinite ones share the probability
-        auto equal = [&](float f, int) -> u64 { return f == m; };
-        u64 mine = 0, before;
-        row_.each([&](float f, int j) { mine += equal(f, j); });
-        const u64 there = row_.gather(mine, &before);
-        mine = warp_sum(mine);
-        u64 ties = there < (u64)r.limit ? there : (u64)r.limit;
+        uint32_t mine = 0;
+        row_.each(row_.mine, [&](float f, int) { mine += f == m; });
+        const u64 there = row_.gather(mine);
+        u64 ties = min(there, (u64)r.limit);
         if (r.p < 1.f) ties = min(ties, (u64)ties_until((double)r.p * (double)(ties << 31), 0, 0x80000000u));
-        const u64 at = target_of(P.uniforms[row], ties << 31) >> 31;
-        if (at >= before && at < before + mine) {
-            const int a = row_.walk(before, at, equal);
-            if (lane == 0 && a >= 0) write_row(P, row, a, m, m, r.inv_t, there << 31, ties << 31);
-        }
+        all = there << 31;
+        row_.pick(0, mine, m, ties, 0x80000000u, uniform, weight, done);
     } else if (r.limit == 1) {
         float part = 0.f;
         uint32_t first = 0;                                  // ~index, so that the lowest wins
-        row_.each([&](float f, int j) {
+        row_.each(row_.mine, [&](float f, int j) {
             part += quick(f);
             if (f == m) first = max(first, ~(uint32_t)j);
         });
-        const u64 all = all_of(part);
+        all = all_of(part);
         const int a = (int)~(uint32_t)row_.gather_max(first);
         if (rank == 0 && tid == 0) write_row(P, row, a, m, m, r.inv_t, all, 0x80000000ull);
     } else if (r.limit == P.A && r.p >= 1.f) {
-        u64 mine = 0, before;
-        float part = 0.f;
-        if (r.low > 0.f) row_.each([&](float f, int) { part += quick(f); mine += weight(f); });
-        else row_.each([&](float f, int) { mine += weight_of(expf(relative(f))); });
-        const u64 kept = row_.gather(mine, &before);
-        finish(kept, r.low > 0.f ? all_of(part) : kept, before, warp_sum(mine), -INFINITY, 0);
+        u64 mine = 0;
+        if (r.low > 0.f) {
+            float part = 0.f;
+            row_.each(row_.mine, [&](float f, int) { part += quick(f); mine += weight(f); });
+            all = all_of(part);
+        } else {
+            row_.each(row_.mine, [&](float f, int) { mine += weight_of(expf(relative(f))); });
+        }
+        row_.pick(mine, 0, -INFINITY, 0, 0, uniform, weight, done);
     } else {
-        bool done = false;
-        u64 all = 0;
+        bool listed_all = false;
         if (r.limit <= kListLimit) {
             Shared& lead = row_.other(0);
             lead.maxima[rank * kT + tid] = my_top;
@@ -586,7 +689,7 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
             row_.sync();
             const float bound = K::value(max(lead.bound, K::of(-INFINITY)));
             float part = 0.f;
-            row_.each([&](float f, int j) {
+            row_.each(row_.mine, [&](float f, int j) {
                 part += quick(f);
                 if (f >= bound && j < P.A) {
                     const uint32_t at = atomicAdd(&lead.listed, 1u);
@@ -595,9 +698,9 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
             });
             all = all_of(part);                              // its barrier also completes the list
             const uint32_t listed = lead.listed;
-            done = listed <= kList;
+            listed_all = listed <= kList;
             row_.sync();                                     // read by all before the room is used again
-            if (done && rank == 0) {
+            if (listed_all && rank == 0) {
                 int size = 32;
                 while (size < (int)listed) size *= 2;
                 for (int i = tid; i < size; i += kT) if (i >= (int)listed) sh.list[i] = 0;
@@ -634,7 +737,7 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                 __syncthreads();
                 u64 kept = 0;
                 for (int k = 0; k < kW; ++k) kept += sh.scan_weight[k];
-                const u64 target = target_of(P.uniforms[row], kept);
+                const u64 target = target_of(uniform, kept);
                 if (w != 0) {
                     u64 upto = 0;
                     for (int k = 0; k < r.limit; ++k) upto += sh.maxima[k] <= (uint32_t)index ? sh.list[k] : 0;
@@ -642,13 +745,13 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                 }
             }
         }
-        if (!done) {
+        if (!listed_all) {
             constexpr float kSteps = kCoarse / 22.25f;       // weights are 0 from 22.18 below the maximum on
             auto bin_of = [&](float f) { return min((int)(relative(f) * -kSteps), kCoarse - 1); };
             for (int i = tid; i < kW * kCoarse * 32; i += kT) (&sh.column[0][0][0])[i] = 0;
             __syncthreads();
             u64* column = &sh.column[warp][0][lane];
-            row_.each([&](float f, int) {
+            row_.each(row_.mine, [&](float f, int) {
                 const float d = relative(f), e = expf(d);
                 const uint32_t w = weight_of(e);
                 if (w != 0) column[min((int)(d * -kSteps), kCoarse - 1) * 32] += kCountOne + (e >= r.low ? w : 0u);
@@ -678,7 +781,7 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
             if (r.low == 0.f && all == 0) all = weighed;
             if (all == 0) {
                 float part = 0.f;
-                row_.each([&](float f, int) { part += quick(f); });
+                row_.each(row_.mine, [&](float f, int) { part += quick(f); });
                 all = all_of(part);
             }
             // the cut where `want` candidates, or `enough` weight, are reached: first the step, then its keys by histograms
@@ -688,12 +791,16 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                 Cut c;
                 c.above_weight = __shfl_sync(~0u, to_weight - bin_weight, b);
                 c.above_count = __shfl_sync(~0u, to_count - bin_count, b);
-                c.at_count = __shfl_sync(~0u, bin_count, b);
-                auto least = [&](int bin) {                  // the least key whose step is at most `bin`
+                auto least = [&](int bin) {                  // the least key whose step is at most `bin`, 32 tried at once
                     uint32_t lo = K::of(-INFINITY), hi = top_key;
                     while (lo < hi) {
-                        const uint32_t mid = lo + (hi - lo) / 2;
-                        if (bin_of(K::value(mid)) <= bin) hi = mid; else lo = mid + 1;
+                        const uint32_t step = (hi - lo + 31) / 32, at = min(lo + lane * step, hi);
+                        const unsigned yes = __ballot_sync(~0u, bin_of(K::value(at)) <= bin);
+                        const int first = yes ? __ffs(yes) - 1 : 32;
+                        const uint32_t from = lo;
+                        if (first < 32) hi = min(from + first * step, hi);
+                        if (first > 0) lo = min(from + (first - 1) * step + 1, hi);
+                        else hi = lo;
                     }
                     return lo;
                 };
@@ -706,7 +813,7 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                     for (int i = tid; i < kFine; i += kT) { sh.fine.weight[i] = 0; sh.fine.count[i] = 0; }
                     __syncthreads();
                     const float low_f = K::value(c.lo), high_f = K::value(c.hi);
-                    row_.each([&](float f, int) {
+                    row_.each(row_.mine, [&](float f, int) {
                         if (!(f >= low_f && f <= high_f)) return;
                         const uint32_t k = K::of(f + 0.f);
                         if (k < c.lo || k > c.hi) return;    // 0 and -0 compare equal
@@ -752,12 +859,10 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                         sh.found_bin = tid * (kFine / kT) + k;
                         sh.found_weight = aw;
                         sh.found_count = an;
-                        sh.found_at = n[k];
                     }
                     __syncthreads();
                     c.above_weight = sh.found_weight;
                     c.above_count = sh.found_count;
-                    c.at_count = sh.found_at;
                     c.hi -= sh.found_bin << shift;
                     const uint32_t width = (1u << shift) - 1;
                     c.lo = c.hi - c.lo > width ? c.hi - width : c.lo;
@@ -765,43 +870,28 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                 return c;
             };
             uint32_t cut = K::of(-INFINITY);                 // nothing cut: -inf weighs 0
-            int ties = P.A, at_cut = P.A;
-            u64 kept = weighed;
+            u64 ties = 0, kept = weighed;
             if ((uint32_t)r.limit < counted) {
                 const Cut c = narrow(true, r.limit, 0.);
                 cut = c.lo;
-                ties = r.limit - (int)c.above_count;
-                at_cut = (int)c.at_count;
-                kept = c.above_weight + (u64)ties * weight(K::value(cut));
+                ties = r.limit - c.above_count;
+                kept = c.above_weight + ties * weight(K::value(cut));
             }
             if (r.p < 1.f) {
                 const double enough = (double)r.p * (double)kept;
                 const Cut c = narrow(false, 0, enough);
-                const uint32_t w = weight(K::value(c.lo));
-                const int more = ties_until(enough, c.above_weight, w);
+                const u64 more = (u64)ties_until(enough, c.above_weight, weight(K::value(c.lo)));
                 if (c.lo > cut || more < ties) ties = more;
                 cut = c.lo;
-                at_cut = (int)c.at_count;
-                kept = c.above_weight + (u64)ties * w;
             }
             const float cut_f = K::value(cut);
-            int tie_end = P.A;
-            if (ties < at_cut) {                             // where in the row the kept ones of the cut's key end
-                auto tied = [&](float f, int) -> u64 { return f == cut_f; };
-                u64 mine = 0, before;
-                row_.each([&](float f, int j) { mine += tied(f, j); });
-                row_.gather(mine, &before);
-                mine = warp_sum(mine);
-                const u64 last = (u64)ties - 1;
-                const int at = last >= before && last < before + mine ? row_.walk(before, last, tied) : -1;
-                tie_end = (int)row_.gather_max((u64)(uint32_t)(at + 1));
-            }
-            u64 mine = 0, before;
-            row_.each([&](float f, int j) {
-                if (f > cut_f || (f == cut_f && j < tie_end)) mine += weight(f);
+            u64 mine = 0;
+            uint32_t tied = 0;
+            row_.each(row_.mine, [&](float f, int) {
+                if (f > cut_f) mine += weight(f);
+                tied += f == cut_f;
             });
-            row_.gather(mine, &before);
-            finish(kept, all, before, warp_sum(mine), cut_f, tie_end);
+            row_.pick(mine, tied, cut_f, ties, weight(cut_f), uniform, weight, done);
         }
     }
     row_.sync();                                             // no block ends while another may read its memory
