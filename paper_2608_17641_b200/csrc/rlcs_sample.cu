@@ -317,8 +317,7 @@ struct Shared {
     union {
         u64 column[kW][kCoarse][32];
         struct {
-            u64 weight[kFine];
-            uint32_t count[kFine];
+            uint32_t count[kFine], low[kFine], high[kFine];      // weight in two words
         } fine;
         struct {
             u64 list[kList];                                 // (key, ~index)
@@ -810,7 +809,7 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                     int shift = 0;
                     while ((c.hi - c.lo) >> shift >= kFine) ++shift;
                     row_.sync();                             // the room, and what others still read there
-                    for (int i = tid; i < kFine; i += kT) { sh.fine.weight[i] = 0; sh.fine.count[i] = 0; }
+                    for (int i = tid; i < kFine; i += kT) { sh.fine.count[i] = 0; sh.fine.low[i] = 0; sh.fine.high[i] = 0; }
                     __syncthreads();
                     const float low_f = K::value(c.lo), high_f = K::value(c.hi);
                     row_.each(row_.mine, [&](float f, int) {
@@ -822,20 +821,25 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                         if (w == 0) return;
                         const uint32_t at = (c.hi - k) >> shift;
                         atomicAdd(&sh.fine.count[at], 1u);
-                        if (e >= r.low) atomicAdd(&sh.fine.weight[at], (u64)w);
+                        if (shift > 0 && e >= r.low) {       // places of one key: their count gives their weight
+                            const uint32_t was = atomicAdd(&sh.fine.low[at], w);
+                            if (was + w < was) atomicAdd(&sh.fine.high[at], 1u);
+                        }
                     });
                     row_.sync();
                     u64 w[kFine / kT], sum_w = 0;
                     uint32_t n[kFine / kT], sum_n = 0;
 #pragma unroll
                     for (int k = 0; k < kFine / kT; ++k) {
+                        const int at = tid * (kFine / kT) + k;
                         w[k] = 0;
                         n[k] = 0;
                         for (int q = 0; q < ranks; ++q) {
                             const Shared& o = row_.other(q);
-                            w[k] += o.fine.weight[tid * (kFine / kT) + k];
-                            n[k] += o.fine.count[tid * (kFine / kT) + k];
+                            n[k] += o.fine.count[at];
+                            if (shift > 0) w[k] += (u64)o.fine.high[at] << 32 | o.fine.low[at];
                         }
+                        if (shift == 0 && n[k] != 0) w[k] = (u64)n[k] * weight(K::value(c.hi - at));
                         sum_w += w[k];
                         sum_n += n[k];
                     }
