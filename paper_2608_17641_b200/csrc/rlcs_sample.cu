@@ -56,12 +56,14 @@ __device__ __forceinline__ float clean(float f) { return fmaxf(f, -INFINITY) + 0
 
 __device__ __forceinline__ float scaled(float x, float m, float inv_t) { return x == m ? 0.f : (x - m) * inv_t; }
 
-// floor(2^31 e + 1/2) for 0 <= e <= 1: the fraction's 24 bits shifted by the exponent, the last place rounded half up.
+// floor(2^31 e + 1/2) for 0 <= e <= 1.  Below 2^-10, nearly every logit of a wide row, one multiply-add rounded down leaves the
+// whole number in the upper bits of its fraction; above, the 24 bits of e are shifted by its exponent and the last place rounded.
 __device__ __forceinline__ uint32_t weight_of(float e) {
+    if (e < 0x1p-10f) return (__float_as_uint(__fmaf_rd(e, 0x1p31f, 4194304.5f)) & 0x7fffffu) >> 1;
     const uint32_t u = __float_as_uint(e);
     const int down = 127 - (int)(u >> 23);
     const uint32_t frac = (u << 8) | 0x80000000u;
-    return down == 0 ? frac : down > 32 ? 0u : ((frac >> (down - 1)) + 1) >> 1;
+    return down == 0 ? frac : ((frac >> (down - 1)) + 1) >> 1;
 }
 
 // A row's settings, with the cases that leave one candidate folded into limit = 1.
@@ -805,6 +807,8 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                 };
                 c.lo = least(b);
                 c.hi = b == 0 ? top_key : least(b - 1) - 1;
+                if (K::kDown && b == kCoarse - 1)            // 16-bit keys are counted without their weights: none of weight 0
+                    while (c.lo < c.hi && weight_of(expf(relative(K::value(c.lo)))) == 0) ++c.lo;
                 while (c.lo < c.hi) {
                     int shift = 0;
                     while ((c.hi - c.lo) >> shift >= kFine) ++shift;
@@ -816,6 +820,10 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                         if (!(f >= low_f && f <= high_f)) return;
                         const uint32_t k = K::of(f + 0.f);
                         if (k < c.lo || k > c.hi) return;    // 0 and -0 compare equal
+                        if (K::kDown && shift == 0) {
+                            atomicAdd(&sh.fine.count[c.hi - k], 1u);
+                            return;
+                        }
                         const float e = expf(relative(f));
                         const uint32_t w = weight_of(e);
                         if (w == 0) return;
@@ -827,19 +835,22 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                         }
                     });
                     row_.sync();
+                    // every block adds up a stretch of the places over the cluster; the stretches' sums say which one holds the
+                    // cut, and its block tells the others
+                    const int stretch = kFine / ranks, per = stretch < kT ? 1 : stretch / kT, first = rank * stretch + tid * per;
                     u64 w[kFine / kT], sum_w = 0;
                     uint32_t n[kFine / kT], sum_n = 0;
 #pragma unroll
                     for (int k = 0; k < kFine / kT; ++k) {
-                        const int at = tid * (kFine / kT) + k;
                         w[k] = 0;
                         n[k] = 0;
+                        if (k >= per || tid * per >= stretch) continue;
                         for (int q = 0; q < ranks; ++q) {
                             const Shared& o = row_.other(q);
-                            n[k] += o.fine.count[at];
-                            if (shift > 0) w[k] += (u64)o.fine.high[at] << 32 | o.fine.low[at];
+                            n[k] += o.fine.count[first + k];
+                            if (shift > 0) w[k] += (u64)o.fine.high[first + k] << 32 | o.fine.low[first + k];
                         }
-                        if (shift == 0 && n[k] != 0) w[k] = (u64)n[k] * weight(K::value(c.hi - at));
+                        if (shift == 0 && n[k] != 0) w[k] = (u64)n[k] * weight(K::value(c.hi - (first + k)));
                         sum_w += w[k];
                         sum_n += n[k];
                     }
@@ -850,21 +861,29 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                         const uint32_t v = __shfl_up_sync(~0u, run_n, o);
                         if (lane >= o) { run_w += u; run_n += v; }
                     }
-                    if (lane == 31) { sh.scan_weight[warp] = run_w; sh.scan_count[warp] = run_n; }
-                    __syncthreads();
+                    row_.turn ^= 1;
+                    if (lane == 31) { sh.trade[row_.turn][warp] = run_w; sh.trade_ties[row_.turn][warp] = run_n; }
+                    row_.sync();
                     u64 aw = c.above_weight;
                     uint32_t an = c.above_count;
-                    for (int k = 0; k < warp; ++k) { aw += sh.scan_weight[k]; an += sh.scan_count[k]; }
+                    for (int k = 0; k < rank * kW + warp; ++k) {
+                        const Shared& o = row_.other(k / kW);
+                        aw += o.trade[row_.turn][k % kW];
+                        an += o.trade_ties[row_.turn][k % kW];
+                    }
                     aw += run_w - sum_w;
                     an += run_n - sum_n;
                     if (!reached(an, aw) && reached(an + sum_n, aw + sum_w)) {
                         int k = 0;
-                        while (k < kFine / kT - 1 && !reached(an + n[k], aw + w[k])) { an += n[k]; aw += w[k]; ++k; }
-                        sh.found_bin = tid * (kFine / kT) + k;
-                        sh.found_weight = aw;
-                        sh.found_count = an;
+                        while (k < per - 1 && !reached(an + n[k], aw + w[k])) { an += n[k]; aw += w[k]; ++k; }
+                        for (int q = 0; q < ranks; ++q) {
+                            Shared& o = row_.other(q);
+                            o.found_bin = first + k;
+                            o.found_weight = aw;
+                            o.found_count = an;
+                        }
                     }
-                    __syncthreads();
+                    row_.sync();
                     c.above_weight = sh.found_weight;
                     c.above_count = sh.found_count;
                     c.hi -= sh.found_bin << shift;
