@@ -132,10 +132,28 @@ __global__ void __launch_bounds__(kSmallRows) sample_small_kernel(const __grid_c
     const int A = P.A, stride = A | 1;
     const int64_t row0 = (int64_t)blockIdx.x * kSmallRows, row = row0 + threadIdx.x;
     const int rows = P.R - row0 < kSmallRows ? (int)(P.R - row0) : kSmallRows;
+    const T* from = P.logits + row0 * P.ld;
+    if (P.ld == A && A % 2 == 0 && (reinterpret_cast<uintptr_t>(from) & 15) == 0) {      // whole vectors; neighbours of an even place share a row
+        constexpr int N = Vec<T>::N;
 #pragma unroll 4
-    for (int i = threadIdx.x; i < rows * A; i += kSmallRows) {
-        const int r = a_mul != 0 ? (int)__umulhi((uint32_t)i, a_mul) : i, j = i - r * A;
-        tile[r * stride + j] = clean(Vec<T>::load(P.logits + (row0 + r) * P.ld + j));
+        for (int i = threadIdx.x * N; i < rows * A - N + 1; i += kSmallRows * N) {
+            float f[N];
+            Vec<T>::unpack(*reinterpret_cast<const uint4*>(from + i), f);
+#pragma unroll
+            for (int k = 0; k < N; k += 2) {
+                const int at = i + k + (int)__umulhi((uint32_t)(i + k), a_mul);
+                tile[at] = clean(f[k]);
+                tile[at + 1] = clean(f[k + 1]);
+            }
+        }
+        for (int i = rows * A / N * N + threadIdx.x; i < rows * A; i += kSmallRows)
+            tile[i + (int)__umulhi((uint32_t)i, a_mul)] = clean(Vec<T>::load(from + i));
+    } else {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < rows * A; i += kSmallRows) {
+            const int r = a_mul != 0 ? (int)__umulhi((uint32_t)i, a_mul) : i, j = i - r * A;
+            tile[r * stride + j] = clean(Vec<T>::load(from + r * P.ld + j));
+        }
     }
     __syncthreads();
     if (row >= P.R) return;
@@ -145,6 +163,22 @@ __global__ void __launch_bounds__(kSmallRows) sample_small_kernel(const __grid_c
     for (int j = 0; j < A; ++j) m = fmaxf(m, x[j]);
     if (m == -INFINITY) return write_none(P, row);
     u64 all = 0, kept = 0, stay = 0;
+    if (r.limit == A && r.p >= 1.f && r.low == 0.f) {          // no filter: the weights take the logits' places
+#pragma unroll 2
+        for (int j = 0; j < A; ++j) {
+            const uint32_t w = weight_of(expf(scaled(x[j], m, r.inv_t)));
+            x[j] = __uint_as_float(w);
+            all += w;
+        }
+        const u64 target = target_of(P.uniforms[row], all);
+        u64 sum = 0;
+        int a = 0;
+        for (; a < A - 1; ++a) {
+            sum += __float_as_uint(x[a]);
+            if (sum > target) break;
+        }
+        return write_row(P, row, a, clean(Vec<T>::load(from + threadIdx.x * P.ld + a)), m, r.inv_t, all, all);
+    }
     for (int j = 0; j < A; ++j) {
         const float e = expf(scaled(x[j], m, r.inv_t));
         const uint32_t w = weight_of(e);
