@@ -783,10 +783,10 @@ def _typed(t, kind: str, shape, what: str, device: int):
     return t.data_ptr()
 
 
-def _output(t, kind: str, shape, what: str, where, device: int):
-    """(tensor, pointer) of an output: the caller's, checked, or a new one."""
+def _output(t, kind: str, shape, what: str, device: int):
+    """(tensor, pointer) of an output: the caller's, checked, or a new one on the current device."""
     if t is None:
-        t = _alloc(shape, _dtype(kind), where)
+        t = _alloc(shape, _dtype(kind), device)
         return t, t.data_ptr()
     return t, _typed(t, kind, shape, what, device)
 
@@ -822,10 +822,9 @@ def _sample_actions(name, kind, logits, uniforms, temperature, top_k, top_p, min
     k, k_all = _per_row(top_k, "i32", n, 0, "top_k", dev)
     p, p_all = _per_row(top_p, "f32", n, 1.0, "top_p", dev)
     m, m_all = _per_row(min_p, "f32", n, 0.0, "min_p", dev)
-    where = logits.device
-    a, ap = _output(actions, "i32", n, "actions", where, dev)
-    lp, lpp = _output(log_probs, "f32", n, "log_probs", where, dev)
-    kp, kpp = _output(kept_log_probs, "f32", n, "kept_log_probs", where, dev)
+    a, ap = _output(actions, "i32", n, "actions", dev)
+    lp, lpp = _output(log_probs, "f32", n, "log_probs", dev)
+    kp, kpp = _output(kept_log_probs, "f32", n, "kept_log_probs", dev)
     _check(getattr(lib(), name)(ptr, ld, _typed(uniforms, "f32", n, "uniforms", dev), t, k, p, m, t_all, min(int(k_all), 2 ** 31 - 1),
                                 p_all, m_all, ap, lpp, kpp, R, A, _stream(stream)))
     return a, lp, kp
@@ -851,19 +850,19 @@ def _policy_grad(name, kind, logits, actions, advantages, old_log_probs, mask, t
     dev = _device_for(logits)
     ptr, ld = _rows(logits, kind, "logits", dev)
     R, A = logits.shape
-    n, where = (R,), logits.device
-    lp, lpp = _output(log_probs, "f32", n, "log_probs", where, dev)
-    ent, entp = _output(entropy, "f32", n, "entropy", where, dev)
+    n = (R,)
+    lp, lpp = _output(log_probs, "f32", n, "log_probs", dev)
+    ent, entp = _output(entropy, "f32", n, "entropy", dev)
     dptr, ldd, lossp = None, 0, None
     if advantages is None:
         if old_log_probs is not None or loss is not None or dlogits is not None:
             raise ValueError("old_log_probs, loss and dlogits go with advantages")
     else:
-        loss, lossp = _output(loss, "f32", n, "loss", where, dev)
+        loss, lossp = _output(loss, "f32", n, "loss", dev)
         if dlogits is not None:
             dptr, ldd = _rows(dlogits, kind, "dlogits", dev, (R, A))
         elif want_grad:
-            dlogits = _alloc((R, A), logits.dtype, where)
+            dlogits = _alloc((R, A), logits.dtype, dev)
             dptr, ldd = dlogits.data_ptr(), A
     _check(getattr(lib(), name)(ptr, ld, _typed(actions, "i32", n, "actions", dev), _ptr(mask, "u8", n),
                                 _typed(advantages, "f32", n, "advantages", dev), _typed(old_log_probs, "f32", n, "old_log_probs", dev),
@@ -890,6 +889,9 @@ def rlcs_policy_grad_bf16(logits, actions, advantages=None, *, old_log_probs=Non
                         entropy_coef, scale, want_grad, loss, log_probs, entropy, dlogits, stream)
 
 
+_attention_bytes: dict = {}            # workspace bytes by sizes
+
+
 def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, block_table, lens, *, scale,
                                max_prefix_len=None, max_len=None, want_lse=True, out=None, lse=None, workspace=None, stream=None):
     """One query a row over its group's paged prefix and its own pages.  q [B, H, d] (rows may be strided), caches
@@ -914,16 +916,21 @@ def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, g
     own_width = block_table.shape[1]
     mp = prefix_width * page if max_prefix_len is None else min(int(max_prefix_len), prefix_width * page)
     ml = own_width * page if max_len is None else min(int(max_len), own_width * page)
-    out, outp = _output(out, "bf16", (B, H, d), "out", q.device, dev)
+    out, outp = _output(out, "bf16", (B, H, d), "out", dev)
     lsep = None
     if lse is not None or want_lse:
-        lse, lsep = _output(lse, "f32", (B, H), "lse", q.device, dev)
+        lse, lsep = _output(lse, "f32", (B, H), "lse", dev)
     if workspace is None or callable(workspace):
-        need = lib().rlcs_prefix_attention_workspace_bytes(B, H, Hk, d, page, groups, mp, ml)
+        sizes = (B, H, Hk, d, page, groups, mp, ml)
+        need = _attention_bytes.get(sizes)
+        if need is None:
+            if len(_attention_bytes) >= 4096:
+                _attention_bytes.clear()
+            need = _attention_bytes[sizes] = int(lib().rlcs_prefix_attention_workspace_bytes(*sizes))
         if workspace is not None:
             workspace = workspace(need)
         else:
-            workspace = _alloc((max(need, 16),), _torch().uint8, q.device)
+            workspace = _alloc((max(need, 16),), _torch().uint8, dev)
             if stream is not None:
                 workspace.record_stream(stream)
     if workspace.get_device() != dev:
@@ -945,11 +952,11 @@ def rlcs_block_tables(cached, added, free_pages, block_table, *, page_size, num_
     if cached.dim() != 1 or free_pages.dim() != 1 or block_table.dim() != 2:
         raise ValueError("expected cached [B], free_pages [F], block_table [B, width]")
     B, width = block_table.shape
-    where, dev = cached.device, _device_for(cached)
-    slots, sp = _output(slots, "i64", (num_slots,), "slots", where, dev)
-    positions, pp = _output(positions, "i32", (num_slots,), "positions", where, dev)
-    offsets, op = _output(offsets, "i32", (B + 1,), "offsets", where, dev)
-    page_offsets, gp = _output(page_offsets, "i32", (B + 1,), "page_offsets", where, dev)
+    dev = _device_for(cached)
+    slots, sp = _output(slots, "i64", (num_slots,), "slots", dev)
+    positions, pp = _output(positions, "i32", (num_slots,), "positions", dev)
+    offsets, op = _output(offsets, "i32", (B + 1,), "offsets", dev)
+    page_offsets, gp = _output(page_offsets, "i32", (B + 1,), "page_offsets", dev)
     _check(lib().rlcs_block_tables(
         _typed(cached, "i32", (B,), "cached", dev), _typed(added, "i32", (B,), "added", dev),
         _typed(free_pages, "i32", None, "free_pages", dev), _typed(block_table, "i32", None, "block_table", dev),

@@ -984,8 +984,12 @@ int sample_run(const SampleParams<T>& P, int64_t A, void* stream) {
         int ranks = 1;
         while (ranks < kMaxCluster && P.R * ranks < 4 * rlcs_device::limits().sms && A / (2 * ranks) >= 4096) ranks *= 2;
         if (P.R * ranks > kMostBlocks) return RLCS_ERR_SIZE;
-        if (cudaFuncSetAttribute(sample_cluster_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)) != cudaSuccess)
-            return RLCS_ERR_CUDA;
+        static bool granted[64];                             // room beyond 48 KB of shared memory, asked for once a device
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RLCS_ERR_CUDA;
+        if (!granted[dev])
+            granted[dev] = cudaFuncSetAttribute(sample_cluster_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)) == cudaSuccess;
+        if (!granted[dev]) return RLCS_ERR_CUDA;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(P.R * ranks));
         cfg.blockDim = dim3(kT);
