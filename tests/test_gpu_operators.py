@@ -649,3 +649,49 @@ def test_tables_repeat_is_the_same_and_large_pages():
         assert torch.equal(a, b)
     base = (2 ** 31 - 1) << 20
     assert one[0].tolist() == [base, base + 1, base + 2, (4 << 20) + 5]       # slots past 32 bits
+
+
+# ------------------------------------------------------------------------------------------ together
+def test_operators_work_together_in_the_example():
+    """The example's policy acts, is credited and learns: its reward rises well above chance (one in six), the same on a second run."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "token_rollout.py")
+    spec = importlib.util.spec_from_file_location("token_rollout", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    history = example.train(iterations=25, say=None)
+    assert abs(history[0] - 1 / 6) < 0.08 and sum(history[-3:]) / 3 > 0.4, history
+    assert example.train(iterations=3, say=None) == history[:3]
+
+
+def test_operators_in_a_graph(api):
+    """Captured with caller-owned outputs and workspace, replayed on new inputs in the same buffers."""
+    from paper_2608_17641_b200 import binding
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.randn(7, 5000, device="cuda", generator=g).bfloat16()
+    u, adv = torch.rand(7, device="cuda", generator=g), torch.randn(7, device="cuda", generator=g)
+
+    def work():
+        a, lp, kp = api.sample_actions(x, u, top_k=30, top_p=0.9)
+        return (a, lp, kp, *api.compute_policy_gradient(x, a, adv, entropy_coef=0.1))
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        work()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    plain = binding._alloc
+    binding._alloc = lambda shape, dtype, device: torch.empty(shape, dtype=dtype, device="cuda")      # guard bands are filled outside a capture only
+    try:
+        with torch.cuda.graph(graph):
+            out = work()
+    finally:
+        binding._alloc = plain
+    for seed in (1, 2):
+        x.copy_(torch.randn(7, 5000, device="cuda", generator=g))
+        u.copy_(torch.rand(7, device="cuda", generator=g))
+        graph.replay()
+        for got, want in zip(out, work()):
+            assert torch.equal(got, want)
