@@ -862,8 +862,15 @@ def _policy_grad(name, kind, logits, actions, advantages, old_log_probs, mask, t
         if dlogits is not None:
             dptr, ldd = _rows(dlogits, kind, "dlogits", dev, (R, A))
         elif want_grad:
-            dlogits = _alloc((R, A), logits.dtype, dev)
-            dptr, ldd = dlogits.data_ptr(), A
+            # rows as far apart, and as far from a 16-byte boundary, as the logits': both are then walked in whole vectors
+            # (rows of up to 64 actions leave as one block of memory, which wants them close together)
+            ldd, lead = (ld, ptr % 16 // logits.element_size()) if A > 64 and ld - A <= A // 8 + 16 else (A, 0)
+            if ldd == A and lead == 0:
+                dlogits = _alloc((R, A), logits.dtype, dev)
+            else:
+                dlogits = _alloc((R * ldd + lead,), logits.dtype, dev)
+                dlogits = dlogits.as_strided((R, A), (ldd, 1), dlogits.storage_offset() + lead)
+            dptr = dlogits.data_ptr()
     _check(getattr(lib(), name)(ptr, ld, _typed(actions, "i32", n, "actions", dev), _ptr(mask, "u8", n),
                                 _typed(advantages, "f32", n, "advantages", dev), _typed(old_log_probs, "f32", n, "old_log_probs", dev),
                                 lossp, lpp, entp, dptr, ldd, R, A, temperature, clip, entropy_coef, scale,

@@ -119,7 +119,119 @@ __device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t 
     return g;
 }
 
-// 65 to 2048 actions: one warp a row, two passes over it, the second from L1 or L2.
+// 65 to 2048 (fp32) or 4096 (bfloat16) actions: G lanes a row, NV vectors of it in the registers of each.
+template <typename T, int G, int NV>
+__global__ void __launch_bounds__(256) policy_group_kernel(const __grid_constant__ PolicyParams<T> P) {
+    constexpr int N = Vec<T>::N;
+    const int lane = threadIdx.x % G;
+    const int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    const bool there = row < P.R;                              // every lane takes part in the sums
+    const T* x = P.logits + (there ? row : 0) * P.ld;
+    const int a = there ? P.actions[row] : -1;
+    const bool live = there && (P.mask == nullptr || P.mask[row] != 0) && a >= 0 && a < P.A;
+    const Given given = given_of(P, row, live);
+    const Span sp = span_of(x, P.A);
+    const int rest = sp.head + sp.vecs * N, singles = sp.head + P.A - rest;
+    const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
+    auto single = [&](int i) { return i < sp.head ? i : rest + i - sp.head; };
+    constexpr int kOnes = (2 * N - 2 + G - 1) / G;             // elements before and behind the vectors, a lane
+    uint4 v[NV];
+    float one[kOnes];
+    const float xa = live ? Vec<T>::load(x + a) : 0.f;
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+        v[q] = live && q * G + lane < sp.vecs ? body[q * G + lane] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+#pragma unroll
+    for (int q = 0; q < kOnes; ++q) one[q] = live && q * G + lane < singles ? Vec<T>::load(x + single(q * G + lane)) : -INFINITY;
+    uint32_t most = Vec<T>::kNothing;
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+        most = Vec<T>::most_number(most, Vec<T>::most_number(Vec<T>::most_number(v[q].x, v[q].y), Vec<T>::most_number(v[q].z, v[q].w)));
+    Stat st = {Vec<T>::most_number_of(most), 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < kOnes; ++q) st.m = fmaxf(st.m, one[q]);
+#pragma unroll
+    for (int o = G / 2; o; o >>= 1) st.m = fmaxf(st.m, __shfl_xor_sync(~0u, st.m, o));
+    const float base = st.m == -INFINITY ? 0.f : st.m;
+    const float2 less = {-base, -base}, scale = {P.exp2_t, P.exp2_t};
+    float2 s = {0.f, 0.f}, u = {0.f, 0.f};
+    auto take = [&](float2 f) {
+        const float2 t = mul2(add2(f, less), scale), w = make_float2(exp2_of(t.x), exp2_of(t.y));
+        s = add2(s, w);
+        u = fma2(w, make_float2(fmaxf(t.x, kLowest), fmaxf(t.y, kLowest)), u);
+    };
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+        float f[N];
+        Vec<T>::unpack(v[q], f);
+#pragma unroll
+        for (int j = 0; j < N; j += 2) take(make_float2(f[j], f[j + 1]));
+    }
+#pragma unroll
+    for (int q = 0; q < kOnes; ++q) take(make_float2(one[q], -INFINITY));
+    st.s = s.x + s.y;
+    st.u = u.x + u.y;
+#pragma unroll
+    for (int o = G / 2; o; o >>= 1) {
+        st.s += __shfl_xor_sync(~0u, st.s, o);
+        st.u += __shfl_xor_sync(~0u, st.u, o);
+    }
+    constexpr float kLn2 = 0.6931471805599453f;
+    if (!there) return;
+    const RowGrad g = finish_row(P, row, given, st, (xa - st.m) * P.inv_t, kLn2, live, lane == 0);
+    if (P.dlogits == nullptr) return;
+    T* y = P.dlogits + row * P.ldd;
+    const float c0 = g.live ? g.c0 * g.inv_s : 0.f, c1 = g.live ? g.c1 * g.inv_s : 0.f;
+    const float2 two0 = {c0, c0}, two1 = {c1, c1};
+#pragma unroll
+    for (int q = 0; q < NV; ++q)                               // unpacked again, not kept unpacked since the sums: half the registers
+        asm volatile("" : "+r"(v[q].x), "+r"(v[q].y), "+r"(v[q].z), "+r"(v[q].w));
+    auto grad2 = [&](float2 f) {
+        const float2 t = mul2(add2(f, less), scale);
+        return mul2(make_float2(exp2_of(t.x), exp2_of(t.y)), fma2(two1, make_float2(fmaxf(t.x, kLowest), fmaxf(t.y, kLowest)), two0));
+    };
+    const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0;
+    uint4* out = reinterpret_cast<uint4*>(y + sp.head);
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+        if (q * G + lane >= sp.vecs) break;
+        const int at = sp.head + (q * G + lane) * N;
+        float f[N];
+        if (g.live) {
+            Vec<T>::unpack(v[q], f);
+#pragma unroll
+            for (int j = 0; j < N; j += 2) {
+                const float2 r = grad2(make_float2(f[j], f[j + 1]));
+                f[j] = r.x;
+                f[j + 1] = r.y;
+            }
+            if (a >= at && a < at + N) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] -= at + j == a ? g.hit : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[j] = 0.f;
+        }
+        if (same) {
+            out[q * G + lane] = Vec<T>::pack(f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) Vec<T>::store(y + at + j, f[j]);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kOnes; ++q)
+        if (q * G + lane < singles) {
+            const int j = single(q * G + lane);
+            Vec<T>::store(y + j, g.live ? grad2(make_float2(one[q], one[q])).x - (j == a ? g.hit : 0.f) : 0.f);
+        }
+}
+
+// Rows of up to 16 KB: one warp a row, two passes over it, the second from L1 or L2 (67 million logits, shares of the copy bandwidth:
+// 4096 fp32 0.63 and 8192 bfloat16 0.55, against 0.58 and 0.47 with a block a row; 8192 fp32 0.52 against 0.86).
+constexpr int kWarpBytes = 16384;
+
 template <typename T>
 __global__ void __launch_bounds__(256) policy_warp_kernel(const __grid_constant__ PolicyParams<T> P) {
     constexpr int N = Vec<T>::N, kAhead = 2, NT = 32;
@@ -693,7 +805,17 @@ int policy_run(const T* logits, int64_t ld, const int32_t* actions, const uint8_
         if (blocks > (int64_t(1) << 31) - 1) return RLCS_ERR_SIZE;
         const uint32_t mul = A > 1 ? (uint32_t)(((uint64_t(1) << 32) + A - 1) / A) : 0;
         policy_small_kernel<T><<<(unsigned)blocks, kSmallRows, kSmallRows * (A | 1) * sizeof(float), s>>>(P, mul);
-    } else if (A <= 2048) {
+    } else if (const int64_t vecs = A / Vec<T>::N; vecs <= 512) {
+        const int lanes = vecs <= 64 ? 8 : 32;
+        const int64_t blocks = (R * lanes + 255) / 256;
+        if (blocks > (int64_t(1) << 31) - 1) return RLCS_ERR_SIZE;
+        const unsigned n = (unsigned)blocks;
+        if (vecs <= 32) policy_group_kernel<T, 8, 4><<<n, 256, 0, s>>>(P);
+        else if (vecs <= 64) policy_group_kernel<T, 8, 8><<<n, 256, 0, s>>>(P);
+        else if (vecs <= 128) policy_group_kernel<T, 32, 4><<<n, 256, 0, s>>>(P);
+        else if (vecs <= 256) policy_group_kernel<T, 32, 8><<<n, 256, 0, s>>>(P);
+        else policy_group_kernel<T, 32, 16><<<n, 256, 0, s>>>(P);
+    } else if (A * (int64_t)sizeof(T) <= kWarpBytes) {
         const int64_t blocks = (R + 7) / 8;
         policy_warp_kernel<T><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, s>>>(P);
     } else {

@@ -231,6 +231,11 @@ __global__ void __launch_bounds__(kSmallRows) sample_small_kernel(const __grid_c
 }
 
 // ---------------------------------------------------------------------------------------------- up to 1024 actions
+// A 64-bit sum over the warp of values below 2^40: two hardware sums.
+__device__ __forceinline__ u64 redux_sum(u64 v) {
+    return (u64)__reduce_add_sync(~0u, (uint32_t)v & 0xfffffu) + ((u64)__reduce_add_sync(~0u, (uint32_t)(v >> 20)) << 20);
+}
+
 // One warp a row, the row's keys and weights in registers (lane l holds elements l, l + 32, ...).  A cut is found bit by
 // bit from the top: 32 (16) rounds of a comparison and an addition an element.
 template <typename T, int PER>
@@ -265,8 +270,8 @@ __global__ void __launch_bounds__(256) sample_warp_kernel(const __grid_constant_
         if (!(e >= r.low)) w[i] = 0;
         kept += w[i];
     }
-    all = warp_sum(all);
-    kept = r.low > 0.f ? warp_sum(kept) : all;
+    all = redux_sum(all);
+    kept = r.low > 0.f ? redux_sum(kept) : all;
     uint32_t cut = 0;
     int ties = A;
     if (r.limit == 1) {
@@ -289,7 +294,7 @@ __global__ void __launch_bounds__(256) sample_warp_kernel(const __grid_constant_
             kept += key[i] > cut ? w[i] : 0u;
         }
         ties = r.limit - __reduce_add_sync(~0u, n);
-        kept = warp_sum(kept) + (u64)ties * weight_at(K::value(cut), m, r);
+        kept = redux_sum(kept) + (u64)ties * weight_at(K::value(cut), m, r);
     }
     if (r.p < 1.f && r.limit > 1) {
         const double enough = (double)r.p * (double)kept;
@@ -300,12 +305,12 @@ __global__ void __launch_bounds__(256) sample_warp_kernel(const __grid_constant_
             u64 n = 0;
 #pragma unroll
             for (int i = 0; i < PER; ++i) n += key[i] >= next ? w[i] : 0u;
-            if ((double)warp_sum(n) >= enough) c = next;
+            if ((double)redux_sum(n) >= enough) c = next;
         }
         u64 above = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) above += key[i] > c ? w[i] : 0u;
-        above = warp_sum(above);
+        above = redux_sum(above);
         const uint32_t at = weight_at(K::value(c), m, r);
         const int more = ties_until(enough, above, at);
         if (c > cut || more < ties) ties = more;
@@ -322,7 +327,7 @@ __global__ void __launch_bounds__(256) sample_warp_kernel(const __grid_constant_
         const bool in = key[i] > cut || (tied && seen + __popc(tie_lanes & ((1u << lane) - 1)) < ties);
         seen += __popc(tie_lanes);
         const u64 mine = in ? w[i] : 0u;
-        const u64 step = warp_sum(mine);
+        const u64 step = redux_sum(mine);
         if (sum + step > target) {
             u64 run = mine;
 #pragma unroll
@@ -826,11 +831,11 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                 Cut c;
                 c.above_weight = __shfl_sync(~0u, to_weight - bin_weight, b);
                 c.above_count = __shfl_sync(~0u, to_count - bin_count, b);
-                auto least = [&](int bin) {                  // the least key whose step is at most `bin`, 32 tried at once
+                auto least_key = [&](auto holds) {           // the least key for which it holds (as for all above), 32 tried at once
                     uint32_t lo = K::of(-INFINITY), hi = top_key;
                     while (lo < hi) {
                         const uint32_t step = (hi - lo + 31) / 32, at = min(lo + lane * step, hi);
-                        const unsigned yes = __ballot_sync(~0u, bin_of(K::value(at)) <= bin);
+                        const unsigned yes = __ballot_sync(~0u, holds(K::value(at)));
                         const int first = yes ? __ffs(yes) - 1 : 32;
                         const uint32_t from = lo;
                         if (first < 32) hi = min(from + first * step, hi);
@@ -839,10 +844,10 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
                     }
                     return lo;
                 };
-                c.lo = least(b);
-                c.hi = b == 0 ? top_key : least(b - 1) - 1;
-                if (K::kDown && b == kCoarse - 1)            // 16-bit keys are counted without their weights: none of weight 0
-                    while (c.lo < c.hi && weight_of(expf(relative(K::value(c.lo)))) == 0) ++c.lo;
+                // the last step also takes all that weighs nothing, which 16-bit keys, counted without their weights, must leave out
+                c.lo = b == kCoarse - 1 ? least_key([&](float f) { return weight_of(expf(relative(f))) != 0; })
+                                        : least_key([&](float f) { return bin_of(f) <= b; });
+                c.hi = b == 0 ? top_key : least_key([&](float f) { return bin_of(f) <= b - 1; }) - 1;
                 while (c.lo < c.hi) {
                     int shift = 0;
                     while ((c.hi - c.lo) >> shift >= kFine) ++shift;
@@ -975,10 +980,13 @@ int sample_run(const SampleParams<T>& P, int64_t A, void* stream) {
         if (blocks > kMostBlocks) return RLCS_ERR_SIZE;
         const uint32_t mul = A > 1 ? (uint32_t)(((uint64_t(1) << 32) + A - 1) / A) : 0;
         sample_small_kernel<T><<<(unsigned)blocks, kSmallRows, kSmallRows * (A | 1) * sizeof(float), s>>>(P, mul);
-    } else if (A <= 1024) {
+    } else if (A <= 2048) {
         if (warps > kMostBlocks) return RLCS_ERR_SIZE;
-        if (A <= 256) sample_warp_kernel<T, 8><<<(unsigned)warps, 256, 0, s>>>(P);
-        else sample_warp_kernel<T, 32><<<(unsigned)warps, 256, 0, s>>>(P);
+        if (A <= 128) sample_warp_kernel<T, 4><<<(unsigned)warps, 256, 0, s>>>(P);
+        else if (A <= 256) sample_warp_kernel<T, 8><<<(unsigned)warps, 256, 0, s>>>(P);
+        else if (A <= 512) sample_warp_kernel<T, 16><<<(unsigned)warps, 256, 0, s>>>(P);
+        else if (A <= 1024) sample_warp_kernel<T, 32><<<(unsigned)warps, 256, 0, s>>>(P);
+        else sample_warp_kernel<T, 64><<<(unsigned)warps, 256, 0, s>>>(P);
     } else {
         // blocks a row: until the GPU has four a multiprocessor, or a part would fall below 4096 actions
         int ranks = 1;

@@ -318,6 +318,51 @@ def test_policy_sizes(api, A, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A", [65, 128, 255, 257, 600, 1030, 4097, 8200, 16390, 33000, 140001, 262144, 700001])
+def test_policy_sizes_of_every_way(api, A, dtype):
+    """Lanes, warps, one block and clusters of 2 to 8 a row, kept on the chip or read twice; rows at odd addresses, disallowed actions and
+    rows left out between the others, more rows than clusters run at once."""
+    R = 9 if A < 20000 else 3
+    x, a, adv, g = policy_inputs(R, A, dtype, A)
+    x[torch.rand(R, A, generator=g) < 0.2] = -math.inf
+    x[torch.arange(R), a.long()] = 1.5
+    mask = torch.ones(R, dtype=torch.bool)
+    mask[1] = False
+    for pad, offset, in_place in ((0, 0, False), (A % 3 + 1, 1, False), (0, 3, True)):
+        check_policy(api, x, a, adv, mask=mask, T=0.8, c=0.05, scale=1 / R, pad=pad, offset=offset, in_place=in_place)
+
+
+def test_policy_gradient_into_a_buffer_of_another_alignment():
+    from paper_2608_17641_b200 import binding
+    for A in (50, 300, 3000, 9000):
+        x, a, adv, _ = policy_inputs(6, A, BF16, A)
+        want = binding.rlcs_policy_grad_bf16(up(x), up(a), up(adv), entropy_coef=0.2)
+        out = strided_rows(torch.zeros(6, A, dtype=BF16), 3, 1)
+        got = binding.rlcs_policy_grad_bf16(up(x), up(a), up(adv), entropy_coef=0.2, dlogits=out)
+        for v, w in zip(got, want):
+            assert torch.equal(v, w)
+
+
+def test_policy_more_rows_than_run_at_once(api):
+    """The persistent clusters of the wide kernel take several rows each, dead ones among them."""
+    R, A = 1300, 10001
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(R, A, device="cuda", generator=g).bfloat16()
+    a = torch.randint(0, A, (R,), device="cuda", generator=g, dtype=torch.int32)
+    adv, mask = torch.randn(R, device="cuda", generator=g), torch.rand(R, device="cuda", generator=g) < 0.7
+    loss, lp, h, grad = api.compute_policy_gradient(x, a, adv, mask=mask, entropy_coef=0.1)
+    ref = torch.log_softmax(x.double(), 1)
+    p = ref.exp()
+    ent = -(p * ref).sum(1)
+    la = ref.gather(1, a[:, None].long())[:, 0]
+    live = mask.double()
+    assert ((lp - la * live).abs() <= 2e-5).all() and ((h - ent * live).abs() <= 2e-5).all()
+    hot = torch.zeros_like(p).scatter_(1, a[:, None].long(), 1.0)
+    want = live[:, None] * (adv.double()[:, None] * (p - hot) + 0.1 * p * (ref + ent[:, None]))
+    assert ((grad - want).abs() <= 2.0 ** -8 * want.abs() + 1e-6).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("R", [1, 7, 8, 9, 1000, 4099])
 def test_policy_row_counts(api, R, dtype):
     x, a, adv, _ = policy_inputs(R, 18, dtype, R)
