@@ -188,14 +188,12 @@ _scratch: dict = {}
 
 
 def _scratch_of(like, nbytes: int, stream):
-    """Uninitialised workspace of at least nbytes, one per (device, stream); replaced by a larger one when a call needs it."""
+    """Uninitialised workspace of at least nbytes, one per (device, stream); replaced by a larger one when a call needs it (pass
+    workspace= to calls that a graph captures)."""
     key = (like.device, _B._stream(stream))
     buf = _scratch.get(key)
     if buf is None or buf.numel() < nbytes:
-        buf = _B._alloc((max(nbytes, 1 << 20),), _torch().uint8, like.device)
-        if stream is not None:
-            buf.record_stream(stream)
-        _scratch[key] = buf
+        buf = _scratch[key] = _B._alloc((max(nbytes, 1 << 20),), _torch().uint8, like.device)
     return buf
 
 

@@ -7,6 +7,7 @@ Nothing is computed here; there is no CPU path.  A missing library raises at fir
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 
@@ -743,6 +744,19 @@ def rlcs_episodic_prefix_sum_time_major(x, dones, *, starts_at=False, sums=None,
 
 
 # ------------------------------------------------------------------ rollout and policy operators
+def _on_stream(wrapper):
+    """stream= makes that stream current for the whole call: what the call allocates then belongs to the stream that writes it, and
+    is not handed out again, or taken from a pending use, in another stream's order.  (Inputs of another stream stay the caller's
+    to order and to record.)"""
+    @functools.wraps(wrapper)
+    def call(*args, stream=None, **kwargs):
+        if stream is None:
+            return wrapper(*args, **kwargs)
+        with _torch().cuda.stream(stream):
+            return wrapper(*args, stream=stream, **kwargs)
+    return call
+
+
 _KINDS = {"f32": "float32", "bf16": "bfloat16", "i32": "int32", "i64": "int64"}
 _dtypes: dict = {}
 
@@ -830,6 +844,7 @@ def _sample_actions(name, kind, logits, uniforms, temperature, top_k, top_p, min
     return a, lp, kp
 
 
+@_on_stream
 def rlcs_sample_actions(logits, uniforms, *, temperature=None, top_k=None, top_p=None, min_p=None, actions=None, log_probs=None,
                         kept_log_probs=None, stream=None):
     """Actions drawn from float32 logits [R, A] (rows may be strided) with one uniform a row; temperature, top_k (int32), top_p
@@ -838,6 +853,7 @@ def rlcs_sample_actions(logits, uniforms, *, temperature=None, top_k=None, top_p
                            kept_log_probs, stream)
 
 
+@_on_stream
 def rlcs_sample_actions_bf16(logits, uniforms, *, temperature=None, top_k=None, top_p=None, min_p=None, actions=None, log_probs=None,
                              kept_log_probs=None, stream=None):
     """rlcs_sample_actions on bfloat16 logits."""
@@ -880,6 +896,7 @@ def _policy_grad(name, kind, logits, actions, advantages, old_log_probs, mask, t
     return (loss, lp, ent, dlogits) if dlogits is not None else (loss, lp, ent)
 
 
+@_on_stream
 def rlcs_policy_grad(logits, actions, advantages=None, *, old_log_probs=None, mask=None, temperature=1.0, clip=0.2, entropy_coef=0.0,
                      scale=1.0, want_grad=True, loss=None, log_probs=None, entropy=None, dlogits=None, stream=None):
     """Policy loss of float32 logits [R, A] (rows may be strided) and its gradient: (loss, log_probs, entropy, dlogits), without
@@ -888,6 +905,7 @@ def rlcs_policy_grad(logits, actions, advantages=None, *, old_log_probs=None, ma
                         scale, want_grad, loss, log_probs, entropy, dlogits, stream)
 
 
+@_on_stream
 def rlcs_policy_grad_bf16(logits, actions, advantages=None, *, old_log_probs=None, mask=None, temperature=1.0, clip=0.2,
                           entropy_coef=0.0, scale=1.0, want_grad=True, loss=None, log_probs=None, entropy=None, dlogits=None,
                           stream=None):
@@ -899,6 +917,7 @@ def rlcs_policy_grad_bf16(logits, actions, advantages=None, *, old_log_probs=Non
 _attention_bytes: dict = {}            # workspace bytes by sizes
 
 
+@_on_stream
 def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, block_table, lens, *, scale,
                                max_prefix_len=None, max_len=None, want_lse=True, out=None, lse=None, workspace=None, stream=None):
     """One query a row over its group's paged prefix and its own pages.  q [B, H, d] (rows may be strided), caches
@@ -938,8 +957,6 @@ def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, g
             workspace = workspace(need)
         else:
             workspace = _alloc((max(need, 16),), _torch().uint8, dev)
-            if stream is not None:
-                workspace.record_stream(stream)
     if workspace.get_device() != dev:
         _require_current_device(workspace, "workspace")
     _check(lib().rlcs_prefix_attention_bf16(
@@ -952,6 +969,7 @@ def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, g
     return out if lse is None else (out, lse)
 
 
+@_on_stream
 def rlcs_block_tables(cached, added, free_pages, block_table, *, page_size, num_slots, slots=None, positions=None, offsets=None,
                       page_offsets=None, stream=None):
     """One step's page tables (block_table [B, width], in place), slot map and positions from int32 lengths on the GPU.  Returns

@@ -710,6 +710,34 @@ def test_operators_work_together_in_the_example():
     assert example.train(iterations=3, say=None) == history[:3]
 
 
+def test_outputs_belong_to_the_stream_that_writes_them(api):
+    """A call on a side stream, right behind a long pending use of freed memory on the current one: its outputs must not lie there."""
+    from paper_2608_17641_b200 import binding
+    plain = binding._alloc
+    binding._alloc = lambda shape, dtype, device: torch.empty(shape, dtype=dtype, device="cuda")
+    try:
+        g = torch.Generator(device="cuda").manual_seed(0)
+        x = torch.randn(64, 4000, device="cuda", generator=g)
+        a = torch.randint(0, 4000, (64,), device="cuda", generator=g, dtype=torch.int32)
+        adv = torch.randn(64, device="cuda", generator=g)
+        want = [v.clone() for v in api.compute_policy_gradient(x, a, adv)]
+        big = torch.randn(6000, 6000, device="cuda", generator=g)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        for _ in range(3):
+            gone = torch.empty(64, 4000, device="cuda")
+            for _ in range(4):
+                big @ big                                     # keeps the current stream busy
+            gone.fill_(7.0)                                   # pending when its memory is given back
+            del gone
+            got = api.compute_policy_gradient(x, a, adv, stream=side)
+            torch.cuda.synchronize()
+            for v, w in zip(got, want):
+                assert torch.equal(v, w)
+    finally:
+        binding._alloc = plain
+
+
 def test_operators_in_a_graph(api):
     """Captured with caller-owned outputs and workspace, replayed on new inputs in the same buffers."""
     from paper_2608_17641_b200 import binding
