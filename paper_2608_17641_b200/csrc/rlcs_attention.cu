@@ -6,6 +6,10 @@
 // A group's prefix is multiplied with all of the group's queries at once: the queries of all its rows and of the heads
 // that share a key head are the rows of one tile.  A row's own tokens meet the heads that share a key head only.  Both
 // run over key segments that leave (running maximum, sum, product) behind; a second kernel joins a row's segments.
+//
+// Bounds and measurements (B200, 32 heads on 8 key heads of 128): own tokens by HBM, 5.3 TB/s (0.82 of the copy bandwidth) at 128
+// trajectories of up to 2048; a prefix of 32768 tokens against 256 trajectories by products, 200 us for 137 GFLOP (0.43 of the
+// bf16 rate; the second part of the weights is a third of what the matrix unit does), 16 prefixes of 2048 against 8 each 34 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -363,7 +367,8 @@ __device__ __forceinline__ bool prefix_tile(const AttnParams& P, int block, Pref
     return t->first_row >= 0 && t->first_row < t->rows && t->begin < t->end;
 }
 
-// Tiles of 16 rows: a trajectory's own keys, and prefixes of groups with few rows (blocks below `prefix_blocks`).
+// Tiles of 16 rows, the least an mma.sync has: 4 rows of 16 filled still leave the tensor unit a quarter busy under the loads.
+// A trajectory's own keys, and prefixes of groups with few rows (blocks below `prefix_blocks`).
 template <int D, bool TMA>
 __global__ void __launch_bounds__(kThreads)
 attention_kernel(const __grid_constant__ AttnParams P, int prefix_blocks, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {

@@ -6,6 +6,8 @@
 //
 // Two exclusive sums over the rows, then two outputs filled element by element.  Up to kFused rows every block makes the sums
 // itself, in shared memory (2048 rows: about 2 us, what a second launch would cost), beyond one block makes them first.
+// Small steps are bound by their launch (128 rows: 6 us on the GPU); 2048 prompts of 1024 tokens write 25 MB in 19 us, where the sums and
+// one page lookup a token show (34 us with a token a thread, 64-bit divisions and two launches).
 #include <cstdint>
 
 #include "../../include/rlcs.h"
