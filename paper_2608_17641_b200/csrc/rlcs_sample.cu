@@ -5,8 +5,8 @@
 // made between the same numbers on every run.
 //
 // The floor is one read of the logits (256 x 131072 bfloat16: 10 us); what bounds these kernels is instructions, about 24 for an exact
-// weight, of which expf is 9.  Measured: 1 x 131072 bfloat16 with top-k 13 us, 256 x 131072 without filters 63, top-k 50 56,
-// top-p 0.9 about 200; 262144 x 18 fp32 without filters 14.
+// weight, of which expf is 9.  Measured: 1 x 131072 bfloat16 with top-k 13 us, 256 x 131072 without filters 56, top-k 50 48,
+// top-p 0.9 178; 262144 x 18 fp32 without filters 14.
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -353,9 +353,10 @@ __global__ void __launch_bounds__(256) sample_warp_kernel(const __grid_constant_
 //   no cut (no top-k, no top-p):  maximum; weights by warp; one warp walks the range that holds the target.
 //   top-k up to 192: the k-th largest of the threads' own maxima bounds the k-th largest logit from below, so that few
 //     candidates pass it (about 200 of 131072 for k = 192 and 2048 threads); one block sorts them and does the rest.
-//   otherwise a histogram of weights and counts over 32 steps of (l - max) / T, one column a lane and so without atomics,
+//   otherwise a histogram of weights and counts over 24 steps of (l - max) / T, one column a lane and so without atomics (48 KB: four
+//     blocks a multiprocessor, 119 us for 256 x 131072 with mixed settings; 32 steps and three blocks: 133),
 //     finds the step that holds a cut; histograms over the keys of that step alone narrow it to one key.
-constexpr int kT = 256, kW = kT / 32, kCoarse = 32, kFine = 1024, kList = 2048, kListLimit = 192, kMaxCluster = 8;
+constexpr int kT = 256, kW = kT / 32, kCoarse = 24, kFine = 1024, kList = 2048, kListLimit = 192, kMaxCluster = 8;
 constexpr u64 kCountOne = 1ull << 48;                        // a column's entry: count above, weight below bit 48
 
 struct Shared {
@@ -630,7 +631,7 @@ struct Cut {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_constant__ SampleParams<T> P) {
+__global__ void __launch_bounds__(kT, 4) sample_cluster_kernel(const __grid_constant__ SampleParams<T> P) {
     typedef Key<T> K;
     extern __shared__ __align__(16) char raw[];
     Shared& sh = *reinterpret_cast<Shared*>(raw);
@@ -812,7 +813,7 @@ __global__ void __launch_bounds__(kT, 3) sample_cluster_kernel(const __grid_cons
             row_.sync();
             u64 bin_weight = 0, to_weight;                   // lane = step: its own, and up to and with it
             uint32_t bin_count = 0, to_count;
-            for (int k = 0; k < ranks; ++k) { bin_weight += row_.other(k).coarse_weight[lane]; bin_count += row_.other(k).coarse_count[lane]; }
+            for (int k = 0; k < ranks && lane < kCoarse; ++k) { bin_weight += row_.other(k).coarse_weight[lane]; bin_count += row_.other(k).coarse_count[lane]; }
             to_weight = bin_weight;
             to_count = bin_count;
             for (int o = 1; o < 32; o <<= 1) {
@@ -992,7 +993,8 @@ int sample_run(const SampleParams<T>& P, int64_t A, void* stream) {
         else if (A <= 1024) sample_warp_kernel<T, 32><<<(unsigned)warps, 256, 0, s>>>(P);
         else sample_warp_kernel<T, 64><<<(unsigned)warps, 256, 0, s>>>(P);
     } else {
-        // blocks a row: until the GPU has four a multiprocessor (256 x 131072, 4 blocks: 133 us; 2: 175, 8: 155), or a part would
+        // blocks a row: until the GPU has four a multiprocessor (256 x 131072 with mixed settings, at three blocks a multiprocessor: 4 blocks a row 133 us,
+        // 2 175, 8 155), or a part would
         // fall below 4096 actions
         int ranks = 1;
         while (ranks < kMaxCluster && P.R * ranks < 4 * rlcs_device::limits().sms && A / (2 * ranks) >= 4096) ranks *= 2;

@@ -554,6 +554,31 @@ def test_attention_blocks_of_128_and_256_rows(api, prefix, page, d):
     check_attention(api, [prefix, max(1, prefix // 3)], [40, 73], [i % 3 for i in range(113)], 4, 1, d, page, seed=prefix)      # 160, 292 rows
 
 
+@pytest.mark.parametrize("d", [8, 40, 72, 104])
+@pytest.mark.parametrize("page", [16, 48])
+def test_attention_many_rows_with_few_dimensions(api, d, page):
+    check_attention(api, [200, 77], [30, 9], [i % 7 for i in range(39)], 8, 1, d, page, seed=d)
+
+
+@pytest.mark.parametrize("page", [16, 48, 64])
+@pytest.mark.parametrize("rows", [10, 40])
+def test_attention_missing_prefix_pages_of_many_rows(api, rows, page):
+    """Pages that are not there in a prefix that 80 and 320 query rows share, whole and partial tiles."""
+    n = 5 * page + 3
+    cache, cut = (Cache(5, [n], [4] * rows, page, 1, 64) for _ in range(2))
+    q = torch.randn(rows, 8, 64, generator=torch.Generator().manual_seed(6)).to(BF16)
+    cache.prefix_table[0, 1] = -1
+    cache.prefix_table[0, 4] = cache.k.shape[0] + 5
+    keep = [i for i in range(n) if i // page not in (1, 4)]
+    cut.keys["p", 0] = tuple(t[keep] for t in cut.keys["p", 0])
+    want, want_lse = plain_attention(q, cut, [0, rows], 0.125, rows, 1)
+    i32 = lambda *v: up(torch.tensor(v, dtype=torch.int32))
+    out, lse = api.shared_prefix_attention(up(q), cache.kd, cache.vd, up(cache.prefix_table), i32(n), i32(0, rows), up(cache.own_table), i32(*[4] * rows))
+    most = max(float(v.abs().max()) for _, v in cut.keys.values())
+    assert ((out.cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -15 * most).all()
+    assert ((lse.cpu().double() - want_lse).abs() <= 1e-5 + 2.0 ** -22 * want_lse.abs()).all()
+
+
 def test_attention_groups_of_any_size_and_rows_outside(api):
     check_attention(api, [40, 0, 33, 70], [0, 4, 1, 0], [3, 1, 0, 9, 12], 8, 4, 64, 16)
     check_attention(api, [40, 33], [2, 2], [3, 1, 0, 9, 12, 0, 5], 8, 4, 64, 16, first=2)      # rows before and after
