@@ -397,9 +397,9 @@ attention_kernel(const __grid_constant__ AttnParams P, int prefix_blocks, const 
 }
 
 // ---------------------------------------------------------------------------------------------- prefixes of many rows
-// RT tiles of 128 rows a block (RT = 2 where groups have more than 128) on tcgen05, each tile: scores S = Q K^T of 64 keys at a time into one of two 64-column buffers of tensor memory, the
-// weights back over them as two bfloat16 parts (32 columns each), O += P V accumulated in tensor memory.  Four warps a row
-// tile: one row a thread (maximum, exponentials, sums).  Two warps copy keys and values through the page table into a ring of
+// RT tiles of 128 rows a block (RT = 2 where groups have more than 128) on tcgen05, each tile: scores S = Q K^T of 64 keys at a
+// time into one of two 64-column buffers of tensor memory, the weights back over them as two bfloat16 parts (32 columns
+// each), O += P V accumulated in tensor memory.  Four warps a row tile: one row a thread (maximum, exponentials, sums).  Two warps copy keys and values through the page table into a ring of
 // slots in the layout that the matrix instructions read (128-byte rows, pieces exchanged by row).  Two warps a row tile issue
 // its products, one the scores and one the values: an issuing warp waits about 100 cycles at each barrier, in which the others
 // keep the matrix unit busy.  With one row tile a block, two blocks share a multiprocessor to the same end.
@@ -461,6 +461,7 @@ __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::l
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
 template <int D, bool TMA, int RT>
 __global__ void __launch_bounds__(PrefixShape<D, RT>::kThreads, 3 - RT)
 prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -629,11 +630,13 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
         bool fine = true;
         if constexpr (TMA) {
             const int whole = (t.end - t.begin) / kTile, box = P.page < kTile ? P.page : kTile;
+            int issued = 0;
             if (me == 0)
                 for (int i = 0; i < 2 * whole && fine; ++i) {
                     fine = room(i);
                     if (!fine) break;
                     const uint32_t bar = full + 8 * (i % kSlots), dst = ring + (i % kSlots) * Shape::kSlot;
+                    issued = i + 1;
                     bar_expect(bar, Shape::kSlot);
                     for (int row = 0; row < kTile; row += box) {
                         const int in = offset + (i >> 1) * kTile + row, pg = page_of(P, in);
@@ -657,6 +660,9 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
                     bar_arrive(full + 8 * ((2 * whole + 1) % kSlots));
                 }
             }
+            // no boxes in flight when the block ends, whoever gave up (the partial tile's slots were free: theirs had arrived)
+            int late = 0;
+            for (int i = max(0, issued - kSlots + (whole < tiles ? 2 : 0)); i < issued; ++i) bar_wait(full + 8 * (i % kSlots), (i / kSlots) & 1, &late);
         } else {
             for (int i = 0; i < 2 * tiles + kAhead && fine; ++i) {
                 if (i < 2 * tiles) {
