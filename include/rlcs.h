@@ -438,7 +438,7 @@ int rlcs_sample_actions_bf16(const uint16_t* logits, int64_t ld, const float* un
 
 /*
  * Log-probability, entropy and policy loss of given actions, and the loss's gradient, from logits [R, A] (row r at
- * logits + r*ld) in one launch.  x = logits / temperature, lp = log softmax(x), a = actions[r]:
+ * logits + r*ld, any alignment of a row; A <= 2^22) in one launch.  x = logits / temperature, lp = log softmax(x), a = actions[r]:
  *   log_probs[r] = lp_a;   entropy[r] = H = -sum_j p_j lp_j;   loss[r] = -scale * (gain + entropy_coef * H)
  *   gain = advantages[r] * lp_a                        where old_log_probs is NULL (policy gradient; V-trace's
  *                                                      pg_advantages, GAE's advantages)

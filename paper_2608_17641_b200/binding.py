@@ -190,9 +190,15 @@ def _check(status: int):
         raise RlcsError(status)
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 _cuda_current_device = None
