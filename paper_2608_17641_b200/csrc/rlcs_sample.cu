@@ -759,10 +759,12 @@ __global__ void __launch_bounds__(kT, 4) sample_cluster_kernel(const __grid_cons
                         }
                         __syncthreads();
                     }
-                const u64 entry = tid < r.limit ? sh.list[tid] : 0;
+                // fewer than the limit where the rest of the row is NaN
+                const int candidates = min(r.limit, (int)listed);
+                const u64 entry = tid < candidates ? sh.list[tid] : 0;
                 const int index = (int)~(uint32_t)entry;
                 const float f = K::value((uint32_t)(entry >> 32));
-                uint32_t w = tid < r.limit ? weight(f) : 0u;
+                uint32_t w = tid < candidates ? weight(f) : 0u;
                 u64 run = w;
                 for (int o = 1; o < 32; o <<= 1) {
                     const u64 u = __shfl_up_sync(~0u, run, o);
@@ -785,7 +787,7 @@ __global__ void __launch_bounds__(kT, 4) sample_cluster_kernel(const __grid_cons
                 const u64 target = target_of(uniform, kept);
                 if (w != 0) {
                     u64 upto = 0;
-                    for (int k = 0; k < r.limit; ++k) upto += sh.maxima[k] <= (uint32_t)index ? sh.list[k] : 0;
+                    for (int k = 0; k < candidates; ++k) upto += sh.maxima[k] <= (uint32_t)index ? sh.list[k] : 0;
                     if (upto > target && upto - w <= target) write_row(P, row, index, f, m, r.inv_t, all, kept);
                 }
             }
