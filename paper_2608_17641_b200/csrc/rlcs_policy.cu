@@ -85,7 +85,7 @@ template <typename T> __device__ __forceinline__ Given given_of(const PolicyPara
 template <typename T>
 __device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t row, const Given& given, Stat st, float d, float unit, bool live,
                                               bool write) {
-    live = live && st.m != -INFINITY;
+    live = live && (st.m != -INFINITY || st.s != st.s);     // maxima pass NaN over: a row of it is told from one of -inf by its sum
     float loss = 0.f, lp = 0.f, h = 0.f, slope = 0.f;
     const float log_s = logf(st.s), inv = 1.f / st.s;
     if (live) {
@@ -502,19 +502,18 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             m = max_nan(m, alone);
             m = gather_all(Stat{m, 0.f, 0.f}).m;
             Stat st = {0.f, 0.f, 0.f};
+            const float base = m == -INFINITY ? 0.f : m;     // -inf then weighs 0, and NaN stays NaN
             auto take = [&](float f) {
-                const float t = (f - m) * k, w = exp2_of(t);
+                const float t = (f - base) * k, w = exp2_of(t);
                 st.s += w;
                 st.u = fmaf(w, fmaxf(t, kLowest), st.u);
             };
-            if (m != -INFINITY) {
-                for (int i = lane; i < n; i += 32) {
-                    float f[N];
-                    Vec<T>::unpack(body[i], f);
-                    for (int j = 0; j < N; ++j) take(f[j]);
-                }
-                if (tid < singles) take(alone);
+            for (int i = lane; i < n; i += 32) {
+                float f[N];
+                Vec<T>::unpack(body[i], f);
+                for (int j = 0; j < N; ++j) take(f[j]);
             }
+            if (tid < singles) take(alone);
             st = gather_all(st);
             st.m = m;
             return st;

@@ -43,3 +43,46 @@ def test_sample_top_k_above_the_numbers_of_a_row(api, R, A, numbers, dtype):
             assert near_log_probs(got[1], want[1]) and near_log_probs(got[2], want[2])
 
 
+# ------------------------------------------------------------------------------------------ policy loss
+# one size (actions, type) for each way through the policy kernels: a thread, eight lanes, a warp in registers, a warp in two passes, a
+# cluster that stages its rows, a cluster that reads them twice
+POLICY_WAYS = [(6, F32), (64, BF16), (70, F32), (300, BF16), (1500, F32), (3000, BF16), (3500, F32), (8000, BF16), (5000, F32), (20000, BF16),
+               (140001, F32), (600000, BF16)]
+
+
+def nan_rows(A, dtype):
+    """Twelve rows: two ordinary ones, then rows without a number in all their kinds, one of -inf alone, one left out."""
+    x, a, adv, _ = policy_inputs(12, A, dtype, 3)
+    x[2:9] = -INF
+    x[2] = NAN
+    x[3, ::2] = NAN
+    x[4, 1::2] = NAN
+    x[5, 0] = NAN
+    x[6, A - 1] = NAN
+    x[7, A // 2] = NAN
+    x[9, A // 3] = INF
+    x[10] = NAN
+    mask = torch.ones(12, dtype=torch.uint8)
+    mask[10] = 0
+    return x, a, adv, mask, [2, 3, 4, 5, 6, 7, 9], [8, 10], [0, 1, 11]
+
+
+@pytest.mark.parametrize("A,dtype", POLICY_WAYS)
+def test_policy_rows_of_nan_are_not_left_out(api, A, dtype):
+    x, a, adv, mask, broken, out, fine = nan_rows(A, dtype)
+    xd, ad, advd, maskd = up(x), up(a), up(adv), up(mask)
+    old = torch.zeros(12, device="cuda")
+    clean = api.compute_policy_gradient(up(x[fine]), up(a[fine]), up(adv[fine]), entropy_coef=0.1)
+    for got in (api.compute_policy_gradient(xd, ad, advd, mask=maskd, entropy_coef=0.1),
+                api.compute_policy_gradient(xd, ad, advd, mask=maskd),
+                api.compute_policy_gradient(xd, ad, advd, mask=maskd, entropy_coef=0.1, old_log_probs=old),
+                api.compute_log_probs(xd, ad, mask=maskd)):
+        for v in got:
+            assert torch.isnan(v[broken]).all(), [i for i in broken if not torch.isnan(v[i]).all()]
+            assert (v[out] == 0).all()
+            assert torch.isfinite(v[fine]).all()
+    got = api.compute_policy_gradient(xd, ad, advd, mask=maskd, entropy_coef=0.1)
+    for v, w in zip(got, clean):
+        assert ((v[fine].double() - w.double()).abs() <= 1e-5 + 2.0 ** -7 * w.double().abs()).all()
+
+
