@@ -447,6 +447,7 @@ int rlcs_sample_actions_bf16(const uint16_t* logits, int64_t ld, const float* un
  * A row whose mask is 0 (mask may be NULL: all rows live), whose action lies outside [0, A) or whose logits are all -inf is
  * left out: its logits may hold anything, its outputs and gradient are 0.  In other rows logits of -inf have probability 0
  * and gradient 0 (an action of probability 0: log_prob -inf); a NaN or +inf, alone or among any others, makes the row's outputs NaN.
+ * An advantage or a ratio that is NaN (old_log_probs NaN, or -inf where the action's own is) makes the row's loss and gradient NaN.
  * loss and dlogits may be NULL; with both NULL, advantages and old_log_probs may be too (scoring only).  dlogits may be
  * the logits themselves (same pointer, ldd = ld).  temperature > 0, clip >= 0.
  */

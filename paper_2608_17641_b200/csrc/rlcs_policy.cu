@@ -100,6 +100,8 @@ __device__ __forceinline__ RowGrad finish_row(const PolicyParams<T>& P, int64_t 
                 const float free_ = ratio * adv, held = fminf(fmaxf(ratio, 1.f - P.clip), 1.f + P.clip) * adv;
                 gain = fminf(free_, held);
                 slope = free_ <= held ? free_ : 0.f;
+                // minimum and comparison pass NaN over; a ratio past the largest float times an advantage of 0 is 0 all the same
+                if (ratio != ratio || adv != adv) gain = slope = ratio + adv;
             }
             loss = -P.scale * (gain + P.bonus * h);
         }

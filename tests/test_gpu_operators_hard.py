@@ -86,3 +86,25 @@ def test_policy_rows_of_nan_are_not_left_out(api, A, dtype):
         assert ((v[fine].double() - w.double()).abs() <= 1e-5 + 2.0 ** -7 * w.double().abs()).all()
 
 
+@pytest.mark.parametrize("A,dtype", POLICY_WAYS)
+def test_policy_nan_in_the_acting_log_probs_is_seen(api, A, dtype):
+    """A ratio or an advantage that is NaN makes the row's loss and gradient NaN (not its log-probability and entropy); a ratio past the
+    largest float against an advantage of 0 does not."""
+    x, a, adv, _ = policy_inputs(8, A, dtype, 4)
+    x[5, a[5]] = -INF                                         # probability 0, and acted with probability 0
+    old = plain_policy(x, a, adv, None, None, 1.0, 0.2, 0, 1)[1].float()
+    old[1] = NAN
+    adv[2] = NAN
+    old[3], adv[3] = -200.0, 0.0
+    old[4], adv[4] = -200.0, -1.0                             # the ratio overflows: as far as the formula goes
+    old[5] = -INF
+    loss, lp, ent, grad = api.compute_policy_gradient(up(x), up(a), up(adv), old_log_probs=up(old), entropy_coef=0.1)
+    for r in (1, 2, 5):
+        assert torch.isnan(loss[r]) and torch.isnan(grad[r]).all(), r
+    assert torch.isfinite(ent).all() and torch.isfinite(lp[[0, 1, 2, 3, 4, 6, 7]]).all() and lp[5] == -INF
+    for r in (0, 3, 6, 7):
+        assert torch.isfinite(loss[r]) and torch.isfinite(grad[r]).all(), r
+    assert abs(float(loss[3] + 0.1 * ent[3])) <= 1e-6
+    assert loss[4] == INF
+
+
