@@ -97,7 +97,7 @@ class RlcsError(RuntimeError):
         super().__init__(lib().rlcs_status_string(status).decode())
 
 
-_recording = threading.local()        # .calls: list while prepare() runs a wrapper, absent otherwise
+_recording = threading.local()        # .calls, .held: lists while prepare() runs a wrapper, absent otherwise
 
 
 class _Recorder:
@@ -124,8 +124,8 @@ class Prepared:
     """A call whose arguments were checked and marshalled once (prepare()).  Calling it only makes the
     C call(s) -- a few microseconds of host time instead of the 12-28 that dtype, shape, device and
     pointer marshalling cost per call -- on the current stream, or on `stream_handle` (a raw
-    cudaStream_t as int) when given.  The tensors are kept alive by this object; `outputs` is what the
-    wrapper would have returned.  The caller must not free or resize them while it is in use, and must
+    cudaStream_t as int) when given.  The tensors are kept alive by this object, those too that the
+    wrapper made for itself (a workspace); `outputs` is what the wrapper would have returned.  The caller must not free or resize them while it is in use, and must
     call it with the device current on which it was prepared."""
 
     def __init__(self, calls, outputs, keep):
@@ -152,19 +152,19 @@ def prepare(wrapper, *args, **kwargs) -> Prepared:
     """
     real = lib()
     global _lib
-    _recording.calls = []
+    _recording.calls, _recording.held = [], []
     with _lock:
         _lib = _Recorder(real)
     try:
         outputs = wrapper(*args, **kwargs)
-        calls = list(_recording.calls)
+        calls, held = _recording.calls, _recording.held
     finally:
         with _lock:
             _lib = real
-        del _recording.calls
+        del _recording.calls, _recording.held
     if not calls:
         raise ValueError("prepare() takes one of the rlcs_* compute wrappers of this module")
-    return Prepared(calls, outputs, (args, kwargs))
+    return Prepared(calls, outputs, (args, kwargs, held))
 
 
 def lib() -> ctypes.CDLL:
@@ -249,6 +249,18 @@ def _alloc(shape, dtype, device):
     return _torch().empty(shape, dtype=dtype, device=device)
 
 
+def _held(t):
+    """A tensor whose pointer goes into a C call: under prepare(), which repeats the call later, it is kept for as long."""
+    held = getattr(_recording, "held", None)
+    if held is not None:
+        held.append(t)
+    return t
+
+
+def _new(shape, dtype, device):
+    return _held(_alloc(shape, dtype, device))
+
+
 _raw_stream = None
 
 
@@ -269,7 +281,7 @@ class Workspace:
     def __init__(self, N: int, T: int, device="cuda", stream=None, nbytes: int | None = None):
         torch = _torch()
         self.nbytes = int(lib().rlcs_workspace_bytes(N, T)) if nbytes is None else int(nbytes)
-        self.buf = _alloc((max(self.nbytes, 16),), torch.uint8, device) if self.nbytes else None
+        self.buf = _new((max(self.nbytes, 16),), torch.uint8, device) if self.nbytes else None
         if self.buf is not None:
             if stream is not None:
                 self.buf.record_stream(stream)     # the caching allocator must not hand it out again before that stream is done
@@ -297,7 +309,7 @@ def _ws(ws: Workspace | None):
 
 def _out(like, out):
     torch = _torch()
-    return _alloc(tuple(like.shape), torch.float32, like.device) if out is None else out
+    return _new(tuple(like.shape), torch.float32, like.device) if out is None else out
 
 
 def rlcs_gae(rewards, values, dones, truncs=None, trunc_bootstrap=None, bootstrap=None, *, gamma, lam,
@@ -564,7 +576,7 @@ def rlcs_debug_time_major_path(path: int = 0):
 # ------------------------------------------------------------------------------------------ bfloat16 tensors
 def _out16(like, out):
     torch = _torch()
-    return _alloc(tuple(like.shape), torch.bfloat16, like.device) if out is None else out
+    return _new(tuple(like.shape), torch.bfloat16, like.device) if out is None else out
 
 
 def rlcs_gae_bf16(rewards, values, dones, truncs=None, trunc_bootstrap=None, bootstrap=None, *, gamma, lam,
@@ -806,7 +818,7 @@ def _typed(t, kind: str, shape, what: str, device: int):
 def _output(t, kind: str, shape, what: str, device: int):
     """(tensor, pointer) of an output: the caller's, checked, or a new one on the current device."""
     if t is None:
-        t = _alloc(shape, _dtype(kind), device)
+        t = _new(shape, _dtype(kind), device)
         return t, t.data_ptr()
     return t, _typed(t, kind, shape, what, device)
 
@@ -888,9 +900,9 @@ def _policy_grad(name, kind, logits, actions, advantages, old_log_probs, mask, t
             # (rows of up to 64 actions leave as one block of memory, which wants them close together)
             ldd, lead = (ld, ptr % 16 // logits.element_size()) if A > 64 and ld - A <= A // 8 + 16 else (A, 0)
             if ldd == A and lead == 0:
-                dlogits = _alloc((R, A), logits.dtype, dev)
+                dlogits = _new((R, A), logits.dtype, dev)
             else:
-                dlogits = _alloc((R * ldd + lead,), logits.dtype, dev)
+                dlogits = _new((R * ldd + lead,), logits.dtype, dev)
                 dlogits = dlogits.as_strided((R, A), (ldd, 1), dlogits.storage_offset() + lead)
             dptr = dlogits.data_ptr()
     _check(getattr(lib(), name)(ptr, ld, _typed(actions, "i32", n, "actions", dev), _ptr(mask, "u8", n),
@@ -960,9 +972,9 @@ def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, g
                 _attention_bytes.clear()
             need = _attention_bytes[sizes] = int(lib().rlcs_prefix_attention_workspace_bytes(*sizes))
         if workspace is not None:
-            workspace = workspace(need)
+            workspace = _held(workspace(need))
         else:
-            workspace = _alloc((max(need, 16),), _torch().uint8, dev)
+            workspace = _new((max(need, 16),), _torch().uint8, dev)
     if workspace.get_device() != dev:
         _require_current_device(workspace, "workspace")
     _check(lib().rlcs_prefix_attention_bf16(

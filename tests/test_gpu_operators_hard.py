@@ -108,3 +108,53 @@ def test_policy_nan_in_the_acting_log_probs_is_seen(api, A, dtype):
     assert loss[4] == INF
 
 
+# ------------------------------------------------------------------------------------------ prepared, captured and concurrent calls
+def plain_memory(monkeypatch):
+    """Memory of torch's own allocator, which hands out again what is dropped (the harness's guard bands keep everything)."""
+    from paper_2608_17641_b200 import binding
+    monkeypatch.setattr(binding, "_alloc", lambda shape, dtype, device: torch.empty(shape, dtype=dtype, device="cuda"))
+
+
+def attention_inputs(B=8, prompt=700, own=300, seed=0):
+    """Two groups of rows, with every key in its own page order: what shared_prefix_attention() takes, and its lengths' bounds."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    page, Hk, d = 16, 2, 64
+    wp, wo = -(-prompt // page), -(-own // page)
+    ids = torch.randperm(2 * wp + B * wo, device="cuda", generator=g).int()
+    k, v = (torch.randn(ids.numel(), page, Hk, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    q = torch.randn(B, 8, d, device="cuda", generator=g).bfloat16()
+    return ((q, k, v, ids[:2 * wp].view(2, wp), i32(prompt, prompt // 2), i32(0, B // 2, B), ids[2 * wp:].view(B, wo),
+             torch.randint(0, own + 1, (B,), device="cuda", generator=g, dtype=torch.int32)), dict(max_prefix_len=prompt, max_len=own))
+
+
+def test_prepared_attention_keeps_its_workspace(monkeypatch):
+    """The workspace that the wrapper made is not handed to anybody else while the prepared call lives."""
+    from paper_2608_17641_b200 import binding
+    plain_memory(monkeypatch)
+    args, bounds = attention_inputs()
+    want = binding.rlcs_prefix_attention_bf16(*args, scale=0.125, **bounds)
+    need = binding.lib().rlcs_prefix_attention_workspace_bytes(8, 8, 2, 64, 16, 2, 700, 300)
+    step = binding.prepare(binding.rlcs_prefix_attention_bf16, *args, scale=0.125, **bounds)
+    others = [torch.full((need,), 85, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    for _ in range(3):
+        got = step()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert all((t == 85).all() for t in others)
+
+
+def test_prepared_sampling_and_policy_repeat_the_direct_call():
+    from paper_2608_17641_b200 import binding
+    x = torch.randn(9, 5000, generator=torch.Generator().manual_seed(0)).cuda()
+    u, adv = torch.rand(9, generator=torch.Generator().manual_seed(1)).cuda(), torch.arange(9.0).cuda()
+    sample = binding.prepare(binding.rlcs_sample_actions, x, u, top_k=30)
+    learn = binding.prepare(binding.rlcs_policy_grad, x, sample.outputs[0], adv, entropy_coef=0.1)
+    for seed in (2, 3):
+        x.copy_(torch.randn(9, 5000, generator=torch.Generator().manual_seed(seed)))
+        got = (*sample(), *learn())
+        want = binding.rlcs_sample_actions(x, u, top_k=30)
+        for v, w in zip(got, (*want, *binding.rlcs_policy_grad(x, want[0], adv, entropy_coef=0.1))):
+            assert torch.equal(v, w)
+
+

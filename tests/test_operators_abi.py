@@ -128,3 +128,100 @@ def test_binding_checks(monkeypatch):
         binding._typed(_FakeTensor(0, torch.int32, (3,)), "i32", (2,), "actions", 0)
     with pytest.raises(TypeError):
         binding._typed(_FakeTensor(0, torch.int64, (2,)), "i32", (2,), "actions", 0)
+
+
+class _FakeLibrary:
+    """The C library's functions by name, type and kind of result; none of them does anything."""
+
+    def __getattr__(self, name):
+        from paper_2608_17641_b200 import binding
+        argtypes, restype = binding.SIGNATURES[name]
+
+        def call(*args):
+            return 4096 if restype is binding._sz else OK
+        call.argtypes, call.restype, call.__name__ = argtypes, restype, name
+        return call
+
+
+class _Rows(_FakeTensor):
+    """A contiguous stand-in for a CUDA tensor of any shape."""
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, i=None):
+        steps = [1]
+        for n in self.shape[:0:-1]:
+            steps.insert(0, steps[0] * n)
+        return tuple(steps) if i is None else steps[i]
+
+    def numel(self):
+        n = 1
+        for d in self.shape:
+            n *= d
+        return n
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def record_stream(self, stream):
+        pass
+
+
+def _attention_args():
+    import torch
+    t = lambda dtype, *shape: _Rows(0, dtype, shape)
+    i32, bf16 = torch.int32, torch.bfloat16
+    cache = t(bf16, 9, 16, 2, 64)
+    return (t(bf16, 4, 8, 64), cache, cache, t(i32, 1, 4), t(i32, 1), t(i32, 2), t(i32, 4, 4), t(i32, 4))
+
+
+@pytest.mark.parametrize("case", ["attention", "attention, given room", "normalised GAE", "sampling", "policy", "tables"])
+def test_prepared_calls_hold_what_their_wrapper_made(monkeypatch, case):
+    """A prepared call repeats raw pointers: everything that the wrapper allocated stays until the prepared call itself is dropped."""
+    import gc
+    import weakref
+    import torch
+    from paper_2608_17641_b200 import binding
+    made = []
+
+    def alloc(shape, dtype, device):
+        shape = shape if isinstance(shape, tuple) else (shape,)
+        t = _Rows(0, dtype, shape)
+        made.append(weakref.ref(t))
+        return t
+
+    monkeypatch.setattr(binding, "_lib", _FakeLibrary())
+    monkeypatch.setattr(binding, "_alloc", alloc)
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_stream", lambda stream=None: 1234)
+    t = lambda dtype, *shape: _Rows(0, dtype, shape)
+    f32, i32 = torch.float32, torch.int32
+    x, u8 = t(f32, 2, 8), t(torch.uint8, 2, 8)
+    prepare = binding.prepare
+    if case.startswith("attention"):
+        room = dict(workspace=lambda nbytes: alloc((nbytes,), torch.uint8, 0)) if "room" in case else {}
+        step = prepare(binding.rlcs_prefix_attention_bf16, *_attention_args(), scale=0.1, **room)
+        assert len(made) == 3
+    elif case == "normalised GAE":
+        step = prepare(binding.rlcs_gae_normalized, x, x, u8, gamma=0.9, lam=0.9)
+        assert len(made) == 3
+    elif case == "sampling":
+        step = prepare(binding.rlcs_sample_actions, x, t(f32, 2))
+        assert len(made) == 3
+    elif case == "policy":
+        step = prepare(binding.rlcs_policy_grad, x, t(i32, 2), t(f32, 2))
+        assert len(made) == 4
+    else:
+        step = prepare(binding.rlcs_block_tables, t(i32, 4), t(i32, 4), t(i32, 9), t(i32, 4, 8), page_size=16, num_slots=5)
+        assert len(made) == 4
+    gc.collect()
+    assert all(m() is not None for m in made)
+    step()
+    step.outputs = None
+    gc.collect()
+    assert all(m() is not None for m in made)
+    assert getattr(binding._recording, "held", None) is None and getattr(binding._recording, "calls", None) is None
+    del step
+    gc.collect()
+    assert all(m() is None for m in made)
