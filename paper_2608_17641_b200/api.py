@@ -184,19 +184,6 @@ def compute_episodic_prefix_sum(x, dones, *, boundary="ends_at", time_major=Fals
 
 
 # ------------------------------------------------------------------ rollout and policy operators
-_scratch: dict = {}
-
-
-def _scratch_of(like, nbytes: int, stream):
-    """Uninitialised workspace of at least nbytes, one per (device, stream); replaced by a larger one when a call needs it (pass
-    workspace= to calls that a graph captures)."""
-    key = (like.device, _B._stream(stream))
-    buf = _scratch.get(key)
-    if buf is None or buf.numel() < nbytes:
-        buf = _scratch[key] = _B._alloc((max(nbytes, 1 << 20),), _torch().uint8, like.device)
-    return buf
-
-
 def _flat_rows(logits):
     """[..., A] logits as [rows, A] (a view) and the leading shape, None where it is [rows, A] already."""
     if logits.dim() == 2:
@@ -251,10 +238,10 @@ def shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, grou
     """Attention of one query a trajectory, q [B, H, d] bfloat16, over the paged prompt that its group shares and its own pages:
     (out [B, H, d], lse [B, H]).  Caches [pages, page, Hk, d]; group g holds rows group_offsets[g] to group_offsets[g+1]-1.
     scale defaults to d ** -0.5; max_prefix_len and max_len bound the lengths (by default what the tables can hold): closer
-    bounds give better launches."""
+    bounds give better launches and a smaller workspace (it grows with rows, heads and both bounds).  workspace: a uint8 tensor of
+    at least rlcs_prefix_attention_workspace_bytes bytes, whose calls the caller keeps ordered on the GPU; by default every call
+    takes one of its own from torch's allocator, so that calls of several threads, streams and captured graphs share none."""
     scale = q.shape[-1] ** -0.5 if scale is None else scale
-    if workspace is None:
-        workspace = lambda nbytes: _scratch_of(q, nbytes, stream)
     return _B.rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, group_offsets, block_table, lens, scale=scale,
                                          max_prefix_len=max_prefix_len, max_len=max_len, workspace=workspace, stream=stream)
 

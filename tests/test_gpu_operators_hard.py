@@ -158,3 +158,33 @@ def test_prepared_sampling_and_policy_repeat_the_direct_call():
             assert torch.equal(v, w)
 
 
+def test_attention_in_graphs_shares_no_workspace(api, monkeypatch):
+    """Captured without a workspace of the caller's, the first call of its stream among them; larger calls in between and other
+    tensors in the memory that they leave; two graphs of one capture stream replayed side by side."""
+    plain_memory(monkeypatch)
+    sets = [attention_inputs(seed=s) for s in (1, 2)]
+    want = [api.shared_prefix_attention(*args, **bounds) for args, bounds in sets]
+    large, large_bounds = attention_inputs(B=64, prompt=6000, own=2000, seed=3)
+    side = torch.cuda.Stream()
+    graphs, out = [torch.cuda.CUDAGraph() for _ in sets], []
+    torch.cuda.synchronize()
+    for graph, (args, bounds) in zip(graphs, sets):
+        with torch.cuda.graph(graph, stream=side):
+            out.append(api.shared_prefix_attention(*args, **bounds))
+    with torch.cuda.stream(side):
+        large_want = api.shared_prefix_attention(*large, **large_bounds)
+        others = [torch.full((n << 20,), 85, dtype=torch.uint8, device="cuda") for n in (1, 1, 2, 4, 8)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(50):
+        for stream, graph in zip(streams, graphs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    with torch.cuda.stream(side):
+        large_got = api.shared_prefix_attention(*large, **large_bounds)
+    torch.cuda.synchronize()
+    for got, exp in zip((*out, large_got), (*want, large_want)):
+        assert torch.equal(got[0], exp[0]) and torch.equal(got[1], exp[1])
+    assert all((t == 85).all() for t in others)
+
+

@@ -225,3 +225,46 @@ def test_prepared_calls_hold_what_their_wrapper_made(monkeypatch, case):
     del step
     gc.collect()
     assert all(m() is None for m in made)
+
+
+def test_attention_calls_share_no_workspace(monkeypatch):
+    """A call is several launches that hand results on through the workspace: another thread's call on the same stream, made while
+    the first is being enqueued, must not get the same one; and none is kept behind the calls' backs."""
+    import gc
+    import threading
+    import weakref
+    from paper_2608_17641_b200 import api, binding
+    made, seen = [], []
+
+    class Memory(_Rows):
+        def data_ptr(self):
+            return id(self)
+
+    def alloc(shape, dtype, device):
+        t = Memory(0, dtype, shape if isinstance(shape, tuple) else (shape,))
+        made.append(weakref.ref(t))
+        return t
+
+    class Library(_FakeLibrary):
+        def __getattr__(self, name):
+            fn = super().__getattr__(name)
+            if name != "rlcs_prefix_attention_bf16":
+                return fn
+
+            def call(*args):
+                seen.append(args[-3])
+                if len(seen) == 1:
+                    t = threading.Thread(target=lambda: api.shared_prefix_attention(*_attention_args()))
+                    t.start()
+                    t.join()
+                return OK
+            return call
+
+    monkeypatch.setattr(binding, "_lib", Library())
+    monkeypatch.setattr(binding, "_alloc", alloc)
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_stream", lambda stream=None: 1234)
+    api.shared_prefix_attention(*_attention_args())
+    assert len(seen) == 2 and seen[0] != seen[1]
+    gc.collect()
+    assert all(m() is None for m in made)
