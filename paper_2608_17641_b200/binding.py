@@ -975,8 +975,12 @@ def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, g
             workspace = _held(workspace(need))
         else:
             workspace = _new((max(need, 16),), _torch().uint8, dev)
+    if not getattr(workspace, "is_cuda", False):
+        raise TypeError("workspace must be a CUDA tensor")
     if workspace.get_device() != dev:
         _require_current_device(workspace, "workspace")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     _check(lib().rlcs_prefix_attention_bf16(
         q.data_ptr(), sq[0] if B > 1 else H * d, k_cache.data_ptr(), v_cache.data_ptr(), pages, sk[0], sk[1], sk[2],
         _typed(prefix_table, "i32", (groups, prefix_width), "prefix_table", dev), prefix_width,

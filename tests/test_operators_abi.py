@@ -268,3 +268,24 @@ def test_attention_calls_share_no_workspace(monkeypatch):
     assert len(seen) == 2 and seen[0] != seen[1]
     gc.collect()
     assert all(m() is None for m in made)
+
+
+def test_attention_workspace_is_checked(monkeypatch):
+    """A workspace in host memory, or with gaps, is refused: its pointer and size go to the kernels as they are."""
+    import torch
+    from paper_2608_17641_b200 import api, binding
+    monkeypatch.setattr(binding, "_lib", _FakeLibrary())
+    monkeypatch.setattr(binding, "_alloc", lambda shape, dtype, device: _Rows(0, dtype, shape))
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_stream", lambda stream=None: 1234)
+    with pytest.raises(TypeError):
+        api.shared_prefix_attention(*_attention_args(), workspace=torch.zeros(1 << 20, dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        api.shared_prefix_attention(*_attention_args(), workspace=4096)
+    with pytest.raises(ValueError):
+        api.shared_prefix_attention(*_attention_args(), workspace=_Rows(1, torch.uint8, (1 << 20,)))
+    gaps = _Rows(0, torch.uint8, (1 << 20,))
+    gaps.is_contiguous = lambda: False
+    with pytest.raises(ValueError):
+        api.shared_prefix_attention(*_attention_args(), workspace=gaps)
+    api.shared_prefix_attention(*_attention_args(), workspace=_Rows(0, torch.uint8, (1 << 20,)))
