@@ -425,7 +425,8 @@ int rlcs_episodic_prefix_sum_bf16(const uint16_t* x, const uint8_t* dones, uint1
  * temperature 1, kept_log_probs 0.  top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN: no such limit.  uniforms [R]
  * in [0, 1).  A logit of -inf or NaN is never drawn; a row with no other gets action -1 and log-probs -inf.  Weights
  * are whole numbers, so their sums, and with them the actions, do not depend on how a row is split over threads; an
- * action less likely than 2^-32 of the most likely one has weight 0.  A logit of +inf shares all weight with the others of the kind.
+ * action less likely than 2^-32 of the most likely one has weight 0 (log_probs, whose sum is of the e_j, counts it; a log-probability is
+ * within 1e-5 of exact, 2^-22 of it more).  A logit of +inf shares all weight with the others of the kind.
  */
 int rlcs_sample_actions(const float* logits, int64_t ld, const float* uniforms, const float* temperature, const int32_t* top_k,
                         const float* top_p, const float* min_p, float temperature_all, int32_t top_k_all, float top_p_all,
@@ -448,6 +449,7 @@ int rlcs_sample_actions_bf16(const uint16_t* logits, int64_t ld, const float* un
  * left out: its logits may hold anything, its outputs and gradient are 0.  In other rows logits of -inf have probability 0
  * and gradient 0 (an action of probability 0: log_prob -inf); a NaN or +inf, alone or among any others, makes the row's outputs NaN.
  * An advantage or a ratio that is NaN (old_log_probs NaN, or -inf where the action's own is) makes the row's loss and gradient NaN.
+ * Exponentials are the hardware's base-2 ones (2^-22 of each); sums are kept in fp32 relative to the running maximum.
  * loss and dlogits may be NULL; with both NULL, advantages and old_log_probs may be too (scoring only).  dlogits may be
  * the logits themselves (same pointer, ldd = ld).  temperature > 0, clip >= 0.
  */

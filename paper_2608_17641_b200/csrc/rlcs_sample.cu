@@ -111,11 +111,12 @@ __device__ __forceinline__ int ties_until(double enough, u64 above, uint32_t w) 
     return n;
 }
 
+// `all`: the softmax's sum, 1 for the most likely action
 template <typename T>
-__device__ __forceinline__ void write_row(const SampleParams<T>& P, int64_t row, int action, float x, float m, float inv_t, u64 all, u64 kept) {
+__device__ __forceinline__ void write_row(const SampleParams<T>& P, int64_t row, int action, float x, float m, float inv_t, double all, u64 kept) {
     const double d = (double)scaled(x, m, inv_t);
     P.actions[row] = action;
-    P.log_probs[row] = (float)(d - log((double)all * 0x1p-31));
+    P.log_probs[row] = (float)(d - log(all));
     P.kept_log_probs[row] = (float)(d - log((double)kept * 0x1p-31));
 }
 
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(kSmallRows) sample_small_kernel(const __grid_c
             sum += __float_as_uint(x[a]);
             if (sum > target) break;
         }
-        return write_row(P, row, a, clean(Vec<T>::load(from + threadIdx.x * P.ld + a)), m, r.inv_t, all, all);
+        return write_row(P, row, a, clean(Vec<T>::load(from + threadIdx.x * P.ld + a)), m, r.inv_t, (double)all * 0x1p-31, all);
     }
     for (int j = 0; j < A; ++j) {
         const float e = expf(scaled(x[j], m, r.inv_t));
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(kSmallRows) sample_small_kernel(const __grid_c
     for (int j = 0; j < A; ++j) {
         if (!(stay >> j & 1)) continue;
         sum += weight_at(x[j], m, r);
-        if (sum > target) return write_row(P, row, j, x[j], m, r.inv_t, all, kept);
+        if (sum > target) return write_row(P, row, j, x[j], m, r.inv_t, (double)all * 0x1p-31, kept);
     }
 }
 
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(256) sample_warp_kernel(const __grid_constant_
                 run += lane >= o ? v : 0;
             }
             const unsigned past = __ballot_sync(~0u, sum + run > target);
-            if (lane == __ffs(past) - 1) write_row(P, row, i * 32 + lane, K::value(key[i]), m, r.inv_t, all, kept);
+            if (lane == __ffs(past) - 1) write_row(P, row, i * 32 + lane, K::value(key[i]), m, r.inv_t, (double)all * 0x1p-31, kept);
             return;
         }
         sum += step;
@@ -372,6 +373,7 @@ struct Shared {
         };
     };
     u64 trade[2][kW], near[kW];
+    double whole[kW];                                        // each warp's part of sum_j e_j
     uint32_t trade_ties[2][kW], near_ties[kW];
     u64 coarse_weight[kCoarse];
     uint32_t coarse_count[kCoarse];
@@ -417,8 +419,11 @@ template <typename T> struct ClusterRow {
     __device__ __forceinline__ int tail_at() const { return sp.head + sp.vecs * Vec<T>::N; }
 
     // f(logit, index) for every element of a range, four vectors of a lane in flight; places behind the range hold -inf.
-    // Logits come as they are: NaN compares false and -0 equal to 0.
-    template <typename F> __device__ __forceinline__ void each(const Range& r, F f) const {
+    // Logits come as they are: NaN compares false and -0 equal to 0.  `then` is called after every vector.
+    struct Nothing {
+        __device__ __forceinline__ void operator()() const {}
+    };
+    template <typename F, typename G = Nothing> __device__ __forceinline__ void each(const Range& r, F f, G then = G()) const {
         constexpr int N = Vec<T>::N, kAhead = 4;
         const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
         const uint4 nothing = make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
@@ -434,12 +439,24 @@ template <typename T> struct ClusterRow {
             g[kAhead - 1] = v + 32 * kAhead < r.v1 ? __ldg(body + v + 32 * kAhead) : nothing;
 #pragma unroll
             for (int k = 0; k < N; ++k) f(e[k], sp.head + v * N + k);
+            then();
         }
         const int singles = r.head ? sp.head : 0, ends = r.tail ? A - tail_at() : 0;
         if (lane < singles + ends) {
             const int j = lane < singles ? lane : tail_at() + lane - singles;
             f(Vec<T>::load(x + j), j);
+            then();
         }
+    }
+    // The softmax's sum: parts left by every warp ahead of a barrier of the cluster, added up by a warp behind it.
+    __device__ __forceinline__ void leave_whole(double part) {
+        part = warp_sum(part);
+        if (lane == 0) sh.whole[warp] = part;
+    }
+    __device__ __forceinline__ double whole() {
+        double total = 0.;
+        for (int i = lane; i < ranks * kW; i += 32) total += other(i / kW).whole[i % kW];
+        return warp_sum(total);
     }
     // the largest logit of the lane's elements
     __device__ __forceinline__ float most() const {
@@ -648,17 +665,22 @@ __global__ void __launch_bounds__(kT, 4) sample_cluster_kernel(const __grid_cons
     const float exp2_t = fminf(r.inv_t * 1.4426950408889634f, 3.4028235e38f);
     // For a finite m.  A quick exponential where only its sum's logarithm counts (ex2.approx: 2^-22), not a choice;
     // far below the maximum, -inf and NaN: 0.
+    // That sum: a vector's terms in 32 bits, vectors in 64.  In 32 bits the thousands of terms that a thread may have would
+    // lose 1e-5 and more of it where their roundings have one sign; and the whole weights leave out what lies below 2^-32 of the
+    // most likely action, a million of which hold 1e-4.
     auto quick = [&](float f) { return exp2_of(fmaxf((f - m) * exp2_t, -1000.f)); };
     auto relative = [&](float f) { return fmaxf((f - m) * r.inv_t, -1000.f); };
     auto weight = [&](float f) {
         const float e = expf(relative(f));
         return e >= r.low ? weight_of(e) : 0u;
     };
-    auto all_of = [&](float part) { return row_.gather((u64)((double)part * 0x1p31 + 0.5)); };
+    float some = 0.f;                                        // of the vector's terms
+    double part = 0.;
+    auto vector_done = [&] { part += (double)some; some = 0.f; };
     const float uniform = P.uniforms[row];
-    u64 all = 0;
     auto done = [&](int a, u64 kept) {
-        if (lane == 0) write_row(P, row, a, clean(Vec<T>::load(x + a)), m, r.inv_t, all != 0 ? all : kept, kept);
+        const double all = row_.whole();
+        if (lane == 0) write_row(P, row, a, clean(Vec<T>::load(x + a)), m, r.inv_t, all, kept);
     };
 
     if (m == -INFINITY) {
@@ -666,30 +688,39 @@ __global__ void __launch_bounds__(kT, 4) sample_cluster_kernel(const __grid_cons
     } else if (m == INFINITY) {                              // the infinite ones share the probability
         uint32_t mine = 0;
         row_.each(row_.mine, [&](float f, int) { mine += f == m; });
+        row_.leave_whole((double)mine);
         const u64 there = row_.gather(mine);
         u64 ties = min(there, (u64)r.limit);
         if (r.p < 1.f) ties = min(ties, (u64)ties_until((double)r.p * (double)(ties << 31), 0, 0x80000000u));
-        all = there << 31;
         row_.pick(0, mine, m, ties, 0x80000000u, uniform, weight, done);
     } else if (r.limit == 1) {
-        float part = 0.f;
         uint32_t first = 0;                                  // ~index, so that the lowest wins
         row_.each(row_.mine, [&](float f, int j) {
-            part += quick(f);
+            some += quick(f);
             if (f == m) first = max(first, ~(uint32_t)j);
-        });
-        all = all_of(part);
+        }, vector_done);
+        row_.leave_whole(part);
         const int a = (int)~(uint32_t)row_.gather_max(first);
-        if (rank == 0 && tid == 0) write_row(P, row, a, m, m, r.inv_t, all, 0x80000000ull);
+        if (rank == 0 && warp == 0) {
+            const double all = row_.whole();
+            if (lane == 0) write_row(P, row, a, m, m, r.inv_t, all, 0x80000000ull);
+        }
     } else if (r.limit == P.A && r.p >= 1.f) {
         u64 mine = 0;
         if (r.low > 0.f) {
-            float part = 0.f;
-            row_.each(row_.mine, [&](float f, int) { part += quick(f); mine += weight(f); });
-            all = all_of(part);
+            row_.each(row_.mine, [&](float f, int) {
+                const float e = expf(relative(f));
+                some += e;
+                mine += e >= r.low ? weight_of(e) : 0u;
+            }, vector_done);
         } else {
-            row_.each(row_.mine, [&](float f, int) { mine += weight_of(expf(relative(f))); });
+            row_.each(row_.mine, [&](float f, int) {
+                const float e = expf(relative(f));
+                some += e;
+                mine += weight_of(e);
+            }, vector_done);
         }
+        row_.leave_whole(part);
         row_.pick(mine, 0, -INFINITY, 0, 0, uniform, weight, done);
     } else {
         bool listed_all = false;
@@ -733,19 +764,21 @@ __global__ void __launch_bounds__(kT, 4) sample_cluster_kernel(const __grid_cons
             }
             row_.sync();
             const float bound = K::value(max(lead.bound, K::of(-INFINITY)));
-            float part = 0.f;
             row_.each(row_.mine, [&](float f, int j) {
-                part += quick(f);
+                some += quick(f);
                 if (f >= bound && j < P.A) {
                     const uint32_t at = atomicAdd(&lead.listed, 1u);
                     if (at < kList) lead.list[at] = (u64)K::of(f + 0.f) << 32 | ~(uint32_t)j;
                 }
-            });
-            all = all_of(part);                              // its barrier also completes the list
+            }, vector_done);
+            row_.leave_whole(part);
+            part = 0.;
+            row_.sync();                                     // the list and the sum are complete
             const uint32_t listed = lead.listed;
             listed_all = listed <= kList;
             row_.sync();                                     // read by all before the room is used again
             if (listed_all && rank == 0) {
+                const double all = row_.whole();
                 int size = 32;
                 while (size < (int)listed) size *= 2;
                 for (int i = tid; i < size; i += kT) if (i >= (int)listed) sh.list[i] = 0;
@@ -801,8 +834,10 @@ __global__ void __launch_bounds__(kT, 4) sample_cluster_kernel(const __grid_cons
             row_.each(row_.mine, [&](float f, int) {
                 const float d = relative(f), e = expf(d);
                 const uint32_t w = weight_of(e);
+                some += e;
                 if (w != 0) column[min((int)(d * -kSteps), kCoarse - 1) * 32] += kCountOne + (e >= r.low ? w : 0u);
-            });
+            }, vector_done);
+            row_.leave_whole(part);
             __syncthreads();
             for (int b = warp; b < kCoarse; b += kW) {
                 u64 w = 0;
@@ -825,12 +860,6 @@ __global__ void __launch_bounds__(kT, 4) sample_cluster_kernel(const __grid_cons
             }
             const u64 weighed = __shfl_sync(~0u, to_weight, 31);
             const uint32_t counted = __shfl_sync(~0u, to_count, 31);
-            if (r.low == 0.f && all == 0) all = weighed;
-            if (all == 0) {
-                float part = 0.f;
-                row_.each(row_.mine, [&](float f, int) { part += quick(f); });
-                all = all_of(part);
-            }
             // the cut where `want` candidates, or `enough` weight, are reached: first the step, then its keys by histograms
             auto narrow = [&](bool by_count, uint32_t want, double enough) {
                 auto reached = [&](uint32_t n, u64 w) { return by_count ? n >= want : (double)w >= enough; };

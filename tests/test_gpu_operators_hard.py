@@ -43,6 +43,39 @@ def test_sample_top_k_above_the_numbers_of_a_row(api, R, A, numbers, dtype):
             assert near_log_probs(got[1], want[1]) and near_log_probs(got[2], want[2])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_sample_log_probs_of_long_even_rows(api, dtype):
+    """Enough rows for one block each, of logits that are all alike but a few: the softmax's sum has 2048 equal terms a thread, whose
+    roundings in 32 bits have one sign (3e-5 of the sum)."""
+    R, A = 600, 1 << 19
+    x = torch.zeros(R, A, dtype=dtype, device="cuda")
+    x[:, 77] = 2.8125
+    u = torch.zeros(R, device="cuda")
+    for k, others in ((0, 0), (30, 40)):
+        x[:, 100:100 + others] = 2.0
+        z = 1.0 + others * math.exp(2.0 - 2.8125) + (A - 1 - others) * math.exp(-2.8125)
+        for kw in (dict(temperature=0.0), dict(top_k=1), dict(min_p=0.5), dict(top_p=0.5), dict(top_p=0.5, min_p=0.01), dict(top_k=300), dict())[:7 if k == 0 else 1] \
+                + ((dict(top_k=k),) if k else ()):
+            a, lp, _ = api.sample_actions(x, u, **kw)
+            at = x.gather(1, a[:, None].long())[:, 0].double()
+            assert near_log_probs(lp, at - 2.8125 - math.log(z)), kw
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R", [1, 600])
+def test_sample_log_probs_count_what_cannot_be_drawn(api, R, dtype):
+    """A million actions 22.5 below the most likely one: each weighs nothing, together they hold 1.8e-4 of the probability."""
+    A = (1 << 20) + 3
+    x = torch.full((R, A), -22.5, dtype=dtype, device="cuda")
+    x[:, 5] = 0
+    want = -math.log(1.0 + (A - 1) * math.exp(-22.5))
+    u = torch.full((R,), 0.5, device="cuda")
+    for kw in (dict(), dict(temperature=0.0), dict(top_k=50), dict(top_k=500), dict(top_p=0.9), dict(min_p=0.01), dict(top_k=500, min_p=0.01)):
+        a, lp, kp = api.sample_actions(x, u, **kw)
+        assert (a == 5).all() and near_log_probs(lp, want), kw
+        assert (kp.abs() <= 1e-6).all(), kw
+
+
 # ------------------------------------------------------------------------------------------ policy loss
 # one size (actions, type) for each way through the policy kernels: a thread, eight lanes, a warp in registers, a warp in two passes, a
 # cluster that stages its rows, a cluster that reads them twice
