@@ -857,7 +857,7 @@ def _sample_actions(name, kind, logits, uniforms, temperature, top_k, top_p, min
     a, ap = _output(actions, "i32", n, "actions", dev)
     lp, lpp = _output(log_probs, "f32", n, "log_probs", dev)
     kp, kpp = _output(kept_log_probs, "f32", n, "kept_log_probs", dev)
-    _check(getattr(lib(), name)(ptr, ld, _typed(uniforms, "f32", n, "uniforms", dev), t, k, p, m, t_all, min(int(k_all), 2 ** 31 - 1),
+    _check(getattr(lib(), name)(ptr, ld, _typed(uniforms, "f32", n, "uniforms", dev), t, k, p, m, t_all, max(0, min(int(k_all), 2 ** 31 - 1)),
                                 p_all, m_all, ap, lpp, kpp, R, A, _stream(stream)))
     return a, lp, kp
 

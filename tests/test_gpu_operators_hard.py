@@ -76,6 +76,17 @@ def test_sample_log_probs_count_what_cannot_be_drawn(api, R, dtype):
         assert (kp.abs() <= 1e-6).all(), kw
 
 
+@pytest.mark.parametrize("A", [9, 300, 3000])
+def test_sample_top_k_of_any_whole_number(api, A):
+    """Numbers of no limit do not become one when they are cut to 32 bits."""
+    x = torch.randn(40, A, generator=torch.Generator().manual_seed(1)).cuda()
+    u = torch.rand(40, generator=torch.Generator().manual_seed(2)).cuda()
+    want = api.sample_actions(x, u)
+    for k in (-1, -2 ** 31, -2 ** 32 + 1, -2 ** 40 + 2, 2 ** 31, 2 ** 32 + 1, 2 ** 40):
+        for v, w in zip(api.sample_actions(x, u, top_k=k), want):
+            assert torch.equal(v, w), k
+
+
 # ------------------------------------------------------------------------------------------ policy loss
 # one size (actions, type) for each way through the policy kernels: a thread, eight lanes, a warp in registers, a warp in two passes, a
 # cluster that stages its rows, a cluster that reads them twice
