@@ -87,6 +87,22 @@ def test_sample_top_k_of_any_whole_number(api, A):
             assert torch.equal(v, w), k
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A", [9, 100, 1000, 5000])
+def test_sample_infinite_temperature(api, A, dtype):
+    """Every allowed action alike, disallowed ones still never drawn."""
+    g = torch.Generator(device="cuda").manual_seed(A)
+    x = torch.randn(200, A, device="cuda", generator=g).to(dtype)
+    x[:, 1::2] = -INF
+    x[::7, 2] = torch.finfo(dtype).min
+    n = (A + 1) // 2
+    u = torch.rand(200, device="cuda", generator=g)
+    for kw in (dict(), dict(top_k=n), dict(min_p=0.5), dict(top_p=1 - 2.0 ** -24)):
+        a, lp, kp = api.sample_actions(x, u, temperature=INF, **kw)
+        assert (a % 2 == 0).all() and (a >= 0).all(), kw
+        assert near_log_probs(lp, -math.log(n)) and near_log_probs(kp, -math.log(n)), kw
+
+
 # ------------------------------------------------------------------------------------------ policy loss
 # one size (actions, type) for each way through the policy kernels: a thread, eight lanes, a warp in registers, a warp in two passes, a
 # cluster that stages its rows, a cluster that reads them twice
