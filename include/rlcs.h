@@ -578,6 +578,13 @@ int rlcs_debug_force_wide_index(int on);
 int rlcs_debug_set_carry_fault(int64_t mute_tile, int64_t spin_cap);
 
 /*
+ * Test hook for the bounded waits of the policy-loss and attention kernels: subsequent calls in this process give up a wait after
+ * that many polls (0 = at once, negative = default).  The rows concerned come out NaN, and a block still ends only when what it
+ * has in flight has landed -- nothing hangs or faults.
+ */
+int rlcs_debug_set_wait_polls(int polls);
+
+/*
  * Test hook: path of the time-major entry points for subsequent calls in this process.  1 = the
  * register walk whatever the alignment; 3 = the shared-memory ring with one column per lane whatever
  * the size; 4 = a cut time axis always by three launches, never the chained kernel; 5 = the chained

@@ -74,6 +74,7 @@ SIGNATURES = {
     "rlcs_debug_set_tile_variant": ([_int], _int),
     "rlcs_debug_tile_elems": ([_int], _int),
     "rlcs_debug_set_carry_fault": ([_i64, _i64], _int),
+    "rlcs_debug_set_wait_polls": ([_int], _int),
     "rlcs_debug_time_major_path": ([_int], None),
     "rlcs_debug_vec_trace_plan": ([_int, _int], None),
     "rlcs_debug_stream_copy": ([_vp, _vp, _sz, _sz, _vp], _int),
@@ -556,6 +557,11 @@ def rlcs_debug_force_wide_index(on: bool):
 
 def rlcs_debug_set_carry_fault(mute_tile: int = -1, spin_cap: int = 0):
     _check(lib().rlcs_debug_set_carry_fault(mute_tile, spin_cap))
+
+
+def rlcs_debug_set_wait_polls(polls: int = -1):
+    """Test hook: polls after which a wait of the policy-loss and attention kernels gives up (0: at once; negative: default)."""
+    _check(lib().rlcs_debug_set_wait_polls(int(polls)))
 
 
 def rlcs_debug_stream_copy(src, dst, read_bytes: int, write_bytes: int, stream=None):

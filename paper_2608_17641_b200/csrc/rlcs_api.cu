@@ -11,6 +11,7 @@ long long g_spin_cap = 0;
 bool g_pdl = true;
 bool g_row_tiles = true;
 int g_row_blocks = -1;
+int g_wait_polls = -1;
 }  // namespace rlcs_hooks
 
 extern "C" {
@@ -405,6 +406,11 @@ int rlcs_debug_force_wide_index(int on) {
 int rlcs_debug_set_carry_fault(int64_t mute_tile, int64_t spin_cap) {
     g_mute_tile = mute_tile;
     g_spin_cap = spin_cap;
+    return RLCS_OK;
+}
+
+int rlcs_debug_set_wait_polls(int polls) {
+    rlcs_hooks::g_wait_polls = polls < 0 ? -1 : polls;
     return RLCS_OK;
 }
 

@@ -20,9 +20,15 @@
 #include "rlcs_device.cuh"
 #include "rlcs_pair.cuh"
 
+namespace rlcs_hooks {
+extern int g_wait_polls;      // rlcs_debug_set_wait_polls; defined in rlcs_api.cu
+}
+
 namespace {
 
 using namespace rlcs_pair;
+
+constexpr int kPolls = 1 << 20;                 // of a wait, before it gives up
 
 struct AttnParams {
     const __nv_bfloat16* q;
@@ -46,6 +52,7 @@ struct AttnParams {
     int prefix_rows;               // rows of a prefix block: 256 or 128 (tensor memory), or 16
     int prefix_tiles, own_tiles;   // slots of prefix tiles over all groups; tiles of 16 rows a trajectory
     int prefix_blocks;             // thread blocks of the prefix part
+    int polls;                     // kPolls, or a test's
     float scale_log2;
 };
 
@@ -86,8 +93,8 @@ __device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 // Bounded: a wait that runs out of polls, or sees that another did, gives up, and the block's rows come out NaN.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int* gave_up) {
-    for (int polls = 0; polls < (1 << 20); ++polls) {
+__device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int* gave_up, int most) {
+    for (int polls = 0; polls < most; ++polls) {
         uint32_t done;
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
@@ -214,11 +221,13 @@ __device__ __forceinline__ void segment(const AttnParams& P, const CUtensorMap* 
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
     bool fine = true;
-    for (int t = 0; t < steps; ++t) {
+    int t = 0;
+    for (; t < steps; ++t) {
         const uint32_t kt = ring + (t % kStages) * Shape::kStage, vt = kt + kValues;
         const int left = len - t * kTile;                     // keys that are there
         if constexpr (TMA) {
-            fine = __all_sync(~0u, bar_wait(bar + 8 * (t % kStages), (t / kStages) & 1, gave_up)) && fine;
+            fine = __all_sync(~0u, bar_wait(bar + 8 * (t % kStages), (t / kStages) & 1, gave_up, P.polls));
+            if (!fine) break;
             if (left < kPart) {                               // values behind the last key: zeros, whatever the page holds
                 for (int i = lane; i < (kPart - left) * (D / 8); i += 32)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vt + at(left + i / (D / 8), i % (D / 8))), "r"(0) : "memory");
@@ -298,7 +307,11 @@ __device__ __forceinline__ void segment(const AttnParams& P, const CUtensorMap* 
         __syncwarp();
         load(t + kStages);
     }
-    if (!fine) l[0] = l[1] = __int_as_float(0x7fffffff);
+    if (!fine) {
+        l[0] = l[1] = __int_as_float(0x7fffffff);
+        int late = 0;                                         // the boxes in flight land before their place is used otherwise
+        for (int u = t; u < min(t + kStages, steps); ++u) bar_wait(bar + 8 * (u % kStages), (u / kStages) & 1, &late, kPolls);
+    }
     __syncthreads();                                          // every warp is done with its stages
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -517,7 +530,7 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
         bool fine = true;
         for (int i = 0; i < tiles && rt < row_tiles; ++i) {
             const uint32_t at = tmem + mine + (i & 1) * kTile;
-            fine = __all_sync(~0u, bar_wait(my_s + 8 * (i & 1), (i >> 1) & 1, &gave_up));
+            fine = __all_sync(~0u, bar_wait(my_s + 8 * (i & 1), (i >> 1) & 1, &gave_up, P.polls));
             if (!fine) break;
             fence_after();
             if (any_row) {
@@ -543,7 +556,7 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
                 if (__any_sync(~0u, now > m + 8.f)) {
                     const float next = fmaxf(m, now), fade = m == -INFINITY ? 0.f : exp2_of(m - next);
                     if (i > 0) {
-                        fine = __all_sync(~0u, bar_wait(my_o + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, &gave_up));
+                        fine = __all_sync(~0u, bar_wait(my_o + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, &gave_up, P.polls));
                         if (!fine) break;
                         fence_after();
 #pragma unroll
@@ -585,7 +598,8 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
         }
         if (any_row) {
             for (int i = max(tiles - 2, 0); i < tiles && fine; ++i)
-                fine = __all_sync(~0u, bar_wait(my_o + 8 * (i & 1), (i >> 1) & 1, &gave_up));
+                fine = __all_sync(~0u, bar_wait(my_o + 8 * (i & 1), (i >> 1) & 1, &gave_up, P.polls));
+            fine = fine && *(volatile int*)&gave_up == 0;         // a thread that copies may have given up alone
             fence_after();
             const int at = t.first_row + warp * 32 + lane;
             const int64_t dst = (int64_t)t.seg * P.B * P.H + (int64_t)(t.b0 + at / P.r) * P.H + t.kv_head * P.r + at % P.r;
@@ -626,7 +640,7 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
                 if (row < kTile) copy16(dst + row * 128 + (((c & 7) ^ (row & 7)) << 4), base + (place[k] < 0 ? 0 : place[k]), place[k] >= 0);
             }
         };
-        auto room = [&](int item) { return item < kSlots || bar_wait(empty + 8 * (item % kSlots), (item / kSlots - 1) & 1, &gave_up); };
+        auto room = [&](int item) { return item < kSlots || bar_wait(empty + 8 * (item % kSlots), (item / kSlots - 1) & 1, &gave_up, P.polls); };
         bool fine = true;
         if constexpr (TMA) {
             const int whole = (t.end - t.begin) / kTile, box = P.page < kTile ? P.page : kTile;
@@ -660,9 +674,10 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
                     bar_arrive(full + 8 * ((2 * whole + 1) % kSlots));
                 }
             }
-            // no boxes in flight when the block ends, whoever gave up (the partial tile's slots were free: theirs had arrived)
+            // no boxes in flight when the block ends, whoever gave up (where the partial tile's slots were free, theirs had arrived)
             int late = 0;
-            for (int i = max(0, issued - kSlots + (whole < tiles ? 2 : 0)); i < issued; ++i) bar_wait(full + 8 * (i % kSlots), (i / kSlots) & 1, &late);
+            for (int i = max(0, issued - kSlots + (fine && whole < tiles ? 2 : 0)); i < issued; ++i)
+                bar_wait(full + 8 * (i % kSlots), (i / kSlots) & 1, &late, kPolls);
         } else {
             for (int i = 0; i < 2 * tiles + kAhead && fine; ++i) {
                 if (i < 2 * tiles) {
@@ -684,7 +699,7 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
         const int rt = (warp - kIssuer) >> 1;
         const uint32_t base = __shfl_sync(~0u, tmem, 0) + rt * 256;
         const uint32_t my_s = s_full + 16 * rt, my_p = p_full + 16 * rt, my_o = o_done + 16 * rt;
-        auto wait = [&](uint32_t bar, int parity) { return (bool)__all_sync(~0u, bar_wait(bar, parity & 1, &gave_up)); };
+        auto wait = [&](uint32_t bar, int parity) { return (bool)__all_sync(~0u, bar_wait(bar, parity & 1, &gave_up, P.polls)); };
         const int n = rt < row_tiles ? tiles : 0;
         bool fine = true;
         if (((warp - kIssuer) & 1) == 0) {
@@ -723,7 +738,7 @@ prefix_kernel(const __grid_constant__ AttnParams P, const __grid_constant__ CUte
         }
         commit(drained);                                          // nothing in flight when the memory is given back
         int late = 0;
-        bar_wait(drained, 0, &late);
+        bar_wait(drained, 0, &late, kPolls);
     }
     __syncwarp();
     __syncthreads();
@@ -962,6 +977,7 @@ int rlcs_prefix_attention_bf16(const uint16_t* q, int64_t q_stride, const uint16
     P.prefix_width = (int)prefix_width;
     P.own_width = (int)own_width;
     P.scale_log2 = scale * 1.4426950408889634f;
+    P.polls = rlcs_hooks::g_wait_polls >= 0 ? rlcs_hooks::g_wait_polls : kPolls;
     const size_t rows = (size_t)(P.prefix_segs + P.own_segs) * P.B * P.H;
     P.part_o = static_cast<float*>(workspace);
     P.part_ml = reinterpret_cast<float2*>(P.part_o + rows * (P.d <= 64 ? 64 : 128));

@@ -248,3 +248,40 @@ def test_attention_in_graphs_shares_no_workspace(api, monkeypatch):
     assert all((t == 85).all() for t in others)
 
 
+# ------------------------------------------------------------------------------------------ waits that run out
+@pytest.fixture
+def wait_polls():
+    from paper_2608_17641_b200 import binding
+    yield binding.rlcs_debug_set_wait_polls
+    binding.rlcs_debug_set_wait_polls(-1)
+
+
+@pytest.mark.parametrize("page", [16, 48])                    # copied by boxes, and piece by piece
+@pytest.mark.parametrize("rows", [4, 30, 70])                 # 16, 128 and 256 rows of a prompt at a time
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_waits_that_run_out(api, wait_polls, rows, page, d):
+    """Waits that give up at once or early: the call ends by itself, its rows are NaN or (where no wait of theirs ran out) right, and
+    nothing of it is still on its way: calls right behind it are as ever."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    prompt, own = 1500, 130
+    wp, wo = -(-prompt // page), -(-own // page)
+    ids = torch.randperm(wp + rows * wo, device="cuda", generator=g).int()
+    k, v = (torch.randn(ids.numel(), page, 1, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    q = torch.randn(rows, 4, d, device="cuda", generator=g).bfloat16()
+    lens = torch.randint(0, own + 1, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    call = lambda: api.shared_prefix_attention(q, k, v, ids[:wp].view(1, wp), i32(prompt), i32(0, rows), ids[wp:].view(rows, wo), lens)
+    want, want_lse = call()
+    for polls in (0, 0, 1, 2, 5, 20, 100):
+        wait_polls(polls)
+        out, lse = call()
+        wait_polls(-1)
+        again, again_lse = call()
+        broken = torch.isnan(lse)
+        assert torch.isnan(out[broken]).all()
+        assert torch.equal(out[~broken], want[~broken]) and torch.equal(lse[~broken], want_lse[~broken])
+        assert torch.equal(again, want) and torch.equal(again_lse, want_lse)
+        if polls == 0 and (page == 16 or rows > 4):           # small tiles copied piece by piece have no waits of this kind
+            assert broken.all()
+
+
