@@ -450,6 +450,8 @@ int rlcs_sample_actions_bf16(const uint16_t* logits, int64_t ld, const float* un
  * and gradient 0 (an action of probability 0: log_prob -inf); a NaN or +inf, alone or among any others, makes the row's outputs NaN.
  * An advantage or a ratio that is NaN (old_log_probs NaN, or -inf where the action's own is) makes the row's loss and gradient NaN.
  * Exponentials are the hardware's base-2 ones (2^-22 of each); sums are kept in fp32 relative to the running maximum.
+ * Every wait inside the kernels is bounded; should one run out, what depended on it comes out NaN (and rows are left unwritten where
+ * a second, longer wait runs out too).
  * loss and dlogits may be NULL; with both NULL, advantages and old_log_probs may be too (scoring only).  dlogits may be
  * the logits themselves (same pointer, ldd = ld).  temperature > 0, clip >= 0.
  */

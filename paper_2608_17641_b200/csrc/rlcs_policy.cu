@@ -18,6 +18,10 @@
 #include "rlcs_pair.cuh"
 #include "rlcs_rows.cuh"
 
+namespace rlcs_hooks {
+extern int g_wait_polls;      // rlcs_debug_set_wait_polls; defined in rlcs_api.cu
+}
+
 namespace {
 
 using namespace rlcs_pair;
@@ -38,6 +42,7 @@ template <typename T> struct PolicyParams {
     int64_t R;
     int A;
     float inv_t, exp2_t, clip, bonus, scale;       // 1 / T and log2(e) / T
+    int polls;                                     // kPolls, or a test's
 };
 
 constexpr float kLowest = -1.0e30f;      // stands for y = -inf where y multiplies exp(y / T) = 0
@@ -351,15 +356,24 @@ constexpr int kPart = kWarps * kShare * 16, kMostRanks = 8;
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+constexpr int kPolls = 1 << 20;                 // of a wait, before it gives up
+
 // Bounded; a wait that runs out leaves NaN in the row's outputs.
-__device__ __forceinline__ bool chunk_wait(uint32_t bar, int parity) {
-    for (int polls = 0; polls < (1 << 20); ++polls) {
+__device__ __forceinline__ bool chunk_wait(uint32_t bar, int parity, int most) {
+    for (int polls = 0; polls < most; ++polls) {
         uint32_t done;
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
         if (done) return true;
     }
     return false;
+}
+
+// What was given up is waited for once more, longer than another block of the cluster takes to give up: its place and its barrier are used
+// again, and no block ends while something is on its way to it.  `stuck`: not even that helped; no more copies, and the block leaves its
+// other rows as they are.
+__device__ __forceinline__ void wait_again(uint32_t bar, int parity, volatile int* stuck) {
+    if (*stuck || !chunk_wait(bar, parity, 8 * kPolls)) *stuck = 1;
 }
 
 // One row as a warp of the cluster sees it.
@@ -396,6 +410,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
     __shared__ Stat part[kWarps], joined;
     __shared__ __align__(16) float4 sent[2][kMostRanks];
     __shared__ RowGrad grad;
+    __shared__ int stuck;
     __shared__ __align__(8) uint64_t full[kWarps][kChunks], got[2];
     namespace cg = cooperative_groups;
     const cg::cluster_group cluster = cg::this_cluster();
@@ -404,6 +419,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
     const float k = P.exp2_t;
     uint4* const held = held_all + warp * kShare;
     if (tid < kWarps * kChunks) asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"(smem_at(&full[0][0] + tid)));
+    if (tid == 0) stuck = 0;
     if (tid < 2) asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"(smem_at(&got[tid])));
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     cluster.sync();
@@ -447,7 +463,8 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
                     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
                                  ::"r"(there), "r"(__float_as_uint(st.m)), "r"(__float_as_uint(st.s)), "r"(__float_as_uint(st.u)), "r"(0), "r"(its_bar) : "memory");
                 }
-                const bool fine = chunk_wait(bar, (turns >> 1) & 1);
+                const bool fine = chunk_wait(bar, (turns >> 1) & 1, P.polls);
+                if (!fine) wait_again(bar, (turns >> 1) & 1, &stuck);
                 const float4 v = sent[turn][lane % ranks];
                 st = shuffled(Stat{v.x, fine ? v.y : __int_as_float(0x7fffffff), v.z}, ranks);
             }
@@ -469,7 +486,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
     if (STAGED && lane == 0 && now.live)
         for (int c = 0; c < kChunks; ++c) fetch(now, c);
     while (now.row < P.R) {
-        const RowPart<T> next(P, now.row + clusters, my_warp, log_warps);
+        RowPart<T> next(P, now.row + clusters, my_warp, log_warps);
         const T* x = now.x;
         T* y = P.dlogits != nullptr ? P.dlogits + now.row * P.ldd : nullptr;
         const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0;
@@ -558,11 +575,16 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             st.u += u.x + u.y;
         };
         for (int c = 0; c * kChunk < n; ++c) {
-            if (STAGED && !chunk_wait(smem_at(&full[warp][c & (kChunks - 1)]), loads & 1)) st.s = __int_as_float(0x7fffffff);
+            const uint32_t bar = smem_at(&full[warp][c & (kChunks - 1)]);
+            if (STAGED && !chunk_wait(bar, loads & 1, P.polls)) {
+                st.s = __int_as_float(0x7fffffff);
+                wait_again(bar, loads & 1, &stuck);
+            }
             if ((c + 1) * kChunk <= n) sum_chunk(c, [] { return true; }); else sum_chunk(c, [] { return false; });
         }
         if (STAGED)                                          // empty chunks have a phase too
-            for (int c = (n + kChunk - 1) / kChunk; c < kChunks; ++c) chunk_wait(smem_at(&full[warp][c]), loads & 1);
+            for (int c = (n + kChunk - 1) / kChunk; c < kChunks; ++c)
+                if (!chunk_wait(smem_at(&full[warp][c]), loads & 1, P.polls)) wait_again(smem_at(&full[warp][c]), loads & 1, &stuck);
         ++loads;
         st = gather(st);
         if (warp == 0) {
@@ -579,6 +601,10 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         if (plain) {
             st = exact();
             g = finish_row(P, now.row, given, st, (xa - st.m) * P.inv_t, kLn2, true, rank == 0 && tid == 0);
+        }
+        if (stuck) {                                         // set ahead of a barrier of the block, if at all
+            next.live = false;
+            next.row = P.R;
         }
         const float c0 = g.c0 * g.inv_s, c1 = g.c1 * g.inv_s;
         const float2 scale = {k, k}, less = {-g.m, -g.m}, two0 = {c0, c0}, two1 = {c1, c1};
@@ -799,7 +825,8 @@ int policy_run(const T* logits, int64_t ld, const int32_t* actions, const uint8_
         if (!aligned_to(p, 4)) return RLCS_ERR_ALIGN;
     if (!aligned_to(logits, sizeof(T)) || !aligned_to(dlogits, sizeof(T))) return RLCS_ERR_ALIGN;
     PolicyParams<T> P = {logits, ld, actions, mask, advantages, old_log_probs, loss, log_probs, entropy, dlogits, ldd, R, (int)A,
-                         1.f / temperature, 1.4426950408889634f / temperature, clip, entropy_coef, scale};
+                         1.f / temperature, 1.4426950408889634f / temperature, clip, entropy_coef, scale,
+                         rlcs_hooks::g_wait_polls >= 0 ? rlcs_hooks::g_wait_polls : kPolls};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (A <= kSmallA) {
         const int64_t blocks = (R + kSmallRows - 1) / kSmallRows;

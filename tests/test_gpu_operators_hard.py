@@ -285,3 +285,30 @@ def test_attention_waits_that_run_out(api, wait_polls, rows, page, d):
             assert broken.all()
 
 
+@pytest.mark.parametrize("R,A,dtype", [(700, 5000, F32), (700, 32768, BF16), (40, 40000, F32), (300, 140001, BF16), (9, 600000, BF16), (3, 20011, F32)])
+def test_policy_waits_that_run_out(api, wait_polls, R, A, dtype):
+    """The same for the policy loss, one block and clusters of 2 to 8 a row, more rows than run at once, rows left out among them, and
+    rows that take the second way of summing."""
+    g = torch.Generator(device="cuda").manual_seed(A)
+    x = torch.randn(R, A, device="cuda", generator=g).to(dtype)
+    x[::5] = torch.finfo(dtype).min
+    a = torch.randint(0, A, (R,), device="cuda", generator=g, dtype=torch.int32)
+    adv, mask = torch.randn(R, device="cuda", generator=g), torch.rand(R, device="cuda", generator=g) < 0.8
+    call = lambda: api.compute_policy_gradient(x, a, adv, mask=mask, entropy_coef=0.1)
+    want = call()
+    for polls in (0, 0, 1, 2, 5, 20, 100):
+        wait_polls(polls)
+        got = call()
+        wait_polls(-1)
+        again = call()
+        for v, w in zip(got, want):
+            broken = torch.isnan(v)
+            assert not broken[~mask].any() and torch.equal(v[~broken], w[~broken])
+            if polls == 0 and v.dim() == 1:                   # (the second way of summing waits for nothing but its cluster)
+                ordinary = mask.clone()
+                ordinary[::5] = False
+                assert broken[ordinary].all()
+        for v, w in zip(again, want):
+            assert torch.equal(v, w)
+
+
