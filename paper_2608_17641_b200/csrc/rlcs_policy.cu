@@ -55,7 +55,8 @@ struct Stat {
 // the sums of `a` relative to a maximum m that is not below its own
 __device__ __forceinline__ Stat rebase(Stat a, float m, float exp2_t) {
     const float y = fmaxf(a.m - m, kLowest), f = exp2_of(y * exp2_t);
-    return Stat{m, a.s * f, f == 0.f ? 0.f : (a.u + a.s * y) * f};            // a NaN stays in s
+    // nothing is left of far lower logits, though their own sums may have overflowed (policy_block_kernel); a NaN stays in s
+    return Stat{m, f == 0.f && a.s == a.s ? 0.f : a.s * f, f == 0.f ? 0.f : (a.u + a.s * y) * f};
 }
 
 __device__ __forceinline__ Stat join(Stat a, Stat b, float exp2_t) {
@@ -350,7 +351,9 @@ __global__ void __launch_bounds__(256) policy_warp_kernel(const __grid_constant_
 //
 // Sums here are in units of log2: t_j = l_j log2(e) / T - M with one fused multiply-add, M the thread's running maximum so
 // scaled (any M serves: it cancels), two logits an instruction.  Logits are held above -1e30, so that t is finite where exp2(t) is
-// 0; a row whose largest logit lies as low as that goes through exact() again.
+// 0.  M is rounded and the fused product is not: from |M| = 2^27 on, t at the maximum itself is more than a few units off 0, and sums
+// may overflow.  Of a thread's logits that lie so far below the row's others (a mask of -1e9, say) nothing is left when the sums
+// are joined; a row whose largest logit itself lies so far from 0 goes through exact().
 constexpr int kBlock = 256, kWarps = kBlock / 32, kAhead = 4, kChunk = kAhead * 32, kChunks = 4, kShare = kChunks * kChunk;      // vectors of a warp
 constexpr int kPart = kWarps * kShare * 16, kMostRanks = 8;
 
@@ -510,7 +513,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         }
         const float xa = Vec<T>::load(x + a);
         const float alone = tid < singles ? Vec<T>::load(x + single) : -INFINITY;
-        // the plain way, for rows whose logits are all about the lowest there are: (l - max) first
+        // the plain way, for rows whose largest logit lies far from 0: (l - max) first
         auto exact = [&]() {
             float m = -INFINITY;
             for (int i = lane; i < n; i += 32) {
@@ -589,8 +592,8 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         st = gather(st);
         if (warp == 0) {
             const float d = xa < kLowest ? xa * P.inv_t : fmaf(xa, k, -st.m) * kLn2;
-            // a temperature that takes -1e30 out of range, or logits as low as that: again, the plain way
-            const bool again = k > 1e7f || !(st.m > -1e29f * k);
+            // a temperature that takes -1e30 out of range, or a maximum too far from 0: again, the plain way
+            const bool again = k > 1e7f || !(fabsf(st.m) < 0x1p27f);
             RowGrad g = finish_row(P, now.row, given, st, d, kLn2, true, !again && rank == 0 && tid == 0);
             g.live = !again;
             if (tid == 0) grad = g;

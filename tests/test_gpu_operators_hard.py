@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from _util import guarded_empty  # noqa: E402,F401
-from test_gpu_operators import BF16, F32, api, plain_policy, policy_inputs, rule_sample, up  # noqa: E402,F401
+from test_gpu_operators import BF16, F32, api, check_policy, plain_policy, policy_inputs, rule_sample, up  # noqa: E402,F401
 
 INF, NAN = math.inf, float("nan")
 
@@ -166,6 +166,27 @@ def test_policy_nan_in_the_acting_log_probs_is_seen(api, A, dtype):
         assert torch.isfinite(loss[r]) and torch.isfinite(grad[r]).all(), r
     assert abs(float(loss[3] + 0.1 * ent[3])) <= 1e-6
     assert loss[4] == INF
+
+
+@pytest.mark.parametrize("A,dtype", POLICY_WAYS)
+def test_policy_masks_of_any_low_value(api, A, dtype):
+    """Disallowed actions marked by a low number instead of -inf, two thirds and all but eight of a row, whole stretches of them among the
+    allowed ones, and rows that lie far from 0 altogether."""
+    R = 7
+    lowest = torch.finfo(dtype).min
+    for low in (-1e4, -1e9, -1e10, -3e20, -9e28, -1e30, -1.2e30, -1e35, lowest):
+        for share in (0.66, 1.0):
+            x, a, adv, g = policy_inputs(R, A, dtype, 5)
+            off = torch.rand(R, A, generator=g) < share
+            off[:, A // 3:A // 2] = True
+            off[torch.arange(R)[:, None], torch.randint(0, A, (R, 8), generator=g)] = False
+            off[torch.arange(R), a.long()] = False
+            x[off] = low
+            x[0] += 3e5
+            x[1, ~off[1]] += 2.0 ** 40
+            x[2, ~off[2]] -= 2.0 ** 33
+            got = check_policy(api, x, a, adv, T=0.8, c=0.05, in_place=share == 1.0)
+            assert all(torch.isfinite(v).all() for v in got)
 
 
 # ------------------------------------------------------------------------------------------ prepared, captured and concurrent calls
