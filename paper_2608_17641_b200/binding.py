@@ -99,6 +99,7 @@ class RlcsError(RuntimeError):
 
 
 _recording = threading.local()        # .calls, .held: lists while prepare() runs a wrapper, absent otherwise
+_preparing = False                    # whether it does, in any thread
 
 
 class _Recorder:
@@ -152,8 +153,9 @@ def prepare(wrapper, *args, **kwargs) -> Prepared:
         adv, ret = step()
     """
     real = lib()
-    global _lib
+    global _lib, _preparing
     _recording.calls, _recording.held = [], []
+    _preparing = True
     with _lock:
         _lib = _Recorder(real)
     try:
@@ -162,6 +164,7 @@ def prepare(wrapper, *args, **kwargs) -> Prepared:
     finally:
         with _lock:
             _lib = real
+        _preparing = False
         del _recording.calls, _recording.held
     if not calls:
         raise ValueError("prepare() takes one of the rlcs_* compute wrappers of this module")
@@ -252,9 +255,10 @@ def _alloc(shape, dtype, device):
 
 def _held(t):
     """A tensor whose pointer goes into a C call: under prepare(), which repeats the call later, it is kept for as long."""
-    held = getattr(_recording, "held", None)
-    if held is not None:
-        held.append(t)
+    if _preparing:
+        held = getattr(_recording, "held", None)
+        if held is not None:
+            held.append(t)
     return t
 
 
@@ -824,7 +828,9 @@ def _typed(t, kind: str, shape, what: str, device: int):
 def _output(t, kind: str, shape, what: str, device: int):
     """(tensor, pointer) of an output: the caller's, checked, or a new one on the current device."""
     if t is None:
-        t = _new(shape, _dtype(kind), device)
+        t = _alloc(shape, _dtype(kind), device)
+        if _preparing:
+            _held(t)
         return t, t.data_ptr()
     return t, _typed(t, kind, shape, what, device)
 
@@ -977,23 +983,25 @@ def rlcs_prefix_attention_bf16(q, k_cache, v_cache, prefix_table, prefix_lens, g
             if len(_attention_bytes) >= 4096:
                 _attention_bytes.clear()
             need = _attention_bytes[sizes] = int(lib().rlcs_prefix_attention_workspace_bytes(*sizes))
-        if workspace is not None:
+    if workspace is None:
+        workspace, room = _new((max(need, 16),), _torch().uint8, dev), max(need, 16)
+    else:
+        if callable(workspace):
             workspace = _held(workspace(need))
-        else:
-            workspace = _new((max(need, 16),), _torch().uint8, dev)
-    if not getattr(workspace, "is_cuda", False):
-        raise TypeError("workspace must be a CUDA tensor")
-    if workspace.get_device() != dev:
-        _require_current_device(workspace, "workspace")
-    if not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
+        if not getattr(workspace, "is_cuda", False):
+            raise TypeError("workspace must be a CUDA tensor")
+        if workspace.get_device() != dev:
+            _require_current_device(workspace, "workspace")
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        room = workspace.numel() * workspace.element_size()
     _check(lib().rlcs_prefix_attention_bf16(
         q.data_ptr(), sq[0] if B > 1 else H * d, k_cache.data_ptr(), v_cache.data_ptr(), pages, sk[0], sk[1], sk[2],
         _typed(prefix_table, "i32", (groups, prefix_width), "prefix_table", dev), prefix_width,
         _typed(prefix_lens, "i32", (groups,), "prefix_lens", dev), _typed(group_offsets, "i32", (groups + 1,), "group_offsets", dev),
         _typed(block_table, "i32", (B, own_width), "block_table", dev), own_width, _typed(lens, "i32", (B,), "lens", dev),
         outp, lsep, B, H, Hk, d, page, groups, mp, ml, scale,
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+        workspace.data_ptr(), room, _stream(stream)))
     return out if lse is None else (out, lse)
 
 
