@@ -790,7 +790,7 @@ int divide_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // How the keys are cut into segments: enough thread blocks for the GPU, segments of at least four tiles.
 int plan_segment(int64_t longest, int64_t units, int page, int64_t most) {
     if (longest <= 0) return kTile;
-    const int64_t want = 148 * 2 * 2;
+    const int64_t want = rlcs_device::limits().sms * 2 * 2;
     int64_t segs = units >= want ? 1 : (want + units - 1) / (units > 0 ? units : 1);
     const int64_t least = divide_up(longest, 4 * kTile);
     if (segs > least) segs = least;
