@@ -91,6 +91,7 @@ def rollout(policy, prompts, generator):
     hidden, actions, log_probs = [], [], []
     for _ in range(STEPS):
         h = policy.hidden(tokens, cache.step(policy, tokens))
+        # of the whole softmax, as the loss scores them: the clipped ratios start at 1
         a, lp, _ = api.sample_actions(policy.logits(h), torch.rand(rows, device="cuda", generator=generator), top_p=0.999)
         hidden.append(h), actions.append(a), log_probs.append(lp)
         tokens = a

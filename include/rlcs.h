@@ -420,13 +420,13 @@ int rlcs_episodic_prefix_sum_bf16(const uint16_t* x, const uint8_t* dones, uint1
  *   candidates, ordered by (logit descending, index ascending): the first top_k of them with e_j >= min_p; of those
  *   the shortest leading part that holds top_p of their weight (one stays while the weight before it < top_p * W1)
  *   action = the first index, in index order, whose kept weights sum to more than floor(uniform * W2), W2 = kept weight
- *   log_probs[r] = d_a - log(sum_j e_j),   kept_log_probs[r] = d_a - log(W2 / 2^31)
+ *   log_probs[r] = d_a - log(sum_j e_j), the whole softmax's;   kept_log_probs[r] = d_a - log(W2 / 2^31), with which a was drawn
  * The most likely candidate always stays.  temperature <= 0 (or NaN): that candidate is taken, log_probs at
  * temperature 1, kept_log_probs 0.  top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN: no such limit.  uniforms [R]
  * in [0, 1).  A logit of -inf or NaN is never drawn; a row with no other gets action -1 and log-probs -inf.  Weights
  * are whole numbers, so their sums, and with them the actions, do not depend on how a row is split over threads; an
- * action less likely than 2^-32 of the most likely one has weight 0 (log_probs, whose sum is of the e_j, counts it; a log-probability is
- * within 1e-5 of exact, 2^-22 of it more).  A logit of +inf shares all weight with the others of the kind.
+ * action less likely than 2^-32 of the most likely one has weight 0 (log_probs, whose sum is of the e_j, counts it, and is within
+ * 1e-5 and 2^-22 of its size of exact).  A logit of +inf shares all weight with the others of the kind.
  */
 int rlcs_sample_actions(const float* logits, int64_t ld, const float* uniforms, const float* temperature, const int32_t* top_k,
                         const float* top_p, const float* min_p, float temperature_all, int32_t top_k_all, float top_p_all,
@@ -476,7 +476,7 @@ int rlcs_policy_grad_bf16(const uint16_t* logits, int64_t ld, const int32_t* act
  * Lengths are cut to max_prefix_len and max_len, the host's upper bounds from which the launch is sized.  A page number
  * outside [0, pages) and a place beyond the table's width hold no keys.  Memory beyond a length is never used.  Products are
  * summed in fp32; the softmax weights enter the second product as two bfloat16 parts (16 bits of mantissa).
- * scale > 0.  workspace: at least rlcs_prefix_attention_workspace_bytes(...) bytes, 16-byte aligned, no initialisation.
+ * Scores scale q.k are meant to lie within 2^26 of 0: fp32 has no fractions beyond.  scale > 0.  workspace: at least rlcs_prefix_attention_workspace_bytes(...) bytes, 16-byte aligned, no initialisation.
  * Every wait inside the kernels is bounded; should one run out, the rows concerned come out NaN.
  */
 size_t rlcs_prefix_attention_workspace_bytes(int64_t B, int64_t H, int64_t Hk, int64_t d, int64_t page_size, int64_t groups,

@@ -197,9 +197,11 @@ def _by_dtype(logits, f32, bf16):
 
 def sample_actions(logits, uniforms, *, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
     """Actions drawn from logits [..., A] (float32 or bfloat16) with one given uniform in [0, 1) a row, and their log-probabilities:
-    (actions int32, log_probs, kept_log_probs).  log_probs is under the whole softmax at that temperature (the behaviour policy of
-    V-trace, Retrace and clipped losses), kept_log_probs under what top_k, min_p and top_p leave.  Parameters are numbers or
-    tensors of one value a row; temperature 0 takes the most likely action; a row that allows none (all -inf) gets action -1."""
+    (actions int32, log_probs, kept_log_probs).  kept_log_probs is the log-probability with which the action was drawn, under what
+    top_k, min_p and top_p leave: the behaviour policy that importance ratios (V-trace, Retrace) divide by.  log_probs is under
+    the whole softmax at that temperature, as compute_log_probs and compute_policy_gradient score actions: a clipped loss that compares
+    the learner's policy with the acting one wants it, so that its ratios start at 1.  Without a cut both say the same.  Parameters
+    are numbers or tensors of one value a row; temperature 0 takes the most likely action; a row that allows none (all -inf) gets action -1."""
     fn = _by_dtype(logits, _B.rlcs_sample_actions, _B.rlcs_sample_actions_bf16)
     rows, lead = _flat_rows(logits)
     flat = lambda v: v.reshape(-1) if lead is not None and hasattr(v, "reshape") else v

@@ -4,9 +4,10 @@
 // so the drawn action does not depend on how a row is split over threads, and every comparison of the filters is
 // made between the same numbers on every run.
 //
-// The floor is one read of the logits (256 x 131072 bfloat16: 10 us); what bounds these kernels is instructions, about 24 for an exact
-// weight, of which expf is 9.  Measured: 1 x 131072 bfloat16 with top-k 13 us, 256 x 131072 without filters 56, top-k 50 48,
-// top-p 0.9 178; 262144 x 18 fp32 without filters 14.
+// The floor is one read of the logits (256 x 131072 bfloat16: 10 us).  An exact weight is about 24 instructions, of which expf is 9: 22 us
+// of the 63 without filters, were they issued without a pause; with a cut the histograms are waited for (1.8 of 4 instructions a cycle).
+// Measured: 1 x 131072 bfloat16 with top-k and top-p 14 us, 256 x 131072 without filters 63, top-k 50 54, top-p 0.9 182, mixed
+// settings 117; 262144 x 18 fp32 without filters 14 (73 instructions a logit with the walks in shared memory).
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(256) sample_warp_kernel(const __grid_constant_
 //   top-k up to 192: the k-th largest of the threads' own maxima bounds the k-th largest logit from below, so that few
 //     candidates pass it (about 200 of 131072 for k = 192 and 2048 threads); one block sorts them and does the rest.
 //   otherwise a histogram of weights and counts over 24 steps of (l - max) / T, one column a lane and so without atomics (48 KB: four
-//     blocks a multiprocessor, 119 us for 256 x 131072 with mixed settings; 32 steps and three blocks: 133),
+//     blocks a multiprocessor, 117 us for 256 x 131072 with mixed settings; 32 steps and three blocks: 133),
 //     finds the step that holds a cut; histograms over the keys of that step alone narrow it to one key.
 constexpr int kT = 256, kW = kT / 32, kCoarse = 24, kFine = 1024, kList = 2048, kListLimit = 192, kMaxCluster = 8;
 constexpr u64 kCountOne = 1ull << 48;                        // a column's entry: count above, weight below bit 48
@@ -1024,9 +1025,8 @@ int sample_run(const SampleParams<T>& P, int64_t A, void* stream) {
         else if (A <= 1024) sample_warp_kernel<T, 32><<<(unsigned)warps, 256, 0, s>>>(P);
         else sample_warp_kernel<T, 64><<<(unsigned)warps, 256, 0, s>>>(P);
     } else {
-        // blocks a row: until the GPU has four a multiprocessor (256 x 131072 with mixed settings, at three blocks a multiprocessor: 4 blocks a row 133 us,
-        // 2 175, 8 155), or a part would
-        // fall below 4096 actions
+        // blocks a row: until the GPU has four a multiprocessor (256 x 131072 with mixed settings: 4 blocks a row 117 us, 2 173, 8 123; without
+        // filters 63, 66, 71), or a part would fall below 4096 actions
         int ranks = 1;
         while (ranks < kMaxCluster && P.R * ranks < 4 * rlcs_device::limits().sms && A / (2 * ranks) >= 4096) ranks *= 2;
         if (P.R * ranks > kMostBlocks) return RLCS_ERR_SIZE;
