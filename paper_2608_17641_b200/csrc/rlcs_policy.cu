@@ -373,8 +373,8 @@ __device__ __forceinline__ bool chunk_wait(uint32_t bar, int parity, int most) {
 }
 
 // What was given up is waited for once more, longer than another block of the cluster takes to give up: its place and its barrier are used
-// again, and no block ends while something is on its way to it.  `stuck`: not even that helped; no more copies, and the block leaves its
-// other rows as they are.
+// again, and no block ends while something is on its way to it.  `stuck`: not even that helped; no more copies and no more sums, and the
+// block leaves its other rows as they are.
 __device__ __forceinline__ void wait_again(uint32_t bar, int parity, volatile int* stuck) {
     if (*stuck || !chunk_wait(bar, parity, 8 * kPolls)) *stuck = 1;
 }
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
     __shared__ Stat part[kWarps], joined;
     __shared__ __align__(16) float4 sent[2][kMostRanks];
     __shared__ RowGrad grad;
-    __shared__ int stuck;
+    __shared__ int stuck, leave;                             // leave: stuck as the whole block saw it
     __shared__ __align__(8) uint64_t full[kWarps][kChunks], got[2];
     namespace cg = cooperative_groups;
     const cg::cluster_group cluster = cg::this_cluster();
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
     const float k = P.exp2_t;
     uint4* const held = held_all + warp * kShare;
     if (tid < kWarps * kChunks) asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"(smem_at(&full[0][0] + tid)));
-    if (tid == 0) stuck = 0;
+    if (tid == 0) stuck = leave = 0;
     if (tid < 2) asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"(smem_at(&got[tid])));
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     cluster.sync();
@@ -458,21 +458,22 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             if (ranks > 1) {
                 const int turn = turns & 1;
                 const uint32_t bar = smem_at(&got[turn]), place = smem_at(&sent[turn][rank]);
-                if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(ranks * 16) : "memory");
-                if (lane < ranks) {
+                const bool apart = *(volatile int*)&stuck != 0;
+                if (lane == 0 && !apart) asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(ranks * 16) : "memory");
+                if (lane < ranks && !apart) {
                     uint32_t there, its_bar;
                     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(place), "r"(lane));
                     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(its_bar) : "r"(bar), "r"(lane));
                     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
                                  ::"r"(there), "r"(__float_as_uint(st.m)), "r"(__float_as_uint(st.s)), "r"(__float_as_uint(st.u)), "r"(0), "r"(its_bar) : "memory");
                 }
-                const bool fine = chunk_wait(bar, (turns >> 1) & 1, P.polls);
+                const bool fine = !apart && chunk_wait(bar, (turns >> 1) & 1, P.polls);
                 if (!fine) wait_again(bar, (turns >> 1) & 1, &stuck);
                 const float4 v = sent[turn][lane % ranks];
                 st = shuffled(Stat{v.x, fine ? v.y : __int_as_float(0x7fffffff), v.z}, ranks);
+                if (!apart) ++turns;
             }
         }
-        ++turns;
         return st;
     };
     auto gather_all = [&](Stat st) {
@@ -596,7 +597,10 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             const bool again = k > 1e7f || !(fabsf(st.m) < 0x1p27f);
             RowGrad g = finish_row(P, now.row, given, st, d, kLn2, true, !again && rank == 0 && tid == 0);
             g.live = !again;
-            if (tid == 0) grad = g;
+            if (tid == 0) {
+                grad = g;
+                leave = *(volatile int*)&stuck;
+            }
         }
         __syncthreads();
         RowGrad g = grad;
@@ -605,7 +609,7 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
             st = exact();
             g = finish_row(P, now.row, given, st, (xa - st.m) * P.inv_t, kLn2, true, rank == 0 && tid == 0);
         }
-        if (stuck) {                                         // set ahead of a barrier of the block, if at all
+        if (leave) {                                         // for all of the block alike
             next.live = false;
             next.row = P.R;
         }
@@ -663,6 +667,11 @@ __global__ void __launch_bounds__(kBlock, 3) policy_block_kernel(const __grid_co
         }
         if (y != nullptr && tid < singles) Vec<T>::store(y + single, slow(alone, single));
         now = next;
+    }
+    if (leave && ranks > 1 && warp == 0) {                   // what the others send before they find this block gone
+        const uint32_t bar = smem_at(&got[turns & 1]);
+        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"((ranks - 1) * 16) : "memory");
+        chunk_wait(bar, (turns >> 1) & 1, 8 * kPolls);
     }
 }
 

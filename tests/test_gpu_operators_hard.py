@@ -7,7 +7,6 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from _util import guarded_empty  # noqa: E402,F401
 from test_gpu_operators import BF16, F32, api, check_policy, plain_policy, policy_inputs, rule_sample, up  # noqa: E402,F401
 
 INF, NAN = math.inf, float("nan")
