@@ -504,6 +504,114 @@ int rlcs_block_tables(const int32_t* cached, const int32_t* added, const int32_t
                       int64_t width, int64_t free_count, int64_t num_slots, int64_t page_size, void* cuda_stream);
 
 /*
+ * Attention of chunks of new tokens (whole prompts, parts of them, drafted tokens, single tokens) over a paged cache that holds the
+ * new tokens' keys and values already.  Tokens offsets[b] to offsets[b+1]-1 of the step (ascending, within [0, T]) are the last ones
+ * of trajectory b, whose first lens[b] tokens lie in the pages block_table[b, :] ([B, width]).  With n = offsets[b+1] - offsets[b] its
+ * token i has place p = lens[b] - n + i and sees the keys 0 to p, itself the last:
+ *   out = sum_{j <= p} exp(scale q.k_j - lse) v_j,   lse = log sum_{j <= p} exp(scale q.k_j);   without keys (p < 0): out 0, lse -inf
+ * q [T, H, d], token t at q + t*q_stride (heads contiguous); out [T, H, d] contiguous; lse [T, H] or NULL.  Tokens outside every
+ * trajectory, and those of a trajectory beyond its first max_new, are left as they were in out and lse.  Caches, strides, head
+ * groups, d, page sizes, missing pages and alignment as in rlcs_prefix_attention_bf16; T at most 2^24.  Lengths are cut to max_len (keys beyond it are not
+ * seen); max_new and max_len are the host's upper bounds from which the launch is sized.  Memory beyond a length is never used; what
+ * lies within it is multiplied, by 0 where a token does not see it, and has to be finite.  Products are summed in fp32; the softmax
+ * weights enter the second product as two bfloat16 parts, or, in chunks of more than 16 rows (tokens times heads on a key head), as one.
+ * scale > 0.  workspace: at least rlcs_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned, no initialisation (may be NULL
+ * where that is 0).  Every wait inside the kernels is bounded; should one run out, the rows concerned come out NaN.
+ */
+size_t rlcs_chunk_attention_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hk, int64_t d, int64_t page_size, int64_t max_new,
+                                            int64_t max_len);
+int rlcs_chunk_attention_bf16(const uint16_t* q, int64_t q_stride, const uint16_t* k_cache, const uint16_t* v_cache, int64_t pages,
+                              int64_t page_stride, int64_t token_stride, int64_t head_stride, const int32_t* block_table, int64_t width,
+                              const int32_t* offsets, const int32_t* lens, uint16_t* out, float* lse, int64_t T, int64_t B, int64_t H,
+                              int64_t Hk, int64_t d, int64_t page_size, int64_t max_new, int64_t max_len, float scale, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Drafted tokens kept or turned down against the target's probabilities, and the token that follows the kept ones.  Rows
+ * offsets[b] to offsets[b+1]-1 (ascending, within [0, T]) of tokens [T] are trajectory b's: its last token, then its drafts.  Row t of
+ * logits [T, A] (row t at logits + t*ld, any alignment of a row; A <= 2^22) is the target's prediction after tokens[t], row t of
+ * draft_logits (likewise; ldd) the one from which the draft policy drew tokens[t+1].  A trajectory's last draft_logits row is
+ * not read; draft_logits NULL: the drafts were not drawn but given, each with probability 1.  Per trajectory, with T its temperature
+ * (temperature [B], or temperature_all where that is NULL), for target and drafts alike:
+ *   w_j = floor(2^31 exp((l_j - max l) / T) + 1/2),  W = sum w;   v_j, V the same of draft_logits
+ *   the draft x = tokens[t+1] stays while  uniforms[t] * (v_x * W) < w_x * V  (in 64-bit floats, from left to right)
+ *   at the first row r whose draft does not stay, or at the last row, a token is drawn: the first index, in index order, whose
+ *   weights sum to more than floor(draw_uniforms[b] * their sum), of the weights
+ *     max(0, floor(w_j 2^40 / W) - floor(v_j 2^40 / V))  at a turned-down draft (w_j where nothing is left of them; without
+ *     draft_logits w_j, but 0 for the draft itself),  and  w_j  at the last row
+ *   out_tokens[t]: the draft for rows before r, the drawn token at r, -1 behind;   accepted[b] = r - offsets[b]
+ *   log_probs[t]: log-probability of out_tokens[t] under the target's whole softmax at T (within 1e-5 and 2^-22 of its size), -inf where that is -1
+ * T <= 0 (or NaN): drafts stay while they are the target's most likely token (of equals the lowest index), which is also what is drawn;
+ * log_probs at temperature 1.  Logits of -inf or NaN have no weight; a target row with no other stops the trajectory there with token -1.
+ * A draft outside [0, A) does not stay.  uniforms [T] and draw_uniforms [B] in [0, 1).  Rows outside every trajectory are left as they were;
+ * an empty trajectory has accepted 0.  workspace: at least rlcs_verify_drafts_workspace_bytes(T, B) bytes, 16-byte aligned, no initialisation.
+ */
+size_t rlcs_verify_drafts_workspace_bytes(int64_t T, int64_t B);
+int rlcs_verify_drafts(const float* logits, int64_t ld, const float* draft_logits, int64_t ldd, const int32_t* tokens, const int32_t* offsets,
+                       const float* uniforms, const float* draw_uniforms, const float* temperature, float temperature_all, int32_t* out_tokens,
+                       float* log_probs, int32_t* accepted, int64_t T, int64_t B, int64_t A, void* workspace, size_t workspace_bytes,
+                       void* cuda_stream);
+int rlcs_verify_drafts_bf16(const uint16_t* logits, int64_t ld, const uint16_t* draft_logits, int64_t ldd, const int32_t* tokens,
+                            const int32_t* offsets, const float* uniforms, const float* draw_uniforms, const float* temperature,
+                            float temperature_all, int32_t* out_tokens, float* log_probs, int32_t* accepted, int64_t T, int64_t B, int64_t A,
+                            void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Loss towards the strongest logits of a teacher, and its gradient, from a student's logits [R, A] (row r at logits + r*ld, any
+ * alignment of a row; A <= 2^22) in one launch.  Row r's teacher entries: teacher_logits[r, i] of teacher_ids[r, i], i < K ([R, K] each, K <= 1024);
+ * an entry whose id lies outside [0, A) (-1, say) is absent.  x = logits / temperature, lq = log softmax(x),
+ * p = softmax(teacher_logits / temperature) over the entries that are there:
+ *   loss[r] = scale * sum_i p_i (log p_i - lq_{id_i})      (entries with p_i = 0 add nothing)
+ *   dlogits[r,j] = scale / temperature * (exp(lq_j) - sum_{i: id_i = j} p_i)      (row r at dlogits + r*ldd; rounded once)
+ * Log-probabilities serve as teacher logits too.  A row whose mask is 0 (mask may be NULL: all rows live), without entries above -inf, or whose
+ * logits are all -inf is left out: loss and gradient 0.  In other rows a logit of -inf has probability 0 and gradient 0 (loss +inf where the
+ * teacher names it); a NaN or +inf among the row's logits or teacher entries makes loss and gradient NaN.  Sums are fp32 relative to the maximum.
+ * loss or dlogits may be NULL; dlogits may be the logits themselves (same pointer, ldd = ld).  temperature > 0.
+ */
+int rlcs_distill_grad(const float* logits, int64_t ld, const int32_t* teacher_ids, const float* teacher_logits, const uint8_t* mask, float* loss,
+                      float* dlogits, int64_t ldd, int64_t R, int64_t A, int64_t K, float temperature, float scale, void* cuda_stream);
+int rlcs_distill_grad_bf16(const uint16_t* logits, int64_t ld, const int32_t* teacher_ids, const float* teacher_logits, const uint8_t* mask,
+                           float* loss, uint16_t* dlogits, int64_t ldd, int64_t R, int64_t A, int64_t K, float temperature, float scale,
+                           void* cuda_stream);
+
+/*
+ * Trajectories continued from others: row i of new_table [N, width] continues row s = sources[i] of block_table [B, width], which holds
+ * lens[s] tokens in its first ceil(lens[s] / page_size) pages (at most `width`).  Whole pages are shared.  A part-filled last page
+ * stays with the first row i that continues s; each other one gets, in row order, the next number of free_pages [free_count] in
+ * its place, and copy_from[i] -> copy_to[i] says which page it has to be copied from (rlcs_copy_pages_bf16, once a layer).  Both
+ * are -1 for rows that copy nothing; where the list has run out (or holds a negative number) they and the table's entry are -1.
+ * Entries behind the pages, and rows whose source lies outside [0, B), are -1.  pages_used [1]: numbers asked of the list.  A part-filled
+ * page beyond the table's width or of a negative number is not copied.  new_table must not be block_table.
+ * workspace: rlcs_fork_block_tables_workspace_bytes(B, N) bytes (0 up to 4096 rows each), 16-byte aligned, no initialisation.
+ */
+size_t rlcs_fork_block_tables_workspace_bytes(int64_t B, int64_t N);
+int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, const int32_t* sources, const int32_t* free_pages,
+                           int32_t* new_table, int32_t* copy_from, int32_t* copy_to, int32_t* pages_used, int64_t B, int64_t N,
+                           int64_t width, int64_t free_count, int64_t page_size, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Pages copied within a cache: copy_from[i] -> copy_to[i] for i < N, in k_cache and (where it is not NULL) v_cache, both laid out as for
+ * the attention calls.  A pair with a number outside [0, pages), or of a page onto itself, is passed over.  No page may be the
+ * destination of two pairs, or of one and the source of another.
+ */
+int rlcs_copy_pages_bf16(uint16_t* k_cache, uint16_t* v_cache, int64_t pages, int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                         const int32_t* copy_from, const int32_t* copy_to, int64_t N, int64_t page_size, int64_t Hk, int64_t d,
+                         void* cuda_stream);
+
+/*
+ * The pages that are free: the numbers in [0, num_pages) that no table names, ascending, in free_pages [num_pages], -1 behind them, and
+ * how many they are in free_count [1].  A table names the first ceil(len / page_size) entries of each row, at most its width:
+ * block_table [B, width] with lens [B], and prefix_table [groups, prefix_width] with prefix_lens [groups].  Pages named several
+ * times are simply not free; other numbers in the tables count for nothing.  The list serves rlcs_block_tables and
+ * rlcs_fork_block_tables as it is: its -1 are no pages to them.  num_pages up to 2^31 - 64.
+ * workspace: rlcs_free_pages_workspace_bytes(num_pages) bytes, 16-byte aligned, no initialisation.
+ */
+size_t rlcs_free_pages_workspace_bytes(int64_t num_pages);
+int rlcs_free_pages(const int32_t* block_table, const int32_t* lens, const int32_t* prefix_table, const int32_t* prefix_lens,
+                    int32_t* free_pages, int32_t* free_count, int64_t B, int64_t width, int64_t groups, int64_t prefix_width,
+                    int64_t num_pages, int64_t page_size, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Test hook: the bare scan of Eq. 1 / Eq. 2 on caller-supplied coefficients, every row with
  * boundary carry 0 (the paper's generic kernel of Section 4.1).
  *   forward == 0:  out_t = alpha_t + (t < T-1 ? beta_t * out_{t+1} : 0)

@@ -255,3 +255,63 @@ def build_block_tables(cached, added, free_pages, block_table, *, page_size, num
     slots, positions, offsets, page_offsets = _B.rlcs_block_tables(cached, added, free_pages, block_table, page_size=page_size,
                                                                    num_slots=num_slots, stream=stream)
     return slots, positions, offsets, page_offsets[-1:]
+
+
+# ------------------------------------------------------------------ speculative rollouts and distillation
+def chunk_attention(q, k_cache, v_cache, block_table, offsets, lens, *, scale=None, max_new=None, max_len=None, workspace=None, stream=None):
+    """Attention of chunks of new tokens over a paged cache that holds them already: whole prompts, parts of prompts, drafts, single
+    tokens, mixed as they come.  q [T, H, d] bfloat16; tokens offsets[b] to offsets[b+1]-1 (int32 [B + 1], as build_block_tables gives
+    them) are the last of trajectory b's lens[b] tokens, and each sees the keys up to its own: (out [T, H, d], lse [T, H]).  Caches
+    [pages, page, Hk, d]; scale defaults to d ** -0.5; max_new and max_len bound the chunks and the lengths (by default T, and what the table can hold):
+    closer bounds give better launches and a smaller workspace.  Tokens outside every trajectory (a padded step) are not written.
+    workspace: as for shared_prefix_attention, of rlcs_chunk_attention_workspace_bytes bytes; by default one of the call's own."""
+    scale = q.shape[-1] ** -0.5 if scale is None else scale
+    return _B.rlcs_chunk_attention_bf16(q, k_cache, v_cache, block_table, offsets, lens, scale=scale, max_new=max_new, max_len=max_len,
+                                        workspace=workspace, stream=stream)
+
+
+def verify_drafts(logits, tokens, offsets, uniforms, draw_uniforms, *, draft_logits=None, temperature=None, stream=None):
+    """Which drafted tokens stay, and the token that follows them: (out_tokens int32 [T], log_probs [T], accepted int32 [B]).  tokens [T]
+    holds, trajectory after trajectory (offsets [B + 1]), the last token and the drafts; logits [T, A] (float32 or bfloat16) the target's
+    prediction after each, draft_logits [T, A] the one each following draft was drawn from at the same temperature (None: drafts were
+    given, not drawn).  One uniform in [0, 1) a row decides on its draft, one a trajectory draws the token that follows.  out_tokens[t] is
+    the token after tokens[t]: kept drafts, the drawn token, then -1; log_probs are the target's, so they serve as old_log_probs
+    of a policy loss.  temperature is a number or a tensor of one a trajectory; 0 keeps and takes the most likely token.  Rows
+    outside every trajectory are not written."""
+    fn = _by_dtype(logits, _B.rlcs_verify_drafts, _B.rlcs_verify_drafts_bf16)
+    return fn(logits, tokens, offsets, uniforms, draw_uniforms, draft_logits=draft_logits, temperature=temperature, stream=stream)
+
+
+def compute_distillation(logits, teacher_ids, teacher_logits, *, mask=None, temperature=1.0, scale=1.0, in_place=False, stream=None):
+    """Loss of a student's logits [..., A] towards the strongest logits of a teacher, [..., K] with their indices teacher_ids (int32; -1 for
+    entries that are not there), and its gradient: (loss [...], dlogits [..., A]).  The loss is the divergence from the teacher's
+    probabilities over its K entries to the student's over all A, both at `temperature`, times scale (temperature ** 2 / rows gives
+    the usual mean).  loss is per row: its sum is what dlogits differentiates.  Rows with mask 0 count as absent.  in_place=True
+    overwrites the logits with the gradient."""
+    rows, lead = _flat_rows(logits)
+    flat = lambda v: v.reshape(-1) if lead is not None and v is not None else v
+    pairs = lambda v: v if lead is None else v.reshape(-1, v.shape[-1])
+    fn = _by_dtype(logits, _B.rlcs_distill_grad, _B.rlcs_distill_grad_bf16)
+    loss, grad = fn(rows, pairs(teacher_ids), pairs(teacher_logits), mask=flat(_mask(mask)), temperature=temperature, scale=scale,
+                    dlogits=rows if in_place else None, stream=stream)
+    return (loss, grad) if lead is None else (loss.view(lead), grad.view(logits.shape))
+
+
+def fork_block_tables(block_table, lens, sources, free_pages, *, page_size, stream=None):
+    """Trajectories continued from others (branches, resampling): row i of the new table continues row sources[i].  Whole pages are
+    shared; a part-filled last page is copied for every row but the first that continues it, to pages taken from free_pages:
+    (new_table, copy_from, copy_to, pages_used).  copy_pages makes the copies, layer by layer; pages_used (one element) above
+    the number of free pages says that the list ran out."""
+    return _B.rlcs_fork_block_tables(block_table, lens, sources, free_pages, page_size=page_size, stream=stream)
+
+
+def copy_pages(k_cache, v_cache, copy_from, copy_to, *, stream=None):
+    """Copies pages copy_from[i] -> copy_to[i] of both caches [pages, page, Hk, d] in place; pairs with a negative number are passed over."""
+    return _B.rlcs_copy_pages_bf16(k_cache, v_cache, copy_from, copy_to, stream=stream)
+
+
+def list_free_pages(block_table, lens, *, num_pages, page_size, prefix_table=None, prefix_lens=None, stream=None):
+    """The pages that no trajectory (and no shared prompt) names any more, ascending: (free_pages int32 [num_pages], -1 behind the last,
+    count [1]).  Freeing a trajectory is setting its length to 0, turning tokens down is lowering it; the list serves
+    build_block_tables and fork_block_tables as it is, without a word from the host."""
+    return _B.rlcs_free_pages(block_table, lens, prefix_table, prefix_lens, num_pages=num_pages, page_size=page_size, stream=stream)

@@ -70,6 +70,18 @@ SIGNATURES = {
     "rlcs_prefix_attention_bf16": ([_vp, _i64, _vp, _vp] + [_i64] * 4 + [_vp, _i64, _vp, _vp, _vp, _i64] + [_vp] * 3 + [_i64] * 8
                                    + [_f] + _TAIL, _int),
     "rlcs_block_tables": ([_vp] * 8 + [_i64] * 5 + [_vp], _int),
+    "rlcs_chunk_attention_workspace_bytes": ([_i64] * 8, _sz),
+    "rlcs_chunk_attention_bf16": ([_vp, _i64, _vp, _vp] + [_i64] * 4 + [_vp, _i64] + [_vp] * 4 + [_i64] * 8 + [_f] + _TAIL, _int),
+    "rlcs_verify_drafts_workspace_bytes": ([_i64] * 2, _sz),
+    "rlcs_verify_drafts": ([_vp, _i64, _vp, _i64] + [_vp] * 5 + [_f] + [_vp] * 3 + [_i64] * 3 + _TAIL, _int),
+    "rlcs_verify_drafts_bf16": ([_vp, _i64, _vp, _i64] + [_vp] * 5 + [_f] + [_vp] * 3 + [_i64] * 3 + _TAIL, _int),
+    "rlcs_distill_grad": ([_vp, _i64] + [_vp] * 5 + [_i64] * 4 + [_f] * 2 + [_vp], _int),
+    "rlcs_distill_grad_bf16": ([_vp, _i64] + [_vp] * 5 + [_i64] * 4 + [_f] * 2 + [_vp], _int),
+    "rlcs_fork_block_tables_workspace_bytes": ([_i64] * 2, _sz),
+    "rlcs_fork_block_tables": ([_vp] * 8 + [_i64] * 5 + _TAIL, _int),
+    "rlcs_copy_pages_bf16": ([_vp] * 2 + [_i64] * 4 + [_vp] * 2 + [_i64] * 4 + [_vp], _int),
+    "rlcs_free_pages_workspace_bytes": ([_i64], _sz),
+    "rlcs_free_pages": ([_vp] * 6 + [_i64] * 6 + _TAIL, _int),
     "rlcs_affine_scan": ([_vp] * 3 + [_i64, _i64, _int] + _TAIL, _int),
     "rlcs_debug_set_tile_variant": ([_int], _int),
     "rlcs_debug_tile_elems": ([_int], _int),
@@ -908,14 +920,7 @@ def _policy_grad(name, kind, logits, actions, advantages, old_log_probs, mask, t
         if dlogits is not None:
             dptr, ldd = _rows(dlogits, kind, "dlogits", dev, (R, A))
         elif want_grad:
-            # rows as far apart, and as far from a 16-byte boundary, as the logits': both are then walked in whole vectors
-            # (rows of up to 64 actions leave as one block of memory, which wants them close together)
-            ldd, lead = (ld, ptr % 16 // logits.element_size()) if A > 64 and ld - A <= A // 8 + 16 else (A, 0)
-            if ldd == A and lead == 0:
-                dlogits = _new((R, A), logits.dtype, dev)
-            else:
-                dlogits = _new((R * ldd + lead,), logits.dtype, dev)
-                dlogits = dlogits.as_strided((R, A), (ldd, 1), dlogits.storage_offset() + lead)
+            dlogits, ldd = _gradient_like(logits, ptr, ld, dev)
             dptr = dlogits.data_ptr()
     _check(getattr(lib(), name)(ptr, ld, _typed(actions, "i32", n, "actions", dev), _ptr(mask, "u8", n),
                                 _typed(advantages, "f32", n, "advantages", dev), _typed(old_log_probs, "f32", n, "old_log_probs", dev),
@@ -1023,3 +1028,217 @@ def rlcs_block_tables(cached, added, free_pages, block_table, *, page_size, num_
         _typed(free_pages, "i32", None, "free_pages", dev), _typed(block_table, "i32", None, "block_table", dev),
         sp, pp, op, gp, B, width, free_pages.shape[0], num_slots, page_size, _stream(stream)))
     return slots, positions, offsets, page_offsets
+
+
+# ------------------------------------------------------------------ speculative rollouts and distillation
+_scratch_bytes: dict = {}              # workspace bytes by entry point and sizes
+
+
+def _scratch(query: str, sizes, workspace, device: int):
+    """(pointer, bytes, tensor) of a call's workspace: the caller's, checked, or one of the call's own from torch's allocator."""
+    if workspace is None:
+        need = _scratch_bytes.get((query, sizes))
+        if need is None:
+            if len(_scratch_bytes) >= 4096:
+                _scratch_bytes.clear()
+            need = _scratch_bytes[query, sizes] = int(getattr(lib(), query)(*sizes))
+        if need == 0:
+            return None, 0, None
+        workspace = _new((need,), _torch().uint8, device)
+        return workspace.data_ptr(), need, workspace
+    if not getattr(workspace, "is_cuda", False):
+        raise TypeError("workspace must be a CUDA tensor")
+    if workspace.get_device() != device:
+        _require_current_device(workspace, "workspace")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _caches(k_cache, v_cache, device: int):
+    """Strides of a pair of caches [pages, page, Hk, d] whose rows of d are contiguous."""
+    if k_cache.dim() != 4 or (v_cache is not None and v_cache.shape != k_cache.shape):
+        raise ValueError("expected caches [pages, page, Hk, d] of one shape")
+    for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if t is not None and not (t.dtype == _dtype("bf16") and t.is_cuda and t.get_device() == device):
+            _refuse(t, "bf16", None, what)
+    s = k_cache.stride()
+    if s[3] != 1:
+        raise ValueError("d of the caches must be contiguous")
+    if v_cache is not None and v_cache.stride() != s:
+        raise ValueError("k_cache and v_cache must have the same strides")
+    return s
+
+
+@_on_stream
+def rlcs_chunk_attention_bf16(q, k_cache, v_cache, block_table, offsets, lens, *, scale, max_new=None, max_len=None, want_lse=True,
+                              out=None, lse=None, workspace=None, stream=None):
+    """Queries of chunks of new tokens, q [T, H, d] (tokens may be strided), over their trajectories' paged keys up to their own: tokens
+    offsets[b] to offsets[b+1]-1 are the last of the lens[b] tokens in the pages block_table[b].  Caches as for
+    rlcs_prefix_attention_bf16.  Returns (out, lse), or out without lse; tokens outside every trajectory are not written."""
+    if q.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("expected q [T, H, d] and block_table [B, width]")
+    dev = _device_for(q)
+    if not (q.dtype == _dtype("bf16") and q.get_device() == dev):
+        _refuse(q, "bf16", None, "q")
+    sk = _caches(k_cache, v_cache, dev)
+    T, H, d = q.shape
+    pages, page, Hk, dk = k_cache.shape
+    sq = q.stride()
+    if dk != d or (d > 1 and sq[2] != 1) or (H > 1 and sq[1] != d):
+        raise ValueError("q and the caches must agree in d, with heads of q contiguous")
+    B, width = block_table.shape
+    mn = T if max_new is None else min(int(max_new), T)
+    ml = width * page if max_len is None else min(int(max_len), width * page)
+    out, outp = _output(out, "bf16", (T, H, d), "out", dev)
+    lsep = None
+    if lse is not None or want_lse:
+        lse, lsep = _output(lse, "f32", (T, H), "lse", dev)
+    wp, room, workspace = _scratch("rlcs_chunk_attention_workspace_bytes", (T, B, H, Hk, d, page, mn, ml), workspace, dev)
+    _check(lib().rlcs_chunk_attention_bf16(
+        q.data_ptr(), sq[0] if T > 1 else H * d, k_cache.data_ptr(), v_cache.data_ptr(), pages, sk[0], sk[1], sk[2],
+        _typed(block_table, "i32", (B, width), "block_table", dev), width, _typed(offsets, "i32", (B + 1,), "offsets", dev),
+        _typed(lens, "i32", (B,), "lens", dev), outp, lsep, T, B, H, Hk, d, page, mn, ml, scale, wp, room, _stream(stream)))
+    return out if lse is None else (out, lse)
+
+
+def _verify_drafts(name, kind, logits, tokens, offsets, uniforms, draw_uniforms, draft_logits, temperature, out_tokens, log_probs, accepted,
+                   workspace, stream):
+    dev = _device_for(logits)
+    ptr, ld = _rows(logits, kind, "logits", dev)
+    T, A = logits.shape
+    dptr, ldd = (None, 0) if draft_logits is None else _rows(draft_logits, kind, "draft_logits", dev, (T, A))
+    if offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("expected offsets [B + 1]")
+    B = offsets.shape[0] - 1
+    t, t_all = _per_row(temperature, "f32", (B,), 1.0, "temperature", dev)
+    out, outp = _output(out_tokens, "i32", (T,), "out_tokens", dev)
+    lp, lpp = _output(log_probs, "f32", (T,), "log_probs", dev)
+    acc, accp = _output(accepted, "i32", (B,), "accepted", dev)
+    wp, room, workspace = _scratch("rlcs_verify_drafts_workspace_bytes", (T, B), workspace, dev)
+    _check(getattr(lib(), name)(ptr, ld, dptr, ldd, _typed(tokens, "i32", (T,), "tokens", dev), _typed(offsets, "i32", (B + 1,), "offsets", dev),
+                                _typed(uniforms, "f32", (T,), "uniforms", dev), _typed(draw_uniforms, "f32", (B,), "draw_uniforms", dev),
+                                t, t_all, outp, lpp, accp, T, B, A, wp, room, _stream(stream)))
+    return out, lp, acc
+
+
+@_on_stream
+def rlcs_verify_drafts(logits, tokens, offsets, uniforms, draw_uniforms, *, draft_logits=None, temperature=None, out_tokens=None,
+                       log_probs=None, accepted=None, workspace=None, stream=None):
+    """Drafts tokens[t+1] against the target's float32 logits [T, A] (rows may be strided), trajectory b in rows offsets[b] to
+    offsets[b+1]-1; temperature is a number or one a trajectory.  Returns (out_tokens int32 [T], log_probs [T], accepted int32 [B])."""
+    return _verify_drafts("rlcs_verify_drafts", "f32", logits, tokens, offsets, uniforms, draw_uniforms, draft_logits, temperature, out_tokens,
+                          log_probs, accepted, workspace, stream)
+
+
+@_on_stream
+def rlcs_verify_drafts_bf16(logits, tokens, offsets, uniforms, draw_uniforms, *, draft_logits=None, temperature=None, out_tokens=None,
+                            log_probs=None, accepted=None, workspace=None, stream=None):
+    """rlcs_verify_drafts on bfloat16 logits."""
+    return _verify_drafts("rlcs_verify_drafts_bf16", "bf16", logits, tokens, offsets, uniforms, draw_uniforms, draft_logits, temperature,
+                          out_tokens, log_probs, accepted, workspace, stream)
+
+
+def _gradient_like(logits, ptr: int, ld: int, device: int):
+    """A gradient for logits [R, A]: rows as far apart, and as far from a 16-byte boundary, as theirs where that costs little memory, so
+    that both are walked in whole vectors (rows of up to 64 actions leave as one block of memory, which wants them close together)."""
+    R, A = logits.shape
+    ldd, lead = (ld, ptr % 16 // logits.element_size()) if A > 64 and ld - A <= A // 8 + 16 else (A, 0)
+    if ldd == A and lead == 0:
+        return _new((R, A), logits.dtype, device), ldd
+    flat = _new((R * ldd + lead,), logits.dtype, device)
+    return flat.as_strided((R, A), (ldd, 1), flat.storage_offset() + lead), ldd
+
+
+def _distill_grad(name, kind, logits, teacher_ids, teacher_logits, mask, temperature, scale, want_grad, loss, dlogits, stream):
+    dev = _device_for(logits)
+    ptr, ld = _rows(logits, kind, "logits", dev)
+    R, A = logits.shape
+    if teacher_ids.dim() != 2:
+        raise ValueError("expected teacher_ids and teacher_logits [rows, K]")
+    K = teacher_ids.shape[1]
+    loss, lossp = _output(loss, "f32", (R,), "loss", dev)
+    dptr, ldd = None, 0
+    if dlogits is not None:
+        dptr, ldd = _rows(dlogits, kind, "dlogits", dev, (R, A))
+    elif want_grad:
+        dlogits, ldd = _gradient_like(logits, ptr, ld, dev)
+        dptr = dlogits.data_ptr()
+    _check(getattr(lib(), name)(ptr, ld, _typed(teacher_ids, "i32", (R, K), "teacher_ids", dev),
+                                _typed(teacher_logits, "f32", (R, K), "teacher_logits", dev), _ptr(mask, "u8", (R,)), lossp, dptr, ldd, R, A, K,
+                                temperature, scale, _stream(stream)))
+    return loss if dlogits is None else (loss, dlogits)
+
+
+@_on_stream
+def rlcs_distill_grad(logits, teacher_ids, teacher_logits, *, mask=None, temperature=1.0, scale=1.0, want_grad=True, loss=None, dlogits=None,
+                      stream=None):
+    """Loss of float32 student logits [R, A] (rows may be strided) towards a teacher's logits [R, K] of teacher_ids [R, K] (int32; outside
+    [0, A): absent) and its gradient: (loss, dlogits), or loss alone if want_grad is False.  dlogits may be logits itself."""
+    return _distill_grad("rlcs_distill_grad", "f32", logits, teacher_ids, teacher_logits, mask, temperature, scale, want_grad, loss, dlogits, stream)
+
+
+@_on_stream
+def rlcs_distill_grad_bf16(logits, teacher_ids, teacher_logits, *, mask=None, temperature=1.0, scale=1.0, want_grad=True, loss=None,
+                           dlogits=None, stream=None):
+    """rlcs_distill_grad on bfloat16 logits (dlogits bfloat16; loss and teacher float32)."""
+    return _distill_grad("rlcs_distill_grad_bf16", "bf16", logits, teacher_ids, teacher_logits, mask, temperature, scale, want_grad, loss, dlogits,
+                         stream)
+
+
+@_on_stream
+def rlcs_fork_block_tables(block_table, lens, sources, free_pages, *, page_size, new_table=None, copy_from=None, copy_to=None, pages_used=None,
+                           workspace=None, stream=None):
+    """Page tables of rows that continue rows `sources` [N] of block_table [B, width]: whole pages shared, part-filled last ones copied
+    for all but the first row that continues them.  Returns (new_table [N, width], copy_from [N], copy_to [N], pages_used [1])."""
+    if block_table.dim() != 2 or sources.dim() != 1 or free_pages.dim() != 1:
+        raise ValueError("expected block_table [B, width], sources [N], free_pages [F]")
+    dev = _device_for(block_table)
+    B, width = block_table.shape
+    N = sources.shape[0]
+    new_table, tp = _output(new_table, "i32", (N, width), "new_table", dev)
+    copy_from, fp = _output(copy_from, "i32", (N,), "copy_from", dev)
+    copy_to, cp = _output(copy_to, "i32", (N,), "copy_to", dev)
+    pages_used, up = _output(pages_used, "i32", (1,), "pages_used", dev)
+    old = _typed(block_table, "i32", None, "block_table", dev)
+    if N * width and tp == old:
+        raise ValueError("new_table must not be block_table")
+    wp, room, workspace = _scratch("rlcs_fork_block_tables_workspace_bytes", (B, N), workspace, dev)
+    _check(lib().rlcs_fork_block_tables(old, _typed(lens, "i32", (B,), "lens", dev), _typed(sources, "i32", None, "sources", dev),
+                                        _typed(free_pages, "i32", None, "free_pages", dev), tp, fp, cp, up, B, N, width, free_pages.shape[0],
+                                        page_size, wp, room, _stream(stream)))
+    return new_table, copy_from, copy_to, pages_used
+
+
+@_on_stream
+def rlcs_copy_pages_bf16(k_cache, v_cache, copy_from, copy_to, *, stream=None):
+    """Pages copy_from[i] -> copy_to[i] (int32; negative: none) copied within k_cache and v_cache (None: keys alone)."""
+    if copy_from.dim() != 1:
+        raise ValueError("expected copy_from [N] and copy_to [N]")
+    dev = _device_for(k_cache)
+    s = _caches(k_cache, v_cache, dev)
+    pages, page, Hk, d = k_cache.shape
+    n = copy_from.shape[0]
+    _check(lib().rlcs_copy_pages_bf16(k_cache.data_ptr(), None if v_cache is None else v_cache.data_ptr(), pages, s[0], s[1], s[2],
+                                      _typed(copy_from, "i32", (n,), "copy_from", dev), _typed(copy_to, "i32", (n,), "copy_to", dev), n, page, Hk,
+                                      d, _stream(stream)))
+    return k_cache if v_cache is None else (k_cache, v_cache)
+
+
+@_on_stream
+def rlcs_free_pages(block_table, lens, prefix_table=None, prefix_lens=None, *, num_pages, page_size, free_pages=None, free_count=None,
+                    workspace=None, stream=None):
+    """The pages below num_pages that no row of block_table [B, width] (lens [B]) or prefix_table (prefix_lens) names, ascending:
+    (free_pages int32 [num_pages], -1 behind the last, free_count int32 [1])."""
+    if block_table.dim() != 2 or (prefix_table is None) != (prefix_lens is None) or (prefix_table is not None and prefix_table.dim() != 2):
+        raise ValueError("expected block_table [B, width], and prefix_table [groups, width] with prefix_lens or neither")
+    dev = _device_for(block_table)
+    B, width = block_table.shape
+    groups, prefix_width = (0, 0) if prefix_table is None else prefix_table.shape
+    free_pages, fp = _output(free_pages, "i32", (num_pages,), "free_pages", dev)
+    free_count, cp = _output(free_count, "i32", (1,), "free_count", dev)
+    wp, room, workspace = _scratch("rlcs_free_pages_workspace_bytes", (num_pages,), workspace, dev)
+    _check(lib().rlcs_free_pages(_typed(block_table, "i32", None, "block_table", dev), _typed(lens, "i32", (B,), "lens", dev),
+                                 _typed(prefix_table, "i32", None, "prefix_table", dev), _typed(prefix_lens, "i32", (groups,), "prefix_lens", dev),
+                                 fp, cp, B, width, groups, prefix_width, num_pages, page_size, wp, room, _stream(stream)))
+    return free_pages, free_count

@@ -1,0 +1,383 @@
+// Pages of a paged cache: trajectories continued from others, copies of pages, and the pages that nobody names.
+//
+//   fork    new row i is the old row sources[i]: whole pages are shared, a part-filled last page stays with the first row that
+//           continues it and is copied for the others, to pages taken from the free list in row order
+//   copy    pages from[i] -> to[i] of keys and values
+//   free    the numbers below num_pages that no live entry of the tables names, ascending
+//
+// What a page is shared by needs no counts: it is free when no table names it.
+#include <cstdint>
+
+#include "../../include/rlcs.h"
+#include "rlcs_device.cuh"
+
+namespace {
+
+constexpr int kThreads = 256, kFused = 4096;
+
+bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// ---------------------------------------------------------------------------------------------- fork
+struct ForkParams {
+    const int32_t* table;
+    const int32_t* lens;
+    const int32_t* sources;
+    const int32_t* free_pages;
+    int32_t* out;
+    int32_t* from;
+    int32_t* to;
+    int32_t* used;
+    int32_t* first;            // [B] first new row of each old one     } of large calls, in the workspace
+    int32_t* number;           // [N] place in the free list, or -1     }
+    int32_t B, N, width, free_count, page;
+};
+
+struct OldRow {
+    int source, have, last;    // last: the page that a second row would copy, -1 without one
+};
+
+__device__ __forceinline__ OldRow old_row(const ForkParams& P, int i) {
+    OldRow r = {P.sources[i], 0, -1};
+    if (r.source < 0 || r.source >= P.B) { r.source = -1; return r; }
+    const int len = max(P.lens[r.source], 0);
+    const uint32_t need = ((uint32_t)len + P.page - 1) / (uint32_t)P.page;      // page <= 2^24: no overflow
+    r.have = (int)min(need, (uint32_t)P.width);
+    if (need <= (uint32_t)P.width && len % P.page != 0) r.last = P.table[(int64_t)r.source * P.width + r.have - 1];
+    return r;
+}
+
+// The page that row i takes from the free list.
+__device__ __forceinline__ int taken(const ForkParams& P, int number) {
+    return number >= 0 && number < P.free_count ? max(P.free_pages[number], -1) : -1;
+}
+
+// Place in the free list of every row that needs a page, the rest -1, by the T threads of a block.
+template <int T> __device__ __forceinline__ void fork_numbers(const ForkParams& P, const int32_t* first, int32_t* number, bool write) {
+    __shared__ int part[T / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int carry = 0;
+    for (int base = 0; base < P.N; base += T) {
+        const int i = base + threadIdx.x;
+        bool fresh = false;
+        if (i < P.N) {
+            const OldRow r = old_row(P, i);
+            fresh = r.last >= 0 && first[r.source] != i;
+        }
+        const unsigned some = __ballot_sync(~0u, fresh);
+        __syncthreads();
+        if (lane == 0) part[warp] = __popc(some);
+        __syncthreads();
+        int before = carry;
+        for (int k = 0; k < T / 32; ++k) {
+            if (k < warp) before += part[k];
+            carry += part[k];
+        }
+        if (i < P.N) number[i] = fresh ? before + __popc(some & ((1u << lane) - 1)) : -1;
+    }
+    if (write && threadIdx.x == 0) *P.used = carry;
+}
+
+__global__ void __launch_bounds__(kThreads) fork_first_kernel(const __grid_constant__ ForkParams P) {
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < P.N; i += gridDim.x * kThreads) {
+        const int s = P.sources[i];
+        if (s >= 0 && s < P.B) atomicMin(P.first + s, i);
+    }
+}
+
+__global__ void __launch_bounds__(1024) fork_numbers_kernel(const __grid_constant__ ForkParams P) { fork_numbers<1024>(P, P.first, P.number, true); }
+
+template <bool FUSED>
+__global__ void __launch_bounds__(kThreads) fork_fill_kernel(const __grid_constant__ ForkParams P) {
+    extern __shared__ int32_t held[];
+    const int32_t* number = P.number;
+    if constexpr (FUSED) {
+        int32_t *first = held, *mine = held + P.B;
+        for (int s = threadIdx.x; s < P.B; s += kThreads) first[s] = P.N;
+        __syncthreads();
+        for (int i = threadIdx.x; i < P.N; i += kThreads) {
+            const int s = P.sources[i];
+            if (s >= 0 && s < P.B) atomicMin(first + s, i);
+        }
+        __syncthreads();
+        fork_numbers<kThreads>(P, first, mine, blockIdx.x == 0);
+        __syncthreads();
+        number = mine;
+    }
+    const int64_t step = (int64_t)gridDim.x * kThreads, me = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    for (int64_t i = me; i < P.N; i += step) {
+        const int page = taken(P, number[i]);
+        P.from[i] = page >= 0 ? old_row(P, (int)i).last : -1;
+        P.to[i] = page;
+    }
+    const int64_t cells = (int64_t)P.N * P.width;
+    for (int64_t e = me; e < cells; e += step) {
+        const int i = cells <= 0x7fffffff ? (int)((uint32_t)e / (uint32_t)P.width) : (int)(e / P.width);
+        const int j = (int)(e - (int64_t)i * P.width);
+        const int s = P.sources[i];
+        int v = -1;
+        if (s >= 0 && s < P.B) {
+            const uint32_t need = ((uint32_t)max(P.lens[s], 0) + P.page - 1) / (uint32_t)P.page;
+            if (j < need) v = j + 1 == need && number[i] >= 0 ? taken(P, number[i]) : P.table[(int64_t)s * P.width + j];
+        }
+        P.out[e] = v;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- copy
+struct CopyParams {
+    char* cache[2];
+    const int32_t* from;
+    const int32_t* to;
+    int64_t pages, page_stride, token_stride, head_stride;      // strides in bytes
+    int32_t N, caches, page, Hk, row;                           // row: bytes of one head of one token
+    int64_t page_bytes;                                         // of a page without gaps, else 0
+};
+
+constexpr int kPairs = 1024, kPiece = kThreads * 16 * 4;        // bytes a block copies at a time
+
+__global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ CopyParams P) {
+    __shared__ int2 pairs[kPairs];
+    __shared__ int count;
+    const int64_t bytes = (int64_t)P.page * P.Hk * P.row, pieces = (bytes + kPiece - 1) / kPiece;
+    for (int base = 0; base < P.N; base += kPairs) {
+        __syncthreads();
+        if (threadIdx.x == 0) count = 0;
+        __syncthreads();
+        const int most = min(P.N - base, kPairs);
+        for (int i = threadIdx.x; i < (most + 31) / 32 * 32; i += kThreads) {      // in any order: every block copies its share of its own list
+            int a = -1, b = -1;
+            if (i < most) { a = P.from[base + i]; b = P.to[base + i]; }
+            pairs[i] = make_int2(a, b);
+        }
+        __syncthreads();
+        // the pairs that are there move to the front, in their order, by the first warp
+        if (threadIdx.x < 32) {
+            int n = 0;
+            for (int i = threadIdx.x; i < (most + 31) / 32 * 32; i += 32) {
+                const int2 p = pairs[i];
+                const bool there = p.x >= 0 && p.x < P.pages && p.y >= 0 && p.y < P.pages && p.x != p.y;
+                const unsigned some = __ballot_sync(~0u, there);
+                if (there) pairs[n + __popc(some & ((1u << threadIdx.x) - 1))] = p;
+                n += __popc(some);
+                __syncwarp();
+            }
+            if (threadIdx.x == 0) count = n;
+        }
+        __syncthreads();
+        const int64_t items = count * pieces * P.caches;
+        for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
+            const int2 p = pairs[w / (pieces * P.caches)];
+            const int64_t rest = w % (pieces * P.caches), piece = rest % pieces;
+            char* cache = P.cache[rest / pieces];
+            const char* src = cache + p.x * P.page_stride;
+            char* dst = cache + p.y * P.page_stride;
+            uint4 v[4];
+            int64_t at[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t o = piece * kPiece + (k * kThreads + threadIdx.x) * 16;
+                at[k] = -1;
+                if (o < bytes) {
+                    if (P.page_bytes) {
+                        at[k] = o;
+                    } else {                                   // tokens, heads, pieces of a head
+                        const int64_t unit = o / P.row;
+                        at[k] = unit / P.Hk * P.token_stride + unit % P.Hk * P.head_stride + o % P.row;
+                    }
+                    v[k] = *reinterpret_cast<const uint4*>(src + at[k]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (at[k] >= 0) *reinterpret_cast<uint4*>(dst + at[k]) = v[k];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- free
+struct FreeParams {
+    const int32_t* table[2];
+    const int32_t* lens[2];
+    int32_t rows[2], width[2];
+    uint32_t* bits;            // of the pages that are named
+    int32_t* out;
+    int32_t* count;
+    int32_t pages, words, page;
+};
+
+__global__ void __launch_bounds__(kThreads) free_mark_kernel(const __grid_constant__ FreeParams P) {
+    const int warps = gridDim.x * (kThreads / 32), lane = threadIdx.x & 31;
+    for (int t = 0; t < 2; ++t)
+        for (int b = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); b < P.rows[t]; b += warps) {
+            const uint32_t need = ((uint32_t)max(P.lens[t][b], 0) + P.page - 1) / (uint32_t)P.page;
+            const int have = (int)min(need, (uint32_t)P.width[t]);
+            for (int j = lane; j < have; j += 32) {
+                const int id = P.table[t][(int64_t)b * P.width[t] + j];
+                if (id >= 0 && id < P.pages) atomicOr(P.bits + (id >> 5), 1u << (id & 31));
+            }
+        }
+}
+
+// Free pages among the 32 of a word.
+__device__ __forceinline__ uint32_t spare_of(const FreeParams& P, int word) {
+    if (word >= P.words) return 0u;
+    const uint32_t beyond = word == P.words - 1 && (P.pages & 31) ? ~0u << (P.pages & 31) : 0u;
+    return ~(P.bits[word] | beyond);
+}
+
+__device__ __forceinline__ int block_sum(int v) {
+    __shared__ int part[kThreads / 32];
+    v = __reduce_add_sync(~0u, v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int k = 0; k < kThreads / 32; ++k) all += part[k];
+    return all;
+}
+
+// Every block counts the free pages before its own words, and of all of them, itself.
+__global__ void __launch_bounds__(kThreads) free_list_kernel(const __grid_constant__ FreeParams P) {
+    const int per = (P.words + gridDim.x - 1) / gridDim.x, begin = min((int)blockIdx.x * per, P.words), end = min(begin + per, P.words);
+    int before = 0, all = 0;
+    for (int w = threadIdx.x; w < P.words; w += kThreads) {
+        const int n = __popc(spare_of(P, w));
+        all += n;
+        if (w < begin) before += n;
+    }
+    before = block_sum(before);
+    all = block_sum(all);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = (end - begin + kThreads / 32 - 1) / (kThreads / 32);
+    const int w0 = min(begin + warp * share, end), w1 = min(w0 + share, end);
+    __shared__ int totals[kThreads / 32];
+    int mine = 0;
+    for (int w = w0 + lane; w < w1; w += 32) mine += __popc(spare_of(P, w));
+    mine = __reduce_add_sync(~0u, mine);
+    if (lane == 0) totals[warp] = mine;
+    __syncthreads();
+    for (int k = 0; k < warp; ++k) before += totals[k];
+    for (int w = w0; w < w1; ++w) {
+        const uint32_t spare = spare_of(P, w);
+        if (spare >> lane & 1) P.out[before + __popc(spare & ((1u << lane) - 1))] = w * 32 + lane;
+        before += __popc(spare);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *P.count = all;
+    for (int64_t i = all + (int64_t)blockIdx.x * kThreads + threadIdx.x; i < P.pages; i += (int64_t)gridDim.x * kThreads) P.out[i] = -1;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t rlcs_fork_block_tables_workspace_bytes(int64_t B, int64_t N) {
+    return B <= 0 || N <= 0 || (B <= kFused && N <= kFused) ? 0 : (size_t)(B + N) * sizeof(int32_t);
+}
+
+int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, const int32_t* sources, const int32_t* free_pages,
+                           int32_t* new_table, int32_t* copy_from, int32_t* copy_to, int32_t* pages_used, int64_t B, int64_t N,
+                           int64_t width, int64_t free_count, int64_t page_size, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    const int64_t kMost = (int64_t(1) << 31) - 1;
+    if (B < 0 || N < 0 || width < 0 || free_count < 0 || page_size < 0) return RLCS_ERR_SIZE;
+    if (B >= (int64_t(1) << 24) || N >= (int64_t(1) << 24) || width > (int64_t(1) << 24) || free_count > kMost || page_size > (int64_t(1) << 24))
+        return RLCS_ERR_SIZE;
+    if (page_size == 0) return RLCS_ERR_ARG;
+    if (pages_used == nullptr || (N > 0 && (sources == nullptr || copy_from == nullptr || copy_to == nullptr || (width > 0 && new_table == nullptr))) ||
+        (N > 0 && B > 0 && (lens == nullptr || (width > 0 && block_table == nullptr))) || (free_count > 0 && free_pages == nullptr))
+        return RLCS_ERR_NULL;
+    const void* words[] = {block_table, lens, sources, free_pages, new_table, copy_from, copy_to, pages_used};
+    for (const void* p : words)
+        if (!aligned_to(p, 4)) return RLCS_ERR_ALIGN;
+    const size_t need = rlcs_fork_block_tables_workspace_bytes(B, N);
+    if (need > 0) {
+        if (workspace == nullptr || workspace_bytes < need) return RLCS_ERR_WORKSPACE;
+        if (!aligned_to(workspace, 16)) return RLCS_ERR_ALIGN;
+    }
+    int32_t* const first = static_cast<int32_t*>(workspace);
+    const ForkParams P = {block_table, lens, sources, free_pages, new_table, copy_from, copy_to, pages_used, first, need > 0 ? first + B : nullptr,
+                          (int32_t)B, (int32_t)N, (int32_t)width, (int32_t)free_count, (int32_t)page_size};
+    const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const int64_t most = N * (width > 0 ? width : 1), sms = rlcs_device::limits().sms;
+    int64_t blocks = (most + kThreads * 4 - 1) / (kThreads * 4);
+    blocks = blocks < 1 ? 1 : blocks > 4 * sms ? 4 * sms : blocks;
+    if (need == 0) {
+        fork_fill_kernel<true><<<(unsigned)blocks, kThreads, (B + N) * sizeof(int32_t), s>>>(P);
+    } else {
+        if (cudaMemsetAsync(first, 0x7f, (size_t)B * sizeof(int32_t), s) != cudaSuccess) return RLCS_ERR_CUDA;
+        fork_first_kernel<<<(unsigned)((N + kThreads - 1) / kThreads < 4 * sms ? (N + kThreads - 1) / kThreads : 4 * sms), kThreads, 0, s>>>(P);
+        fork_numbers_kernel<<<1, 1024, 0, s>>>(P);
+        fork_fill_kernel<false><<<(unsigned)blocks, kThreads, 0, s>>>(P);
+    }
+    return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
+}
+
+int rlcs_copy_pages_bf16(uint16_t* k_cache, uint16_t* v_cache, int64_t pages, int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                         const int32_t* copy_from, const int32_t* copy_to, int64_t N, int64_t page_size, int64_t Hk, int64_t d,
+                         void* cuda_stream) {
+    if (N < 0 || pages < 0 || page_size < 0 || Hk < 0 || d < 0) return RLCS_ERR_SIZE;
+    if (N > (1 << 30) || pages > (int64_t(1) << 31) - 1 || page_size > (1 << 24) || Hk > 4096 || d > (1 << 16) || d % 8 != 0) return RLCS_ERR_SIZE;
+    if (page_stride < 0 || token_stride < 0 || head_stride < 0) return RLCS_ERR_SIZE;
+    if (N == 0 || pages == 0 || page_size == 0 || Hk == 0 || d == 0) return RLCS_OK;
+    if (k_cache == nullptr || copy_from == nullptr || copy_to == nullptr) return RLCS_ERR_NULL;
+    if (!aligned_to(k_cache, 16) || !aligned_to(v_cache, 16) || !aligned_to(copy_from, 4) || !aligned_to(copy_to, 4)) return RLCS_ERR_ALIGN;
+    if (page_stride % 8 || token_stride % 8 || head_stride % 8) return RLCS_ERR_ALIGN;
+    // a page's tokens and heads, one after the other in either order
+    const bool tight = (head_stride == d || Hk == 1) && (token_stride == Hk * d || page_size == 1);
+    const bool heads_first = (token_stride == d || page_size == 1) && (head_stride == page_size * d || Hk == 1);
+    const int64_t bytes = page_size * Hk * d * 2;
+    CopyParams P = {};
+    P.cache[0] = reinterpret_cast<char*>(k_cache);
+    P.cache[1] = reinterpret_cast<char*>(v_cache);
+    P.from = copy_from;
+    P.to = copy_to;
+    P.pages = pages;
+    P.page_stride = page_stride * 2;
+    P.token_stride = token_stride * 2;
+    P.head_stride = head_stride * 2;
+    P.N = (int32_t)N;
+    P.caches = v_cache != nullptr ? 2 : 1;
+    P.page = (int32_t)page_size;
+    P.Hk = (int32_t)Hk;
+    P.row = (int32_t)(d * 2);
+    P.page_bytes = tight || heads_first ? bytes : 0;
+    const int64_t sms = rlcs_device::limits().sms, items = N * P.caches * ((bytes + kPiece - 1) / kPiece);
+    copy_kernel<<<(unsigned)(items < 8 * sms ? items : 8 * sms), kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(P);
+    return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
+}
+
+size_t rlcs_free_pages_workspace_bytes(int64_t num_pages) {
+    return num_pages <= 0 || num_pages > (int64_t(1) << 31) - 1 ? 0 : (size_t)((num_pages + 31) / 32) * sizeof(uint32_t);
+}
+
+int rlcs_free_pages(const int32_t* block_table, const int32_t* lens, const int32_t* prefix_table, const int32_t* prefix_lens,
+                    int32_t* free_pages, int32_t* free_count, int64_t B, int64_t width, int64_t groups, int64_t prefix_width,
+                    int64_t num_pages, int64_t page_size, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (B < 0 || width < 0 || groups < 0 || prefix_width < 0 || num_pages < 0 || page_size < 0) return RLCS_ERR_SIZE;
+    if (B >= (int64_t(1) << 24) || groups >= (int64_t(1) << 24) || width > (int64_t(1) << 24) || prefix_width > (int64_t(1) << 24) ||
+        num_pages > (int64_t(1) << 31) - 64 || page_size > (int64_t(1) << 24))
+        return RLCS_ERR_SIZE;
+    if (page_size == 0) return RLCS_ERR_ARG;
+    if (free_count == nullptr || (num_pages > 0 && free_pages == nullptr) || (B > 0 && (lens == nullptr || (width > 0 && block_table == nullptr))) ||
+        (groups > 0 && (prefix_lens == nullptr || (prefix_width > 0 && prefix_table == nullptr))))
+        return RLCS_ERR_NULL;
+    const void* all[] = {block_table, lens, prefix_table, prefix_lens, free_pages, free_count};
+    for (const void* p : all)
+        if (!aligned_to(p, 4)) return RLCS_ERR_ALIGN;
+    const size_t need = rlcs_free_pages_workspace_bytes(num_pages);
+    if (need > 0) {
+        if (workspace == nullptr || workspace_bytes < need) return RLCS_ERR_WORKSPACE;
+        if (!aligned_to(workspace, 16)) return RLCS_ERR_ALIGN;
+    }
+    const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    FreeParams P = {{block_table, prefix_table}, {lens, prefix_lens}, {(int32_t)B, (int32_t)groups}, {(int32_t)width, (int32_t)prefix_width},
+                    static_cast<uint32_t*>(workspace), free_pages, free_count, (int32_t)num_pages, (int32_t)((num_pages + 31) / 32),
+                    (int32_t)page_size};
+    const int64_t sms = rlcs_device::limits().sms, rows = (B > groups ? B : groups), blocks = (rows + kThreads / 32 - 1) / (kThreads / 32);
+    if (need > 0 && cudaMemsetAsync(workspace, 0, need, s) != cudaSuccess) return RLCS_ERR_CUDA;
+    if (rows > 0) free_mark_kernel<<<(unsigned)(blocks < 8 * sms ? blocks : 8 * sms), kThreads, 0, s>>>(P);
+    const int64_t parts = (P.words + kThreads - 1) / kThreads;
+    free_list_kernel<<<(unsigned)(parts < 1 ? 1 : parts < sms ? parts : sms), kThreads, 0, s>>>(P);
+    return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
+}
+
+}  // extern "C"

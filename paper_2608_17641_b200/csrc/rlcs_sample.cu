@@ -16,13 +16,12 @@
 #include "../../include/rlcs.h"
 #include "rlcs_device.cuh"
 #include "rlcs_pair.cuh"
-#include "rlcs_rows.cuh"
+#include "rlcs_weights.cuh"
 
 namespace {
 
 using namespace rlcs_pair;
 using namespace rlcs_rows;
-typedef unsigned long long u64;
 
 constexpr int64_t kMostBlocks = (int64_t(1) << 31) - 1;
 
@@ -56,21 +55,6 @@ template <typename T> struct Key {
     }
 };
 
-// The logit as compared: NaN counts as -inf (never drawn), -0 as +0.
-__device__ __forceinline__ float clean(float f) { return fmaxf(f, -INFINITY) + 0.f; }
-
-__device__ __forceinline__ float scaled(float x, float m, float inv_t) { return x == m ? 0.f : (x - m) * inv_t; }
-
-// floor(2^31 e + 1/2) for 0 <= e <= 1.  Below 2^-10, nearly every logit of a wide row, one multiply-add rounded down leaves the
-// whole number in the upper bits of its fraction; above, the 24 bits of e are shifted by its exponent and the last place rounded.
-__device__ __forceinline__ uint32_t weight_of(float e) {
-    if (e < 0x1p-10f) return (__float_as_uint(__fmaf_rd(e, 0x1p31f, 4194304.5f)) & 0x7fffffu) >> 1;
-    const uint32_t u = __float_as_uint(e);
-    const int down = 127 - (int)(u >> 23);
-    const uint32_t frac = (u << 8) | 0x80000000u;
-    return down == 0 ? frac : ((frac >> (down - 1)) + 1) >> 1;
-}
-
 // A row's settings, with the cases that leave one candidate folded into limit = 1.
 struct Rules {
     float inv_t, p, low;
@@ -84,7 +68,7 @@ template <typename T> __device__ __forceinline__ Rules rules_of(const SamplePara
     r.p = P.top_p != nullptr ? P.top_p[row] : P.top_p_all;
     r.low = P.min_p != nullptr ? P.min_p[row] : P.min_p_all;
     const bool greedy = !(t > 0.f);
-    r.inv_t = greedy ? 1.f : fminf(1.f / t, 3.4028235e38f);       // finite: 0 stays 0 in what it multiplies
+    r.inv_t = inverse_of(t);
     r.limit = k > 0 && k < P.A ? k : P.A;
     if (greedy || r.p <= 0.f || r.low > 1.f) r.limit = 1;
     if (!(r.low > 0.f) || r.low > 1.f) r.low = 0.f;
@@ -95,12 +79,6 @@ template <typename T> __device__ __forceinline__ Rules rules_of(const SamplePara
 __device__ __forceinline__ uint32_t weight_at(float x, float m, const Rules& r) {
     const float e = expf(scaled(x, m, r.inv_t));
     return e >= r.low ? weight_of(e) : 0u;
-}
-
-__device__ __forceinline__ u64 target_of(float uniform, u64 kept) {
-    const double u = (double)uniform;
-    const u64 t = u > 0. ? (u64)(u * (double)kept) : 0;
-    return t < kept ? t : kept - 1;
 }
 
 // How many of equally weighted candidates stay when `above` lies before them: the least n with above + n w >= enough.
