@@ -14,7 +14,8 @@ struct ChunkParams {
     AttnParams a;                  // B: tokens of the step; block_table, lens: of the trajectories
     const int32_t* offsets;        // [seqs + 1]
     int seqs, max_new;
-    int tiles;                     // of 16 rows, a trajectory
+    int tiles;                     // of 16 rows, a trajectory; 0: blocks of 256 rows
+    int slots;                     // of blocks of 256 rows over all trajectories
 };
 
 struct Chunk {
@@ -34,6 +35,8 @@ __device__ __forceinline__ Chunk chunk_of(const ChunkParams& C, int b) {
 __device__ __forceinline__ int keys_of(const ChunkParams& C, const Chunk& c, int rows) {
     return clamp_to(c.start + (rows + C.a.r - 1) / C.a.r, 0, C.a.max_len);
 }
+
+__device__ __forceinline__ int divide_up_device(int a, int b) { return (a + b - 1) / b; }
 
 template <int D, bool TMA>
 __global__ void __launch_bounds__(kThreads)
@@ -56,6 +59,393 @@ chunk_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUte
     if (begin >= end) return;
     segment<D, TMA, true>(P, &k_map, &v_map, raw, ids, bars, &gave_up, P.block_table + (int64_t)b * P.own_width, P.own_width, begin, end, kv_head,
                           first_row, rows, c.first, seg, c.start + 1 - begin);
+}
+
+// ---------------------------------------------------------------------------------------------- chunks of more than 16 rows
+// Two tiles of 128 rows a block on tcgen05, 128 keys a step.  A row tile has 256 columns of tensor memory: the scores of a step,
+// over which the weights are written back as bfloat16, and O.  Four warps a row tile: one row a thread (maximum, exponentials, sums),
+// its 128 scores in registers, which two more warpgroups' worth of registers pays for (setmaxnreg).  One warp a row tile issues its
+// products; while one tile's scores are weighed the other's products run.  The weights leave in two halves, so that the second
+// product starts while the second half is computed.  Keys and values come through the page table into a ring of slots, as TMA
+// boxes where pages divide 128 keys into parts of at least eight rows or are whole tiles, piece by piece otherwise.
+//
+// One rounding of the weights to bfloat16 (2^-9 of each on average of the largest half step 2^-8) is as large as the output's own;
+// a second part would be a third of the products.
+constexpr int kKeys = 128, kWideRows = 256, kWideThreads = 384, kCopiers = 64, kMostSegment = 65536;
+
+template <int D> struct WideShape {
+    static constexpr int kSlot = kKeys * D * 2, kSlots = D == 128 ? 4 : 8, kQ = 128 * D * 2;
+    static constexpr int kBytes = 2 * kQ + kSlots * kSlot + 1024;      // + alignment
+    static constexpr int kMore = 208, kLess = 88;                      // registers a thread: 256 * 208 + 128 * 88 = 384 * 168
+};
+
+struct WideTile {
+    int b, first_row;
+};
+
+// Which rows a slot has, for the first warp: blocks with many keys first, so that the last to start are short.  Up to 128 trajectories
+// go by the tile's place in its chunk (level by level from the highest), more by trajectory.
+__device__ __forceinline__ WideTile wide_tile(const ChunkParams& C, int slot, int lane) {
+    auto tiles_of = [&](int b) { return b < C.seqs ? (int)(((int64_t)chunk_of(C, b).count * C.a.r + kWideRows - 1) / kWideRows) : 0; };
+    if (C.seqs <= 128) {
+        int n[4], most = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            n[q] = tiles_of(q * 32 + lane);
+            most = max(most, n[q]);
+        }
+        most = __reduce_max_sync(~0u, most);
+        auto from = [&](int level) {                              // tiles at or above a level
+            int sum = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum += max(n[q] - level, 0);
+            return __reduce_add_sync(~0u, sum);
+        };
+        if (slot >= from(0)) return WideTile{-1, 0};
+        int lo = 0, hi = most - 1;                                // the highest level with more than `slot` tiles at or above it
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (from(mid) > slot) lo = mid; else hi = mid - 1;
+        }
+        int rank = slot - from(lo + 1);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const unsigned some = __ballot_sync(~0u, n[q] > lo);
+            if (rank < __popc(some)) return WideTile{q * 32 + (int)__fns(some, 0, rank + 1), lo * kWideRows};
+            rank -= __popc(some);
+        }
+        return WideTile{-1, 0};
+    }
+    // trajectory b's tiles start at slot floor(offset_b r / 256) + b: at least as many slots as tiles for any sizes
+    int lo = 0, hi = C.seqs - 1;
+    auto first_slot = [&](int b) { return (int)((int64_t)clamp_to(C.offsets[b], 0, C.a.B) * C.a.r / kWideRows) + b; };
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (first_slot(mid) <= slot) lo = mid; else hi = mid - 1;
+    }
+    const int at = slot - first_slot(lo), n = tiles_of(lo);
+    return at >= 0 && at < n ? WideTile{lo, (n - 1 - at) * kWideRows} : WideTile{-1, 0};
+}
+
+template <int D, bool TMA>
+__global__ void __launch_bounds__(kWideThreads, 1)
+wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    typedef WideShape<D> Shape;
+    constexpr int kSlots = Shape::kSlots, kPieces = D / 8;
+    constexpr uint32_t kScores = 1u << 4 | 1u << 7 | 1u << 10 | (kKeys >> 3) << 17 | (128 >> 4) << 24;
+    constexpr uint32_t kValues = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 16 | (D >> 3) << 17 | (128 >> 4) << 24;      // V: keys by rows
+    extern __shared__ char raw[];
+    __shared__ int ids[kMaxIds + kKeys + 8];
+    __shared__ __align__(8) uint64_t bars[2 * kSlots + 9];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    __shared__ WideTile which;
+    const AttnParams& P = C.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (warp == 0) {
+        const WideTile w = wide_tile(C, (int)(blockIdx.x % C.slots), lane);
+        if (lane == 0) which = w;
+    }
+    __syncthreads();
+    const int b = which.b, first_row = which.first_row;
+    if (b < 0) return;
+    const int kv_head = (int)(blockIdx.x / C.slots) % P.Hk, seg = (int)(blockIdx.x / C.slots) / P.Hk;
+    const Chunk c = chunk_of(C, b);
+    const int rows = c.count * P.r;
+    const int begin = seg * P.own_seg, end = min(begin + P.own_seg, keys_of(C, c, min(first_row + kWideRows, rows)));
+    const bool whole_row = P.own_segs <= 1;                       // outputs leave at once, not as parts to be joined
+    if (begin >= end) {
+        if (whole_row && seg == 0)
+            for (int i = tid; i < min(kWideRows, rows - first_row) * (P.d / 8); i += kWideThreads) {
+                const int row = first_row + i / (P.d / 8);
+                const int64_t at = (int64_t)(c.first + row / P.r) * P.H + kv_head * P.r + row % P.r;
+                *reinterpret_cast<uint4*>(P.out + at * P.d + i % (P.d / 8) * 8) = make_uint4(0, 0, 0, 0);
+                if (i % (P.d / 8) == 0 && P.lse != nullptr) P.lse[at] = -INFINITY;
+            }
+        return;
+    }
+    const uint32_t q_at = (smem_at(raw) + 1023) & ~1023u, ring = q_at + 2 * Shape::kQ;
+    const uint32_t full = smem_at(bars), empty = full + 8 * kSlots, drained = empty + 8 * kSlots;
+    const uint32_t s_full = drained + 8, p_full = s_full + 16, o_done = p_full + 32;      // one a row tile; two halves of p a row tile
+    const int row_tiles = rows - first_row > 128 ? 2 : 1, tiles = divide_up_device(end - begin, kKeys);
+    const int held = clamp_to(P.lens[b], 0, 0x7fffff00);          // tokens whose memory may be read
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_at)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (tid == 0) {
+        gave_up = 0;
+        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kCopiers); bar_init(empty + 8 * i, row_tiles); }
+        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(o_done + 8 * i, 1); }
+        for (int i = 0; i < 4; ++i) bar_init(p_full + 8 * i, 128);
+        bar_init(drained, 2);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    // queries, zeros where there are none
+    for (int i = tid; i < kWideRows * kPieces; i += kWideThreads) {
+        const int row = i / kPieces, piece = i % kPieces, at = first_row + row;
+        uint4 v = {0, 0, 0, 0};
+        if (at < rows && piece * 8 < P.d)
+            v = *reinterpret_cast<const uint4*>(P.q + (int64_t)(c.first + at / P.r) * P.q_stride + (int64_t)(kv_head * P.r + at % P.r) * P.d + piece * 8);
+        const uint32_t dst = q_at + (row >> 7) * Shape::kQ + (piece >> 3) * (128 * 128) + (row & 127) * 128 + (((piece & 7) ^ (row & 7)) << 4);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    }
+    fence_async();
+    fence_before();
+    const int missing = read_ids(P, ids, P.block_table + (int64_t)b * P.own_width, P.own_width, begin, min(begin + tiles * kKeys, held), tid, kWideThreads);
+    fence_after();
+    const uint32_t tmem = tmem_at;
+    const int offset = begin % P.page;
+    // keys that row tile rt sees, in this segment
+    auto sees_of = [&](int rt) { return clamp_to(keys_of(C, c, min(first_row + (rt + 1) * 128, rows)) - begin, 0, end - begin); };
+
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kMore));
+        const int rt = warp >> 2, row = first_row + warp * 32 + lane;
+        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + rt * 256, o_at = mine + 128;
+        const uint32_t my_s = s_full + 8 * rt, my_p = p_full + 16 * rt, my_o = o_done + 8 * rt;
+        const bool any_row = first_row + warp * 32 < rows;
+        const int n = rt < row_tiles ? divide_up_device(sees_of(rt), kKeys) : 0;
+        const int lim = row < rows ? clamp_to(min(c.start + row / P.r + 1, P.max_len) - begin, 0, end - begin) : end - begin;
+        const int least = __reduce_min_sync(~0u, lim);
+        float m = -INFINITY, l = 0.f;
+        bool fine = true;
+        for (int i = 0; i < n; ++i) {
+            fine = __all_sync(~0u, bar_wait(my_s, i & 1, &gave_up, P.polls));
+            if (!fine) break;
+            fence_after();
+            if (any_row) {
+                uint32_t s[kKeys];
+#pragma unroll
+                for (int k = 0; k < kKeys; k += 32) tmem_load32(s + k, mine + k);
+                tmem_wait_load();
+                if ((i + 1) * kKeys > least || missing) {
+                    const int left = lim - i * kKeys;
+#pragma unroll
+                    for (int k = 0; k < kKeys; ++k) {
+                        const bool there = k < left && (!missing || ids[page_of(P, offset + i * kKeys + k)] >= 0);
+                        if (!there) s[k] = __float_as_uint(-INFINITY);
+                    }
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < kKeys; k += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top[e] = fmaxf(fmaxf(top[e], __uint_as_float(s[k + 2 * e])), __uint_as_float(s[k + 2 * e + 1]));
+                const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * P.scale_log2;
+                // the base follows the maximum only when it is 2^8 behind: the weights stay below 2^8, and O is seldom rescaled
+                if (__any_sync(~0u, now > m + 8.f)) {
+                    const float next = fmaxf(m, now), fade = m == -INFINITY ? 0.f : exp2_of(m - next);
+                    if (i > 0) {                                  // the scores came after the last step's second product
+#pragma unroll
+                        for (int k = 0; k < D; k += 16) {
+                            uint32_t o[16];
+                            tmem_load16(o, o_at + k);
+                            tmem_wait_load();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fade);
+                            tmem_store16(o_at + k, o);
+                        }
+                    }
+                    l *= fade;
+                    m = next;
+                }
+                const float base = m == -INFINITY ? 0.f : m;
+                const float2 scale = {P.scale_log2, P.scale_log2}, less = {-base, -base};
+                float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+                for (int part = 0; part < 4; ++part) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float2 p = fma2(make_float2(__uint_as_float(s[part * 32 + 2 * k]), __uint_as_float(s[part * 32 + 2 * k + 1])), scale, less);
+                        p = make_float2(exp2_of(p.x), exp2_of(p.y));
+                        sum[k & 1] = add2(sum[k & 1], p);
+                        w[k] = pack2(p.x, p.y);
+                    }
+                    tmem_store16(mine + part * 16, w);
+                    if (part & 1) {
+                        tmem_wait_store();
+                        fence_before();
+                        bar_arrive(my_p + 8 * (part >> 1));
+                    }
+                }
+                l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+            } else {
+                fence_before();
+                bar_arrive(my_p);
+                bar_arrive(my_p + 8);
+            }
+        }
+        if (any_row && rt < row_tiles) {
+            if (n > 0 && fine) fine = __all_sync(~0u, bar_wait(my_o, (n - 1) & 1, &gave_up, P.polls));
+            fine = fine && *(volatile int*)&gave_up == 0;         // a thread that copies may have given up alone
+            fence_after();
+            const int64_t at = (int64_t)(c.first + row / P.r) * P.H + kv_head * P.r + row % P.r, dst = (int64_t)seg * P.B * P.H + at;
+            if (!fine) l = __int_as_float(0x7fffffff);
+            const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+            for (int k = 0; k < D; k += 32) {
+                uint32_t o[32];
+                if (n > 0) {
+                    tmem_load32(o, o_at + k);
+                    tmem_wait_load();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0;
+                }
+                if (row >= rows) continue;
+                if (whole_row) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+                        if (k + e < P.d) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) w[h] = l == 0.f ? 0u : pack2(__uint_as_float(o[e + 2 * h]) * inv, __uint_as_float(o[e + 2 * h + 1]) * inv);
+                            *reinterpret_cast<uint4*>(P.out + at * P.d + k + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<uint4*>(P.part_o + dst * D + k + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+            }
+            if (row < rows) {
+                if (!whole_row) P.part_ml[dst] = fine ? make_float2(m, l) : make_float2(0.f, l);
+                else if (P.lse != nullptr) P.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            }
+        }
+        fence_before();
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kLess));
+        if (warp == 8 || warp == 11) {
+            const int me = (warp == 8 ? 0 : 32) + lane, piece = me % kPieces, row0 = me / kPieces;
+            constexpr int kStep = kCopiers / kPieces, kRows = kKeys / kStep;
+            const uint32_t lane_at = ring + (piece >> 3) * (kKeys * 128);
+            auto pieces = [&](int item) {                         // one tile of keys or values, zeros where there is no key
+                const __nv_bfloat16* from = (item & 1 ? P.v : P.k) + kv_head * P.head_stride + piece * 8;
+                const uint32_t dst = lane_at + (item % kSlots) * Shape::kSlot;
+#pragma unroll 4
+                for (int k = 0; k < kRows; ++k) {
+                    const int row = row0 + k * kStep, local = (item >> 1) * kKeys + row;
+                    int64_t place = 0;
+                    bool there = begin + local < held && piece * 8 < P.d;
+                    if (there) {
+                        const int in = offset + local, pg = page_of(P, in), id = ids[pg];
+                        there = id >= 0;
+                        if (there) place = id * P.page_stride + (in - pg * P.page) * P.token_stride;
+                    }
+                    copy16(dst + row * 128 + (((piece & 7) ^ (row & 7)) << 4), from + place, there);
+                }
+            };
+            auto room = [&](int item) { return item < kSlots || bar_wait(empty + 8 * (item % kSlots), (item / kSlots - 1) & 1, &gave_up, P.polls); };
+            bool fine = true;
+            if constexpr (TMA) {
+                // all but the tile in which the trajectory ends: what lies behind its last value may be anything
+                const int whole = min(tiles, (held - begin) / kKeys), box = P.page < kKeys ? P.page : kKeys;
+                int issued = 0;
+                if (me == 0)
+                    for (int i = 0; i < 2 * whole && fine; ++i) {
+                        fine = room(i);
+                        if (!fine) break;
+                        const uint32_t bar = full + 8 * (i % kSlots), dst = ring + (i % kSlots) * Shape::kSlot;
+                        issued = i + 1;
+                        bar_expect(bar, Shape::kSlot);
+                        for (int row = 0; row < kKeys; row += box) {
+                            const int in = offset + (i >> 1) * kKeys + row, pg = page_of(P, in);
+#pragma unroll
+                            for (int half = 0; half < D / 64; ++half)     // a page number of -1 lies outside the map: zeros
+                                box_load(dst + half * (kKeys * 128) + row * 128, i & 1 ? &v_map : &k_map, bar, half * 64, in - pg * P.page, kv_head, ids[pg]);
+                        }
+                    }
+                if (whole < tiles) {
+                    asm volatile("bar.sync 1, %0;" ::"n"(kCopiers) : "memory");
+                    for (int i = 2 * whole; i < 2 * whole + 2 && fine; ++i) {
+                        fine = room(i);
+                        if (fine) pieces(i);
+                    }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    fence_async();
+                    asm volatile("bar.sync 1, %0;" ::"n"(kCopiers) : "memory");
+                    if (me == 0 && fine) {
+                        bar_arrive(full + 8 * (2 * whole % kSlots));
+                        bar_arrive(full + 8 * ((2 * whole + 1) % kSlots));
+                    }
+                }
+                // no boxes in flight when the block ends, whoever gave up (where the partial tile's slots were free, theirs had arrived)
+                int late = 0;
+                for (int i = max(0, issued - kSlots + (fine && whole < tiles ? 2 : 0)); i < issued; ++i)
+                    bar_wait(full + 8 * (i % kSlots), (i / kSlots) & 1, &late, kPolls);
+            } else {
+                for (int i = 0; i < 2 * tiles && fine; ++i) {
+                    fine = room(i);
+                    if (!fine) break;
+                    pieces(i);
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    fence_async();
+                    bar_arrive(full + 8 * (i % kSlots));
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        } else {
+            const int rt = warp - 9;
+            const uint32_t base = __shfl_sync(~0u, tmem, 0) + rt * 256;
+            const uint32_t my_s = s_full + 8 * rt, my_p = p_full + 16 * rt, my_o = o_done + 8 * rt;
+            auto wait = [&](uint32_t bar, int parity) { return (bool)__all_sync(~0u, bar_wait(bar, parity & 1, &gave_up, P.polls)); };
+            const int n = rt < row_tiles ? divide_up_device(sees_of(rt), kKeys) : 0;
+            const uint64_t q_desc = describe(q_at + rt * Shape::kQ, 16), k_desc = describe(ring, 16), v_desc = describe(ring, kKeys * 128);
+            bool fine = rt < row_tiles;
+            for (int i = 0; i < tiles && fine; ++i) {
+                int slot = 2 * i % kSlots;
+                fine = wait(full + 8 * slot, 2 * i / kSlots);
+                if (!fine) break;
+                if (i < n) {
+                    // the last step's weights lie where these scores go: they must have been multiplied
+                    fine = i == 0 || wait(my_o, i - 1);
+                    if (!fine) break;
+                    fence_after();
+                    const uint64_t k_at = k_desc + slot * (Shape::kSlot >> 4);
+#pragma unroll
+                    for (int s = 0; s < D / 16; ++s)
+                        mma_ss(base, q_desc + (((s >> 2) * (128 * 128) + (s & 3) * 32) >> 4), k_at + (((s >> 2) * (kKeys * 128) + (s & 3) * 32) >> 4),
+                               kScores, s > 0);
+                    commit(my_s);
+                    commit(empty + 8 * slot);
+                } else if (lane == 0) {
+                    bar_arrive(empty + 8 * slot);
+                }
+                slot = (2 * i + 1) % kSlots;
+                fine = wait(full + 8 * slot, (2 * i + 1) / kSlots);
+                if (!fine) break;
+                if (i < n) {
+                    const uint64_t v_at = v_desc + slot * (Shape::kSlot >> 4);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        fine = wait(my_p + 8 * half, i);
+                        if (!fine) break;
+                        fence_after();
+#pragma unroll
+                        for (int s = half * (kKeys / 32); s < (half + 1) * (kKeys / 32); ++s)
+                            mma_ts(base + 128, base + s * 8, v_at + ((s * 2048) >> 4), kValues, i > 0 || s > 0);
+                    }
+                    if (!fine) break;
+                    commit(my_o);
+                    commit(empty + 8 * slot);
+                } else if (lane == 0) {
+                    bar_arrive(empty + 8 * slot);
+                }
+            }
+            commit(drained);                                      // nothing in flight when the memory is given back
+            int late = 0;
+            bar_wait(drained, 0, &late, kPolls);
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (warp == 9) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+    }
 }
 
 // Joins a row's segments: one warp a (token, head).
@@ -94,6 +484,20 @@ __global__ void __launch_bounds__(kThreads) chunk_join_kernel(const __grid_const
     if (lane == 0 && P.lse != nullptr) P.lse[at] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
+// Blocks of 256 rows: whole rows while there are two blocks a multiprocessor or more, else the number of segments that makes the
+// rounds of blocks shortest, a segment costing three tiles beyond its own (start, first loads, the partial result).
+int plan_wide(int64_t longest, int64_t units, int page, int64_t sms) {
+    const int64_t by_ids = (int64_t)(kMaxIds - 2) * page / kKeys * kKeys, most = (by_ids < kMostSegment ? by_ids : kMostSegment) / kKeys;
+    const int64_t tiles = divide_up(longest > 0 ? longest : 1, kKeys);
+    int64_t best = most, cost = INT64_MAX;
+    for (int64_t segs = divide_up(tiles, most); segs <= tiles && segs <= 256; ++segs) {
+        const int64_t per = divide_up(tiles, segs), c = divide_up(units * segs, sms) * (per + 3);
+        if (c < cost) { cost = c; best = per; }
+        if (units >= 2 * sms) break;
+    }
+    return (int)(best * kKeys);
+}
+
 // Sizes only: shared by the call and its workspace query.
 int check_shape(ChunkParams& C, int64_t T, int64_t seqs, int64_t H, int64_t Hk, int64_t d, int64_t page, int64_t max_new, int64_t max_len) {
     AttnParams& P = C.a;
@@ -114,14 +518,21 @@ int check_shape(ChunkParams& C, int64_t T, int64_t seqs, int64_t H, int64_t Hk, 
     C.max_new = (int)(max_new < T ? max_new : T);
     if (T == 0 || H == 0 || seqs == 0 || C.max_new == 0) return RLCS_OK;
     if ((int64_t)C.max_new * P.r > (1 << 30)) return RLCS_ERR_SIZE;
-    C.tiles = divide_up((int64_t)C.max_new * P.r, 16);
-    P.own_seg = plan_segment(P.max_len, (int64_t)C.tiles * Hk * seqs, P.page, 1024);
+    if ((int64_t)C.max_new * P.r <= 16) {
+        C.tiles = 1;
+        P.own_seg = plan_segment(P.max_len, Hk * seqs, P.page, 1024);
+    } else {
+        const int64_t rows = T * P.r;
+        C.slots = (int)(rows / kWideRows + seqs);
+        P.own_seg = plan_wide(P.max_len, Hk * (rows / kWideRows + (seqs + 1) / 2), P.page, rlcs_device::limits().sms);
+    }
     P.own_segs = divide_up(P.max_len, P.own_seg);
-    if ((double)C.tiles * Hk * seqs * P.own_segs > 2147483647.0) return RLCS_ERR_SIZE;
+    if ((double)(C.tiles > 0 ? seqs : C.slots) * Hk * (P.own_segs > 0 ? P.own_segs : 1) > 2147483647.0 || T * H > (int64_t(1) << 32)) return RLCS_ERR_SIZE;
     return RLCS_OK;
 }
 
 size_t workspace_of(const ChunkParams& C) {
+    if (C.tiles == 0 && C.a.own_segs <= 1) return 0;
     const size_t rows = (size_t)C.a.own_segs * C.a.B * C.a.H;
     return rows * ((C.a.d <= 64 ? 64 : 128) + 2) * sizeof(float) + 16;
 }
@@ -134,9 +545,25 @@ int launch_chunk(const ChunkParams& C, int64_t blocks, const CUtensorMap& k_map,
     return RLCS_OK;
 }
 
+template <int D, bool TMA>
+int launch_wide(const ChunkParams& C, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t s) {
+    static bool granted[64];
+    if (!grant(wide_kernel<D, TMA>, WideShape<D>::kBytes, granted)) return RLCS_ERR_CUDA;
+    const int segs = C.a.own_segs > 0 ? C.a.own_segs : 1;         // rows without keys are written too
+    wide_kernel<D, TMA><<<(unsigned)(C.slots * C.a.Hk * segs), kWideThreads, WideShape<D>::kBytes, s>>>(C, k_map, v_map);
+    return RLCS_OK;
+}
+
 template <int D> int launch(const ChunkParams& C, cudaStream_t s) {
     CUtensorMap k_map = {}, v_map = {};
     const AttnParams& P = C.a;
+    if (C.tiles == 0) {
+        const bool boxes = box_map(&k_map, P, P.k, kKeys) && box_map(&v_map, P, P.v, kKeys);
+        const int st = boxes ? launch_wide<D, true>(C, k_map, v_map, s) : launch_wide<D, false>(C, k_map, v_map, s);
+        if (st != RLCS_OK || P.own_segs <= 1) return st != RLCS_OK ? st : cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
+        chunk_join_kernel<D><<<(unsigned)divide_up((int64_t)P.B * P.H, kThreads / 32), kThreads, 0, s>>>(C);
+        return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
+    }
     const int64_t blocks = (int64_t)C.tiles * P.Hk * C.seqs * P.own_segs;
     if (blocks > 0) {
         const bool boxes = box_map(&k_map, P, P.k, kPart) && box_map(&v_map, P, P.v, kPart);
@@ -178,7 +605,8 @@ int rlcs_chunk_attention_bf16(const uint16_t* q, int64_t q_stride, const uint16_
         if (!aligned_to(p, 4)) return RLCS_ERR_ALIGN;
     if (!aligned_to(q, 16) || !aligned_to(k_cache, 16) || !aligned_to(v_cache, 16) || !aligned_to(out, 16)) return RLCS_ERR_ALIGN;
     if (q_stride % 8 || page_stride % 8 || token_stride % 8 || head_stride % 8) return RLCS_ERR_ALIGN;
-    if (workspace == nullptr || workspace_bytes < workspace_of(C)) return RLCS_ERR_WORKSPACE;
+    const size_t need = workspace_of(C);
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return RLCS_ERR_WORKSPACE;
     if (!aligned_to(workspace, 16)) return RLCS_ERR_ALIGN;
     P.q = reinterpret_cast<const __nv_bfloat16*>(q);
     P.k = reinterpret_cast<const __nv_bfloat16*>(k_cache);
