@@ -16,10 +16,12 @@ struct ChunkParams {
     int seqs, max_new;
     int tiles;                     // of 16 rows, a trajectory; 0: blocks of 256 rows
     int slots;                     // of blocks of 256 rows over all trajectories
+    uint32_t r_mul;                // ceil(2^32 / r); 0 for r = 1
 };
 
 struct Chunk {
     int first, count, start;       // first token of the step, tokens, place of the first in its trajectory (may be negative)
+    int all;                       // tokens before the cut to max_new
 };
 
 __device__ __forceinline__ Chunk chunk_of(const ChunkParams& C, int b) {
@@ -27,6 +29,7 @@ __device__ __forceinline__ Chunk chunk_of(const ChunkParams& C, int b) {
     c.first = clamp_to(C.offsets[b], 0, C.a.B);
     c.count = clamp_to(C.offsets[b + 1], c.first, C.a.B) - c.first;
     c.start = clamp_to(C.a.lens[b], 0, 0x7fffff00) - c.count;      // no sum with rows of a tile wraps
+    c.all = c.count;
     c.count = min(c.count, C.max_new);
     return c;
 }
@@ -71,27 +74,57 @@ chunk_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUte
 //
 // One rounding of the weights to bfloat16 (2^-9 of each on average of the largest half step 2^-8) is as large as the output's own;
 // a second part would be a third of the products.
-constexpr int kKeys = 128, kWideRows = 256, kWideThreads = 384, kCopiers = 64, kMostSegment = 65536;
+constexpr int kKeys = 64, kWideRows = 256, kWideThreads = 448, kCopiers = 64, kMostSegment = 65536;
+
+// For one thread of a warp, the same one throughout.
+__device__ __forceinline__ bool one_lane() {
+    uint32_t r;
+    asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\nselp.u32 %0, 1, 0, e;\n}" : "=r"(r));
+    return r != 0;
+}
+
+__device__ __forceinline__ void issue_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void issue_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, int add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"(add) : "memory");
+}
+
+__device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, int add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"(add) : "memory");
+}
 
 template <int D> struct WideShape {
-    static constexpr int kSlot = kKeys * D * 2, kSlots = D == 128 ? 4 : 8, kQ = 128 * D * 2;
+    static constexpr int kSlot = kKeys * D * 2, kSlots = 8, kQ = 128 * D * 2;
     static constexpr int kBytes = 2 * kQ + kSlots * kSlot + 1024;      // + alignment
-    static constexpr int kMore = 208, kLess = 88;                      // registers a thread: 256 * 208 + 128 * 88 = 384 * 168
 };
 
 struct WideTile {
-    int b, first_row;
+    int b, first_row;              // b: -1 where the slot has no rows
+    Chunk c;
+    int held;                      // tokens of the trajectory: what of its memory may be read
 };
 
-// Which rows a slot has, for the first warp: blocks with many keys first, so that the last to start are short.  Up to 128 trajectories
+// Which rows a slot has, for one warp: blocks with many keys first, so that the last to start are short.  Up to 128 trajectories
 // go by the tile's place in its chunk (level by level from the highest), more by trajectory.
 __device__ __forceinline__ WideTile wide_tile(const ChunkParams& C, int slot, int lane) {
-    auto tiles_of = [&](int b) { return b < C.seqs ? (int)(((int64_t)chunk_of(C, b).count * C.a.r + kWideRows - 1) / kWideRows) : 0; };
+    WideTile t;
+    t.b = -1;
+    auto tiles_of = [&](const Chunk& c) { return (int)(((int64_t)c.count * C.a.r + kWideRows - 1) / kWideRows); };
     if (C.seqs <= 128) {
+        Chunk c[4];
         int n[4], most = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            n[q] = tiles_of(q * 32 + lane);
+            c[q] = Chunk{0, 0, 0, 0};
+            if (q * 32 + lane < C.seqs) c[q] = chunk_of(C, q * 32 + lane);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            n[q] = tiles_of(c[q]);
             most = max(most, n[q]);
         }
         most = __reduce_max_sync(~0u, most);
@@ -101,7 +134,7 @@ __device__ __forceinline__ WideTile wide_tile(const ChunkParams& C, int slot, in
             for (int q = 0; q < 4; ++q) sum += max(n[q] - level, 0);
             return __reduce_add_sync(~0u, sum);
         };
-        if (slot >= from(0)) return WideTile{-1, 0};
+        if (slot >= from(0)) return t;
         int lo = 0, hi = most - 1;                                // the highest level with more than `slot` tiles at or above it
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -111,20 +144,31 @@ __device__ __forceinline__ WideTile wide_tile(const ChunkParams& C, int slot, in
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const unsigned some = __ballot_sync(~0u, n[q] > lo);
-            if (rank < __popc(some)) return WideTile{q * 32 + (int)__fns(some, 0, rank + 1), lo * kWideRows};
+            if (t.b < 0 && rank < __popc(some)) {
+                const int at = (int)__fns(some, 0, rank + 1);
+                t.b = q * 32 + at;
+                t.c = Chunk{__shfl_sync(~0u, c[q].first, at), __shfl_sync(~0u, c[q].count, at), __shfl_sync(~0u, c[q].start, at),
+                            __shfl_sync(~0u, c[q].all, at)};
+            }
             rank -= __popc(some);
         }
-        return WideTile{-1, 0};
+        t.first_row = lo * kWideRows;
+    } else {
+        // trajectory b's tiles start at slot floor(offset_b r / 256) + b: at least as many slots as tiles for any sizes
+        int lo = 0, hi = C.seqs - 1;
+        auto first_slot = [&](int b) { return (int)((int64_t)clamp_to(C.offsets[b], 0, C.a.B) * C.a.r / kWideRows) + b; };
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first_slot(mid) <= slot) lo = mid; else hi = mid - 1;
+        }
+        t.c = chunk_of(C, lo);
+        const int at = slot - first_slot(lo), n = tiles_of(t.c);
+        if (at < 0 || at >= n) return t;
+        t.b = lo;
+        t.first_row = (n - 1 - at) * kWideRows;
     }
-    // trajectory b's tiles start at slot floor(offset_b r / 256) + b: at least as many slots as tiles for any sizes
-    int lo = 0, hi = C.seqs - 1;
-    auto first_slot = [&](int b) { return (int)((int64_t)clamp_to(C.offsets[b], 0, C.a.B) * C.a.r / kWideRows) + b; };
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (first_slot(mid) <= slot) lo = mid; else hi = mid - 1;
-    }
-    const int at = slot - first_slot(lo), n = tiles_of(lo);
-    return at >= 0 && at < n ? WideTile{lo, (n - 1 - at) * kWideRows} : WideTile{-1, 0};
+    t.held = max(t.c.start + t.c.all, 0);
+    return t;
 }
 
 template <int D, bool TMA>
@@ -136,88 +180,99 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
     constexpr uint32_t kValues = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 16 | (D >> 3) << 17 | (128 >> 4) << 24;      // V: keys by rows
     extern __shared__ char raw[];
     __shared__ int ids[kMaxIds + kKeys + 8];
-    __shared__ __align__(8) uint64_t bars[2 * kSlots + 9];
+    __shared__ __align__(8) uint64_t bars[2 * kSlots + 15];
     __shared__ uint32_t tmem_at;
-    __shared__ int gave_up;
+    __shared__ int gave_up, missing_any;
     __shared__ WideTile which;
     const AttnParams& P = C.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t q_at = (smem_at(raw) + 1023) & ~1023u, ring = q_at + 2 * Shape::kQ;
+    const uint32_t full = smem_at(bars), empty = full + 8 * kSlots, drained = empty + 8 * kSlots;
+    const uint32_t s_full = drained + 8, p_full = s_full + 32, o_done = p_full + 32;      // two a row tile, taken in turn
+    const uint32_t q_full = o_done + 32;                          // one a row tile
+    const int kv_head = (int)(blockIdx.x / C.slots) % P.Hk, seg = (int)(blockIdx.x / C.slots) / P.Hk;
     if (warp == 0) {
         const WideTile w = wide_tile(C, (int)(blockIdx.x % C.slots), lane);
         if (lane == 0) which = w;
+    } else if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_at)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else if (tid == 32) {
+        gave_up = missing_any = 0;
+        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kCopiers); bar_init(empty + 8 * i, 2); }
+        for (int i = 0; i < 4; ++i) { bar_init(s_full + 8 * i, 1); bar_init(p_full + 8 * i, 128); bar_init(o_done + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) bar_init(q_full + 8 * i, 128);
+        bar_init(drained, 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    fence_before();
     __syncthreads();
-    const int b = which.b, first_row = which.first_row;
-    if (b < 0) return;
-    const int kv_head = (int)(blockIdx.x / C.slots) % P.Hk, seg = (int)(blockIdx.x / C.slots) / P.Hk;
-    const Chunk c = chunk_of(C, b);
+    fence_after();
+    const uint32_t tmem = tmem_at;
+    const int b = which.b, first_row = which.first_row, held = which.held;
+    const Chunk c = which.c;
     const int rows = c.count * P.r;
-    const int begin = seg * P.own_seg, end = min(begin + P.own_seg, keys_of(C, c, min(first_row + kWideRows, rows)));
+    const int begin = seg * P.own_seg, end = b < 0 ? begin : min(begin + P.own_seg, keys_of(C, c, min(first_row + kWideRows, rows)));
     const bool whole_row = P.own_segs <= 1;                       // outputs leave at once, not as parts to be joined
+    const int row_tiles = rows - first_row > 128 ? 2 : 1, tiles = divide_up_device(end - begin, kKeys);
+    const int offset = begin % P.page;
+    // the block's rows, counted from its first: tokens and heads
+    const int token0 = first_row / P.r, head0 = first_row % P.r;
+    auto token_of = [&](int k) { return C.r_mul != 0 ? (int)__umulhi((uint32_t)(head0 + k), C.r_mul) : k; };      // from token0 on; (r + 256) r < 2^32
+    // keys that row tile rt sees, in this segment
+    auto sees_of = [&](int rt) { return clamp_to(keys_of(C, c, min(first_row + (rt + 1) * 128, rows)) - begin, 0, end - begin); };
     if (begin >= end) {
-        if (whole_row && seg == 0)
+        if (b >= 0 && whole_row && seg == 0)
             for (int i = tid; i < min(kWideRows, rows - first_row) * (P.d / 8); i += kWideThreads) {
                 const int row = first_row + i / (P.d / 8);
                 const int64_t at = (int64_t)(c.first + row / P.r) * P.H + kv_head * P.r + row % P.r;
                 *reinterpret_cast<uint4*>(P.out + at * P.d + i % (P.d / 8) * 8) = make_uint4(0, 0, 0, 0);
                 if (i % (P.d / 8) == 0 && P.lse != nullptr) P.lse[at] = -INFINITY;
             }
-        return;
-    }
-    const uint32_t q_at = (smem_at(raw) + 1023) & ~1023u, ring = q_at + 2 * Shape::kQ;
-    const uint32_t full = smem_at(bars), empty = full + 8 * kSlots, drained = empty + 8 * kSlots;
-    const uint32_t s_full = drained + 8, p_full = s_full + 16, o_done = p_full + 32;      // one a row tile; two halves of p a row tile
-    const int row_tiles = rows - first_row > 128 ? 2 : 1, tiles = divide_up_device(end - begin, kKeys);
-    const int held = clamp_to(P.lens[b], 0, 0x7fffff00);          // tokens whose memory may be read
-    if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_at)), "n"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
-    if (tid == 0) {
-        gave_up = 0;
-        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kCopiers); bar_init(empty + 8 * i, row_tiles); }
-        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(o_done + 8 * i, 1); }
-        for (int i = 0; i < 4; ++i) bar_init(p_full + 8 * i, 128);
-        bar_init(drained, 2);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    // queries, zeros where there are none
-    for (int i = tid; i < kWideRows * kPieces; i += kWideThreads) {
-        const int row = i / kPieces, piece = i % kPieces, at = first_row + row;
-        uint4 v = {0, 0, 0, 0};
-        if (at < rows && piece * 8 < P.d)
-            v = *reinterpret_cast<const uint4*>(P.q + (int64_t)(c.first + at / P.r) * P.q_stride + (int64_t)(kv_head * P.r + at % P.r) * P.d + piece * 8);
-        const uint32_t dst = q_at + (row >> 7) * Shape::kQ + (piece >> 3) * (128 * 128) + (row & 127) * 128 + (((piece & 7) ^ (row & 7)) << 4);
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-    }
-    fence_async();
-    fence_before();
-    const int missing = read_ids(P, ids, P.block_table + (int64_t)b * P.own_width, P.own_width, begin, min(begin + tiles * kKeys, held), tid, kWideThreads);
-    fence_after();
-    const uint32_t tmem = tmem_at;
-    const int offset = begin % P.page;
-    // keys that row tile rt sees, in this segment
-    auto sees_of = [&](int rt) { return clamp_to(keys_of(C, c, min(first_row + (rt + 1) * 128, rows)) - begin, 0, end - begin); };
-
+    } else
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kMore));
         const int rt = warp >> 2, row = first_row + warp * 32 + lane;
         const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + rt * 256, o_at = mine + 128;
-        const uint32_t my_s = s_full + 8 * rt, my_p = p_full + 16 * rt, my_o = o_done + 8 * rt;
+        const uint32_t my_s = s_full + 16 * rt, my_p = p_full + 16 * rt, my_o = o_done + 16 * rt;
         const bool any_row = first_row + warp * 32 < rows;
         const int n = rt < row_tiles ? divide_up_device(sees_of(rt), kKeys) : 0;
         const int lim = row < rows ? clamp_to(min(c.start + row / P.r + 1, P.max_len) - begin, 0, end - begin) : end - begin;
         const int least = __reduce_min_sync(~0u, lim);
+        const int64_t rows_at = (int64_t)(c.first + token0) * P.H + kv_head * P.r;      // of the outputs [T, H]
+        auto row_at = [&](int k) { return rows_at + (int64_t)token_of(k) * P.H + (head0 + k - token_of(k) * P.r); };
+        {
+            // the warp's queries, zeros where there are none: kPieces lanes a row
+            constexpr int kLoads = kPieces, kTogether = 32 / kPieces;
+            uint4 v[kLoads];
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int k = warp * 32 + j * kTogether + lane / kPieces, piece = lane % kPieces, token = token_of(k);
+                v[j] = make_uint4(0, 0, 0, 0);
+                if (first_row + k < rows && piece * 8 < P.d)
+                    v[j] = *reinterpret_cast<const uint4*>(P.q + (int64_t)(c.first + token0 + token) * P.q_stride + (int64_t)(kv_head * P.r + head0 + k - token * P.r) * P.d + piece * 8);
+            }
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int k = (warp & 3) * 32 + j * kTogether + lane / kPieces, piece = lane % kPieces;
+                const uint32_t dst = q_at + rt * Shape::kQ + (piece >> 3) * (128 * 128) + k * 128 + (((piece & 7) ^ (k & 7)) << 4);
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v[j].x), "r"(v[j].y), "r"(v[j].z), "r"(v[j].w) : "memory");
+            }
+            fence_async();
+            bar_arrive(q_full + 8 * rt);
+        }
+        bool missing = false;
         float m = -INFINITY, l = 0.f;
         bool fine = true;
         for (int i = 0; i < n; ++i) {
-            fine = __all_sync(~0u, bar_wait(my_s, i & 1, &gave_up, P.polls));
+            const uint32_t s_at = mine + (i & 1) * kKeys;
+            fine = __all_sync(~0u, bar_wait(my_s + 8 * (i & 1), (i >> 1) & 1, &gave_up, P.polls));
             if (!fine) break;
             fence_after();
+            if (i == 0) missing = *(volatile int*)&missing_any != 0;      // written before the first key was fetched
             if (any_row) {
                 uint32_t s[kKeys];
 #pragma unroll
-                for (int k = 0; k < kKeys; k += 32) tmem_load32(s + k, mine + k);
+                for (int k = 0; k < kKeys; k += 32) tmem_load32(s + k, s_at + k);
                 tmem_wait_load();
                 if ((i + 1) * kKeys > least || missing) {
                     const int left = lim - i * kKeys;
@@ -236,7 +291,10 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                 // the base follows the maximum only when it is 2^8 behind: the weights stay below 2^8, and O is seldom rescaled
                 if (__any_sync(~0u, now > m + 8.f)) {
                     const float next = fmaxf(m, now), fade = m == -INFINITY ? 0.f : exp2_of(m - next);
-                    if (i > 0) {                                  // the scores came after the last step's second product
+                    if (i > 0) {
+                        fine = __all_sync(~0u, bar_wait(my_o + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, &gave_up, P.polls));
+                        if (!fine) break;
+                        fence_after();
 #pragma unroll
                         for (int k = 0; k < D; k += 16) {
                             uint32_t o[16];
@@ -254,7 +312,7 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                 const float2 scale = {P.scale_log2, P.scale_log2}, less = {-base, -base};
                 float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
-                for (int part = 0; part < 4; ++part) {
+                for (int part = 0; part < 2; ++part) {
                     uint32_t w[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
@@ -263,62 +321,93 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                         sum[k & 1] = add2(sum[k & 1], p);
                         w[k] = pack2(p.x, p.y);
                     }
-                    tmem_store16(mine + part * 16, w);
-                    if (part & 1) {
-                        tmem_wait_store();
-                        fence_before();
-                        bar_arrive(my_p + 8 * (part >> 1));
-                    }
+                    tmem_store16(s_at + part * 16, w);
                 }
                 l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
-            } else {
-                fence_before();
-                bar_arrive(my_p);
-                bar_arrive(my_p + 8);
+                tmem_wait_store();
             }
+            fence_before();
+            bar_arrive(my_p + 8 * (i & 1));
         }
         if (any_row && rt < row_tiles) {
-            if (n > 0 && fine) fine = __all_sync(~0u, bar_wait(my_o, (n - 1) & 1, &gave_up, P.polls));
+            for (int i = max(n - 2, 0); i < n && fine; ++i)
+                fine = __all_sync(~0u, bar_wait(my_o + 8 * (i & 1), (i >> 1) & 1, &gave_up, P.polls));
             fine = fine && *(volatile int*)&gave_up == 0;         // a thread that copies may have given up alone
             fence_after();
-            const int64_t at = (int64_t)(c.first + row / P.r) * P.H + kv_head * P.r + row % P.r, dst = (int64_t)seg * P.B * P.H + at;
             if (!fine) l = __int_as_float(0x7fffffff);
             const float inv = l != 0.f ? 1.f / l : 0.f;
+            // rows leave through the place of the warp's queries, which are done with (nothing was multiplied if n is 0): 256 bytes of a row at a
+            // time, written by the row's thread, stored by sixteen lanes a row
+            const uint32_t mine_at = q_at + rt * Shape::kQ + (warp & 3) * (Shape::kQ / 4);
+            constexpr int kRound = D == 128 ? 16 : 8;                 // 16-byte pieces of a row a round: D values of 16 bits, D / 2 of 32
+            char* const parts = reinterpret_cast<char*>(P.part_o + (int64_t)seg * P.B * P.H * D);
+            const int rounds = whole_row ? 1 : 2;
+            for (int round = 0; round < rounds; ++round) {
+                __syncwarp();
 #pragma unroll
-            for (int k = 0; k < D; k += 32) {
-                uint32_t o[32];
-                if (n > 0) {
-                    tmem_load32(o, o_at + k);
-                    tmem_wait_load();
-                } else {
+                for (int k = 0; k < D; k += 32) {
+                    if (!whole_row && k / (D / 2) != round) continue;
+                    uint32_t o[32];
+                    if (n > 0) {
+                        tmem_load32(o, o_at + k);
+                        tmem_wait_load();
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0;
-                }
-                if (row >= rows) continue;
-                if (whole_row) {
+                        for (int e = 0; e < 32; ++e) o[e] = 0;
+                    }
+                    auto put = [&](int piece, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(mine_at + lane * (kRound * 16) + ((piece ^ (lane & (kRound - 1))) << 4)), "r"(x),
+                                     "r"(y), "r"(z), "r"(w) : "memory");
+                    };
+                    if (whole_row) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-                        if (k + e < P.d) {
+                        for (int e = 0; e < 32; e += 8) {
                             uint32_t w[4];
 #pragma unroll
                             for (int h = 0; h < 4; ++h) w[h] = l == 0.f ? 0u : pack2(__uint_as_float(o[e + 2 * h]) * inv, __uint_as_float(o[e + 2 * h + 1]) * inv);
-                            *reinterpret_cast<uint4*>(P.out + at * P.d + k + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                            put((k + e) / 8, w[0], w[1], w[2], w[3]);
                         }
-                } else {
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4*>(P.part_o + dst * D + k + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        for (int e = 0; e < 32; e += 4) put((k % (D / 2) + e) / 4, o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    }
+                }
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < kRound; ++j) {
+                    const int k = j * (32 / kRound) + lane / kRound, piece = lane % kRound;
+                    uint4 v;
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                                 : "r"(mine_at + k * (kRound * 16) + ((piece ^ (k & (kRound - 1))) << 4)) : "memory");
+                    if (first_row + warp * 32 + k >= rows) continue;
+                    const int64_t at = row_at(warp * 32 + k);
+                    if (!whole_row) *reinterpret_cast<uint4*>(parts + at * (D * 4) + round * (D * 2) + piece * 16) = v;
+                    else if (piece * 8 < P.d) *reinterpret_cast<uint4*>(P.out + at * P.d + piece * 8) = v;
                 }
             }
             if (row < rows) {
-                if (!whole_row) P.part_ml[dst] = fine ? make_float2(m, l) : make_float2(0.f, l);
+                const int64_t at = row_at(warp * 32 + lane);
+                if (!whole_row) P.part_ml[(int64_t)seg * P.B * P.H + at] = fine ? make_float2(m, l) : make_float2(0.f, l);
                 else if (P.lse != nullptr) P.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
             }
         }
         fence_before();
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kLess));
-        if (warp == 8 || warp == 11) {
+        // page numbers of the keys, by the six warps that are left; -1: no such page
+        {
+            const int32_t* table = P.block_table + (int64_t)b * P.own_width;
+            const int first = begin / P.page, count = (min(begin + tiles * kKeys, held) - 1) / P.page - first + 1;
+            bool some = false;
+#pragma unroll 4
+            for (int i = tid - 256; i < count; i += kWideThreads - 256) {
+                int id = first + i < P.own_width ? table[first + i] : -1;
+                if (id < 0 || id >= P.pages) { id = -1; some = true; }
+                ids[i] = id;
+            }
+            if (some) missing_any = 1;
+            asm volatile("bar.sync 2, %0;" ::"n"(kWideThreads - 256) : "memory");
+        }
+        if (warp == 8 || warp == 13) {
             const int me = (warp == 8 ? 0 : 32) + lane, piece = me % kPieces, row0 = me / kPieces;
             constexpr int kStep = kCopiers / kPieces, kRows = kKeys / kStep;
             const uint32_t lane_at = ring + (piece >> 3) * (kKeys * 128);
@@ -388,56 +477,61 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
         } else {
-            const int rt = warp - 9;
+            const int rt = (warp - 9) >> 1;
             const uint32_t base = __shfl_sync(~0u, tmem, 0) + rt * 256;
-            const uint32_t my_s = s_full + 8 * rt, my_p = p_full + 16 * rt, my_o = o_done + 8 * rt;
-            auto wait = [&](uint32_t bar, int parity) { return (bool)__all_sync(~0u, bar_wait(bar, parity & 1, &gave_up, P.polls)); };
+            const uint32_t my_s = s_full + 16 * rt, my_p = p_full + 16 * rt, my_o = o_done + 16 * rt;
             const int n = rt < row_tiles ? divide_up_device(sees_of(rt), kKeys) : 0;
-            const uint64_t q_desc = describe(q_at + rt * Shape::kQ, 16), k_desc = describe(ring, 16), v_desc = describe(ring, kKeys * 128);
-            bool fine = rt < row_tiles;
-            for (int i = 0; i < tiles && fine; ++i) {
-                int slot = 2 * i % kSlots;
-                fine = wait(full + 8 * slot, 2 * i / kSlots);
-                if (!fine) break;
-                if (i < n) {
-                    // the last step's weights lie where these scores go: they must have been multiplied
-                    fine = i == 0 || wait(my_o, i - 1);
-                    if (!fine) break;
-                    fence_after();
-                    const uint64_t k_at = k_desc + slot * (Shape::kSlot >> 4);
-#pragma unroll
-                    for (int s = 0; s < D / 16; ++s)
-                        mma_ss(base, q_desc + (((s >> 2) * (128 * 128) + (s & 3) * 32) >> 4), k_at + (((s >> 2) * (kKeys * 128) + (s & 3) * 32) >> 4),
-                               kScores, s > 0);
-                    commit(my_s);
-                    commit(empty + 8 * slot);
-                } else if (lane == 0) {
-                    bar_arrive(empty + 8 * slot);
-                }
-                slot = (2 * i + 1) % kSlots;
-                fine = wait(full + 8 * slot, (2 * i + 1) / kSlots);
-                if (!fine) break;
-                if (i < n) {
-                    const uint64_t v_at = v_desc + slot * (Shape::kSlot >> 4);
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        fine = wait(my_p + 8 * half, i);
+            if (one_lane()) {
+                auto wait = [&](uint32_t bar, int parity) { return bar_wait(bar, parity & 1, &gave_up, P.polls); };
+                bool fine = true;
+                if (((warp - 9) & 1) == 0) {
+                    const uint64_t q_desc = describe(q_at + rt * Shape::kQ, 16), k_desc = describe(ring, 16);
+                    fine = wait(q_full + 8 * rt, 0) && fine;
+                    for (int i = 0; i < tiles && fine; ++i) {
+                        const int item = 2 * i, slot = item % kSlots;
+                        fine = wait(full + 8 * slot, item / kSlots);
                         if (!fine) break;
-                        fence_after();
+                        if (i < n) {
+                            // the buffer's weights must have been multiplied before new scores go there
+                            fine = i < 2 || wait(my_o + 8 * (i & 1), (i - 2) >> 1);
+                            if (!fine) break;
+                            fence_after();
+                            const uint64_t k_at = k_desc + slot * (Shape::kSlot >> 4);
 #pragma unroll
-                        for (int s = half * (kKeys / 32); s < (half + 1) * (kKeys / 32); ++s)
-                            mma_ts(base + 128, base + s * 8, v_at + ((s * 2048) >> 4), kValues, i > 0 || s > 0);
+                            for (int s = 0; s < D / 16; ++s)
+                                issue_ss(base + (i & 1) * kKeys, q_desc + (((s >> 2) * (128 * 128) + (s & 3) * 32) >> 4),
+                                         k_at + (((s >> 2) * (kKeys * 128) + (s & 3) * 32) >> 4), kScores, s > 0);
+                            issue_commit(my_s + 8 * (i & 1));
+                            issue_commit(empty + 8 * slot);
+                        } else {
+                            bar_arrive(empty + 8 * slot);
+                        }
                     }
-                    if (!fine) break;
-                    commit(my_o);
-                    commit(empty + 8 * slot);
-                } else if (lane == 0) {
-                    bar_arrive(empty + 8 * slot);
+                } else {
+                    const uint64_t v_desc = describe(ring, kKeys * 128);
+                    for (int i = 0; i < tiles && fine; ++i) {
+                        const int item = 2 * i + 1, slot = item % kSlots;
+                        fine = wait(full + 8 * slot, item / kSlots);
+                        if (!fine) break;
+                        if (i < n) {
+                            fine = wait(my_p + 8 * (i & 1), i >> 1);
+                            if (!fine) break;
+                            fence_after();
+                            const uint64_t v_at = v_desc + slot * (Shape::kSlot >> 4);
+#pragma unroll
+                            for (int s = 0; s < kKeys / 16; ++s)
+                                issue_ts(base + 128, base + (i & 1) * kKeys + s * 8, v_at + ((s * 2048) >> 4), kValues, i > 0 || s > 0);
+                            issue_commit(my_o + 8 * (i & 1));
+                            issue_commit(empty + 8 * slot);
+                        } else {
+                            bar_arrive(empty + 8 * slot);
+                        }
+                    }
                 }
+                issue_commit(drained);                            // nothing in flight when the memory is given back
+                int late = 0;
+                bar_wait(drained, 0, &late, kPolls);
             }
-            commit(drained);                                      // nothing in flight when the memory is given back
-            int late = 0;
-            bar_wait(drained, 0, &late, kPolls);
         }
     }
     __syncwarp();
@@ -515,6 +609,7 @@ int check_shape(ChunkParams& C, int64_t T, int64_t seqs, int64_t H, int64_t Hk, 
     P.max_len = (int)max_len;
     P.page_mul = page > 1 ? (uint32_t)(((uint64_t(1) << 32) + page - 1) / page) : 0;
     C.seqs = (int)seqs;
+    C.r_mul = P.r > 1 ? (uint32_t)(((uint64_t(1) << 32) + P.r - 1) / P.r) : 0;
     C.max_new = (int)(max_new < T ? max_new : T);
     if (T == 0 || H == 0 || seqs == 0 || C.max_new == 0) return RLCS_OK;
     if ((int64_t)C.max_new * P.r > (1 << 30)) return RLCS_ERR_SIZE;
@@ -524,7 +619,8 @@ int check_shape(ChunkParams& C, int64_t T, int64_t seqs, int64_t H, int64_t Hk, 
     } else {
         const int64_t rows = T * P.r;
         C.slots = (int)(rows / kWideRows + seqs);
-        P.own_seg = plan_wide(P.max_len, Hk * (rows / kWideRows + (seqs + 1) / 2), P.page, rlcs_device::limits().sms);
+        const int64_t some = seqs < T ? seqs : T, units = rows / kWideRows + (some + 1) / 2;
+        P.own_seg = plan_wide(P.max_len, Hk * (units > some ? units : some), P.page, rlcs_device::limits().sms);
     }
     P.own_segs = divide_up(P.max_len, P.own_seg);
     if ((double)(C.tiles > 0 ? seqs : C.slots) * Hk * (P.own_segs > 0 ? P.own_segs : 1) > 2147483647.0 || T * H > (int64_t(1) << 32)) return RLCS_ERR_SIZE;
