@@ -14,8 +14,8 @@ struct ChunkParams {
     AttnParams a;                  // B: tokens of the step; block_table, lens: of the trajectories
     const int32_t* offsets;        // [seqs + 1]
     int seqs, max_new;
-    int tiles;                     // of 16 rows, a trajectory; 0: blocks of 256 rows
-    int slots;                     // of blocks of 256 rows over all trajectories
+    int tiles;                     // of 16 rows, a trajectory; 0: blocks of 128 rows
+    int slots;                     // of blocks of 128 rows over all trajectories
     uint32_t r_mul;                // ceil(2^32 / r); 0 for r = 1
 };
 
@@ -65,41 +65,27 @@ chunk_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUte
 }
 
 // ---------------------------------------------------------------------------------------------- chunks of more than 16 rows
-// Two tiles of 128 rows a block on tcgen05, 128 keys a step.  A row tile has 256 columns of tensor memory: the scores of a step,
-// over which the weights are written back as bfloat16, and O.  Four warps a row tile: one row a thread (maximum, exponentials, sums),
-// its 128 scores in registers, which two more warpgroups' worth of registers pays for (setmaxnreg).  One warp a row tile issues its
-// products; while one tile's scores are weighed the other's products run.  The weights leave in two halves, so that the second
-// product starts while the second half is computed.  Keys and values come through the page table into a ring of slots, as TMA
-// boxes where pages divide 128 keys into parts of at least eight rows or are whole tiles, piece by piece otherwise.
+// A tile of 128 rows a block on tcgen05, 64 keys a step.  Scores go into one of two 64-column buffers of tensor memory, the weights
+// back over them as bfloat16 (32 columns), O += P V is accumulated in tensor memory.  Four warps have one row a thread (maximum,
+// exponentials, sums).  Two warps issue the products, one the scores and one the values: the scores of the next step are there when the
+// weights of this one leave.  Two warps copy keys and values through the page table into a ring of slots, as TMA boxes where pages
+// divide 64 keys into parts of at least eight rows or are whole tiles, piece by piece otherwise.  Two blocks share a
+// multiprocessor, so that one's start (lookups, queries) and end run under the other's products.
 //
-// One rounding of the weights to bfloat16 (2^-9 of each on average of the largest half step 2^-8) is as large as the output's own;
-// a second part would be a third of the products.
-constexpr int kKeys = 64, kWideRows = 256, kWideThreads = 448, kCopiers = 64, kMostSegment = 65536;
-
-// For one thread of a warp, the same one throughout.
-__device__ __forceinline__ bool one_lane() {
-    uint32_t r;
-    asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\nselp.u32 %0, 1, 0, e;\n}" : "=r"(r));
-    return r != 0;
-}
-
-__device__ __forceinline__ void issue_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-
-__device__ __forceinline__ void issue_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, int add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"(add) : "memory");
-}
-
-__device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, int add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"(add) : "memory");
-}
+// One rounding of the weights to bfloat16, at most 2^-8 of each, is as large as the output's own; a second part would be half as many
+// value products again.
+//
+// Bound by shared memory: a step's scores read 48 KB (queries and keys), its values 16, its copies write 32, for two blocks 192 KB or 1500
+// cycles of 128 bytes, against 1024 cycles of products and 1024 of exponentials.  Measured (32 heads on 8 key heads of 128): 7 prompts of up to
+// 4096 tokens 375 us for 321 GFLOP (0.52 of the bf16 rate), 1000 tokens behind 32768 463 us for 477 GFLOP (0.62), 64 chunks of up to 8 tokens
+// behind 4096 160 us (0.77 of the copy bandwidth).  Not kept: two row tiles a block that share their keys, one block a multiprocessor
+// (377, 488 us, and 216 for the chunks of drafts: nothing runs under a block's start and end); 128 keys a step into a single
+// buffer (467, 516: scores, weights and values in turn, some 250 cycles at every barrier); a quarter of the exponentials by polynomial (no change).
+constexpr int kKeys = 64, kRows = 128, kWideThreads = 256, kCopiers = 64, kMostSegment = 65536;
 
 template <int D> struct WideShape {
-    static constexpr int kSlot = kKeys * D * 2, kSlots = 8, kQ = 128 * D * 2;
-    static constexpr int kBytes = 2 * kQ + kSlots * kSlot + 1024;      // + alignment
+    static constexpr int kSlot = kKeys * D * 2, kSlots = D == 128 ? 4 : 8, kQ = kRows * D * 2;
+    static constexpr int kBytes = kQ + kSlots * kSlot + 1024;          // + alignment
 };
 
 struct WideTile {
@@ -113,7 +99,7 @@ struct WideTile {
 __device__ __forceinline__ WideTile wide_tile(const ChunkParams& C, int slot, int lane) {
     WideTile t;
     t.b = -1;
-    auto tiles_of = [&](const Chunk& c) { return (int)(((int64_t)c.count * C.a.r + kWideRows - 1) / kWideRows); };
+    auto tiles_of = [&](const Chunk& c) { return (int)(((int64_t)c.count * C.a.r + kRows - 1) / kRows); };
     if (C.seqs <= 128) {
         Chunk c[4];
         int n[4], most = 0;
@@ -152,11 +138,11 @@ __device__ __forceinline__ WideTile wide_tile(const ChunkParams& C, int slot, in
             }
             rank -= __popc(some);
         }
-        t.first_row = lo * kWideRows;
+        t.first_row = lo * kRows;
     } else {
-        // trajectory b's tiles start at slot floor(offset_b r / 256) + b: at least as many slots as tiles for any sizes
+        // trajectory b's tiles start at slot floor(offset_b r / kRows) + b: at least as many slots as tiles for any sizes
         int lo = 0, hi = C.seqs - 1;
-        auto first_slot = [&](int b) { return (int)((int64_t)clamp_to(C.offsets[b], 0, C.a.B) * C.a.r / kWideRows) + b; };
+        auto first_slot = [&](int b) { return (int)((int64_t)clamp_to(C.offsets[b], 0, C.a.B) * C.a.r / kRows) + b; };
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (first_slot(mid) <= slot) lo = mid; else hi = mid - 1;
@@ -165,14 +151,14 @@ __device__ __forceinline__ WideTile wide_tile(const ChunkParams& C, int slot, in
         const int at = slot - first_slot(lo), n = tiles_of(t.c);
         if (at < 0 || at >= n) return t;
         t.b = lo;
-        t.first_row = (n - 1 - at) * kWideRows;
+        t.first_row = (n - 1 - at) * kRows;
     }
     t.held = max(t.c.start + t.c.all, 0);
     return t;
 }
 
 template <int D, bool TMA>
-__global__ void __launch_bounds__(kWideThreads, 1)
+__global__ void __launch_bounds__(kWideThreads, 2)
 wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     typedef WideShape<D> Shape;
     constexpr int kSlots = Shape::kSlots, kPieces = D / 8;
@@ -180,29 +166,28 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
     constexpr uint32_t kValues = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 16 | (D >> 3) << 17 | (128 >> 4) << 24;      // V: keys by rows
     extern __shared__ char raw[];
     __shared__ int ids[kMaxIds + kKeys + 8];
-    __shared__ __align__(8) uint64_t bars[2 * kSlots + 15];
+    __shared__ __align__(8) uint64_t bars[2 * kSlots + 8];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up, missing_any;
     __shared__ WideTile which;
     const AttnParams& P = C.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t q_at = (smem_at(raw) + 1023) & ~1023u, ring = q_at + 2 * Shape::kQ;
+    const uint32_t q_at = (smem_at(raw) + 1023) & ~1023u, ring = q_at + Shape::kQ;
     const uint32_t full = smem_at(bars), empty = full + 8 * kSlots, drained = empty + 8 * kSlots;
-    const uint32_t s_full = drained + 8, p_full = s_full + 32, o_done = p_full + 32;      // two a row tile, taken in turn
-    const uint32_t q_full = o_done + 32;                          // one a row tile
+    const uint32_t s_full = drained + 8, p_full = s_full + 16, o_done = p_full + 16, q_full = o_done + 16;      // two each, taken in turn
     const int kv_head = (int)(blockIdx.x / C.slots) % P.Hk, seg = (int)(blockIdx.x / C.slots) / P.Hk;
     if (warp == 0) {
         const WideTile w = wide_tile(C, (int)(blockIdx.x % C.slots), lane);
         if (lane == 0) which = w;
-    } else if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_at)), "n"(512) : "memory");
+    } else if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_at)), "n"(256) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     } else if (tid == 32) {
         gave_up = missing_any = 0;
-        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kCopiers); bar_init(empty + 8 * i, 2); }
-        for (int i = 0; i < 4; ++i) { bar_init(s_full + 8 * i, 1); bar_init(p_full + 8 * i, 128); bar_init(o_done + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) bar_init(q_full + 8 * i, 128);
-        bar_init(drained, 4);
+        for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kCopiers); bar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(p_full + 8 * i, 128); bar_init(o_done + 8 * i, 1); }
+        bar_init(q_full, 128);
+        bar_init(drained, 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     fence_before();
@@ -212,30 +197,26 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
     const int b = which.b, first_row = which.first_row, held = which.held;
     const Chunk c = which.c;
     const int rows = c.count * P.r;
-    const int begin = seg * P.own_seg, end = b < 0 ? begin : min(begin + P.own_seg, keys_of(C, c, min(first_row + kWideRows, rows)));
+    const int begin = seg * P.own_seg, end = b < 0 ? begin : min(begin + P.own_seg, keys_of(C, c, min(first_row + kRows, rows)));
     const bool whole_row = P.own_segs <= 1;                       // outputs leave at once, not as parts to be joined
-    const int row_tiles = rows - first_row > 128 ? 2 : 1, tiles = divide_up_device(end - begin, kKeys);
+    const int tiles = divide_up_device(end - begin, kKeys);
     const int offset = begin % P.page;
     // the block's rows, counted from its first: tokens and heads
     const int token0 = first_row / P.r, head0 = first_row % P.r;
     auto token_of = [&](int k) { return C.r_mul != 0 ? (int)__umulhi((uint32_t)(head0 + k), C.r_mul) : k; };      // from token0 on; (r + 256) r < 2^32
-    // keys that row tile rt sees, in this segment
-    auto sees_of = [&](int rt) { return clamp_to(keys_of(C, c, min(first_row + (rt + 1) * 128, rows)) - begin, 0, end - begin); };
     if (begin >= end) {
         if (b >= 0 && whole_row && seg == 0)
-            for (int i = tid; i < min(kWideRows, rows - first_row) * (P.d / 8); i += kWideThreads) {
+            for (int i = tid; i < min(kRows, rows - first_row) * (P.d / 8); i += kWideThreads) {
                 const int row = first_row + i / (P.d / 8);
                 const int64_t at = (int64_t)(c.first + row / P.r) * P.H + kv_head * P.r + row % P.r;
                 *reinterpret_cast<uint4*>(P.out + at * P.d + i % (P.d / 8) * 8) = make_uint4(0, 0, 0, 0);
                 if (i % (P.d / 8) == 0 && P.lse != nullptr) P.lse[at] = -INFINITY;
             }
     } else
-    if (warp < 8) {
-        const int rt = warp >> 2, row = first_row + warp * 32 + lane;
-        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + rt * 256, o_at = mine + 128;
-        const uint32_t my_s = s_full + 16 * rt, my_p = p_full + 16 * rt, my_o = o_done + 16 * rt;
+    if (warp < 4) {
+        const int row = first_row + warp * 32 + lane;
+        const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16), o_at = mine + 128;
         const bool any_row = first_row + warp * 32 < rows;
-        const int n = rt < row_tiles ? divide_up_device(sees_of(rt), kKeys) : 0;
         const int lim = row < rows ? clamp_to(min(c.start + row / P.r + 1, P.max_len) - begin, 0, end - begin) : end - begin;
         const int least = __reduce_min_sync(~0u, lim);
         const int64_t rows_at = (int64_t)(c.first + token0) * P.H + kv_head * P.r;      // of the outputs [T, H]
@@ -253,19 +234,19 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
             }
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
-                const int k = (warp & 3) * 32 + j * kTogether + lane / kPieces, piece = lane % kPieces;
-                const uint32_t dst = q_at + rt * Shape::kQ + (piece >> 3) * (128 * 128) + k * 128 + (((piece & 7) ^ (k & 7)) << 4);
+                const int k = warp * 32 + j * kTogether + lane / kPieces, piece = lane % kPieces;
+                const uint32_t dst = q_at + (piece >> 3) * (128 * 128) + k * 128 + (((piece & 7) ^ (k & 7)) << 4);
                 asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v[j].x), "r"(v[j].y), "r"(v[j].z), "r"(v[j].w) : "memory");
             }
             fence_async();
-            bar_arrive(q_full + 8 * rt);
+            bar_arrive(q_full);
         }
         bool missing = false;
         float m = -INFINITY, l = 0.f;
         bool fine = true;
-        for (int i = 0; i < n; ++i) {
+        for (int i = 0; i < tiles; ++i) {
             const uint32_t s_at = mine + (i & 1) * kKeys;
-            fine = __all_sync(~0u, bar_wait(my_s + 8 * (i & 1), (i >> 1) & 1, &gave_up, P.polls));
+            fine = __all_sync(~0u, bar_wait(s_full + 8 * (i & 1), (i >> 1) & 1, &gave_up, P.polls));
             if (!fine) break;
             fence_after();
             if (i == 0) missing = *(volatile int*)&missing_any != 0;      // written before the first key was fetched
@@ -292,7 +273,7 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                 if (__any_sync(~0u, now > m + 8.f)) {
                     const float next = fmaxf(m, now), fade = m == -INFINITY ? 0.f : exp2_of(m - next);
                     if (i > 0) {
-                        fine = __all_sync(~0u, bar_wait(my_o + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, &gave_up, P.polls));
+                        fine = __all_sync(~0u, bar_wait(o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, &gave_up, P.polls));
                         if (!fine) break;
                         fence_after();
 #pragma unroll
@@ -327,18 +308,18 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                 tmem_wait_store();
             }
             fence_before();
-            bar_arrive(my_p + 8 * (i & 1));
+            bar_arrive(p_full + 8 * (i & 1));
         }
-        if (any_row && rt < row_tiles) {
-            for (int i = max(n - 2, 0); i < n && fine; ++i)
-                fine = __all_sync(~0u, bar_wait(my_o + 8 * (i & 1), (i >> 1) & 1, &gave_up, P.polls));
+        if (any_row) {
+            for (int i = max(tiles - 2, 0); i < tiles && fine; ++i)
+                fine = __all_sync(~0u, bar_wait(o_done + 8 * (i & 1), (i >> 1) & 1, &gave_up, P.polls));
             fine = fine && *(volatile int*)&gave_up == 0;         // a thread that copies may have given up alone
             fence_after();
             if (!fine) l = __int_as_float(0x7fffffff);
             const float inv = l != 0.f ? 1.f / l : 0.f;
-            // rows leave through the place of the warp's queries, which are done with (nothing was multiplied if n is 0): 256 bytes of a row at a
+            // rows leave through the place of the warp's queries, which are done with256 bytes of a row at a
             // time, written by the row's thread, stored by sixteen lanes a row
-            const uint32_t mine_at = q_at + rt * Shape::kQ + (warp & 3) * (Shape::kQ / 4);
+            const uint32_t mine_at = q_at + warp * (Shape::kQ / 4);
             constexpr int kRound = D == 128 ? 16 : 8;                 // 16-byte pieces of a row a round: D values of 16 bits, D / 2 of 32
             char* const parts = reinterpret_cast<char*>(P.part_o + (int64_t)seg * P.B * P.H * D);
             const int rounds = whole_row ? 1 : 2;
@@ -348,13 +329,8 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                 for (int k = 0; k < D; k += 32) {
                     if (!whole_row && k / (D / 2) != round) continue;
                     uint32_t o[32];
-                    if (n > 0) {
-                        tmem_load32(o, o_at + k);
-                        tmem_wait_load();
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0;
-                    }
+                    tmem_load32(o, o_at + k);
+                    tmem_wait_load();
                     auto put = [&](int piece, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
                         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(mine_at + lane * (kRound * 16) + ((piece ^ (lane & (kRound - 1))) << 4)), "r"(x),
                                      "r"(y), "r"(z), "r"(w) : "memory");
@@ -393,22 +369,22 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
         }
         fence_before();
     } else {
-        // page numbers of the keys, by the six warps that are left; -1: no such page
+        // page numbers of the keys, by the four warps that are left; -1: no such page
         {
             const int32_t* table = P.block_table + (int64_t)b * P.own_width;
             const int first = begin / P.page, count = (min(begin + tiles * kKeys, held) - 1) / P.page - first + 1;
             bool some = false;
 #pragma unroll 4
-            for (int i = tid - 256; i < count; i += kWideThreads - 256) {
+            for (int i = tid - 128; i < count; i += 128) {
                 int id = first + i < P.own_width ? table[first + i] : -1;
                 if (id < 0 || id >= P.pages) { id = -1; some = true; }
                 ids[i] = id;
             }
             if (some) missing_any = 1;
-            asm volatile("bar.sync 2, %0;" ::"n"(kWideThreads - 256) : "memory");
+            asm volatile("bar.sync 2, %0;" ::"n"(128) : "memory");
         }
-        if (warp == 8 || warp == 13) {
-            const int me = (warp == 8 ? 0 : 32) + lane, piece = me % kPieces, row0 = me / kPieces;
+        if (warp == 4 || warp == 7) {
+            const int me = (warp == 4 ? 0 : 32) + lane, piece = me % kPieces, row0 = me / kPieces;
             constexpr int kStep = kCopiers / kPieces, kRows = kKeys / kStep;
             const uint32_t lane_at = ring + (piece >> 3) * (kKeys * 128);
             auto pieces = [&](int item) {                         // one tile of keys or values, zeros where there is no key
@@ -477,35 +453,28 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
         } else {
-            const int rt = (warp - 9) >> 1;
-            const uint32_t base = __shfl_sync(~0u, tmem, 0) + rt * 256;
-            const uint32_t my_s = s_full + 16 * rt, my_p = p_full + 16 * rt, my_o = o_done + 16 * rt;
-            const int n = rt < row_tiles ? divide_up_device(sees_of(rt), kKeys) : 0;
+            const uint32_t base = __shfl_sync(~0u, tmem, 0);
             if (one_lane()) {
                 auto wait = [&](uint32_t bar, int parity) { return bar_wait(bar, parity & 1, &gave_up, P.polls); };
                 bool fine = true;
-                if (((warp - 9) & 1) == 0) {
-                    const uint64_t q_desc = describe(q_at + rt * Shape::kQ, 16), k_desc = describe(ring, 16);
-                    fine = wait(q_full + 8 * rt, 0) && fine;
+                if (warp == 5) {
+                    const uint64_t q_desc = describe(q_at, 16), k_desc = describe(ring, 16);
+                    fine = wait(q_full, 0);
                     for (int i = 0; i < tiles && fine; ++i) {
                         const int item = 2 * i, slot = item % kSlots;
                         fine = wait(full + 8 * slot, item / kSlots);
                         if (!fine) break;
-                        if (i < n) {
-                            // the buffer's weights must have been multiplied before new scores go there
-                            fine = i < 2 || wait(my_o + 8 * (i & 1), (i - 2) >> 1);
-                            if (!fine) break;
-                            fence_after();
-                            const uint64_t k_at = k_desc + slot * (Shape::kSlot >> 4);
+                        // the buffer's weights must have been multiplied before new scores go there
+                        fine = i < 2 || wait(o_done + 8 * (i & 1), (i - 2) >> 1);
+                        if (!fine) break;
+                        fence_after();
+                        const uint64_t k_at = k_desc + slot * (Shape::kSlot >> 4);
 #pragma unroll
-                            for (int s = 0; s < D / 16; ++s)
-                                issue_ss(base + (i & 1) * kKeys, q_desc + (((s >> 2) * (128 * 128) + (s & 3) * 32) >> 4),
-                                         k_at + (((s >> 2) * (kKeys * 128) + (s & 3) * 32) >> 4), kScores, s > 0);
-                            issue_commit(my_s + 8 * (i & 1));
-                            issue_commit(empty + 8 * slot);
-                        } else {
-                            bar_arrive(empty + 8 * slot);
-                        }
+                        for (int s = 0; s < D / 16; ++s)
+                            issue_ss(base + (i & 1) * kKeys, q_desc + (((s >> 2) * (128 * 128) + (s & 3) * 32) >> 4),
+                                     k_at + (((s >> 2) * (kKeys * 128) + (s & 3) * 32) >> 4), kScores, s > 0);
+                        issue_commit(s_full + 8 * (i & 1));
+                        issue_commit(empty + 8 * slot);
                     }
                 } else {
                     const uint64_t v_desc = describe(ring, kKeys * 128);
@@ -513,19 +482,15 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                         const int item = 2 * i + 1, slot = item % kSlots;
                         fine = wait(full + 8 * slot, item / kSlots);
                         if (!fine) break;
-                        if (i < n) {
-                            fine = wait(my_p + 8 * (i & 1), i >> 1);
-                            if (!fine) break;
-                            fence_after();
-                            const uint64_t v_at = v_desc + slot * (Shape::kSlot >> 4);
+                        fine = wait(p_full + 8 * (i & 1), i >> 1);
+                        if (!fine) break;
+                        fence_after();
+                        const uint64_t v_at = v_desc + slot * (Shape::kSlot >> 4);
 #pragma unroll
-                            for (int s = 0; s < kKeys / 16; ++s)
-                                issue_ts(base + 128, base + (i & 1) * kKeys + s * 8, v_at + ((s * 2048) >> 4), kValues, i > 0 || s > 0);
-                            issue_commit(my_o + 8 * (i & 1));
-                            issue_commit(empty + 8 * slot);
-                        } else {
-                            bar_arrive(empty + 8 * slot);
-                        }
+                        for (int s = 0; s < kKeys / 16; ++s)
+                            issue_ts(base + 128, base + (i & 1) * kKeys + s * 8, v_at + ((s * 2048) >> 4), kValues, i > 0 || s > 0);
+                        issue_commit(o_done + 8 * (i & 1));
+                        issue_commit(empty + 8 * slot);
                     }
                 }
                 issue_commit(drained);                            // nothing in flight when the memory is given back
@@ -536,9 +501,9 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
     }
     __syncwarp();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == 5) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(256) : "memory");
     }
 }
 
@@ -578,16 +543,16 @@ __global__ void __launch_bounds__(kThreads) chunk_join_kernel(const __grid_const
     if (lane == 0 && P.lse != nullptr) P.lse[at] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Blocks of 256 rows: whole rows while there are two blocks a multiprocessor or more, else the number of segments that makes the
-// rounds of blocks shortest, a segment costing three tiles beyond its own (start, first loads, the partial result).
-int plan_wide(int64_t longest, int64_t units, int page, int64_t sms) {
+// Wide blocks run `slots` at once: whole rows while there are two rounds of blocks or more, else the number of segments that makes
+// the rounds shortest, a segment costing about eight steps beyond its own (start, first loads, the partial result and its joining).
+int plan_wide(int64_t longest, int64_t units, int page, int64_t slots) {
     const int64_t by_ids = (int64_t)(kMaxIds - 2) * page / kKeys * kKeys, most = (by_ids < kMostSegment ? by_ids : kMostSegment) / kKeys;
     const int64_t tiles = divide_up(longest > 0 ? longest : 1, kKeys);
     int64_t best = most, cost = INT64_MAX;
     for (int64_t segs = divide_up(tiles, most); segs <= tiles && segs <= 256; ++segs) {
-        const int64_t per = divide_up(tiles, segs), c = divide_up(units * segs, sms) * (per + 3);
+        const int64_t per = divide_up(tiles, segs), c = divide_up(units * segs, slots) * (per + 8);
         if (c < cost) { cost = c; best = per; }
-        if (units >= 2 * sms) break;
+        if (units >= 2 * slots) break;
     }
     return (int)(best * kKeys);
 }
@@ -617,10 +582,9 @@ int check_shape(ChunkParams& C, int64_t T, int64_t seqs, int64_t H, int64_t Hk, 
         C.tiles = 1;
         P.own_seg = plan_segment(P.max_len, Hk * seqs, P.page, 1024);
     } else {
-        const int64_t rows = T * P.r;
-        C.slots = (int)(rows / kWideRows + seqs);
-        const int64_t some = seqs < T ? seqs : T, units = rows / kWideRows + (some + 1) / 2;
-        P.own_seg = plan_wide(P.max_len, Hk * (units > some ? units : some), P.page, rlcs_device::limits().sms);
+        const int64_t rows = T * P.r, some = seqs < T ? seqs : T, units = rows / kRows + (some + 1) / 2;
+        C.slots = (int)(rows / kRows + seqs);
+        P.own_seg = plan_wide(P.max_len, Hk * (units > some ? units : some), P.page, rlcs_device::limits().sms * 2);
     }
     P.own_segs = divide_up(P.max_len, P.own_seg);
     if ((double)(C.tiles > 0 ? seqs : C.slots) * Hk * (P.own_segs > 0 ? P.own_segs : 1) > 2147483647.0 || T * H > (int64_t(1) << 32)) return RLCS_ERR_SIZE;
