@@ -83,6 +83,28 @@ chunk_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUte
 // buffer (467, 516: scores, weights and values in turn, some 250 cycles at every barrier); a quarter of the exponentials by polynomial (no change).
 constexpr int kKeys = 64, kRows = 128, kWideThreads = 256, kCopiers = 64, kMostSegment = 65536;
 
+// Products and commits are issued by one thread of a warp: elected once, it waits and issues by itself, which takes a third of the
+// time at each barrier that a whole warp with an election an instruction takes.
+__device__ __forceinline__ bool one_lane() {
+    uint32_t r;
+    asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\nselp.u32 %0, 1, 0, e;\n}" : "=r"(r));
+    return r != 0;
+}
+
+__device__ __forceinline__ void issue_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void issue_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, int add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"(add) : "memory");
+}
+
+__device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, int add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"(add) : "memory");
+}
+
 template <int D> struct WideShape {
     static constexpr int kSlot = kKeys * D * 2, kSlots = D == 128 ? 4 : 8, kQ = kRows * D * 2;
     static constexpr int kBytes = kQ + kSlots * kSlot + 1024;          // + alignment
