@@ -7,25 +7,33 @@
 // All choices go by whole weights w_j = floor(2^31 exp((l_j - max) / T) + 1/2), as action sampling's do: their sums are exact, so that
 // neither verdict nor draw depends on how a row is split over threads.  A difference of two distributions is taken in units of
 // 2^-40: floor(w_j 2^40 / W) - floor(v_j 2^40 / V).
+//
+// Two kernels.  The first reads every row once, at the rate of the memory, and leaves its maximum and the sum of its exponentials
+// (the hardware's, summed in fp32 over 32 and in 64 bits beyond: within 2^-15 of the whole weights' sum, but for one half a weight).  The
+// second has a cluster a trajectory.  A draft whose verdict is the same anywhere within those bounds, nearly every one, needs no
+// more; another row's weights are summed up exactly, and so are those of the row from which the next token is drawn.
+#include <cooperative_groups.h>
+
 #include <cmath>
 #include <cstdint>
 
 #include "../../include/rlcs.h"
 #include "rlcs_device.cuh"
+#include "rlcs_pair.cuh"
 #include "rlcs_weights.cuh"
 
 namespace {
 
+namespace cg = cooperative_groups;
+using namespace rlcs_pair;
 using namespace rlcs_rows;
 
 constexpr double kShareOne = 0x1p40;      // a probability of 1 in a difference
 
-// What is known of a row of logits: maximum and its first place, whole and plain sums of the exponentials, the drafted token's weight.
-struct RowStat {
-    u64 sum;
+// A part of a row of logits: its maximum, the first place that has it, the sum of exp((l - top) / T).
+struct PartStat {
     double all;
-    float top, drafted;                   // drafted: the token's logit
-    uint32_t weight;
+    float top;
     int32_t best;
 };
 
@@ -41,194 +49,404 @@ template <typename T> struct VerifyParams {
     int32_t* out;
     float* log_probs;
     int32_t* accepted;
-    RowStat* stats;                       // [2][T]: of the target's rows, of the draft policy's
+    PartStat* stats;                      // [2][rows][parts]: of the target's rows, of the draft policy's
     int64_t ld, ldd;
-    int32_t rows, seqs, A;
+    int32_t rows, seqs, A, parts;
+    int32_t share;                        // entries of a row that a block of the second kernel has
 };
 
-constexpr int kThreads = 512;
+template <typename T> __device__ __forceinline__ float temperature_of(const VerifyParams<T>& P, int b) {
+    return P.temperature != nullptr ? P.temperature[b] : P.temperature_all;
+}
 
-// The trajectory that row t belongs to, -1 where there is none; the rows [begin, end) of it.
-template <typename T> __device__ __forceinline__ int seq_of(const VerifyParams<T>& P, int t, int* begin, int* end) {
-    int lo = 0, hi = P.seqs - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (P.offsets[mid] <= t) lo = mid; else hi = mid - 1;
+// exp((x - top) / T) as the weights are made of it; NaN, and what an infinite temperature makes of -inf, count nothing.
+__device__ __forceinline__ float e_of(float x, float top, float inv) {
+    const float e = expf(scaled(clean(x), top, inv));
+    return e >= 0.f ? e : 0.f;
+}
+
+// The trajectory that row t belongs to, by a whole warp; -1 where there is none.  [begin, end): its rows.
+template <typename T> __device__ __forceinline__ int seq_of(const VerifyParams<T>& P, int t, int lane, int* begin, int* end) {
+    int lo = 0, n = P.seqs;                                  // the last trajectory that starts at or before t
+    while (n > 1) {
+        const int step = (n + 31) / 32, at = lo + lane * step;
+        const unsigned some = __ballot_sync(~0u, lane * step < n && P.offsets[at] <= t);
+        const int last = some == 0 ? 0 : 31 - __clz(some);
+        n = min(step, n - last * step);
+        lo += last * step;
     }
     *begin = max(P.offsets[lo], 0);
     *end = min(P.offsets[lo + 1], P.rows);
     return t >= *begin && t < *end ? lo : -1;
 }
 
-template <typename T> __device__ __forceinline__ float temperature_of(const VerifyParams<T>& P, int b) {
-    return P.temperature != nullptr ? P.temperature[b] : P.temperature_all;
-}
+// ---------------------------------------------------------------------------------------------- every row once
+// G threads a row (a warp, eight rows a block; or the block), which may be one of P.parts of it.
+constexpr int kScan = 256, kAhead = 4;       // threads; 16-byte vectors of a row that a thread has at a time
 
-template <typename V> __device__ __forceinline__ V block_total(V v) {
-    __shared__ V part[kThreads / 32];
-    v = warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    V all = 0;
-    for (int k = 0; k < kThreads / 32; ++k) all += part[k];
-    return all;
-}
-
-// One block a row: target rows first, then the draft policy's.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) verify_rows_kernel(const __grid_constant__ VerifyParams<T> P) {
-    const int t = blockIdx.x % P.rows, which = blockIdx.x / P.rows, tid = threadIdx.x;
+template <typename T, int G>
+__global__ void __launch_bounds__(kScan) verify_scan_kernel(const __grid_constant__ VerifyParams<T> P) {
+    constexpr int N = Vec<T>::N;
+    __shared__ double sums[kScan / 32];
+    __shared__ float tops[kScan / 32];
+    __shared__ int bests[kScan / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, me = tid % G;
+    const int64_t item = G == 32 ? (int64_t)blockIdx.x * (kScan / 32) + warp : blockIdx.x;
+    const int part = (int)(item % P.parts);
+    const int64_t row = item / P.parts;
+    const int which = row >= P.rows ? 1 : 0, t = (int)(row - (which ? P.rows : 0));
+    if (t >= P.rows || (which == 1 && P.drafts == nullptr)) return;      // warps of the last block
     int begin, end;
-    const int b = seq_of(P, t, &begin, &end);
-    if (b < 0 || (which == 1 && t + 1 == end)) return;
+    const int b = seq_of(P, t, lane, &begin, &end);
+    const float temperature = b >= 0 ? temperature_of(P, b) : 0.f;
+    if (b < 0 || (which == 1 && (t + 1 == end || !(temperature > 0.f)))) return;
+    const float inv = inverse_of(temperature), k = inv * 1.4426950408889634f;
     const T* x = which ? P.drafts + t * P.ldd : P.logits + t * P.ld;
-    const float inv = inverse_of(temperature_of(P, b));
-    __shared__ u64 best;
-    if (tid == 0) best = 0;
+    const Span sp = span_of(x, P.A);
+    const int per = (sp.vecs + P.parts - 1) / P.parts, v0 = min(part * per, sp.vecs), n = min(per, sp.vecs - v0);
+    const int rest = sp.head + sp.vecs * N, singles = part == 0 ? sp.head + P.A - rest : 0;      // before and behind the vectors
+    const uint4* body = reinterpret_cast<const uint4*>(x + sp.head) + v0;
+    auto single = [&](int i) { return i < sp.head ? i : rest + i - sp.head; };
+
     float m = -INFINITY;
-    int at = P.A;
-    for (int j = tid; j < P.A; j += kThreads) {
-        const float f = clean(Vec<T>::load(x + j));
-        if (f > m) { m = f; at = j; }
-    }
-    __syncthreads();
-    // the largest, and of equals the first: a key that grows with the value and falls with the place
-    const uint32_t u = __float_as_uint(m), key = u ^ (((int32_t)u >> 31) | 0x80000000u);
-    atomicMax(&best, (u64)key << 32 | (uint32_t)(~at));
-    __syncthreads();
-    const uint32_t top_key = (uint32_t)(best >> 32), bits = top_key & 0x80000000u ? top_key ^ 0x80000000u : ~top_key;
-    const float top = __uint_as_float(bits);
-    u64 sum = 0;
     double all = 0.;
-    if (top != -INFINITY)
-        for (int j = tid; j < P.A; j += kThreads) {
-            const float e = expf(scaled(clean(Vec<T>::load(x + j)), top, inv));
-            sum += weight_of(e);
-            all += (double)e;
+    int chunk = -1;                                          // where the thread's maximum came first: a chunk of vectors, or -2 - a single
+    for (int i = me; i < singles; i += G) {
+        const float f = Vec<T>::load(x + single(i));
+        if (f > m) {
+            all = all * (double)exp2_of((m - f) * k);
+            m = f;
+            chunk = -2 - i;
         }
-    sum = block_total(sum);
-    all = block_total(all);
-    if (tid != 0) return;
-    const int token = t + 1 < end ? P.tokens[t + 1] : -1;
-    RowStat s = {sum, all, top, 0.f, 0u, (int32_t)~(uint32_t)best};
-    if (token >= 0 && token < P.A && top != -INFINITY) {
-        s.drafted = clean(Vec<T>::load(x + token));
-        s.weight = weight_of(expf(scaled(s.drafted, top, inv)));
+        if (m != -INFINITY) all += (double)exp2_of((f - m) * k);
     }
-    P.stats[(int64_t)which * P.rows + t] = s;
+    auto take = [&](int c, auto whole) {
+        uint4 v[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int i = (c * kAhead + q) * G + me;
+            v[q] = whole() || i < n ? __ldcs(body + i) : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+        }
+        uint32_t most = Vec<T>::kNothing;
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            most = Vec<T>::most_number(most, Vec<T>::most_number(Vec<T>::most_number(v[q].x, v[q].y), Vec<T>::most_number(v[q].z, v[q].w)));
+        const float top = Vec<T>::most_number_of(most);
+        if (top > m || (top == m && chunk < -1)) {           // of equals a vector's place, unless a single's comes before: below
+            all = m == -INFINITY ? 0. : all * (double)exp2_of((m - top) * k);
+            m = top;
+            chunk = c;
+        }
+        if (m == -INFINITY) return;
+        const float2 less = {-m, -m}, scale = {k, k};
+        float2 s[2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            float f[N];
+            Vec<T>::unpack(v[q], f);
+#pragma unroll
+            for (int j = 0; j < N; j += 2) {
+                const float2 d = mul2(add2(make_float2(f[j], f[j + 1]), less), scale);
+                s[j >> 1 & 1] = add2(s[j >> 1 & 1], make_float2(exp2_of(d.x), exp2_of(d.y)));
+            }
+        }
+        all += (double)((s[0].x + s[1].x) + (s[0].y + s[1].y));
+    };
+    int c = 0;
+    for (; (c + 1) * kAhead * G <= n; ++c) take(c, [] { return true; });
+    if (c * kAhead * G < n) take(c, [] { return false; });
+
+    // the row's maximum, and the first place that has it
+    float top = m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    if (G > 32) {
+        if (lane == 0) tops[warp] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < G / 32; ++w) top = fmaxf(top, tops[w]);
+    }
+    int best = P.A;
+    if (m == top && top != -INFINITY) {
+        if (chunk < 0) {
+            best = single(-2 - chunk);
+        } else {
+            for (int q = kAhead - 1; q >= 0; --q) {
+                const int i = (chunk * kAhead + q) * G + me;
+                for (int j = N - 1; j >= 0; --j)
+                    if (i < n && Vec<T>::load(x + sp.head + (int64_t)(v0 + i) * N + j) == top) best = sp.head + (v0 + i) * N + j;
+            }
+        }
+        for (int i = me; i < singles; i += G)                // a place among the singles may come before the chunk's
+            if (Vec<T>::load(x + single(i)) == top) { best = min(best, single(i)); break; }
+    }
+    best = __reduce_min_sync(~0u, best);
+    if (m != top) all = m == -INFINITY ? 0. : all * (double)exp2_of((m - top) * k);
+    all = warp_sum(all);
+    if (G > 32) {
+        if (lane == 0) { sums[warp] = all; bests[warp] = best; }
+        __syncthreads();
+        all = 0.;
+#pragma unroll
+        for (int w = 0; w < G / 32; ++w) { all += sums[w]; best = min(best, bests[w]); }
+    }
+    if (!(all == all) || all > 1e300) {                      // NaN or +inf in the row, or a temperature next to 0 or infinite
+        double sum = 0.;
+        for (int i = me; i < n; i += G)
+            for (int j = 0; j < N; ++j) sum += (double)e_of(Vec<T>::load(x + sp.head + (int64_t)(v0 + i) * N + j), top, inv);
+        for (int i = me; i < singles; i += G) sum += (double)e_of(Vec<T>::load(x + single(i)), top, inv);
+        all = warp_sum(sum);
+        if (G > 32) {
+            __syncthreads();
+            if (lane == 0) sums[warp] = all;
+            __syncthreads();
+            all = 0.;
+            for (int w = 0; w < G / 32; ++w) all += sums[w];
+        }
+    }
+    if (me == 0) P.stats[row * P.parts + part] = PartStat{top == -INFINITY ? 0. : all, top, best};
 }
 
-template <typename T> __device__ __forceinline__ bool stays(const VerifyParams<T>& P, int t, bool greedy) {
-    const RowStat& p = P.stats[t];
-    const int token = P.tokens[t + 1];
-    if (token < 0 || token >= P.A || p.sum == 0) return false;
-    if (greedy) return token == p.best;
-    double v = 1., V = 1.;
-    if (P.drafts != nullptr) {
-        const RowStat& q = P.stats[P.rows + t];
-        v = (double)q.weight;
-        V = (double)q.sum;
+// ---------------------------------------------------------------------------------------------- verdict and draw
+struct RowStat {
+    double all;
+    float top;
+    int32_t best;
+};
+
+template <typename T> __device__ __forceinline__ RowStat join_parts(const VerifyParams<T>& P, int64_t row, float inv) {
+    const PartStat* s = P.stats + row * P.parts;
+    RowStat r = {0., -INFINITY, P.A};
+    for (int i = 0; i < P.parts; ++i)
+        if (s[i].top > r.top || (s[i].top == r.top && s[i].best < r.best)) { r.top = s[i].top; r.best = s[i].best; }
+    if (r.top == -INFINITY) return r;
+    for (int i = 0; i < P.parts; ++i) {
+        const float d = scaled(s[i].top, r.top, inv);
+        if (s[i].top != -INFINITY && d == d) r.all += s[i].all * exp((double)d);
     }
-    return (double)P.uniforms[t] * (v * (double)p.sum) < (double)p.weight * V;
+    return r;
 }
 
-// One block a trajectory: its verdict, and the token after the kept ones.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// NT threads a block, a cluster a trajectory.  HELD: a block's weights of both rows stay in shared memory (share entries each).
+template <typename T, int NT, bool HELD>
+__global__ void __launch_bounds__(NT) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
+    extern __shared__ uint32_t held[];                       // [2][share]
+    __shared__ u64 part[2][NT / 32], sent[2][16][2];
+    __shared__ int stop;                                     // least 2 t + 1 of a row whose draft does not stay, 2 t where that is unclear
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int b = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int begin = max(P.offsets[b], 0), end = min(P.offsets[b + 1], P.rows);
-    if (begin >= end) {
-        if (tid == 0) P.accepted[b] = 0;
+    if (begin >= end) {                                      // for all of the cluster alike
+        if (rank == 0 && tid == 0) P.accepted[b] = 0;
         return;
     }
+    if (ranks > 1) cluster.sync();                           // all of the cluster's blocks run
     const float temperature = temperature_of(P, b), inv = inverse_of(temperature);
     const bool greedy = !(temperature > 0.f);
-    __shared__ int stop;
-    if (tid == 0) stop = end - 1;
-    __syncthreads();
-    for (int t = begin + tid; t < end - 1; t += kThreads)
-        if (!stays(P, t, greedy)) atomicMin(&stop, t);
-    __syncthreads();
-    const int r = stop;
-    auto score = [&](int t, float x) {                        // log-probability under the whole softmax
-        const RowStat& p = P.stats[t];
-        return (float)((double)scaled(x, p.top, inv) - log(p.all));
+    const int j0 = min(rank * P.share, P.A), j1 = min(j0 + P.share, P.A);
+
+    // (x, y) summed over the block, then over the cluster; two sets of places, taken in turn
+    int turns = 0;
+    auto block_sum = [&](u64* x, u64* y) {
+        *x = warp_sum(*x);
+        *y = warp_sum(*y);
+        __syncthreads();
+        if (lane == 0) { part[0][warp] = *x; part[1][warp] = *y; }
+        __syncthreads();
+        *x = *y = 0;
+        for (int w = 0; w < NT / 32; ++w) { *x += part[0][w]; *y += part[1][w]; }
     };
-    for (int t = begin + tid; t < end; t += kThreads) {
-        if (t == r) continue;
-        P.out[t] = t < r ? P.tokens[t + 1] : -1;
-        P.log_probs[t] = t < r ? score(t, P.stats[t].drafted) : -INFINITY;
+    auto cluster_sum = [&](u64* x, u64* y) {
+        block_sum(x, y);
+        if (ranks == 1) return;
+        const int turn = turns++ & 1;
+        if (tid < ranks) {
+            u64* to = cluster.map_shared_rank(&sent[turn][rank][0], tid);
+            to[0] = *x;
+            to[1] = *y;
+        }
+        cluster.sync();
+        *x = *y = 0;
+        for (int r = 0; r < ranks; ++r) { *x += sent[turn][r][0]; *y += sent[turn][r][1]; }
+    };
+    auto target_weight = [&](int t, const RowStat& p, int j) { return weight_of(e_of(Vec<T>::load(P.logits + t * P.ld + j), p.top, inv)); };
+    auto draft_weight = [&](int t, const RowStat& q, int j) { return weight_of(e_of(Vec<T>::load(P.drafts + t * P.ldd + j), q.top, inv)); };
+    // whole sums of both rows' weights (of the target's alone where `two` is false)
+    auto whole_sums = [&](int t, const RowStat& p, const RowStat& q, bool two, u64* W, u64* V) {
+        u64 x = 0, y = 0;
+        if (p.top != -INFINITY)
+            for (int j = j0 + tid; j < j1; j += NT) {
+                const uint32_t w = target_weight(t, p, j);
+                if (HELD) held[j - j0] = w;
+                x += w;
+            }
+        if (two && q.top != -INFINITY)
+            for (int j = j0 + tid; j < j1; j += NT) {
+                const uint32_t w = draft_weight(t, q, j);
+                if (HELD) held[P.share + j - j0] = w;
+                y += w;
+            }
+        cluster_sum(&x, &y);
+        *W = x;
+        *V = y;
+    };
+    // does u (v W) < w V hold?
+    auto decide = [&](int t, double w, double W, double v, double V) { return (double)P.uniforms[t] * (v * W) < w * V; };
+    auto weight_at = [&](const T* x, const RowStat& r, int token) { return r.top == -INFINITY ? 0u : weight_of(e_of(Vec<T>::load(x + token), r.top, inv)); };
+
+    int from = begin, r;
+    while (true) {
+        __syncthreads();
+        if (tid == 0) stop = 2 * (end - 1) + 1;
+        __syncthreads();
+        for (int t = from + tid; t < end - 1; t += NT) {
+            const int token = P.tokens[t + 1];
+            const RowStat p = join_parts(P, t, inv);
+            bool yes = false, no = true;
+            if (token >= 0 && token < P.A && p.top != -INFINITY) {
+                if (greedy) {
+                    yes = token == p.best;
+                } else {
+                    const double w = weight_at(P.logits + t * P.ld, p, token), slack = P.A;
+                    double v = 1., least_v = 1., most_v = 1.;
+                    if (P.drafts != nullptr) {
+                        const RowStat q = join_parts(P, (int64_t)P.rows + t, inv);
+                        v = weight_at(P.drafts + t * P.ldd, q, token);
+                        least_v = fmax(q.all * (0x1p31 * (1. - 0x1p-15)) - slack, 0.);
+                        most_v = q.all * (0x1p31 * (1. + 0x1p-15)) + slack;
+                    }
+                    const double least_w = fmax(p.all * (0x1p31 * (1. - 0x1p-15)) - slack, 0.), most_w = p.all * (0x1p31 * (1. + 0x1p-15)) + slack;
+                    // the same verdict at both ends, moved apart by more than the products' roundings
+                    yes = decide(t, w * (1. - 0x1p-40), most_w, v, least_v);
+                    no = !decide(t, w * (1. + 0x1p-40), least_w, v, most_v);
+                }
+            }
+            if (!yes) {
+                atomicMin(&stop, 2 * t + (no ? 1 : 0));
+                break;
+            }
+        }
+        __syncthreads();
+        r = stop >> 1;
+        if (stop & 1) break;
+        const int token = P.tokens[r + 1];
+        const RowStat p = join_parts(P, r, inv);
+        RowStat q = {0., -INFINITY, 0};
+        if (P.drafts != nullptr) q = join_parts(P, (int64_t)P.rows + r, inv);
+        u64 W, V;
+        whole_sums(r, p, q, P.drafts != nullptr, &W, &V);
+        const double v = P.drafts != nullptr ? weight_at(P.drafts + r * P.ldd, q, token) : 1.;
+        if (!decide(r, weight_at(P.logits + r * P.ld, p, token), (double)W, v, P.drafts != nullptr ? (double)V : 1.)) break;
+        from = r + 1;
     }
-    const RowStat p = P.stats[r];
-    if (tid == 0) P.accepted[b] = r - begin;
-    if (p.sum == 0 || greedy) {
-        if (tid == 0) {
-            P.out[r] = p.sum == 0 ? -1 : p.best;
-            P.log_probs[r] = p.sum == 0 ? -INFINITY : score(r, p.top);
+    const RowStat p = join_parts(P, r, inv);
+    auto score = [&](const RowStat& s, float x) { return (float)((double)scaled(x, s.top, inv) - log(s.all)); };      // under the whole softmax
+    if (rank == 0) {
+        for (int t = begin + tid; t < end; t += NT) {
+            if (t == r) continue;
+            P.out[t] = t < r ? P.tokens[t + 1] : -1;
+            P.log_probs[t] = t < r ? score(join_parts(P, t, inv), clean(Vec<T>::load(P.logits + t * P.ld + P.tokens[t + 1]))) : -INFINITY;
+        }
+        if (tid == 0) P.accepted[b] = r - begin;
+    }
+    if (p.top == -INFINITY || greedy) {
+        if (rank == 0 && tid == 0) {
+            P.out[r] = p.top == -INFINITY ? -1 : p.best;
+            P.log_probs[r] = p.top == -INFINITY ? -INFINITY : score(p, p.top);
         }
         return;
     }
-    const T* x = P.logits + r * P.ld;
-    const T* y = r + 1 < end && P.drafts != nullptr ? P.drafts + r * P.ldd : nullptr;
+    const bool two = r + 1 < end && P.drafts != nullptr;
     const int turned = r + 1 < end && P.drafts == nullptr ? P.tokens[r + 1] : -1;
-    RowStat q = {};
-    if (y != nullptr) q = P.stats[P.rows + r];
-    const double p_unit = kShareOne / (double)p.sum, q_unit = q.sum > 0 ? kShareOne / (double)q.sum : 0.;
-    auto weight = [&](int j, bool plain) -> u64 {
-        const uint32_t w = weight_of(expf(scaled(clean(Vec<T>::load(x + j)), p.top, inv)));
+    RowStat q = {0., -INFINITY, 0};
+    if (two) q = join_parts(P, (int64_t)P.rows + r, inv);
+    u64 W, V;
+    whole_sums(r, p, q, two, &W, &V);
+    const double p_unit = kShareOne / (double)W, q_unit = V > 0 ? kShareOne / (double)V : 0.;
+    bool plain = !two && turned < 0;
+    auto weight = [&](int j) -> u64 {
+        const uint32_t w = HELD ? held[j - j0] : target_weight(r, p, j);
         if (plain) return w;
-        if (y == nullptr) return j == turned ? 0 : w;
+        if (!two) return j == turned ? 0 : w;
+        if (w == 0) return 0;
         const u64 share = (u64)((double)w * p_unit);
-        const u64 less = q.sum > 0 ? (u64)((double)weight_of(expf(scaled(clean(Vec<T>::load(y + j)), q.top, inv))) * q_unit) : 0;
+        u64 less = 0;
+        if (V > 0) less = (u64)((double)(HELD ? held[P.share + j - j0] : draft_weight(r, q, j)) * q_unit);
         return share > less ? share - less : 0;
     };
-    // every warp has a share of the row, in order
-    const int per = ((P.A + kThreads / 32 - 1) / (kThreads / 32) + 31) / 32 * 32, j0 = min(warp * per, P.A), j1 = min(j0 + per, P.A);
-    __shared__ u64 part[kThreads / 32];
-    bool plain = y == nullptr && turned < 0;
-    u64 total = 0;
+    if (HELD) __syncthreads();
+    // every warp has a stretch of the block's share, in order
+    const int per = ((j1 - j0 + NT / 32 - 1) / (NT / 32) + 31) / 32 * 32, k0 = min(j0 + warp * per, j1), k1 = min(k0 + per, j1);
+    u64 mine = 0, total = 0, none = 0;
     for (int round = 0; round < 2; ++round) {
-        u64 mine = 0;
-        for (int j = j0 + lane; j < j1; j += 32) mine += weight(j, plain);
+        mine = 0;
+        for (int j = k0 + lane; j < k1; j += 32) mine += weight(j);
         mine = warp_sum(mine);
-        __syncthreads();
-        if (lane == 0) part[warp] = mine;
-        __syncthreads();
-        total = 0;
-        for (int k = 0; k < kThreads / 32; ++k) total += part[k];
+        total = lane == 0 ? mine : 0;
+        none = 0;
+        cluster_sum(&total, &none);
         if (total > 0 || plain) break;
         plain = true;                                         // nothing is left of the difference: the target's own probabilities
     }
     const u64 target = target_of(P.draw_uniforms[b], total);
     u64 before = 0;
-    int holder = 0;
-    for (; holder < kThreads / 32 - 1 && before + part[holder] <= target; ++holder) before += part[holder];
-    if (warp != holder) return;
-    for (int base = j0; base < j1; base += 32) {
-        const int j = base + lane;
-        const u64 w = j < j1 ? weight(j, plain) : 0;
-        u64 run = w;
+    if (ranks > 1)
+        for (int k = 0; k < rank; ++k) before += sent[(turns - 1) & 1][k][0];
+    for (int w = 0; w < warp; ++w) before += part[0][w];
+    if (before <= target && target < before + mine) {
+        for (int base = k0; base < k1; base += 32) {
+            const int j = base + lane;
+            const u64 w = j < k1 ? weight(j) : 0;
+            u64 run = w;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const u64 up = __shfl_up_sync(~0u, run, o);
-            if (lane >= o) run += up;
-        }
-        const unsigned over = __ballot_sync(~0u, before + run > target);
-        if (over) {
-            if (lane == __ffs(over) - 1) {
-                P.out[r] = j;
-                P.log_probs[r] = score(r, clean(Vec<T>::load(x + j)));
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 up = __shfl_up_sync(~0u, run, o);
+                if (lane >= o) run += up;
             }
-            return;
+            const unsigned over = __ballot_sync(~0u, before + run > target);
+            if (over) {
+                if (lane == __ffs(over) - 1) {
+                    P.out[r] = j;
+                    P.log_probs[r] = score(p, clean(Vec<T>::load(P.logits + r * P.ld + j)));
+                }
+                break;
+            }
+            before += __shfl_sync(~0u, run, 31);
         }
-        before += __shfl_sync(~0u, run, 31);
     }
 }
 
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-size_t workspace_of(int64_t rows) { return (size_t)(2 * rows) * sizeof(RowStat) + 16; }
+constexpr int kMostParts = 16, kMostShare = 28 * 1024;
+
+// Rows are cut into parts only while all parts are fewer than four a multiprocessor.
+size_t workspace_of(int64_t rows) { return (size_t)(2 * rows + 4 * rlcs_device::limits().sms) * sizeof(PartStat) + 16; }
+
+// One cluster a trajectory.  Room beyond 48 KB of shared memory is asked for once a device.
+template <typename T, int NT, bool HELD> int launch_draw(const VerifyParams<T>& P, int ranks, cudaStream_t s) {
+    const auto kernel = verify_draw_kernel<T, NT, HELD>;
+    static bool granted[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RLCS_ERR_CUDA;
+    if (HELD && !granted[dev]) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShare * 8) != cudaSuccess) return RLCS_ERR_CUDA;
+        granted[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(P.seqs * ranks));
+    cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = HELD ? 8 * (size_t)P.share : 0;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P) == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
+}
 
 template <typename T>
 int verify_run(const T* logits, int64_t ld, const T* drafts, int64_t ldd, const int32_t* tokens, const int32_t* offsets, const float* uniforms,
@@ -248,11 +466,26 @@ int verify_run(const T* logits, int64_t ld, const T* drafts, int64_t ldd, const 
     if (!aligned_to(logits, sizeof(T)) || !aligned_to(drafts, sizeof(T))) return RLCS_ERR_ALIGN;
     if (rows > 0 && (workspace == nullptr || workspace_bytes < workspace_of(rows))) return RLCS_ERR_WORKSPACE;
     if (!aligned_to(workspace, 16)) return RLCS_ERR_ALIGN;
-    const VerifyParams<T> P = {logits, drafts, tokens, offsets, uniforms, draw_uniforms, temperature, temperature_all, out, log_probs, accepted,
-                               static_cast<RowStat*>(workspace), ld, ldd, (int32_t)rows, (int32_t)seqs, (int32_t)A};
+    VerifyParams<T> P = {logits, drafts, tokens, offsets, uniforms, draw_uniforms, temperature, temperature_all, out, log_probs, accepted,
+                         static_cast<PartStat*>(workspace), ld, ldd, (int32_t)rows, (int32_t)seqs, (int32_t)A, 1, 0};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (rows > 0) verify_rows_kernel<T><<<(unsigned)(rows * (drafts != nullptr ? 2 : 1)), kThreads, 0, s>>>(P);
-    verify_draw_kernel<T><<<(unsigned)seqs, kThreads, 0, s>>>(P);
+    const int64_t all = rows * (drafts != nullptr ? 2 : 1), sms = rlcs_device::limits().sms, vecs = A / Vec<T>::N;
+    if (rows > 0) {
+        if (vecs <= 512) {                                       // a warp's 16 loads at most
+            verify_scan_kernel<T, 32><<<(unsigned)((all + kScan / 32 - 1) / (kScan / 32)), kScan, 0, s>>>(P);
+        } else {
+            // rows in parts while there are fewer than two blocks a multiprocessor and a thread keeps a round of loads
+            while (P.parts < kMostParts && all * P.parts < 2 * sms && vecs / (2 * P.parts) >= kScan * kAhead) P.parts *= 2;
+            verify_scan_kernel<T, kScan><<<(unsigned)(all * P.parts), kScan, 0, s>>>(P);
+        }
+    }
+    // a block's share of a row: few thousand entries; both rows' weights in shared memory up to 224 KB
+    int ranks = 1;
+    while (ranks < 8 && (A + ranks - 1) / ranks > 4096) ranks *= 2;
+    P.share = (int32_t)((A + ranks - 1) / ranks);
+    const bool hold = P.share <= kMostShare;
+    const int st = A <= 4096 ? launch_draw<T, 128, true>(P, ranks, s) : hold ? launch_draw<T, 512, true>(P, ranks, s) : launch_draw<T, 512, false>(P, ranks, s);
+    if (st != RLCS_OK) return st;
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }
 
