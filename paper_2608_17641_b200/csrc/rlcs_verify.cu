@@ -50,6 +50,7 @@ template <typename T> struct VerifyParams {
     float* log_probs;
     int32_t* accepted;
     PartStat* stats;                      // [2][rows][parts]: of the target's rows, of the draft policy's
+    float* picked;                        // [2][rows]: the draft's logit
     int64_t ld, ldd;
     int32_t rows, seqs, A, parts;
     int32_t share;                        // entries of a row that a block of the second kernel has
@@ -108,6 +109,11 @@ __global__ void __launch_bounds__(kScan) verify_scan_kernel(const __grid_constan
     const uint4* body = reinterpret_cast<const uint4*>(x + sp.head) + v0;
     auto single = [&](int i) { return i < sp.head ? i : rest + i - sp.head; };
 
+    float picked = -INFINITY;
+    if (part == 0 && me == 0 && t + 1 < end) {
+        const int token = P.tokens[t + 1];
+        if (token >= 0 && token < P.A) picked = clean(Vec<T>::load(x + token));
+    }
     float m = -INFINITY;
     double all = 0.;
     int chunk = -1;                                          // where the thread's maximum came first: a chunk of vectors, or -2 - a single
@@ -205,33 +211,97 @@ __global__ void __launch_bounds__(kScan) verify_scan_kernel(const __grid_constan
         }
     }
     if (me == 0) P.stats[row * P.parts + part] = PartStat{top == -INFINITY ? 0. : all, top, best};
+    if (me == 0 && part == 0) P.picked[row] = picked;
 }
 
 // ---------------------------------------------------------------------------------------------- verdict and draw
+// A row of logits: the parts joined.
 struct RowStat {
     double all;
-    float top;
+    float top, picked;
     int32_t best;
 };
 
-template <typename T> __device__ __forceinline__ RowStat join_parts(const VerifyParams<T>& P, int64_t row, float inv) {
-    const PartStat* s = P.stats + row * P.parts;
-    RowStat r = {0., -INFINITY, P.A};
-    for (int i = 0; i < P.parts; ++i)
-        if (s[i].top > r.top || (s[i].top == r.top && s[i].best < r.best)) { r.top = s[i].top; r.best = s[i].best; }
-    if (r.top == -INFINITY) return r;
-    for (int i = 0; i < P.parts; ++i) {
-        const float d = scaled(s[i].top, r.top, inv);
-        if (s[i].top != -INFINITY && d == d) r.all += s[i].all * exp((double)d);
+constexpr int kMostParts = 16;
+
+// Both of row t's, by a warp: sixteen lanes each.  Lanes below 16 have the target's, the others the draft policy's (nothing without it).
+template <typename T> __device__ __forceinline__ RowStat join_parts(const VerifyParams<T>& P, int t, bool both, float inv, int lane) {
+    const int part = lane & 15, which = lane >> 4;
+    const int64_t row = (int64_t)which * P.rows + t;
+    const bool there = which == 0 || both;
+    PartStat v = {0., -INFINITY, P.A};
+    if (there && part < P.parts) v = P.stats[row * P.parts + part];
+    RowStat r;
+    r.picked = there ? P.picked[row] : -INFINITY;
+    r.top = v.top;
+#pragma unroll
+    for (int o = 8; o; o >>= 1) r.top = fmaxf(r.top, __shfl_xor_sync(~0u, r.top, o));
+    const float d = scaled(v.top, r.top, inv);
+    r.all = v.top == -INFINITY || d != d ? 0. : v.all * (double)expf(d);
+    r.best = v.top == r.top ? v.best : P.A;
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {
+        r.all += __shfl_xor_sync(~0u, r.all, o);
+        r.best = min(r.best, __shfl_xor_sync(~0u, r.best, o));
     }
     return r;
 }
 
-// NT threads a block, a cluster a trajectory.  HELD: a block's weights of both rows stay in shared memory (share entries each).
+// Weights of the n entries from x on, by the NT threads of a block: written to `to` (16-byte aligned at the row's first vector) and added
+// up.  `top` is finite: an entry that equals it is 0 away, and one of -inf or NaN ends as 0.
+template <typename T, int NT> __device__ __forceinline__ u64 weigh_row(const T* x, int n, float top, float inv, uint32_t* to) {
+    constexpr int N = Vec<T>::N;
+    const Span sp = span_of(x, n);
+    const int tid = threadIdx.x, rest = sp.head + sp.vecs * N;
+    u64 sum = 0;
+    for (int i = tid; i < sp.head + n - rest; i += NT) {
+        const int j = i < sp.head ? i : rest + i - sp.head;
+        const uint32_t w = weight_of(e_of(Vec<T>::load(x + j), top, inv));
+        to[j] = w;
+        sum += w;
+    }
+    const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
+    uint4* out = reinterpret_cast<uint4*>(to + sp.head);
+    for (int i = tid; i < sp.vecs; i += NT) {
+        float e[N];
+        Vec<T>::unpack(body[i], e);
+        float most = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            e[j] = expf((e[j] - top) * inv);
+            most = max_nan(most, e[j]);
+        }
+        uint32_t w[N];
+        if (most < 0x1p-10f) {                               // nearly always: weight_of's short way, sums of 2^24 at most
+            uint32_t all = 0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                w[j] = (__float_as_uint(__fmaf_rd(e[j], 0x1p31f, 4194304.5f)) & 0x7fffffu) >> 1;
+                all += w[j];
+            }
+            sum += all;
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                w[j] = weight_of(e[j] >= 0.f ? e[j] : 0.f);
+                sum += w[j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < N; j += 4) out[i * (N / 4) + j / 4] = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+    }
+    return sum;
+}
+
+// Log-probability of an entry under the whole softmax.
+__device__ __noinline__ float score(double all, float x, float top, float inv) { return (float)((double)scaled(x, top, inv) - log(all)); }
+
+// NT threads a block, a cluster a trajectory.  HELD: a block's weights of both rows stay in shared memory.
 template <typename T, int NT, bool HELD>
 __global__ void __launch_bounds__(NT) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
-    extern __shared__ uint32_t held[];                       // [2][share]
+    extern __shared__ __align__(16) uint32_t held[];         // [2][share and up to a vector before it]
     __shared__ u64 part[2][NT / 32], sent[2][16][2];
+    __shared__ RowStat stat[2];                              // of row r below
     __shared__ int stop;                                     // least 2 t + 1 of a row whose draft does not stay, 2 t where that is unclear
     const cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -241,188 +311,189 @@ __global__ void __launch_bounds__(NT) verify_draw_kernel(const __grid_constant__
         if (rank == 0 && tid == 0) P.accepted[b] = 0;
         return;
     }
-    if (ranks > 1) cluster.sync();                           // all of the cluster's blocks run
+    if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // this block runs
     const float temperature = temperature_of(P, b), inv = inverse_of(temperature);
     const bool greedy = !(temperature > 0.f);
     const int j0 = min(rank * P.share, P.A), j1 = min(j0 + P.share, P.A);
 
-    // (x, y) summed over the block, then over the cluster; two sets of places, taken in turn
+    // (x, y), the same for all lanes of a warp, summed over the cluster; x stays in part[0].  Two sets of places, taken in turn.
     int turns = 0;
-    auto block_sum = [&](u64* x, u64* y) {
-        *x = warp_sum(*x);
-        *y = warp_sum(*y);
+    auto cluster_sum = [&](u64* x, u64* y) {
         __syncthreads();
         if (lane == 0) { part[0][warp] = *x; part[1][warp] = *y; }
         __syncthreads();
-        *x = *y = 0;
-        for (int w = 0; w < NT / 32; ++w) { *x += part[0][w]; *y += part[1][w]; }
-    };
-    auto cluster_sum = [&](u64* x, u64* y) {
-        block_sum(x, y);
+        *x = warp_sum(lane < NT / 32 ? part[0][lane] : 0);
+        *y = warp_sum(lane < NT / 32 ? part[1][lane] : 0);
         if (ranks == 1) return;
         const int turn = turns++ & 1;
+        if (turns == 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");            // all of the cluster's blocks run
         if (tid < ranks) {
             u64* to = cluster.map_shared_rank(&sent[turn][rank][0], tid);
             to[0] = *x;
             to[1] = *y;
         }
         cluster.sync();
-        *x = *y = 0;
-        for (int r = 0; r < ranks; ++r) { *x += sent[turn][r][0]; *y += sent[turn][r][1]; }
-    };
-    auto target_weight = [&](int t, const RowStat& p, int j) { return weight_of(e_of(Vec<T>::load(P.logits + t * P.ld + j), p.top, inv)); };
-    auto draft_weight = [&](int t, const RowStat& q, int j) { return weight_of(e_of(Vec<T>::load(P.drafts + t * P.ldd + j), q.top, inv)); };
-    // whole sums of both rows' weights (of the target's alone where `two` is false)
-    auto whole_sums = [&](int t, const RowStat& p, const RowStat& q, bool two, u64* W, u64* V) {
-        u64 x = 0, y = 0;
-        if (p.top != -INFINITY)
-            for (int j = j0 + tid; j < j1; j += NT) {
-                const uint32_t w = target_weight(t, p, j);
-                if (HELD) held[j - j0] = w;
-                x += w;
-            }
-        if (two && q.top != -INFINITY)
-            for (int j = j0 + tid; j < j1; j += NT) {
-                const uint32_t w = draft_weight(t, q, j);
-                if (HELD) held[P.share + j - j0] = w;
-                y += w;
-            }
-        cluster_sum(&x, &y);
-        *W = x;
-        *V = y;
+        *x = warp_sum(lane < ranks ? sent[turn][lane][0] : 0);
+        *y = warp_sum(lane < ranks ? sent[turn][lane][1] : 0);
     };
     // does u (v W) < w V hold?
     auto decide = [&](int t, double w, double W, double v, double V) { return (double)P.uniforms[t] * (v * W) < w * V; };
-    auto weight_at = [&](const T* x, const RowStat& r, int token) { return r.top == -INFINITY ? 0u : weight_of(e_of(Vec<T>::load(x + token), r.top, inv)); };
+    // a row's weights in shared memory begin where its vectors are aligned there too
+    auto lead = [&](const T* x) { return (Vec<T>::N - span_of(x + j0, j1 - j0).head) % Vec<T>::N; };
 
-    int from = begin, r;
+    // Row r: the first whose draft does not stay, or the last; a warp a row.  Then the exact sums of its weights.
+    int r, from = begin;
+    bool turned, two;                                        // a draft was turned down; a difference is drawn from
+    u64 sums[2];
     while (true) {
         __syncthreads();
-        if (tid == 0) stop = 2 * (end - 1) + 1;
+        if (tid == 0) stop = INT32_MAX;
         __syncthreads();
-        for (int t = from + tid; t < end - 1; t += NT) {
-            const int token = P.tokens[t + 1];
-            const RowStat p = join_parts(P, t, inv);
+        RowStat mine;
+        int failed = -1;
+        for (int t = from + warp; t < end && failed < 0; t += NT / 32) {
+            const bool last = t == end - 1;
+            mine = join_parts(P, t, P.drafts != nullptr && !last && !greedy, inv, lane);
+            const int token = last ? -1 : P.tokens[t + 1];
+            const float top = __shfl_sync(~0u, mine.top, 0), picked = __shfl_sync(~0u, mine.picked, 0);
+            const double all = __shfl_sync(~0u, mine.all, 0), all_q = __shfl_sync(~0u, mine.all, 16);
+            const double at = mine.top == -INFINITY ? 0. : (double)weight_of(e_of(mine.picked, mine.top, inv)), slack = P.A;
+            const double w = __shfl_sync(~0u, at, 0), v_q = __shfl_sync(~0u, at, 16);
             bool yes = false, no = true;
-            if (token >= 0 && token < P.A && p.top != -INFINITY) {
+            if (token >= 0 && token < P.A && top != -INFINITY) {
                 if (greedy) {
-                    yes = token == p.best;
-                } else {
-                    const double w = weight_at(P.logits + t * P.ld, p, token), slack = P.A;
-                    double v = 1., least_v = 1., most_v = 1.;
-                    if (P.drafts != nullptr) {
-                        const RowStat q = join_parts(P, (int64_t)P.rows + t, inv);
-                        v = weight_at(P.drafts + t * P.ldd, q, token);
-                        least_v = fmax(q.all * (0x1p31 * (1. - 0x1p-15)) - slack, 0.);
-                        most_v = q.all * (0x1p31 * (1. + 0x1p-15)) + slack;
-                    }
-                    const double least_w = fmax(p.all * (0x1p31 * (1. - 0x1p-15)) - slack, 0.), most_w = p.all * (0x1p31 * (1. + 0x1p-15)) + slack;
-                    // the same verdict at both ends, moved apart by more than the products' roundings
-                    yes = decide(t, w * (1. - 0x1p-40), most_w, v, least_v);
-                    no = !decide(t, w * (1. + 0x1p-40), least_w, v, most_v);
+                    yes = token == __shfl_sync(~0u, mine.best, 0);
+                } else {                                     // the same verdict at both ends, moved apart by more than the products' roundings
+                    constexpr double kLess = 0x1p31 * (1. - 0x1p-15), kMore = 0x1p31 * (1. + 0x1p-15);
+                    const bool drawn = P.drafts != nullptr;
+                    const double v = drawn ? v_q : 1., least_v = drawn ? fmax(all_q * kLess - slack, 0.) : 1., most_v = drawn ? all_q * kMore + slack : 1.;
+                    yes = decide(t, w * (1. - 0x1p-40), all * kMore + slack, v, least_v);
+                    no = !decide(t, w * (1. + 0x1p-40), fmax(all * kLess - slack, 0.), v, most_v);
                 }
             }
             if (!yes) {
-                atomicMin(&stop, 2 * t + (no ? 1 : 0));
-                break;
+                failed = t;
+                if (lane == 0) atomicMin(&stop, 2 * t + (no ? 1 : 0));
+            } else if (rank == 0 && lane == 0) {             // unless a row before it fails: below
+                P.out[t] = token;
+                P.log_probs[t] = score(all, picked, top, inv);
             }
         }
         __syncthreads();
         r = stop >> 1;
-        if (stop & 1) break;
-        const int token = P.tokens[r + 1];
-        const RowStat p = join_parts(P, r, inv);
-        RowStat q = {0., -INFINITY, 0};
-        if (P.drafts != nullptr) q = join_parts(P, (int64_t)P.rows + r, inv);
-        u64 W, V;
-        whole_sums(r, p, q, P.drafts != nullptr, &W, &V);
-        const double v = P.drafts != nullptr ? weight_at(P.drafts + r * P.ldd, q, token) : 1.;
-        if (!decide(r, weight_at(P.logits + r * P.ld, p, token), (double)W, v, P.drafts != nullptr ? (double)V : 1.)) break;
+        const bool clear = stop & 1;
+        if (failed == r && (lane & 15) == 0) stat[lane >> 4] = mine;
+        __syncthreads();
+        turned = r + 1 < end;
+        two = turned && P.drafts != nullptr;
+        if (greedy || stat[0].top == -INFINITY) break;
+        sums[0] = sums[1] = 0;
+#pragma unroll 1
+        for (int which = 0; which < (two ? 2 : 1); ++which) {
+            const T* x = which ? P.drafts + r * P.ldd : P.logits + r * P.ld;
+            const float top = stat[which].top;
+            uint32_t* to = held + which * (P.share + 8);
+            u64 sum = 0;
+            if (HELD && top != -INFINITY && top < INFINITY) {
+                sum = weigh_row<T, NT>(x + j0, j1 - j0, top, inv, to + lead(x));
+            } else {
+                for (int j = j0 + tid; j < j1; j += NT) {
+                    const uint32_t w = top == -INFINITY ? 0 : weight_of(e_of(Vec<T>::load(x + j), top, inv));
+                    if (HELD) to[lead(x) + j - j0] = w;
+                    sum += w;
+                }
+            }
+            (which ? sums[1] : sums[0]) = warp_sum(sum);
+        }
+        cluster_sum(&sums[0], &sums[1]);
+        if (clear) break;
+        const double w = weight_of(e_of(stat[0].picked, stat[0].top, inv));
+        const double v = !two ? 1. : stat[1].top == -INFINITY ? 0. : (double)weight_of(e_of(stat[1].picked, stat[1].top, inv));
+        if (!decide(r, w, (double)sums[0], v, two ? (double)sums[1] : 1.)) break;
+        if (rank == 0 && tid == 0) {
+            P.out[r] = P.tokens[r + 1];
+            P.log_probs[r] = score(stat[0].all, stat[0].picked, stat[0].top, inv);
+        }
         from = r + 1;
     }
-    const RowStat p = join_parts(P, r, inv);
-    auto score = [&](const RowStat& s, float x) { return (float)((double)scaled(x, s.top, inv) - log(s.all)); };      // under the whole softmax
+
+    const float top = stat[0].top;
     if (rank == 0) {
-        for (int t = begin + tid; t < end; t += NT) {
-            if (t == r) continue;
-            P.out[t] = t < r ? P.tokens[t + 1] : -1;
-            P.log_probs[t] = t < r ? score(join_parts(P, t, inv), clean(Vec<T>::load(P.logits + t * P.ld + P.tokens[t + 1]))) : -INFINITY;
-        }
         if (tid == 0) P.accepted[b] = r - begin;
+        for (int t = r + tid; t < end; t += NT)
+            if (t > r || top == -INFINITY) {
+                P.out[t] = -1;
+                P.log_probs[t] = -INFINITY;
+            }
     }
-    if (p.top == -INFINITY || greedy) {
-        if (rank == 0 && tid == 0) {
-            P.out[r] = p.top == -INFINITY ? -1 : p.best;
-            P.log_probs[r] = p.top == -INFINITY ? -INFINITY : score(p, p.top);
+    int drawn = -1;                                          // the token of row r, where this thread has it
+    const T* const x = P.logits + r * P.ld;
+    if (greedy || top == -INFINITY) {
+        if (rank == 0 && tid == 0 && top != -INFINITY) drawn = stat[0].best;
+        if (ranks > 1 && turns == 0) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    } else {
+        const double p_unit = kShareOne / (double)sums[0], q_unit = sums[1] > 0 ? kShareOne / (double)sums[1] : 0.;
+        const int given = turned && !two ? P.tokens[r + 1] : -1;
+        bool plain = !turned || (!two && given < 0);
+        const T* const y = two ? P.drafts + r * P.ldd : x;
+        const uint32_t *my_w = held + lead(x) - j0, *my_v = held + P.share + 8 + lead(y) - j0;
+        const float top_q = stat[1].top;
+        auto weight = [&](int j) -> u64 {
+            const uint32_t w = HELD ? my_w[j] : weight_of(e_of(Vec<T>::load(x + j), top, inv));
+            if (plain) return w;
+            if (!two) return j == given ? 0 : w;
+            const uint32_t v = HELD ? my_v[j] : top_q == -INFINITY ? 0 : weight_of(e_of(Vec<T>::load(y + j), top_q, inv));
+            const u64 share = (u64)((double)w * p_unit), less = (u64)((double)v * q_unit);
+            return share > less ? share - less : 0;
+        };
+        // every warp has a stretch of the block's share, in order
+        const int per = ((j1 - j0 + NT / 32 - 1) / (NT / 32) + 31) / 32 * 32, k0 = min(j0 + warp * per, j1), k1 = min(k0 + per, j1);
+        u64 mine, total, none = 0;
+        __syncthreads();
+        while (true) {
+            mine = 0;
+#pragma unroll 4
+            for (int j = k0 + lane; j < k1; j += 32) mine += weight(j);
+            total = mine = warp_sum(mine);
+            cluster_sum(&total, &none);
+            if (total > 0 || plain) break;
+            plain = true;                                     // nothing is left of the difference: the target's own probabilities
         }
-        return;
-    }
-    const bool two = r + 1 < end && P.drafts != nullptr;
-    const int turned = r + 1 < end && P.drafts == nullptr ? P.tokens[r + 1] : -1;
-    RowStat q = {0., -INFINITY, 0};
-    if (two) q = join_parts(P, (int64_t)P.rows + r, inv);
-    u64 W, V;
-    whole_sums(r, p, q, two, &W, &V);
-    const double p_unit = kShareOne / (double)W, q_unit = V > 0 ? kShareOne / (double)V : 0.;
-    bool plain = !two && turned < 0;
-    auto weight = [&](int j) -> u64 {
-        const uint32_t w = HELD ? held[j - j0] : target_weight(r, p, j);
-        if (plain) return w;
-        if (!two) return j == turned ? 0 : w;
-        if (w == 0) return 0;
-        const u64 share = (u64)((double)w * p_unit);
-        u64 less = 0;
-        if (V > 0) less = (u64)((double)(HELD ? held[P.share + j - j0] : draft_weight(r, q, j)) * q_unit);
-        return share > less ? share - less : 0;
-    };
-    if (HELD) __syncthreads();
-    // every warp has a stretch of the block's share, in order
-    const int per = ((j1 - j0 + NT / 32 - 1) / (NT / 32) + 31) / 32 * 32, k0 = min(j0 + warp * per, j1), k1 = min(k0 + per, j1);
-    u64 mine = 0, total = 0, none = 0;
-    for (int round = 0; round < 2; ++round) {
-        mine = 0;
-        for (int j = k0 + lane; j < k1; j += 32) mine += weight(j);
-        mine = warp_sum(mine);
-        total = lane == 0 ? mine : 0;
-        none = 0;
-        cluster_sum(&total, &none);
-        if (total > 0 || plain) break;
-        plain = true;                                         // nothing is left of the difference: the target's own probabilities
-    }
-    const u64 target = target_of(P.draw_uniforms[b], total);
-    u64 before = 0;
-    if (ranks > 1)
-        for (int k = 0; k < rank; ++k) before += sent[(turns - 1) & 1][k][0];
-    for (int w = 0; w < warp; ++w) before += part[0][w];
-    if (before <= target && target < before + mine) {
-        for (int base = k0; base < k1; base += 32) {
-            const int j = base + lane;
-            const u64 w = j < k1 ? weight(j) : 0;
-            u64 run = w;
+        const u64 target = target_of(P.draw_uniforms[b], total);
+        u64 before = lane < warp ? part[0][lane] : 0;
+        if (lane < rank) before += sent[(turns - 1) & 1][lane][0];
+        before = warp_sum(before);
+        if (before <= target && target < before + mine) {
+            for (int base = k0; base < k1; base += 32) {
+                const int j = base + lane;
+                const u64 w = j < k1 ? weight(j) : 0;
+                u64 run = w;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const u64 up = __shfl_up_sync(~0u, run, o);
-                if (lane >= o) run += up;
-            }
-            const unsigned over = __ballot_sync(~0u, before + run > target);
-            if (over) {
-                if (lane == __ffs(over) - 1) {
-                    P.out[r] = j;
-                    P.log_probs[r] = score(p, clean(Vec<T>::load(P.logits + r * P.ld + j)));
+                for (int o = 1; o < 32; o <<= 1) {
+                    const u64 up = __shfl_up_sync(~0u, run, o);
+                    if (lane >= o) run += up;
                 }
-                break;
+                const unsigned over = __ballot_sync(~0u, before + run > target);
+                if (over) {
+                    if (lane == __ffs(over) - 1) drawn = j;
+                    break;
+                }
+                before += __shfl_sync(~0u, run, 31);
             }
-            before += __shfl_sync(~0u, run, 31);
         }
+    }
+    if (drawn >= 0) {
+        P.out[r] = drawn;
+        P.log_probs[r] = score(stat[0].all, clean(Vec<T>::load(x + drawn)), top, inv);
     }
 }
 
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-constexpr int kMostParts = 16, kMostShare = 28 * 1024;
+constexpr int kMostShare = 28 * 1024, kMostRanks = 16;
 
 // Rows are cut into parts only while all parts are fewer than four a multiprocessor.
-size_t workspace_of(int64_t rows) { return (size_t)(2 * rows + 4 * rlcs_device::limits().sms) * sizeof(PartStat) + 16; }
+size_t workspace_of(int64_t rows) { return (size_t)(2 * rows + 4 * rlcs_device::limits().sms) * sizeof(PartStat) + (size_t)(2 * rows) * sizeof(float); }
 
 // One cluster a trajectory.  Room beyond 48 KB of shared memory is asked for once a device.
 template <typename T, int NT, bool HELD> int launch_draw(const VerifyParams<T>& P, int ranks, cudaStream_t s) {
@@ -430,14 +501,16 @@ template <typename T, int NT, bool HELD> int launch_draw(const VerifyParams<T>& 
     static bool granted[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RLCS_ERR_CUDA;
-    if (HELD && !granted[dev]) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShare * 8) != cudaSuccess) return RLCS_ERR_CUDA;
+    if (!granted[dev]) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * (kMostShare + 8)) != cudaSuccess ||
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+            return RLCS_ERR_CUDA;
         granted[dev] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(P.seqs * ranks));
     cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = HELD ? 8 * (size_t)P.share : 0;
+    cfg.dynamicSmemBytes = HELD ? 8 * (size_t)(P.share + 8) : 0;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -467,7 +540,8 @@ int verify_run(const T* logits, int64_t ld, const T* drafts, int64_t ldd, const 
     if (rows > 0 && (workspace == nullptr || workspace_bytes < workspace_of(rows))) return RLCS_ERR_WORKSPACE;
     if (!aligned_to(workspace, 16)) return RLCS_ERR_ALIGN;
     VerifyParams<T> P = {logits, drafts, tokens, offsets, uniforms, draw_uniforms, temperature, temperature_all, out, log_probs, accepted,
-                         static_cast<PartStat*>(workspace), ld, ldd, (int32_t)rows, (int32_t)seqs, (int32_t)A, 1, 0};
+                         static_cast<PartStat*>(workspace),
+                         reinterpret_cast<float*>(static_cast<PartStat*>(workspace) + 2 * rows + 4 * rlcs_device::limits().sms), ld, ldd, (int32_t)rows, (int32_t)seqs, (int32_t)A, 1, 0};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int64_t all = rows * (drafts != nullptr ? 2 : 1), sms = rlcs_device::limits().sms, vecs = A / Vec<T>::N;
     if (rows > 0) {
@@ -481,8 +555,8 @@ int verify_run(const T* logits, int64_t ld, const T* drafts, int64_t ldd, const 
     }
     // a block's share of a row: few thousand entries; both rows' weights in shared memory up to 224 KB
     int ranks = 1;
-    while (ranks < 8 && (A + ranks - 1) / ranks > 4096) ranks *= 2;
-    P.share = (int32_t)((A + ranks - 1) / ranks);
+    while (ranks < kMostRanks && (A + ranks - 1) / ranks > 4096) ranks *= 2;
+    P.share = (int32_t)(((A + ranks - 1) / ranks + 7) / 8 * 8);
     const bool hold = P.share <= kMostShare;
     const int st = A <= 4096 ? launch_draw<T, 128, true>(P, ranks, s) : hold ? launch_draw<T, 512, true>(P, ranks, s) : launch_draw<T, 512, false>(P, ranks, s);
     if (st != RLCS_OK) return st;

@@ -448,6 +448,47 @@ def test_verify_extreme_uniforms(api):
             check_verify(api, x, tokens, offsets, torch.full_like(u, a), torch.full_like(du, c), None)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A", [40, 3000, 20000])
+def test_verify_uniforms_at_the_border(api, A, dtype):
+    """Uniforms within a few places of w V / (v W), where the verdict takes the whole weights' own sums."""
+    x, tokens, offsets, u, du, drafts = verify_inputs([6, 9, 2], A, dtype, A, near=0.5)
+    for drawn in (True, False):
+        for step in (-2, -1, 0, 1, 2):
+            for t in range(len(u) - 1):
+                w, v = plain_weights(x[t], 1.0)[0], plain_weights(drafts[t], 1.0)[0]
+                tok = int(tokens[t + 1])
+                at = w[tok] * sum(v) / max(1, v[tok] * sum(w)) if drawn else w[tok] / sum(w)
+                edge = np.float32(min(at, 1 - 2.0 ** -24))
+                for _ in range(abs(step)):
+                    edge = np.nextafter(edge, np.float32(step))
+                u[t] = min(float(edge), 1 - 2.0 ** -24)
+            check_verify(api, x, tokens, offsets, u, du, drafts if drawn else None)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A", [7, 700, 9000])
+def test_verify_infinite_and_tiny_temperatures(api, A, dtype):
+    """An infinite temperature makes all allowed tokens alike and no other one possible; a tiny one all but decides."""
+    x, tokens, offsets, u, du, _ = verify_inputs([3, 4, 1, 2], A, dtype, A)
+    off = torch.rand(x.shape, generator=torch.Generator().manual_seed(1)) < 0.5
+    off[:, 0] = False
+    x[off] = -math.inf
+    x[2, A // 2] = float("nan")
+    out, lp, acc = api.verify_drafts(up(x), up(tokens), up(ints(offsets)), up(u), up(du), temperature=math.inf)
+    allowed = (x > -math.inf)
+    out, lp = out.tolist(), lp.tolist()
+    for t, tok in enumerate(out):
+        if tok >= 0:
+            assert allowed[t, tok] and abs(lp[t] + math.log(int(allowed[t].sum()))) < 1e-5
+    assert max(out) >= 0
+    out, lp, acc = api.verify_drafts(up(x), up(tokens), up(ints(offsets)), up(u), up(du), temperature=1e-30)
+    best = torch.where(torch.isnan(x.float()), -math.inf, x.float()).max(1)
+    for t, tok in enumerate(out.tolist()):
+        if tok >= 0:
+            assert float(x[t, tok]) == float(best.values[t])
+
+
 def test_verify_turned_down_draft_that_is_certain(api):
     """Nothing is left of the difference (p = q, turned down by u = 1) and of a certain, given draft: the target's own probabilities."""
     x = torch.full((4, 40), -math.inf)
