@@ -264,7 +264,15 @@ template <typename T, int NT> __device__ __forceinline__ u64 weigh_row(const T* 
     uint4* out = reinterpret_cast<uint4*>(to + sp.head);
     for (int i = tid; i < sp.vecs; i += NT) {
         float e[N];
-        Vec<T>::unpack(body[i], e);
+        const uint4 v = body[i];
+        // a vector of nothing but weights of 0 (exp below 2^-32): -inf counts among them, NaN is passed over
+        const float best = Vec<T>::most_number_of(Vec<T>::most_number(Vec<T>::most_number(v.x, v.y), Vec<T>::most_number(v.z, v.w)));
+        if ((best - top) * inv < -22.5f) {
+#pragma unroll
+            for (int j = 0; j < N; j += 4) out[i * (N / 4) + j / 4] = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        Vec<T>::unpack(v, e);
         float most = 0.f;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -293,12 +301,18 @@ template <typename T, int NT> __device__ __forceinline__ u64 weigh_row(const T* 
     return sum;
 }
 
+// 2^52 + floor(w unit), for floor(w unit) < 2^52, as the bits of a double: differences of two are those of the floors.  Conversions between
+// integers and doubles, which this does without, have a quarter of the rate of 64-bit additions.
+__device__ __forceinline__ long long shares_of(uint32_t w, double unit) {
+    return __double_as_longlong(__dadd_rd((__hiloint2double(0x43300000, (int)w) - 0x1p52) * unit, 0x1p52));
+}
+
 // Log-probability of an entry under the whole softmax.
 __device__ __noinline__ float score(double all, float x, float top, float inv) { return (float)((double)scaled(x, top, inv) - log(all)); }
 
 // NT threads a block, a cluster a trajectory.  HELD: a block's weights of both rows stay in shared memory.
 template <typename T, int NT, bool HELD>
-__global__ void __launch_bounds__(NT) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
+__global__ void __launch_bounds__(NT, NT == 512 ? 3 : 1) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
     extern __shared__ __align__(16) uint32_t held[];         // [2][share and up to a vector before it]
     __shared__ u64 part[2][NT / 32], sent[2][16][2];
     __shared__ RowStat stat[2];                              // of row r below
@@ -443,8 +457,8 @@ __global__ void __launch_bounds__(NT) verify_draw_kernel(const __grid_constant__
             if (plain) return w;
             if (!two) return j == given ? 0 : w;
             const uint32_t v = HELD ? my_v[j] : top_q == -INFINITY ? 0 : weight_of(e_of(Vec<T>::load(y + j), top_q, inv));
-            const u64 share = (u64)((double)w * p_unit), less = (u64)((double)v * q_unit);
-            return share > less ? share - less : 0;
+            const long long more = shares_of(w, p_unit) - shares_of(v, q_unit);
+            return more > 0 ? (u64)more : 0;
         };
         // every warp has a stretch of the block's share, in order
         const int per = ((j1 - j0 + NT / 32 - 1) / (NT / 32) + 31) / 32 * 32, k0 = min(j0 + warp * per, j1), k1 = min(k0 + per, j1);
