@@ -704,6 +704,30 @@ def test_distill_towards_itself_is_zero_and_shapes(api):
     assert loss.shape == (2, 3) and grad.shape == (2, 3, 50) and loss.abs().max() < 1e-5 and grad.abs().max() < 1e-5
 
 
+@pytest.mark.parametrize("polls", [0, 1, 3])
+@pytest.mark.parametrize("R,A,dtype", [(2, 9000, F32), (400, 70000, BF16), (40, 150000, BF16)])
+def test_distill_waits_that_run_out(api, polls, R, A, dtype):
+    """A wait that gives up leaves NaN, the right value or nothing written, and the next call is right."""
+    from paper_2608_17641_b200 import binding
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(R, A, device="cuda", generator=g).to(dtype)
+    ids = torch.randint(0, A, (R, 7), device="cuda", generator=g, dtype=I32)
+    teacher = torch.randn(R, 7, device="cuda", generator=g)
+    want = api.compute_distillation(x, ids, teacher)
+    fn = binding.rlcs_distill_grad if dtype == F32 else binding.rlcs_distill_grad_bf16
+    loss, grad = guarded_empty((R,), F32).fill_(77), guarded_empty((R, A), dtype).fill_(77)
+    binding.rlcs_debug_set_wait_polls(polls)
+    try:
+        fn(x, ids, teacher, loss=loss, dlogits=grad)
+        torch.cuda.synchronize()
+    finally:
+        binding.rlcs_debug_set_wait_polls(-1)
+    for got, w in zip((loss, grad), want):
+        assert (torch.isnan(got) | (got == w) | (got == 77)).all()
+    again = api.compute_distillation(x, ids, teacher)
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
+
+
 def test_distill_into_a_buffer_and_on_a_stream(api):
     from paper_2608_17641_b200 import binding
     s = torch.cuda.Stream()
