@@ -281,6 +281,7 @@ __global__ void __launch_bounds__(kBlock, 3) distill_block_kernel(const __grid_c
     extern __shared__ uint4 held_all[];
     __shared__ Both part[kWarps], joined;
     __shared__ __align__(8) float2 sent[2][kMostRanks];
+    __shared__ uint16_t listed[kWarps][32];                  // teacher entries that fall to a warp
     __shared__ int stuck, leave;                             // leave: stuck as the whole block saw it
     __shared__ __align__(8) uint64_t full[kWarps][kChunks], got[2];
     namespace cg = cooperative_groups;
@@ -516,24 +517,43 @@ __global__ void __launch_bounds__(kBlock, 3) distill_block_kernel(const __grid_c
             // entries that fall to this warp: its vectors', and the single elements' to the first block's first warp
             const int lo = head + v0 * N, hi = lo + n * N;
             const bool ends = rank == 0 && warp == 0;
+            const float z = 1.f / r.teacher.s;
+            auto mine = [&](int e) { return e >= 0 && ((e >= lo && e < hi) || (ends && (e < head || e >= rest))); };
+            int count = 0;
             for (int i0 = 0; i0 < P.K; i0 += 32) {
-                const int e = i0 + lane < P.K ? id[i0 + lane] : -1;
-                unsigned hits = __ballot_sync(~0u, e >= 0 && ((e >= lo && e < hi) || (ends && (e < head || e >= rest))));
-                while (hits != 0) {
-                    const int src = __ffs(hits) - 1, which = __shfl_sync(~0u, e, src);
-                    hits &= hits - 1;
-                    float p = 0.f;
-                    bool before = false;                     // another entry of the same number, served already
-                    for (int k0 = 0; k0 < P.K; k0 += 32)
-                        if (k0 + lane < P.K && id[k0 + lane] == which) {
-                            p += chance(t[k0 + lane], r, k);
-                            before = before || k0 + lane < i0 + src;
-                        }
-                    p = warp_sum(p);
-                    if (__any_sync(~0u, before)) continue;
-                    if (lane == 0) Vec<T>::store(y + which, slow(xs[i0 + src]) - unit * p);
+                const bool hit = mine(i0 + lane < P.K ? id[i0 + lane] : -1);
+                const unsigned hits = __ballot_sync(~0u, hit);
+                const int at = count + __popc(hits & ((1u << lane) - 1));
+                if (hit && at < 32) listed[warp][at] = (uint16_t)(i0 + lane);
+                count += __popc(hits);
+            }
+            __syncwarp();
+            const int i = lane < count && lane < 32 ? listed[warp][lane] : -1;
+            const int which = i >= 0 ? id[i] : -1 - lane;
+            const bool alone_in_place = __popc(__match_any_sync(~0u, which)) == 1;
+            if (count <= 32 && __all_sync(~0u, alone_in_place)) {
+                if (i >= 0) Vec<T>::store(y + which, slow(xs[i]) - unit * (exp2_of((t[i] - r.teacher.m) * k) * z));
+            } else {                                         // many, or some named twice: one after the other, with all that name it
+                for (int i0 = 0; i0 < P.K; i0 += 32) {
+                    const int e = i0 + lane < P.K ? id[i0 + lane] : -1;
+                    unsigned hits = __ballot_sync(~0u, mine(e));
+                    while (hits != 0) {
+                        const int src = __ffs(hits) - 1, one = __shfl_sync(~0u, e, src);
+                        hits &= hits - 1;
+                        float p = 0.f;
+                        bool before = false;                 // served already
+                        for (int k0 = 0; k0 < P.K; k0 += 32)
+                            if (k0 + lane < P.K && id[k0 + lane] == one) {
+                                p += exp2_of((t[k0 + lane] - r.teacher.m) * k) * z;
+                                before = before || k0 + lane < i0 + src;
+                            }
+                        p = warp_sum(p);
+                        if (__any_sync(~0u, before)) continue;
+                        if (lane == 0) Vec<T>::store(y + one, slow(xs[i0 + src]) - unit * p);
+                    }
                 }
             }
+            __syncwarp();                                    // the list has been read
         }
         now = next;
     }
