@@ -354,6 +354,15 @@ __device__ __forceinline__ void segment(const AttnParams& P, const CUtensorMap* 
                 all += sml[w * 16 + row].y * f;
             }
             const int rr = first_row + row;
+            if constexpr (CAUSAL)
+                if (P.own_segs == 1) {                            // the only segment: nothing to be joined
+                    const int64_t to = (int64_t)(b0 + rr / P.r) * P.H + kv_head * P.r + rr % P.r;
+                    const float inv = all != 0.f ? 1.f / all : 0.f;
+                    if (c < P.d)
+                        *reinterpret_cast<uint2*>(P.out + to * P.d + c) = all != 0.f ? make_uint2(pack2(sum.x * inv, sum.y * inv), pack2(sum.z * inv, sum.w * inv)) : make_uint2(0, 0);
+                    if (c == 0 && P.lse != nullptr) P.lse[to] = all != 0.f ? (top + log2f(all)) * 0.6931471805599453f : -INFINITY;
+                    continue;
+                }
             const int64_t at = seg_rows + (int64_t)(b0 + rr / P.r) * P.H + kv_head * P.r + rr % P.r;
             *reinterpret_cast<float4*>(P.part_o + at * D + c) = sum;
             if (c == 0) P.part_ml[at] = make_float2(top, all);

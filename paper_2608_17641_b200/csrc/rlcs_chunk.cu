@@ -59,7 +59,16 @@ chunk_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUte
     const int rows = c.count * P.r, first_row = tile * 16;
     if (first_row >= rows) return;
     const int begin = seg * P.own_seg, end = min(begin + P.own_seg, keys_of(C, c, min(first_row + 16, rows)));
-    if (begin >= end) return;
+    if (begin >= end) {
+        if (P.own_segs <= 1)                                      // rows without keys, which nobody joins
+            for (int i = threadIdx.x; i < min(16, rows - first_row) * (P.d / 8); i += kThreads) {
+                const int row = first_row + i / (P.d / 8);
+                const int64_t at = (int64_t)(c.first + row / P.r) * P.H + kv_head * P.r + row % P.r;
+                *reinterpret_cast<uint4*>(P.out + at * P.d + i % (P.d / 8) * 8) = make_uint4(0, 0, 0, 0);
+                if (i % (P.d / 8) == 0 && P.lse != nullptr) P.lse[at] = -INFINITY;
+            }
+        return;
+    }
     segment<D, TMA, true>(P, &k_map, &v_map, raw, ids, bars, &gave_up, P.block_table + (int64_t)b * P.own_width, P.own_width, begin, end, kv_head,
                           first_row, rows, c.first, seg, c.start + 1 - begin);
 }
@@ -614,7 +623,7 @@ int check_shape(ChunkParams& C, int64_t T, int64_t seqs, int64_t H, int64_t Hk, 
 }
 
 size_t workspace_of(const ChunkParams& C) {
-    if (C.tiles == 0 && C.a.own_segs <= 1) return 0;
+    if (C.a.own_segs <= 1) return 0;
     const size_t rows = (size_t)C.a.own_segs * C.a.B * C.a.H;
     return rows * ((C.a.d <= 64 ? 64 : 128) + 2) * sizeof(float) + 16;
 }
@@ -646,12 +655,10 @@ template <int D> int launch(const ChunkParams& C, cudaStream_t s) {
         chunk_join_kernel<D><<<(unsigned)divide_up((int64_t)P.B * P.H, kThreads / 32), kThreads, 0, s>>>(C);
         return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
     }
-    const int64_t blocks = (int64_t)C.tiles * P.Hk * C.seqs * P.own_segs;
-    if (blocks > 0) {
-        const bool boxes = box_map(&k_map, P, P.k, kPart) && box_map(&v_map, P, P.v, kPart);
-        const int st = boxes ? launch_chunk<D, true>(C, blocks, k_map, v_map, s) : launch_chunk<D, false>(C, blocks, k_map, v_map, s);
-        if (st != RLCS_OK) return st;
-    }
+    const int64_t blocks = (int64_t)C.tiles * P.Hk * C.seqs * (P.own_segs > 0 ? P.own_segs : 1);      // rows without keys are written too
+    const bool boxes = box_map(&k_map, P, P.k, kPart) && box_map(&v_map, P, P.v, kPart);
+    const int st = boxes ? launch_chunk<D, true>(C, blocks, k_map, v_map, s) : launch_chunk<D, false>(C, blocks, k_map, v_map, s);
+    if (st != RLCS_OK || P.own_segs <= 1) return st != RLCS_OK ? st : cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
     chunk_join_kernel<D><<<(unsigned)divide_up((int64_t)P.B * P.H, kThreads / 32), kThreads, 0, s>>>(C);
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }

@@ -51,28 +51,38 @@ __device__ __forceinline__ int taken(const ForkParams& P, int number) {
     return number >= 0 && number < P.free_count ? max(P.free_pages[number], -1) : -1;
 }
 
-// Place in the free list of every row that needs a page, the rest -1, by the T threads of a block.
+// Place in the free list of every row that needs a page, the rest -1, by the T threads of a block; four rows a thread at a time, whose
+// lookups (source, length, page) go together.
 template <int T> __device__ __forceinline__ void fork_numbers(const ForkParams& P, const int32_t* first, int32_t* number, bool write) {
-    __shared__ int part[T / 32];
+    constexpr int kRows = 4;
+    __shared__ int part[kRows][T / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int carry = 0;
-    for (int base = 0; base < P.N; base += T) {
-        const int i = base + threadIdx.x;
-        bool fresh = false;
-        if (i < P.N) {
-            const OldRow r = old_row(P, i);
-            fresh = r.last >= 0 && first[r.source] != i;
+    for (int base = 0; base < P.N; base += kRows * T) {
+        OldRow r[kRows];
+        unsigned some[kRows];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int i = base + k * T + threadIdx.x;
+            r[k] = OldRow{-1, 0, -1};
+            if (i < P.N) r[k] = old_row(P, i);
         }
-        const unsigned some = __ballot_sync(~0u, fresh);
         __syncthreads();
-        if (lane == 0) part[warp] = __popc(some);
-        __syncthreads();
-        int before = carry;
-        for (int k = 0; k < T / 32; ++k) {
-            if (k < warp) before += part[k];
-            carry += part[k];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int i = base + k * T + threadIdx.x;
+            some[k] = __ballot_sync(~0u, r[k].last >= 0 && first[r[k].source] != i);
+            if (lane == 0) part[k][warp] = __popc(some[k]);
         }
-        if (i < P.N) number[i] = fresh ? before + __popc(some & ((1u << lane) - 1)) : -1;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int i = base + k * T + threadIdx.x;
+            const int each = lane < T / 32 ? part[k][lane] : 0;
+            const int before = carry + __reduce_add_sync(~0u, lane < warp ? each : 0);
+            carry += __reduce_add_sync(~0u, each);
+            if (i < P.N) number[i] = some[k] >> lane & 1 ? before + __popc(some[k] & ((1u << lane) - 1)) : -1;
+        }
     }
     if (write && threadIdx.x == 0) *P.used = carry;
 }
@@ -86,24 +96,25 @@ __global__ void __launch_bounds__(kThreads) fork_first_kernel(const __grid_const
 
 __global__ void __launch_bounds__(1024) fork_numbers_kernel(const __grid_constant__ ForkParams P) { fork_numbers<1024>(P, P.first, P.number, true); }
 
+constexpr int kWide = 1024;                  // threads where a block goes through all rows
+
 template <bool FUSED>
-__global__ void __launch_bounds__(kThreads) fork_fill_kernel(const __grid_constant__ ForkParams P) {
+__global__ void __launch_bounds__(kWide) fork_fill_kernel(const __grid_constant__ ForkParams P) {
     extern __shared__ int32_t held[];
     const int32_t* number = P.number;
     if constexpr (FUSED) {
         int32_t *first = held, *mine = held + P.B;
-        for (int s = threadIdx.x; s < P.B; s += kThreads) first[s] = P.N;
+        for (int s = threadIdx.x; s < P.B; s += kWide) first[s] = P.N;
         __syncthreads();
-        for (int i = threadIdx.x; i < P.N; i += kThreads) {
+        for (int i = threadIdx.x; i < P.N; i += kWide) {
             const int s = P.sources[i];
             if (s >= 0 && s < P.B) atomicMin(first + s, i);
         }
-        __syncthreads();
-        fork_numbers<kThreads>(P, first, mine, blockIdx.x == 0);
+        fork_numbers<kWide>(P, first, mine, blockIdx.x == 0);
         __syncthreads();
         number = mine;
     }
-    const int64_t step = (int64_t)gridDim.x * kThreads, me = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t step = (int64_t)gridDim.x * kWide, me = (int64_t)blockIdx.x * kWide + threadIdx.x;
     for (int64_t i = me; i < P.N; i += step) {
         const int page = taken(P, number[i]);
         P.from[i] = page >= 0 ? old_row(P, (int)i).last : -1;
@@ -205,65 +216,96 @@ struct FreeParams {
     int32_t pages, words, page;
 };
 
-__global__ void __launch_bounds__(kThreads) free_mark_kernel(const __grid_constant__ FreeParams P) {
-    const int warps = gridDim.x * (kThreads / 32), lane = threadIdx.x & 31;
+// Marks what the tables name, a warp a row, four entries a lane at a time.
+__device__ __forceinline__ void mark_rows(const FreeParams& P, uint32_t* bits, int first, int warps) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
     for (int t = 0; t < 2; ++t)
-        for (int b = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); b < P.rows[t]; b += warps) {
+        for (int b = first; b < P.rows[t]; b += warps) {
             const uint32_t need = ((uint32_t)max(P.lens[t][b], 0) + P.page - 1) / (uint32_t)P.page;
             const int have = (int)min(need, (uint32_t)P.width[t]);
-            for (int j = lane; j < have; j += 32) {
-                const int id = P.table[t][(int64_t)b * P.width[t] + j];
-                if (id >= 0 && id < P.pages) atomicOr(P.bits + (id >> 5), 1u << (id & 31));
+            const int32_t* row = P.table[t] + (int64_t)b * P.width[t];
+            for (int j = lane; j < have; j += 128) {
+                int id[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) id[k] = j + k * 32 < have ? row[j + k * 32] : -1;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (id[k] >= 0 && id[k] < P.pages) atomicOr(bits + (id[k] >> 5), 1u << (id[k] & 31));
             }
         }
 }
 
-// Free pages among the 32 of a word.
-__device__ __forceinline__ uint32_t spare_of(const FreeParams& P, int word) {
+__global__ void __launch_bounds__(kThreads) free_mark_kernel(const __grid_constant__ FreeParams P) {
+    mark_rows(P, P.bits, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32));
+}
+
+// Free pages among the 32 of a word; the words behind the last are a whole vector's, and 0.
+__device__ __forceinline__ uint32_t spare_of(const FreeParams& P, uint32_t bits, int word) {
     if (word >= P.words) return 0u;
-    const uint32_t beyond = word == P.words - 1 && (P.pages & 31) ? ~0u << (P.pages & 31) : 0u;
-    return ~(P.bits[word] | beyond);
+    return ~bits & (word == P.words - 1 && (P.pages & 31) ? ~(~0u << (P.pages & 31)) : ~0u);
 }
 
-__device__ __forceinline__ int block_sum(int v) {
-    __shared__ int part[kThreads / 32];
-    v = __reduce_add_sync(~0u, v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int k = 0; k < kThreads / 32; ++k) all += part[k];
-    return all;
-}
+constexpr int kList = 1024;
 
-// Every block counts the free pages before its own words, and of all of them, itself.
-__global__ void __launch_bounds__(kThreads) free_list_kernel(const __grid_constant__ FreeParams P) {
-    const int per = (P.words + gridDim.x - 1) / gridDim.x, begin = min((int)blockIdx.x * per, P.words), end = min(begin + per, P.words);
+// The list of words [begin, end), and this block's share of the -1 behind the list: every block counts the free pages before its own
+// words, and of all of them, itself, sixteen words a thread at a time.
+__device__ __forceinline__ void list_words(const FreeParams& P, const uint32_t* bits, int begin, int end, int block, int blocks) {
+    __shared__ int part[2][kList / 32], totals[kList / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int before = 0, all = 0;
-    for (int w = threadIdx.x; w < P.words; w += kThreads) {
-        const int n = __popc(spare_of(P, w));
-        all += n;
-        if (w < begin) before += n;
+    const uint4* quads = reinterpret_cast<const uint4*>(bits);
+    const int n = (P.words + 3) / 4;
+    for (int w = threadIdx.x; w < n; w += 4 * kList) {
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = w + k * kList < n ? quads[w + k * kList] : make_uint4(~0u, ~0u, ~0u, ~0u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = (w + k * kList) * 4;
+            const uint32_t x[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int spare = __popc(spare_of(P, x[e], at + e));
+                all += spare;
+                before += at + e < begin ? spare : 0;
+            }
+        }
     }
-    before = block_sum(before);
-    all = block_sum(all);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = (end - begin + kThreads / 32 - 1) / (kThreads / 32);
-    const int w0 = min(begin + warp * share, end), w1 = min(w0 + share, end);
-    __shared__ int totals[kThreads / 32];
+    before = __reduce_add_sync(~0u, before);
+    all = __reduce_add_sync(~0u, all);
+    const int share = (end - begin + kList / 32 - 1) / (kList / 32), w0 = min(begin + warp * share, end), w1 = min(w0 + share, end);
     int mine = 0;
-    for (int w = w0 + lane; w < w1; w += 32) mine += __popc(spare_of(P, w));
+    for (int w = w0 + lane; w < w1; w += 32) mine += __popc(spare_of(P, bits[w], w));
     mine = __reduce_add_sync(~0u, mine);
-    if (lane == 0) totals[warp] = mine;
+    if (lane == 0) { part[0][warp] = before; part[1][warp] = all; totals[warp] = mine; }
     __syncthreads();
-    for (int k = 0; k < warp; ++k) before += totals[k];
+    before = __reduce_add_sync(~0u, part[0][lane] + (lane < warp ? totals[lane] : 0));
+    all = __reduce_add_sync(~0u, part[1][lane]);
     for (int w = w0; w < w1; ++w) {
-        const uint32_t spare = spare_of(P, w);
+        const uint32_t spare = spare_of(P, bits[w], w);
         if (spare >> lane & 1) P.out[before + __popc(spare & ((1u << lane) - 1))] = w * 32 + lane;
         before += __popc(spare);
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *P.count = all;
-    for (int64_t i = all + (int64_t)blockIdx.x * kThreads + threadIdx.x; i < P.pages; i += (int64_t)gridDim.x * kThreads) P.out[i] = -1;
+    if (block == 0 && threadIdx.x == 0) *P.count = all;
+    for (int64_t i = all + (int64_t)block * kList + threadIdx.x; i < P.pages; i += (int64_t)blocks * kList) P.out[i] = -1;
+}
+
+__global__ void __launch_bounds__(kList) free_list_kernel(const __grid_constant__ FreeParams P) {
+    const int per = (P.words + gridDim.x - 1) / gridDim.x, begin = min((int)blockIdx.x * per, P.words);
+    list_words(P, P.bits, begin, min(begin + per, P.words), blockIdx.x, gridDim.x);
+}
+
+// Small caches and tables: one block, the marks in shared memory.
+constexpr int kAlonePages = 65536, kAloneEntries = 32768;
+
+__global__ void __launch_bounds__(kList) free_alone_kernel(const __grid_constant__ FreeParams P) {
+    __shared__ __align__(16) uint32_t bits[kAlonePages / 32 + 4];
+    for (int w = threadIdx.x; w < (P.words + 3) / 4 * 4; w += kList) bits[w] = 0;
+    __syncthreads();
+    mark_rows(P, bits, threadIdx.x >> 5, kList / 32);
+    __syncthreads();
+    list_words(P, bits, 0, P.words, 0, 1);
 }
 
 }  // namespace
@@ -298,15 +340,15 @@ int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, cons
                           (int32_t)B, (int32_t)N, (int32_t)width, (int32_t)free_count, (int32_t)page_size};
     const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const int64_t most = N * (width > 0 ? width : 1), sms = rlcs_device::limits().sms;
-    int64_t blocks = (most + kThreads * 4 - 1) / (kThreads * 4);
-    blocks = blocks < 1 ? 1 : blocks > 4 * sms ? 4 * sms : blocks;
+    int64_t blocks = (most + kWide * 2 - 1) / (kWide * 2);
+    blocks = blocks < 1 ? 1 : blocks > 2 * sms ? 2 * sms : blocks;
     if (need == 0) {
-        fork_fill_kernel<true><<<(unsigned)blocks, kThreads, (B + N) * sizeof(int32_t), s>>>(P);
+        fork_fill_kernel<true><<<(unsigned)blocks, kWide, (B + N) * sizeof(int32_t), s>>>(P);
     } else {
         if (cudaMemsetAsync(first, 0x7f, (size_t)B * sizeof(int32_t), s) != cudaSuccess) return RLCS_ERR_CUDA;
         fork_first_kernel<<<(unsigned)((N + kThreads - 1) / kThreads < 4 * sms ? (N + kThreads - 1) / kThreads : 4 * sms), kThreads, 0, s>>>(P);
         fork_numbers_kernel<<<1, 1024, 0, s>>>(P);
-        fork_fill_kernel<false><<<(unsigned)blocks, kThreads, 0, s>>>(P);
+        fork_fill_kernel<false><<<(unsigned)blocks, kWide, 0, s>>>(P);
     }
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }
@@ -346,7 +388,7 @@ int rlcs_copy_pages_bf16(uint16_t* k_cache, uint16_t* v_cache, int64_t pages, in
 }
 
 size_t rlcs_free_pages_workspace_bytes(int64_t num_pages) {
-    return num_pages <= 0 || num_pages > (int64_t(1) << 31) - 1 ? 0 : (size_t)((num_pages + 31) / 32) * sizeof(uint32_t);
+    return num_pages <= 0 || num_pages > (int64_t(1) << 31) - 1 ? 0 : (size_t)((num_pages + 127) / 128) * 16;      // whole vectors of marks
 }
 
 int rlcs_free_pages(const int32_t* block_table, const int32_t* lens, const int32_t* prefix_table, const int32_t* prefix_lens,
@@ -372,11 +414,15 @@ int rlcs_free_pages(const int32_t* block_table, const int32_t* lens, const int32
     FreeParams P = {{block_table, prefix_table}, {lens, prefix_lens}, {(int32_t)B, (int32_t)groups}, {(int32_t)width, (int32_t)prefix_width},
                     static_cast<uint32_t*>(workspace), free_pages, free_count, (int32_t)num_pages, (int32_t)((num_pages + 31) / 32),
                     (int32_t)page_size};
-    const int64_t sms = rlcs_device::limits().sms, rows = (B > groups ? B : groups), blocks = (rows + kThreads / 32 - 1) / (kThreads / 32);
-    if (need > 0 && cudaMemsetAsync(workspace, 0, need, s) != cudaSuccess) return RLCS_ERR_CUDA;
-    if (rows > 0) free_mark_kernel<<<(unsigned)(blocks < 8 * sms ? blocks : 8 * sms), kThreads, 0, s>>>(P);
-    const int64_t parts = (P.words + kThreads - 1) / kThreads;
-    free_list_kernel<<<(unsigned)(parts < 1 ? 1 : parts < sms ? parts : sms), kThreads, 0, s>>>(P);
+    if (num_pages <= kAlonePages && B * width + groups * prefix_width <= kAloneEntries) {
+        free_alone_kernel<<<1, kList, 0, s>>>(P);
+    } else {
+        const int64_t sms = rlcs_device::limits().sms, rows = B > groups ? B : groups, blocks = (rows + kThreads / 32 - 1) / (kThreads / 32);
+        if (need > 0 && cudaMemsetAsync(workspace, 0, need, s) != cudaSuccess) return RLCS_ERR_CUDA;
+        if (rows > 0) free_mark_kernel<<<(unsigned)(blocks < 8 * sms ? blocks : 8 * sms), kThreads, 0, s>>>(P);
+        const int64_t parts = (P.words + kThreads - 1) / kThreads;
+        free_list_kernel<<<(unsigned)(parts < 1 ? 1 : parts < sms ? parts : sms), kList, 0, s>>>(P);
+    }
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }
 
