@@ -262,6 +262,13 @@ def _ptr(t, dtype_kind: str, shape=None):
 def _alloc(shape, dtype, device):
     """Device memory for outputs and workspaces the binding creates itself (torch's allocator).  A
     module-level function so that a test harness can substitute an allocator that adds guard bands."""
+    n = len(shape)                                            # with strides given, torch takes 1.5 us instead of 2.4
+    if n == 1:
+        return _torch().empty_strided(shape, (1,), dtype=dtype, device=device)
+    if n == 2:
+        return _torch().empty_strided(shape, (shape[1], 1), dtype=dtype, device=device)
+    if n == 3:
+        return _torch().empty_strided(shape, (shape[1] * shape[2], shape[2], 1), dtype=dtype, device=device)
     return _torch().empty(shape, dtype=dtype, device=device)
 
 
@@ -1037,11 +1044,12 @@ _scratch_bytes: dict = {}              # workspace bytes by entry point and size
 def _scratch(query: str, sizes, workspace, device: int):
     """(pointer, bytes, tensor) of a call's workspace: the caller's, checked, or one of the call's own from torch's allocator."""
     if workspace is None:
-        need = _scratch_bytes.get((query, sizes))
+        key = (query, *sizes)
+        need = _scratch_bytes.get(key)
         if need is None:
             if len(_scratch_bytes) >= 4096:
                 _scratch_bytes.clear()
-            need = _scratch_bytes[query, sizes] = int(getattr(lib(), query)(*sizes))
+            need = _scratch_bytes[key] = int(getattr(lib(), query)(*sizes))
         if need == 0:
             return None, 0, None
         workspace = _new((need,), _torch().uint8, device)
@@ -1059,9 +1067,11 @@ def _caches(k_cache, v_cache, device: int):
     """Strides of a pair of caches [pages, page, Hk, d] whose rows of d are contiguous."""
     if k_cache.dim() != 4 or (v_cache is not None and v_cache.shape != k_cache.shape):
         raise ValueError("expected caches [pages, page, Hk, d] of one shape")
-    for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if t is not None and not (t.dtype == _dtype("bf16") and t.is_cuda and t.get_device() == device):
-            _refuse(t, "bf16", None, what)
+    bf16 = _dtype("bf16")
+    if k_cache.dtype != bf16 or k_cache.get_device() != device:
+        _refuse(k_cache, "bf16", None, "k_cache")
+    if v_cache is not None and (v_cache.dtype != bf16 or v_cache.get_device() != device):
+        _refuse(v_cache, "bf16", None, "v_cache")
     s = k_cache.stride()
     if s[3] != 1:
         raise ValueError("d of the caches must be contiguous")

@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 1) verify_draw_kernel(cons
     int drawn = -1;                                          // the token of row r, where this thread has it
     const T* const x = P.logits + r * P.ld;
     if (greedy || top == -INFINITY) {
-        if (rank == 0 && tid == 0 && top != -INFINITY) drawn = stat[0].best;
+        if (rank == 0 && tid == 0 && top != -INFINITY) drawn = max(0, min(stat[0].best, P.A - 1));      // rows of offsets that do not ascend may hold anything
         if (ranks > 1 && turns == 0) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     } else {
         const double p_unit = kShareOne / (double)sums[0], q_unit = sums[1] > 0 ? kShareOne / (double)sums[1] : 0.;

@@ -182,6 +182,29 @@ def test_chunk_layouts_strides_and_bounds():
         check_chunks([300, 210], [new, 7], 8, 2, 128, 20, factor=6.0)
 
 
+def test_chunk_many_trajectories():
+    """More trajectories than the lookup goes through level by level, of all sizes, some of them empty."""
+    g = torch.Generator().manual_seed(4)
+    counts = [int(c) for c in torch.randint(0, 4, (200,), generator=g)]
+    counts[7], counts[100], counts[199] = 90, 33, 200
+    check_chunks([c + int(k) for c, k in zip(counts, torch.randint(0, 60, (200,), generator=g))], counts, 8, 2, 64, 16, first=1, behind=2)
+    counts = [int(c) for c in torch.randint(0, 3, (150,), generator=g)]
+    check_chunks([c + int(k) for c, k in zip(counts, torch.randint(0, 60, (150,), generator=g))], counts, 4, 2, 128, 16)
+
+
+def test_chunk_lengths_out_of_all_proportion(api):
+    """Lengths beyond the table, up to the largest number: what the table holds is seen; negative ones: nothing."""
+    for new in (2, 100):
+        cache = Paged(5, [320], 16, 2, 64)
+        q = torch.randn(new, 4, 64, generator=torch.Generator().manual_seed(9)).to(BF16)
+        args = (up(q), cache.kd, cache.vd, up(cache.table), up(ints([0, new])))
+        want = api.chunk_attention(*args, up(ints([320 + new])))
+        got = api.chunk_attention(*args, up(ints([2 ** 31 - 1])))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        out, lse = api.chunk_attention(*args, up(ints([-2 ** 31])))
+        assert (out == 0).all() and (lse == -math.inf).all()
+
+
 def test_chunk_longer_than_max_new_is_cut(api):
     from paper_2608_17641_b200 import binding
     for most, new in ((2, 6), (90, 300)):
@@ -404,6 +427,12 @@ def test_verify_wide_rows_and_many_trajectories(api, A, B, dtype):
     want = check_verify(api, x, tokens, offsets, u, du, drafts, temps=0.9, pad=1)
     assert B < 100 or (any(a == 0 for a in want[2]) and any(a == 2 for a in want[2]))
     check_verify(api, x, tokens, offsets, u, du, None, temps=1.1)
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_verify_rows_too_wide_for_shared_memory(api, drawn):
+    x, tokens, offsets, u, du, drafts = verify_inputs([3], 500001, BF16, 2, near=0.3)
+    check_verify(api, x, tokens, offsets, u, du, drafts if drawn else None, pad=3)
 
 
 @pytest.mark.parametrize("A", [9, 3000])
@@ -954,3 +983,44 @@ def test_prepared_calls_repeat_the_direct_ones(api):
         for _ in range(2):
             for a, b in zip(call(), want):
                 assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------ the example
+def test_operators_work_together_in_the_example(api):
+    """Two rounds of generation: the log-probabilities that verification reported along the way, through pages given back and
+    tables forked, against a dense recomputation from the tokens alone.  Logits of up to 10 are bfloat16 on both sides, off by 2^-8 of
+    themselves each, from hidden states that are bfloat16 too: 0.16 a token bounds it, a wrong page costs whole units."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import speculative_rollout as ex
+    generator = torch.Generator(device="cuda").manual_seed(1)
+    target, draft = ex.Target(generator), ex.Draft(generator)
+    for _ in range(2):
+        prompts = torch.randint(0, ex.VOCAB, (ex.ROWS, ex.PROMPT), device="cuda", generator=generator, dtype=torch.int32)
+        texts, total, kept, losses = ex.generate(target, draft, prompts, generator, rate=2.0)
+        assert len(kept) == len(losses) and all(math.isfinite(v) for v in losses) and 0 <= min(kept) <= max(kept) <= ex.DRAFTS
+        for b in range(ex.ROWS):
+            text = torch.tensor(texts[b], device="cuda")
+            x = target.embed[text].float()
+            q = (x @ target.wq.float()).view(-1, ex.HEADS, ex.DIM)
+            k, v = (t.repeat_interleave(ex.HEADS // ex.KV_HEADS, 1) for t in (x @ target.wkv.float()).view(-1, 2, ex.KV_HEADS, ex.DIM).unbind(1))
+            c = torch.einsum("ihd,jhd->hij", q, k) * ex.DIM ** -0.5
+            c = c.masked_fill(torch.ones(len(text), len(text), device="cuda").triu(1).bool(), -math.inf)
+            a = torch.einsum("hij,jhd->ihd", torch.softmax(c, -1), v).reshape(len(text), -1)
+            lp = torch.log_softmax(torch.tanh(x + a @ target.wo.float()) @ target.out.float(), 1)
+            new = torch.arange(ex.PROMPT, len(text), device="cuda")
+            want = lp[new - 1, text[new]].sum()
+            assert abs(float(total[b] - want)) <= 0.16 * len(new), (b, float(total[b]), float(want))
+    # the draft policy's gradient against autograd
+    before, last = (torch.randint(0, ex.VOCAB, (20,), device="cuda", generator=generator) for _ in range(2))
+    teacher = torch.randn(20, ex.VOCAB, device="cuda", generator=generator)
+    top, ids = teacher.topk(ex.TOP, 1)
+    features = draft.features(before, last)
+    out = draft.out.double().requires_grad_()
+    lq = torch.log_softmax(features.double() @ out, 1)
+    p = torch.softmax(top.double(), 1)
+    ((p * (p.log() - lq.gather(1, ids))).sum() / 20).backward()
+    _, grad = api.compute_distillation(features @ draft.out, ids.int(), top, scale=1 / 20)
+    # products of 256 fp32 terms: 2^-16 of their size
+    assert (features.t() @ grad - out.grad).abs().max() <= 2.0 ** -15 * out.grad.abs().max() + 1e-6
