@@ -247,31 +247,28 @@ template <typename T> __device__ __forceinline__ RowStat join_parts(const Verify
     return r;
 }
 
-// Weights of the n entries from x on, by the NT threads of a block: written to `to` (16-byte aligned at the row's first vector) and added
-// up.  `top` is finite: an entry that equals it is 0 away, and one of -inf or NaN ends as 0.
-template <typename T, int NT> __device__ __forceinline__ u64 weigh_row(const T* x, int n, float top, float inv, uint32_t* to) {
-    constexpr int N = Vec<T>::N;
-    const Span sp = span_of(x, n);
-    const int tid = threadIdx.x, rest = sp.head + sp.vecs * N;
-    u64 sum = 0;
-    for (int i = tid; i < sp.head + n - rest; i += NT) {
-        const int j = i < sp.head ? i : rest + i - sp.head;
-        const uint32_t w = weight_of(e_of(Vec<T>::load(x + j), top, inv));
-        to[j] = w;
-        sum += w;
-    }
-    const uint4* body = reinterpret_cast<const uint4*>(x + sp.head);
-    uint4* out = reinterpret_cast<uint4*>(to + sp.head);
-    for (int i = tid; i < sp.vecs; i += NT) {
-        float e[N];
-        const uint4 v = body[i];
+// A row's part as a block weighs it: n entries from x on, their maximum finite; their weights go to `to` (16-byte aligned at the row's
+// first vector).  An entry that equals the maximum is 0 away, and one of -inf or NaN ends as 0.
+template <typename T> struct Weigher {
+    static constexpr int N = Vec<T>::N;
+    const T* x;
+    uint32_t* to;
+    Span sp;
+    int n;
+    float top, inv;
+
+    __device__ __forceinline__ uint4 load(int i) const { return reinterpret_cast<const uint4*>(x + sp.head)[i]; }
+
+    __device__ __forceinline__ u64 vector(int i, const uint4& v) const {
+        uint4* const out = reinterpret_cast<uint4*>(to + sp.head) + i * (N / 4);
         // a vector of nothing but weights of 0 (exp below 2^-32): -inf counts among them, NaN is passed over
         const float best = Vec<T>::most_number_of(Vec<T>::most_number(Vec<T>::most_number(v.x, v.y), Vec<T>::most_number(v.z, v.w)));
         if ((best - top) * inv < -22.5f) {
 #pragma unroll
-            for (int j = 0; j < N; j += 4) out[i * (N / 4) + j / 4] = make_uint4(0, 0, 0, 0);
-            continue;
+            for (int j = 0; j < N; j += 4) out[j / 4] = make_uint4(0, 0, 0, 0);
+            return 0;
         }
+        float e[N];
         Vec<T>::unpack(v, e);
         float most = 0.f;
 #pragma unroll
@@ -280,6 +277,7 @@ template <typename T, int NT> __device__ __forceinline__ u64 weigh_row(const T* 
             most = max_nan(most, e[j]);
         }
         uint32_t w[N];
+        u64 sum = 0;
         if (most < 0x1p-10f) {                               // nearly always: weight_of's short way, sums of 2^24 at most
             uint32_t all = 0;
 #pragma unroll
@@ -287,7 +285,7 @@ template <typename T, int NT> __device__ __forceinline__ u64 weigh_row(const T* 
                 w[j] = (__float_as_uint(__fmaf_rd(e[j], 0x1p31f, 4194304.5f)) & 0x7fffffu) >> 1;
                 all += w[j];
             }
-            sum += all;
+            sum = all;
         } else {
 #pragma unroll
             for (int j = 0; j < N; ++j) {
@@ -296,9 +294,27 @@ template <typename T, int NT> __device__ __forceinline__ u64 weigh_row(const T* 
             }
         }
 #pragma unroll
-        for (int j = 0; j < N; j += 4) out[i * (N / 4) + j / 4] = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+        for (int j = 0; j < N; j += 4) out[j / 4] = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+        return sum;
     }
-    return sum;
+
+    __device__ __forceinline__ u64 singles(int first, int step) const {
+        u64 sum = 0;
+        const int rest = sp.head + sp.vecs * N;
+        for (int i = first; i < sp.head + n - rest; i += step) {
+            const int j = i < sp.head ? i : rest + i - sp.head;
+            const uint32_t w = weight_of(e_of(Vec<T>::load(x + j), top, inv));
+            to[j] = w;
+            sum += w;
+        }
+        return sum;
+    }
+};
+
+// The sum over a warp of numbers below 2^60: three hardware sums.
+__device__ __forceinline__ u64 redux_sum(u64 v) {
+    const uint32_t a = __reduce_add_sync(~0u, (uint32_t)v & 0xfffffu), b = __reduce_add_sync(~0u, (uint32_t)(v >> 20) & 0xfffffu);
+    return (u64)a + ((u64)b << 20) + ((u64)__reduce_add_sync(~0u, (uint32_t)(v >> 40)) << 40);
 }
 
 // 2^52 + floor(w unit), for floor(w unit) < 2^52, as the bits of a double: differences of two are those of the floors.  Conversions between
@@ -314,7 +330,7 @@ __device__ __noinline__ float score(double all, float x, float top, float inv) {
 template <typename T, int NT, bool HELD>
 __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 1) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
     extern __shared__ __align__(16) uint32_t held[];         // [2][share and up to a vector before it]
-    __shared__ u64 part[2][NT / 32], sent[2][16][2];
+    __shared__ u64 part[2][NT / 32], sent[2][16][2], total_of[2];
     __shared__ RowStat stat[2];                              // of row r below
     __shared__ int stop;                                     // least 2 t + 1 of a row whose draft does not stay, 2 t where that is unclear
     const cg::cluster_group cluster = cg::this_cluster();
@@ -330,25 +346,30 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 1) verify_draw_kernel(cons
     const bool greedy = !(temperature > 0.f);
     const int j0 = min(rank * P.share, P.A), j1 = min(j0 + P.share, P.A);
 
-    // (x, y), the same for all lanes of a warp, summed over the cluster; x stays in part[0].  Two sets of places, taken in turn.
+    // (x, y), the same for all lanes of a warp, summed over the cluster by the first warp; x stays in part[0].  Two sets of places, in turn.
     int turns = 0;
     auto cluster_sum = [&](u64* x, u64* y) {
         __syncthreads();
         if (lane == 0) { part[0][warp] = *x; part[1][warp] = *y; }
         __syncthreads();
-        *x = warp_sum(lane < NT / 32 ? part[0][lane] : 0);
-        *y = warp_sum(lane < NT / 32 ? part[1][lane] : 0);
-        if (ranks == 1) return;
         const int turn = turns++ & 1;
-        if (turns == 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");            // all of the cluster's blocks run
-        if (tid < ranks) {
-            u64* to = cluster.map_shared_rank(&sent[turn][rank][0], tid);
-            to[0] = *x;
-            to[1] = *y;
+        if (ranks > 1 && turns == 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // all of the cluster's blocks run
+        if (warp == 0) {
+            const u64 a = redux_sum(lane < NT / 32 ? part[0][lane] : 0), c = redux_sum(lane < NT / 32 ? part[1][lane] : 0);
+            if (lane < ranks) {
+                u64* to = cluster.map_shared_rank(&sent[turn][rank][0], lane);
+                to[0] = a;
+                to[1] = c;
+            }
         }
-        cluster.sync();
-        *x = warp_sum(lane < ranks ? sent[turn][lane][0] : 0);
-        *y = warp_sum(lane < ranks ? sent[turn][lane][1] : 0);
+        if (ranks > 1) cluster.sync(); else __syncthreads();
+        if (warp == 0) {
+            const u64 a = redux_sum(lane < ranks ? sent[turn][lane][0] : 0), c = redux_sum(lane < ranks ? sent[turn][lane][1] : 0);
+            if (lane == 0) { total_of[0] = a; total_of[1] = c; }
+        }
+        __syncthreads();
+        *x = total_of[0];
+        *y = total_of[1];
     };
     // does u (v W) < w V hold?
     auto decide = [&](int t, double w, double W, double v, double V) { return (double)P.uniforms[t] * (v * W) < w * V; };
@@ -401,23 +422,41 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 1) verify_draw_kernel(cons
         turned = r + 1 < end;
         two = turned && P.drafts != nullptr;
         if (greedy || stat[0].top == -INFINITY) break;
-        sums[0] = sums[1] = 0;
-#pragma unroll 1
-        for (int which = 0; which < (two ? 2 : 1); ++which) {
-            const T* x = which ? P.drafts + r * P.ldd : P.logits + r * P.ld;
-            const float top = stat[which].top;
-            uint32_t* to = held + which * (P.share + 8);
-            u64 sum = 0;
-            if (HELD && top != -INFINITY && top < INFINITY) {
-                sum = weigh_row<T, NT>(x + j0, j1 - j0, top, inv, to + lead(x));
-            } else {
-                for (int j = j0 + tid; j < j1; j += NT) {
-                    const uint32_t w = top == -INFINITY ? 0 : weight_of(e_of(Vec<T>::load(x + j), top, inv));
-                    if (HELD) to[lead(x) + j - j0] = w;
-                    sum += w;
+        Weigher<T> of[2];
+        bool quick[2];
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            of[which].x = (which ? P.drafts + r * P.ldd : P.logits + r * P.ld) + j0;
+            of[which].n = j1 - j0;
+            of[which].top = stat[which].top;
+            of[which].inv = inv;
+            quick[which] = HELD && (which == 0 || two) && stat[which].top != -INFINITY && stat[which].top < INFINITY;
+            of[which].sp = quick[which] ? span_of(of[which].x, j1 - j0) : Span{0, 0};
+            of[which].to = held + which * (P.share + 8) + (which == 0 || two ? lead(of[which].x - j0) : 0);
+            sums[which] = 0;
+        }
+        // both rows' vectors are on the way together
+        for (int i = tid; i < max(of[0].sp.vecs, of[1].sp.vecs); i += NT) {
+            uint4 v[2];
+#pragma unroll
+            for (int which = 0; which < 2; ++which)
+                if (i < of[which].sp.vecs) v[which] = of[which].load(i);
+#pragma unroll
+            for (int which = 0; which < 2; ++which)
+                if (i < of[which].sp.vecs) sums[which] += of[which].vector(i, v[which]);
+        }
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (quick[which]) {
+                sums[which] += of[which].singles(tid, NT);
+            } else if (which == 0 || two) {
+                for (int j = tid; j < j1 - j0; j += NT) {
+                    const uint32_t w = of[which].top == -INFINITY ? 0 : weight_of(e_of(Vec<T>::load(of[which].x + j), of[which].top, inv));
+                    if (HELD) of[which].to[j] = w;
+                    sums[which] += w;
                 }
             }
-            (which ? sums[1] : sums[0]) = warp_sum(sum);
+            sums[which] = redux_sum(sums[which]);
         }
         cluster_sum(&sums[0], &sums[1]);
         if (clear) break;
@@ -468,7 +507,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 1) verify_draw_kernel(cons
             mine = 0;
 #pragma unroll 4
             for (int j = k0 + lane; j < k1; j += 32) mine += weight(j);
-            total = mine = warp_sum(mine);
+            total = mine = redux_sum(mine);
             cluster_sum(&total, &none);
             if (total > 0 || plain) break;
             plain = true;                                     // nothing is left of the difference: the target's own probabilities
@@ -476,7 +515,7 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 1) verify_draw_kernel(cons
         const u64 target = target_of(P.draw_uniforms[b], total);
         u64 before = lane < warp ? part[0][lane] : 0;
         if (lane < rank) before += sent[(turns - 1) & 1][lane][0];
-        before = warp_sum(before);
+        before = redux_sum(before);
         if (before <= target && target < before + mine) {
             for (int base = k0; base < k1; base += 32) {
                 const int j = base + lane;
