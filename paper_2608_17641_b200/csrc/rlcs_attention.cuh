@@ -444,18 +444,25 @@ template <typename F> bool grant(F kernel, int bytes, bool* granted) {
     return granted[dev];
 }
 
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder of tensor maps, null where it has none.
+inline EncodeTiled encode_tiled() {
+    static const EncodeTiled encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess) fn = nullptr;
+        return reinterpret_cast<EncodeTiled>(fn);
+    }();
+    return encode;
+}
+
 // The cache as a map of boxes [at most `rows` places of a page, 64 dimensions]; false where pages cannot be cut into such boxes of at
 // least eight places, or the driver takes no such strides.
 inline bool box_map(CUtensorMap* map, const AttnParams& P, const void* base, int rows) {
     if (P.page >= rows ? P.page % rows != 0 : P.page < 8 || rows % P.page != 0) return false;
-    typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const Encode encode = [] {
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess) fn = nullptr;
-        return reinterpret_cast<Encode>(fn);
-    }();
+    const EncodeTiled encode = encode_tiled();
     if (encode == nullptr || P.pages < 1) return false;
     const cuuint64_t extent[4] = {(cuuint64_t)P.d, (cuuint64_t)P.page, (cuuint64_t)P.Hk, (cuuint64_t)P.pages};
     const cuuint64_t stride[3] = {(cuuint64_t)P.token_stride * 2, (cuuint64_t)P.head_stride * 2, (cuuint64_t)P.page_stride * 2};

@@ -17,6 +17,7 @@ struct ChunkParams {
     int tiles;                     // of 16 rows, a trajectory; 0: blocks of 128 rows
     int slots;                     // of blocks of 128 rows over all trajectories
     uint32_t r_mul;                // ceil(2^32 / r); 0 for r = 1
+    int boxes;                     // whether a block's queries come, and its outputs leave, as boxes of whole tokens
 };
 
 struct Chunk {
@@ -91,6 +92,16 @@ chunk_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUte
 // (377, 488 us, and 216 for the chunks of drafts: nothing runs under a block's start and end); 128 keys a step into a single
 // buffer (467, 516: scores, weights and values in turn, some 250 cycles at every barrier); a quarter of the exponentials by polynomial (no change).
 constexpr int kKeys = 64, kRows = 128, kWideThreads = 256, kCopiers = 64, kMostSegment = 65536;
+
+// Boxes of queries and outputs [T, H, d].
+__device__ __forceinline__ void box_load3(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
+__device__ __forceinline__ void box_store3(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
 
 // Products and commits are issued by one thread of a warp: elected once, it waits and issues by itself, which takes a third of the
 // time at each barrier that a whole warp with an election an instruction takes.
@@ -190,7 +201,8 @@ __device__ __forceinline__ WideTile wide_tile(const ChunkParams& C, int slot, in
 
 template <int D, bool TMA>
 __global__ void __launch_bounds__(kWideThreads, 2)
-wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+            const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap out_map) {
     typedef WideShape<D> Shape;
     constexpr int kSlots = Shape::kSlots, kPieces = D / 8;
     constexpr uint32_t kScores = 1u << 4 | 1u << 7 | 1u << 10 | (kKeys >> 3) << 17 | (128 >> 4) << 24;
@@ -217,7 +229,7 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
         gave_up = missing_any = 0;
         for (int i = 0; i < kSlots; ++i) { bar_init(full + 8 * i, TMA ? 1 : kCopiers); bar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(p_full + 8 * i, 128); bar_init(o_done + 8 * i, 1); }
-        bar_init(q_full, 128);
+        bar_init(q_full, C.boxes ? 1 : 128);
         bar_init(drained, 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -227,8 +239,8 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
     const uint32_t tmem = tmem_at;
     const int b = which.b, first_row = which.first_row, held = which.held;
     const Chunk c = which.c;
-    const int rows = c.count * P.r;
-    const int begin = seg * P.own_seg, end = b < 0 ? begin : min(begin + P.own_seg, keys_of(C, c, min(first_row + kRows, rows)));
+    const int mine_rows = min(kRows, c.count * P.r - first_row);      // the block's
+    const int begin = seg * P.own_seg, end = b < 0 ? begin : min(begin + P.own_seg, keys_of(C, c, first_row + mine_rows));
     const bool whole_row = P.own_segs <= 1;                       // outputs leave at once, not as parts to be joined
     const int tiles = divide_up_device(end - begin, kKeys);
     const int offset = begin % P.page;
@@ -237,7 +249,7 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
     auto token_of = [&](int k) { return C.r_mul != 0 ? (int)__umulhi((uint32_t)(head0 + k), C.r_mul) : k; };      // from token0 on; (r + 256) r < 2^32
     if (begin >= end) {
         if (b >= 0 && whole_row && seg == 0)
-            for (int i = tid; i < min(kRows, rows - first_row) * (P.d / 8); i += kWideThreads) {
+            for (int i = tid; i < mine_rows * (P.d / 8); i += kWideThreads) {
                 const int row = first_row + i / (P.d / 8);
                 const int64_t at = (int64_t)(c.first + row / P.r) * P.H + kv_head * P.r + row % P.r;
                 *reinterpret_cast<uint4*>(P.out + at * P.d + i % (P.d / 8) * 8) = make_uint4(0, 0, 0, 0);
@@ -245,14 +257,14 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
             }
     } else
     if (warp < 4) {
-        const int row = first_row + warp * 32 + lane;
+        const int row = warp * 32 + lane;                         // of the block's
         const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16), o_at = mine + 128;
-        const bool any_row = first_row + warp * 32 < rows;
-        const int lim = row < rows ? clamp_to(min(c.start + row / P.r + 1, P.max_len) - begin, 0, end - begin) : end - begin;
+        const bool any_row = warp * 32 < mine_rows;
+        const int lim = row < mine_rows ? clamp_to(min(c.start + token0 + token_of(row) + 1, P.max_len) - begin, 0, end - begin) : end - begin;
         const int least = __reduce_min_sync(~0u, lim);
         const int64_t rows_at = (int64_t)(c.first + token0) * P.H + kv_head * P.r;      // of the outputs [T, H]
         auto row_at = [&](int k) { return rows_at + (int64_t)token_of(k) * P.H + (head0 + k - token_of(k) * P.r); };
-        {
+        if (!C.boxes) {
             // the warp's queries, zeros where there are none: kPieces lanes a row
             constexpr int kLoads = kPieces, kTogether = 32 / kPieces;
             uint4 v[kLoads];
@@ -260,7 +272,7 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
             for (int j = 0; j < kLoads; ++j) {
                 const int k = warp * 32 + j * kTogether + lane / kPieces, piece = lane % kPieces, token = token_of(k);
                 v[j] = make_uint4(0, 0, 0, 0);
-                if (first_row + k < rows && piece * 8 < P.d)
+                if (k < mine_rows && piece * 8 < P.d)
                     v[j] = *reinterpret_cast<const uint4*>(P.q + (int64_t)(c.first + token0 + token) * P.q_stride + (int64_t)(kv_head * P.r + head0 + k - token * P.r) * P.d + piece * 8);
             }
 #pragma unroll
@@ -347,9 +359,38 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
             fine = fine && *(volatile int*)&gave_up == 0;         // a thread that copies may have given up alone
             fence_after();
             if (!fine) l = __int_as_float(0x7fffffff);
+        }
+        if (C.boxes && whole_row && mine_rows == kRows) {
+            // whole tokens leave as boxes, through the place of the queries, which are done with; in their layout
             const float inv = l != 0.f ? 1.f / l : 0.f;
-            // rows leave through the place of the warp's queries, which are done with256 bytes of a row at a
-            // time, written by the row's thread, stored by sixteen lanes a row
+#pragma unroll
+            for (int k = 0; k < D; k += 32) {
+                uint32_t o[32];
+                tmem_load32(o, o_at + k);
+                tmem_wait_load();
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    uint32_t w[4];
+                    const int piece = (k + e) / 8;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) w[h] = l == 0.f ? 0u : pack2(__uint_as_float(o[e + 2 * h]) * inv, __uint_as_float(o[e + 2 * h + 1]) * inv);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q_at + (piece >> 3) * (128 * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4)),
+                                 "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+            }
+            fence_async();
+            asm volatile("bar.sync 3, 128;" ::: "memory");
+            if (tid == 0) {
+#pragma unroll
+                for (int half = 0; half < D / 64; ++half)
+                    box_store3(&out_map, q_at + half * (128 * 128), half * 64, kv_head * P.r, c.first + token0);
+                asm volatile("cp.async.bulk.commit_group;\ncp.async.bulk.wait_group.read 0;" ::: "memory");
+            }
+            if (row < mine_rows && P.lse != nullptr) P.lse[row_at(row)] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        } else if (any_row) {
+            // rows leave through the place of the warp's queries, 256 bytes of a row at a time, written by the row's thread, stored by sixteen
+            // lanes a row
+            const float inv = l != 0.f ? 1.f / l : 0.f;
             const uint32_t mine_at = q_at + warp * (Shape::kQ / 4);
             constexpr int kRound = D == 128 ? 16 : 8;                 // 16-byte pieces of a row a round: D values of 16 bits, D / 2 of 32
             char* const parts = reinterpret_cast<char*>(P.part_o + (int64_t)seg * P.B * P.H * D);
@@ -386,20 +427,26 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                     uint4 v;
                     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                                  : "r"(mine_at + k * (kRound * 16) + ((piece ^ (k & (kRound - 1))) << 4)) : "memory");
-                    if (first_row + warp * 32 + k >= rows) continue;
+                    if (warp * 32 + k >= mine_rows) continue;
                     const int64_t at = row_at(warp * 32 + k);
                     if (!whole_row) *reinterpret_cast<uint4*>(parts + at * (D * 4) + round * (D * 2) + piece * 16) = v;
                     else if (piece * 8 < P.d) *reinterpret_cast<uint4*>(P.out + at * P.d + piece * 8) = v;
                 }
             }
-            if (row < rows) {
-                const int64_t at = row_at(warp * 32 + lane);
+            if (row < mine_rows) {
+                const int64_t at = row_at(row);
                 if (!whole_row) P.part_ml[(int64_t)seg * P.B * P.H + at] = fine ? make_float2(m, l) : make_float2(0.f, l);
                 else if (P.lse != nullptr) P.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
             }
         }
         fence_before();
     } else {
+        if (C.boxes && tid == 128) {                              // queries; rows behind the chunk's are somebody else's and come to nothing
+            bar_expect(q_full, (D / 64) * kRows * 128);
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half)
+                box_load3(q_at + half * (128 * 128), &q_map, q_full, half * 64, kv_head * P.r, c.first + token0);
+        }
         // page numbers of the keys, by the four warps that are left; -1: no such page
         {
             const int32_t* table = P.block_table + (int64_t)b * P.own_width;
@@ -416,13 +463,13 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
         }
         if (warp == 4 || warp == 7) {
             const int me = (warp == 4 ? 0 : 32) + lane, piece = me % kPieces, row0 = me / kPieces;
-            constexpr int kStep = kCopiers / kPieces, kRows = kKeys / kStep;
+            constexpr int kStep = kCopiers / kPieces, kEach = kKeys / kStep;
             const uint32_t lane_at = ring + (piece >> 3) * (kKeys * 128);
             auto pieces = [&](int item) {                         // one tile of keys or values, zeros where there is no key
                 const __nv_bfloat16* from = (item & 1 ? P.v : P.k) + kv_head * P.head_stride + piece * 8;
                 const uint32_t dst = lane_at + (item % kSlots) * Shape::kSlot;
 #pragma unroll 4
-                for (int k = 0; k < kRows; ++k) {
+                for (int k = 0; k < kEach; ++k) {
                     const int row = row0 + k * kStep, local = (item >> 1) * kKeys + row;
                     int64_t place = 0;
                     bool there = begin + local < held && piece * 8 < P.d;
@@ -483,6 +530,10 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                 }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
+            if (C.boxes && me == 0) {
+                int late = 0;
+                bar_wait(q_full, 0, &late, kPolls);
+            }
         } else {
             const uint32_t base = __shfl_sync(~0u, tmem, 0);
             if (one_lane()) {
@@ -638,12 +689,25 @@ int launch_chunk(const ChunkParams& C, int64_t blocks, const CUtensorMap& k_map,
     return RLCS_OK;
 }
 
+// Queries or outputs [T, H, d] as a map of boxes [whole tokens of a block, heads on a key head, 64 dimensions].
+bool token_map(CUtensorMap* map, const ChunkParams& C, const void* base, int64_t stride) {
+    const EncodeTiled encode = encode_tiled();
+    if (encode == nullptr) return false;
+    const cuuint64_t extent[3] = {(cuuint64_t)C.a.d, (cuuint64_t)C.a.H, (cuuint64_t)C.a.B};
+    const cuuint64_t strides[2] = {(cuuint64_t)C.a.d * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)C.a.r, (cuuint32_t)(kRows / C.a.r)}, step[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), extent, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, bool TMA>
-int launch_wide(const ChunkParams& C, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t s) {
+int launch_wide(ChunkParams C, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t s) {
+    CUtensorMap q_map = {}, out_map = {};
+    C.boxes = kRows % C.a.r == 0 && token_map(&q_map, C, C.a.q, C.a.q_stride) && token_map(&out_map, C, C.a.out, (int64_t)C.a.H * C.a.d);
     static bool granted[64];
     if (!grant(wide_kernel<D, TMA>, WideShape<D>::kBytes, granted)) return RLCS_ERR_CUDA;
     const int segs = C.a.own_segs > 0 ? C.a.own_segs : 1;         // rows without keys are written too
-    wide_kernel<D, TMA><<<(unsigned)(C.slots * C.a.Hk * segs), kWideThreads, WideShape<D>::kBytes, s>>>(C, k_map, v_map);
+    wide_kernel<D, TMA><<<(unsigned)(C.slots * C.a.Hk * segs), kWideThreads, WideShape<D>::kBytes, s>>>(C, k_map, v_map, q_map, out_map);
     return RLCS_OK;
 }
 
