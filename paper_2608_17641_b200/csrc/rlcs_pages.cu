@@ -144,38 +144,39 @@ struct CopyParams {
     int64_t page_bytes;                                         // of a page without gaps, else 0
 };
 
-constexpr int kPairs = 1024, kPiece = kThreads * 16 * 4;        // bytes a block copies at a time
+constexpr int kPairs = 1024, kCopyBlocks = 4, kPiece = kThreads * 16 * 4;        // bytes a block copies at a time
 
-__global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ CopyParams P) {
+__global__ void __launch_bounds__(kThreads, kCopyBlocks) copy_kernel(const __grid_constant__ CopyParams P) {
     __shared__ int2 pairs[kPairs];
-    __shared__ int count;
+    __shared__ int counts[kPairs / 32];
+    static_assert(kPairs == 32 * 32, "a lane a count");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t bytes = (int64_t)P.page * P.Hk * P.row, pieces = (bytes + kPiece - 1) / kPiece;
     for (int base = 0; base < P.N; base += kPairs) {
-        __syncthreads();
-        if (threadIdx.x == 0) count = 0;
-        __syncthreads();
+        // the pairs that are there, in their order: every block has the same list
         const int most = min(P.N - base, kPairs);
-        for (int i = threadIdx.x; i < (most + 31) / 32 * 32; i += kThreads) {      // in any order: every block copies its share of its own list
-            int a = -1, b = -1;
-            if (i < most) { a = P.from[base + i]; b = P.to[base + i]; }
-            pairs[i] = make_int2(a, b);
+        int2 p[kPairs / kThreads];
+        unsigned some[kPairs / kThreads];
+        __syncthreads();                                      // the last list has been read
+#pragma unroll
+        for (int k = 0; k < kPairs / kThreads; ++k) {
+            const int i = k * kThreads + threadIdx.x;
+            p[k] = i < most ? make_int2(P.from[base + i], P.to[base + i]) : make_int2(-1, -1);
+        }
+#pragma unroll
+        for (int k = 0; k < kPairs / kThreads; ++k) {
+            some[k] = __ballot_sync(~0u, p[k].x >= 0 && p[k].x < P.pages && p[k].y >= 0 && p[k].y < P.pages && p[k].x != p[k].y);
+            if (lane == 0) counts[k * (kThreads / 32) + warp] = __popc(some[k]);
         }
         __syncthreads();
-        // the pairs that are there move to the front, in their order, by the first warp
-        if (threadIdx.x < 32) {
-            int n = 0;
-            for (int i = threadIdx.x; i < (most + 31) / 32 * 32; i += 32) {
-                const int2 p = pairs[i];
-                const bool there = p.x >= 0 && p.x < P.pages && p.y >= 0 && p.y < P.pages && p.x != p.y;
-                const unsigned some = __ballot_sync(~0u, there);
-                if (there) pairs[n + __popc(some & ((1u << threadIdx.x) - 1))] = p;
-                n += __popc(some);
-                __syncwarp();
-            }
-            if (threadIdx.x == 0) count = n;
+        const int each = counts[lane], count = __reduce_add_sync(~0u, each);
+#pragma unroll
+        for (int k = 0; k < kPairs / kThreads; ++k) {
+            const int before = __reduce_add_sync(~0u, lane < k * (kThreads / 32) + warp ? each : 0);
+            if (some[k] >> lane & 1) pairs[before + __popc(some[k] & ((1u << lane) - 1))] = p[k];
         }
         __syncthreads();
-        const int64_t items = count * pieces * P.caches;
+        const int64_t items = (int64_t)count * pieces * P.caches;
         for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
             const int2 p = pairs[w / (pieces * P.caches)];
             const int64_t rest = w % (pieces * P.caches), piece = rest % pieces;
@@ -253,7 +254,7 @@ constexpr int kList = 1024;
 __device__ __forceinline__ void list_words(const FreeParams& P, const uint32_t* bits, int begin, int end, int block, int blocks) {
     __shared__ int part[2][kList / 32], totals[kList / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int before = 0, all = 0;
+    int before = 0, all = 0;                                  // of whole vectors: `begin` is a multiple of four
     const uint4* quads = reinterpret_cast<const uint4*>(bits);
     const int n = (P.words + 3) / 4;
     for (int w = threadIdx.x; w < n; w += 4 * kList) {
@@ -262,14 +263,13 @@ __device__ __forceinline__ void list_words(const FreeParams& P, const uint32_t* 
         for (int k = 0; k < 4; ++k) v[k] = w + k * kList < n ? quads[w + k * kList] : make_uint4(~0u, ~0u, ~0u, ~0u);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int at = (w + k * kList) * 4;
-            const uint32_t x[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int spare = __popc(spare_of(P, x[e], at + e));
-                all += spare;
-                before += at + e < begin ? spare : 0;
-            }
+            const int at = w + k * kList;
+            int spare = __popc(~v[k].x) + __popc(~v[k].y) + __popc(~v[k].z) + __popc(~v[k].w);
+            if (at == n - 1)                                  // words and bits behind the last page count as marked
+                spare = __popc(spare_of(P, v[k].x, at * 4)) + __popc(spare_of(P, v[k].y, at * 4 + 1)) + __popc(spare_of(P, v[k].z, at * 4 + 2)) +
+                        __popc(spare_of(P, v[k].w, at * 4 + 3));
+            all += spare;
+            before += at * 4 < begin ? spare : 0;
         }
     }
     before = __reduce_add_sync(~0u, before);
@@ -292,7 +292,7 @@ __device__ __forceinline__ void list_words(const FreeParams& P, const uint32_t* 
 }
 
 __global__ void __launch_bounds__(kList) free_list_kernel(const __grid_constant__ FreeParams P) {
-    const int per = (P.words + gridDim.x - 1) / gridDim.x, begin = min((int)blockIdx.x * per, P.words);
+    const int per = ((P.words + gridDim.x - 1) / gridDim.x + 3) / 4 * 4, begin = min((int)blockIdx.x * per, (P.words + 3) / 4 * 4);
     list_words(P, P.bits, begin, min(begin + per, P.words), blockIdx.x, gridDim.x);
 }
 
@@ -383,7 +383,7 @@ int rlcs_copy_pages_bf16(uint16_t* k_cache, uint16_t* v_cache, int64_t pages, in
     P.row = (int32_t)(d * 2);
     P.page_bytes = tight || heads_first ? bytes : 0;
     const int64_t sms = rlcs_device::limits().sms, items = N * P.caches * ((bytes + kPiece - 1) / kPiece);
-    copy_kernel<<<(unsigned)(items < 8 * sms ? items : 8 * sms), kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(P);
+    copy_kernel<<<(unsigned)(items < kCopyBlocks * sms ? items : kCopyBlocks * sms), kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(P);
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }
 
