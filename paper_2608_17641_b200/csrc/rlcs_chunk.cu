@@ -85,12 +85,16 @@ chunk_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUte
 // One rounding of the weights to bfloat16, at most 2^-8 of each, is as large as the output's own; a second part would be half as many
 // value products again.
 //
+// Where the heads on a key head divide 128, a block's queries come, and its outputs leave, as boxes of whole tokens: sixteen loads a thread
+// took 2.6 us under the other block's exponentials.
+//
 // Bound by shared memory: a step's scores read 48 KB (queries and keys), its values 16, its copies write 32, for two blocks 192 KB or 1500
-// cycles of 128 bytes, against 1024 cycles of products and 1024 of exponentials.  Measured (32 heads on 8 key heads of 128): 7 prompts of up to
-// 4096 tokens 375 us for 321 GFLOP (0.52 of the bf16 rate), 1000 tokens behind 32768 463 us for 477 GFLOP (0.62), 64 chunks of up to 8 tokens
-// behind 4096 160 us (0.77 of the copy bandwidth).  Not kept: two row tiles a block that share their keys, one block a multiprocessor
-// (377, 488 us, and 216 for the chunks of drafts: nothing runs under a block's start and end); 128 keys a step into a single
-// buffer (467, 516: scores, weights and values in turn, some 250 cycles at every barrier); a quarter of the exponentials by polynomial (no change).
+// cycles of 128 bytes, against 1024 cycles of products and 1024 of exponentials; a step takes about 1700.  Measured (heads of 128): 7 prompts
+// of up to 4096 tokens, 32 heads on 8, 341 us for 321 GFLOP (0.57 of the bf16 rate); 1000 tokens behind 32768, 28 on 4, 458 us for
+// 477 GFLOP (0.63); 64 chunks of up to 8 tokens behind 4096 159 us (0.78 of the copy bandwidth).  Not kept: two row tiles a block that share
+// their keys, one block a multiprocessor (377, 488 us, and 216 for the chunks of drafts: nothing runs under a block's start and end); 128 keys a step into a single
+// buffer (467, 516: scores, weights and values in turn, some 250 cycles at every barrier); a quarter of the exponentials by polynomial
+// (no change); blocks of 126 rows where 7 heads share a key head, to have their boxes (500: one tile more is a round of blocks more).
 constexpr int kKeys = 64, kRows = 128, kWideThreads = 256, kCopiers = 64, kMostSegment = 65536;
 
 // Boxes of queries and outputs [T, H, d].

@@ -6,6 +6,10 @@
 // One read of the logits and one write of the gradient are the floor.  With m the row's maximum, S = sum exp((l - m) / T) and q_j =
 // exp((l_j - m) / T) / S: the gradient is q_j scale / T everywhere but at the teacher's entries, which are written once more, after the
 // rest, with what they lack: a row's K entries are few.  The maximum is taken off before the division, so that logits far from 0 lose nothing.
+//
+// Measured: 4096 x 131072 bfloat16, K = 64, 440 us (0.75 of the copy bandwidth; 413 without the teacher's entries): the exponential unit 59 % busy,
+// a row's chain (sums over the cluster, entries) under it; 1021 x 50021 fp32, K = 20, 15 % masked, 92 us (0.63: 9.8 rows a cluster
+// count as ten and more).  Not kept: entries one after the other by a whole warp (484 us), eight blocks a row (648).
 #include <cooperative_groups.h>
 
 #include <cmath>

@@ -12,6 +12,12 @@
 // (the hardware's, summed in fp32 over 32 and in 64 bits beyond: within 2^-15 of the whole weights' sum, but for one half a weight).  The
 // second has a cluster a trajectory.  A draft whose verdict is the same anywhere within those bounds, nearly every one, needs no
 // more; another row's weights are summed up exactly, and so are those of the row from which the next token is drawn.
+//
+// Measured: 128 trajectories of up to 7 drafts, 131072 entries in bfloat16, 137 us: 55 in the first kernel (0.75 of the copy bandwidth), in the
+// second 26 for exact weights (18 instructions each, expf's among them), 10 for their differences and 47 of waiting: six rounds of
+// clusters, each with a verdict and two sums over the cluster.  One trajectory: 18 us (7 + 11).  Not kept: exact weights of every row (585 us);
+// clusters of eight with twice the share (168), 256 threads a block (137) or 384 (131, but 20 us for one trajectory), dependent
+// launch of the second kernel (0.4 us).
 #include <cooperative_groups.h>
 
 #include <cmath>
