@@ -221,28 +221,27 @@ struct FreeParams {
     int32_t pages, words, page;
 };
 
-// Marks what the tables name, a warp a row, four entries a lane at a time.
-__device__ __forceinline__ void mark_rows(const FreeParams& P, uint32_t* bits, int first, int warps) {
+// Marks what a table names, a warp a row, four entries a lane at a time.
+__device__ __forceinline__ void mark_rows(const FreeParams& P, int t, uint32_t* bits, int first, int warps) {
     const int lane = threadIdx.x & 31;
-#pragma unroll 1
-    for (int t = 0; t < 2; ++t)
-        for (int b = first; b < P.rows[t]; b += warps) {
-            const uint32_t need = ((uint32_t)max(P.lens[t][b], 0) + P.page - 1) / (uint32_t)P.page;
-            const int have = (int)min(need, (uint32_t)P.width[t]);
-            const int32_t* row = P.table[t] + (int64_t)b * P.width[t];
-            for (int j = lane; j < have; j += 128) {
-                int id[4];
+    for (int b = first; b < P.rows[t]; b += warps) {
+        const uint32_t need = ((uint32_t)max(P.lens[t][b], 0) + P.page - 1) / (uint32_t)P.page;
+        const int have = (int)min(need, (uint32_t)P.width[t]);
+        const int32_t* row = P.table[t] + (int64_t)b * P.width[t];
+        for (int j = lane; j < have; j += 128) {
+            int id[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) id[k] = j + k * 32 < have ? row[j + k * 32] : -1;
+            for (int k = 0; k < 4; ++k) id[k] = j + k * 32 < have ? row[j + k * 32] : -1;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (id[k] >= 0 && id[k] < P.pages) atomicOr(bits + (id[k] >> 5), 1u << (id[k] & 31));
-            }
+            for (int k = 0; k < 4; ++k)
+                if (id[k] >= 0 && id[k] < P.pages) atomicOr(bits + (id[k] >> 5), 1u << (id[k] & 31));
         }
+    }
 }
 
 __global__ void __launch_bounds__(kThreads) free_mark_kernel(const __grid_constant__ FreeParams P) {
-    mark_rows(P, P.bits, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32));
+#pragma unroll 1
+    for (int t = 0; t < 2; ++t) mark_rows(P, t, P.bits, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32));
 }
 
 // Free pages among the 32 of a word; the words behind the last are a whole vector's, and 0.
@@ -300,14 +299,36 @@ __global__ void __launch_bounds__(kList) free_list_kernel(const __grid_constant_
     list_words(P, P.bits, begin, min(begin + per, P.words), blockIdx.x, gridDim.x);
 }
 
-// Small caches and tables: one block, the marks in shared memory.
+// Small caches and tables: one block, the marks in shared memory.  A warp a row up to 256 rows (128 rows of 64: 6.8 us, 8.1 the other way),
+// an entry a thread wherever its row is beyond (1401 rows of three: 12 us, 30 the other way).
 constexpr int kAlonePages = 65536, kAloneEntries = 32768;
 
 __global__ void __launch_bounds__(kList) free_alone_kernel(const __grid_constant__ FreeParams P) {
     __shared__ __align__(16) uint32_t bits[kAlonePages / 32 + 4];
     for (int w = threadIdx.x; w < (P.words + 3) / 4 * 4; w += kList) bits[w] = 0;
     __syncthreads();
-    mark_rows(P, bits, threadIdx.x >> 5, kList / 32);
+#pragma unroll 1
+    for (int t = 0; t < 2; ++t) {
+        if (P.rows[t] <= 256) {
+            mark_rows(P, t, bits, threadIdx.x >> 5, kList / 32);
+            continue;
+        }
+        const int cells = P.rows[t] * P.width[t];             // at most kAloneEntries
+        for (int e = threadIdx.x; e < cells; e += 4 * kList) {
+            int id[4], len[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int at = e + k * kList;
+                id[k] = at < cells ? P.table[t][at] : -1;
+                len[k] = at < cells ? P.lens[t][at / P.width[t]] : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t need = ((uint32_t)max(len[k], 0) + P.page - 1) / (uint32_t)P.page;
+                if ((uint32_t)(e + k * kList) % (uint32_t)P.width[t] < need && id[k] >= 0 && id[k] < P.pages) atomicOr(bits + (id[k] >> 5), 1u << (id[k] & 31));
+            }
+        }
+    }
     __syncthreads();
     list_words(P, bits, 0, P.words, 0, 1);
 }
