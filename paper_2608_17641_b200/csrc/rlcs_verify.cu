@@ -334,8 +334,8 @@ __device__ __noinline__ float score(double all, float x, float top, float inv) {
 
 // NT threads a block, a cluster a trajectory.  HELD: a block's weights of both rows stay in shared memory.
 template <typename T, int NT, bool HELD>
-__global__ void __launch_bounds__(NT, NT == 512 ? 3 : 1) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
-    extern __shared__ __align__(16) uint32_t held[];         // [2][share and up to a vector before it]
+__global__ void __launch_bounds__(NT, NT == 512 ? 3 : NT == 256 ? 6 : 1) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
+    extern __shared__ __align__(16) uint32_t held[];         // [2, or 1 without drafts' logits][share and up to a vector before it]
     __shared__ u64 part[2][NT / 32], sent[2][16][2], total_of[2];
     __shared__ RowStat stat[2];                              // of row r below
     __shared__ int stop;                                     // least 2 t + 1 of a row whose draft does not stay, 2 t where that is unclear
@@ -569,7 +569,7 @@ template <typename T, int NT, bool HELD> int launch_draw(const VerifyParams<T>& 
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(P.seqs * ranks));
     cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = HELD ? 8 * (size_t)(P.share + 8) : 0;
+    cfg.dynamicSmemBytes = HELD ? (P.drafts != nullptr ? 8 : 4) * (size_t)(P.share + 8) : 0;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -612,12 +612,18 @@ int verify_run(const T* logits, int64_t ld, const T* drafts, int64_t ldd, const 
             verify_scan_kernel<T, kScan><<<(unsigned)(all * P.parts), kScan, 0, s>>>(P);
         }
     }
-    // a block's share of a row: few thousand entries; both rows' weights in shared memory up to 224 KB
+    // a block's share of a row: at most 8192 entries where sixteen blocks hold a row so (1000 rows of 50000: 283 us, 479 with shares of
+    // half of that), less while there are fewer than two blocks a multiprocessor and a share keeps 2048; the weights of both rows (of one,
+    // where the drafts have no logits) in shared memory up to 224 KB
     int ranks = 1;
-    while (ranks < kMostRanks && (A + ranks - 1) / ranks > 4096) ranks *= 2;
+    while (ranks < kMostRanks && ((A + ranks - 1) / ranks > 8192 || (seqs * ranks < 2 * sms && (A + ranks - 1) / ranks >= 4096))) ranks *= 2;
     P.share = (int32_t)(((A + ranks - 1) / ranks + 7) / 8 * 8);
     const bool hold = P.share <= kMostShare;
-    const int st = A <= 4096 ? launch_draw<T, 128, true>(P, ranks, s) : hold ? launch_draw<T, 512, true>(P, ranks, s) : launch_draw<T, 512, false>(P, ranks, s);
+    // more than one round, and shares of which more than three fit into a multiprocessor: half the threads, up to twice the blocks at
+    // once (1000 rows of 50000 198 us, 283 with 512 threads; 2000 of 9000 with the drafts' logits 161, 198)
+    const bool queue = P.share <= (drafts != nullptr ? 6144 : 12288) && seqs * ranks > 3 * sms;
+    const int st = A <= 1024 ? launch_draw<T, 128, true>(P, ranks, s) : queue ? launch_draw<T, 256, true>(P, ranks, s)
+                   : hold ? launch_draw<T, 512, true>(P, ranks, s) : launch_draw<T, 512, false>(P, ranks, s);
     if (st != RLCS_OK) return st;
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }
