@@ -87,17 +87,41 @@ __device__ __forceinline__ void add_one(Sum* a, float f, float k) {
 }
 
 // ---------------------------------------------------------------------------------------------- short rows
-// Up to 2048 (fp32) or 4096 (bfloat16) entries: G lanes a row, NV vectors of it in the registers of each.  What the teacher's
-// entries are to get waits in shared memory until the rest is written; a bit a student's entry tells whether one is named twice.
-template <typename T, int G, int NV>
+// What G lanes have, joined: by shuffles in a warp, over the block through shared memory (`room` serves one join).
+template <int G> struct Lanes {
+    static __device__ __forceinline__ void sync() {
+        if constexpr (G > 32) __syncthreads(); else __syncwarp();
+    }
+    template <typename F> static __device__ __forceinline__ float join(float v, float nothing, float* room, F op) {
+#pragma unroll
+        for (int o = (G < 32 ? G : 32) / 2; o; o >>= 1) v = op(v, __shfl_xor_sync(~0u, v, o));
+        if constexpr (G > 32) {
+            if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
+            __syncthreads();
+            v = nothing;
+#pragma unroll
+            for (int w = 0; w < G / 32; ++w) v = op(v, room[w]);
+        }
+        return v;
+    }
+    static __device__ __forceinline__ float most(float v, float* room) { return join(v, -INFINITY, room, [](float a, float b) { return fmaxf(a, b); }); }
+    static __device__ __forceinline__ float sum(float v, float* room) { return join(v, 0.f, room, [](float a, float b) { return a + b; }); }
+};
+
+// Up to 2048 (fp32) or 4096 (bfloat16) entries, up to four times that with G = 256: G lanes a row, NV vectors of it in the registers
+// of each, and up to E of the teacher's entries (E = 0: any number, read again when needed; what they are to get waits in shared
+// memory until the rest is written).  A bit a student's entry tells whether one is named twice.
+template <typename T, int G, int NV, int E>
 __global__ void __launch_bounds__(256) distill_group_kernel(const __grid_constant__ DistillParams<T> P) {
     constexpr int N = Vec<T>::N;
-    extern __shared__ uint32_t room[];                       // a row: K values, then a bit for each of the A entries
+    extern __shared__ uint32_t room[];                       // a row: K values (E = 0), then a bit for each of the A entries
+    __shared__ float joined[6][8];
     const int lane = threadIdx.x % G, words = (P.A + 31) / 32;
     const int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
     const bool there = row < P.R && (P.mask == nullptr || P.mask[row] != 0);       // every lane takes part in the sums
-    float* const value = reinterpret_cast<float*>(room + threadIdx.x / G * (P.K + words));
-    uint32_t* const named = room + threadIdx.x / G * (P.K + words) + P.K;
+    const int kept = E > 0 ? 0 : P.K;
+    float* const value = reinterpret_cast<float*>(room + threadIdx.x / G * (kept + words));
+    uint32_t* const named = room + threadIdx.x / G * (kept + words) + kept;
     const T* x = P.logits + (row < P.R ? row : 0) * P.ld;
     const Span sp = span_of(x, P.A);
     const int rest = sp.head + sp.vecs * N, singles = sp.head + P.A - rest;
@@ -111,21 +135,39 @@ __global__ void __launch_bounds__(256) distill_group_kernel(const __grid_constan
         v[q] = there && q * G + lane < sp.vecs ? body[q * G + lane] : make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
 #pragma unroll
     for (int q = 0; q < kOnes; ++q) one[q] = there && q * G + lane < singles ? Vec<T>::load(x + single(q * G + lane)) : -INFINITY;
-    for (int i = lane; i < words; i += G) named[i] = 0;
-    __syncwarp();
     const int32_t* ids = P.ids + row * P.K;
     const float* teacher = P.teacher + row * P.K;
+    int my_id[E > 0 ? E : 1];
+    float my_t[E > 0 ? E : 1], my_x[E > 0 ? E : 1];
+#pragma unroll
+    for (int q = 0; q < E; ++q) {
+        const bool any = there && q * G + lane < P.K;
+        my_id[q] = any ? ids[q * G + lane] : -1;
+        my_t[q] = any ? teacher[q * G + lane] : 0.f;
+    }
+    for (int i = lane; i < words; i += G) named[i] = 0;
+    Lanes<G>::sync();
     Both r = {{-INFINITY, 0.f}, {-INFINITY, 0.f}};
     bool twice = false;
-    if (there)
+#pragma unroll
+    for (int q = 0; q < E; ++q) {
+        if (my_id[q] >= P.A) my_id[q] = -1;
+        if (my_id[q] < 0) continue;
+        my_x[q] = Vec<T>::load(x + my_id[q]);
+        r.teacher.m = max_nan(r.teacher.m, my_t[q]);
+        twice = twice || (atomicOr(named + my_id[q] / 32, 1u << my_id[q] % 32) >> my_id[q] % 32 & 1);
+    }
+#pragma unroll
+    for (int q = 0; q < E; ++q)
+        if (my_id[q] >= 0 && r.teacher.m != -INFINITY) r.teacher.s += exp2_of((my_t[q] - r.teacher.m) * P.exp2_t);
+    if (E == 0 && there)
         for (int i = lane; i < P.K; i += G) {
             const int id = ids[i];
             if (id < 0 || id >= P.A) continue;
             add_one(&r.teacher, teacher[i], P.exp2_t);
             twice = twice || (atomicOr(named + id / 32, 1u << id % 32) >> id % 32 & 1);
         }
-#pragma unroll
-    for (int o = G / 2; o; o >>= 1) twice = __shfl_xor_sync(~0u, (int)twice, o) | (int)twice;
+    twice = Lanes<G>::most(twice ? 1.f : 0.f, joined[0]) > 0.f;
     uint32_t most = Vec<T>::kNothing;
 #pragma unroll
     for (int q = 0; q < NV; ++q)
@@ -133,8 +175,7 @@ __global__ void __launch_bounds__(256) distill_group_kernel(const __grid_constan
     float m = Vec<T>::most_number_of(most);
 #pragma unroll
     for (int q = 0; q < kOnes; ++q) m = fmaxf(m, one[q]);
-#pragma unroll
-    for (int o = G / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    m = Lanes<G>::most(m, joined[1]);
     const float base = m == -INFINITY ? 0.f : m;             // -inf then weighs 0, and NaN stays NaN
     const float2 less = {-base, -base}, scale = {P.exp2_t, P.exp2_t};
     float2 s = {0.f, 0.f};
@@ -151,17 +192,30 @@ __global__ void __launch_bounds__(256) distill_group_kernel(const __grid_constan
     }
 #pragma unroll
     for (int q = 0; q < kOnes; ++q) s.x += weight2(make_float2(one[q], -INFINITY)).x;
-    r.student = Sum{m, s.x + s.y};
-#pragma unroll
-    for (int o = G / 2; o; o >>= 1) r.student.s += __shfl_xor_sync(~0u, r.student.s, o);
-    r.teacher = join_lanes(r.teacher, G, P.exp2_t);
+    r.student = Sum{m, Lanes<G>::sum(s.x + s.y, joined[2])};
+    {
+        const float tm = Lanes<G>::most(r.teacher.m, joined[3]);
+        r.teacher = Sum{tm, Lanes<G>::sum(faded(r.teacher, tm, P.exp2_t), joined[4])};
+    }
     const bool live = there && r.live();
     const float unit = live ? P.scale * P.inv_t : 0.f;
     const float c = r.teacher.s == r.teacher.s ? unit / r.student.s : r.teacher.s;      // a teacher of NaN: the whole row
     float loss = 0.f;
     if (live) {
         const float log_gap = logf(r.student.s) - logf(r.teacher.s);
-        for (int i = lane; i < P.K; i += G) {
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+            if (my_id[q] < 0) continue;
+            float p = chance(my_t[q], r, P.exp2_t);
+            loss += term(P, my_t[q], my_x[q], r, log_gap);
+            if (twice) {
+                p = 0.f;
+                for (int k = 0; k < P.K; ++k)
+                    if (ids[k] == my_id[q]) p += chance(teacher[k], r, P.exp2_t);
+            }
+            my_t[q] = exp2_of((my_x[q] - base) * P.exp2_t) * c - unit * p;      // what the entry is to get
+        }
+        for (int i = lane; E == 0 && i < P.K; i += G) {
             const int id = ids[i];
             if (id < 0 || id >= P.A) continue;
             const float xi = Vec<T>::load(x + id);
@@ -175,10 +229,9 @@ __global__ void __launch_bounds__(256) distill_group_kernel(const __grid_constan
             value[i] = exp2_of((xi - base) * P.exp2_t) * c - unit * p;
         }
     }
-#pragma unroll
-    for (int o = G / 2; o; o >>= 1) loss += __shfl_xor_sync(~0u, loss, o);
+    loss = Lanes<G>::sum(loss, joined[5]);
     if (row < P.R && lane == 0 && P.loss != nullptr) P.loss[row] = live ? P.scale * loss : 0.f;
-    __syncwarp();                                            // logits that are overwritten have been read
+    Lanes<G>::sync();                                        // logits that are overwritten have been read
     if (row < P.R && P.dlogits != nullptr) {
         T* y = P.dlogits + row * P.ldd;
         const float2 two = {c, c};
@@ -215,12 +268,16 @@ __global__ void __launch_bounds__(256) distill_group_kernel(const __grid_constan
         for (int q = 0; q < kOnes; ++q)
             if (q * G + lane < singles) Vec<T>::store(y + single(q * G + lane), live ? weight2(make_float2(one[q], one[q])).x * c : 0.f);
     }
-    __syncwarp();
-    if (live && P.dlogits != nullptr)
-        for (int i = lane; i < P.K; i += G) {
+    Lanes<G>::sync();
+    if (live && P.dlogits != nullptr) {
+#pragma unroll
+        for (int q = 0; q < E; ++q)
+            if (my_id[q] >= 0) Vec<T>::store(P.dlogits + row * P.ldd + my_id[q], my_t[q]);      // all that name an entry have the same value for it
+        for (int i = lane; E == 0 && i < P.K; i += G) {
             const int id = ids[i];
-            if (id >= 0 && id < P.A) Vec<T>::store(P.dlogits + row * P.ldd + id, value[i]);      // all that name an entry have the same value for it
+            if (id >= 0 && id < P.A) Vec<T>::store(P.dlogits + row * P.ldd + id, value[i]);
         }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- long rows
@@ -573,8 +630,10 @@ bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t
 template <typename T, int G, int NV> int launch_group(const DistillParams<T>& P, cudaStream_t s) {
     const int64_t blocks = (P.R * G + 255) / 256;
     if (blocks > (int64_t(1) << 31) - 1) return RLCS_ERR_SIZE;
-    const int bytes = 256 / G * (P.K + (P.A + 31) / 32) * 4;                       // at most 8 (1024 + 128) or 32 (64 + 16) words
-    distill_group_kernel<T, G, NV><<<(unsigned)blocks, 256, bytes, s>>>(P);
+    const int words = (P.A + 31) / 32;
+    if (P.K <= 2 * G) distill_group_kernel<T, G, NV, 2><<<(unsigned)blocks, 256, 256 / G * words * 4, s>>>(P);
+    else if (P.K <= 8 * G) distill_group_kernel<T, G, NV, 8><<<(unsigned)blocks, 256, 256 / G * words * 4, s>>>(P);
+    else if constexpr (8 * G < kMostTop) distill_group_kernel<T, G, NV, 0><<<(unsigned)blocks, 256, 256 / G * (P.K + words) * 4, s>>>(P);      // at most 8 (1024 + 128) words
     return RLCS_OK;
 }
 
@@ -631,6 +690,8 @@ int distill_run(const T* logits, int64_t ld, const int32_t* ids, const float* te
         else if (vecs <= 128) st = launch_group<T, 32, 4>(P, s);
         else if (vecs <= 256) st = launch_group<T, 32, 8>(P, s);
         else st = launch_group<T, 32, 16>(P, s);
+    } else if (vecs <= 2048 && R >= 2 * rlcs_device::limits().sms) {      // a block a row (29245 rows of 11 KB 169 us, 320 from shared memory); fewer rows are cut over clusters
+        st = vecs <= 1024 ? launch_group<T, 256, 4>(P, s) : launch_group<T, 256, 8>(P, s);
     } else {
         // blocks a row: parts of at most 64 KB; more while the GPU has room for two a multiprocessor and a part keeps 8 KB
         const int64_t bytes = A * (int64_t)sizeof(T);

@@ -698,6 +698,36 @@ def test_distill_row_counts(api, R, A):
     check_distill(api, x, ids, teacher, mask, scale=1.0 / R)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A,K", [(2049, 2), (4095, 600), (4097, 9), (6001, 1024), (8192, 33), (8194, 5), (12345, 520), (16384, 12), (16390, 300)])
+def test_distill_many_rows_of_middle_width(api, A, K, dtype):
+    """More than two rows a multiprocessor, of 8 to 64 KB; the rows that are checked hold what can go wrong, the others repeat them."""
+    x, ids, teacher, g = distill_inputs(10, A, K, dtype, A)
+    ids[0] = ids[0, 0]
+    ids[1, K // 2:] = -1
+    ids[2] = -1
+    ids[3, 0], ids[3, 1] = A, -2 ** 31
+    teacher[4, 1:] = -math.inf
+    teacher[5] = -math.inf
+    off = torch.rand(10, A, generator=g) < 0.4
+    off.scatter_(1, ids.clamp(0, A - 1).long(), False)
+    x[6][off[6]], x[7][off[7]] = -math.inf, torch.finfo(dtype).min
+    mask = torch.ones(10, dtype=torch.bool)
+    mask[8] = False
+    want, want_grad, prob = plain_distill(x, ids, teacher, mask, 1.2, 0.9)
+    loss, grad = api.compute_distillation(strided_rows(x.repeat(31, 1), K % 3, A % 2), up(ids.repeat(31, 1)), up(teacher.repeat(31, 1)),
+                                          mask=up(mask.repeat(31)), temperature=1.2, scale=0.9, in_place=K % 2 == 0)
+    loss, grad = loss.cpu().view(31, 10), grad.cpu().view(31, 10, A)
+    assert ((loss[0].double() - want).abs() <= 1e-5 + 2.0 ** -22 * want.abs()).all()
+    bound = 1e-5 * (prob + (prob - want_grad).abs()) + (2.0 ** -8 if dtype == BF16 else 2.0 ** -22) * want_grad.abs() + 1e-38
+    assert ((grad[0].double() - want_grad).abs() <= bound * 1.01).all()
+    if A % 8 == 0 and K % 3 == 0:                                      # rows at the same alignment: the same bits
+        assert (loss == loss[0]).all() and (grad == grad[0]).all()
+    else:
+        assert ((loss.double() - want).abs() <= 1e-5 + 2.0 ** -22 * want.abs()).all()
+        assert ((grad.double() - want_grad).abs() <= bound * 1.01).all()
+
+
 def test_distill_more_rows_than_run_at_once(api):
     R, A, K = 1300, 10001, 16
     g = torch.Generator(device="cuda").manual_seed(5)
