@@ -13,11 +13,11 @@
 // second has a cluster a trajectory.  A draft whose verdict is the same anywhere within those bounds, nearly every one, needs no
 // more; another row's weights are summed up exactly, and so are those of the row from which the next token is drawn.
 //
-// Measured: 128 trajectories of up to 7 drafts, 131072 entries in bfloat16, 137 us: 55 in the first kernel (0.75 of the copy bandwidth), in the
-// second 26 for exact weights (18 instructions each, expf's among them), 10 for their differences and 47 of waiting: six rounds of
+// Measured: 128 trajectories of up to 7 drafts, 131072 entries in bfloat16, 132 us: 55 in the first kernel (0.75 of the copy bandwidth), in the
+// second 26 for exact weights (18 instructions each, expf's among them), 10 for their differences and 42 of waiting: five rounds of
 // clusters, each with a verdict and two sums over the cluster.  One trajectory: 18 us (7 + 11).  Not kept: exact weights of every row (585 us);
-// clusters of eight with twice the share (168), 256 threads a block (137) or 384 (131, but 20 us for one trajectory), dependent
-// launch of the second kernel (0.4 us).
+// clusters of eight with twice the share (168), 256 threads a block (137), 512 (137; kept where clusters do not queue: 384 make one
+// trajectory's 20 us), dependent launch of the second kernel (0.4 us).
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -334,7 +334,7 @@ __device__ __noinline__ float score(double all, float x, float top, float inv) {
 
 // NT threads a block, a cluster a trajectory.  HELD: a block's weights of both rows stay in shared memory.
 template <typename T, int NT, bool HELD>
-__global__ void __launch_bounds__(NT, NT == 512 ? 3 : NT == 256 ? 6 : 1) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
+__global__ void __launch_bounds__(NT, NT >= 384 ? 3 : NT == 256 ? 6 : 1) verify_draw_kernel(const __grid_constant__ VerifyParams<T> P) {
     extern __shared__ __align__(16) uint32_t held[];         // [2, or 1 without drafts' logits][share and up to a vector before it]
     __shared__ u64 part[2][NT / 32], sent[2][16][2], total_of[2];
     __shared__ RowStat stat[2];                              // of row r below
@@ -619,10 +619,13 @@ int verify_run(const T* logits, int64_t ld, const T* drafts, int64_t ldd, const 
     while (ranks < kMostRanks && ((A + ranks - 1) / ranks > 8192 || (seqs * ranks < 2 * sms && (A + ranks - 1) / ranks >= 4096))) ranks *= 2;
     P.share = (int32_t)(((A + ranks - 1) / ranks + 7) / 8 * 8);
     const bool hold = P.share <= kMostShare;
-    // more than one round, and shares of which more than three fit into a multiprocessor: half the threads, up to twice the blocks at
-    // once (1000 rows of 50000 198 us, 283 with 512 threads; 2000 of 9000 with the drafts' logits 161, 198)
-    const bool queue = P.share <= (drafts != nullptr ? 6144 : 12288) && seqs * ranks > 3 * sms;
-    const int st = A <= 1024 ? launch_draw<T, 128, true>(P, ranks, s) : queue ? launch_draw<T, 256, true>(P, ranks, s)
+    // more than one round: where more than three shares fit into a multiprocessor half the threads, up to twice the blocks at once (1000
+    // rows of 50000 198 us, 283 with 512 threads; 2000 of 9000 with the drafts' logits 161, 198); where three do, fewer warps to sum over
+    // (300 of 150000 264 us, 284 with 512)
+    const int64_t room = P.share * (drafts != nullptr ? 8 : 4);
+    const bool queue = seqs * ranks > 3 * sms;
+    const int st = A <= 1024 ? launch_draw<T, 128, true>(P, ranks, s) : queue && room <= 48 * 1024 ? launch_draw<T, 256, true>(P, ranks, s)
+                   : queue && room <= 74 * 1024 ? launch_draw<T, 384, true>(P, ranks, s)
                    : hold ? launch_draw<T, 512, true>(P, ranks, s) : launch_draw<T, 512, false>(P, ranks, s);
     if (st != RLCS_OK) return st;
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
