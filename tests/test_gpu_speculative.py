@@ -429,6 +429,27 @@ def test_verify_wide_rows_and_many_trajectories(api, A, B, dtype):
     check_verify(api, x, tokens, offsets, u, du, None, temps=1.1)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A,times", [(1500, 100), (9001, 130), (20245, 50), (130000, 9), (147000, 9), (200003, 8)])
+def test_verify_more_trajectories_than_run_at_once(api, A, times, dtype):
+    """Some trajectories against the plain form, and many times over in one call, which may split a row otherwise: the same tokens."""
+    x, tokens, offsets, u, du, drafts = verify_inputs([3, 1, 2, 0, 4], A, dtype, A, near=0.5)
+    x[5, : A // 2] = -math.inf
+    x[6] = -math.inf
+    temps = [0.8, 1.0, 1.3, 1.0, 0.0]
+    for q, pad in ((drafts, A % 3), (None, 0)):
+        check_verify(api, x, tokens, offsets, u, du, q, temps=temps, pad=pad)
+        rows, results = x.shape[0], []
+        for n in (1, times):
+            starts = ints([k * rows + o for k in range(n) for o in offsets[:-1]] + [n * rows])
+            out, lp, acc = api.verify_drafts(strided_rows(x.repeat(n, 1), pad, 0), up(tokens.repeat(n)), up(starts), up(u.repeat(n)), up(du.repeat(n)),
+                                             draft_logits=None if q is None else up(q.repeat(n, 1)), temperature=up(torch.tensor(temps * n)))
+            results.append((out.cpu().view(n, rows), lp.cpu().view(n, rows), acc.cpu().view(n, 5)))
+        (out, lp, acc), (outs, lps, accs) = results
+        assert (outs == out).all() and (accs == acc).all()
+        assert ((lps - lp).abs().nan_to_num(0.0) <= 3e-5).all()        # twice what one may be off; nan: -inf on both sides
+
+
 @pytest.mark.parametrize("drawn", [True, False])
 def test_verify_rows_too_wide_for_shared_memory(api, drawn):
     x, tokens, offsets, u, du, drafts = verify_inputs([3], 500001, BF16, 2, near=0.3)
