@@ -192,6 +192,59 @@ def test_chunk_many_trajectories():
     check_chunks([c + int(k) for c, k in zip(counts, torch.randint(0, 60, (150,), generator=g))], counts, 4, 2, 128, 16)
 
 
+def check_wide(lens, counts, H, Hk, d, page, **more):
+    """The same calls with a table for longer trajectories, where rows go in blocks of 128."""
+    check_chunks(lens, counts, H, Hk, d, page, bounds=False, width=-(-800 // page), **more)
+
+
+@pytest.mark.parametrize("H,Hk,d", [(8, 8, 64), (8, 2, 128), (28, 4, 64), (20, 1, 128), (4, 4, 8), (6, 2, 40), (33, 1, 80), (4, 1, 96)])
+@pytest.mark.parametrize("page", [1, 7, 16, 64, 100, 256])
+def test_chunk_long_tables_heads_and_pages(H, Hk, d, page):
+    check_wide([65, 130, 1, 9], [3, 1, 1, 9], H, Hk, d, page, seed=page)
+    check_wide([65, 130, 200], [40, 0, 33], H, Hk, d, page, seed=page + 1)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [1, 8, 16, 24, 32, 64, 128, 192, 256])
+@pytest.mark.parametrize("r", [1, 4, 7])
+def test_chunk_long_tables_blocks_of_many_rows(r, page, d):
+    check_wide([500, 257, 300], [400, 257, 20], 2 * r, 2, d, page, seed=page)
+    check_wide([700], [131], r, 1, d, page, seed=page + 5)
+
+
+@pytest.mark.parametrize("new", [17, 64, 65, 130, 300])
+@pytest.mark.parametrize("cached", [0, 1, 15, 63, 64, 65, 127, 129])
+def test_chunk_long_tables_lengths(cached, new):
+    check_wide([cached + new, new, cached + 1], [new, new, 1], 8, 2, 64, 16, seed=cached + new)
+
+
+def test_chunk_long_tables_empty_outside_and_strided():
+    check_wide([0, 30, 0, 10], [50, 70, 0, 0], 8, 2, 128, 16)
+    check_wide([0, 0], [300, 3], 4, 2, 64, 16)
+    check_wide([200, 300], [100, 230], 8, 2, 128, 64, first=40, behind=50)
+    check_wide([300, 210], [200, 7], 8, 2, 64, 32, layout="heads")
+    check_wide([300, 210], [200, 7], 8, 2, 128, 64, layout="heads", q_pad=24)
+    check_wide([300, 210], [200, 7], 8, 2, 128, 20, factor=6.0)
+    check_wide([200, 300, 77], [70, 300, 1], 8, 2, 72, 48)
+
+
+@pytest.mark.parametrize("page", [7, 16, 64])
+def test_chunk_long_tables_pages_that_are_not_there(api, page):
+    lens, counts = [400, 333], [150, 150]
+    cache = Paged(4, lens, page, 2, 64)
+    table, missing = cache.table.clone(), [torch.zeros(400, dtype=torch.bool) for _ in lens]
+    for b, j, what in ((0, 0, -1), (0, 2, 2 ** 31 - 1), (1, 1, -2 ** 31), (1, (332 // page), cache.k.shape[0])):
+        table[b, j] = what
+        missing[b][j * page:(j + 1) * page] = True
+    table = torch.cat([table, torch.full((2, -(-800 // page)), -1, dtype=I32)], 1)
+    q = torch.randn(300, 4, 64, generator=torch.Generator().manual_seed(9)).to(BF16)
+    want = plain_chunks(q, cache.keys, lens, [0, 150, 300], 0.2, 400, missing)
+    out, lse = api.chunk_attention(up(q), cache.kd, cache.vd, up(table), up(ints([0, 150, 300])), up(ints(lens)), scale=0.2)
+    compare_chunks(out, lse, *want, 5.0)
+    out, lse = api.chunk_attention(up(q), cache.kd, cache.vd, up(torch.full_like(table, -1)), up(ints([0, 150, 300])), up(ints(lens)), scale=0.2)
+    assert (out == 0).all() and (lse == -math.inf).all()
+
+
 def test_chunk_lengths_out_of_all_proportion(api):
     """Lengths beyond the table, up to the largest number: what the table holds is seen; negative ones: nothing."""
     for new in (2, 100):
