@@ -802,6 +802,23 @@ def test_distill_many_rows_of_middle_width(api, A, K, dtype):
         assert ((grad.double() - want_grad).abs() <= bound * 1.01).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A", [4100, 8190])
+def test_distill_nan_in_many_rows_of_middle_width(api, A, dtype):
+    x, ids, teacher, _ = distill_inputs(6, A, 3, dtype, 8)
+    again = lambda: [v.cpu().view(60, 6, -1) for v in api.compute_distillation(up(x.repeat(60, 1)), up(ids.repeat(60, 1)), up(teacher.repeat(60, 1)))]
+    clean = again()
+    x[1, A // 2] = float("nan")
+    x[2, A - 1] = math.inf
+    teacher[3, 1] = float("nan")
+    teacher[4] = torch.tensor([-math.inf, -math.inf, float("nan")])
+    x[5, ids[5, 0].long()] = -math.inf
+    loss, grad = again()
+    assert torch.isnan(loss[:, 1:5]).all() and torch.isnan(grad[:, 1:5]).all()
+    assert (loss[:, 5] == math.inf).all() and torch.isfinite(grad[:, 5]).all()
+    assert (loss[:, 0] == clean[0][:, 0]).all() and (grad[:, 0] == clean[1][:, 0]).all()
+
+
 def test_distill_more_rows_than_run_at_once(api):
     R, A, K = 1300, 10001, 16
     g = torch.Generator(device="cuda").manual_seed(5)
