@@ -698,6 +698,16 @@ def test_distill_many_entries_and_wide_rows(api, A, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A,K", [(3, 40), (7, 17), (11, 16), (16, 4), (23, 33), (33, 64), (70, 9)])
+def test_distill_short_rows(api, A, K, dtype):
+    for R, pad, lead in ((1, 0, 0), (515, 0, 1), (130, 5, 3)):
+        x, ids, teacher, g = distill_inputs(R, A, K, dtype, A + R)
+        ids[R // 2] = ids[R // 2, 0]
+        ids[R // 3, K // 2:] = -1
+        check_distill(api, x, ids, teacher, torch.rand(R, generator=g) < 0.9, T=0.7, pad=pad, lead=lead, in_place=pad == 0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("A", [3, 40, 500, 12000])
 def test_distill_entries_named_twice_or_absent(api, A, dtype):
     x, ids, teacher, g = distill_inputs(8, A, 12, dtype, A)
