@@ -514,8 +514,8 @@ int rlcs_block_tables(const int32_t* cached, const int32_t* added, const int32_t
  * groups, d, page sizes, missing pages and alignment as in rlcs_prefix_attention_bf16; T at most 2^24.  Lengths are cut to max_len (keys beyond it are not
  * seen); max_new and max_len are the host's upper bounds from which the launch is sized.  Memory beyond a length is never used; what
  * lies within it is multiplied, by 0 where a token does not see it, and has to be finite.  Products are summed in fp32; the softmax
- * weights enter the second product as two bfloat16 parts where rows go in tiles of 16 (max_new times the heads on a key head up to 16, or a few
- * tiles of keys up to 768), and as one where they go in tiles of 128.
+ * weights enter the second product as two bfloat16 parts (16 bits of mantissa).  Rows go in tiles of 16 or of 128, by the bounds and the
+ * number of trajectories: the same token in another step may differ by the order of its fp32 sums, and by no more.
  * scale > 0.  workspace: at least rlcs_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned, no initialisation (may be NULL
  * where that is 0).  Every wait inside the kernels is bounded; should one run out, the rows concerned come out NaN.
  */

@@ -76,22 +76,23 @@ chunk_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUte
 
 // ---------------------------------------------------------------------------------------------- chunks of more than 16 rows
 // A tile of 128 rows a block on tcgen05, 64 keys a step.  Scores go into one of two 64-column buffers of tensor memory, the weights
-// back over them as bfloat16 (32 columns), O += P V is accumulated in tensor memory.  Four warps have one row a thread (maximum,
+// back over them as two bfloat16 parts (32 columns each), O += P V is accumulated in tensor memory.  Four warps have one row a thread (maximum,
 // exponentials, sums).  Two warps issue the products, one the scores and one the values: the scores of the next step are there when the
 // weights of this one leave.  Two warps copy keys and values through the page table into a ring of slots, as TMA boxes where pages
 // divide 64 keys into parts of at least eight rows or are whole tiles, piece by piece otherwise.  Two blocks share a
 // multiprocessor, so that one's start (lookups, queries) and end run under the other's products.
 //
-// One rounding of the weights to bfloat16, at most 2^-8 of each, is as large as the output's own; a second part would be half as many
-// value products again.
+// The weights' two parts hold 16 bits, as those of the 16-row tiles do: a token comes out the same, but for the order of fp32 sums, whatever
+// else is in its step.  The second part is half as many value products again, 8 to 21 % of the time (7 prompts 341 us with one part, long context
+// 458, drafts 158); one rounding, 2^-8 of each weight, would be an error as large as the output's own.
 //
 // Where the heads on a key head divide 128, a block's queries come, and its outputs leave, as boxes of whole tokens: sixteen loads a thread
 // took 2.6 us under the other block's exponentials.
 //
-// Bound by shared memory: a step's scores read 48 KB (queries and keys), its values 16, its copies write 32, for two blocks 192 KB or 1500
-// cycles of 128 bytes, against 1024 cycles of products and 1024 of exponentials; a step takes about 1700.  Measured (heads of 128): 7 prompts
-// of up to 4096 tokens, 32 heads on 8, 341 us for 321 GFLOP (0.57 of the bf16 rate); 1000 tokens behind 32768, 28 on 4, 458 us for
-// 477 GFLOP (0.63); 64 chunks of up to 8 tokens behind 4096 159 us (0.78 of the copy bandwidth).  Not kept: two row tiles a block that share
+// Bound by shared memory: a step's scores read 48 KB (queries and keys), its values 32, its copies write 32, for two blocks 224 KB or 1790
+// cycles of 128 bytes, against 1536 cycles of products and 1024 of exponentials; a step takes about 2000.  Measured (heads of 128): 7 prompts
+// of up to 4096 tokens, 32 heads on 8, 385 us for 321 GFLOP (0.50 of the bf16 rate); 1000 tokens behind 32768, 28 on 4, 557 us for
+// 477 GFLOP (0.52); 64 chunks of up to 8 tokens behind 4096 171 us (0.73 of the copy bandwidth).  Not kept, measured with one part: two row tiles a block that share
 // their keys, one block a multiprocessor (377, 488 us, and 216 for the chunks of drafts: nothing runs under a block's start and end); 128 keys a step into a single
 // buffer (467, 516: scores, weights and values in turn, some 250 cycles at every barrier); a quarter of the exponentials by polynomial
 // (no change); blocks of 126 rows where 7 heads share a key head, to have their boxes (500: one tile more is a round of blocks more).
@@ -341,15 +342,18 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                 float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
-                    uint32_t w[16];
+                    uint32_t hi[16], lo[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
                         float2 p = fma2(make_float2(__uint_as_float(s[part * 32 + 2 * k]), __uint_as_float(s[part * 32 + 2 * k + 1])), scale, less);
                         p = make_float2(exp2_of(p.x), exp2_of(p.y));
                         sum[k & 1] = add2(sum[k & 1], p);
-                        w[k] = pack2(p.x, p.y);
+                        hi[k] = pack2(p.x, p.y);
+                        p = fma2(make_float2(__uint_as_float(hi[k] << 16), __uint_as_float(hi[k] & 0xffff0000u)), make_float2(-1.f, -1.f), p);
+                        lo[k] = pack2(p.x, p.y);
                     }
-                    tmem_store16(s_at + part * 16, w);
+                    tmem_store16(s_at + part * 16, hi);
+                    tmem_store16(s_at + kKeys / 2 + part * 16, lo);
                 }
                 l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
                 tmem_wait_store();
@@ -574,7 +578,9 @@ wide_kernel(const __grid_constant__ ChunkParams C, const __grid_constant__ CUten
                         const uint64_t v_at = v_desc + slot * (Shape::kSlot >> 4);
 #pragma unroll
                         for (int s = 0; s < kKeys / 16; ++s)
-                            issue_ts(base + 128, base + (i & 1) * kKeys + s * 8, v_at + ((s * 2048) >> 4), kValues, i > 0 || s > 0);
+#pragma unroll
+                            for (int part = 0; part < 2; ++part)
+                                issue_ts(base + 128, base + (i & 1) * kKeys + part * (kKeys / 2) + s * 8, v_at + ((s * 2048) >> 4), kValues, i > 0 || s > 0 || part > 0);
                         issue_commit(o_done + 8 * (i & 1));
                         issue_commit(empty + 8 * slot);
                     }
