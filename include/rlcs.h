@@ -578,11 +578,15 @@ int rlcs_distill_grad_bf16(const uint16_t* logits, int64_t ld, const int32_t* te
 /*
  * Trajectories continued from others: row i of new_table [N, width] continues row s = sources[i] of block_table [B, width], which holds
  * lens[s] tokens in its first ceil(lens[s] / page_size) pages (at most `width`).  Whole pages are shared.  A part-filled last page
- * stays with the first row i that continues s; each other one gets, in row order, the next number of free_pages [free_count] in
+ * stays with the first row i that ends in that page, unless another new row has it as a whole page (branches that share a page and were cut
+ * back); every other row that ends in it gets, in row order, the next number of free_pages [free_count] in
  * its place, and copy_from[i] -> copy_to[i] says which page it has to be copied from (rlcs_copy_pages_bf16, once a layer).  Both
  * are -1 for rows that copy nothing; where the list has run out (or holds a negative number) they and the table's entry are -1.
  * Entries behind the pages, and rows whose source lies outside [0, B), are -1.  pages_used [1]: numbers asked of the list.  A part-filled
  * page beyond the table's width or of a negative number is not copied.  new_table must not be block_table.
+ * Tokens are written where a table says, whoever else names the page: a length that is lowered below the end of a page that another row
+ * names too wants a fork (sources = the rows' own numbers) before the row grows again.  Afterwards no part-filled page has two rows.  Pages
+ * that a prefix table names are not looked at: a row must not be cut back into one.
  * workspace: rlcs_fork_block_tables_workspace_bytes(B, N) bytes (0 up to 4096 rows each), 16-byte aligned, no initialisation.
  */
 size_t rlcs_fork_block_tables_workspace_bytes(int64_t B, int64_t N);

@@ -299,9 +299,10 @@ def compute_distillation(logits, teacher_ids, teacher_logits, *, mask=None, temp
 
 def fork_block_tables(block_table, lens, sources, free_pages, *, page_size, stream=None):
     """Trajectories continued from others (branches, resampling): row i of the new table continues row sources[i].  Whole pages are
-    shared; a part-filled last page is copied for every row but the first that continues it, to pages taken from free_pages:
-    (new_table, copy_from, copy_to, pages_used).  copy_pages makes the copies, layer by layer; pages_used (one element) above
-    the number of free pages says that the list ran out."""
+    shared; a part-filled last page is copied for every row but the first that ends in it (for all where another new row has that page
+    whole), to pages taken from free_pages: (new_table, copy_from, copy_to, pages_used).  copy_pages makes the copies, layer by layer;
+    pages_used (one element) above the number of free pages says that the list ran out.  Branches share pages: after lengths were lowered into
+    pages that other rows name, fork with sources 0 to B-1 before the rows grow, or they write over one another's keys."""
     return _B.rlcs_fork_block_tables(block_table, lens, sources, free_pages, page_size=page_size, stream=stream)
 
 
@@ -312,6 +313,6 @@ def copy_pages(k_cache, v_cache, copy_from, copy_to, *, stream=None):
 
 def list_free_pages(block_table, lens, *, num_pages, page_size, prefix_table=None, prefix_lens=None, stream=None):
     """The pages that no trajectory (and no shared prompt) names any more, ascending: (free_pages int32 [num_pages], -1 behind the last,
-    count [1]).  Freeing a trajectory is setting its length to 0, turning tokens down is lowering it; the list serves
-    build_block_tables and fork_block_tables as it is, without a word from the host."""
+    count [1]).  Freeing a trajectory is setting its length to 0, turning tokens down is lowering it (into a page that another row shares: see
+    fork_block_tables); the list serves build_block_tables and fork_block_tables as it is, without a word from the host."""
     return _B.rlcs_free_pages(block_table, lens, prefix_table, prefix_lens, num_pages=num_pages, page_size=page_size, stream=stream)

@@ -1200,7 +1200,7 @@ def rlcs_distill_grad_bf16(logits, teacher_ids, teacher_logits, *, mask=None, te
 def rlcs_fork_block_tables(block_table, lens, sources, free_pages, *, page_size, new_table=None, copy_from=None, copy_to=None, pages_used=None,
                            workspace=None, stream=None):
     """Page tables of rows that continue rows `sources` [N] of block_table [B, width]: whole pages shared, part-filled last ones copied
-    for all but the first row that continues them.  Returns (new_table [N, width], copy_from [N], copy_to [N], pages_used [1])."""
+    for all but the first row that ends in them (for all that do, where another new row has the page whole).  Returns (new_table [N, width], copy_from [N], copy_to [N], pages_used [1])."""
     if block_table.dim() != 2 or sources.dim() != 1 or free_pages.dim() != 1:
         raise ValueError("expected block_table [B, width], sources [N], free_pages [F]")
     dev = _device_for(block_table)

@@ -1,15 +1,17 @@
 // Pages of a paged cache: trajectories continued from others, copies of pages, and the pages that nobody names.
 //
-//   fork    new row i is the old row sources[i]: whole pages are shared, a part-filled last page stays with the first row that
-//           continues it and is copied for the others, to pages taken from the free list in row order
+//   fork    new row i is the old row sources[i]: whole pages are shared, a part-filled last page stays with the first row that ends
+//           in it, unless another has it whole, and is copied for the others, to pages taken from the free list in row order
 //   copy    pages from[i] -> to[i] of keys and values
 //   free    the numbers below num_pages that no live entry of the tables names, ascending
 //
 // What a page is shared by needs no counts: it is free when no table names it.
 //
-// Measured: 2048 rows forked and about 750 pages of 128 KB copied in both caches 75 us, of which the copies 65 (0.92 of the copy bandwidth),
-// a block's numbering of all rows 8; free pages among 9192 of 128 rows 6.8 us (one block), among 2.2 million of 4096 rows 22 us: 13 for 1.4 million
+// Measured: 2048 rows forked and about 750 pages of 128 KB copied in both caches 78 us, of which the copies 65 (0.92 of the copy bandwidth),
+// tables and numbers of all rows 12; 8 rows 8.5 us with their copies, a chain of a block's lookups; free pages among 9192 of 128 rows 6.8 us (one block), among 2.2 million of 4096 rows 22 us: 13 for 1.4 million
 // marks in L2 (plain stores of bytes took 10 more), 8 for the list, whose counts every block makes itself instead of another launch.
+#include <cooperative_groups.h>
+
 #include <cstdint>
 
 #include "../../include/rlcs.h"
@@ -17,11 +19,16 @@
 
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kThreads = 256, kFused = 4096;
 
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // ---------------------------------------------------------------------------------------------- fork
+// Who keeps a part-filled page goes by its number, not by the row that it comes from: branches share pages, and when they are cut back a
+// page that is whole for one may be part-filled for another, or for both.  A table of the part-filled pages' numbers (open addressing, at
+// most half full) has the first new row that ends in each, and whether a new row has it as a whole page; then nobody may write there.
 struct ForkParams {
     const int32_t* table;
     const int32_t* lens;
@@ -31,23 +38,51 @@ struct ForkParams {
     int32_t* from;
     int32_t* to;
     int32_t* used;
-    int32_t* first;            // [B] first new row of each old one     } of large calls, in the workspace
-    int32_t* number;           // [N] place in the free list, or -1     }
+    int32_t* keys;             // [slots] page numbers, -1: none                         } of large calls, in the workspace
+    uint32_t* owner;           // [slots] first new row that ends there + 1, 0: nobody   }
+    int32_t* number;           // [N] slot, then place in the free list; -1: none        }
     int32_t B, N, width, free_count, page;
+    int32_t slots, shift;      // a power of two, and 32 - its logarithm
+    bool fill;                 // whether fork_kernel writes whole tables
 };
 
 struct OldRow {
     int source, have, last;    // last: the page that a second row would copy, -1 without one
 };
 
+__device__ __forceinline__ uint32_t pages_of(int len, int page) { return ((uint32_t)max(len, 0) + page - 1) / (uint32_t)page; }      // page <= 2^24: no overflow
+
 __device__ __forceinline__ OldRow old_row(const ForkParams& P, int i) {
     OldRow r = {P.sources[i], 0, -1};
     if (r.source < 0 || r.source >= P.B) { r.source = -1; return r; }
     const int len = max(P.lens[r.source], 0);
-    const uint32_t need = ((uint32_t)len + P.page - 1) / (uint32_t)P.page;      // page <= 2^24: no overflow
+    const uint32_t need = pages_of(len, P.page);
     r.have = (int)min(need, (uint32_t)P.width);
     if (need <= (uint32_t)P.width && len % P.page != 0) r.last = P.table[(int64_t)r.source * P.width + r.have - 1];
     return r;
+}
+
+// Pages that a row of this length fills, of those that the table holds.
+__device__ __forceinline__ int whole_of(const ForkParams& P, int len) { return min(max(len, 0) / P.page, P.width); }
+
+__device__ __forceinline__ int slot_at(const ForkParams& P, int page) { return (int)((uint32_t)page * 2654435769u >> P.shift); }
+
+__device__ __forceinline__ int find_slot(const ForkParams& P, const int32_t* keys, int page) {
+    for (int h = slot_at(P, page);; h = (h + 1) & (P.slots - 1)) {      // half of the slots are free
+        const int k = keys[h];
+        if (k == page || k < 0) return k < 0 ? -1 : h;
+    }
+}
+
+// Row i ends in `page`: its slot.
+__device__ __forceinline__ int enter_page(const ForkParams& P, int32_t* keys, uint32_t* owner, int page, int i) {
+    int h = slot_at(P, page);
+    for (;; h = (h + 1) & (P.slots - 1)) {
+        const int k = atomicCAS(keys + h, -1, page);
+        if (k == -1 || k == page) break;
+    }
+    atomicMin(owner + h, (uint32_t)i + 1);
+    return h;
 }
 
 // The page that row i takes from the free list.
@@ -55,27 +90,26 @@ __device__ __forceinline__ int taken(const ForkParams& P, int number) {
     return number >= 0 && number < P.free_count ? max(P.free_pages[number], -1) : -1;
 }
 
-// Place in the free list of every row that needs a page, the rest -1, by the T threads of a block; four rows a thread at a time, whose
-// lookups (source, length, page) go together.
-template <int T> __device__ __forceinline__ void fork_numbers(const ForkParams& P, const int32_t* first, int32_t* number, bool write) {
+// number[i] from slots to places in the free list, for every row that needs a page; the rest -1.  By the T threads of a block, four rows a
+// thread at a time.
+template <int T> __device__ __forceinline__ void fork_numbers(const ForkParams& P, const uint32_t* owner, int32_t* number, bool write) {
     constexpr int kRows = 4;
     __shared__ int part[kRows][T / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int carry = 0;
     for (int base = 0; base < P.N; base += kRows * T) {
-        OldRow r[kRows];
+        int slot[kRows];
         unsigned some[kRows];
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             const int i = base + k * T + threadIdx.x;
-            r[k] = OldRow{-1, 0, -1};
-            if (i < P.N) r[k] = old_row(P, i);
+            slot[k] = i < P.N ? number[i] : -1;
         }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             const int i = base + k * T + threadIdx.x;
-            some[k] = __ballot_sync(~0u, r[k].last >= 0 && first[r[k].source] != i);
+            some[k] = __ballot_sync(~0u, slot[k] >= 0 && owner[slot[k]] != (uint32_t)i + 1);
             if (lane == 0) part[k][warp] = __popc(some[k]);
         }
         __syncthreads();
@@ -91,51 +125,125 @@ template <int T> __device__ __forceinline__ void fork_numbers(const ForkParams& 
     if (write && threadIdx.x == 0) *P.used = carry;
 }
 
-__global__ void __launch_bounds__(kThreads) fork_first_kernel(const __grid_constant__ ForkParams P) {
-    for (int i = blockIdx.x * kThreads + threadIdx.x; i < P.N; i += gridDim.x * kThreads) {
-        const int s = P.sources[i];
-        if (s >= 0 && s < P.B) atomicMin(P.first + s, i);
-    }
-}
-
-__global__ void __launch_bounds__(1024) fork_numbers_kernel(const __grid_constant__ ForkParams P) { fork_numbers<1024>(P, P.first, P.number, true); }
-
-constexpr int kWide = 1024;                  // threads where a block goes through all rows
-
-template <bool FUSED>
-__global__ void __launch_bounds__(kWide) fork_fill_kernel(const __grid_constant__ ForkParams P) {
-    extern __shared__ int32_t held[];
-    const int32_t* number = P.number;
-    if constexpr (FUSED) {
-        int32_t *first = held, *mine = held + P.B;
-        for (int s = threadIdx.x; s < P.B; s += kWide) first[s] = P.N;
-        __syncthreads();
-        for (int i = threadIdx.x; i < P.N; i += kWide) {
-            const int s = P.sources[i];
-            if (s >= 0 && s < P.B) atomicMin(first + s, i);
-        }
-        fork_numbers<kWide>(P, first, mine, blockIdx.x == 0);
-        __syncthreads();
-        number = mine;
-    }
-    const int64_t step = (int64_t)gridDim.x * kWide, me = (int64_t)blockIdx.x * kWide + threadIdx.x;
-    for (int64_t i = me; i < P.N; i += step) {
-        const int page = taken(P, number[i]);
-        P.from[i] = page >= 0 ? old_row(P, (int)i).last : -1;
-        P.to[i] = page;
-    }
+// The new tables as if nothing were copied, entries from `me` on.
+__device__ __forceinline__ void gather_tables(const ForkParams& P, int64_t me, int64_t step) {
     const int64_t cells = (int64_t)P.N * P.width;
     for (int64_t e = me; e < cells; e += step) {
         const int i = cells <= 0x7fffffff ? (int)((uint32_t)e / (uint32_t)P.width) : (int)(e / P.width);
         const int j = (int)(e - (int64_t)i * P.width);
         const int s = P.sources[i];
-        int v = -1;
-        if (s >= 0 && s < P.B) {
-            const uint32_t need = ((uint32_t)max(P.lens[s], 0) + P.page - 1) / (uint32_t)P.page;
-            if (j < need) v = j + 1 == need && number[i] >= 0 ? taken(P, number[i]) : P.table[(int64_t)s * P.width + j];
-        }
-        P.out[e] = v;
+        P.out[e] = s >= 0 && s < P.B && (uint32_t)j < pages_of(P.lens[s], P.page) ? P.table[(int64_t)s * P.width + j] : -1;
     }
+}
+
+// What row i copies, and its table's last entry where it does.
+__device__ __forceinline__ void give_page(const ForkParams& P, int i, int number) {
+    const int page = taken(P, number);
+    P.to[i] = page;
+    int from = -1;
+    if (number >= 0) {
+        const OldRow r = old_row(P, i);
+        P.out[(int64_t)i * P.width + r.have - 1] = page;
+        if (page >= 0) from = r.last;
+    }
+    P.from[i] = from;
+}
+
+constexpr int kWide = 1024;                  // threads where a block goes through all rows
+constexpr int kMostWays = 8;                 // blocks that share the whole pages
+
+// Up to kFused rows: the table of pages in the shared memory of each block of one cluster.  All blocks enter all rows; each looks a share of
+// the old tables' whole pages up, and tells the others what it finds (seldom anything); the numbers are again every block's own.
+__global__ void __launch_bounds__(kWide) fork_kernel(const __grid_constant__ ForkParams P) {
+    extern __shared__ int32_t held[];
+    int32_t* const keys = held;
+    uint32_t* const owner = reinterpret_cast<uint32_t*>(held + P.slots);
+    int32_t* const number = held + 2 * P.slots;
+    uint32_t* const continued = reinterpret_cast<uint32_t*>(number + P.N);      // a bit an old row
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int ways = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), tid = threadIdx.x;
+    auto sync = [&] { if (ways > 1) cluster.sync(); else __syncthreads(); };
+    for (int h = tid; h < P.slots; h += kWide) { keys[h] = -1; owner[h] = ~0u; }
+    for (int w = tid; w < (P.B + 31) / 32; w += kWide) continued[w] = 0;
+    __syncthreads();
+    for (int base = 0; base < P.N; base += 4 * kWide) {
+        OldRow r[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = base + k * kWide + tid;
+            r[k] = OldRow{-1, 0, -1};
+            if (i < P.N) r[k] = old_row(P, i);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = base + k * kWide + tid;
+            if (r[k].source >= 0) atomicOr(continued + (r[k].source >> 5), 1u << (r[k].source & 31));
+            if (i < P.N) number[i] = r[k].last >= 0 ? enter_page(P, keys, owner, r[k].last, i) : -1;
+        }
+    }
+    sync();
+    const int64_t cells = (int64_t)P.B * P.width, step = (int64_t)ways * kWide, me = (int64_t)rank * kWide + tid;
+    for (int64_t e = me; e < cells; e += 4 * step) {
+        int id[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t at = e + k * step;
+            id[k] = -1;
+            if (at >= cells) continue;
+            const int s = cells <= 0x7fffffff ? (int)((uint32_t)at / (uint32_t)P.width) : (int)(at / P.width);
+            if ((continued[s >> 5] >> (s & 31) & 1) && (int)(at - (int64_t)s * P.width) < whole_of(P, P.lens[s])) id[k] = P.table[at];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (id[k] < 0 || find_slot(P, keys, id[k]) < 0) continue;
+            for (int w = 0; w < ways; ++w) {                  // each block has its own order of the keys
+                const int h = find_slot(P, cluster.map_shared_rank(keys, w), id[k]);
+                if (h >= 0) cluster.map_shared_rank(owner, w)[h] = 0;
+            }
+        }
+    }
+    sync();
+    fork_numbers<kWide>(P, owner, number, rank == 0);
+    if (P.fill) gather_tables(P, me, step);
+    sync();                                                   // the last entries below may be another block's
+    for (int64_t i = me; i < P.N; i += step) give_page(P, (int)i, number[i]);
+}
+
+__global__ void __launch_bounds__(kThreads) fork_gather_kernel(const __grid_constant__ ForkParams P) {
+    gather_tables(P, (int64_t)blockIdx.x * kThreads + threadIdx.x, (int64_t)gridDim.x * kThreads);
+}
+
+// The same for more rows, the table of pages in the workspace.
+__global__ void __launch_bounds__(kThreads) fork_enter_kernel(const __grid_constant__ ForkParams P) {
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < P.N; i += gridDim.x * kThreads) {
+        const int last = old_row(P, i).last;
+        P.number[i] = last >= 0 ? enter_page(P, P.keys, P.owner, last, i) : -1;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) fork_whole_kernel(const __grid_constant__ ForkParams P) {
+    const int64_t cells = (int64_t)P.N * P.width;
+    for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < cells; e += (int64_t)gridDim.x * kThreads) {
+        const int i = cells <= 0x7fffffff ? (int)((uint32_t)e / (uint32_t)P.width) : (int)(e / P.width), j = (int)(e - (int64_t)i * P.width);
+        const int s = P.sources[i];
+        if (s < 0 || s >= P.B || j >= whole_of(P, P.lens[s])) continue;
+        const int id = P.table[(int64_t)s * P.width + j], h = id >= 0 ? find_slot(P, P.keys, id) : -1;
+        if (h >= 0) P.owner[h] = 0;
+    }
+}
+
+__global__ void __launch_bounds__(kWide) fork_numbers_kernel(const __grid_constant__ ForkParams P) { fork_numbers<kWide>(P, P.owner, P.number, true); }
+
+__global__ void __launch_bounds__(kThreads) fork_give_kernel(const __grid_constant__ ForkParams P) {
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < P.N; i += gridDim.x * kThreads) give_page(P, i, P.number[i]);
+}
+
+// Slots for the part-filled pages: twice as many as there can be, a power of two.
+int64_t fork_slots(int64_t B, int64_t N) {
+    const int64_t least = 2 * (B < N ? B : N);
+    int64_t slots = 2;
+    while (slots < least) slots *= 2;
+    return slots;
 }
 
 // ---------------------------------------------------------------------------------------------- copy
@@ -338,7 +446,8 @@ __global__ void __launch_bounds__(kList) free_alone_kernel(const __grid_constant
 extern "C" {
 
 size_t rlcs_fork_block_tables_workspace_bytes(int64_t B, int64_t N) {
-    return B <= 0 || N <= 0 || (B <= kFused && N <= kFused) ? 0 : (size_t)(B + N) * sizeof(int32_t);
+    if (B <= 0 || N <= 0 || (B <= kFused && N <= kFused) || B >= (int64_t(1) << 24) || N >= (int64_t(1) << 24)) return 0;
+    return (size_t)(2 * fork_slots(B, N) + N) * sizeof(int32_t);
 }
 
 int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, const int32_t* sources, const int32_t* free_pages,
@@ -360,20 +469,52 @@ int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, cons
         if (workspace == nullptr || workspace_bytes < need) return RLCS_ERR_WORKSPACE;
         if (!aligned_to(workspace, 16)) return RLCS_ERR_ALIGN;
     }
-    int32_t* const first = static_cast<int32_t*>(workspace);
-    const ForkParams P = {block_table, lens, sources, free_pages, new_table, copy_from, copy_to, pages_used, first, need > 0 ? first + B : nullptr,
-                          (int32_t)B, (int32_t)N, (int32_t)width, (int32_t)free_count, (int32_t)page_size};
     const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const int64_t most = N * (width > 0 ? width : 1), sms = rlcs_device::limits().sms;
-    int64_t blocks = (most + kWide * 2 - 1) / (kWide * 2);
-    blocks = blocks < 1 ? 1 : blocks > 2 * sms ? 2 * sms : blocks;
+    const int64_t slots = fork_slots(B, N);
+    int32_t* const keys = static_cast<int32_t*>(workspace);
+    ForkParams P = {block_table, lens, sources, free_pages, new_table, copy_from, copy_to, pages_used, keys, nullptr, nullptr,
+                    (int32_t)B, (int32_t)N, (int32_t)width, (int32_t)free_count, (int32_t)page_size, (int32_t)slots, 32, false};
+    for (int64_t n = slots; n > 1; n /= 2) --P.shift;
+    const int64_t cells = N * width, sms = rlcs_device::limits().sms;
+    auto blocks_for = [&](int64_t items) { const int64_t n = (items + kThreads - 1) / kThreads; return (unsigned)(n < 1 ? 1 : n < 8 * sms ? n : 8 * sms); };
     if (need == 0) {
-        fork_fill_kernel<true><<<(unsigned)blocks, kWide, (B + N) * sizeof(int32_t), s>>>(P);
+        static bool granted[64];
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RLCS_ERR_CUDA;
+        if (!granted[dev]) {
+            const int most = (2 * (int)fork_slots(kFused, kFused) + kFused + kFused / 32) * (int)sizeof(int32_t);
+            if (cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return RLCS_ERR_CUDA;
+            granted[dev] = true;
+        }
+        // one block while every thread has up to four entries, else eight; tables of more than two entries a thread of those are written by
+        // a launch of their own
+        int ways = 1;
+        if (B * width > 4 * kWide || cells > 4 * kWide) ways = kMostWays;
+        P.fill = cells <= 2 * kMostWays * kWide;
+        if (!P.fill) fork_gather_kernel<<<blocks_for(cells), kThreads, 0, s>>>(P);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)ways);
+        cfg.blockDim = dim3(kWide);
+        cfg.dynamicSmemBytes = (size_t)(2 * slots + N + (B + 31) / 32) * sizeof(int32_t);
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = ways;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaLaunchKernelEx(&cfg, fork_kernel, P) != cudaSuccess) return RLCS_ERR_CUDA;
     } else {
-        if (cudaMemsetAsync(first, 0x7f, (size_t)B * sizeof(int32_t), s) != cudaSuccess) return RLCS_ERR_CUDA;
-        fork_first_kernel<<<(unsigned)((N + kThreads - 1) / kThreads < 4 * sms ? (N + kThreads - 1) / kThreads : 4 * sms), kThreads, 0, s>>>(P);
-        fork_numbers_kernel<<<1, 1024, 0, s>>>(P);
-        fork_fill_kernel<false><<<(unsigned)blocks, kWide, 0, s>>>(P);
+        P.owner = reinterpret_cast<uint32_t*>(keys + slots);
+        P.number = keys + 2 * slots;
+        if (cudaMemsetAsync(keys, 0xff, (size_t)slots * 2 * sizeof(int32_t), s) != cudaSuccess) return RLCS_ERR_CUDA;
+        fork_enter_kernel<<<blocks_for(N), kThreads, 0, s>>>(P);
+        if (cells > 0) {
+            fork_whole_kernel<<<blocks_for(cells), kThreads, 0, s>>>(P);
+            fork_gather_kernel<<<blocks_for(cells), kThreads, 0, s>>>(P);
+        }
+        fork_numbers_kernel<<<1, kWide, 0, s>>>(P);
+        fork_give_kernel<<<blocks_for(N), kThreads, 0, s>>>(P);
     }
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;
 }

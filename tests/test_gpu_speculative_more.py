@@ -36,3 +36,147 @@ def test_chunk_weights_keep_sixteen_bits_whatever_else_is_in_the_step(api, H, Hk
         assert ((lse - want_lse[:n]).abs() <= 1e-5 + 2.0 ** -22 * want_lse[:n].abs()).all()
         err = (out - want[:n]).abs() - 2.0 ** -8 * want[:n].abs() - 2.0 ** -15 * (size[:n] + most)
         assert (err <= 0).all(), err.max()
+
+
+# ------------------------------------------------------------------------------------------ pages
+def plain_fork_by_page(table, lens, sources, free, page):
+    """A part-filled page belongs to the first new row that ends in it, and to none where a new row has it whole."""
+    B, width = table.shape
+    rows, ends, whole, first = [], [], set(), {}
+    for i, s in enumerate(sources):
+        row, end = [-1] * width, -1
+        if 0 <= s < B:
+            n = max(int(lens[s]), 0)
+            need = -(-n // page)
+            row[:min(need, width)] = [int(v) for v in table[s, :min(need, width)]]
+            whole.update(row[:min(n // page, width)])
+            if n % page and need <= width and row[need - 1] >= 0:
+                end = need - 1
+                first.setdefault(row[end], i)
+        rows.append(row), ends.append(end)
+    come, go, used = [-1] * len(rows), [-1] * len(rows), 0
+    for i, (row, end) in enumerate(zip(rows, ends)):
+        if end >= 0 and (row[end] in whole or first[row[end]] != i):
+            new = max(int(free[used]), -1) if used < len(free) else -1
+            come[i], go[i], row[end] = (row[end] if new >= 0 else -1), new, new
+            used += 1
+    return rows, come, go, used
+
+
+@pytest.mark.parametrize("B,N,width", [(1, 3, 4), (5, 9, 3), (40, 40, 7), (300, 200, 20), (1000, 1500, 33), (4096, 4096, 9), (700, 5000, 6), (6000, 6000, 5), (5000, 3, 4)])
+def test_fork_goes_by_the_page_that_is_shared(api, B, N, width):
+    """Tables whose rows share pages with one another at any place, as whole pages, as part-filled ones and as both."""
+    page = 16
+    g = torch.Generator().manual_seed(B + N)
+    table = torch.randperm(4 * B * width, generator=g)[:B * width].to(I32).view(B, width)
+    like = torch.randint(0, B, (B,), generator=g)
+    upto = torch.randint(0, width + 1, (B,), generator=g)
+    for _ in range(2):                                                 # branches, and branches of branches
+        table = torch.where(torch.arange(width)[None] < upto[:, None], table[like], table)
+    some = torch.rand(B, generator=g) < 0.1                            # and pages at another place than their owner's
+    table[some, width - 1] = table[like[some], 0]
+    lens = torch.randint(0, width * page + 20, (B,), generator=g, dtype=I32)
+    sources = torch.randint(-1, B + 1, (N,), generator=g, dtype=I32)
+    if N == B:
+        sources = torch.arange(B, dtype=I32)                           # every row continues itself
+    for free in (torch.arange(4 * B * width, 4 * B * width + N, dtype=I32), torch.arange(4 * B * width, 4 * B * width + N // 4, dtype=I32)):
+        want = plain_fork_by_page(table, lens.tolist(), sources.tolist(), free.tolist(), page)
+        got = api.fork_block_tables(up(table), up(lens), up(sources), up(free), page_size=page)
+        for a, b in zip(got, want[:3] + ([want[3]],)):
+            assert torch.equal(a.cpu(), torch.tensor(b, dtype=I32).view(a.shape))
+        # with pages enough nobody can write into what another row has
+        if N == len(free):
+            ends = {}
+            new = got[0].tolist()
+            for i, s in enumerate(sources.tolist()):
+                n = max(int(lens[s]), 0) if 0 <= s < B else 0
+                if n % page and -(-n // page) <= width:
+                    ends[i] = new[i][n // page]
+            for i, s in enumerate(sources.tolist()):
+                n = max(int(lens[s]), 0) if 0 <= s < B else 0
+                for j, p in enumerate(new[i][:min(-(-n // page), width)]):
+                    new[i][j] = (p, j == n // page)
+            owners = {}
+            for i, p in ends.items():
+                assert owners.setdefault(p, i) == i                    # one row a part-filled page
+            assert not any(p in owners and not last for row in new for p, last in (v for v in row if isinstance(v, tuple)))
+
+
+def test_branches_cut_back_into_a_shared_page_grow_apart(api):
+    """Fork, lower both branches into a page that they share, fork again, add tokens: every row keeps its own keys."""
+    page, width, Hk, d = 16, 6, 1, 64
+    pages = 40
+    k = torch.zeros(pages, page, Hk, d, dtype=BF16, device="cuda")
+    v = torch.zeros_like(k)
+    table = torch.full((4, width), -1, dtype=I32, device="cuda")
+    lens = torch.zeros(4, dtype=I32, device="cuda")
+    texts = [[] for _ in range(4)]                                     # a number a token
+
+    def add(counts, values):
+        nonlocal lens
+        free, _ = api.list_free_pages(table, lens, num_pages=pages, page_size=page)
+        slots, _, _, _ = api.build_block_tables(lens, up(ints(counts)), free, table, page_size=page, num_slots=sum(counts))
+        assert len(set(slots.tolist())) == sum(counts)                 # no two tokens in one place
+        k.view(-1, Hk, d)[slots] = up(torch.tensor(values, dtype=F32).to(BF16))[:, None, None].expand(-1, Hk, d)
+        v.view(-1, Hk, d)[slots] = -k.view(-1, Hk, d)[slots]
+        lens = lens + up(ints(counts))
+        at = 0
+        for b, n in enumerate(counts):
+            texts[b] = texts[b] + values[at:at + n]
+            at += n
+
+    def cut(to):
+        nonlocal lens
+        lens = torch.minimum(lens, up(ints(to)))
+        for b, n in enumerate(to):
+            texts[b] = texts[b][:n]
+
+    def fork(sources):
+        nonlocal table, lens, texts
+        free, _ = api.list_free_pages(table, lens, num_pages=pages, page_size=page)
+        table, come, go, _ = api.fork_block_tables(table, lens, up(ints(sources)), free, page_size=page)
+        api.copy_pages(k, v, come, go)
+        lens, texts = lens[up(ints(sources)).long()], [list(texts[s]) for s in sources]
+        return [c for c in come.tolist() if c >= 0]
+
+    def check():
+        for b, text in enumerate(texts):
+            assert int(lens[b]) == len(text)
+            at = [int(table[b, i // page]) * page + i % page for i in range(len(text))]
+            assert k.view(-1, d)[at, 0].tolist() == text and (v.view(-1, d)[at, 0] == -k.view(-1, d)[at, 0]).all()
+
+    add([40, 3, 0, 0], [float(i) for i in range(43)])
+    fork([0, 0, 0, 1])                                                 # three rows of 40, one of 3
+    check()
+    cut([20, 24, 40, 3])                                               # two end in the second page, which the third has whole
+    assert len(fork([0, 1, 2, 3])) == 2
+    check()
+    add([15, 9, 5, 20], [float(100 + i) for i in range(49)])
+    check()
+    fork([0, 0, 1, 2])
+    cut([25, 22, 30, 35])                                              # two end in a page that nobody has whole, one of them may stay
+    assert len(fork([0, 1, 2, 3])) == 1
+    add([20, 20, 7, 2], [float(160 + i) for i in range(49)])
+    check()
+
+
+def test_fork_captured_twice_and_replayed(api):
+    """Two graphs of forks of more rows than one block holds share nothing."""
+    g = torch.Generator().manual_seed(1)
+    graphs = []
+    for n in (300, 5000):
+        table, lens = up(torch.randperm(4 * n, generator=g).to(I32).view(n, 4)), up(torch.randint(0, 65, (n,), generator=g, dtype=I32))
+        sources, free = up(torch.randint(0, n, (n,), generator=g, dtype=I32)), up(torch.arange(4 * n, 5 * n, dtype=I32))
+        api.fork_block_tables(table, lens, sources, free, page_size=16)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = api.fork_block_tables(table, lens, sources, free, page_size=16)
+        graphs.append((graph, got, (table, lens, sources, free)))
+    for _ in range(2):
+        for _, _, (table, lens, sources, free) in graphs:
+            lens.copy_(torch.randint(0, 65, lens.shape, generator=g, dtype=I32))
+        for graph, _, _ in graphs:
+            graph.replay()
+        for _, got, (table, lens, sources, free) in graphs:
+            for a, b in zip(got, api.fork_block_tables(table, lens, sources, free, page_size=16)):
+                assert torch.equal(a, b)
