@@ -470,6 +470,14 @@ int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, cons
         if (!aligned_to(workspace, 16)) return RLCS_ERR_ALIGN;
     }
     const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    if (B == 0 || N == 0) {                                       // nothing to continue, or nobody who does
+        if (cudaMemsetAsync(pages_used, 0, sizeof(int32_t), s) != cudaSuccess) return RLCS_ERR_CUDA;
+        if (N > 0 && (cudaMemsetAsync(copy_from, 0xff, (size_t)N * sizeof(int32_t), s) != cudaSuccess ||
+                      cudaMemsetAsync(copy_to, 0xff, (size_t)N * sizeof(int32_t), s) != cudaSuccess ||
+                      (width > 0 && cudaMemsetAsync(new_table, 0xff, (size_t)(N * width) * sizeof(int32_t), s) != cudaSuccess)))
+            return RLCS_ERR_CUDA;
+        return RLCS_OK;
+    }
     const int64_t slots = fork_slots(B, N);
     int32_t* const keys = static_cast<int32_t*>(workspace);
     ForkParams P = {block_table, lens, sources, free_pages, new_table, copy_from, copy_to, pages_used, keys, nullptr, nullptr,

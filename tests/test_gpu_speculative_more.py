@@ -160,6 +160,12 @@ def test_branches_cut_back_into_a_shared_page_grow_apart(api):
     check()
 
 
+def test_fork_of_no_rows_into_many(api):
+    new, come, go, used = api.fork_block_tables(torch.zeros(0, 3, dtype=I32, device="cuda"), up(ints([])), up(torch.zeros(20000, dtype=I32)), up(ints([1])),
+                                                page_size=16)
+    assert (new == -1).all() and new.shape == (20000, 3) and (come == -1).all() and (go == -1).all() and used.tolist() == [0]
+
+
 def test_fork_captured_twice_and_replayed(api):
     """Two graphs of forks of more rows than one block holds share nothing."""
     g = torch.Generator().manual_seed(1)
