@@ -565,8 +565,8 @@ int rlcs_verify_drafts_bf16(const uint16_t* logits, int64_t ld, const uint16_t* 
  *   loss[r] = scale * sum_i p_i (log p_i - lq_{id_i})      (entries with p_i = 0 add nothing)
  *   dlogits[r,j] = scale / temperature * (exp(lq_j) - sum_{i: id_i = j} p_i)      (row r at dlogits + r*ldd; rounded once)
  * Log-probabilities serve as teacher logits too.  A row whose mask is 0 (mask may be NULL: all rows live), without entries above -inf, or whose
- * logits are all -inf is left out: loss and gradient 0.  In other rows a logit of -inf has probability 0 and gradient 0 (loss +inf where the
- * teacher names it); a NaN or +inf among the row's logits or teacher entries makes loss and gradient NaN.  Sums are fp32 relative to the maximum.
+ * logits are all -inf is left out: loss and gradient 0.  In other rows a logit of -inf has probability 0, and gradient 0 unless the teacher
+ * gives it some (then loss +inf, and the gradient what the formula leaves, -scale / temperature * its probability); a NaN or +inf among the row's logits or teacher entries makes loss and gradient NaN.  Sums are fp32 relative to the maximum.
  * loss or dlogits may be NULL; dlogits may be the logits themselves (same pointer, ldd = ld).  temperature > 0.
  */
 int rlcs_distill_grad(const float* logits, int64_t ld, const int32_t* teacher_ids, const float* teacher_logits, const uint8_t* mask, float* loss,

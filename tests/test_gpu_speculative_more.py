@@ -186,3 +186,38 @@ def test_fork_captured_twice_and_replayed(api):
         for _, got, (table, lens, sources, free) in graphs:
             for a, b in zip(got, api.fork_block_tables(table, lens, sources, free, page_size=16)):
                 assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------ distillation
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A,K,times", [(3, 2, 1), (18, 5, 40), (100, 40, 1), (700, 20, 1), (1500, 300, 1), (6000, 9, 70), (6000, 9, 1), (70001, 33, 1), (600000, 4, 1)])
+def test_distill_gradient_of_excluded_logits_is_the_formulas(api, A, K, times, dtype):
+    """Logits of -inf, named by the teacher (once, twice, with no probability) and not: scale / T (0 - sum p), to a rounding of p and the
+    result's own; in short rows, rows of a block, and rows of a cluster."""
+    g = torch.Generator().manual_seed(A)
+    R, T, scale = 6, 1.3, 0.7
+    x = (torch.randn(R, A, generator=g) * 2).to(dtype)
+    ids = torch.stack([torch.randperm(A, generator=g)[:K] for _ in range(R)]).to(I32)
+    teacher = torch.randn(R, K, generator=g)
+    other = torch.rand(R, A, generator=g) < 0.3
+    other.scatter_(1, ids.long(), False)
+    x[other] = -math.inf
+    for r in range(R):
+        x[r, ids[r, r % K].long()] = -math.inf
+    ids[3, 1] = ids[3, 0]
+    x[3, ids[3, 0].long()] = -math.inf
+    teacher[4, 4 % K] = -math.inf                                      # named, but with no probability
+    if A == 3:
+        x[:, [a for a in range(3) if a not in ids[0].tolist()]] = 0.5
+    some = (x > -math.inf).any(1)
+    p = torch.softmax(teacher.double() / T, 1)
+    dense = torch.zeros(R, A, dtype=torch.float64).scatter_add_(1, ids.long(), p)
+    want = scale / T * (torch.softmax(x.double() / T, 1) - dense)
+    loss, grad = api.compute_distillation(up(x.repeat(times, 1)), up(ids.repeat(times, 1)), up(teacher.repeat(times, 1)), temperature=T, scale=scale)
+    loss, grad = loss.cpu().view(times, R), grad.cpu().double().view(times, R, A)
+    out = (x == -math.inf) & some[:, None]
+    assert (grad[:, out & (dense == 0)] == 0).all()
+    bound = (1e-5 + (2.0 ** -8 if dtype == BF16 else 2.0 ** -22)) * want.abs()
+    assert ((grad - want)[:, out].abs() <= bound[out]).all()
+    named = out & (dense > 0)
+    assert torch.equal(loss[0] == math.inf, named.any(1)) and (loss == loss[0]).all()
