@@ -538,8 +538,9 @@ int rlcs_chunk_attention_bf16(const uint16_t* q, int64_t q_stride, const uint16_
  *   the draft x = tokens[t+1] stays while  uniforms[t] * (v_x * W) < w_x * V  (in 64-bit floats, from left to right)
  *   at the first row r whose draft does not stay, or at the last row, a token is drawn: the first index, in index order, whose
  *   weights sum to more than floor(draw_uniforms[b] * their sum), of the weights
- *     max(0, floor(w_j 2^40 / W) - floor(v_j 2^40 / V))  at a turned-down draft (w_j where nothing is left of them; without
- *     draft_logits w_j, but 0 for the draft itself),  and  w_j  at the last row
+ *     max(0, floor(w_j P) - floor(v_j Q))  at a turned-down draft, with P = 2^40 / W and Q = 2^40 / V (Q = 0 where V is) rounded to 64-bit
+ *     floats, and so each product before its floor (w_j where nothing is left of them; without draft_logits w_j, but 0 for the draft
+ *     itself),  and  w_j  at the last row
  *   out_tokens[t]: the draft for rows before r, the drawn token at r, -1 behind;   accepted[b] = r - offsets[b]
  *   log_probs[t]: log-probability of out_tokens[t] under the target's whole softmax at T (within 1e-5 and 2^-22 of its size), -inf where that is -1
  * T <= 0 (or NaN): drafts stay while they are the target's most likely token (of equals the lowest index), which is also what is drawn;

@@ -6,7 +6,8 @@
 //
 // All choices go by whole weights w_j = floor(2^31 exp((l_j - max) / T) + 1/2), as action sampling's do: their sums are exact, so that
 // neither verdict nor draw depends on how a row is split over threads.  A difference of two distributions is taken in units of
-// 2^-40: floor(w_j 2^40 / W) - floor(v_j 2^40 / V).
+// 2^-40: floor(w_j P) - floor(v_j Q) with P = 2^40 / W, Q = 2^40 / V and the products rounded to 64-bit floats: a multiplication an entry instead of a
+// division, and the same whole numbers in any program that rounds there.
 //
 // Two kernels.  The first reads every row once, at the rate of the memory, and leaves its maximum and the sum of its exponentials
 // (the hardware's, summed in fp32 over 32 and in 64 bits beyond: within 2^-15 of the whole weights' sum, but for one half a weight).  The
@@ -323,8 +324,8 @@ __device__ __forceinline__ u64 redux_sum(u64 v) {
     return (u64)a + ((u64)b << 20) + ((u64)__reduce_add_sync(~0u, (uint32_t)(v >> 40)) << 40);
 }
 
-// 2^52 + floor(w unit), for floor(w unit) < 2^52, as the bits of a double: differences of two are those of the floors.  Conversions between
-// integers and doubles, which this does without, have a quarter of the rate of 64-bit additions.
+// 2^52 + floor(w unit), the product rounded to nearest before its floor, for floor(w unit) < 2^52, as the bits of a double: differences of two
+// are those of the floors.  Conversions between integers and doubles, which this does without, have a quarter of the rate of 64-bit additions.
 __device__ __forceinline__ long long shares_of(uint32_t w, double unit) {
     return __double_as_longlong(__dadd_rd((__hiloint2double(0x43300000, (int)w) - 0x1p52) * unit, 0x1p52));
 }

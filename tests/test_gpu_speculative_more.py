@@ -221,3 +221,65 @@ def test_distill_gradient_of_excluded_logits_is_the_formulas(api, A, K, times, d
     assert ((grad - want)[:, out].abs() <= bound[out]).all()
     named = out & (dense > 0)
     assert torch.equal(loss[0] == math.inf, named.any(1)) and (loss == loss[0]).all()
+
+
+# ------------------------------------------------------------------------------------------ verification
+def nearest(n, d):
+    """n / d (whole numbers) rounded to 53 bits, ties to even, as a fraction of whole numbers: by long division alone."""
+    if n == 0:
+        return 0, 1
+    down = n.bit_length() - d.bit_length() - 54                        # the quotient has 54 or 55 bits
+    q, rest = divmod(n << max(-down, 0), d << max(down, 0))
+    over = q.bit_length() - 53
+    low, q = q & ((1 << over) - 1), q >> over
+    half = 1 << (over - 1)
+    if low > half or (low == half and (rest or q & 1)):
+        q += 1
+    return (q << max(down + over, 0)), (1 << max(-down - over, 0))
+
+
+def test_nearest_is_what_it_says():
+    for n, d in ((2 ** 40, 3), (2 ** 40, 5071373719), (1, 7), (2 ** 60 + 1, 1), (2 ** 54 + 2, 1), (2 ** 54 + 6, 1), (10 ** 18 + 1, 10 ** 3)):
+        a, b = nearest(n, d)
+        assert a / b == n / d
+
+
+def shares(weights, total, rounded):
+    """Shares of 2^40: the header's (quotient and product rounded) or the exact floors."""
+    if not rounded:
+        return [w * 2 ** 40 // total for w in weights]
+    a, b = nearest(2 ** 40, total)
+    return [n // d for n, d in (nearest(w * a, b) for w in weights)]
+
+
+def test_verify_difference_is_rounded_as_the_header_says(api):
+    """Rows where the header's shares draw another token than exact floors would: a draft policy with one more, weak entry, so that the
+    difference is a few thousand units in which every single one can be drawn."""
+    g = torch.Generator().manual_seed(11)
+    R, A = 60000, 8
+    x = -torch.rand(R, A, generator=g)
+    x[:, 0] = 0.0
+    drafts = x.clone()
+    x[:, 7], drafts[:, 7] = -math.inf, -16.0 - torch.rand(R, generator=g)
+    weights = [(torch.exp(up(v)).cpu().double() * 2.0 ** 31 + 0.5).floor().long().tolist() for v in (x, drafts)]
+    rows, u, want, other = [], [], [], []
+    for r, (w, v) in enumerate(zip(*weights)):
+        sums = []
+        for rounded in (True, False):
+            left = [max(0, a - b) for a, b in zip(shares(w, sum(w), rounded), shares(v, sum(v), rounded))]
+            sums.append([sum(left[:j + 1]) for j in range(A)])
+        if sums[0] == sums[1] or not 0 < sums[0][-1] < 2 ** 20:
+            continue
+        draw = lambda s, c: next(j for j in range(A) if s[j] > math.floor(c * s[-1]))
+        for j in range(A - 1):                                         # uniforms on both sides of every border
+            for at in (sums[0][j] - 0.5, sums[0][j] + 0.5):
+                c = float(torch.tensor(at / sums[0][-1], dtype=F32))
+                if 0 <= c < 1 and draw(sums[0], c) != draw(sums[1], c):
+                    rows.append(r), u.append(c), want.append(draw(sums[0], c)), other.append(draw(sums[1], c))
+    assert len(rows) >= 5
+    n = len(rows)
+    pick = torch.tensor(rows).repeat_interleave(2)                     # a draft of entry 7, which the target never takes, and the last row
+    tokens = ints([0, 7] * n)
+    out, _, acc = api.verify_drafts(up(x[pick]), up(tokens), up(ints(list(range(0, 2 * n + 1, 2)))), up(torch.full((2 * n,), 0.5)),
+                                    up(torch.tensor(u, dtype=F32)), draft_logits=up(drafts[pick]))
+    assert (acc == 0).all() and out[::2].tolist() == want and want != other
