@@ -10,7 +10,7 @@
 // division, and the same whole numbers in any program that rounds there.
 //
 // Two kernels.  The first reads every row once, at the rate of the memory, and leaves its maximum and the sum of its exponentials
-// (the hardware's, summed in fp32 over 32 and in 64 bits beyond: within 2^-15 of the whole weights' sum, but for one half a weight).  The
+// (the hardware's, summed in fp32 over 32 and in 64 bits beyond: within 2^-15 of the whole weights' sum, but for a weight an entry; derived below).  The
 // second has a cluster a trajectory.  A draft whose verdict is the same anywhere within those bounds, nearly every one, needs no
 // more; another row's weights are summed up exactly, and so are those of the row from which the next token is drawn.
 //
@@ -92,6 +92,16 @@ template <typename T> __device__ __forceinline__ int seq_of(const VerifyParams<T
 // G threads a row (a warp, eight rows a block; or the block), which may be one of P.parts of it.
 constexpr int kScan = 256, kAhead = 4;       // threads; 16-byte vectors of a row that a thread has at a time
 
+// How far off a row's sum S = sum 2^-d_j may be, d_j = (max l - l_j) log2(e) / T.  A thread's base follows its maximum only when it is kBehind
+// binary places behind: if it followed every time, a rising row would be rescaled by up to 1024 approximations in a row, whose errors add up.  An
+// entry's exponential is a product of at most 3 + (d + 8) / 8 of the hardware's (2^-22 each): its own, one for each time that the base moved on, the
+// thread's join and the part's.  Their exponents add up to d in pieces of at most d + 16 in all, each rounded five times (1 / T, log2(e) / T with its constant, difference, product:
+// 4.5 * 2^-24 of it).  The mean of d over the row's probabilities is at most log2 A <= 22, so that the sum is off by
+//   ln 2 (22 + 16) 4.5 * 2^-24 + (3 + 30 / 8) 2^-22  and  10 * 2^-24 of the fp32 sums of 32,  together 39 * 2^-22 = 9.2e-6 of itself:
+// below the 1e-5 of log-probabilities.  The whole weights come from expf (2^-23) of an argument rounded twice, another 4 * 2^-22, and half a
+// weight an entry: 43 * 2^-22 < 2^-15 and A / 2; entries beyond d = 32, whose share may be off by more, weigh nothing and are within the other A / 2.
+constexpr float kBehind = 8.f;
+
 template <typename T, int G>
 __global__ void __launch_bounds__(kScan) verify_scan_kernel(const __grid_constant__ VerifyParams<T> P) {
     constexpr int N = Vec<T>::N;
@@ -121,17 +131,22 @@ __global__ void __launch_bounds__(kScan) verify_scan_kernel(const __grid_constan
         const int token = P.tokens[t + 1];
         if (token >= 0 && token < P.A) picked = clean(Vec<T>::load(x + token));
     }
-    float m = -INFINITY;
+    float m = -INFINITY, base = -INFINITY;                   // the thread's maximum, and what its sum is relative to
     double all = 0.;
     int chunk = -1;                                          // where the thread's maximum came first: a chunk of vectors, or -2 - a single
+    auto follow = [&] {
+        if ((m - base) * k <= kBehind) return;
+        all = base == -INFINITY ? 0. : all * (double)exp2_of((base - m) * k);
+        base = m;
+    };
     for (int i = me; i < singles; i += G) {
         const float f = Vec<T>::load(x + single(i));
         if (f > m) {
-            all = all * (double)exp2_of((m - f) * k);
             m = f;
             chunk = -2 - i;
+            follow();
         }
-        if (m != -INFINITY) all += (double)exp2_of((f - m) * k);
+        if (m != -INFINITY) all += (double)exp2_of((f - base) * k);
     }
     auto take = [&](int c, auto whole) {
         uint4 v[kAhead];
@@ -146,12 +161,12 @@ __global__ void __launch_bounds__(kScan) verify_scan_kernel(const __grid_constan
             most = Vec<T>::most_number(most, Vec<T>::most_number(Vec<T>::most_number(v[q].x, v[q].y), Vec<T>::most_number(v[q].z, v[q].w)));
         const float top = Vec<T>::most_number_of(most);
         if (top > m || (top == m && chunk < -1)) {           // of equals a vector's place, unless a single's comes before: below
-            all = m == -INFINITY ? 0. : all * (double)exp2_of((m - top) * k);
             m = top;
             chunk = c;
+            follow();
         }
         if (m == -INFINITY) return;
-        const float2 less = {-m, -m}, scale = {k, k};
+        const float2 less = {-base, -base}, scale = {k, k};
         float2 s[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
@@ -194,7 +209,7 @@ __global__ void __launch_bounds__(kScan) verify_scan_kernel(const __grid_constan
             if (Vec<T>::load(x + single(i)) == top) { best = min(best, single(i)); break; }
     }
     best = __reduce_min_sync(~0u, best);
-    if (m != top) all = m == -INFINITY ? 0. : all * (double)exp2_of((m - top) * k);
+    if (base != top) all = base == -INFINITY ? 0. : all * (double)exp2_of((base - top) * k);
     all = warp_sum(all);
     if (G > 32) {
         if (lane == 0) { sums[warp] = all; bests[warp] = best; }

@@ -4,6 +4,7 @@ and rows and weights at the edges of what the formulas say.
 Tolerances count roundings: a bfloat16 result is off by at most 2^-8 of its value (half a step), a fp32 one by 2^-24."""
 import math
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -11,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 from _util import guarded_empty  # noqa: E402
 from test_gpu_operators import BF16, F32, up  # noqa: E402
-from test_gpu_speculative import I32, Paged, api, ints, plain_chunks  # noqa: E402,F401
+from test_gpu_speculative import I32, Paged, api, check_verify, ints, plain_chunks, plain_weights, verify_inputs  # noqa: E402,F401
 
 
 # ------------------------------------------------------------------------------------------ attention of chunks
@@ -283,3 +284,39 @@ def test_verify_difference_is_rounded_as_the_header_says(api):
     out, _, acc = api.verify_drafts(up(x[pick]), up(tokens), up(ints(list(range(0, 2 * n + 1, 2)))), up(torch.full((2 * n,), 0.5)),
                                     up(torch.tensor(u, dtype=F32)), draft_logits=up(drafts[pick]))
     assert (acc == 0).all() and out[::2].tolist() == want and want != other
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_verify_log_probs_of_rows_that_keep_rising(api, dtype):
+    """Rows whose maximum rises with every load of every thread, by steps of 1e-8 to 0.01 (bfloat16: powers of two): 1e-5 and 2^-22 of the value."""
+    R, A = 300, 1 << 22
+    each = 4096 if dtype == F32 else 8192
+    place = torch.arange(A, device="cuda") // each
+    rise = 1e-8 * 1.047 ** torch.arange(R, device="cuda") if dtype == F32 else 2.0 ** -(4 + torch.arange(R, device="cuda") % 4).float()
+    x = (place[None] * rise[:, None]).to(dtype)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    du = torch.rand(R, device="cuda", generator=g)
+    out, lp, acc = api.verify_drafts(x, torch.zeros(R, dtype=I32, device="cuda"), torch.arange(R + 1, dtype=I32, device="cuda"), torch.zeros(R, device="cuda"), du)
+    for r in range(R):
+        want = torch.log_softmax(x[r].double(), 0)[out[r].long()]
+        assert abs(float(lp[r] - want)) <= 1e-5 + 2.0 ** -22 * abs(float(want)), (r, float(lp[r] - want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("A,top", [(20000, 3.0), (70003, 30.0)])
+def test_verify_uniforms_at_the_border_of_rising_rows(api, A, top, dtype):
+    x, tokens, offsets, u, du, drafts = verify_inputs([3, 2], A, dtype, A, near=0.1)
+    x = (x.float() * 0.02 + torch.linspace(0, top, A)).to(dtype)
+    drafts = (drafts.float() * 0.02 + torch.linspace(0, top, A)).to(dtype)
+    tokens[1:] = torch.tensor([A - 5, A // 2 + A // 3, A - 100, A - 1], dtype=I32)
+    for drawn in (True, False):
+        for step in (-1, 0, 1):
+            for t in range(len(u) - 1):
+                w, v = plain_weights(x[t], 1.0)[0], plain_weights(drafts[t], 1.0)[0]
+                tok = int(tokens[t + 1])
+                at = w[tok] * sum(v) / max(1, v[tok] * sum(w)) if drawn else w[tok] / sum(w)
+                edge = np.float32(min(at, 1 - 2.0 ** -24))
+                if step:
+                    edge = np.nextafter(edge, np.float32(step * 2))
+                u[t] = min(float(edge), 1 - 2.0 ** -24)
+            check_verify(api, x, tokens, offsets, u, du, drafts if drawn else None)
