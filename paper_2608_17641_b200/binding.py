@@ -1038,13 +1038,13 @@ def rlcs_block_tables(cached, added, free_pages, block_table, *, page_size, num_
 
 
 # ------------------------------------------------------------------ speculative rollouts and distillation
-_scratch_bytes: dict = {}              # workspace bytes by entry point and sizes
+_scratch_bytes: dict = {}              # workspace bytes by entry point, device and sizes
 
 
 def _scratch(query: str, sizes, workspace, device: int):
     """(pointer, bytes, tensor) of a call's workspace: the caller's, checked, or one of the call's own from torch's allocator."""
     if workspace is None:
-        key = (query, *sizes)
+        key = (query, device, *sizes)
         need = _scratch_bytes.get(key)
         if need is None:
             if len(_scratch_bytes) >= 4096:
