@@ -545,6 +545,9 @@ int rlcs_chunk_attention_bf16(const uint16_t* q, int64_t q_stride, const uint16_
  *   log_probs[t]: log-probability of out_tokens[t] under the target's whole softmax at T (within 1e-5 and 2^-22 of its size), -inf where that is -1
  * T <= 0 (or NaN): drafts stay while they are the target's most likely token (of equals the lowest index), which is also what is drawn;
  * log_probs at temperature 1.  Logits of -inf or NaN have no weight; a target row with no other stops the trajectory there with token -1.
+ * The softmaxes compared are those of whole rows.  Where drafts were drawn under top_k, top_p or min_p (rlcs_sample_actions), or the target is
+ * to be sampled under them, the rows given here have to be -inf where the filter leaves nothing; with rows as they came, what
+ * comes out is distributed as neither.  log_probs are then the filtered policy's.
  * A draft outside [0, A) does not stay.  uniforms [T] and draw_uniforms [B] in [0, 1).  Rows outside every trajectory are left as they were;
  * an empty trajectory has accepted 0.  workspace: at least rlcs_verify_drafts_workspace_bytes(T, B) bytes, 16-byte aligned, no initialisation.
  */

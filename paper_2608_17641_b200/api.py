@@ -277,7 +277,8 @@ def verify_drafts(logits, tokens, offsets, uniforms, draw_uniforms, *, draft_log
     given, not drawn).  One uniform in [0, 1) a row decides on its draft, one a trajectory draws the token that follows.  out_tokens[t] is
     the token after tokens[t]: kept drafts, the drawn token, then -1; log_probs are the target's, so they serve as old_log_probs
     of a policy loss.  temperature is a number or a tensor of one a trajectory; 0 keeps and takes the most likely token.  Rows
-    outside every trajectory are not written."""
+    outside every trajectory are not written.  Verification knows no top_k, top_p or min_p: where drafts were drawn with them (sample_actions), or
+    the target is to be, give both rows with -inf for what the filter leaves out, or the tokens follow neither distribution."""
     fn = _by_dtype(logits, _B.rlcs_verify_drafts, _B.rlcs_verify_drafts_bf16)
     return fn(logits, tokens, offsets, uniforms, draw_uniforms, draft_logits=draft_logits, temperature=temperature, stream=stream)
 

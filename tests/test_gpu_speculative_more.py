@@ -320,3 +320,22 @@ def test_verify_uniforms_at_the_border_of_rising_rows(api, A, top, dtype):
                     edge = np.nextafter(edge, np.float32(step * 2))
                 u[t] = min(float(edge), 1 - 2.0 ** -24)
             check_verify(api, x, tokens, offsets, u, du, drafts if drawn else None)
+
+
+def test_verify_follows_a_filtered_target(api):
+    """Drafts drawn with top_k, both policies' rows -inf outside it: tokens follow the filtered target, five standard deviations."""
+    B, A, K = 40000, 9, 3
+    g = torch.Generator(device="cuda").manual_seed(6)
+    rand = lambda n: torch.rand(n, device="cuda", generator=g)
+    p, q = torch.randn(A, device="cuda", generator=g) * 1.5, torch.randn(A, device="cuda", generator=g) * 1.5
+    p_kept, q_kept = (v.masked_fill(v < v.topk(K).values[-1], -math.inf) for v in (p, q))
+    tokens, _, kept = api.sample_actions(q.repeat(2 * B, 1), rand(2 * B), top_k=K)
+    assert (kept - torch.log_softmax(q_kept, 0)[tokens.long()]).abs().max() < 1e-5
+    out, lp, acc = api.verify_drafts(p_kept.repeat(2 * B, 1), tokens, torch.arange(0, 2 * B + 1, 2, device="cuda", dtype=I32), rand(2 * B), rand(B),
+                                     draft_logits=q_kept.repeat(2 * B, 1))
+    want = torch.softmax(p_kept, 0)
+    share = torch.bincount(out[::2].long(), minlength=A) / B
+    assert ((share - want).abs() <= 5 * (want * (1 - want) / B).sqrt()).all()
+    keep = float(torch.minimum(want, torch.softmax(q_kept, 0)).sum())
+    assert abs(float(acc.float().mean()) - keep) <= 5 * math.sqrt(keep * (1 - keep) / B)
+    assert (lp[::2] - torch.log(want)[out[::2].long()]).abs().max() < 1e-5
