@@ -108,7 +108,8 @@ __device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap* map, u
 
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Page (from the segment's first) of place `in` of that page's and the following tokens; in and page below 2^16.
+// Page (from the segment's first) of place `in` of that page's and the following tokens; exact while in * page < 2^32: pages hold up to 32768
+// tokens and segments up to 65536 and a tile, so that in stays below 98368.
 __device__ __forceinline__ int page_of(const AttnParams& P, int in) { return P.page_mul != 0 ? (int)__umulhi((uint32_t)in, P.page_mul) : in; }
 
 __device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
