@@ -685,8 +685,11 @@ int distill_run(const T* logits, int64_t ld, const int32_t* ids, const float* te
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     int st = RLCS_OK;
     if (const int64_t vecs = A / Vec<T>::N; vecs <= 512) {
-        // as few lanes a row as hold it: 154059 rows of 3 in bfloat16 8.9 us, 25 with eight lanes; 111610 of 28 12, 21 with eight, and 4000
-        // of 18 in fp32 3.1 with four or eight, 4.4 with two
+        // As few lanes a row as hold it, and as few vectors a lane (us, bfloat16; fp32 is alike): 100000 rows of 19 8.1 with two lanes, 10 with
+        // four; of 67 12 with four, 20 with eight; 50000 of 259 15 with eight and four vectors, 20 with eight vectors, 37 with a warp; of 515
+        // 34 with eight lanes, 41 with a warp; 20000 of 1027 21 with four vectors, 27 with eight; 10000 of 2051 20 with eight, 27 with sixteen.  The
+        // other way where entries are many (50000 of 515 with 64: 53 with eight lanes, 45 with a warp) or rows few (2000 of 403: 5.6, 3.9).  A warp
+        // wherever a row has more than 64 entries: 50000 of 163 with 128 63 us, 90 with eight lanes (of 67 with 90 it is 419 and 381)
         if (vecs <= 2 && K <= 64) st = launch_group<T, 2, 2>(P, s);
         else if (vecs <= 8 && K <= 64) st = launch_group<T, 4, 2>(P, s);
         else if (vecs <= 32 && K <= 64) st = launch_group<T, 8, 4>(P, s);
@@ -694,7 +697,9 @@ int distill_run(const T* logits, int64_t ld, const int32_t* ids, const float* te
         else if (vecs <= 128) st = launch_group<T, 32, 4>(P, s);
         else if (vecs <= 256) st = launch_group<T, 32, 8>(P, s);
         else st = launch_group<T, 32, 16>(P, s);
-    } else if (vecs <= 2048 && R >= 2 * rlcs_device::limits().sms) {      // a block a row (29245 rows of 11 KB 169 us, 320 from shared memory); fewer rows are cut over clusters
+    } else if (vecs <= 2048 && R >= 2 * rlcs_device::limits().sms) {
+        // a block a row: 29245 rows of 11 KB 169 us, 320 from shared memory; 3000 of 8003 in bfloat16 26 (34 with eight vectors a thread, 44 from
+        // shared memory), 2000 of 16003 30 (38).  A warp a row up to 512 vectors: 5000 of 4099 21, 35 with a block.  Fewer rows are cut over clusters
         st = vecs <= 1024 ? launch_group<T, 256, 4>(P, s) : launch_group<T, 256, 8>(P, s);
     } else {
         // blocks a row: parts of at most 64 KB; more while the GPU has room for two a multiprocessor and a part keeps 8 KB
