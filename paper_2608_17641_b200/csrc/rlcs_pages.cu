@@ -7,8 +7,8 @@
 //
 // What a page is shared by needs no counts: it is free when no table names it.
 //
-// Measured: 2048 rows forked and about 750 pages of 128 KB copied in both caches 78 us, of which the copies 65 (0.92 of the copy bandwidth),
-// tables and numbers of all rows 12; 8 rows 8.5 us with their copies, a chain of a block's lookups; free pages among 9192 of 128 rows 6.8 us (one block), among 2.2 million of 4096 rows 22 us: 13 for 1.4 million
+// Measured: 2048 rows forked and about 750 pages of 128 KB copied in both caches 77 us, of which the copies 65 (0.92 of the copy bandwidth),
+// tables and numbers of all rows 12; 8 rows 8.3 us with their copies, a chain of a block's lookups; free pages among 9192 of 128 rows 6.8 us (one block), among 2.2 million of 4096 rows 22 us: 13 for 1.4 million
 // marks in L2 (plain stores of bytes took 10 more), 8 for the list, whose counts every block makes itself instead of another launch.
 #include <cooperative_groups.h>
 
