@@ -38,7 +38,7 @@ struct ForkParams {
     int32_t* from;
     int32_t* to;
     int32_t* used;
-    int32_t* keys;             // [slots] page numbers, -1: none                         } of large calls, in the workspace
+    int32_t* keys;             // [slots] page numbers, -1: none                         } of large calls
     uint32_t* owner;           // [slots] first new row that ends there + 1, 0: nobody   }
     int32_t* number;           // [N] slot, then place in the free list; -1: none        }
     int32_t B, N, width, free_count, page;
@@ -151,8 +151,10 @@ __device__ __forceinline__ void give_page(const ForkParams& P, int i, int number
 
 constexpr int kWide = 1024;                  // threads where a block goes through all rows
 constexpr int kMostWays = 8;                 // blocks that share the whole pages
+constexpr int64_t kMostCells = 98304;        // entries of either table up to which they do (1024 rows of 64 15 us; 4096 of 64 36, and
+                                             // 18 in launches of their own)
 
-// Up to kFused rows: the table of pages in the shared memory of each block of one cluster.  All blocks enter all rows; each looks a share of
+// Up to kFused rows and kMostCells entries: the table of pages in the shared memory of each block of one cluster.  All blocks enter all rows; each looks a share of
 // the old tables' whole pages up, and tells the others what it finds (seldom anything); the numbers are again every block's own.
 __global__ void __launch_bounds__(kWide) fork_kernel(const __grid_constant__ ForkParams P) {
     extern __shared__ int32_t held[];
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(kThreads) fork_gather_kernel(const __grid_cons
     gather_tables(P, (int64_t)blockIdx.x * kThreads + threadIdx.x, (int64_t)gridDim.x * kThreads);
 }
 
-// The same for more rows, the table of pages in the workspace.
+// The same for larger tables, the table of pages in the workspace or in place of outputs that are written later.
 __global__ void __launch_bounds__(kThreads) fork_enter_kernel(const __grid_constant__ ForkParams P) {
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < P.N; i += gridDim.x * kThreads) {
         const int last = old_row(P, i).last;
@@ -485,7 +487,8 @@ int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, cons
     for (int64_t n = slots; n > 1; n /= 2) --P.shift;
     const int64_t cells = N * width, sms = rlcs_device::limits().sms;
     auto blocks_for = [&](int64_t items) { const int64_t n = (items + kThreads - 1) / kThreads; return (unsigned)(n < 1 ? 1 : n < 8 * sms ? n : 8 * sms); };
-    if (need == 0) {
+    const bool own_launches = need > 0 || (width >= 8 && (B > N ? B : N) * width > kMostCells);
+    if (!own_launches) {
         static bool granted[64];
         int dev = 0;
         if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RLCS_ERR_CUDA;
@@ -494,10 +497,9 @@ int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, cons
             if (cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return RLCS_ERR_CUDA;
             granted[dev] = true;
         }
-        // one block while every thread has up to four entries, else eight; tables of more than two entries a thread of those are written by
+        // one block while every thread has an entry at most, else eight; tables of more than two entries a thread of those are written by
         // a launch of their own
-        int ways = 1;
-        if (B * width > 4 * kWide || cells > 4 * kWide) ways = kMostWays;
+        const int ways = B * width > kWide || cells > kWide ? kMostWays : 1;
         P.fill = cells <= 2 * kMostWays * kWide;
         if (!P.fill) fork_gather_kernel<<<blocks_for(cells), kThreads, 0, s>>>(P);
         cudaLaunchConfig_t cfg = {};
@@ -513,15 +515,16 @@ int rlcs_fork_block_tables(const int32_t* block_table, const int32_t* lens, cons
         cfg.numAttrs = 1;
         if (cudaLaunchKernelEx(&cfg, fork_kernel, P) != cudaSuccess) return RLCS_ERR_CUDA;
     } else {
-        P.owner = reinterpret_cast<uint32_t*>(keys + slots);
-        P.number = keys + 2 * slots;
-        if (cudaMemsetAsync(keys, 0xff, (size_t)slots * 2 * sizeof(int32_t), s) != cudaSuccess) return RLCS_ERR_CUDA;
+        // without a workspace the table of pages lies where the new table is written afterwards (2 * slots < 8 * N), and the numbers where the
+        // copies are: each is read before it is overwritten
+        if (need == 0) P.keys = new_table;
+        P.owner = reinterpret_cast<uint32_t*>(P.keys + slots);
+        P.number = need == 0 ? copy_to : P.keys + 2 * slots;
+        if (cudaMemsetAsync(P.keys, 0xff, (size_t)slots * 2 * sizeof(int32_t), s) != cudaSuccess) return RLCS_ERR_CUDA;
         fork_enter_kernel<<<blocks_for(N), kThreads, 0, s>>>(P);
-        if (cells > 0) {
-            fork_whole_kernel<<<blocks_for(cells), kThreads, 0, s>>>(P);
-            fork_gather_kernel<<<blocks_for(cells), kThreads, 0, s>>>(P);
-        }
+        if (cells > 0) fork_whole_kernel<<<blocks_for(cells), kThreads, 0, s>>>(P);
         fork_numbers_kernel<<<1, kWide, 0, s>>>(P);
+        if (cells > 0) fork_gather_kernel<<<blocks_for(cells), kThreads, 0, s>>>(P);
         fork_give_kernel<<<blocks_for(N), kThreads, 0, s>>>(P);
     }
     return cudaGetLastError() == cudaSuccess ? RLCS_OK : RLCS_ERR_CUDA;

@@ -64,7 +64,8 @@ def plain_fork_by_page(table, lens, sources, free, page):
     return rows, come, go, used
 
 
-@pytest.mark.parametrize("B,N,width", [(1, 3, 4), (5, 9, 3), (40, 40, 7), (300, 200, 20), (1000, 1500, 33), (4096, 4096, 9), (700, 5000, 6), (6000, 6000, 5), (5000, 3, 4)])
+@pytest.mark.parametrize("B,N,width", [(1, 3, 4), (5, 9, 3), (40, 40, 7), (300, 200, 20), (1000, 1500, 33), (4096, 4096, 9), (700, 5000, 6), (6000, 6000, 5), (5000, 3, 4),
+                                       (2048, 3001, 40), (4096, 4096, 26), (3, 13, 9000), (4000, 5, 26)])
 def test_fork_goes_by_the_page_that_is_shared(api, B, N, width):
     """Tables whose rows share pages with one another at any place, as whole pages, as part-filled ones and as both."""
     page = 16
